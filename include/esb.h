@@ -46,13 +46,20 @@ extern "C" {
 #define ESB_E_INVALID (-1)     /* bad n/k_sig, sizes, NULL pointer, layout, descriptor */
 #define ESB_E_OVERFLOW (-3)    /* reduction length * max|mA| * max|mB| > 2^31 - 1 */
 #define ESB_E_UNSUPPORTED (-4) /* decoded integers exceed the split int8 range (|m| > 32639),
-                                  or a format / length outside the packed 4-bit storage */
+                                  a format / length outside the packed 4-bit storage, or a
+                                  type / size that a decoder operator does not take */
 #define ESB_E_HIP (-5)         /* HIP launch / runtime failure, see esb_last_hip_error() */
 #define ESB_E_WORKSPACE (-6)   /* workspace NULL or smaller than its *_workspace_size() */
 #define ESB_E_SCRATCH (-7)     /* input larger than the static scratch of a *_noalloc call */
 
 #define ESB_B_NK 0 /* B stored N x K, row-major (K contiguous) */
 #define ESB_B_KN 1 /* B stored K x N, row-major (N contiguous) */
+
+/* Element types of float tensors: IEEE binary32, bfloat16, IEEE binary16, OCP E4M3 bytes. */
+#define ESB_F32 0
+#define ESB_BF16 1
+#define ESB_F16 2
+#define ESB_E4M3 3
 
 /* Library version as MAJOR*10000 + MINOR*100 + PATCH. */
 int esb_version(void);
@@ -487,6 +494,89 @@ int esb_conv2d_relu_maxpool(const esb_conv_desc* d, const uint8_t* x, int nX, in
                             const float* alphaW, const esb_post* post, int pool_window,
                             int pool_stride, int pool_pad, float* y, void* workspace,
                             size_t ws_bytes, void* stream);
+
+/*
+ * Decoder operators: the products of a language model's layers over 4-bit weights with a scale
+ * per group, and the row operators between them, which hand over 8-bit activations.  Matrices
+ * are row-major with a row pitch in elements and may start at any element's alignment (weights
+ * in the packed layout: 16 bytes); `type` is ESB_F32, ESB_BF16 or ESB_F16 unless said
+ * otherwise.  Sums, statistics and scales are held in fp32 or fp64 and every output is rounded
+ * once, to nearest even.
+ *
+ * 8-bit rows: OCP E4M3 bytes with one fp32 scale per row,
+ *   s = max(fl32(max_i |y_i| / 448), 2^-126),   byte_i = E4M3(y_i * fl32(1 / s)),
+ * so that a row stands for s * byte_i; a row of zeros has s = 2^-126.  A NaN or an infinity
+ * among the y_i makes the scale and every byte of that row NaN.
+ *
+ * esb_rmsnorm: per row of d elements, z = x + residual (z = x when residual is NULL) in fp32,
+ *   y = z * rstd * w,   rstd = 1 / sqrt(mean(z^2) + eps)   (the sum of squares in fp64);
+ *   w        device, d fp32, or NULL (ones);  eps: positive and finite;
+ *   sum_out  z in `type`, or NULL; may be the buffer of x or of residual (same pitch);
+ *   y        y in `type`, or NULL; may be the buffer of x or of residual (same pitch);
+ *   y8, scale  the 8-bit row (pitch ld8 bytes) and its scales (device, `rows` fp32), or NULL;
+ *            at least one of y, y8.
+ * esb_swiglu: y = gate / (1 + exp(-gate)) * up, the same two outputs; y may be the buffer of
+ *   gate or of up (same pitch).  gate and up are usually the two halves of one product's rows.
+ * Both: 0 <= d <= 65536 (more: ESB_E_UNSUPPORTED); rows == 0 or d == 0 enqueues nothing.
+ */
+int esb_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int type,
+                int64_t rows, int64_t d, const float* w, float eps, void* sum_out, int64_t lds,
+                void* y, int64_t ldy, uint8_t* y8, int64_t ld8, float* scale, void* stream);
+int esb_swiglu(const void* gate, int64_t ldg, const void* up, int64_t ldu, int type,
+               int64_t rows, int64_t d, void* y, int64_t ldy, uint8_t* y8, int64_t ld8,
+               float* scale, void* stream);
+
+/*
+ * 4-bit weights with a scale per group of 32, 64 or 128 consecutive elements of a row (the last
+ * group of a row may be cut off by K): an N x K matrix W is held as
+ *   W[n][k] ~ alpha[n][k / group] * q[n][k],
+ * q the values of ESB(4,1) (OCP E2M1: 0, .5, 1, 1.5, 2, 3, 4, 6 and signs), alpha in bf16.
+ * The packed form (esb_w4_size bytes, 16-byte aligned, 0 for invalid arguments) is what the
+ * matrix cores read and is not position-independent of (N, K, group), which every call gets:
+ *   tiles of 16 rows x 128 columns, 1 KB each, tile (n / 16, k / 128) at index
+ *   (n / 16) * ceil(K / 128) + k / 128.  Within a tile, row r = n % 16, the E2M1 nibble of
+ *   column k is nibble k % 8 (lowest first) of the 32-bit word
+ *   4 * (16 * ((k / 8) % 4) + r) + (k / 32) % 4;  then, after all tiles, the bf16 scales,
+ *   alpha[n][g] at index ((n / 16) * ceil(K / 128) * (128 / group) + g) * 16 + r.
+ *   Rows and columns past N and K hold zeros.
+ *
+ * esb_w4_quantize: codes and scales of W (device, `type`).  Per group, over the candidates
+ *     alpha_j = bf16(max(fl32(fl32(max|w| * factors[j]) / 6), 2^-126)),   0 <= j < candidates,
+ *   the nearest values q_j of w / alpha_j (ties to the larger magnitude, zero with sign 0); the
+ *   candidate with the least sum of (w - alpha_j q_j)^2 is taken, the lowest index on ties: the
+ *   aligner's objective, eq. (9) and (13), on the group.  factors: device, `candidates` (at most
+ *   64) fp32, or NULL with candidates == 1 for the single factor 1.  Factors that are not
+ *   positive and finite, and candidates that overflow, are passed over; if none is left, or a
+ *   weight of the group is NaN or infinite, the group's scale is NaN and its codes 0.
+ * esb_w4_pack: the packed form of given ESB(4,1) codes (one per byte, as esb_project writes
+ *   them; device, N x K) and scales (device, bf16, N x ceil(K / group)).
+ * esb_w4_unpack: the unscaled values as E4M3 bytes (exact; N x K) and / or the scales (bf16,
+ *   N x ceil(K / group)); either may be NULL.
+ * Errors: ESB_E_WORKSPACE when w4_bytes is less than esb_w4_size; ESB_E_UNSUPPORTED above 2^26
+ * rows or 2^25 tiles.  N == 0 or K == 0 enqueues nothing.
+ */
+size_t esb_w4_size(int N, int K, int group);
+int esb_w4_quantize(const void* w, int64_t ldw, int type, int N, int K, int group,
+                    const float* factors, int candidates, void* w4, size_t w4_bytes,
+                    void* stream);
+int esb_w4_pack(const uint8_t* codes, int64_t ldc, const void* alpha, int64_t lda, int N, int K,
+                int group, void* w4, size_t w4_bytes, void* stream);
+int esb_w4_unpack(const void* w4, int N, int K, int group, uint8_t* values, int64_t ldv,
+                  void* alpha, int64_t lda, void* stream);
+
+/*
+ * Products with packed 4-bit weights, from one row of activations (a token) to many (a prompt):
+ *   y[m][n] = s_m * sum_g alpha[n][g] * (sum over k of group g of x[m][k] q[n][k]),
+ *   x       device, M x K: ESB_BF16, ESB_F16, or ESB_E4M3 bytes (ESB_F32: ESB_E_UNSUPPORTED);
+ *   x_scale device, M fp32 (s_m), or NULL (ones);
+ *   w4      device, the packed form of N x K weights with this group;
+ *   y       device, M x N, y_type ESB_F32, ESB_BF16 or ESB_F16.
+ * Products are exact in the matrix cores' inputs, sums fp32 in an order fixed by the arguments
+ * (the same call gives the same bits).  K == 0 writes zeros; M == 0 or N == 0 enqueues nothing.
+ */
+int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int x_type,
+                const float* x_scale, const void* w4, void* y, int64_t ldy, int y_type,
+                void* stream);
 
 #ifdef __cplusplus
 }

@@ -111,7 +111,7 @@ const char* esb_strerror(int status) {
         case ESB_OK: return "ok";
         case ESB_E_INVALID: return "invalid argument";
         case ESB_E_OVERFLOW: return "int32 accumulator bound exceeded";
-        case ESB_E_UNSUPPORTED: return "decoded integers exceed the split int8 range";
+        case ESB_E_UNSUPPORTED: return "format, type or size outside what the kernels support";
         case ESB_E_HIP: return "HIP runtime error";
         case ESB_E_WORKSPACE: return "workspace missing or too small";
         case ESB_E_SCRATCH: return "input needs more scratch than the static device buffer holds";
@@ -708,6 +708,112 @@ int esb_dda_normal(int n, int k_sig, const float* grid, int G, float* alpha_out,
     if (!valid_fmt(n, k_sig) || G < 1 || !grid || !alpha_out || !D_out) return ESB_E_INVALID;
     return hip_status(launch_dda_normal(make_fmt(n, k_sig), grid, G, alpha_out, D_out,
                                         dD_out, (hipStream_t)stream));
+}
+
+// ----------------------------------------------------------- decoder operators
+static bool float_type(int t) { return t == ESB_F32 || t == ESB_BF16 || t == ESB_F16; }
+static bool aligned_for(const void* p, int type) {
+    return (uintptr_t)p % (type == ESB_F32 ? 4 : type == ESB_E4M3 ? 1 : 2) == 0;
+}
+
+// The checks that both row operators share; ESB_OK with rows == 0 or d == 0 means nothing to do.
+static int rows_check(const RowsParams& p, int type, bool need_b) {
+    if (!float_type(type) || p.rows < 0 || p.d < 0) return ESB_E_INVALID;
+    if (p.lda < p.d || (p.b && p.ldb < p.d) || (p.sum && p.lds < p.d) || (p.y && p.ldy < p.d) ||
+        (p.y8 && p.ld8 < p.d))
+        return ESB_E_INVALID;
+    if (p.rows == 0 || p.d == 0) return ESB_OK;
+    if (!p.y && !p.y8) return ESB_E_INVALID;
+    if (!p.a || (need_b && !p.b) || (p.y8 && !p.scale)) return ESB_E_INVALID;
+    if (!aligned_for(p.a, type) || !aligned_for(p.b, type) || !aligned_for(p.sum, type) ||
+        !aligned_for(p.y, type) || (uintptr_t)p.w % 4 || (p.y8 && (uintptr_t)p.scale % 4))
+        return ESB_E_INVALID;
+    return ESB_OK;
+}
+
+int esb_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int type, int64_t rows,
+                int64_t d, const float* w, float eps, void* sum_out, int64_t lds, void* y, int64_t ldy,
+                uint8_t* y8, int64_t ld8, float* scale, void* stream) {
+    if (!(eps > 0.0f) || eps == INFINITY || d < 0) return ESB_E_INVALID;
+    if (d > kRowsMax) return ESB_E_UNSUPPORTED;
+    const RowsParams p = {x, residual, ldx, ldr, rows, (int)d, w, eps, sum_out, lds, y, ldy, y8, ld8, scale};
+    const int st = rows_check(p, type, false);
+    if (st || rows == 0 || d == 0) return st;
+    return hip_status(launch_rows(kRowsNorm, type, p, (hipStream_t)stream));
+}
+
+int esb_swiglu(const void* gate, int64_t ldg, const void* up, int64_t ldu, int type, int64_t rows,
+               int64_t d, void* y, int64_t ldy, uint8_t* y8, int64_t ld8, float* scale, void* stream) {
+    if (d < 0) return ESB_E_INVALID;
+    if (d > kRowsMax) return ESB_E_UNSUPPORTED;
+    const RowsParams p = {gate, up, ldg, ldu, rows, (int)d, nullptr, 0.0f, nullptr, 0, y, ldy, y8, ld8, scale};
+    const int st = rows_check(p, type, true);
+    if (st || rows == 0 || d == 0) return st;
+    return hip_status(launch_rows(kRowsGated, type, p, (hipStream_t)stream));
+}
+
+// Launches count tiles in 32 bits: up to 2^22 row tiles and 2^25 tiles of 1 KB.
+static int w4_check(int N, int K, int group) {
+    if (N < 0 || K < 0 || (group != 32 && group != 64 && group != 128)) return ESB_E_INVALID;
+    const int64_t tiles = ((int64_t)N + 15) / 16, chunks = ((int64_t)K + 127) / 128;
+    if (tiles > (1 << 22) || tiles * chunks > (1 << 25)) return ESB_E_UNSUPPORTED;
+    return ESB_OK;
+}
+
+size_t esb_w4_size(int N, int K, int group) {
+    return w4_check(N, K, group) ? 0 : (size_t)w4_layout(N, K, group).bytes;
+}
+
+int esb_w4_quantize(const void* w, int64_t ldw, int type, int N, int K, int group, const float* factors,
+                    int candidates, void* w4, size_t w4_bytes, void* stream) {
+    if (!float_type(type)) return ESB_E_INVALID;
+    const int st = w4_check(N, K, group);
+    if (st) return st;
+    if (ldw < K || candidates < 1 || candidates > 64 || (!factors && candidates != 1)) return ESB_E_INVALID;
+    if (N == 0 || K == 0) return ESB_OK;
+    const W4Layout L = w4_layout(N, K, group);
+    if (!w || !aligned_for(w, type) || (uintptr_t)factors % 4 || !w4 || (uintptr_t)w4 % 16) return ESB_E_INVALID;
+    if (w4_bytes < (size_t)L.bytes) return ESB_E_WORKSPACE;
+    return hip_status(launch_w4_quantize(L, type, w, ldw, factors, candidates, w4, (hipStream_t)stream));
+}
+
+int esb_w4_pack(const uint8_t* codes, int64_t ldc, const void* alpha, int64_t lda, int N, int K, int group,
+                void* w4, size_t w4_bytes, void* stream) {
+    const int st = w4_check(N, K, group);
+    if (st) return st;
+    const int64_t groups = ((int64_t)K + group - 1) / group;
+    if (ldc < K || lda < groups) return ESB_E_INVALID;
+    if (N == 0 || K == 0) return ESB_OK;
+    const W4Layout L = w4_layout(N, K, group);
+    if (!codes || !alpha || (uintptr_t)alpha % 2 || !w4 || (uintptr_t)w4 % 16) return ESB_E_INVALID;
+    if (w4_bytes < (size_t)L.bytes) return ESB_E_WORKSPACE;
+    return hip_status(launch_w4_pack(L, codes, ldc, alpha, lda, w4, (hipStream_t)stream));
+}
+
+int esb_w4_unpack(const void* w4, int N, int K, int group, uint8_t* values, int64_t ldv, void* alpha,
+                  int64_t lda, void* stream) {
+    const int st = w4_check(N, K, group);
+    if (st) return st;
+    const int64_t groups = ((int64_t)K + group - 1) / group;
+    if ((!values && !alpha) || (values && ldv < K) || (alpha && lda < groups)) return ESB_E_INVALID;
+    if (N == 0 || K == 0) return ESB_OK;
+    if (!w4 || (uintptr_t)w4 % 16 || (uintptr_t)alpha % 2) return ESB_E_INVALID;
+    return hip_status(launch_w4_unpack(w4_layout(N, K, group), w4, values, ldv, alpha, lda, (hipStream_t)stream));
+}
+
+int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int x_type, const float* x_scale,
+                const void* w4, void* y, int64_t ldy, int y_type, void* stream) {
+    if (x_type == ESB_F32) return ESB_E_UNSUPPORTED;
+    if ((!float_type(x_type) && x_type != ESB_E4M3) || !float_type(y_type) || M < 0) return ESB_E_INVALID;
+    const int st = w4_check(N, K, group);
+    if (st) return st;
+    if (ldx < K || ldy < N) return ESB_E_INVALID;
+    if (M == 0 || N == 0) return ESB_OK;
+    if (!y || !aligned_for(y, y_type)) return ESB_E_INVALID;
+    if (K > 0 && (!x || !aligned_for(x, x_type) || (uintptr_t)x_scale % 4 || !w4 || (uintptr_t)w4 % 16))
+        return ESB_E_INVALID;
+    const W4GemmParams p = {w4_layout(N, K, group), M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type};
+    return hip_status(launch_w4_gemm(p, x_type, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -563,4 +563,57 @@ hipError_t launch_dwconv(const ConvGeom& g, const uint8_t* x, const Fmt& fx, con
                          const uint8_t* w, const Fmt& fw, const float* alphaW, int32_t* acc,
                          float* y, hipStream_t s, const Post* post = nullptr);
 
+// ----------------------------------------------------------- decoder operators
+// Element types of float tensors, as the ABI numbers them.
+constexpr int kF32 = 0, kBF16 = 1, kF16 = 2, kE4M3 = 3;
+
+// Row operators (rows.hip): the root-mean-square norm of a + b (b may be NULL), the gated
+// activation of gate a and up b.  d <= kRowsMax; pitches in elements.
+constexpr int kRowsNorm = 0, kRowsGated = 1;
+constexpr int kRowsMax = 65536;
+struct RowsParams {
+    const void* a;
+    const void* b;
+    int64_t lda, ldb, rows;
+    int d;
+    const float* w;    // norm: d weights, or NULL (ones)
+    float eps;
+    void* sum;         // norm: a + b, or NULL
+    int64_t lds;
+    void* y;           // or NULL
+    int64_t ldy;
+    uint8_t* y8;       // E4M3 bytes, or NULL
+    int64_t ld8;
+    float* scale;      // one per row, with y8
+};
+hipError_t launch_rows(int op, int type, const RowsParams& p, hipStream_t s);
+
+// 4-bit weights (w4.hip): tiles of 16 rows x 128 columns, then the scales.
+struct W4Layout {
+    int N, K, group;
+    int tiles, chunks, groups;   // row tiles, column chunks, groups of a row (whole chunks)
+    int64_t scale_offset, bytes;
+};
+W4Layout w4_layout(int N, int K, int group);
+hipError_t launch_w4_quantize(const W4Layout& L, int type, const void* w, int64_t ldw,
+                              const float* factors, int nf, void* out, hipStream_t s);
+hipError_t launch_w4_pack(const W4Layout& L, const uint8_t* codes, int64_t ldc, const void* alpha,
+                          int64_t lda, void* out, hipStream_t s);
+hipError_t launch_w4_unpack(const W4Layout& L, const void* in, uint8_t* values, int64_t ldv,
+                            void* alpha, int64_t lda, hipStream_t s);
+
+// Products with them (w4_gemm.hip).
+struct W4GemmParams {
+    W4Layout L;
+    int64_t M;
+    const void* x;
+    int64_t ldx;
+    const float* x_scale;   // one per row of x, or NULL
+    const uint8_t* w4;
+    void* y;
+    int64_t ldy;
+    int y_type;
+};
+hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s);
+
 }  // namespace esb

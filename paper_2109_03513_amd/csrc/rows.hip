@@ -1,0 +1,141 @@
+// Row operators between a decoder's products, each one pass over its rows with 8-bit outputs:
+//
+//  * the root-mean-square norm with the residual's addition: z = x + r, y = z rstd w,
+//    rstd = 1 / sqrt(mean z^2 + eps);
+//  * the gated activation h = gate / (1 + exp(-gate)) * up.
+//
+// Outputs are the rows in the inputs' type and / or OCP E4M3 bytes under one scale per row,
+// s = max(max|y| / 448, 2^-126), byte = y (1/s) rounded to nearest even: the operand of
+// esb_w4_gemm.  A row stays in registers between its two reductions (the sum of squares, the
+// maximum), so HBM sees each input and output once.
+//
+// The sum of squares is held in fp64: squares of fp32 values up to the largest do not overflow,
+// and rstd is the correctly rounded fp32 value up to the last bit.  Everything else is fp32,
+// rounded once to the output's type.
+#include "float_rows.h"
+
+namespace esb {
+
+namespace {
+
+constexpr float kE4M3Max = 448.0f;
+constexpr float kTiny = 0x1p-126f;
+
+template <int OP, typename T, int TPR, int NV>
+__global__ __launch_bounds__(TPR) void k_rows(RowsParams p) {
+    typedef typename Vec8<T>::type V;
+    __shared__ double red[TPR / 64];
+    __shared__ uint32_t redm[TPR / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x;
+    const int d = p.d;
+    const T* a = (const T*)p.a + row * p.lda;
+    const T* b = p.b ? (const T*)p.b + row * p.ldb : nullptr;
+
+    f32x8 v[NV];
+    double ss = 0.0;
+#pragma unroll
+    for (int u = 0; u < NV; u++) {
+        const int e = 8 * (u * TPR + tid);
+        v[u] = f32x8{};
+        if (e >= d) continue;
+        const int n = d - e;
+        f32x8 x = __builtin_convertvector(load8(a + e, n), f32x8);
+        if (OP == kRowsNorm) {
+            if (b) x += __builtin_convertvector(load8(b + e, n), f32x8);
+            if (p.sum) store8((T*)p.sum + row * p.lds + e, __builtin_convertvector(x, V), n);
+#pragma unroll
+            for (int i = 0; i < 8; i++) ss += (double)x[i] * (double)x[i];
+        } else {
+            const f32x8 up = __builtin_convertvector(load8(b + e, n), f32x8);
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = x[i] / (1.0f + expf(-x[i])) * up[i];
+        }
+        v[u] = x;
+    }
+    if (OP == kRowsNorm) {
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) ss += __shfl_xor(ss, o);
+        if (lane == 0) red[wave] = ss;
+        __syncthreads();
+        ss = 0.0;
+#pragma unroll
+        for (int i = 0; i < TPR / 64; i++) ss += red[i];
+        const float rstd = (float)(1.0 / sqrt(ss / (double)d + (double)p.eps));
+#pragma unroll
+        for (int u = 0; u < NV; u++) {
+            const int e = 8 * (u * TPR + tid);
+            if (e >= d) continue;
+            const f32x8 w = p.w ? load8(p.w + e, d - e) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+            v[u] = v[u] * rstd * w;
+        }
+    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int u = 0; u < NV; u++) {
+        const int e = 8 * (u * TPR + tid);
+        if (e >= d) continue;
+        if (p.y) store8((T*)p.y + row * p.ldy + e, __builtin_convertvector(v[u], V), d - e);
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[u][i]) & 0x7fffffffu);
+    }
+    if (!p.y8) return;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+    if (lane == 0) redm[wave] = m;
+    __syncthreads();
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < TPR / 64; i++) m = max(m, redm[i]);
+    // a NaN or an infinity in the row: no scale fits it
+    const float s = m < 0x7f800000u ? fmaxf(__uint_as_float(m) / kE4M3Max, kTiny) : __builtin_nanf("");
+    const float inv = 1.0f / s;
+    if (tid == 0) p.scale[row] = s;
+#pragma unroll
+    for (int u = 0; u < NV; u++) {
+        const int e = 8 * (u * TPR + tid);
+        if (e >= d) continue;
+        const uint2 q = to_e4m3(v[u] * inv);
+        uint8_t* o = p.y8 + row * p.ld8 + e;
+        if (d - e >= 8) {
+            ((Loose<uint2, uint8_t>*)o)->v = q;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (i < d - e) o[i] = (uint8_t)((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
+        }
+    }
+}
+
+template <int OP, typename T>
+hipError_t launch_t(const RowsParams& p, hipStream_t s) {
+    const int64_t most = 1 << 21;      // workgroups of one launch
+    for (int64_t r = 0; r < p.rows; r += most) {
+        RowsParams q = p;
+        q.rows = p.rows - r < most ? p.rows - r : most;
+        q.a = (const T*)p.a + r * p.lda;
+        if (p.b) q.b = (const T*)p.b + r * p.ldb;
+        if (p.sum) q.sum = (T*)p.sum + r * p.lds;
+        if (p.y) q.y = (T*)p.y + r * p.ldy;
+        if (p.y8) q.y8 = p.y8 + r * p.ld8, q.scale = p.scale + r;
+        k_rows<OP, T, 1024, 8><<<(unsigned)q.rows, 1024, 0, s>>>(q);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_rows(int op, int type, const RowsParams& p, hipStream_t s) {
+    if (op == kRowsNorm) {
+        if (type == kF32) return launch_t<kRowsNorm, float>(p, s);
+        if (type == kBF16) return launch_t<kRowsNorm, __bf16>(p, s);
+        return launch_t<kRowsNorm, _Float16>(p, s);
+    }
+    if (type == kF32) return launch_t<kRowsGated, float>(p, s);
+    if (type == kBF16) return launch_t<kRowsGated, __bf16>(p, s);
+    return launch_t<kRowsGated, _Float16>(p, s);
+}
+
+}  // namespace esb

@@ -1,0 +1,230 @@
+// 4-bit weights with a scale per group: quantization, packing and unpacking.
+//
+// A row's reduction is cut into groups of G = 32, 64 or 128 weights, each with its own bf16 scale.
+// The codes are ESB(4,1), which is OCP E2M1: value q in {0, .5, 1, 1.5, 2, 3, 4, 6} and a sign.
+// The scale of a group is the aligner's search (eq. (9), (13)) on that group: candidates
+//   alpha_j = bf16(max(fl32(max|w| f_j) / 6, 2^-126)),
+// the one of the least sum of (w - alpha_j q)^2, the lowest index on ties.  A bf16 scale makes the
+// cell bounds mid * alpha exact in fp32 (3 + 8 bits), so codes are the exact nearest values of
+// w / alpha, ties to the larger magnitude, with no division.
+//
+// Layout (w4_layout): what one wave of the products reads per step is contiguous.  Tiles of 16
+// rows x 128 columns, 1 KB each, [row tile][column chunk]; lane 16j + r of a tile owns row r and
+// 16 bytes: dword t holds columns 32t + 8j .. + 7, lowest nibble first.  Dword t of the 64 lanes is
+// then the operand of one 16x16x32 MFMA over the columns 32t .. 32t+31 (a whole group of 32), and
+// the 16 bytes are the operand of one 16x16x128 MFMA.  The scales follow, [row tile][group][16
+// rows].  Rows and columns beyond N and K hold codes and scales of 0.
+#include "float_rows.h"
+
+namespace esb {
+
+namespace {
+
+constexpr float kTiny = 0x1p-126f;
+
+__device__ __forceinline__ float bf16_round(float x) { return (float)(__bf16)x; }
+
+// Number of cell bounds of alpha at or below |w|: the E2M1 code of the magnitude.
+__device__ __forceinline__ int magnitude_code(float aw, float alpha) {
+    return (aw >= 0.25f * alpha) + (aw >= 0.75f * alpha) + (aw >= 1.25f * alpha) +
+           (aw >= 1.75f * alpha) + (aw >= 2.5f * alpha) + (aw >= 3.5f * alpha) + (aw >= 5.0f * alpha);
+}
+__device__ __forceinline__ float code_value(int c) {
+    return c < 2 ? 0.5f * (float)c : __uint_as_float(((uint32_t)(126 + (c >> 1)) << 23) | ((uint32_t)(c & 1) << 22));
+}
+
+// A wave per tile of 16 x 128 weights; lane 16j + r holds 32 weights of row r.
+template <typename T, int G>
+__global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __restrict__ w, int64_t ldw,
+                                                     const float* __restrict__ factors, int nf,
+                                                     uint8_t* __restrict__ out) {
+    const int lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
+    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (tile >= (int64_t)L.tiles * L.chunks) return;
+    const int kc = (int)(tile % L.chunks), nt = (int)(tile / L.chunks);
+    const int n = 16 * nt + r;
+    constexpr int TG = G / 32;      // dwords of a lane in one group
+
+    float v[4][8];
+#pragma unroll
+    for (int t = 0; t < 4; t++) {
+        const int k = 128 * kc + 32 * t + 8 * j;
+        const int left = n < L.N ? L.K - k : 0;
+        const f32x8 x = __builtin_convertvector(load8(w + (int64_t)n * ldw + k, left), f32x8);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[t][i] = x[i];
+    }
+    uint32_t packed[4];
+    __bf16* scales = (__bf16*)(out + L.scale_offset);
+#pragma unroll
+    for (int g = 0; g < 4 / TG; g++) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int t = g * TG; t < (g + 1) * TG; t++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[t][i]) & 0x7fffffffu);
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+        const float top = __uint_as_float(m);
+        float alpha = __builtin_nanf("");
+        double least = __builtin_inf();
+        for (int c = 0; c < nf; c++) {
+            const float f = factors ? factors[c] : 1.0f;
+            const float a = bf16_round(fmaxf(top * f / 6.0f, kTiny));
+            if (!(f > 0.0f) || !(top < __builtin_inff()) || !(a < __builtin_inff())) continue;
+            double err = 0.0;
+#pragma unroll
+            for (int t = g * TG; t < (g + 1) * TG; t++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float aw = fabsf(v[t][i]);
+                    const double e = (double)aw - (double)a * (double)code_value(magnitude_code(aw, a));
+                    err += e * e;
+                }
+            err += __shfl_xor(err, 16);
+            err += __shfl_xor(err, 32);
+            if (err < least) {
+                least = err;
+                alpha = a;
+            }
+        }
+#pragma unroll
+        for (int t = g * TG; t < (g + 1) * TG; t++) {
+            uint32_t d = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t c = (uint32_t)magnitude_code(fabsf(v[t][i]), alpha);
+                d |= (c | (c && v[t][i] < 0.0f ? 8u : 0u)) << (4 * i);
+            }
+            packed[t] = d;
+        }
+        const int k0 = 128 * kc + G * g;
+        if (j == 0)
+            scales[((int64_t)nt * L.groups + (int64_t)kc * (4 / TG) + g) * 16 + r] =
+                n < L.N && k0 < L.K ? (__bf16)alpha : (__bf16)0.0f;
+    }
+    *(uint4*)(out + 1024 * tile + 16 * lane) = uint4{packed[0], packed[1], packed[2], packed[3]};
+}
+
+// ESB(4,1) codes and row-major scales into the layout; the same owner of each code as above.
+__global__ __launch_bounds__(256) void k_w4_pack(W4Layout L, const uint8_t* __restrict__ codes, int64_t ldc,
+                                                 const __bf16* __restrict__ alpha, int64_t lda,
+                                                 uint8_t* __restrict__ out) {
+    const int lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
+    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (tile >= (int64_t)L.tiles * L.chunks) return;
+    const int kc = (int)(tile % L.chunks), nt = (int)(tile / L.chunks);
+    const int n = 16 * nt + r;
+    uint32_t packed[4];
+#pragma unroll
+    for (int t = 0; t < 4; t++) {
+        const int k = 128 * kc + 32 * t + 8 * j;
+        uint32_t d = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (n >= L.N || k + i >= L.K) continue;
+            const uint32_t c = codes[(int64_t)n * ldc + k + i];
+            // one more in the exponent field, modulo 4: the all-ones (subnormal) binade becomes 0
+            const uint32_t m = (c + 2) & 7;
+            d |= (m | (m ? c & 8 : 0)) << (4 * i);
+        }
+        packed[t] = d;
+    }
+    *(uint4*)(out + 1024 * tile + 16 * lane) = uint4{packed[0], packed[1], packed[2], packed[3]};
+    __bf16* scales = (__bf16*)(out + L.scale_offset);
+    const int per = 128 / L.group;
+    if (j < per) {
+        const int g = kc * per + j;
+        scales[((int64_t)nt * L.groups + g) * 16 + r] =
+            n < L.N && g * L.group < L.K ? alpha[(int64_t)n * lda + g] : (__bf16)0.0f;
+    }
+}
+
+// Unscaled values as E4M3 bytes, and row-major scales.
+__global__ __launch_bounds__(256) void k_w4_unpack(W4Layout L, const uint8_t* __restrict__ in,
+                                                   uint8_t* __restrict__ values, int64_t ldv,
+                                                   __bf16* __restrict__ alpha, int64_t lda) {
+    const int lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
+    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (tile >= (int64_t)L.tiles * L.chunks) return;
+    const int kc = (int)(tile % L.chunks), nt = (int)(tile / L.chunks);
+    const int n = 16 * nt + r;
+    if (n >= L.N) return;
+    const uint4 p = *(const uint4*)(in + 1024 * tile + 16 * lane);
+    const uint32_t packed[4] = {p.x, p.y, p.z, p.w};
+    if (values) {
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const int k = 128 * kc + 32 * t + 8 * j;
+            // the eight magnitudes as E4M3 bytes, picked by v_perm_b32
+            uint32_t o[2];
+            const uint32_t ev = packed[t] & 0x0f0f0f0fu, od = (packed[t] >> 4) & 0x0f0f0f0fu;
+            const uint32_t be = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, ev & 0x07070707u) | ((ev & 0x08080808u) << 4);
+            const uint32_t bo = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, od & 0x07070707u) | ((od & 0x08080808u) << 4);
+            o[0] = __builtin_amdgcn_perm(bo, be, 0x05010400u);
+            o[1] = __builtin_amdgcn_perm(bo, be, 0x07030602u);
+            uint8_t* dst = values + (int64_t)n * ldv + k;
+            if (L.K - k >= 8) {
+                ((Loose<uint2, uint8_t>*)dst)->v = uint2{o[0], o[1]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (k + i < L.K) dst[i] = (uint8_t)(o[i >> 2] >> (8 * (i & 3)));
+            }
+        }
+    }
+    const __bf16* scales = (const __bf16*)(in + L.scale_offset);
+    const int per = 128 / L.group;
+    if (alpha && j < per) {
+        const int g = kc * per + j;
+        if (g * L.group < L.K) alpha[(int64_t)n * lda + g] = scales[((int64_t)nt * L.groups + g) * 16 + r];
+    }
+}
+
+unsigned tile_blocks(const W4Layout& L) { return (unsigned)(((int64_t)L.tiles * L.chunks + 3) / 4); }
+
+template <typename T>
+hipError_t quantize_t(const W4Layout& L, const void* w, int64_t ldw, const float* f, int nf, void* out,
+                      hipStream_t s) {
+    const unsigned b = tile_blocks(L);
+    if (L.group == 32) k_w4_quantize<T, 32><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
+    else if (L.group == 64) k_w4_quantize<T, 64><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
+    else k_w4_quantize<T, 128><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+W4Layout w4_layout(int N, int K, int group) {
+    W4Layout L;
+    L.N = N;
+    L.K = K;
+    L.group = group;
+    L.tiles = (int)(((int64_t)N + 15) / 16);
+    L.chunks = (int)(((int64_t)K + 127) / 128);
+    L.groups = L.chunks * (128 / group);
+    L.scale_offset = (int64_t)L.tiles * L.chunks * 1024;
+    L.bytes = L.scale_offset + (int64_t)L.tiles * L.groups * 32;
+    return L;
+}
+
+hipError_t launch_w4_quantize(const W4Layout& L, int type, const void* w, int64_t ldw, const float* factors,
+                              int nf, void* out, hipStream_t s) {
+    if (type == kF32) return quantize_t<float>(L, w, ldw, factors, nf, out, s);
+    if (type == kBF16) return quantize_t<__bf16>(L, w, ldw, factors, nf, out, s);
+    return quantize_t<_Float16>(L, w, ldw, factors, nf, out, s);
+}
+
+hipError_t launch_w4_pack(const W4Layout& L, const uint8_t* codes, int64_t ldc, const void* alpha, int64_t lda,
+                          void* out, hipStream_t s) {
+    k_w4_pack<<<tile_blocks(L), 256, 0, s>>>(L, codes, ldc, (const __bf16*)alpha, lda, (uint8_t*)out);
+    return hipGetLastError();
+}
+
+hipError_t launch_w4_unpack(const W4Layout& L, const void* in, uint8_t* values, int64_t ldv, void* alpha,
+                            int64_t lda, hipStream_t s) {
+    k_w4_unpack<<<tile_blocks(L), 256, 0, s>>>(L, (const uint8_t*)in, values, ldv, (__bf16*)alpha, lda);
+    return hipGetLastError();
+}
+
+}  // namespace esb

@@ -23,6 +23,10 @@ ESB_E_SCRATCH = -7
 ESB_DDA_NOALLOC_SCRATCH = 4 << 20
 ESB_B_NK = 0
 ESB_B_KN = 1
+ESB_F32 = 0
+ESB_BF16 = 1
+ESB_F16 = 2
+ESB_E4M3 = 3
 
 _lib = None
 _torch = None        # torch, once lib() has loaded (its attribute look-ups cost less than an import)
@@ -74,6 +78,7 @@ def lib():
             pass
         L = ctypes.CDLL(LIB_PATH)
         P, i32, i64, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
+        f32 = ctypes.c_float
         sig = {
             "esb_version": (i32, []),
             "esb_strerror": (ctypes.c_char_p, [i32]),
@@ -120,6 +125,13 @@ def lib():
             "esb_dn_stats": (i32, [P, i64, P, P, sz, P]),
             "esb_project_dn": (i32, [P, i64, P, P, i32, i32, P, P]),
             "esb_dda_normal": (i32, [i32, i32, P, i32, P, P, P, P]),
+            "esb_rmsnorm": (i32, [P, i64, P, i64, i32, i64, i64, P, f32, P, i64, P, i64, P, i64, P, P]),
+            "esb_swiglu": (i32, [P, i64, P, i64, i32, i64, i64, P, i64, P, i64, P, P]),
+            "esb_w4_size": (sz, [i32, i32, i32]),
+            "esb_w4_quantize": (i32, [P, i64, i32, i32, i32, i32, P, i32, P, sz, P]),
+            "esb_w4_pack": (i32, [P, i64, P, i64, i32, i32, i32, P, sz, P]),
+            "esb_w4_unpack": (i32, [P, i32, i32, i32, P, i64, P, i64, P]),
+            "esb_w4_gemm": (i32, [i32, i32, i32, i32, P, i64, i32, P, P, P, i64, i32, P]),
             "esb_gemm_packed": (i32, [i32, i32, i32, P, i64, i32, i32, P, P, i32, i32, P, P, P, i64,
                                       P, sz, P]),
         }
@@ -642,3 +654,221 @@ def esb_conv2d(x, nX, kX_sig, alphaX, w, nW, kW_sig, alphaW, stride=(1, 1), pad=
                                                     _ptr(alphaX), _ptr(w), nW, kW_sig, _ptr(alphaW),
                                                     _ptr(acc), _ptr(y), wp, wb, _stream(stream)))
     return acc, y
+
+
+# ---- decoder operators ----------------------------------------------------------------------
+
+_types = None        # dtype -> ESB_F32 / ESB_BF16 / ESB_F16 / ESB_E4M3
+
+
+def _type(t, name, allowed):
+    """Number of the tensor's (or dtype's) element type, one of `allowed`."""
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: ESB_F32, torch.bfloat16: ESB_BF16, torch.float16: ESB_F16,
+                  torch.float8_e4m3fn: ESB_E4M3}
+    n = _types.get(getattr(t, "dtype", t))
+    if n not in allowed:
+        raise TypeError("%s has an element type that this call does not take" % name)
+    return n
+
+
+_FLOATS = (ESB_F32, ESB_BF16, ESB_F16)
+
+
+def _matrix(t, name):
+    """(rows, columns, pitch) of a device matrix whose columns are adjacent; rows may be apart."""
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions" % name)
+    rows, cols = t.shape
+    sr, sc = t.stride()
+    if cols > 1 and sc != 1:
+        raise ValueError("%s must have adjacent columns" % name)
+    if rows <= 1:
+        return rows, cols, cols
+    if sr < cols:
+        raise ValueError("%s must not have overlapping rows" % name)
+    return rows, cols, sr
+
+
+def _like(t, name, shape, dtype, device):
+    """Pitch of a matrix that has to have this shape, type and device."""
+    rows, cols, ld = _matrix(t, name)
+    if (rows, cols) != shape or t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be %s of %s on %s" % (name, shape, dtype, device))
+    return ld
+
+
+def _vector(t, name, n, dtype, device):
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.device != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous elements on %s" % (name, n, device))
+
+
+def _row_outputs(rows, d, dtype, device, y, want_y, y8, scale, want_y8):
+    """y, y8 and scale as given or new, and the pitches of y and y8."""
+    torch = _torch
+    if y is None and want_y:
+        y = torch.empty((rows, d), dtype=dtype, device=device)
+        ldy = d
+    else:
+        ldy = 0 if y is None else _like(y, "y", (rows, d), dtype, device)
+    if y8 is None and want_y8:
+        y8 = torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=device)
+        ld8 = d
+    else:
+        ld8 = 0 if y8 is None else _like(y8, "y8", (rows, d), torch.float8_e4m3fn, device)
+    if y8 is not None:
+        if scale is None:
+            scale = torch.empty(rows, dtype=torch.float32, device=device)
+        else:
+            _vector(scale, "scale", rows, torch.float32, device)
+    return y, ldy, y8, ld8, scale
+
+
+def esb_rmsnorm(x, w, eps, residual=None, sum_out=None, want_sum=False, y=None, want_y=False,
+                y8=None, scale=None, want_y8=True, stream=None):
+    """Rows of z = x + residual, normalized: y = z / sqrt(mean(z^2) + eps) * w.  x, residual,
+    sum_out, y: rows x d, fp32, bf16 or fp16 (row pitches allowed); w: d fp32, or None.
+    Returns (sum, y, y8, scale): z and y in x's type, and y as float8_e4m3fn under one fp32 scale
+    per row; what is neither given nor wanted is None."""
+    L = _lib or lib()
+    t = _type(x, "x", _FLOATS)
+    rows, d, ldx = _matrix(x, "x")
+    dtype, device = x.dtype, x.device
+    ldr = 0 if residual is None else _like(residual, "residual", (rows, d), dtype, device)
+    if w is not None:
+        _vector(w, "w", d, _torch.float32, device)
+    if sum_out is None and want_sum:
+        sum_out = _torch.empty((rows, d), dtype=dtype, device=device)
+    lds = 0 if sum_out is None else _like(sum_out, "sum_out", (rows, d), dtype, device)
+    y, ldy, y8, ld8, scale = _row_outputs(rows, d, dtype, device, y, want_y, y8, scale, want_y8)
+    st = L.esb_rmsnorm(x.data_ptr(), ldx, _addr(residual), ldr, t, rows, d, _addr(w), eps,
+                       _addr(sum_out), lds, _addr(y), ldy, _addr(y8), ld8, _addr(scale),
+                       _stream(stream))
+    if st:
+        raise EsbError("esb_rmsnorm", st)
+    return sum_out, y, y8, scale
+
+
+def esb_swiglu(gate, up, y=None, want_y=False, y8=None, scale=None, want_y8=True, stream=None):
+    """gate / (1 + exp(-gate)) * up, rows x d; returns (y, y8, scale) as esb_rmsnorm does."""
+    L = _lib or lib()
+    t = _type(gate, "gate", _FLOATS)
+    rows, d, ldg = _matrix(gate, "gate")
+    dtype, device = gate.dtype, gate.device
+    ldu = _like(up, "up", (rows, d), dtype, device)
+    y, ldy, y8, ld8, scale = _row_outputs(rows, d, dtype, device, y, want_y, y8, scale, want_y8)
+    st = L.esb_swiglu(gate.data_ptr(), ldg, up.data_ptr(), ldu, t, rows, d, _addr(y), ldy, _addr(y8),
+                      ld8, _addr(scale), _stream(stream))
+    if st:
+        raise EsbError("esb_swiglu", st)
+    return y, y8, scale
+
+
+def esb_w4_size(N, K, group):
+    return int(lib().esb_w4_size(N, K, group))
+
+
+def _w4_buffer(w4, N, K, group, device):
+    need = esb_w4_size(N, K, group)
+    if w4 is None:
+        if need == 0 and N and K:
+            raise EsbError("esb_w4_size", ESB_E_INVALID)
+        return _torch.empty(max(need, 1), dtype=_torch.uint8, device=device)
+    return _w4_check(w4, device)
+
+
+def _w4_check(w4, device):
+    if w4.dtype != _torch.uint8 or w4.device != device or not w4.is_contiguous():
+        raise ValueError("w4 must be contiguous uint8 on %s" % (device,))
+    return w4
+
+
+def esb_w4_quantize(w, group, factors=None, w4=None, stream=None):
+    """4-bit codes and group scales of w (N x K, fp32, bf16 or fp16), packed: a uint8 tensor of
+    esb_w4_size(N, K, group) bytes.  factors: device fp32 candidates of the scale, as multiples
+    of max|w| / 6 of the group (None: 1)."""
+    L = _lib or lib()
+    t = _type(w, "w", _FLOATS)
+    N, K, ld = _matrix(w, "w")
+    if factors is not None:
+        _vector(factors, "factors", factors.numel(), _torch.float32, w.device)
+    w4 = _w4_buffer(w4, N, K, group, w.device)
+    st = L.esb_w4_quantize(w.data_ptr(), ld, t, N, K, group, _addr(factors),
+                           1 if factors is None else factors.numel(), w4.data_ptr(), w4.numel(),
+                           _stream(stream))
+    if st:
+        raise EsbError("esb_w4_quantize", st)
+    return w4
+
+
+def esb_w4_pack(codes, alpha, group, w4=None, stream=None):
+    """The packed form of ESB(4,1) codes (N x K uint8) and bf16 scales (N x ceil(K / group))."""
+    L = _lib or lib()
+    if codes.dtype != _torch.uint8:
+        raise TypeError("codes must be uint8")
+    N, K, ldc = _matrix(codes, "codes")
+    lda = _like(alpha, "alpha", (N, -(-K // group) if group > 0 else 0), _torch.bfloat16, codes.device)
+    w4 = _w4_buffer(w4, N, K, group, codes.device)
+    st = L.esb_w4_pack(codes.data_ptr(), ldc, alpha.data_ptr(), lda, N, K, group, w4.data_ptr(),
+                       w4.numel(), _stream(stream))
+    if st:
+        raise EsbError("esb_w4_pack", st)
+    return w4
+
+
+def _w4_holds(w4, N, K, group):
+    need = esb_w4_size(N, K, group)
+    if w4.numel() < need or (need == 0 and N and K):
+        raise EsbError("esb_w4_size", ESB_E_WORKSPACE if need else ESB_E_INVALID)
+
+
+def esb_w4_unpack(w4, N, K, group, values=None, alpha=None, stream=None):
+    """(values, alpha): the unscaled values (N x K float8_e4m3fn, exact) and the group scales
+    (N x ceil(K / group) bf16) of packed weights."""
+    L = _lib or lib()
+    torch = _torch
+    _w4_check(w4, w4.device)
+    _w4_holds(w4, N, K, group)
+    groups = -(-K // group) if group > 0 else 0
+    if values is None:
+        values = torch.empty((N, K), dtype=torch.float8_e4m3fn, device=w4.device)
+    if alpha is None:
+        alpha = torch.empty((N, groups), dtype=torch.bfloat16, device=w4.device)
+    ldv = _like(values, "values", (N, K), torch.float8_e4m3fn, w4.device)
+    lda = _like(alpha, "alpha", (N, groups), torch.bfloat16, w4.device)
+    st = L.esb_w4_unpack(w4.data_ptr(), N, K, group, values.data_ptr(), ldv, alpha.data_ptr(), lda,
+                         _stream(stream))
+    if st:
+        raise EsbError("esb_w4_unpack", st)
+    return values, alpha
+
+
+def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, stream=None):
+    """y = x W^T for x (M x K: bf16, fp16, or float8_e4m3fn with x_scale, M fp32) and packed
+    weights W (N x K); y in y_dtype (None: x's type; bf16 for float8)."""
+    L = _lib or lib()
+    tx = _type(x, "x", (ESB_F32, ESB_BF16, ESB_F16, ESB_E4M3))   # fp32: the library's refusal
+    M, K, ldx = _matrix(x, "x")
+    device = x.device
+    _w4_check(w4, device)
+    _w4_holds(w4, N, K, group)
+    if x_scale is not None:
+        _vector(x_scale, "x_scale", M, _torch.float32, device)
+    if y is None:
+        if y_dtype is None:
+            y_dtype = _torch.bfloat16 if tx == ESB_E4M3 else x.dtype
+        y = _torch.empty((M, N), dtype=y_dtype, device=device)
+        ldy = N
+    else:
+        ldy = _like(y, "y", (M, N), y_dtype or y.dtype, device)
+    st = L.esb_w4_gemm(M, N, K, group, x.data_ptr(), ldx, tx, _addr(x_scale), w4.data_ptr(),
+                       y.data_ptr(), ldy, _type(y, "y", _FLOATS), _stream(stream))
+    if st:
+        raise EsbError("esb_w4_gemm", st)
+    return y
