@@ -533,11 +533,11 @@ int esb_swiglu(const void* gate, int64_t ldg, const void* up, int64_t ldu, int t
  * q the values of ESB(4,1) (OCP E2M1: 0, .5, 1, 1.5, 2, 3, 4, 6 and signs), alpha in bf16.
  * The packed form (esb_w4_size bytes, 16-byte aligned, 0 for invalid arguments) is what the
  * matrix cores read and is not position-independent of (N, K, group), which every call gets:
- *   tiles of 16 rows x 128 columns, 1 KB each, tile (n / 16, k / 128) at index
- *   (n / 16) * ceil(K / 128) + k / 128.  Within a tile, row r = n % 16, the E2M1 nibble of
- *   column k is nibble k % 8 (lowest first) of the 32-bit word
- *   4 * (16 * ((k / 8) % 4) + r) + (k / 32) % 4;  then, after all tiles, the bf16 scales,
- *   alpha[n][g] at index ((n / 16) * ceil(K / 128) * (128 / group) + g) * 16 + r.
+ *   tiles of 32 rows x 64 columns, 1 KB each, tile (n / 32, k / 64) at index
+ *   (n / 32) * ceil(K / 64) + k / 64.  Within a tile, with r = n % 32, c = k % 64 and
+ *   t = c / 16, the E2M1 nibble of (n, k) is nibble c % 8 (lowest first) of the 32-bit word
+ *   4 * (32 * ((c / 8) % 2) + r) + (t / 2 + 2 * (t % 2));  then, after all tiles, the bf16
+ *   scales, alpha[n][g] at index ((n / 32) * ceil(64 * ceil(K / 64) / group) + g) * 32 + r.
  *   Rows and columns past N and K hold zeros.
  *
  * esb_w4_quantize: codes and scales of W (device, `type`).  Per group, over the candidates

@@ -588,10 +588,10 @@ struct RowsParams {
 };
 hipError_t launch_rows(int op, int type, const RowsParams& p, hipStream_t s);
 
-// 4-bit weights (w4.hip): tiles of 16 rows x 128 columns, then the scales.
+// 4-bit weights (w4.hip): tiles of 32 rows x 64 columns, then the scales.
 struct W4Layout {
     int N, K, group;
-    int tiles, chunks, groups;   // row tiles, column chunks, groups of a row (whole chunks)
+    int tiles, chunks, groups;   // row tiles, column chunks, groups of a row of whole chunks
     int64_t scale_offset, bytes;
 };
 W4Layout w4_layout(int N, int K, int group);

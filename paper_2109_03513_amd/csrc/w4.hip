@@ -8,11 +8,15 @@
 // cell bounds mid * alpha exact in fp32 (3 + 8 bits), so codes are the exact nearest values of
 // w / alpha, ties to the larger magnitude, with no division.
 //
-// Layout (w4_layout): what one wave of the products reads per step is contiguous.  Tiles of 16
-// rows x 128 columns, 1 KB each, [row tile][column chunk]; lane 16j + r of a tile owns row r and
-// 16 bytes: dword t holds columns 32t + 8j .. + 7, lowest nibble first.  Dword t of the 64 lanes is
-// then the operand of one 16x16x32 MFMA over the columns 32t .. 32t+31 (a whole group of 32), and
-// the 16 bytes are the operand of one 16x16x128 MFMA.  The scales follow, [row tile][group][16
+// Layout (w4_layout): what a wave of the products reads per step is contiguous.  Tiles of 32 rows x
+// 64 columns, 1 KB each, [row tile][column chunk]; lane 32h + r of a tile owns row r and 16 bytes,
+// four words of eight columns 16t + 8h .. + 7 (lowest nibble first) in the order t = 0, 2, 1, 3.
+//  * Word t of the 64 lanes is the operand of one 32x32x16 MFMA over columns 16t .. 16t+15;
+//  * the 16 bytes are the operand of one 32x32x64 MFMA on 4-bit values (any order of the
+//    reduction that both operands share is right);
+//  * the low or high half of the 16 bytes of 16 rows, lane 16(2h + e) + r, are words t = e and 2 + e:
+//    operands of two 16x16x32 MFMAs over columns 0 .. 31 and 32 .. 63.
+// So every MFMA stays within one group of 32, 64 or 128.  The scales follow, [row tile][group][32
 // rows].  Rows and columns beyond N and K hold codes and scales of 0.
 #include "float_rows.h"
 
@@ -33,37 +37,63 @@ __device__ __forceinline__ float code_value(int c) {
     return c < 2 ? 0.5f * (float)c : __uint_as_float(((uint32_t)(126 + (c >> 1)) << 23) | ((uint32_t)(c & 1) << 22));
 }
 
-// A wave per tile of 16 x 128 weights; lane 16j + r holds 32 weights of row r.
+// Owner of the weights in the kernels below: a wave takes two adjacent tiles (128 columns, one
+// group of 128), lane 32h + r of it the columns 64u + 16t + 8h .. + 7 of row r, word 4u + t.
+struct Owner {
+    int r, h, nt, kc;    // row and half in the tile, row tile, first chunk
+    int64_t n;
+};
+__device__ __forceinline__ bool own(const W4Layout& L, Owner* o) {
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int pairs = (L.chunks + 1) / 2;
+    if (wave >= (int64_t)L.tiles * pairs) return false;
+    o->r = lane & 31;
+    o->h = lane >> 5;
+    o->nt = (int)(wave / pairs);
+    o->kc = 2 * (int)(wave % pairs);
+    o->n = 32 * (int64_t)o->nt + o->r;
+    return true;
+}
+__device__ __forceinline__ int column(const Owner& o, int word) {
+    return 64 * (o.kc + (word >> 2)) + 16 * (word & 3) + 8 * o.h;
+}
+// The lane's eight words into the two tiles.
+__device__ __forceinline__ void put_tiles(const W4Layout& L, const Owner& o, const uint32_t (&w)[8], uint8_t* out) {
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+        if (o.kc + u < L.chunks)
+            *(uint4*)(out + 1024 * ((int64_t)o.nt * L.chunks + o.kc + u) + 16 * (32 * o.h + o.r)) =
+                uint4{w[4 * u], w[4 * u + 2], w[4 * u + 1], w[4 * u + 3]};
+}
+__device__ __forceinline__ int64_t scale_index(const W4Layout& L, const Owner& o, int g) {
+    return ((int64_t)o.nt * L.groups + g) * 32 + o.r;
+}
+
 template <typename T, int G>
 __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __restrict__ w, int64_t ldw,
                                                      const float* __restrict__ factors, int nf,
                                                      uint8_t* __restrict__ out) {
-    const int lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (tile >= (int64_t)L.tiles * L.chunks) return;
-    const int kc = (int)(tile % L.chunks), nt = (int)(tile / L.chunks);
-    const int n = 16 * nt + r;
-    constexpr int TG = G / 32;      // dwords of a lane in one group
-
-    float v[4][8];
+    Owner o;
+    if (!own(L, &o)) return;
+    constexpr int WG = G / 16;      // words of a lane in one group
+    float v[8][8];
 #pragma unroll
-    for (int t = 0; t < 4; t++) {
-        const int k = 128 * kc + 32 * t + 8 * j;
-        const int left = n < L.N ? L.K - k : 0;
-        const f32x8 x = __builtin_convertvector(load8(w + (int64_t)n * ldw + k, left), f32x8);
+    for (int t = 0; t < 8; t++) {
+        const int k = column(o, t);
+        const f32x8 x = __builtin_convertvector(load8(w + o.n * ldw + k, o.n < L.N ? L.K - k : 0), f32x8);
 #pragma unroll
         for (int i = 0; i < 8; i++) v[t][i] = x[i];
     }
-    uint32_t packed[4];
+    uint32_t packed[8];
     __bf16* scales = (__bf16*)(out + L.scale_offset);
 #pragma unroll
-    for (int g = 0; g < 4 / TG; g++) {
+    for (int g = 0; g < 8 / WG; g++) {
         uint32_t m = 0;
 #pragma unroll
-        for (int t = g * TG; t < (g + 1) * TG; t++)
+        for (int t = g * WG; t < (g + 1) * WG; t++)
 #pragma unroll
             for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[t][i]) & 0x7fffffffu);
-        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
         m = max(m, (uint32_t)__shfl_xor((int)m, 32));
         const float top = __uint_as_float(m);
         float alpha = __builtin_nanf("");
@@ -74,14 +104,13 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
             if (!(f > 0.0f) || !(top < __builtin_inff()) || !(a < __builtin_inff())) continue;
             double err = 0.0;
 #pragma unroll
-            for (int t = g * TG; t < (g + 1) * TG; t++)
+            for (int t = g * WG; t < (g + 1) * WG; t++)
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     const float aw = fabsf(v[t][i]);
                     const double e = (double)aw - (double)a * (double)code_value(magnitude_code(aw, a));
                     err += e * e;
                 }
-            err += __shfl_xor(err, 16);
             err += __shfl_xor(err, 32);
             if (err < least) {
                 least = err;
@@ -89,7 +118,7 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
             }
         }
 #pragma unroll
-        for (int t = g * TG; t < (g + 1) * TG; t++) {
+        for (int t = g * WG; t < (g + 1) * WG; t++) {
             uint32_t d = 0;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
@@ -98,90 +127,83 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
             }
             packed[t] = d;
         }
-        const int k0 = 128 * kc + G * g;
-        if (j == 0)
-            scales[((int64_t)nt * L.groups + (int64_t)kc * (4 / TG) + g) * 16 + r] =
-                n < L.N && k0 < L.K ? (__bf16)alpha : (__bf16)0.0f;
+        const int gi = 64 * o.kc / G + g;
+        if (o.h == 0 && gi < L.groups)
+            scales[scale_index(L, o, gi)] = o.n < L.N && gi * G < L.K ? (__bf16)alpha : (__bf16)0.0f;
     }
-    *(uint4*)(out + 1024 * tile + 16 * lane) = uint4{packed[0], packed[1], packed[2], packed[3]};
+    put_tiles(L, o, packed, out);
 }
 
-// ESB(4,1) codes and row-major scales into the layout; the same owner of each code as above.
+// ESB(4,1) codes and row-major scales into the layout.
 __global__ __launch_bounds__(256) void k_w4_pack(W4Layout L, const uint8_t* __restrict__ codes, int64_t ldc,
                                                  const __bf16* __restrict__ alpha, int64_t lda,
                                                  uint8_t* __restrict__ out) {
-    const int lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (tile >= (int64_t)L.tiles * L.chunks) return;
-    const int kc = (int)(tile % L.chunks), nt = (int)(tile / L.chunks);
-    const int n = 16 * nt + r;
-    uint32_t packed[4];
+    Owner o;
+    if (!own(L, &o)) return;
+    uint32_t packed[8];
 #pragma unroll
-    for (int t = 0; t < 4; t++) {
-        const int k = 128 * kc + 32 * t + 8 * j;
+    for (int t = 0; t < 8; t++) {
+        const int k = column(o, t);
         uint32_t d = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            if (n >= L.N || k + i >= L.K) continue;
-            const uint32_t c = codes[(int64_t)n * ldc + k + i];
+            if (o.n >= L.N || k + i >= L.K) continue;
+            const uint32_t c = codes[o.n * ldc + k + i];
             // one more in the exponent field, modulo 4: the all-ones (subnormal) binade becomes 0
             const uint32_t m = (c + 2) & 7;
             d |= (m | (m ? c & 8 : 0)) << (4 * i);
         }
         packed[t] = d;
     }
-    *(uint4*)(out + 1024 * tile + 16 * lane) = uint4{packed[0], packed[1], packed[2], packed[3]};
+    put_tiles(L, o, packed, out);
     __bf16* scales = (__bf16*)(out + L.scale_offset);
-    const int per = 128 / L.group;
-    if (j < per) {
-        const int g = kc * per + j;
-        scales[((int64_t)nt * L.groups + g) * 16 + r] =
-            n < L.N && g * L.group < L.K ? alpha[(int64_t)n * lda + g] : (__bf16)0.0f;
-    }
+    if (o.h) return;
+    const int g0 = 64 * o.kc / L.group, per = 128 / L.group;
+    for (int g = g0; g < g0 + per && g < L.groups; g++)
+        scales[scale_index(L, o, g)] = o.n < L.N && (int64_t)g * L.group < L.K ? alpha[o.n * lda + g] : (__bf16)0.0f;
 }
 
 // Unscaled values as E4M3 bytes, and row-major scales.
 __global__ __launch_bounds__(256) void k_w4_unpack(W4Layout L, const uint8_t* __restrict__ in,
                                                    uint8_t* __restrict__ values, int64_t ldv,
                                                    __bf16* __restrict__ alpha, int64_t lda) {
-    const int lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (tile >= (int64_t)L.tiles * L.chunks) return;
-    const int kc = (int)(tile % L.chunks), nt = (int)(tile / L.chunks);
-    const int n = 16 * nt + r;
-    if (n >= L.N) return;
-    const uint4 p = *(const uint4*)(in + 1024 * tile + 16 * lane);
-    const uint32_t packed[4] = {p.x, p.y, p.z, p.w};
+    Owner o;
+    if (!own(L, &o) || o.n >= L.N) return;
     if (values) {
 #pragma unroll
-        for (int t = 0; t < 4; t++) {
-            const int k = 128 * kc + 32 * t + 8 * j;
-            // the eight magnitudes as E4M3 bytes, picked by v_perm_b32
-            uint32_t o[2];
-            const uint32_t ev = packed[t] & 0x0f0f0f0fu, od = (packed[t] >> 4) & 0x0f0f0f0fu;
-            const uint32_t be = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, ev & 0x07070707u) | ((ev & 0x08080808u) << 4);
-            const uint32_t bo = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, od & 0x07070707u) | ((od & 0x08080808u) << 4);
-            o[0] = __builtin_amdgcn_perm(bo, be, 0x05010400u);
-            o[1] = __builtin_amdgcn_perm(bo, be, 0x07030602u);
-            uint8_t* dst = values + (int64_t)n * ldv + k;
-            if (L.K - k >= 8) {
-                ((Loose<uint2, uint8_t>*)dst)->v = uint2{o[0], o[1]};
-            } else {
+        for (int u = 0; u < 2; u++) {
+            if (o.kc + u >= L.chunks) break;
+            const uint4 p = *(const uint4*)(in + 1024 * ((int64_t)o.nt * L.chunks + o.kc + u) + 16 * (32 * o.h + o.r));
+            const uint32_t packed[4] = {p.x, p.z, p.y, p.w};
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if (k + i < L.K) dst[i] = (uint8_t)(o[i >> 2] >> (8 * (i & 3)));
+            for (int t = 0; t < 4; t++) {
+                const int k = column(o, 4 * u + t);
+                // the eight magnitudes as E4M3 bytes, picked by v_perm_b32
+                const uint32_t ev = packed[t] & 0x0f0f0f0fu, od = (packed[t] >> 4) & 0x0f0f0f0fu;
+                const uint32_t be = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, ev & 0x07070707u) | ((ev & 0x08080808u) << 4);
+                const uint32_t bo = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, od & 0x07070707u) | ((od & 0x08080808u) << 4);
+                const uint32_t q[2] = {__builtin_amdgcn_perm(bo, be, 0x05010400u),
+                                       __builtin_amdgcn_perm(bo, be, 0x07030602u)};
+                uint8_t* dst = values + o.n * ldv + k;
+                if (L.K - k >= 8) {
+                    ((Loose<uint2, uint8_t>*)dst)->v = uint2{q[0], q[1]};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        if (k + i < L.K) dst[i] = (uint8_t)(q[i >> 2] >> (8 * (i & 3)));
+                }
             }
         }
     }
+    if (!alpha || o.h) return;
     const __bf16* scales = (const __bf16*)(in + L.scale_offset);
-    const int per = 128 / L.group;
-    if (alpha && j < per) {
-        const int g = kc * per + j;
-        if (g * L.group < L.K) alpha[(int64_t)n * lda + g] = scales[((int64_t)nt * L.groups + g) * 16 + r];
-    }
+    const int g0 = 64 * o.kc / L.group, per = 128 / L.group;
+    for (int g = g0; g < g0 + per && (int64_t)g * L.group < L.K; g++) alpha[o.n * lda + g] = scales[scale_index(L, o, g)];
 }
 
-unsigned tile_blocks(const W4Layout& L) { return (unsigned)(((int64_t)L.tiles * L.chunks + 3) / 4); }
+unsigned tile_blocks(const W4Layout& L) {   // a wave per two chunks
+    return (unsigned)(((int64_t)L.tiles * ((L.chunks + 1) / 2) + 3) / 4);
+}
 
 template <typename T>
 hipError_t quantize_t(const W4Layout& L, const void* w, int64_t ldw, const float* f, int nf, void* out,
@@ -200,11 +222,11 @@ W4Layout w4_layout(int N, int K, int group) {
     L.N = N;
     L.K = K;
     L.group = group;
-    L.tiles = (int)(((int64_t)N + 15) / 16);
-    L.chunks = (int)(((int64_t)K + 127) / 128);
-    L.groups = L.chunks * (128 / group);
+    L.tiles = (int)(((int64_t)N + 31) / 32);
+    L.chunks = (int)(((int64_t)K + 63) / 64);
+    L.groups = (int)((64 * (int64_t)L.chunks + group - 1) / group);
     L.scale_offset = (int64_t)L.tiles * L.chunks * 1024;
-    L.bytes = L.scale_offset + (int64_t)L.tiles * L.groups * 32;
+    L.bytes = L.scale_offset + (int64_t)L.tiles * L.groups * 64;
     return L;
 }
 

@@ -51,8 +51,9 @@ def test_rows(L):
 
 def test_weights(L):
     size = L.esb_w4_size
-    assert size(16, 128, 128) == 1024 + 32
-    assert size(17, 129, 32) == 4 * (1024 + 4 * 32)
+    assert size(32, 128, 128) == 2 * 1024 + 64
+    assert size(33, 129, 32) == 2 * 3 * (1024 + 2 * 64)
+    assert size(1, 65, 128) == 2 * 1024 + 64 and size(1, 1, 128) == 1024 + 64
     assert size(0, 128, 128) == 0 and size(16, 0, 128) == 0
     assert size(-1, 128, 128) == 0 and size(16, -1, 128) == 0 and size(16, 128, 16) == 0
     assert size((1 << 31) - 1, 1, 128) == 0 and size(1 << 26, 1 << 20, 128) == 0

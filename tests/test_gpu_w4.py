@@ -101,18 +101,20 @@ def test_pack_layout_and_unpack(esb, N, K, group):
     assert torch.equal(q.cpu().double(), want) and torch.equal(a.cpu(), alpha)
     assert not bool(torch.signbit(q.cpu().float()[q.cpu().float() == 0]).any())
     raw = w4.cpu().numpy()
-    tiles, chunks = -(-N // 16), -(-K // 128)
-    per = 128 // group
-    assert raw.size == 1024 * tiles * chunks + 32 * tiles * chunks * per
+    tiles, chunks = -(-N // 32), -(-K // 64)
+    per_row = -(-64 * chunks // group)
+    assert raw.size == 1024 * tiles * chunks + 64 * tiles * per_row
     words = raw[:1024 * tiles * chunks].view(np.uint32)
-    n, k = np.meshgrid(np.arange(16 * tiles), np.arange(128 * chunks), indexing="ij")
-    at = 256 * ((n // 16) * chunks + k // 128) + 4 * (16 * ((k // 8) % 4) + n % 16) + (k // 32) % 4
-    nib = (words[at] >> (4 * (k % 8)).astype(np.uint32)) & 15
+    n, k = np.meshgrid(np.arange(32 * tiles), np.arange(64 * chunks), indexing="ij")
+    c = k % 64
+    t = c // 16
+    at = 256 * ((n // 32) * chunks + k // 64) + 4 * (32 * ((c // 8) % 2) + n % 32) + t // 2 + 2 * (t % 2)
+    nib = (words[at] >> (4 * (c % 8)).astype(np.uint32)) & 15
     val = ref.LEVELS.numpy()[nib & 7] * np.where(nib & 8, -1.0, 1.0)
     np.testing.assert_array_equal(val[:N, :K], want.numpy())
     assert not nib[N:].any() and not nib[:, K:].any()
-    sc = torch.from_numpy(raw[1024 * tiles * chunks:].copy()).view(torch.bfloat16).view(tiles, chunks * per, 16)
-    sc = sc.permute(0, 2, 1).reshape(16 * tiles, chunks * per)
+    sc = torch.from_numpy(raw[1024 * tiles * chunks:].copy()).view(torch.bfloat16).view(tiles, per_row, 32)
+    sc = sc.permute(0, 2, 1).reshape(32 * tiles, per_row)
     assert torch.equal(sc[:N, :groups], alpha)
     assert not bool(sc[N:].any()) and not bool(sc[:, groups:].any())
 

@@ -164,15 +164,15 @@ def test_offsets_beyond_32_bits(esb):
 
 def test_weights_beyond_32_bits(esb):
     """Packed weights of more than 2^32 bytes: the last rows read their own tiles."""
-    N, K, group = 270000, 32768, 128
+    N, K, group = 270016, 32768, 128
     w4 = torch.zeros(esb.esb_w4_size(N, K, group), dtype=torch.uint8, device="cuda")
     assert w4.numel() > 1 << 32
     codes, alpha = weights(8, 32, K, group)
     part = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), group)
-    tiles, chunks = 2, K // 128
-    first = (N // 16 - tiles) * chunks
+    tiles, chunks, groups = 1, K // 64, K // 128
+    first = (N // 32 - tiles) * chunks
     w4[1024 * first:1024 * (first + tiles * chunks)] = part[:1024 * tiles * chunks]
-    w4[w4.numel() - 32 * tiles * chunks:] = part[1024 * tiles * chunks:]
+    w4[w4.numel() - 64 * tiles * groups:] = part[1024 * tiles * chunks:]
     for M, x in ((1, "bf16"), (40, "e4m3"), (300, "bf16"), (300, "e4m3")):
         xv, s = acts(2, M, K, x)
         y = esb.esb_w4_gemm(xv.cuda(), w4, N, group, x_scale=None if s is None else s.cuda())
