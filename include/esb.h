@@ -534,9 +534,9 @@ int esb_swiglu(const void* gate, int64_t ldg, const void* up, int64_t ldu, int t
  * The packed form (esb_w4_size bytes, 16-byte aligned, 0 for invalid arguments) is what the
  * matrix cores read and is not position-independent of (N, K, group), which every call gets:
  *   tiles of 32 rows x 64 columns, 1 KB each, tile (n / 32, k / 64) at index
- *   (n / 32) * ceil(K / 64) + k / 64.  Within a tile, with r = n % 32, c = k % 64 and
- *   t = c / 16, the E2M1 nibble of (n, k) is nibble c % 8 (lowest first) of the 32-bit word
- *   4 * (32 * ((c / 8) % 2) + r) + (t / 2 + 2 * (t % 2));  then, after all tiles, the bf16
+ *   (n / 32) * ceil(K / 64) + k / 64.  Within a tile, with r = n % 32 and c = k % 64, the E2M1
+ *   nibble of (n, k) is nibble c % 8 (lowest first) of the 32-bit word
+ *   4 * (32 * ((c / 16) % 2) + r) + c / 32 + 2 * ((c / 8) % 2);  then, after all tiles, the bf16
  *   scales, alpha[n][g] at index ((n / 32) * ceil(64 * ceil(K / 64) / group) + g) * 32 + r.
  *   Rows and columns past N and K hold zeros.
  *
@@ -571,12 +571,19 @@ int esb_w4_unpack(const void* w4, int N, int K, int group, uint8_t* values, int6
  *   x_scale device, M fp32 (s_m), or NULL (ones);
  *   w4      device, the packed form of N x K weights with this group;
  *   y       device, M x N, y_type ESB_F32, ESB_BF16 or ESB_F16.
- * Products are exact in the matrix cores' inputs, sums fp32 in an order fixed by the arguments
- * (the same call gives the same bits).  K == 0 writes zeros; M == 0 or N == 0 enqueues nothing.
+ * A group's products are exact and its sum is fp32, in an order fixed by the arguments and the
+ * alignment of x (the same call gives the same bits); with 8-bit x, groups of 64 or 128 and a
+ * 16-bit y the matrix cores may drop products below 2^-13 of the largest of their 64.
+ *   workspace  device, 32-byte aligned, at least esb_w4_gemm_workspace_size() bytes (fp32 sums
+ *              of column ranges where few rows leave CUs idle; 0 for most shapes), or NULL: no
+ *              such split.  ESB_E_WORKSPACE if it is non-NULL and ws_bytes is too small.  It
+ *              carries nothing between calls; concurrent calls need distinct ones.
+ * K == 0 writes zeros; M == 0 or N == 0 enqueues nothing.
  */
+size_t esb_w4_gemm_workspace_size(int M, int N, int K, int group, int x_type, int y_type);
 int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int x_type,
                 const float* x_scale, const void* w4, void* y, int64_t ldy, int y_type,
-                void* stream);
+                void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

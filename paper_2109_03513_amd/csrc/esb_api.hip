@@ -801,18 +801,30 @@ int esb_w4_unpack(const void* w4, int N, int K, int group, uint8_t* values, int6
     return hip_status(launch_w4_unpack(w4_layout(N, K, group), w4, values, ldv, alpha, lda, (hipStream_t)stream));
 }
 
-int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int x_type, const float* x_scale,
-                const void* w4, void* y, int64_t ldy, int y_type, void* stream) {
+// What a product refuses whatever its buffers are.
+static int w4_gemm_check(int M, int N, int K, int group, int x_type, int y_type) {
     if (x_type == ESB_F32) return ESB_E_UNSUPPORTED;
     if ((!float_type(x_type) && x_type != ESB_E4M3) || !float_type(y_type) || M < 0) return ESB_E_INVALID;
-    const int st = w4_check(N, K, group);
+    return w4_check(N, K, group);
+}
+
+size_t esb_w4_gemm_workspace_size(int M, int N, int K, int group, int x_type, int y_type) {
+    if (w4_gemm_check(M, N, K, group, x_type, y_type) || M == 0 || N == 0) return 0;
+    return w4_gemm_workspace(M, w4_layout(N, K, group), x_type, y_type);
+}
+
+int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int x_type, const float* x_scale,
+                const void* w4, void* y, int64_t ldy, int y_type, void* workspace, size_t ws_bytes, void* stream) {
+    const int st = w4_gemm_check(M, N, K, group, x_type, y_type);
     if (st) return st;
     if (ldx < K || ldy < N) return ESB_E_INVALID;
     if (M == 0 || N == 0) return ESB_OK;
-    if (!y || !aligned_for(y, y_type)) return ESB_E_INVALID;
+    if (!y || !aligned_for(y, y_type) || (uintptr_t)workspace % 32) return ESB_E_INVALID;
     if (K > 0 && (!x || !aligned_for(x, x_type) || (uintptr_t)x_scale % 4 || !w4 || (uintptr_t)w4 % 16))
         return ESB_E_INVALID;
-    const W4GemmParams p = {w4_layout(N, K, group), M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type};
+    const W4Layout L = w4_layout(N, K, group);
+    if (workspace && ws_bytes < w4_gemm_workspace(M, L, x_type, y_type)) return ESB_E_WORKSPACE;
+    const W4GemmParams p = {L, M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type, (float*)workspace};
     return hip_status(launch_w4_gemm(p, x_type, (hipStream_t)stream));
 }
 

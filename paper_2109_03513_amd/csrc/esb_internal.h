@@ -613,7 +613,10 @@ struct W4GemmParams {
     void* y;
     int64_t ldy;
     int y_type;
+    float* part;            // room for the sums of column ranges, [range][M][32 tiles], or NULL
 };
+// Bytes of p.part for these arguments (0: no split).
+size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type);
 hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s);
 
 }  // namespace esb

@@ -10,11 +10,13 @@
 //
 // Layout (w4_layout): what a wave of the products reads per step is contiguous.  Tiles of 32 rows x
 // 64 columns, 1 KB each, [row tile][column chunk]; lane 32h + r of a tile owns row r and 16 bytes,
-// four words of eight columns 16t + 8h .. + 7 (lowest nibble first) in the order t = 0, 2, 1, 3.
-//  * Word t of the 64 lanes is the operand of one 32x32x16 MFMA over columns 16t .. 16t+15;
-//  * the 16 bytes are the operand of one 32x32x64 MFMA on 4-bit values (any order of the
-//    reduction that both operands share is right);
-//  * the low or high half of the 16 bytes of 16 rows, lane 16(2h + e) + r, are words t = e and 2 + e:
+// words i of eight columns 8b .. 8b+7, b = 2h + i % 2 + 4 (i / 2) (lowest nibble first), in the order
+// i = 0, 2, 1, 3.
+//  * Word i of the 64 lanes is the operand of one 32x32x16 MFMA, words 0 and 1 (2 and 3) of the two
+//    over columns 0 .. 31 (32 .. 63);
+//  * the four words are the operand of one 32x32x64 MFMA on 4-bit values: that instruction pairs them
+//    with 8-bit values of which a lane holds 32 consecutive columns;
+//  * the low or high half of the 16 bytes of 16 rows, lane 16(2h + e) + r, are words e and 2 + e:
 //    operands of two 16x16x32 MFMAs over columns 0 .. 31 and 32 .. 63.
 // So every MFMA stays within one group of 32, 64 or 128.  The scales follow, [row tile][group][32
 // rows].  Rows and columns beyond N and K hold codes and scales of 0.
@@ -38,7 +40,7 @@ __device__ __forceinline__ float code_value(int c) {
 }
 
 // Owner of the weights in the kernels below: a wave takes two adjacent tiles (128 columns, one
-// group of 128), lane 32h + r of it the columns 64u + 16t + 8h .. + 7 of row r, word 4u + t.
+// group of 128), lane 32h + r of it words i of both tiles (word 4u + i) of row r.
 struct Owner {
     int r, h, nt, kc;    // row and half in the tile, row tile, first chunk
     int64_t n;
@@ -56,7 +58,7 @@ __device__ __forceinline__ bool own(const W4Layout& L, Owner* o) {
     return true;
 }
 __device__ __forceinline__ int column(const Owner& o, int word) {
-    return 64 * (o.kc + (word >> 2)) + 16 * (word & 3) + 8 * o.h;
+    return 64 * (o.kc + (word >> 2)) + 8 * (2 * o.h + (word & 1) + 4 * ((word >> 1) & 1));
 }
 // The lane's eight words into the two tiles.
 __device__ __forceinline__ void put_tiles(const W4Layout& L, const Owner& o, const uint32_t (&w)[8], uint8_t* out) {

@@ -6,11 +6,15 @@
 // bf16 and fp16, E4M3 activations in bf16, so a group's products are exact and its sum fp32; the
 // group's scale multiplies that sum in fp32, and the sums of the groups are added in fp32.
 //
-// Three kernels, by how many rows share the weights:
-//  * k_w4_token (M <= 16): 16 outputs per workgroup, the reduction split over its waves; the weights
+// By how many rows share the weights:
+//  * k_w4_token (few rows): 16 outputs per workgroup, the reduction split over its waves; the weights
 //    are read once from HBM and are all that costs.
-//  * k_w4_batch: 32 outputs x up to 64 rows per workgroup, split the same way.
-//  * k_w4_tile: large tiles, the activations through LDS, the weights straight into registers.
+//  * k_w4_tile: tiles of 32 to 128 rows, everything through a ring in LDS; with few tiles the
+//    reduction is split over workgroups and k_w4_sum adds the parts.
+#include <math.h>
+
+#include <type_traits>
+
 #include "float_rows.h"
 
 namespace esb {
@@ -18,6 +22,7 @@ namespace esb {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // Four pairs of 16-bit values as one fragment.
@@ -104,45 +109,58 @@ __device__ __forceinline__ void with_y(const W4GemmParams& p, F f) {
     else f((float*)p.y);
 }
 
-// 16 outputs n x 16 rows m per workgroup, the column chunks dealt to its NW waves and their sums
+// 16 outputs n x up to 16 rows m per workgroup, the column chunks dealt to its NW waves and their sums
 // added in LDS in wave order.
-template <typename X, int G, int NW>
+template <typename X, int G, int NW, int U>
 __global__ __launch_bounds__(64 * NW) void k_w4_token(W4GemmParams p) {
     typedef typename Act<X>::M M;
     __shared__ f32x4 red[NW][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, s = lane >> 4;
     const int nt = blockIdx.x >> 1, row = 16 * (blockIdx.x & 1) + r;
     if (32 * nt + 16 * (int)(blockIdx.x & 1) >= p.L.N) return;
-    const int64_t m0 = (int64_t)blockIdx.y * 16;
-    const bool live = m0 + r < p.M;
-    const X* x = (const X*)p.x + (live ? m0 + r : 0) * p.ldx;
+    const bool live = r < p.M;
+    const X* x = (const X*)p.x + (live ? r : 0) * p.ldx;
     const int h = s >> 1, e = s & 1;
     const uint8_t* w = p.w4 + (int64_t)nt * p.L.chunks * 1024 + 16 * (32 * h + row) + 8 * e;
     const uint16_t* sc = (const uint16_t*)(p.w4 + p.L.scale_offset) + (int64_t)nt * p.L.groups * 32 + row;
     f32x4 acc = {0, 0, 0, 0};
-    for (int kc = wave; kc < p.L.chunks; kc += NW) {
-        const uint2 q = *(const uint2*)(w + (int64_t)kc * 1024);
-        typename Act<X>::raw raw[2] = {};
-        const int k = 64 * kc + 16 * e + 8 * h;
-        if (live) {
-            raw[0] = Act<X>::load(x + k, p.L.K - k);
-            raw[1] = Act<X>::load(x + k + 32, p.L.K - k - 32);
-        }
-        const f32x4 zero = {0, 0, 0, 0};
-        if (G == 32) {
-            const f32x4 p0 = M::mma(Act<X>::frag(raw[0]), M::decode(q.x), zero);
-            const f32x4 p1 = M::mma(Act<X>::frag(raw[1]), M::decode(q.y), zero);
-            const float a0 = scale_value(sc[(int64_t)kc * 64]), a1 = scale_value(sc[(int64_t)kc * 64 + 32]);
+    constexpr int NG = G == 32 ? 2 : 1;
+    // U chunks at a time, every load in flight before the first product
+    auto go = [&](int k0, auto full) {
+        constexpr int n = decltype(full)::value;
+        uint2 q[n];
+        uint16_t a[n][NG];
+        typename Act<X>::raw raw[n][2];
 #pragma unroll
-            for (int i = 0; i < 4; i++) acc[i] = fmaf(a1, p1[i], fmaf(a0, p0[i], acc[i]));
-        } else {
-            const f32x4 p0 = M::mma(Act<X>::frag(raw[0]), M::decode(q.x), zero);
-            const f32x4 p1 = M::mma(Act<X>::frag(raw[1]), M::decode(q.y), p0);
-            const float a = scale_value(sc[(int64_t)(G == 64 ? kc : kc >> 1) * 32]);
+        for (int u = 0; u < n; u++) {
+            const int kc = k0 + u * NW;
+            q[u] = *(const uint2*)(w + (int64_t)kc * 1024);
 #pragma unroll
-            for (int i = 0; i < 4; i++) acc[i] = fmaf(a, p1[i], acc[i]);
+            for (int g = 0; g < NG; g++) a[u][g] = sc[(int64_t)(G == 128 ? kc >> 1 : NG * kc + g) * 32];
         }
-    }
+#pragma unroll
+        for (int u = 0; u < n; u++) {
+            raw[u][0] = raw[u][1] = typename Act<X>::raw{};
+            const int k = 64 * (k0 + u * NW) + 16 * h + 8 * e;
+            if (live) {
+                raw[u][0] = Act<X>::load(x + k, p.L.K - k);
+                raw[u][1] = Act<X>::load(x + k + 32, p.L.K - k - 32);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < n; u++) {
+            const f32x4 p0 = M::mma(Act<X>::frag(raw[u][0]), M::decode(q[u].x), f32x4{0, 0, 0, 0});
+            const f32x4 p1 = M::mma(Act<X>::frag(raw[u][1]), M::decode(q[u].y), NG == 2 ? f32x4{0, 0, 0, 0} : p0);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if (NG == 2) acc[i] = fmaf(scale_value(a[u][0]), p0[i], acc[i]);
+                acc[i] = fmaf(scale_value(a[u][NG - 1]), p1[i], acc[i]);
+            }
+        }
+    };
+    int kc = wave;
+    for (; kc + (U - 1) * NW < p.L.chunks; kc += U * NW) go(kc, std::integral_constant<int, U>{});
+    for (; kc < p.L.chunks; kc += NW) go(kc, std::integral_constant<int, 1>{});
     red[wave][lane] = acc;
     __syncthreads();
     if (wave) return;
@@ -152,72 +170,8 @@ __global__ __launch_bounds__(64 * NW) void k_w4_token(W4GemmParams p) {
     with_y(p, [&](auto* y) {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const int64_t m = m0 + 4 * s + i;
+            const int64_t m = 4 * s + i;
             if (m < p.M) y[m * p.ldy + n] = p.x_scale ? acc[i] * p.x_scale[m] : acc[i];
-        }
-    });
-}
-
-// 32 outputs n x 32 MT rows m per workgroup, the column chunks dealt to its NW waves; each wave then
-// adds its share of the sums of all, in wave order.
-template <typename X, int G, int MT, int NW>
-__global__ __launch_bounds__(64 * NW) void k_w4_batch(W4GemmParams p) {
-    typedef typename Act<X>::M M;
-    __shared__ float red[NW][MT * 16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
-    const int nt = blockIdx.x;
-    const int64_t m0 = (int64_t)blockIdx.y * 32 * MT;
-    const X* x[MT];
-    bool live[MT];
-#pragma unroll
-    for (int i = 0; i < MT; i++) {
-        live[i] = m0 + 32 * i + r < p.M;
-        x[i] = (const X*)p.x + (live[i] ? m0 + 32 * i + r : 0) * p.ldx;
-    }
-    const uint8_t* w = p.w4 + (int64_t)nt * p.L.chunks * 1024 + 16 * lane;
-    const uint16_t* sc = (const uint16_t*)(p.w4 + p.L.scale_offset) + (int64_t)nt * p.L.groups * 32 + r;
-    f32x16 acc[MT] = {};
-    for (int kc = wave; kc < p.L.chunks; kc += NW) {
-        const uint4 q = *(const uint4*)(w + (int64_t)kc * 1024);
-        typename Act<X>::raw raw[MT][4] = {};
-        const int k = 64 * kc + 8 * h;
-#pragma unroll
-        for (int i = 0; i < MT; i++)
-            if (live[i])
-#pragma unroll
-                for (int t = 0; t < 4; t++) raw[i][t] = Act<X>::load(x[i] + k + 16 * t, p.L.K - k - 16 * t);
-        const typename M::frag wf[4] = {M::decode(q.x), M::decode(q.z), M::decode(q.y), M::decode(q.w)};
-        constexpr int NG = G == 32 ? 2 : 1;
-        float a[NG];
-#pragma unroll
-        for (int g = 0; g < NG; g++) a[g] = scale_value(sc[(int64_t)(G == 128 ? kc >> 1 : NG * kc + g) * 32]);
-#pragma unroll
-        for (int i = 0; i < MT; i++)
-#pragma unroll
-            for (int g = 0; g < NG; g++) {
-                f32x16 part = {};
-#pragma unroll
-                for (int t = 0; t < 4 / NG; t++)
-                    part = M::mma(Act<X>::frag(raw[i][4 / NG * g + t]), wf[4 / NG * g + t], part);
-#pragma unroll
-                for (int j = 0; j < 16; j++) acc[i][j] = fmaf(a[g], part[j], acc[i][j]);
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; i++)
-#pragma unroll
-        for (int j = 0; j < 16; j++) red[wave][16 * i + j][lane] = acc[i][j];
-    __syncthreads();
-    const int n = 32 * nt + r;
-    if (n >= p.L.N) return;
-    with_y(p, [&](auto* y) {
-        for (int j = wave; j < 16 * MT; j += NW) {
-            const int64_t m = m0 + 32 * (j >> 4) + 8 * ((j >> 2) & 3) + 4 * h + (j & 3);
-            if (m >= p.M) continue;
-            float v = red[0][j][lane];
-#pragma unroll
-            for (int u = 1; u < NW; u++) v += red[u][j][lane];
-            y[m * p.ldy + n] = p.x_scale ? v * p.x_scale[m] : v;
         }
     });
 }
@@ -232,245 +186,467 @@ __device__ __forceinline__ int xcd_run(int id, int total) {
 }
 
 // Tiles of BM = 32 TM WM rows m x BN = 64 WN outputs n, a wave of the workgroup 32 TM x 64 of it.
-// A step is 128 bytes of every row of the tile in LDS: 64 columns of 16-bit values (F8 == 0; E4M3
-// activations become bf16 on their way) or 128 columns of E4M3 (F8 == 1).  16-byte piece c of row i
-// is at c ^ ((i / 2) % 8) of its row, so that the 16 rows which one quarter of a wave reads at a time
-// lie in different banks.  While a step's MFMAs run, the next step's weights and the activations of
-// the one after it are on their way to registers.
-template <typename X, int F8, int G, int TM, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int tiles_m, int tiles) {
+// A step is 128 bytes of every row of the tile: 64 columns of 16-bit values (F8 == 0; E4M3 activations
+// become bf16 on their way) or 128 columns of E4M3 (F8 == 1), and the weights and scales of these
+// columns.  All of it lies in a ring of R stages in LDS, fetched R - 1 steps ahead by DMA, which holds
+// no registers; activations that DMA cannot take (DMA == 0: rows that are not 16-byte aligned, or that
+// need the conversion) go through registers one step ahead.
+//
+// 16-byte piece c of row i is at c ^ ((i / 2) % 8) of its row, so that the 16 rows which one quarter of
+// a wave reads at a time lie in different banks.  One barrier per step.  A step's products go group by
+// group and tile by tile: the MFMAs of one (tile, group) are issued, then the sums of an earlier one
+// are scaled and added under them.
+//
+// F8: within one instruction, products below 2^-13 of its largest are dropped (measured with single
+// instructions).  Of 128 products of E4M3 rows that is at most 2^-6 and in practice some 10^-4 of
+// their root mean square: under the rounding of a 16-bit output (2^-9, 2^-12), so fp32 outputs
+// take the bf16 MFMAs, which keep every product.
+__device__ __align__(16) const uint8_t kZero16[16] = {0};
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
+__device__ __forceinline__ void dma16(const void* g, uint8_t* wave_base) {
+    __builtin_amdgcn_global_load_lds((global_void*)g, (lds_void*)wave_base, 16, 0, 0);
+}
+__device__ __forceinline__ void dma4(const void* g, uint8_t* wave_base) {
+    __builtin_amdgcn_global_load_lds((global_void*)g, (lds_void*)wave_base, 4, 0, 0);
+}
+// s_waitcnt vmcnt(N), the other counters at their maxima.
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+// Barrier for LDS alone: DMAs stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0), seen by the compiler's own tracking
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+template <typename X, int F8, int G, int TM, int WM, int WN, int R, int DMA>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int tiles_m, int tiles, int per_split) {
     typedef typename Act<X>::M M;
-    constexpr int T = 64 * WM * WN, BM = 32 * TM * WM;
+    typedef typename Act<X>::raw Raw;
+    typedef typename FragOf<F8, typename M::frag>::type Frag;
+    constexpr int NW = WM * WN, T = 64 * NW, BM = 32 * TM * WM;
     constexpr int BK = F8 ? 128 : 64, EP = F8 ? 16 : 8;       // columns of a step, of a piece
-    constexpr int P = BM * 8 / T;                             // pieces of a thread
     constexpr int NC = F8 ? 2 : 1;                            // column chunks of a step
     constexpr int NG = F8 ? 128 / G : G == 32 ? 2 : 1;        // scales of a step
-    __shared__ __align__(16) uint8_t lds[2][BM * 128];
+    constexpr int NX = BM / (8 * NW), NT = 2 * WN * NC / NW;  // DMAs of a wave: rows, weight tiles
+    static_assert(NX * 8 * NW == BM && NT * NW == 2 * WN * NC, "whole DMAs per wave");
+    constexpr int PER = (DMA ? NX : 0) + NT + 1;
+    constexpr int XB = BM * 128, WB = 2 * WN * NC * 1024, STAGE = XB + WB + 256 * NW;
+    constexpr int GM = 4;                                     // tiles of rows in a band
+    constexpr int SLAB = 68;                                  // floats of a slab's row
+    static_assert(NW * 32 * SLAB * 4 <= R * STAGE, "the slabs fit the ring");
+    __shared__ __align__(16) uint8_t ring[R * STAGE];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const int t = xcd_run(blockIdx.x, tiles);
-    const int64_t m0 = (int64_t)(t % tiles_m) * BM;
-    const int nt0 = (t / tiles_m) * (2 * WN) + 2 * wn;
+    // A run of tiles goes through bands of up to GM tiles of rows, n by n: the workgroups of an XCD that
+    // run together then share few rows and few columns, and its L2 fetches each once.
+    const int id = xcd_run(blockIdx.x, gridDim.x), z = id / tiles, t = id - z * tiles, tiles_n = tiles / tiles_m;
+    const int band = t / (GM * tiles_n), in_band = t - band * GM * tiles_n, high = min(GM, tiles_m - band * GM);
+    const int64_t m0 = (int64_t)(band * GM + in_band % high) * BM;
+    const int nt0 = in_band / high * (2 * WN);
     const int K = p.L.K, chunks = p.L.chunks, steps = (chunks + NC - 1) / NC;
+    const int first = z * per_split, end = min(first + per_split, steps);
 
-    // this thread's pieces: piece tid % 8 of rows tid / 8 + i T / 8
-    const int pc = tid & 7, pr = tid >> 3;
-    const X* xp[P];
-    uint32_t at[P];
+    // Rows: DMA i of the wave serves rows 8 (wave + i NW) + lane / 8 and writes slot lane % 8 of each,
+    // so it fetches piece (lane % 8) ^ (row / 2 % 8).  Through registers, the same rows and pieces.
+    const X* xp[NX];
+    const int pc = (lane & 7) ^ (((8 * wave + (lane >> 3)) >> 1) & 7);      // 8 NW is a multiple of 16
+    static_assert(NW % 2 == 0, "the swizzle of a lane's rows is the same");
 #pragma unroll
-    for (int i = 0; i < P; i++) {
-        const int row = pr + i * (T / 8);
-        const int64_t m = m0 + row < p.M ? m0 + row : p.M - 1;
-        xp[i] = (const X*)p.x + m * p.ldx + EP * pc;
-        at[i] = row * 128;
+    for (int i = 0; i < NX; i++) {
+        const int64_t m = m0 + 8 * (wave + i * NW) + (lane >> 3);
+        xp[i] = (const X*)p.x + (m < p.M ? m : p.M - 1) * p.ldx + EP * pc;
     }
-    typedef typename Act<X>::raw Raw;
-    Raw st[P][F8 ? 2 : 1];
-    auto fetch = [&](int s) {
+    // Weight tiles wave + i NW of the stage's [row tile][chunk]; rows of tiles past N read the last.
+    const uint8_t* wp[NT];
+#pragma unroll
+    for (int i = 0; i < NT; i++) {
+        const int q = wave + i * NW;
+        wp[i] = p.w4 + ((int64_t)min(nt0 + q / NC, p.L.tiles - 1) * chunks + q % NC) * 1024 + 16 * lane;
+    }
+    // The wave's own scales, [row tile j][group g of the step][32 rows], 16 lanes each.
+    const int sj = (lane >> 4) / NG & 1, sg = (lane >> 4) % NG;
+    const uint8_t* sp = p.w4 + p.L.scale_offset +
+                        (int64_t)min(nt0 + 2 * wn + sj, p.L.tiles - 1) * p.L.groups * 64 + 4 * (lane & 15);
+
+    // every stage issues the same number of DMAs, also past the last step
+    auto fetch = [&](int s, uint8_t* slot) {
+        if constexpr (DMA) {
+            const bool in = s * BK + EP * pc < K;
+#pragma unroll
+            for (int i = 0; i < NX; i++)
+                dma16(in ? (const void*)(xp[i] + s * BK) : (const void*)kZero16, slot + 1024 * (wave + i * NW));
+        }
+#pragma unroll
+        for (int i = 0; i < NT; i++) {
+            const bool in = s * NC + (wave + i * NW) % NC < chunks;
+            dma16(in ? (const void*)(wp[i] + (int64_t)s * (NC * 1024)) : (const void*)kZero16,
+                    slot + XB + 1024 * (wave + i * NW));
+        }
+        const int gi = min(F8 || G < 128 ? NG * s + sg : s >> 1, p.L.groups - 1);
+        dma4(sp + (int64_t)gi * 64, slot + XB + WB + 256 * wave);
+    };
+    Raw st[DMA ? 1 : NX][F8 ? 2 : 1];
+    auto load = [&](int s) {
         const int k = s * BK;
         if (k + BK <= K) {
 #pragma unroll
-            for (int i = 0; i < P; i++)
+            for (int i = 0; i < NX; i++)
 #pragma unroll
                 for (int u = 0; u < (F8 ? 2 : 1); u++) st[i][u] = Act<X>::load(xp[i] + k + 8 * u, 8);
         } else {
 #pragma unroll
-            for (int i = 0; i < P; i++)
+            for (int i = 0; i < NX; i++)
 #pragma unroll
                 for (int u = 0; u < (F8 ? 2 : 1); u++)
                     st[i][u] = Act<X>::load(xp[i] + k + 8 * u, K - k - EP * pc - 8 * u);
         }
     };
-    auto put = [&](int b) {
+    auto put = [&](uint8_t* slot) {
 #pragma unroll
-        for (int i = 0; i < P; i++) {
-            const int sw = ((pr + i * (T / 8)) >> 1) & 7;
+        for (int i = 0; i < NX; i++) {
+            uint8_t* d = slot + 1024 * (wave + i * NW) + 16 * lane;
             if constexpr (F8) {
-                // The instruction pairs 8-bit lane half h, 16-byte piece c with 4-bit lane half c, words
-                // 2h and 2h + 1, which hold columns 16t + 8c .. + 7 of t = h and h + 2.
-                const int u = pc >> 2, tt = pc & 3;
-#pragma unroll
-                for (int c = 0; c < 2; c++)
-                    *(Raw*)(lds[b] + at[i] + 16 * ((4 * u + 2 * (tt & 1) + c) ^ sw) + 8 * (tt >> 1)) = st[i][c];
+                *(Raw*)d = st[i][0];
+                *(Raw*)(d + 8) = st[i][1];
             } else {
-                *(typename M::frag*)(lds[b] + at[i] + 16 * (pc ^ sw)) = Act<X>::frag(st[i][0]);
+                *(typename M::frag*)d = Act<X>::frag(st[i][0]);
             }
         }
     };
 
-    const uint8_t* wp[2];
-    const uint16_t* sp[2];
-#pragma unroll
-    for (int j = 0; j < 2; j++) {
-        const int nt = min(nt0 + j, p.L.tiles - 1);
-        wp[j] = p.w4 + (int64_t)nt * chunks * 1024 + 16 * lane;
-        sp[j] = (const uint16_t*)(p.w4 + p.L.scale_offset) + (int64_t)nt * p.L.groups * 32 + r;
-    }
-    uint4 wq[2][NC];
-    uint16_t ws[2][NG];
-    auto weights = [&](int s) {
-#pragma unroll
-        for (int j = 0; j < 2; j++) {
-#pragma unroll
-            for (int c = 0; c < NC; c++)
-                wq[j][c] = NC == 1 || NC * s + c < chunks ? *(const uint4*)(wp[j] + (int64_t)(NC * s + c) * 1024)
-                                                          : uint4{0, 0, 0, 0};
-#pragma unroll
-            for (int g = 0; g < NG; g++) {
-                const int gi = F8 ? min(NG * s + g, p.L.groups - 1) : G == 128 ? s >> 1 : NG * s + g;
-                ws[j][g] = sp[j][(int64_t)gi * 32];
-            }
-        }
-    };
-
-    // A step's products go group by group and tile by tile: the MFMAs of one (tile, group) are issued,
-    // then the sums of the one before it are scaled and added under them.
     f32x16 acc[TM][2] = {};
     const uint32_t arow = (uint32_t)(wm * 32 * TM + r) * 128;
     const int swz = (r >> 1) & 7;
     constexpr int NF = F8 ? 2 : 4;      // MFMAs of a tile in a step
-    constexpr int U = TM * 2 * NG;
-    auto step = [&](int b, int next) {
-        typedef typename FragOf<F8, typename M::frag>::type Frag;
+    // two behind where the registers allow, so that no sum is waited for
+    constexpr int U = TM * 2 * NG, LAG = TM == 4 && !(F8 && G == 128) ? 1 : 2;
+    auto step = [&](const uint8_t* slot) {
         float a[2][NG];
         Frag wf[2][NF], x[NF];
 #pragma unroll
         for (int j = 0; j < 2; j++) {
-#pragma unroll
-            for (int g = 0; g < NG; g++) a[j][g] = scale_value(ws[j][g]);
+            const uint8_t* wb = slot + XB + (2 * wn + j) * (NC * 1024) + 16 * lane;
             if constexpr (F8) {
 #pragma unroll
-                for (int c = 0; c < NC; c++)
-                    wf[j][c] = i32x8{(int)wq[j][c].x, (int)wq[j][c].y, (int)wq[j][c].z, (int)wq[j][c].w, 0, 0, 0, 0};
-            } else {
-                wf[j][0] = M::decode(wq[j][0].x);
-                wf[j][1] = M::decode(wq[j][0].z);
-                wf[j][2] = M::decode(wq[j][0].y);
-                wf[j][3] = M::decode(wq[j][0].w);
-            }
-        }
-        if (next < steps) weights(next);
-        f32x16 part[2];
-#pragma unroll
-        for (int u = 0; u <= U; u++) {
-            if (u < U) {
-                const int i = u / (2 * NG), j = u / NG % 2, g = u % NG;
-                if (u % (2 * NG) == 0) {
-                    const uint8_t* base = lds[b] + arow + i * 32 * 128;
-#pragma unroll
-                    for (int c = 0; c < NF; c++) {
-                        if constexpr (F8) {
-                            const uint4 lo = *(const uint4*)(base + 16 * ((4 * c + 2 * h) ^ swz));
-                            const uint4 hi = *(const uint4*)(base + 16 * ((4 * c + 2 * h + 1) ^ swz));
-                            x[c] = i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w,
-                                         (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-                        } else {
-                            x[c] = *(const Frag*)(base + 16 * ((2 * c + h) ^ swz));
-                        }
-                    }
+                for (int c = 0; c < 2; c++) {
+                    const i32x4 q = *(const i32x4*)(wb + 1024 * c);
+                    wf[j][c] = i32x8{q[0], q[2], q[1], q[3], 0, 0, 0, 0};
                 }
+            } else {
+                const i32x4 q = *(const i32x4*)wb;
+                wf[j][0] = M::decode(q[0]);
+                wf[j][1] = M::decode(q[2]);
+                wf[j][2] = M::decode(q[1]);
+                wf[j][3] = M::decode(q[3]);
+            }
+#pragma unroll
+            for (int g = 0; g < NG; g++)
+                a[j][g] = scale_value(*(const uint16_t*)(slot + XB + WB + 256 * wave + 64 * (j * NG + g) + 2 * r));
+        }
+        auto rows = [&](int i) {
+            const uint8_t* base = slot + arow + i * 32 * 128;
+#pragma unroll
+            for (int c = 0; c < NF; c++) {
+                if constexpr (F8) {
+                    const i32x4 lo = *(const i32x4*)(base + 16 * ((4 * c + 2 * h) ^ swz));
+                    const i32x4 hi = *(const i32x4*)(base + 16 * ((4 * c + 2 * h + 1) ^ swz));
+                    x[c] = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                } else {
+                    x[c] = *(const Frag*)(base + 16 * ((2 * h + (c & 1) + 4 * (c >> 1)) ^ swz));
+                }
+            }
+        };
+        rows(0);
+        f32x16 part[LAG + 1];
+#pragma unroll
+        for (int u = 0; u < U + LAG; u++) {
+            if (u < U) {
+                const int j = u / NG % 2, g = u % NG;
                 f32x16 d = {};
 #pragma unroll
                 for (int c = NF / NG * g; c < NF / NG * (g + 1); c++) {
                     if constexpr (F8) d = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[c], wf[j][c], d, 0, 4, 0, 127, 0, 127);
                     else d = M::mma(x[c], wf[j][c], d);
                 }
-                part[u & 1] = d;
+                part[u % (LAG + 1)] = d;
+                if ((u + 1) % (2 * NG) == 0 && u + 1 < U) rows((u + 1) / (2 * NG));
             }
-            if (u > 0) {
-                const int v = u - 1, i = v / (2 * NG), j = v / NG % 2, g = v % NG;
+            if (u >= LAG) {
+                const int v = u - LAG, i = v / (2 * NG), j = v / NG % 2, g = v % NG;
 #pragma unroll
-                for (int q = 0; q < 16; q++) acc[i][j][q] = fmaf(a[j][g], part[v & 1][q], acc[i][j][q]);
+                for (int q = 0; q < 16; q++) acc[i][j][q] = fmaf(a[j][g], part[v % (LAG + 1)][q], acc[i][j][q]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
 
-    if (steps > 0) {
-        fetch(0);
-        put(0);
-        fetch(1);
-        weights(0);
-        __syncthreads();
-        for (int s = 0; s < steps; s++) {
-            if (s + 1 < steps) put((s + 1) & 1);
-            if (s + 2 < steps) fetch(s + 2);
-            step(s & 1, s + 1);
-            __syncthreads();
+    if (first < end) {
+        // stage first + s in slot s % R
+        if constexpr (!DMA) {
+            load(first);
+            put(ring);
+            load(first + 1);
         }
+#pragma unroll
+        for (int q = 0; q < R - 1; q++) fetch(first + q, ring + q * STAGE);
+        int cur = 0, last = R - 1;           // slots of this step and of the one before it
+        for (int s = first; s < end; s++) {
+            vm_wait<(R - 2) * PER>();        // this wave's part of stage s has landed
+            lds_barrier();                   // all of it; every read of the last step is done
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(s + R - 1, ring + last * STAGE);
+            if constexpr (!DMA) {
+                put(ring + (cur + 1 == R ? 0 : cur + 1) * STAGE);
+                load(s + 2);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            step(ring + cur * STAGE);
+            last = cur;
+            cur = cur + 1 == R ? 0 : cur + 1;
+        }
+        vm_wait<0>();                        // no DMA outlives its workgroup
     }
 
-    with_y(p, [&](auto* y) {
+    // Outputs, 32 rows at a time through a slab of LDS of each wave's own: lanes hold columns, stores
+    // want rows of 16-byte pieces.
+    __syncthreads();
+    float* slab = (float*)(ring + wave * (32 * SLAB * 4));
+    // f(row m, first column n, eight values): every lane, column n may lie past the last
+    auto outputs = [&](auto f) {
 #pragma unroll
-        for (int i = 0; i < TM; i++)
+        for (int i = 0; i < TM; i++) {
 #pragma unroll
-            for (int q = 0; q < 16; q++) {
-                const int64_t m = m0 + wm * 32 * TM + 32 * i + 8 * (q >> 2) + 4 * h + (q & 3);
-                if (m >= p.M) continue;
-                const float s = p.x_scale ? p.x_scale[m] : 1.0f;
+            for (int q = 0; q < 16; q++)
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const int n = 32 * (nt0 + j) + r;
-                    if (n < p.L.N) y[m * p.ldy + n] = s * acc[i][j][q];
-                }
+                for (int j = 0; j < 2; j++)
+                    slab[(8 * (q >> 2) + 4 * h + (q & 3)) * SLAB + 32 * j + r] = acc[i][j][q];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int row = 8 * e + (lane >> 3);
+                const f32x4 lo = *(const f32x4*)(slab + row * SLAB + 8 * (lane & 7));
+                const f32x4 hi = *(const f32x4*)(slab + row * SLAB + 8 * (lane & 7) + 4);
+                const int64_t m = m0 + wm * 32 * TM + 32 * i + row;
+                if (m < p.M) f(m, 32 * (nt0 + 2 * wn) + 8 * (lane & 7), f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
             }
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    if (p.part) {
+        const int64_t np = 32 * (int64_t)p.L.tiles;
+        outputs([&](int64_t m, int n, f32x8 v) {
+            if (n < np) *(f32x8*)(p.part + ((int64_t)z * p.M + m) * np + n) = v;
+        });
+        return;
+    }
+    with_y(p, [&](auto* y) {
+        typedef std::remove_reference_t<decltype(*y)> Y;
+        outputs([&](int64_t m, int n, f32x8 v) {
+            if (p.x_scale) v *= p.x_scale[m];
+            if (n < p.L.N) store8(y + m * p.ldy + n, __builtin_convertvector(v, typename Vec8<Y>::type), p.L.N - n);
+        });
     });
 }
 
-template <typename X, int F8, int G, int TM, int WM, int WN>
-hipError_t launch_tile(const W4GemmParams& p, hipStream_t s) {
+// y from the sums of the column ranges, added in order.
+__global__ __launch_bounds__(256) void k_w4_sum(W4GemmParams p, int splits) {
+    const int64_t np = 32 * (int64_t)p.L.tiles, cols = np / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.M * cols) return;
+    const int64_t m = i / cols;
+    const int n = 8 * (int)(i - m * cols);
+    const float* q = p.part + m * np + n;
+    f32x8 v = *(const f32x8*)q;
+    for (int z = 1; z < splits; z++) v += *(const f32x8*)(q + z * p.M * np);
+    if (p.x_scale) v *= p.x_scale[m];
+    if (n >= p.L.N) return;
+    with_y(p, [&](auto* y) {
+        typedef std::remove_reference_t<decltype(*y)> Y;
+        store8(y + m * p.ldy + n, __builtin_convertvector(v, typename Vec8<Y>::type), p.L.N - n);
+    });
+}
+
+template <typename X, int F8, int G, int TM, int WM, int WN, int R>
+hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
     const int tm = (int)((p.M + 32 * TM * WM - 1) / (32 * TM * WM)), tn = (p.L.tiles + 2 * WN - 1) / (2 * WN);
-    k_w4_tile<X, F8, G, TM, WM, WN><<<tm * tn, 64 * WM * WN, 0, s>>>(p, tm, tm * tn);
-    return hipGetLastError();
+    const int es = sizeof(X), steps = F8 ? (p.L.chunks + 1) / 2 : p.L.chunks;
+    const int gm = 4;
+    const int per = (steps + splits - 1) / splits;
+    splits = (steps + per - 1) / per;
+    W4GemmParams q = p;
+    if (splits <= 1) q.part = nullptr;
+    const bool aligned = (uintptr_t)p.x % 16 == 0 && p.ldx * es % 16 == 0 && (int64_t)p.L.K * es % 16 == 0;
+    const unsigned grid = (unsigned)tm * tn * splits;
+    if ((F8 || es == 2) && aligned)
+        k_w4_tile<X, F8, G, TM, WM, WN, R, F8 || sizeof(X) == 2><<<grid, 64 * WM * WN, 0, s>>>(q, tm, tm * tn, gm, per);
+    else
+        k_w4_tile<X, F8, G, TM, WM, WN, R, 0><<<grid, 64 * WM * WN, 0, s>>>(q, tm, tm * tn, gm, per);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && splits > 1) {
+        k_w4_sum<<<(unsigned)((p.M * p.L.tiles * 4 + 255) / 256), 256, 0, s>>>(p, splits);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+// The shapes of k_w4_tile and what a step costs, us on one CU holding 1 .. slots of its workgroups
+// (measured with the rows in DMA, G = 128: 256, 512, .. workgroups, K = 4096 and 9216).  Small tiles
+// spread few rows over the chip, large ones read less per product.
+struct TileShape {
+    int bm, bn, slots;
+    float step[3];
+};
+constexpr TileShape kShapes16[4] = {{32, 256, 3, {0.41f, 0.63f, 0.85f}},
+                                    {64, 256, 2, {0.615f, 1.025f}},
+                                    {128, 256, 1, {1.03f}},
+                                    {128, 256, 2, {1.10f, 1.96f}}};
+constexpr TileShape kShapes8[4] = {{32, 256, 1, {0.42f}},
+                                   {64, 128, 2, {0.44f, 0.60f}},
+                                   {128, 256, 1, {1.0f}},
+                                   {128, 256, 2, {0.97f, 1.72f}}};
+
+// The shape and the ranges of columns (splits) that should take the least time: rounds of full CUs,
+// then one of what is left; splits write and read fp32 sums at about 4 TB/s and launch one more kernel.
+// DMA == 0 has two shapes.  part: whether there is room for the sums of two ranges or more.
+struct TilePlan {
+    int shape, splits;
+};
+TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, bool part) {
+    const int steps = f8 ? (L.chunks + 1) / 2 : L.chunks;
+    const double cus = num_cus();
+    TilePlan best = {0, 1};
+    double least = 1e30;
+    // the last shape's registers do not hold two scales per step of its 128 x 64 waves
+    const int shapes = !dma ? 2 : L.group == 32 ? 3 : 4;
+    for (int v = 0; v < shapes; v++) {
+        const TileShape& s = f8 ? kShapes8[v] : kShapes16[v];
+        const double tiles = (double)((M + s.bm - 1) / s.bm) * ((L.N + s.bn - 1) / s.bn);
+        for (int z : {1, 2, 3, 4, 6, 8}) {
+            if (z > 1 && (!part || steps < 4 * z)) break;
+            const double held = ceil(tiles * z / cus), rounds = floor((held - 1) / s.slots);
+            const int rest = (int)(held - rounds * s.slots);
+            double us = (rounds * s.step[s.slots - 1] + s.step[rest - 1]) * ceil((double)steps / z);
+            if (z > 1) us += 3.5 + z * (double)M * L.tiles * 32 * 8 / 4e6;
+            if (us < least) {
+                least = us;
+                best = {v, z};
+            }
+        }
+    }
+    return best;
+}
+
+constexpr int64_t kRowsOfALaunch = 1 << 17;     // tiles of one launch stay below 2^31
+
+// Whether products of E4M3 rows take the mixed MFMA: its dropped small products (k_w4_tile) stay below
+// the rounding of a 16-bit output, not of fp32, and it covers groups of 64 at least.
+bool takes_f8(int x_type, int y_type, int group) { return x_type == kE4M3 && y_type != kF32 && group >= 64; }
+// Whether the rows can be fetched by DMA, 16-byte pieces in place; E4M3 for the bf16 MFMAs needs the
+// conversion on its way.
+bool takes_dma(const W4GemmParams& p, int x_type, bool f8) {
+    const int es = x_type == kE4M3 ? 1 : 2;
+    return (f8 || es == 2) && (uintptr_t)p.x % 16 == 0 && p.ldx * es % 16 == 0 && (int64_t)p.L.K * es % 16 == 0;
+}
+
+template <typename X, int F8, int G, int TM, int WM, int WN, int R, int DMA>
+hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
+    const int tm = (int)((p.M + 32 * TM * WM - 1) / (32 * TM * WM)), tn = (p.L.tiles + 2 * WN - 1) / (2 * WN);
+    const int steps = F8 ? (p.L.chunks + 1) / 2 : p.L.chunks, per = steps ? (steps + splits - 1) / splits : 0;
+    splits = steps ? (steps + per - 1) / per : 1;
+    W4GemmParams q = p;
+    if (splits == 1) q.part = nullptr;
+    k_w4_tile<X, F8, G, TM, WM, WN, R, DMA><<<(unsigned)(tm * tn * splits), 64 * WM * WN, 0, s>>>(q, tm, tm * tn, per);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && splits > 1) {
+        k_w4_sum<<<(unsigned)((p.M * p.L.tiles * 4 + 255) / 256), 256, 0, s>>>(p, splits);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+template <typename X, int F8, int G>
+hipError_t launch_shape(const W4GemmParams& p, int x_type, hipStream_t s) {
+    const bool dma = takes_dma(p, x_type, F8);
+    const TilePlan t = tile_plan(p.M, p.L, F8, dma, p.part != nullptr);
+    if constexpr (F8 || sizeof(X) == 2) {
+        if (dma) {
+            if (t.shape == 0) return launch_tile<X, F8, G, 1, 1, 4, 4, 1>(p, t.splits, s);
+            if (t.shape == 1) {
+                if constexpr (F8) return launch_tile<X, F8, G, 1, 2, 2, 4, 1>(p, t.splits, s);
+                else return launch_tile<X, F8, G, 2, 1, 4, 4, 1>(p, t.splits, s);
+            }
+            if (t.shape == 2) return launch_tile<X, F8, G, 2, 2, 4, 4, 1>(p, t.splits, s);
+            if constexpr (G > 32) return launch_tile<X, F8, G, 4, 1, 4, F8 ? 2 : 3, 1>(p, t.splits, s);
+        }
+    }
+    if (t.shape == 0) return launch_tile<X, F8, G, 1, 1, 4, 4, 0>(p, t.splits, s);
+    if constexpr (F8) return launch_tile<X, F8, G, 1, 2, 2, 4, 0>(p, t.splits, s);
+    else return launch_tile<X, F8, G, 2, 1, 4, 4, 0>(p, t.splits, s);
+}
+
+// A token's kernel reads the weights once, without LDS; it also reads every row in pieces, so that with
+// many weights and more than a few rows the tiles are faster (18432 x 4096: 8 rows 17.3 against 15.5 us,
+// 16 rows 23.5 against 16.2; 4096 x 9216, 16 rows: 12.8 against 16.4).
+bool takes_token(int64_t M, const W4Layout& L) {
+    return M <= 4 || (M <= 16 && (int64_t)L.N * L.K <= (int64_t)48 << 20);
 }
 
 template <typename X, int G>
-hipError_t launch_g(const W4GemmParams& p, hipStream_t s) {
-    if (p.M <= 16) {
-        const dim3 grid(2 * p.L.tiles, (unsigned)((p.M + 15) / 16));
-        k_w4_token<X, G, 8><<<grid, 512, 0, s>>>(p);
+hipError_t launch_g(const W4GemmParams& p, int x_type, hipStream_t s) {
+    if (takes_token(p.M, p.L)) {
+        // 16 waves where the row tiles leave CUs with one workgroup at most, else 8 with few registers
+        const unsigned grid = 2 * p.L.tiles;
+        if ((int)grid <= num_cus() * 3 / 2) k_w4_token<X, G, 16, 4><<<grid, 1024, 0, s>>>(p);
+        else k_w4_token<X, G, 8, 1><<<grid, 512, 0, s>>>(p);
         return hipGetLastError();
     }
-    const int64_t t128 = (p.M + 127) / 128 * ((p.L.N + 127) / 128);
-    if (p.M <= 64 || t128 < num_cus() / 2) {
-        if (p.M <= 32) {
-            const dim3 grid(p.L.tiles, (unsigned)((p.M + 31) / 32));
-            k_w4_batch<X, G, 1, 8><<<grid, 512, 0, s>>>(p);
-        } else {
-            const dim3 grid(p.L.tiles, (unsigned)((p.M + 63) / 64));
-            k_w4_batch<X, G, 2, 8><<<grid, 512, 0, s>>>(p);
-        }
-        return hipGetLastError();
-    }
-    // dropped small products (k_w4_tile) stay below the rounding of a 16-bit output, not of fp32
     if constexpr (sizeof(X) == 1 && G >= 64) {
-        if (p.y_type != kF32) return launch_tile<X, 1, G, 2, 2, 2>(p, s);
+        if (takes_f8(x_type, p.y_type, G)) return launch_shape<X, 1, G>(p, x_type, s);
     }
-    return launch_tile<X, 0, G, 2, 2, 2>(p, s);
+    return launch_shape<X, 0, G>(p, x_type, s);
 }
 
 template <typename X>
-hipError_t launch_x(const W4GemmParams& p, hipStream_t s) {
-    if (p.L.group == 32) return launch_g<X, 32>(p, s);
-    if (p.L.group == 64) return launch_g<X, 64>(p, s);
-    return launch_g<X, 128>(p, s);
+hipError_t launch_x(const W4GemmParams& p, int x_type, hipStream_t s) {
+    if (p.L.group == 32) return launch_g<X, 32>(p, x_type, s);
+    if (p.L.group == 64) return launch_g<X, 64>(p, x_type, s);
+    return launch_g<X, 128>(p, x_type, s);
 }
 
 }  // namespace
 
+size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type) {
+    M = M < kRowsOfALaunch ? M : kRowsOfALaunch;
+    if (takes_token(M, L)) return 0;
+    size_t most = 0;
+    const bool f8 = takes_f8(x_type, y_type, L.group);
+    for (bool dma : {false, true}) {        // the call knows the alignment, its caller need not
+        const TilePlan t = tile_plan(M, L, f8, dma, true);
+        const size_t b = t.splits > 1 ? (size_t)t.splits * M * L.tiles * 32 * 4 : 0;
+        most = b > most ? b : most;
+    }
+    return most;
+}
+
 hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s) {
-    const int64_t most = 1 << 19;      // rows of one launch: the grid's second dimension
     const int xs = x_type == kE4M3 ? 1 : 2, ys = p.y_type == kF32 ? 4 : 2;
-    for (int64_t m = 0; m < p.M; m += most) {
+    for (int64_t m = 0; m < p.M; m += kRowsOfALaunch) {
         W4GemmParams q = p;
-        q.M = p.M - m < most ? p.M - m : most;
+        q.M = p.M - m < kRowsOfALaunch ? p.M - m : kRowsOfALaunch;
         q.x = (const char*)p.x + m * p.ldx * xs;
         if (p.x_scale) q.x_scale = p.x_scale + m;
         q.y = (char*)p.y + m * p.ldy * ys;
-        const hipError_t e = x_type == kBF16  ? launch_x<__bf16>(q, s)
-                             : x_type == kF16 ? launch_x<_Float16>(q, s)
-                                              : launch_x<uint8_t>(q, s);
+        const hipError_t e = x_type == kBF16  ? launch_x<__bf16>(q, x_type, s)
+                             : x_type == kF16 ? launch_x<_Float16>(q, x_type, s)
+                                              : launch_x<uint8_t>(q, x_type, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

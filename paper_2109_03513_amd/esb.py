@@ -131,7 +131,8 @@ def lib():
             "esb_w4_quantize": (i32, [P, i64, i32, i32, i32, i32, P, i32, P, sz, P]),
             "esb_w4_pack": (i32, [P, i64, P, i64, i32, i32, i32, P, sz, P]),
             "esb_w4_unpack": (i32, [P, i32, i32, i32, P, i64, P, i64, P]),
-            "esb_w4_gemm": (i32, [i32, i32, i32, i32, P, i64, i32, P, P, P, i64, i32, P]),
+            "esb_w4_gemm_workspace_size": (sz, [i32, i32, i32, i32, i32, i32]),
+            "esb_w4_gemm": (i32, [i32, i32, i32, i32, P, i64, i32, P, P, P, i64, i32, P, sz, P]),
             "esb_gemm_packed": (i32, [i32, i32, i32, P, i64, i32, i32, P, P, i32, i32, P, P, P, i64,
                                       P, sz, P]),
         }
@@ -849,9 +850,14 @@ def esb_w4_unpack(w4, N, K, group, values=None, alpha=None, stream=None):
     return values, alpha
 
 
-def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, stream=None):
+def esb_w4_gemm_workspace_size(M, N, K, group, x_type, y_type):
+    return int(lib().esb_w4_gemm_workspace_size(M, N, K, group, x_type, y_type))
+
+
+def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=None, stream=None):
     """y = x W^T for x (M x K: bf16, fp16, or float8_e4m3fn with x_scale, M fp32) and packed
-    weights W (N x K); y in y_dtype (None: x's type; bf16 for float8)."""
+    weights W (N x K); y in y_dtype (None: x's type; bf16 for float8).  workspace: at least
+    esb_w4_gemm_workspace_size() bytes; without one the call allocates what it needs from torch."""
     L = _lib or lib()
     tx = _type(x, "x", (ESB_F32, ESB_BF16, ESB_F16, ESB_E4M3))   # fp32: the library's refusal
     M, K, ldx = _matrix(x, "x")
@@ -867,8 +873,14 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, stream=None
         ldy = N
     else:
         ldy = _like(y, "y", (M, N), y_dtype or y.dtype, device)
+    ty = _type(y, "y", _FLOATS)
+    if workspace is None:
+        need = L.esb_w4_gemm_workspace_size(M, N, K, group, tx, ty)
+        if need:
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
+    wp, wb = _ws(workspace)
     st = L.esb_w4_gemm(M, N, K, group, x.data_ptr(), ldx, tx, _addr(x_scale), w4.data_ptr(),
-                       y.data_ptr(), ldy, _type(y, "y", _FLOATS), _stream(stream))
+                       y.data_ptr(), ldy, ty, wp, wb, _stream(stream))
     if st:
         raise EsbError("esb_w4_gemm", st)
     return y

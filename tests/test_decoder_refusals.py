@@ -85,13 +85,21 @@ def test_weights(L):
 
 
 def test_products(L):
-    def gemm(M=3, N=40, K=200, g=64, x=FAKE, ldx=200, t=BF16, s=None, w4=FAKE, y=FAKE, ldy=40, yt=BF16):
-        return L.esb_w4_gemm(M, N, K, g, x, ldx, t, s, w4, y, ldy, yt, None)
+    def gemm(M=3, N=40, K=200, g=64, x=FAKE, ldx=200, t=BF16, s=None, w4=FAKE, y=FAKE, ldy=40, yt=BF16,
+             ws=None, wb=0):
+        return L.esb_w4_gemm(M, N, K, g, x, ldx, t, s, w4, y, ldy, yt, ws, wb, None)
 
     assert gemm(t=F32) == UNSUPPORTED
     for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(g=0), dict(ldx=199), dict(ldy=39), dict(t=4),
                 dict(yt=E4M3), dict(x=None), dict(w4=None), dict(y=None), dict(x=ODD), dict(y=ODD), dict(s=ODD),
-                dict(w4=ctypes.c_void_p(0x1004))):
+                dict(w4=ctypes.c_void_p(0x1004)), dict(ws=ctypes.c_void_p(0x1010), wb=1 << 30)):
         assert gemm(**bad) == INVALID, bad
     assert gemm(N=(1 << 31) - 1, ldy=1 << 40) == UNSUPPORTED
     assert gemm(M=0, x=None, y=None) == 0 and gemm(N=0, y=None) == 0
+    size = L.esb_w4_gemm_workspace_size
+    need = size(64, 4096, 4096, 128, BF16, BF16)
+    assert need > 0 and need % (64 * 4096 * 4) == 0          # whole sets of fp32 sums
+    big = dict(M=64, N=4096, K=4096, g=128, ldx=4096, ldy=4096, ws=FAKE)
+    assert gemm(**big, wb=need - 1) == WORKSPACE
+    assert size(1, 4096, 4096, 128, BF16, BF16) == 0 and size(4096, 18432, 4096, 128, E4M3, BF16) == 0
+    assert size(64, 4096, 4096, 100, BF16, BF16) == 0 and size(64, 4096, 4096, 128, F32, BF16) == 0

@@ -107,8 +107,7 @@ def test_pack_layout_and_unpack(esb, N, K, group):
     words = raw[:1024 * tiles * chunks].view(np.uint32)
     n, k = np.meshgrid(np.arange(32 * tiles), np.arange(64 * chunks), indexing="ij")
     c = k % 64
-    t = c // 16
-    at = 256 * ((n // 32) * chunks + k // 64) + 4 * (32 * ((c // 8) % 2) + n % 32) + t // 2 + 2 * (t % 2)
+    at = 256 * ((n // 32) * chunks + k // 64) + 4 * (32 * ((c // 16) % 2) + n % 32) + c // 32 + 2 * ((c // 8) % 2)
     nib = (words[at] >> (4 * (c % 8)).astype(np.uint32)) & 15
     val = ref.LEVELS.numpy()[nib & 7] * np.where(nib & 8, -1.0, 1.0)
     np.testing.assert_array_equal(val[:N, :K], want.numpy())
