@@ -72,68 +72,206 @@ __device__ __forceinline__ int64_t scale_index(const W4Layout& L, const Owner& o
     return ((int64_t)o.nt * L.groups + g) * 32 + o.r;
 }
 
+// The quantizer's lanes hold four words (32 weights) each: of one tile for groups of 32 and 64, two
+// lanes to a row; of half a row tile and two tiles for groups of 128, four lanes to a row.
+template <int G>
+struct Share {
+    int r, h, nt, kc;    // row and half in the tile, row tile, chunk of this lane
+    int64_t n;
+    __device__ __forceinline__ bool own(const W4Layout& L) {
+        const int lane = threadIdx.x & 63;
+        const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+        const int pairs = (L.chunks + 1) / 2;
+        if (wave >= (G == 128 ? (int64_t)L.tiles * 2 * pairs : (int64_t)L.tiles * L.chunks)) return false;
+        if (G == 128) {
+            r = 16 * (int)(wave / pairs & 1) + (lane & 15);
+            nt = (int)(wave / pairs / 2);
+            kc = 2 * (int)(wave % pairs) + (lane >> 4 & 1);
+        } else {
+            r = lane & 31;
+            nt = (int)(wave / L.chunks);
+            kc = (int)(wave % L.chunks);
+        }
+        h = lane >> 5;
+        n = 32 * (int64_t)nt + r;
+        return true;
+    }
+    __device__ __forceinline__ int column(int i) const { return 64 * kc + 8 * (2 * h + (i & 1) + 4 * (i >> 1)); }
+};
+// Over the lanes of a row.
+template <int G, typename F>
+__device__ __forceinline__ uint32_t over_row(uint32_t v, F f) {
+    auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = f(s[0], s[1]);
+    if (G == 128) {
+        s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = f(s[0], s[1]);
+    }
+    return v;
+}
+template <int G>
+__device__ __forceinline__ float row_sum(float v) {
+    return __uint_as_float(over_row<G>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+
+// One group of a row's lanes, in any range of values: errors in fp64 from exact cell bounds.  Rare: it
+// reads the group's weights again rather than keep them.
+template <typename T, int G, int WG>
+__device__ __forceinline__ float search_exact(const Share<G>& o, const T* row, int K, int word, float top,
+                                              const float* factors, int nf) {
+    float alpha = __builtin_nanf("");
+    double least = __builtin_inf();
+    for (int c = 0; c < nf; c++) {
+        const float f = factors ? factors[c] : 1.0f;
+        const float a = bf16_round(fmaxf(top * f / 6.0f, kTiny));
+        if (!(f > 0.0f) || !(f < __builtin_inff())) continue;
+        double err = 0.0;
+#pragma unroll 1
+        for (int t = word; t < word + WG; t++) {
+            const int k = o.column(t);
+            const f32x8 x = __builtin_convertvector(load8(row + k, K - k), f32x8);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float aw = fabsf(x[i]);
+                const double e = (double)aw - (double)a * (double)code_value(magnitude_code(aw, a));
+                err += e * e;
+            }
+        }
+        err += __shfl_xor(err, 32);
+        if (G == 128) err += __shfl_xor(err, 16);
+        if (a < __builtin_inff() && err < least) {
+            least = err;
+            alpha = a;
+        }
+    }
+    return alpha;
+}
+
+// Eight values to E2M1 nibbles, rounded to nearest even, at most 6.
+__device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
+    uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[0] * by, x[1] * by, 1.0f, 0);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[2] * by, x[3] * by, 1.0f, 1);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[4] * by, x[5] * by, 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[6] * by, x[7] * by, 1.0f, 3);
+}
+
+// The search needs no exact codes: the error is continuous where a code changes, so a candidate's q is
+// the conversion to fp4 of w (1/alpha), and e = w - alpha q one fma.  The group is scaled by a power of
+// two that brings its largest weight into [1, 2), which keeps e^2 in range.  Sums of up to 128 squares
+// in 8 fp32 parts a lane are within 2^-20 of their value; a second candidate within 2^-18 of the least,
+// or candidates far below the weights, send the wave to search_exact (a few waves in a thousand).
+//
+// Codes: for 16-bit weights w / alpha is a tie or at least 2^-11 from one, so w (1/alpha) (1 + 2^-22)
+// rounds to the nearest value with ties up; 32-bit weights are compared with the exact bounds.
+//
+// Bound by the conversions to fp4 (a quarter of the fp32 rate, two values each): some 22 cycles of a
+// SIMD per 64 weights and candidate.
 template <typename T, int G>
 __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __restrict__ w, int64_t ldw,
                                                      const float* __restrict__ factors, int nf,
                                                      uint8_t* __restrict__ out) {
-    Owner o;
-    if (!own(L, &o)) return;
-    constexpr int WG = G / 16;      // words of a lane in one group
-    float v[8][8];
+    Share<G> o;
+    if (!o.own(L)) return;
+    constexpr int WG = G == 32 ? 2 : 4;      // words of a lane in one group
+    const int lane = threadIdx.x & 63;
+    const float fs = factors && lane < nf ? factors[lane] : 1.0f;
+    float v[32];
 #pragma unroll
-    for (int t = 0; t < 8; t++) {
-        const int k = column(o, t);
+    for (int t = 0; t < 4; t++) {
+        const int k = o.column(t);
         const f32x8 x = __builtin_convertvector(load8(w + o.n * ldw + k, o.n < L.N ? L.K - k : 0), f32x8);
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[t][i] = x[i];
+        for (int i = 0; i < 8; i++) v[8 * t + i] = x[i];
     }
-    uint32_t packed[8];
+    uint32_t packed[4];
     __bf16* scales = (__bf16*)(out + L.scale_offset);
 #pragma unroll
-    for (int g = 0; g < 8 / WG; g++) {
+    for (int g = 0; g < 4 / WG; g++) {
+        float* n = v + 8 * WG * g;
         uint32_t m = 0;
 #pragma unroll
-        for (int t = g * WG; t < (g + 1) * WG; t++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[t][i]) & 0x7fffffffu);
-        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+        for (int i = 0; i < 8 * WG; i++) m = max(m, __float_as_uint(n[i]) & 0x7fffffffu);
+        m = over_row<G>(m, [](uint32_t a, uint32_t b) { return max(a, b); });
         const float top = __uint_as_float(m);
-        float alpha = __builtin_nanf("");
-        double least = __builtin_inf();
-        for (int c = 0; c < nf; c++) {
-            const float f = factors ? factors[c] : 1.0f;
-            const float a = bf16_round(fmaxf(top * f / 6.0f, kTiny));
-            if (!(f > 0.0f) || !(top < __builtin_inff()) || !(a < __builtin_inff())) continue;
-            double err = 0.0;
+        const bool finite = m < 0x7f800000u;
+
+        // 2^-shift brings the largest weight into [1, 2)
+        const int shift = finite && m ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
 #pragma unroll
-            for (int t = g * WG; t < (g + 1) * WG; t++)
+        for (int i = 0; i < 8 * WG; i++) n[i] = finite ? __builtin_amdgcn_ldexpf(n[i], -shift) : 0.0f;
+        float alpha = __builtin_nanf(""), least = __builtin_inff(), second = __builtin_inff();
+        bool far = false;
+        for (int c = 0; c < nf; c++) {
+            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fs), c));
+            if (!(f > 0.0f) || !(f < __builtin_inff())) continue;
+            const float a = bf16_round(fmaxf(top * f / 6.0f, kTiny));
+            const float as = m ? __builtin_amdgcn_ldexpf(a, -shift) : 1.0f;
+            const float inv = __builtin_amdgcn_rcpf(as);
+            far |= as < 0x1p-100f;
+            float sum[8] = {};
+#pragma unroll
+            for (int t = 0; t < WG; t++) {
+                const float* x = n + 8 * t;
+                const uint32_t q = to_e2m1(x, inv);
+                const auto d0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0);
+                const auto d1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1);
+                const auto d2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2);
+                const auto d3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3);
+                const float d[8] = {d0[0], d0[1], d1[0], d1[1], d2[0], d2[1], d3[0], d3[1]};
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const float aw = fabsf(v[t][i]);
-                    const double e = (double)aw - (double)a * (double)code_value(magnitude_code(aw, a));
-                    err += e * e;
+                    const float e = fmaf(-as, d[i], x[i]);
+                    sum[i] = fmaf(e, e, sum[i]);
                 }
-            err += __shfl_xor(err, 32);
+            }
+            const float err = row_sum<G>(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
+            // a candidate that overflows is passed over; one equal to the best so far adds nothing
+            if (!(a < __builtin_inff()) || a == alpha) continue;
             if (err < least) {
+                second = least;
                 least = err;
                 alpha = a;
+            } else {
+                second = fminf(second, err);
             }
         }
-#pragma unroll
-        for (int t = g * WG; t < (g + 1) * WG; t++) {
-            uint32_t d = 0;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const uint32_t c = (uint32_t)magnitude_code(fabsf(v[t][i]), alpha);
-                d |= (c | (c && v[t][i] < 0.0f ? 8u : 0u)) << (4 * i);
-            }
-            packed[t] = d;
+        if (__any(finite && m && (far || second <= least * (1.0f + 0x1p-18f)))) {
+            const float exact = search_exact<T, G, WG>(o, w + (o.n < L.N ? o.n : 0) * ldw, o.n < L.N ? L.K : 0, WG * g, top, factors, nf);
+            if (finite) alpha = exact;
         }
-        const int gi = 64 * o.kc / G + g;
-        if (o.h == 0 && gi < L.groups)
-            scales[scale_index(L, o, gi)] = o.n < L.N && gi * G < L.K ? (__bf16)alpha : (__bf16)0.0f;
+        if (!finite) alpha = __builtin_nanf("");
+        const float as = __builtin_amdgcn_ldexpf(alpha, -shift);
+
+        if constexpr (sizeof(T) == 2) {
+            const float inv = m && alpha == alpha ? 1.0f / as * (1.0f + 0x1p-22f) : 0.0f;
+#pragma unroll
+            for (int t = 0; t < WG; t++) {
+                const uint32_t q = to_e2m1(n + 8 * t, inv);
+                // zeros without a sign: bit 3 stays where a magnitude bit is set
+                packed[WG * g + t] = q & (0x77777777u | ((q & 0x77777777u) + 0x77777777u));
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < WG; t++) {
+                uint32_t d = 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const uint32_t c = (uint32_t)magnitude_code(fabsf(n[8 * t + i]), as);
+                    d |= (c | (c && n[8 * t + i] < 0.0f ? 8u : 0u)) << (4 * i);
+                }
+                packed[WG * g + t] = d;
+            }
+        }
+        const int gi = G == 128 ? o.kc / 2 : 64 * o.kc / G + g;
+        if (o.h == 0 && (G < 128 || o.kc % 2 == 0))
+            scales[((int64_t)o.nt * L.groups + gi) * 32 + o.r] =
+                o.n < L.N && (int64_t)gi * G < L.K ? (__bf16)alpha : (__bf16)0.0f;
     }
-    put_tiles(L, o, packed, out);
+    if (o.kc < L.chunks)
+        *(uint4*)(out + 1024 * ((int64_t)o.nt * L.chunks + o.kc) + 16 * (32 * o.h + o.r)) =
+            uint4{packed[0], packed[2], packed[1], packed[3]};
 }
 
 // ESB(4,1) codes and row-major scales into the layout.
@@ -178,20 +316,24 @@ __global__ __launch_bounds__(256) void k_w4_unpack(W4Layout L, const uint8_t* __
             const uint4 p = *(const uint4*)(in + 1024 * ((int64_t)o.nt * L.chunks + o.kc + u) + 16 * (32 * o.h + o.r));
             const uint32_t packed[4] = {p.x, p.z, p.y, p.w};
 #pragma unroll
-            for (int t = 0; t < 4; t++) {
+            for (int t = 0; t < 4; t += 2) {        // two words are 16 adjacent columns
+                uint32_t q[4];
+#pragma unroll
+                for (int d = 0; d < 2; d++) {
+                    // the eight magnitudes as E4M3 bytes, picked by v_perm_b32
+                    const uint32_t ev = packed[t + d] & 0x0f0f0f0fu, od = (packed[t + d] >> 4) & 0x0f0f0f0fu;
+                    const uint32_t be = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, ev & 0x07070707u) | ((ev & 0x08080808u) << 4);
+                    const uint32_t bo = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, od & 0x07070707u) | ((od & 0x08080808u) << 4);
+                    q[2 * d] = __builtin_amdgcn_perm(bo, be, 0x05010400u);
+                    q[2 * d + 1] = __builtin_amdgcn_perm(bo, be, 0x07030602u);
+                }
                 const int k = column(o, 4 * u + t);
-                // the eight magnitudes as E4M3 bytes, picked by v_perm_b32
-                const uint32_t ev = packed[t] & 0x0f0f0f0fu, od = (packed[t] >> 4) & 0x0f0f0f0fu;
-                const uint32_t be = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, ev & 0x07070707u) | ((ev & 0x08080808u) << 4);
-                const uint32_t bo = __builtin_amdgcn_perm(0x4c484440u, 0x3c383000u, od & 0x07070707u) | ((od & 0x08080808u) << 4);
-                const uint32_t q[2] = {__builtin_amdgcn_perm(bo, be, 0x05010400u),
-                                       __builtin_amdgcn_perm(bo, be, 0x07030602u)};
                 uint8_t* dst = values + o.n * ldv + k;
-                if (L.K - k >= 8) {
-                    ((Loose<uint2, uint8_t>*)dst)->v = uint2{q[0], q[1]};
+                if (L.K - k >= 16) {
+                    ((Loose<uint4, uint8_t>*)dst)->v = uint4{q[0], q[1], q[2], q[3]};
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; i++)
+                    for (int i = 0; i < 16; i++)
                         if (k + i < L.K) dst[i] = (uint8_t)(q[i >> 2] >> (8 * (i & 3)));
                 }
             }
@@ -210,7 +352,8 @@ unsigned tile_blocks(const W4Layout& L) {   // a wave per two chunks
 template <typename T>
 hipError_t quantize_t(const W4Layout& L, const void* w, int64_t ldw, const float* f, int nf, void* out,
                       hipStream_t s) {
-    const unsigned b = tile_blocks(L);
+    const int64_t waves = L.group == 128 ? (int64_t)L.tiles * 2 * ((L.chunks + 1) / 2) : (int64_t)L.tiles * L.chunks;
+    const unsigned b = (unsigned)((waves + 3) / 4);
     if (L.group == 32) k_w4_quantize<T, 32><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
     else if (L.group == 64) k_w4_quantize<T, 64><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
     else k_w4_quantize<T, 128><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
