@@ -7,7 +7,7 @@
 // Outputs are the rows in the inputs' type and / or OCP E4M3 bytes under one scale per row,
 // s = max(max|y| / 448, 2^-126), byte = y (1/s) rounded to nearest even: the operand of
 // esb_w4_gemm.  A row stays in registers between its two reductions (the sum of squares, the
-// maximum), so HBM sees each input and output once.
+// maximum), so HBM sees each input and output once; that bounds them.
 //
 // The sum of squares is held in fp64: squares of fp32 values up to the largest do not overflow,
 // and rstd is the correctly rounded fp32 value up to the last bit.  Everything else is fp32,
@@ -21,72 +21,104 @@ namespace {
 constexpr float kE4M3Max = 448.0f;
 constexpr float kTiny = 0x1p-126f;
 
+// g / (1 + exp(-g)) within 9 roundings: exp by the hardware's exp2 of the rounded product -g log2(e),
+// corrected by what the product lost; the quotient by the hardware's reciprocal.
+__device__ __forceinline__ float silu(float g) {
+    const float c = __builtin_amdgcn_fmed3f(-g, -104.0f, 104.0f);     // exp is 0 or infinite beyond
+    const float hi = c * 0x1.715476p+0f;
+    const float lo = fmaf(c, 0x1.4ae0cp-26f, fmaf(c, 0x1.715476p+0f, -hi));
+    const float e = __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0x1.62e43p-1f, 1.0f);
+    return g * __builtin_amdgcn_rcpf(1.0f + e);
+}
+
+// TPR threads to a row, NV vectors of eight elements to a thread (d <= 8 TPR NV).  With 64 threads a wave
+// works alone, four of them to a workgroup; else a row has a workgroup.
 template <int OP, typename T, int TPR, int NV>
-__global__ __launch_bounds__(TPR) void k_rows(RowsParams p) {
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows(RowsParams p) {
     typedef typename Vec8<T>::type V;
-    __shared__ double red[TPR / 64];
-    __shared__ uint32_t redm[TPR / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = blockIdx.x;
+    constexpr int W = TPR / 64;
+    __shared__ double red[W];
+    __shared__ uint32_t redm[W];
+    const int tid = threadIdx.x % TPR, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = W > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (row >= p.rows) return;
     const int d = p.d;
     const T* a = (const T*)p.a + row * p.lda;
     const T* b = p.b ? (const T*)p.b + row * p.ldb : nullptr;
 
+    // every load before the first store: outputs may lie over the inputs
+    V ra[NV], rb[NV];
+#pragma unroll
+    for (int u = 0; u < NV; u++) {
+        const int e = 8 * (u * TPR + tid);
+        ra[u] = rb[u] = V{};
+        if (e < d) {
+            ra[u] = load8(a + e, d - e);
+            if (b) rb[u] = load8(b + e, d - e);
+        }
+    }
     f32x8 v[NV];
     double ss = 0.0;
 #pragma unroll
     for (int u = 0; u < NV; u++) {
         const int e = 8 * (u * TPR + tid);
-        v[u] = f32x8{};
-        if (e >= d) continue;
-        const int n = d - e;
-        f32x8 x = __builtin_convertvector(load8(a + e, n), f32x8);
+        f32x8 x = __builtin_convertvector(ra[u], f32x8);
+        const f32x8 y = __builtin_convertvector(rb[u], f32x8);
         if (OP == kRowsNorm) {
-            if (b) x += __builtin_convertvector(load8(b + e, n), f32x8);
-            if (p.sum) store8((T*)p.sum + row * p.lds + e, __builtin_convertvector(x, V), n);
+            if (b) x += y;
+            if (p.sum && e < d) store8((T*)p.sum + row * p.lds + e, __builtin_convertvector(x, V), d - e);
 #pragma unroll
-            for (int i = 0; i < 8; i++) ss += (double)x[i] * (double)x[i];
+            for (int i = 0; i < 8; i++) ss = fma((double)x[i], (double)x[i], ss);
         } else {
-            const f32x8 up = __builtin_convertvector(load8(b + e, n), f32x8);
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = x[i] / (1.0f + expf(-x[i])) * up[i];
+            for (int i = 0; i < 8; i++) x[i] = silu(x[i]) * y[i];
         }
         v[u] = x;
     }
     if (OP == kRowsNorm) {
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) ss += __shfl_xor(ss, o);
-        if (lane == 0) red[wave] = ss;
-        __syncthreads();
-        ss = 0.0;
-#pragma unroll
-        for (int i = 0; i < TPR / 64; i++) ss += red[i];
-        const float rstd = (float)(1.0 / sqrt(ss / (double)d + (double)p.eps));
+        f32x8 w[NV];
 #pragma unroll
         for (int u = 0; u < NV; u++) {
             const int e = 8 * (u * TPR + tid);
-            if (e >= d) continue;
-            const f32x8 w = p.w ? load8(p.w + e, d - e) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
-            v[u] = v[u] * rstd * w;
+            w[u] = p.w && e < d ? load8(p.w + e, d - e) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) ss += __shfl_xor(ss, o);
+        if (W > 1) {
+            if (lane == 0) red[wave] = ss;
+            __syncthreads();
+            ss = 0.0;
+#pragma unroll
+            for (int i = 0; i < W; i++) ss += red[i];
+        }
+        const float rstd = (float)(1.0 / sqrt(ss / (double)d + (double)p.eps));
+#pragma unroll
+        for (int u = 0; u < NV; u++) v[u] = v[u] * rstd * w[u];
+    }
+    if (p.y) {
+#pragma unroll
+        for (int u = 0; u < NV; u++) {
+            const int e = 8 * (u * TPR + tid);
+            if (e < d) store8((T*)p.y + row * p.ldy + e, __builtin_convertvector(v[u], V), d - e);
         }
     }
+    if (!p.y8) return;
+    // max |y|, on bit patterns: a NaN is above every number
     uint32_t m = 0;
 #pragma unroll
-    for (int u = 0; u < NV; u++) {
-        const int e = 8 * (u * TPR + tid);
-        if (e >= d) continue;
-        if (p.y) store8((T*)p.y + row * p.ldy + e, __builtin_convertvector(v[u], V), d - e);
+    for (int u = 0; u < NV; u++)
+        if (8 * (u * TPR + tid) < d)
 #pragma unroll
-        for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[u][i]) & 0x7fffffffu);
-    }
-    if (!p.y8) return;
+            for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[u][i]) & 0x7fffffffu);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-    if (lane == 0) redm[wave] = m;
-    __syncthreads();
-    m = 0;
+    if (W > 1) {
+        if (lane == 0) redm[wave] = m;
+        __syncthreads();
+        m = 0;
 #pragma unroll
-    for (int i = 0; i < TPR / 64; i++) m = max(m, redm[i]);
+        for (int i = 0; i < W; i++) m = max(m, redm[i]);
+    }
     // a NaN or an infinity in the row: no scale fits it
     const float s = m < 0x7f800000u ? fmaxf(__uint_as_float(m) / kE4M3Max, kTiny) : __builtin_nanf("");
     const float inv = 1.0f / s;
@@ -107,9 +139,9 @@ __global__ __launch_bounds__(TPR) void k_rows(RowsParams p) {
     }
 }
 
-template <int OP, typename T>
-hipError_t launch_t(const RowsParams& p, hipStream_t s) {
-    const int64_t most = 1 << 21;      // workgroups of one launch
+template <int OP, typename T, int TPR, int NV>
+hipError_t launch_n(const RowsParams& p, hipStream_t s) {
+    const int64_t most = 1 << 21;      // rows of one launch
     for (int64_t r = 0; r < p.rows; r += most) {
         RowsParams q = p;
         q.rows = p.rows - r < most ? p.rows - r : most;
@@ -118,11 +150,27 @@ hipError_t launch_t(const RowsParams& p, hipStream_t s) {
         if (p.sum) q.sum = (T*)p.sum + r * p.lds;
         if (p.y) q.y = (T*)p.y + r * p.ldy;
         if (p.y8) q.y8 = p.y8 + r * p.ld8, q.scale = p.scale + r;
-        k_rows<OP, T, 1024, 8><<<(unsigned)q.rows, 1024, 0, s>>>(q);
+        k_rows<OP, T, TPR, NV><<<(unsigned)(TPR > 64 ? q.rows : (q.rows + 3) / 4), TPR > 64 ? TPR : 256, 0, s>>>(q);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <int OP, typename T>
+hipError_t launch_t(const RowsParams& p, hipStream_t s) {
+    const int d = p.d;
+    if (d <= 1024) return launch_n<OP, T, 64, 2>(p, s);
+    // many rows: a wave each, no barriers; few: many threads with little each
+    if (p.rows >= 4 * num_cus() && d <= 4096) return launch_n<OP, T, 64, 8>(p, s);
+    if (d <= 2048) return launch_n<OP, T, 256, 1>(p, s);
+    if (p.rows >= num_cus()) {
+        if (d <= 4096) return launch_n<OP, T, 256, 2>(p, s);
+        if (d <= 8192) return launch_n<OP, T, 256, 4>(p, s);
+    }
+    if (d <= 8192) return launch_n<OP, T, 1024, 1>(p, s);
+    if (d <= 16384) return launch_n<OP, T, 1024, 2>(p, s);
+    return launch_n<OP, T, 1024, 8>(p, s);
 }
 
 }  // namespace

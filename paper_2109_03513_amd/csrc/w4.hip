@@ -116,6 +116,13 @@ __device__ __forceinline__ float row_sum(float v) {
     }));
 }
 
+template <int G>
+__device__ __forceinline__ double row_sum(double v) {
+    v += __shfl_xor(v, 32);
+    if (G == 128) v += __shfl_xor(v, 16);
+    return v;
+}
+
 // One group of a row's lanes, in any range of values: errors in fp64 from exact cell bounds.  Rare: it
 // reads the group's weights again rather than keep them.
 template <typename T, int G, int WG>
@@ -139,8 +146,7 @@ __device__ __forceinline__ float search_exact(const Share<G>& o, const T* row, i
                 err += e * e;
             }
         }
-        err += __shfl_xor(err, 32);
-        if (G == 128) err += __shfl_xor(err, 16);
+        err = row_sum<G>(err);
         if (a < __builtin_inff() && err < least) {
             least = err;
             alpha = a;
@@ -149,6 +155,18 @@ __device__ __forceinline__ float search_exact(const Share<G>& o, const T* row, i
     return alpha;
 }
 
+// Squared error of one lane's weights n under scale a, fp64 from exact cell bounds.
+template <int WG>
+__device__ __forceinline__ double exact_error(const float* n, float a) {
+    double err = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8 * WG; i++) {
+        const float aw = fabsf(n[i]);
+        const double e = (double)aw - (double)a * (double)code_value(magnitude_code(aw, a));
+        err += e * e;
+    }
+    return err;
+}
 // Eight values to E2M1 nibbles, rounded to nearest even, at most 6.
 __device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
     uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[0] * by, x[1] * by, 1.0f, 0);
@@ -160,8 +178,9 @@ __device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
 // The search needs no exact codes: the error is continuous where a code changes, so a candidate's q is
 // the conversion to fp4 of w (1/alpha), and e = w - alpha q one fma.  The group is scaled by a power of
 // two that brings its largest weight into [1, 2), which keeps e^2 in range.  Sums of up to 128 squares
-// in 8 fp32 parts a lane are within 2^-20 of their value; a second candidate within 2^-18 of the least,
-// or candidates far below the weights, send the wave to search_exact (a few waves in a thousand).
+// in 8 fp32 parts a lane are within 2^-20 of their value; where the second least is within 2^-19 of the
+// least (a few groups in ten thousand), the two are compared in fp64.  Three candidates so close, or
+// candidates far below the weights, are left to search_exact.
 //
 // Codes: for 16-bit weights w / alpha is a tie or at least 2^-11 from one, so w (1/alpha) (1 + 2^-22)
 // rounds to the nearest value with ties up; 32-bit weights are compared with the exact bounds.
@@ -201,8 +220,9 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
         const int shift = finite && m ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
 #pragma unroll
         for (int i = 0; i < 8 * WG; i++) n[i] = finite ? __builtin_amdgcn_ldexpf(n[i], -shift) : 0.0f;
-        float alpha = __builtin_nanf(""), least = __builtin_inff(), second = __builtin_inff();
-        bool far = false;
+        const float inf = __builtin_inff();
+        float alpha = __builtin_nanf(""), other = alpha, least = inf, second = inf, third = inf;
+        bool far = false, other_first = false;
         for (int c = 0; c < nf; c++) {
             const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fs), c));
             if (!(f > 0.0f) || !(f < __builtin_inff())) continue;
@@ -227,19 +247,32 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
                 }
             }
             const float err = row_sum<G>(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
-            // a candidate that overflows is passed over; one equal to the best so far adds nothing
-            if (!(a < __builtin_inff()) || a == alpha) continue;
+            // a candidate that overflows is passed over; one equal to a kept one adds nothing
+            if (!(a < inf) || a == alpha || a == other) continue;
             if (err < least) {
+                third = second;
                 second = least;
+                other = alpha;
+                other_first = true;
                 least = err;
                 alpha = a;
+            } else if (err < second) {
+                third = second;
+                second = err;
+                other = a;
+                other_first = false;
             } else {
-                second = fminf(second, err);
+                third = fminf(third, err);
             }
         }
-        if (__any(finite && m && (far || second <= least * (1.0f + 0x1p-18f)))) {
+        const float near = least * (1.0f + 0x1p-19f);
+        if (__any(finite && m && (far || third <= near))) {
             const float exact = search_exact<T, G, WG>(o, w + (o.n < L.N ? o.n : 0) * ldw, o.n < L.N ? L.K : 0, WG * g, top, factors, nf);
             if (finite) alpha = exact;
+        } else if (__any(finite && m && second <= near)) {
+            const double e0 = row_sum<G>(exact_error<WG>(n, __builtin_amdgcn_ldexpf(alpha, -shift)));
+            const double e1 = row_sum<G>(exact_error<WG>(n, __builtin_amdgcn_ldexpf(other, -shift)));
+            if (second <= near && (other_first ? e1 <= e0 : e1 < e0)) alpha = other;
         }
         if (!finite) alpha = __builtin_nanf("");
         const float as = __builtin_amdgcn_ldexpf(alpha, -shift);
