@@ -158,9 +158,12 @@ def _stream(stream):
     """Handle of a stream: an int, an object with .cuda_stream, or the current one for None."""
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    import torch
+    torch = _torch
+    if torch is None:
+        import torch
     try:   # the raw handle, without building a Stream object (which costs several us a call)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        c = torch._C
+        return c._cuda_getCurrentRawStream(c._cuda_getDevice())
     except AttributeError:
         return torch.cuda.current_stream().cuda_stream
 
@@ -682,11 +685,12 @@ def _matrix(t, name):
     """(rows, columns, pitch) of a device matrix whose columns are adjacent; rows may be apart."""
     if not isinstance(t, _torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA (HIP) tensor" % name)
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError("%s must have two dimensions" % name)
-    rows, cols = t.shape
+    rows, cols = shape
     sr, sc = t.stride()
-    if cols > 1 and sc != 1:
+    if sc != 1 and cols > 1:
         raise ValueError("%s must have adjacent columns" % name)
     if rows <= 1:
         return rows, cols, cols
@@ -695,39 +699,37 @@ def _matrix(t, name):
     return rows, cols, sr
 
 
-def _like(t, name, shape, dtype, device):
-    """Pitch of a matrix that has to have this shape, type and device."""
-    rows, cols, ld = _matrix(t, name)
-    if (rows, cols) != shape or t.dtype != dtype or t.device != device:
-        raise ValueError("%s must be %s of %s on %s" % (name, shape, dtype, device))
+def _like(t, name, rows, cols, dtype, index):
+    """Pitch of a matrix that has to have this shape and type, on this device."""
+    r, c, ld = _matrix(t, name)
+    if r != rows or c != cols or t.dtype != dtype or t.get_device() != index:
+        raise ValueError("%s must be %d x %d of %s on cuda:%d" % (name, rows, cols, dtype, index))
     return ld
 
 
-def _vector(t, name, n, dtype, device):
+def _vector(t, name, n, dtype, index):
     if t.dtype != dtype:
         raise TypeError("%s must be %s" % (name, dtype))
-    if t.device != device or t.numel() != n or not t.is_contiguous():
-        raise ValueError("%s must be %d contiguous elements on %s" % (name, n, device))
+    if t.get_device() != index or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous elements on cuda:%d" % (name, n, index))
 
 
-def _row_outputs(rows, d, dtype, device, y, want_y, y8, scale, want_y8):
+def _row_outputs(x, rows, d, index, y, want_y, y8, scale, want_y8):
     """y, y8 and scale as given or new, and the pitches of y and y8."""
-    torch = _torch
-    if y is None and want_y:
-        y = torch.empty((rows, d), dtype=dtype, device=device)
-        ldy = d
-    else:
-        ldy = 0 if y is None else _like(y, "y", (rows, d), dtype, device)
-    if y8 is None and want_y8:
-        y8 = torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=device)
-        ld8 = d
-    else:
-        ld8 = 0 if y8 is None else _like(y8, "y8", (rows, d), torch.float8_e4m3fn, device)
+    ldy = ld8 = d
+    if y is not None:
+        ldy = _like(y, "y", rows, d, x.dtype, index)
+    elif want_y:
+        y = x.new_empty((rows, d))
+    if y8 is not None:
+        ld8 = _like(y8, "y8", rows, d, _torch.float8_e4m3fn, index)
+    elif want_y8:
+        y8 = x.new_empty((rows, d), dtype=_torch.float8_e4m3fn)
     if y8 is not None:
         if scale is None:
-            scale = torch.empty(rows, dtype=torch.float32, device=device)
+            scale = x.new_empty(rows, dtype=_torch.float32)
         else:
-            _vector(scale, "scale", rows, torch.float32, device)
+            _vector(scale, "scale", rows, _torch.float32, index)
     return y, ldy, y8, ld8, scale
 
 
@@ -738,16 +740,19 @@ def esb_rmsnorm(x, w, eps, residual=None, sum_out=None, want_sum=False, y=None, 
     Returns (sum, y, y8, scale): z and y in x's type, and y as float8_e4m3fn under one fp32 scale
     per row; what is neither given nor wanted is None."""
     L = _lib or lib()
-    t = _type(x, "x", _FLOATS)
     rows, d, ldx = _matrix(x, "x")
-    dtype, device = x.dtype, x.device
-    ldr = 0 if residual is None else _like(residual, "residual", (rows, d), dtype, device)
+    t = _type(x, "x", _FLOATS)
+    index = x.get_device()
+    ldr = lds = 0
+    if residual is not None:
+        ldr = _like(residual, "residual", rows, d, x.dtype, index)
     if w is not None:
-        _vector(w, "w", d, _torch.float32, device)
-    if sum_out is None and want_sum:
-        sum_out = _torch.empty((rows, d), dtype=dtype, device=device)
-    lds = 0 if sum_out is None else _like(sum_out, "sum_out", (rows, d), dtype, device)
-    y, ldy, y8, ld8, scale = _row_outputs(rows, d, dtype, device, y, want_y, y8, scale, want_y8)
+        _vector(w, "w", d, _torch.float32, index)
+    if sum_out is not None:
+        lds = _like(sum_out, "sum_out", rows, d, x.dtype, index)
+    elif want_sum:
+        sum_out, lds = x.new_empty((rows, d)), d
+    y, ldy, y8, ld8, scale = _row_outputs(x, rows, d, index, y, want_y, y8, scale, want_y8)
     st = L.esb_rmsnorm(x.data_ptr(), ldx, _addr(residual), ldr, t, rows, d, _addr(w), eps,
                        _addr(sum_out), lds, _addr(y), ldy, _addr(y8), ld8, _addr(scale),
                        _stream(stream))
@@ -759,11 +764,11 @@ def esb_rmsnorm(x, w, eps, residual=None, sum_out=None, want_sum=False, y=None, 
 def esb_swiglu(gate, up, y=None, want_y=False, y8=None, scale=None, want_y8=True, stream=None):
     """gate / (1 + exp(-gate)) * up, rows x d; returns (y, y8, scale) as esb_rmsnorm does."""
     L = _lib or lib()
-    t = _type(gate, "gate", _FLOATS)
     rows, d, ldg = _matrix(gate, "gate")
-    dtype, device = gate.dtype, gate.device
-    ldu = _like(up, "up", (rows, d), dtype, device)
-    y, ldy, y8, ld8, scale = _row_outputs(rows, d, dtype, device, y, want_y, y8, scale, want_y8)
+    t = _type(gate, "gate", _FLOATS)
+    index = gate.get_device()
+    ldu = _like(up, "up", rows, d, gate.dtype, index)
+    y, ldy, y8, ld8, scale = _row_outputs(gate, rows, d, index, y, want_y, y8, scale, want_y8)
     st = L.esb_swiglu(gate.data_ptr(), ldg, up.data_ptr(), ldu, t, rows, d, _addr(y), ldy, _addr(y8),
                       ld8, _addr(scale), _stream(stream))
     if st:
@@ -775,19 +780,25 @@ def esb_w4_size(N, K, group):
     return int(lib().esb_w4_size(N, K, group))
 
 
-def _w4_buffer(w4, N, K, group, device):
+def _w4_buffer(w4, N, K, group, like):
     need = esb_w4_size(N, K, group)
     if w4 is None:
         if need == 0 and N and K:
             raise EsbError("esb_w4_size", ESB_E_INVALID)
-        return _torch.empty(max(need, 1), dtype=_torch.uint8, device=device)
-    return _w4_check(w4, device)
+        return like.new_empty(max(need, 1), dtype=_torch.uint8)
+    return _w4_check(w4, like.get_device())
 
 
-def _w4_check(w4, device):
-    if w4.dtype != _torch.uint8 or w4.device != device or not w4.is_contiguous():
-        raise ValueError("w4 must be contiguous uint8 on %s" % (device,))
+def _w4_check(w4, index):
+    if w4.dtype != _torch.uint8 or w4.get_device() != index or not w4.is_contiguous():
+        raise ValueError("w4 must be contiguous uint8 on cuda:%d" % index)
     return w4
+
+
+def _w4_holds(L, w4, N, K, group):
+    need = L.esb_w4_size(N, K, group)
+    if w4.numel() < need or (need == 0 and N and K):
+        raise EsbError("esb_w4_size", ESB_E_WORKSPACE if need else ESB_E_INVALID)
 
 
 def esb_w4_quantize(w, group, factors=None, w4=None, stream=None):
@@ -795,11 +806,11 @@ def esb_w4_quantize(w, group, factors=None, w4=None, stream=None):
     esb_w4_size(N, K, group) bytes.  factors: device fp32 candidates of the scale, as multiples
     of max|w| / 6 of the group (None: 1)."""
     L = _lib or lib()
-    t = _type(w, "w", _FLOATS)
     N, K, ld = _matrix(w, "w")
+    t = _type(w, "w", _FLOATS)
     if factors is not None:
-        _vector(factors, "factors", factors.numel(), _torch.float32, w.device)
-    w4 = _w4_buffer(w4, N, K, group, w.device)
+        _vector(factors, "factors", factors.numel(), _torch.float32, w.get_device())
+    w4 = _w4_buffer(w4, N, K, group, w)
     st = L.esb_w4_quantize(w.data_ptr(), ld, t, N, K, group, _addr(factors),
                            1 if factors is None else factors.numel(), w4.data_ptr(), w4.numel(),
                            _stream(stream))
@@ -811,11 +822,12 @@ def esb_w4_quantize(w, group, factors=None, w4=None, stream=None):
 def esb_w4_pack(codes, alpha, group, w4=None, stream=None):
     """The packed form of ESB(4,1) codes (N x K uint8) and bf16 scales (N x ceil(K / group))."""
     L = _lib or lib()
+    N, K, ldc = _matrix(codes, "codes")
     if codes.dtype != _torch.uint8:
         raise TypeError("codes must be uint8")
-    N, K, ldc = _matrix(codes, "codes")
-    lda = _like(alpha, "alpha", (N, -(-K // group) if group > 0 else 0), _torch.bfloat16, codes.device)
-    w4 = _w4_buffer(w4, N, K, group, codes.device)
+    lda = _like(alpha, "alpha", N, -(-K // group) if group > 0 else 0, _torch.bfloat16,
+                codes.get_device())
+    w4 = _w4_buffer(w4, N, K, group, codes)
     st = L.esb_w4_pack(codes.data_ptr(), ldc, alpha.data_ptr(), lda, N, K, group, w4.data_ptr(),
                        w4.numel(), _stream(stream))
     if st:
@@ -823,26 +835,23 @@ def esb_w4_pack(codes, alpha, group, w4=None, stream=None):
     return w4
 
 
-def _w4_holds(w4, N, K, group):
-    need = esb_w4_size(N, K, group)
-    if w4.numel() < need or (need == 0 and N and K):
-        raise EsbError("esb_w4_size", ESB_E_WORKSPACE if need else ESB_E_INVALID)
-
-
 def esb_w4_unpack(w4, N, K, group, values=None, alpha=None, stream=None):
     """(values, alpha): the unscaled values (N x K float8_e4m3fn, exact) and the group scales
     (N x ceil(K / group) bf16) of packed weights."""
     L = _lib or lib()
-    torch = _torch
-    _w4_check(w4, w4.device)
-    _w4_holds(w4, N, K, group)
+    index = w4.get_device()
+    _w4_check(w4, index)
+    _w4_holds(L, w4, N, K, group)
     groups = -(-K // group) if group > 0 else 0
+    ldv, lda = K, groups
     if values is None:
-        values = torch.empty((N, K), dtype=torch.float8_e4m3fn, device=w4.device)
+        values = w4.new_empty((N, K), dtype=_torch.float8_e4m3fn)
+    else:
+        ldv = _like(values, "values", N, K, _torch.float8_e4m3fn, index)
     if alpha is None:
-        alpha = torch.empty((N, groups), dtype=torch.bfloat16, device=w4.device)
-    ldv = _like(values, "values", (N, K), torch.float8_e4m3fn, w4.device)
-    lda = _like(alpha, "alpha", (N, groups), torch.bfloat16, w4.device)
+        alpha = w4.new_empty((N, groups), dtype=_torch.bfloat16)
+    else:
+        lda = _like(alpha, "alpha", N, groups, _torch.bfloat16, index)
     st = L.esb_w4_unpack(w4.data_ptr(), N, K, group, values.data_ptr(), ldv, alpha.data_ptr(), lda,
                          _stream(stream))
     if st:
@@ -859,25 +868,26 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=N
     weights W (N x K); y in y_dtype (None: x's type; bf16 for float8).  workspace: at least
     esb_w4_gemm_workspace_size() bytes; without one the call allocates what it needs from torch."""
     L = _lib or lib()
-    tx = _type(x, "x", (ESB_F32, ESB_BF16, ESB_F16, ESB_E4M3))   # fp32: the library's refusal
     M, K, ldx = _matrix(x, "x")
-    device = x.device
-    _w4_check(w4, device)
-    _w4_holds(w4, N, K, group)
+    tx = _type(x, "x", (ESB_F32, ESB_BF16, ESB_F16, ESB_E4M3))   # fp32: the library's refusal
+    index = x.get_device()
+    _w4_check(w4, index)
+    _w4_holds(L, w4, N, K, group)
     if x_scale is not None:
-        _vector(x_scale, "x_scale", M, _torch.float32, device)
+        _vector(x_scale, "x_scale", M, _torch.float32, index)
+    ldy = N
     if y is None:
         if y_dtype is None:
             y_dtype = _torch.bfloat16 if tx == ESB_E4M3 else x.dtype
-        y = _torch.empty((M, N), dtype=y_dtype, device=device)
-        ldy = N
+        ty = _type(y_dtype, "y", _FLOATS)
+        y = x.new_empty((M, N), dtype=y_dtype)
     else:
-        ldy = _like(y, "y", (M, N), y_dtype or y.dtype, device)
-    ty = _type(y, "y", _FLOATS)
+        ty = _type(y, "y", _FLOATS)
+        ldy = _like(y, "y", M, N, y_dtype or y.dtype, index)
     if workspace is None:
         need = L.esb_w4_gemm_workspace_size(M, N, K, group, tx, ty)
         if need:
-            workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
+            workspace = x.new_empty(need, dtype=_torch.uint8)
     wp, wb = _ws(workspace)
     st = L.esb_w4_gemm(M, N, K, group, x.data_ptr(), ldx, tx, _addr(x_scale), w4.data_ptr(),
                        y.data_ptr(), ldy, ty, wp, wb, _stream(stream))
