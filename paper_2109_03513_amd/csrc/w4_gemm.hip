@@ -197,6 +197,11 @@ __device__ __forceinline__ int xcd_run(int id, int total) {
 // group and tile by tile: the MFMAs of one (tile, group) are issued, then the sums of an earlier one
 // are scaled and added under them.
 //
+// KW parts of WM x WN waves, each with a ring of its own, take every KW-th step of the tile, and the first
+// part adds their sums: a step's chain of barrier, LDS reads, decoding and dependent MFMAs is about
+// 1000 cycles that only other waves can fill (32 x 256, 64 steps, one workgroup per CU: 28 us with
+// one part, 21 with two, 17 with four).
+//
 // F8: within one instruction, products below 2^-13 of its largest are dropped (measured with single
 // instructions).  Of 128 products of E4M3 rows that is at most 2^-6 and in practice some 10^-4 of
 // their root mean square: under the rounding of a 16-bit output (2^-9, 2^-12), so fp32 outputs
@@ -224,12 +229,12 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-template <typename X, int F8, int G, int TM, int WM, int WN, int R, int DMA>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int tiles_m, int tiles, int per_split) {
+template <typename X, int F8, int G, int TM, int WM, int WN, int KW, int R, int DMA>
+__global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(W4GemmParams p, int tiles_m, int tiles, int per_split) {
     typedef typename Act<X>::M M;
     typedef typename Act<X>::raw Raw;
     typedef typename FragOf<F8, typename M::frag>::type Frag;
-    constexpr int NW = WM * WN, T = 64 * NW, BM = 32 * TM * WM;
+    constexpr int NW = WM * WN, BM = 32 * TM * WM;            // waves and rows of one part
     constexpr int BK = F8 ? 128 : 64, EP = F8 ? 16 : 8;       // columns of a step, of a piece
     constexpr int NC = F8 ? 2 : 1;                            // column chunks of a step
     constexpr int NG = F8 ? 128 / G : G == 32 ? 2 : 1;        // scales of a step
@@ -240,11 +245,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int
     constexpr int GM = 4;                                     // tiles of rows in a band
     constexpr int SLAB = 68;                                  // floats of a slab's row
     static_assert(NW * 32 * SLAB * 4 <= R * STAGE, "the slabs fit the ring");
-    __shared__ __align__(16) uint8_t ring[R * STAGE];
+    static_assert((KW - 1) * NW * TM * 8192 <= KW * R * STAGE, "the other parts' sums fit the rings");
+    __shared__ __align__(16) uint8_t rings[KW * R * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part_k = __builtin_amdgcn_readfirstlane(tid >> 6) / NW;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) % NW;
     const int wm = wave / WN, wn = wave % WN;
+    uint8_t* ring = rings + part_k * (R * STAGE);
     // A run of tiles goes through bands of up to GM tiles of rows, n by n: the workgroups of an XCD that
     // run together then share few rows and few columns, and its L2 fetches each once.
     const int id = xcd_run(blockIdx.x, gridDim.x), z = id / tiles, t = id - z * tiles, tiles_n = tiles / tiles_m;
@@ -279,7 +287,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int
     // every stage issues the same number of DMAs, also past the last step
     auto fetch = [&](int s, uint8_t* slot) {
         if constexpr (DMA) {
-            const bool in = s * BK + EP * pc < K;
+            const bool in = s * BK + EP * pc < K && s < end;
 #pragma unroll
             for (int i = 0; i < NX; i++)
                 dma16(in ? (const void*)(xp[i] + s * BK) : (const void*)kZero16, slot + 1024 * (wave + i * NW));
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int
     };
     Raw st[DMA ? 1 : NX][F8 ? 2 : 1];
     auto load = [&](int s) {
-        const int k = s * BK;
+        const int k = s < end ? s * BK : K;
         if (k + BK <= K) {
 #pragma unroll
             for (int i = 0; i < NX; i++)
@@ -389,23 +397,25 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int
     };
 
     if (first < end) {
-        // stage first + s in slot s % R
+        // step first + i KW + part_k in slot i % R; a part's steps past the end add zeros
+        const int begin = first + part_k, turns = (end - first + KW - 1) / KW;
         if constexpr (!DMA) {
-            load(first);
+            load(begin);
             put(ring);
-            load(first + 1);
+            load(begin + KW);
         }
 #pragma unroll
-        for (int q = 0; q < R - 1; q++) fetch(first + q, ring + q * STAGE);
-        int cur = 0, last = R - 1;           // slots of this step and of the one before it
-        for (int s = first; s < end; s++) {
-            vm_wait<(R - 2) * PER>();        // this wave's part of stage s has landed
-            lds_barrier();                   // all of it; every read of the last step is done
+        for (int q = 0; q < R - 1; q++) fetch(begin + q * KW, ring + q * STAGE);
+        int cur = 0, last = R - 1;           // slots of this turn and of the one before it
+        for (int i = 0; i < turns; i++) {
+            const int s = begin + i * KW;
+            vm_wait<(R - 2) * PER>();        // this wave's part of step s has landed
+            lds_barrier();                   // all of it; every read of the last turn is done
             __builtin_amdgcn_sched_barrier(0);
-            fetch(s + R - 1, ring + last * STAGE);
+            fetch(s + (R - 1) * KW, ring + last * STAGE);
             if constexpr (!DMA) {
                 put(ring + (cur + 1 == R ? 0 : cur + 1) * STAGE);
-                load(s + 2);
+                load(s + 2 * KW);
             }
             __builtin_amdgcn_sched_barrier(0);
             step(ring + cur * STAGE);
@@ -414,10 +424,32 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_w4_tile(W4GemmParams p, int
         }
         vm_wait<0>();                        // no DMA outlives its workgroup
     }
+    __syncthreads();
+    if constexpr (KW > 1) {
+        // the first part adds the sums of the others, in order
+        f32x4* red = (f32x4*)rings + wave * (TM * 512) + lane;
+        if (part_k > 0)
+#pragma unroll
+            for (int q = 0; q < TM * 8; q++) {
+                const f32x16& v = acc[q / 8][q / 4 % 2];
+                red[(part_k - 1) * (NW * TM * 512) + 64 * q] = f32x4{v[4 * (q % 4)], v[4 * (q % 4) + 1], v[4 * (q % 4) + 2], v[4 * (q % 4) + 3]};
+            }
+        __syncthreads();
+        if (part_k == 0)
+#pragma unroll
+            for (int k = 0; k < KW - 1; k++)
+#pragma unroll
+                for (int q = 0; q < TM * 8; q++) {
+                    const f32x4 o = red[k * (NW * TM * 512) + 64 * q];
+#pragma unroll
+                    for (int c = 0; c < 4; c++) acc[q / 8][q / 4 % 2][4 * (q % 4) + c] += o[c];
+                }
+        __syncthreads();
+        if (part_k > 0) return;
+    }
 
     // Outputs, 32 rows at a time through a slab of LDS of each wave's own: lanes hold columns, stores
     // want rows of 16-byte pieces.
-    __syncthreads();
     float* slab = (float*)(ring + wave * (32 * SLAB * 4));
     // f(row m, first column n, eight values): every lane, column n may lie past the last
     auto outputs = [&](auto f) {
@@ -497,25 +529,30 @@ hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
     return e;
 }
 
-// The shapes of k_w4_tile and what a step costs, us on one CU holding 1 .. slots of its workgroups
-// (measured with the rows in DMA, G = 128: 256, 512, .. workgroups, K = 4096 and 9216).  Small tiles
-// spread few rows over the chip, large ones read less per product.
+// The shapes of k_w4_tile and what a step of theirs costs, us on one CU holding 1 .. slots of its
+// workgroups (fitted to 24 shapes of 32 to 1024 rows, 4096 to 18432 outputs, K = 4096 and 9216, G = 128,
+// each with every shape and number of splits; the choice is within 5 % of the best in all but a few of
+// the 48, 13 % at worst).  Small tiles spread few rows over the chip, large ones read less per product;
+// the first and the third split a tile's steps over parts of a workgroup.
 struct TileShape {
     int bm, bn, slots;
     float step[3];
 };
-constexpr TileShape kShapes16[4] = {{32, 256, 3, {0.41f, 0.63f, 0.85f}},
-                                    {64, 256, 2, {0.615f, 1.025f}},
-                                    {128, 256, 1, {1.03f}},
-                                    {128, 256, 2, {1.10f, 1.96f}}};
-constexpr TileShape kShapes8[4] = {{32, 256, 1, {0.42f}},
-                                   {64, 128, 2, {0.44f, 0.60f}},
-                                   {128, 256, 1, {1.0f}},
-                                   {128, 256, 2, {0.97f, 1.72f}}};
+constexpr int kShapes = 5;
+constexpr TileShape kShapes16[kShapes] = {{32, 256, 2, {0.36f, 0.58f}},
+                                          {64, 256, 2, {0.615f, 1.025f}},
+                                          {64, 256, 1, {0.54f}},
+                                          {128, 256, 1, {1.03f}},
+                                          {128, 256, 2, {1.10f, 1.96f}}};
+constexpr TileShape kShapes8[kShapes] = {{64, 128, 1, {0.35f}},
+                                         {64, 128, 2, {0.44f, 0.66f}},
+                                         {128, 128, 1, {0.56f}},
+                                         {128, 256, 1, {0.98f}},
+                                         {128, 256, 2, {1.09f, 1.72f}}};
 
 // The shape and the ranges of columns (splits) that should take the least time: rounds of full CUs,
 // then one of what is left; splits write and read fp32 sums at about 4 TB/s and launch one more kernel.
-// DMA == 0 has two shapes.  part: whether there is room for the sums of two ranges or more.
+// DMA == 0 has the first two.  part: whether there is room for the sums of two ranges or more.
 struct TilePlan {
     int shape, splits;
 };
@@ -525,7 +562,7 @@ TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, bool part) {
     TilePlan best = {0, 1};
     double least = 1e30;
     // the last shape's registers do not hold two scales per step of its 128 x 64 waves
-    const int shapes = !dma ? 2 : L.group == 32 ? 3 : 4;
+    const int shapes = !dma ? 2 : L.group == 32 ? kShapes - 1 : kShapes;
     for (int v = 0; v < shapes; v++) {
         const TileShape& s = f8 ? kShapes8[v] : kShapes16[v];
         const double tiles = (double)((M + s.bm - 1) / s.bm) * ((L.N + s.bn - 1) / s.bn);
@@ -534,7 +571,7 @@ TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, bool part) {
             const double held = ceil(tiles * z / cus), rounds = floor((held - 1) / s.slots);
             const int rest = (int)(held - rounds * s.slots);
             double us = (rounds * s.step[s.slots - 1] + s.step[rest - 1]) * ceil((double)steps / z);
-            if (z > 1) us += 3.5 + z * (double)M * L.tiles * 32 * 8 / 4e6;
+            if (z > 1) us += 4.5 + z * (double)M * L.tiles * 32 * 8 / 4e6;
             if (us < least) {
                 least = us;
                 best = {v, z};
@@ -556,14 +593,14 @@ bool takes_dma(const W4GemmParams& p, int x_type, bool f8) {
     return (f8 || es == 2) && (uintptr_t)p.x % 16 == 0 && p.ldx * es % 16 == 0 && (int64_t)p.L.K * es % 16 == 0;
 }
 
-template <typename X, int F8, int G, int TM, int WM, int WN, int R, int DMA>
+template <typename X, int F8, int G, int TM, int WM, int WN, int KW, int R, int DMA>
 hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
     const int tm = (int)((p.M + 32 * TM * WM - 1) / (32 * TM * WM)), tn = (p.L.tiles + 2 * WN - 1) / (2 * WN);
     const int steps = F8 ? (p.L.chunks + 1) / 2 : p.L.chunks, per = steps ? (steps + splits - 1) / splits : 0;
     splits = steps ? (steps + per - 1) / per : 1;
     W4GemmParams q = p;
     if (splits == 1) q.part = nullptr;
-    k_w4_tile<X, F8, G, TM, WM, WN, R, DMA><<<(unsigned)(tm * tn * splits), 64 * WM * WN, 0, s>>>(q, tm, tm * tn, per);
+    k_w4_tile<X, F8, G, TM, WM, WN, KW, R, DMA><<<(unsigned)(tm * tn * splits), 64 * WM * WN * KW, 0, s>>>(q, tm, tm * tn, per);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && splits > 1) {
         k_w4_sum<<<(unsigned)((p.M * p.L.tiles * 4 + 255) / 256), 256, 0, s>>>(p, splits);
@@ -576,20 +613,29 @@ template <typename X, int F8, int G>
 hipError_t launch_shape(const W4GemmParams& p, int x_type, hipStream_t s) {
     const bool dma = takes_dma(p, x_type, F8);
     const TilePlan t = tile_plan(p.M, p.L, F8, dma, p.part != nullptr);
-    if constexpr (F8 || sizeof(X) == 2) {
-        if (dma) {
-            if (t.shape == 0) return launch_tile<X, F8, G, 1, 1, 4, 4, 1>(p, t.splits, s);
-            if (t.shape == 1) {
-                if constexpr (F8) return launch_tile<X, F8, G, 1, 2, 2, 4, 1>(p, t.splits, s);
-                else return launch_tile<X, F8, G, 2, 1, 4, 4, 1>(p, t.splits, s);
-            }
-            if (t.shape == 2) return launch_tile<X, F8, G, 2, 2, 4, 4, 1>(p, t.splits, s);
-            if constexpr (G > 32) return launch_tile<X, F8, G, 4, 1, 4, F8 ? 2 : 3, 1>(p, t.splits, s);
+    if constexpr (F8) {
+        if (!dma) {
+            if (t.shape == 0) return launch_tile<X, 1, G, 1, 2, 2, 4, 2, 0>(p, t.splits, s);
+            return launch_tile<X, 1, G, 1, 2, 2, 1, 4, 0>(p, t.splits, s);
         }
+        if (t.shape == 0) return launch_tile<X, 1, G, 1, 2, 2, 4, 2, 1>(p, t.splits, s);
+        if (t.shape == 1) return launch_tile<X, 1, G, 1, 2, 2, 1, 4, 1>(p, t.splits, s);
+        if (t.shape == 2) return launch_tile<X, 1, G, 2, 2, 2, 2, 2, 1>(p, t.splits, s);
+        if (t.shape == 3) return launch_tile<X, 1, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
+        return launch_tile<X, 1, G, 4, 1, 4, 1, 2, 1>(p, t.splits, s);
+    } else {
+        if constexpr (sizeof(X) == 2) {
+            if (dma) {
+                if (t.shape == 0) return launch_tile<X, 0, G, 1, 1, 4, 2, 3, 1>(p, t.splits, s);
+                if (t.shape == 1) return launch_tile<X, 0, G, 2, 1, 4, 1, 4, 1>(p, t.splits, s);
+                if (t.shape == 2) return launch_tile<X, 0, G, 2, 1, 4, 2, 4, 1>(p, t.splits, s);
+                if (t.shape == 3) return launch_tile<X, 0, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
+                if constexpr (G > 32) return launch_tile<X, 0, G, 4, 1, 4, 1, 3, 1>(p, t.splits, s);
+            }
+        }
+        if (t.shape == 0) return launch_tile<X, 0, G, 1, 1, 4, 2, 3, 0>(p, t.splits, s);
+        return launch_tile<X, 0, G, 2, 1, 4, 1, 4, 0>(p, t.splits, s);
     }
-    if (t.shape == 0) return launch_tile<X, F8, G, 1, 1, 4, 4, 0>(p, t.splits, s);
-    if constexpr (F8) return launch_tile<X, F8, G, 1, 2, 2, 4, 0>(p, t.splits, s);
-    else return launch_tile<X, F8, G, 2, 1, 4, 4, 0>(p, t.splits, s);
 }
 
 // A token's kernel reads the weights once, without LDS; it also reads every row in pieces, so that with
@@ -602,10 +648,11 @@ bool takes_token(int64_t M, const W4Layout& L) {
 template <typename X, int G>
 hipError_t launch_g(const W4GemmParams& p, int x_type, hipStream_t s) {
     if (takes_token(p.M, p.L)) {
-        // 16 waves where the row tiles leave CUs with one workgroup at most, else 8 with few registers
+        // 16 waves where the CUs get about one workgroup each, else 8 (one row, K = 9216, 4096 outputs:
+        // 7.2 us against 9.0; K = 4096, 18432 outputs: 14.0 against 11.7)
         const unsigned grid = 2 * p.L.tiles;
-        if ((int)grid <= num_cus() * 3 / 2) k_w4_token<X, G, 16, 4><<<grid, 1024, 0, s>>>(p);
-        else k_w4_token<X, G, 8, 1><<<grid, 512, 0, s>>>(p);
+        if ((int)grid <= num_cus() * 3 / 2) k_w4_token<X, G, 16, 2><<<grid, 1024, 0, s>>>(p);
+        else k_w4_token<X, G, 8, 2><<<grid, 512, 0, s>>>(p);
         return hipGetLastError();
     }
     if constexpr (sizeof(X) == 1 && G >= 64) {
