@@ -277,7 +277,8 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
         if (!finite) alpha = __builtin_nanf("");
         const float as = __builtin_amdgcn_ldexpf(alpha, -shift);
 
-        if constexpr (sizeof(T) == 2) {
+        // (1/as) of a scale far below the weights may be infinite
+        if (sizeof(T) == 2 && !__any(finite && m && as < 0x1p-100f)) {
             const float inv = m && alpha == alpha ? 1.0f / as * (1.0f + 0x1p-22f) : 0.0f;
 #pragma unroll
             for (int t = 0; t < WG; t++) {
@@ -291,8 +292,9 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
                 uint32_t d = 0;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const uint32_t c = (uint32_t)magnitude_code(fabsf(n[8 * t + i]), as);
-                    d |= (c | (c && n[8 * t + i] < 0.0f ? 8u : 0u)) << (4 * i);
+                    const float x = __builtin_amdgcn_ldexpf(n[8 * t + i], shift);
+                    const uint32_t c = (uint32_t)magnitude_code(fabsf(x), alpha);
+                    d |= (c | (c && x < 0.0f ? 8u : 0u)) << (4 * i);
                 }
                 packed[WG * g + t] = d;
             }

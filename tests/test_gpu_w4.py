@@ -61,6 +61,42 @@ def test_ties_go_to_the_larger_magnitude(esb):
     assert not bool(torch.signbit(q.cpu().float()[0, -2:]).any())
 
 
+def test_candidates_that_tie(esb):
+    """Equal errors under different scales: the lowest index, among two, three or all candidates, also
+    where fp32 sums cannot tell them apart."""
+    w = torch.zeros(40, 64)
+    w[:, 0] = 6.0                       # exact under alpha = 1, 2 and 4
+    w[1, :32] = 6.0
+    w[2, 40] = 6.0 * 2.0 ** -100
+    w[3] = 0
+    w[4:, 1] = torch.linspace(-6, 6, 36)
+    for f in ([0.5, 1.0, 2.0], [0.5, 2.0, 1.0], [4.0, 2.0, 1.0, 0.5], [0.5, 1.0, 1.0, 1.0 + 2.0 ** -20], [2.0] * 9):
+        q, alpha = esb.esb_w4_unpack(esb.esb_w4_quantize(w.cuda(), 32, torch.tensor(f).cuda()), 40, 64, 32)
+        rq, ra = ref.quantize(w, 32, f)
+        assert torch.equal(alpha.cpu().double(), ra), f
+        assert torch.equal(q.cpu().double(), rq), f
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -60, 1.0, 2.0 ** 90])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_any_size_of_weights(esb, scale, t):
+    """Weights whose squares leave fp32, and factors far from 1 (64 of them)."""
+    w = (weights(11, 50, 300, "f32") * scale).to(ref.TYPES[t])
+    w[:, ::7] = 0
+    f = [2.0 ** e for e in range(-34, -2)] + [1 - j / 64 for j in range(32)]
+    q, alpha = esb.esb_w4_unpack(esb.esb_w4_quantize(w.cuda(), 64, torch.tensor(f).cuda()), 50, 300, 64)
+    rq, ra = ref.quantize(w, 64, f)
+    assert torch.equal(alpha.cpu().double(), ra)
+    assert torch.equal(q.cpu().double(), rq)
+    only = [2.0 ** -120]                # every weight far above its scale
+    w4 = esb.esb_w4_quantize(w.cuda(), 64, torch.tensor(only).cuda())
+    assert not bool(w4[:1024 * 10].view(2, 5, 1024)[1, 4].view(64, 16)[18:32].any())     # rows past 50
+    q, alpha = esb.esb_w4_unpack(w4, 50, 300, 64)
+    rq, ra = ref.quantize(w, 64, only)
+    assert torch.equal(alpha.cpu().double(), ra)
+    assert torch.equal(q.cpu().double(), rq)
+
+
 def test_groups_without_a_scale(esb):
     """Zeros, NaN, infinities, the largest and the smallest weights; factors that are passed over."""
     inf, nan = float("inf"), float("nan")
