@@ -819,12 +819,13 @@ int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int 
     if (st) return st;
     if (ldx < K || ldy < N) return ESB_E_INVALID;
     if (M == 0 || N == 0) return ESB_OK;
-    if (!y || !aligned_for(y, y_type) || (uintptr_t)workspace % 32) return ESB_E_INVALID;
+    if (!y || !aligned_for(y, y_type) || (uintptr_t)workspace % 256) return ESB_E_INVALID;
     if (K > 0 && (!x || !aligned_for(x, x_type) || (uintptr_t)x_scale % 4 || !w4 || (uintptr_t)w4 % 16))
         return ESB_E_INVALID;
     const W4Layout L = w4_layout(N, K, group);
     if (workspace && ws_bytes < w4_gemm_workspace(M, L, x_type, y_type)) return ESB_E_WORKSPACE;
-    const W4GemmParams p = {L, M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type, (float*)workspace};
+    const W4GemmParams p = {L, M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type,
+                            workspace, ws_bytes, nullptr, nullptr, false};
     return hip_status(launch_w4_gemm(p, x_type, (hipStream_t)stream));
 }
 

@@ -613,9 +613,14 @@ struct W4GemmParams {
     void* y;
     int64_t ldy;
     int y_type;
+    void* ws;               // the caller's workspace, or NULL
+    size_t ws_bytes;
+    // filled by launch_w4_gemm from it:
     float* part;            // room for the sums of column ranges, [range][M][32 tiles], or NULL
+    uint8_t* align;         // room for aligned rows, or NULL
+    bool aligned;           // x is aligned, its last pieces are filled with zeros
 };
-// Bytes of p.part for these arguments (0: no split).
+// Bytes of workspace that these arguments may use.
 size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type);
 hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s);
 

@@ -488,6 +488,24 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
     });
 }
 
+// Rows that DMA cannot take, once into aligned ones with whole 64-column pieces (zeros past K); E4M3 rows
+// for the bf16 MFMAs (TO == 2) are converted.
+template <typename X, int TO>
+__global__ __launch_bounds__(256) void k_w4_align(W4GemmParams p, uint8_t* __restrict__ out, int pieces) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = i / pieces;
+    if (m >= p.M) return;
+    constexpr int EP = 16 / TO;
+    const int k = EP * (int)(i - m * pieces);
+    const X* x = (const X*)p.x + m * p.ldx + k;
+    if constexpr (EP == 16) {
+        const uint2 lo = Act<X>::load(x, p.L.K - k), hi = Act<X>::load(x + 8, p.L.K - k - 8);
+        *(uint4*)(out + 16 * i) = uint4{lo.x, lo.y, hi.x, hi.y};
+    } else {
+        *(typename Act<X>::M::frag*)(out + 16 * i) = Act<X>::frag(Act<X>::load(x, p.L.K - k));
+    }
+}
+
 // y from the sums of the column ranges, added in order.
 __global__ __launch_bounds__(256) void k_w4_sum(W4GemmParams p, int splits) {
     const int64_t np = 32 * (int64_t)p.L.tiles, cols = np / 8;
@@ -504,29 +522,6 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4GemmParams p, int splits) {
         typedef std::remove_reference_t<decltype(*y)> Y;
         store8(y + m * p.ldy + n, __builtin_convertvector(v, typename Vec8<Y>::type), p.L.N - n);
     });
-}
-
-template <typename X, int F8, int G, int TM, int WM, int WN, int R>
-hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
-    const int tm = (int)((p.M + 32 * TM * WM - 1) / (32 * TM * WM)), tn = (p.L.tiles + 2 * WN - 1) / (2 * WN);
-    const int es = sizeof(X), steps = F8 ? (p.L.chunks + 1) / 2 : p.L.chunks;
-    const int gm = 4;
-    const int per = (steps + splits - 1) / splits;
-    splits = (steps + per - 1) / per;
-    W4GemmParams q = p;
-    if (splits <= 1) q.part = nullptr;
-    const bool aligned = (uintptr_t)p.x % 16 == 0 && p.ldx * es % 16 == 0 && (int64_t)p.L.K * es % 16 == 0;
-    const unsigned grid = (unsigned)tm * tn * splits;
-    if ((F8 || es == 2) && aligned)
-        k_w4_tile<X, F8, G, TM, WM, WN, R, F8 || sizeof(X) == 2><<<grid, 64 * WM * WN, 0, s>>>(q, tm, tm * tn, gm, per);
-    else
-        k_w4_tile<X, F8, G, TM, WM, WN, R, 0><<<grid, 64 * WM * WN, 0, s>>>(q, tm, tm * tn, gm, per);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && splits > 1) {
-        k_w4_sum<<<(unsigned)((p.M * p.L.tiles * 4 + 255) / 256), 256, 0, s>>>(p, splits);
-        e = hipGetLastError();
-    }
-    return e;
 }
 
 // The shapes of k_w4_tile and what a step of theirs costs, us on one CU holding 1 .. slots of its
@@ -590,6 +585,7 @@ bool takes_f8(int x_type, int y_type, int group) { return x_type == kE4M3 && y_t
 // conversion on its way.
 bool takes_dma(const W4GemmParams& p, int x_type, bool f8) {
     const int es = x_type == kE4M3 ? 1 : 2;
+    if (p.aligned) return true;
     return (f8 || es == 2) && (uintptr_t)p.x % 16 == 0 && p.ldx * es % 16 == 0 && (int64_t)p.L.K * es % 16 == 0;
 }
 
@@ -609,8 +605,39 @@ hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
     return e;
 }
 
+// From so many rows on, rows that DMA cannot take are aligned first, where there is room for them (4000
+// outputs of K = 4001, us aligned first and not: bf16 64 rows 17.8 / 16.9, 512 rows 31.1 / 36.7, 4000 rows
+// 135 / 153; E4M3 64 rows 15.0 / 15.2, 128 rows 16.8 / 20.2, 4000 rows 74 / 123).
+constexpr int64_t kAlignRows = 128;
+int64_t aligned_pitch(const W4Layout& L) { return 64 * (int64_t)L.chunks; }      // elements
+
+// What of a workspace the sums of column ranges take, the largest of the two alignments' plans.
+size_t part_bytes(int64_t M, const W4Layout& L, bool f8) {
+    size_t most = 0;
+    for (bool dma : {false, true}) {        // the call knows the alignment, its caller need not
+        const TilePlan t = tile_plan(M, L, f8, dma, true);
+        const size_t b = t.splits > 1 ? (size_t)t.splits * M * L.tiles * 32 * 4 : 0;
+        most = b > most ? b : most;
+    }
+    return most;
+}
+
 template <typename X, int F8, int G>
 hipError_t launch_shape(const W4GemmParams& p, int x_type, hipStream_t s) {
+    if (!takes_dma(p, x_type, F8) && p.align && p.M >= kAlignRows) {
+        constexpr int to = F8 ? 1 : 2;
+        W4GemmParams q = p;
+        q.x = p.align;
+        q.ldx = aligned_pitch(p.L);
+        q.align = nullptr;
+        q.aligned = true;                    // pieces that K cuts hold zeros past it
+        const int pieces = (int)(q.ldx * to / 16);
+        k_w4_align<X, to><<<(unsigned)((p.M * pieces + 255) / 256), 256, 0, s>>>(p, (uint8_t*)p.align, pieces);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if constexpr (sizeof(X) == 1 && !F8) return launch_shape<__bf16, 0, G>(q, kBF16, s);
+        else return launch_shape<X, F8, G>(q, x_type, s);
+    }
     const bool dma = takes_dma(p, x_type, F8);
     const TilePlan t = tile_plan(p.M, p.L, F8, dma, p.part != nullptr);
     if constexpr (F8) {
@@ -672,22 +699,27 @@ hipError_t launch_x(const W4GemmParams& p, int x_type, hipStream_t s) {
 
 size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type) {
     M = M < kRowsOfALaunch ? M : kRowsOfALaunch;
-    if (takes_token(M, L)) return 0;
-    size_t most = 0;
+    if (L.K == 0 || takes_token(M, L)) return 0;
     const bool f8 = takes_f8(x_type, y_type, L.group);
-    for (bool dma : {false, true}) {        // the call knows the alignment, its caller need not
-        const TilePlan t = tile_plan(M, L, f8, dma, true);
-        const size_t b = t.splits > 1 ? (size_t)t.splits * M * L.tiles * 32 * 4 : 0;
-        most = b > most ? b : most;
-    }
-    return most;
+    const size_t part = (part_bytes(M, L, f8) + 255) / 256 * 256;
+    // rows of whole 16-byte pieces are expected to be aligned; others cannot be
+    const int es = x_type == kE4M3 ? 1 : 2;
+    const bool align = M >= kAlignRows && ((int64_t)L.K * es % 16 != 0 || (es == 1 && !f8));
+    return part + (align ? (size_t)M * aligned_pitch(L) * (f8 ? 1 : 2) : 0);
 }
 
 hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s) {
     const int xs = x_type == kE4M3 ? 1 : 2, ys = p.y_type == kF32 ? 4 : 2;
+    const int64_t rows = p.M < kRowsOfALaunch ? p.M : kRowsOfALaunch;
+    const bool f8 = takes_f8(x_type, p.y_type, p.L.group);
+    const size_t part = p.ws ? (part_bytes(rows, p.L, f8) + 255) / 256 * 256 : 0;
+    const size_t align = (size_t)rows * aligned_pitch(p.L) * (f8 ? 1 : 2);
     for (int64_t m = 0; m < p.M; m += kRowsOfALaunch) {
         W4GemmParams q = p;
         q.M = p.M - m < kRowsOfALaunch ? p.M - m : kRowsOfALaunch;
+        q.part = p.ws && p.ws_bytes >= part ? (float*)p.ws : nullptr;
+        q.align = p.ws && p.ws_bytes >= part + align ? (uint8_t*)p.ws + part : nullptr;
+        q.aligned = false;
         q.x = (const char*)p.x + m * p.ldx * xs;
         if (p.x_scale) q.x_scale = p.x_scale + m;
         q.y = (char*)p.y + m * p.ldy * ys;

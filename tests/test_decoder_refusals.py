@@ -92,7 +92,7 @@ def test_products(L):
     assert gemm(t=F32) == UNSUPPORTED
     for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(g=0), dict(ldx=199), dict(ldy=39), dict(t=4),
                 dict(yt=E4M3), dict(x=None), dict(w4=None), dict(y=None), dict(x=ODD), dict(y=ODD), dict(s=ODD),
-                dict(w4=ctypes.c_void_p(0x1004)), dict(ws=ctypes.c_void_p(0x1010), wb=1 << 30)):
+                dict(w4=ctypes.c_void_p(0x1004)), dict(ws=ctypes.c_void_p(0x1020), wb=1 << 30)):
         assert gemm(**bad) == INVALID, bad
     assert gemm(N=(1 << 31) - 1, ldy=1 << 40) == UNSUPPORTED
     assert gemm(M=0, x=None, y=None) == 0 and gemm(N=0, y=None) == 0
@@ -102,4 +102,5 @@ def test_products(L):
     big = dict(M=64, N=4096, K=4096, g=128, ldx=4096, ldy=4096, ws=FAKE)
     assert gemm(**big, wb=need - 1) == WORKSPACE
     assert size(1, 4096, 4096, 128, BF16, BF16) == 0 and size(4096, 18432, 4096, 128, E4M3, BF16) == 0
+    assert size(2000, 4000, 4001, 64, BF16, BF16) >= 2000 * 4001 * 2       # rows to be aligned
     assert size(64, 4096, 4096, 100, BF16, BF16) == 0 and size(64, 4096, 4096, 128, F32, BF16) == 0

@@ -180,6 +180,30 @@ def test_weights_beyond_32_bits(esb):
         check(y[:, N - 32:], xv, s, codes, alpha, group)
 
 
+@pytest.mark.parametrize("M,N,K,x,group", [(20, 300, 520, "bf16", 64), (64, 512, 2048, "f16", 32),
+                                           (130, 257, 333, "bf16", 128), (150, 300, 777, "e4m3", 128),
+                                           (140, 200, 640, "e4m3", 32)])
+def test_with_and_without_workspace(esb, M, N, K, x, group):
+    """The C entry without a workspace, and with one full of NaN: both right, nothing written past it."""
+    L = esb.lib()
+    xv, s = acts(M, M, K, x)
+    xd, sd = xv.cuda(), None if s is None else s.cuda()
+    codes, alpha = weights(N, N, K, group)
+    w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), group)
+    tx = {"bf16": 1, "f16": 2, "e4m3": 3}[x]
+    need = L.esb_w4_gemm_workspace_size(M, N, K, group, tx, 1)
+    for ws in (None, torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")):
+        if ws is not None and need == 0:
+            continue
+        y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+        st = L.esb_w4_gemm(M, N, K, group, xd.data_ptr(), K, tx, None if sd is None else sd.data_ptr(),
+                           w4.data_ptr(), y.data_ptr(), N, 1, None if ws is None else ws.data_ptr(), need,
+                           torch.cuda.current_stream().cuda_stream)
+        assert st == 0
+        check(y, xv, s, codes, alpha, group)
+        assert ws is None or bool((ws[need:] == 0xFF).all())
+
+
 def test_empty(esb):
     codes, alpha = weights(1, 20, 64, 32)
     w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), 32)
