@@ -825,7 +825,7 @@ int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int 
     const W4Layout L = w4_layout(N, K, group);
     if (workspace && ws_bytes < w4_gemm_workspace(M, L, x_type, y_type)) return ESB_E_WORKSPACE;
     const W4GemmParams p = {L, M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type,
-                            workspace, ws_bytes, nullptr, nullptr, false};
+                            (uint8_t*)workspace, workspace ? ws_bytes : 0, false, nullptr};
     return hip_status(launch_w4_gemm(p, x_type, (hipStream_t)stream));
 }
 

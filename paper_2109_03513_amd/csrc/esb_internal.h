@@ -613,12 +613,10 @@ struct W4GemmParams {
     void* y;
     int64_t ldy;
     int y_type;
-    void* ws;               // the caller's workspace, or NULL
+    uint8_t* ws;            // the caller's workspace, or NULL (0 bytes)
     size_t ws_bytes;
-    // filled by launch_w4_gemm from it:
-    float* part;            // room for the sums of column ranges, [range][M][32 tiles], or NULL
-    uint8_t* align;         // room for aligned rows, or NULL
-    bool aligned;           // x is aligned, its last pieces are filled with zeros
+    bool aligned;           // x was aligned by the call: its last pieces are filled with zeros
+    float* part;            // sums of column ranges, [range][M][32 tiles], or NULL: no ranges
 };
 // Bytes of workspace that these arguments may use.
 size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type);

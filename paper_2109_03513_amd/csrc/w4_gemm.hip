@@ -547,11 +547,14 @@ constexpr TileShape kShapes8[kShapes] = {{64, 128, 1, {0.35f}},
 
 // The shape and the ranges of columns (splits) that should take the least time: rounds of full CUs,
 // then one of what is left; splits write and read fp32 sums at about 4 TB/s and launch one more kernel.
-// DMA == 0 has the first two.  part: whether there is room for the sums of two ranges or more.
+// DMA == 0 has the first two.  room: bytes for the sums.
 struct TilePlan {
     int shape, splits;
 };
-TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, bool part) {
+size_t sums_bytes(int64_t M, const W4Layout& L, int splits) {
+    return splits > 1 ? (size_t)splits * M * L.tiles * 32 * 4 : 0;
+}
+TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, size_t room) {
     const int steps = f8 ? (L.chunks + 1) / 2 : L.chunks;
     const double cus = num_cus();
     TilePlan best = {0, 1};
@@ -562,7 +565,8 @@ TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, bool part) {
         const TileShape& s = f8 ? kShapes8[v] : kShapes16[v];
         const double tiles = (double)((M + s.bm - 1) / s.bm) * ((L.N + s.bn - 1) / s.bn);
         for (int z : {1, 2, 3, 4, 6, 8}) {
-            if (z > 1 && (!part || steps < 4 * z)) break;
+            if (steps < 4 * z && z > 1) break;
+            if (sums_bytes(M, L, z) > room) break;
             const double held = ceil(tiles * z / cus), rounds = floor((held - 1) / s.slots);
             const int rest = (int)(held - rounds * s.slots);
             double us = (rounds * s.step[s.slots - 1] + s.step[rest - 1]) * ceil((double)steps / z);
@@ -595,11 +599,11 @@ hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
     const int steps = F8 ? (p.L.chunks + 1) / 2 : p.L.chunks, per = steps ? (steps + splits - 1) / splits : 0;
     splits = steps ? (steps + per - 1) / per : 1;
     W4GemmParams q = p;
-    if (splits == 1) q.part = nullptr;
+    q.part = splits > 1 ? (float*)p.ws : nullptr;
     k_w4_tile<X, F8, G, TM, WM, WN, KW, R, DMA><<<(unsigned)(tm * tn * splits), 64 * WM * WN * KW, 0, s>>>(q, tm, tm * tn, per);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && splits > 1) {
-        k_w4_sum<<<(unsigned)((p.M * p.L.tiles * 4 + 255) / 256), 256, 0, s>>>(p, splits);
+        k_w4_sum<<<(unsigned)((p.M * p.L.tiles * 4 + 255) / 256), 256, 0, s>>>(q, splits);
         e = hipGetLastError();
     }
     return e;
@@ -610,36 +614,28 @@ hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
 // 135 / 153; E4M3 64 rows 15.0 / 15.2, 128 rows 16.8 / 20.2, 4000 rows 74 / 123).
 constexpr int64_t kAlignRows = 128;
 int64_t aligned_pitch(const W4Layout& L) { return 64 * (int64_t)L.chunks; }      // elements
-
-// What of a workspace the sums of column ranges take, the largest of the two alignments' plans.
-size_t part_bytes(int64_t M, const W4Layout& L, bool f8) {
-    size_t most = 0;
-    for (bool dma : {false, true}) {        // the call knows the alignment, its caller need not
-        const TilePlan t = tile_plan(M, L, f8, dma, true);
-        const size_t b = t.splits > 1 ? (size_t)t.splits * M * L.tiles * 32 * 4 : 0;
-        most = b > most ? b : most;
-    }
-    return most;
-}
+size_t aligned_bytes(int64_t M, const W4Layout& L, bool f8) { return (size_t)M * aligned_pitch(L) * (f8 ? 1 : 2); }
 
 template <typename X, int F8, int G>
 hipError_t launch_shape(const W4GemmParams& p, int x_type, hipStream_t s) {
-    if (!takes_dma(p, x_type, F8) && p.align && p.M >= kAlignRows) {
+    const bool dma = takes_dma(p, x_type, F8);
+    const size_t copy = aligned_bytes(p.M, p.L, F8);
+    if (!dma && p.M >= kAlignRows && p.ws_bytes >= copy) {
         constexpr int to = F8 ? 1 : 2;
         W4GemmParams q = p;
-        q.x = p.align;
+        q.x = p.ws;
         q.ldx = aligned_pitch(p.L);
-        q.align = nullptr;
         q.aligned = true;                    // pieces that K cuts hold zeros past it
+        q.ws = p.ws + copy;
+        q.ws_bytes = p.ws_bytes - copy;
         const int pieces = (int)(q.ldx * to / 16);
-        k_w4_align<X, to><<<(unsigned)((p.M * pieces + 255) / 256), 256, 0, s>>>(p, (uint8_t*)p.align, pieces);
+        k_w4_align<X, to><<<(unsigned)((p.M * pieces + 255) / 256), 256, 0, s>>>(p, p.ws, pieces);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if constexpr (sizeof(X) == 1 && !F8) return launch_shape<__bf16, 0, G>(q, kBF16, s);
         else return launch_shape<X, F8, G>(q, x_type, s);
     }
-    const bool dma = takes_dma(p, x_type, F8);
-    const TilePlan t = tile_plan(p.M, p.L, F8, dma, p.part != nullptr);
+    const TilePlan t = tile_plan(p.M, p.L, F8, dma, p.ws_bytes);
     if constexpr (F8) {
         if (!dma) {
             if (t.shape == 0) return launch_tile<X, 1, G, 1, 2, 2, 4, 2, 0>(p, t.splits, s);
@@ -701,25 +697,17 @@ size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type) {
     M = M < kRowsOfALaunch ? M : kRowsOfALaunch;
     if (L.K == 0 || takes_token(M, L)) return 0;
     const bool f8 = takes_f8(x_type, y_type, L.group);
-    const size_t part = (part_bytes(M, L, f8) + 255) / 256 * 256;
     // rows of whole 16-byte pieces are expected to be aligned; others cannot be
     const int es = x_type == kE4M3 ? 1 : 2;
-    const bool align = M >= kAlignRows && ((int64_t)L.K * es % 16 != 0 || (es == 1 && !f8));
-    return part + (align ? (size_t)M * aligned_pitch(L) * (f8 ? 1 : 2) : 0);
+    const bool dma = (f8 || es == 2) && (int64_t)L.K * es % 16 == 0, copy = !dma && M >= kAlignRows;
+    return (copy ? aligned_bytes(M, L, f8) : 0) + sums_bytes(M, L, tile_plan(M, L, f8, dma || copy, SIZE_MAX).splits);
 }
 
 hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s) {
     const int xs = x_type == kE4M3 ? 1 : 2, ys = p.y_type == kF32 ? 4 : 2;
-    const int64_t rows = p.M < kRowsOfALaunch ? p.M : kRowsOfALaunch;
-    const bool f8 = takes_f8(x_type, p.y_type, p.L.group);
-    const size_t part = p.ws ? (part_bytes(rows, p.L, f8) + 255) / 256 * 256 : 0;
-    const size_t align = (size_t)rows * aligned_pitch(p.L) * (f8 ? 1 : 2);
     for (int64_t m = 0; m < p.M; m += kRowsOfALaunch) {
         W4GemmParams q = p;
         q.M = p.M - m < kRowsOfALaunch ? p.M - m : kRowsOfALaunch;
-        q.part = p.ws && p.ws_bytes >= part ? (float*)p.ws : nullptr;
-        q.align = p.ws && p.ws_bytes >= part + align ? (uint8_t*)p.ws + part : nullptr;
-        q.aligned = false;
         q.x = (const char*)p.x + m * p.ldx * xs;
         if (p.x_scale) q.x_scale = p.x_scale + m;
         q.y = (char*)p.y + m * p.ldy * ys;
