@@ -720,11 +720,11 @@ def _row_outputs(x, rows, d, index, y, want_y, y8, scale, want_y8):
     if y is not None:
         ldy = _like(y, "y", rows, d, x.dtype, index)
     elif want_y:
-        y = x.new_empty((rows, d))
+        y = x.new_empty(rows, d)
     if y8 is not None:
         ld8 = _like(y8, "y8", rows, d, _torch.float8_e4m3fn, index)
     elif want_y8:
-        y8 = x.new_empty((rows, d), dtype=_torch.float8_e4m3fn)
+        y8 = x.new_empty(rows, d, dtype=_torch.float8_e4m3fn)
     if y8 is not None:
         if scale is None:
             scale = x.new_empty(rows, dtype=_torch.float32)
@@ -751,7 +751,7 @@ def esb_rmsnorm(x, w, eps, residual=None, sum_out=None, want_sum=False, y=None, 
     if sum_out is not None:
         lds = _like(sum_out, "sum_out", rows, d, x.dtype, index)
     elif want_sum:
-        sum_out, lds = x.new_empty((rows, d)), d
+        sum_out, lds = x.new_empty(rows, d), d
     y, ldy, y8, ld8, scale = _row_outputs(x, rows, d, index, y, want_y, y8, scale, want_y8)
     st = L.esb_rmsnorm(x.data_ptr(), ldx, _addr(residual), ldr, t, rows, d, _addr(w), eps,
                        _addr(sum_out), lds, _addr(y), ldy, _addr(y8), ld8, _addr(scale),
@@ -845,11 +845,11 @@ def esb_w4_unpack(w4, N, K, group, values=None, alpha=None, stream=None):
     groups = -(-K // group) if group > 0 else 0
     ldv, lda = K, groups
     if values is None:
-        values = w4.new_empty((N, K), dtype=_torch.float8_e4m3fn)
+        values = w4.new_empty(N, K, dtype=_torch.float8_e4m3fn)
     else:
         ldv = _like(values, "values", N, K, _torch.float8_e4m3fn, index)
     if alpha is None:
-        alpha = w4.new_empty((N, groups), dtype=_torch.bfloat16)
+        alpha = w4.new_empty(N, groups, dtype=_torch.bfloat16)
     else:
         lda = _like(alpha, "alpha", N, groups, _torch.bfloat16, index)
     st = L.esb_w4_unpack(w4.data_ptr(), N, K, group, values.data_ptr(), ldv, alpha.data_ptr(), lda,
@@ -880,7 +880,7 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=N
         if y_dtype is None:
             y_dtype = _torch.bfloat16 if tx == ESB_E4M3 else x.dtype
         ty = _type(y_dtype, "y", _FLOATS)
-        y = x.new_empty((M, N), dtype=y_dtype)
+        y = x.new_empty(M, N, dtype=y_dtype)
     else:
         ty = _type(y, "y", _FLOATS)
         ldy = _like(y, "y", M, N, y_dtype or y.dtype, index)
