@@ -66,11 +66,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows(RowsParams p) {
 #pragma unroll
         for (int u = 0; u < AHEAD; u++) {
             const int e = 8 * ((u0 + u) * TPR + tid);
+            v[u0 + u] = f32x8{};
+            if (e >= d) continue;
             f32x8 x = __builtin_convertvector(ra[u], f32x8);
             const f32x8 y = __builtin_convertvector(rb[u], f32x8);
             if (OP == kRowsNorm) {
                 if (b) x += y;
-                if (p.sum && e < d) store8((T*)p.sum + row * p.lds + e, __builtin_convertvector(x, V), d - e);
+                if (p.sum) store8((T*)p.sum + row * p.lds + e, __builtin_convertvector(x, V), d - e);
 #pragma unroll
                 for (int i = 0; i < 8; i++) ss = fma((double)x[i], (double)x[i], ss);
             } else {

@@ -226,7 +226,9 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
         for (int c = 0; c < nf; c++) {
             const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fs), c));
             if (!(f > 0.0f) || !(f < __builtin_inff())) continue;
-            const float a = bf16_round(fmaxf(top * f / 6.0f, kTiny));
+            // x / 6 rounded correctly: the product with the reciprocal, corrected by its exact remainder
+            const float x6 = top * f, q6 = x6 * (1.0f / 6.0f), d6 = fmaf(fmaf(-6.0f, q6, x6), 1.0f / 6.0f, q6);
+            const float a = bf16_round(fmaxf(d6, kTiny));
             const float as = m ? __builtin_amdgcn_ldexpf(a, -shift) : 1.0f;
             const float inv = __builtin_amdgcn_rcpf(as);
             far |= as < 0x1p-100f;
@@ -246,24 +248,16 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
                     sum[i] = fmaf(e, e, sum[i]);
                 }
             }
-            const float err = row_sum<G>(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
+            float err = row_sum<G>(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
             // a candidate that overflows is passed over; one equal to a kept one adds nothing
-            if (!(a < inf) || a == alpha || a == other) continue;
-            if (err < least) {
-                third = second;
-                second = least;
-                other = alpha;
-                other_first = true;
-                least = err;
-                alpha = a;
-            } else if (err < second) {
-                third = second;
-                second = err;
-                other = a;
-                other_first = false;
-            } else {
-                third = fminf(third, err);
-            }
+            err = x6 < inf && a != alpha && a != other ? err : inf;
+            const bool first = err < least, next = err < second;
+            other = first ? alpha : next ? a : other;
+            other_first = first || (other_first && !next);
+            alpha = first ? a : alpha;
+            third = fminf(third, fmaxf(second, err));
+            second = __builtin_amdgcn_fmed3f(least, second, err);
+            least = fminf(least, err);
         }
         const float near = least * (1.0f + 0x1p-19f);
         if (__any(finite && m && (far || third <= near))) {
