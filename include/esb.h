@@ -553,7 +553,7 @@ int esb_swiglu(const void* gate, int64_t ldg, const void* up, int64_t ldu, int t
  * esb_w4_unpack: the unscaled values as E4M3 bytes (exact; N x K) and / or the scales (bf16,
  *   N x ceil(K / group)); either may be NULL.
  * Errors: ESB_E_WORKSPACE when w4_bytes is less than esb_w4_size; ESB_E_UNSUPPORTED above 2^26
- * rows or 2^25 tiles.  N == 0 or K == 0 enqueues nothing.
+ * rows, 2^30 columns or 2^25 tiles.  N == 0 or K == 0 enqueues nothing.
  */
 size_t esb_w4_size(int N, int K, int group);
 int esb_w4_quantize(const void* w, int64_t ldw, int type, int N, int K, int group,

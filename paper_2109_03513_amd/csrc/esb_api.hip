@@ -752,11 +752,11 @@ int esb_swiglu(const void* gate, int64_t ldg, const void* up, int64_t ldu, int t
     return hip_status(launch_rows(kRowsGated, type, p, (hipStream_t)stream));
 }
 
-// Launches count tiles in 32 bits: up to 2^21 row tiles and 2^25 tiles of 1 KB.
+// Launches count tiles and columns in 32 bits: up to 2^21 row tiles, 2^25 tiles of 1 KB, 2^30 columns.
 static int w4_check(int N, int K, int group) {
     if (N < 0 || K < 0 || (group != 32 && group != 64 && group != 128)) return ESB_E_INVALID;
     const int64_t tiles = ((int64_t)N + 31) / 32, chunks = ((int64_t)K + 63) / 64;
-    if (tiles > (1 << 21) || tiles * chunks > (1 << 25)) return ESB_E_UNSUPPORTED;
+    if (tiles > (1 << 21) || K > (1 << 30) || tiles * chunks > (1 << 25)) return ESB_E_UNSUPPORTED;
     return ESB_OK;
 }
 

@@ -681,6 +681,14 @@ def _type(t, name, allowed):
 _FLOATS = (ESB_F32, ESB_BF16, ESB_F16)
 
 
+def _on(stream):
+    """Context in which `stream` (an object or a handle) is the current one: what a call allocates
+    then belongs to the stream that uses it."""
+    if isinstance(stream, int):
+        stream = _torch.cuda.ExternalStream(stream)
+    return _torch.cuda.stream(stream)
+
+
 def _matrix(t, name):
     """(rows, columns, pitch) of a device matrix whose columns are adjacent; rows may be apart."""
     if not isinstance(t, _torch.Tensor) or not t.is_cuda:
@@ -740,6 +748,9 @@ def esb_rmsnorm(x, w, eps, residual=None, sum_out=None, want_sum=False, y=None, 
     Returns (sum, y, y8, scale): z and y in x's type, and y as float8_e4m3fn under one fp32 scale
     per row; what is neither given nor wanted is None."""
     L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_rmsnorm(x, w, eps, residual, sum_out, want_sum, y, want_y, y8, scale, want_y8)
     rows, d, ldx = _matrix(x, "x")
     t = _type(x, "x", _FLOATS)
     index = x.get_device()
@@ -755,7 +766,7 @@ def esb_rmsnorm(x, w, eps, residual=None, sum_out=None, want_sum=False, y=None, 
     y, ldy, y8, ld8, scale = _row_outputs(x, rows, d, index, y, want_y, y8, scale, want_y8)
     st = L.esb_rmsnorm(x.data_ptr(), ldx, _addr(residual), ldr, t, rows, d, _addr(w), eps,
                        _addr(sum_out), lds, _addr(y), ldy, _addr(y8), ld8, _addr(scale),
-                       _stream(stream))
+                       _stream(None))
     if st:
         raise EsbError("esb_rmsnorm", st)
     return sum_out, y, y8, scale
@@ -764,13 +775,16 @@ def esb_rmsnorm(x, w, eps, residual=None, sum_out=None, want_sum=False, y=None, 
 def esb_swiglu(gate, up, y=None, want_y=False, y8=None, scale=None, want_y8=True, stream=None):
     """gate / (1 + exp(-gate)) * up, rows x d; returns (y, y8, scale) as esb_rmsnorm does."""
     L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_swiglu(gate, up, y, want_y, y8, scale, want_y8)
     rows, d, ldg = _matrix(gate, "gate")
     t = _type(gate, "gate", _FLOATS)
     index = gate.get_device()
     ldu = _like(up, "up", rows, d, gate.dtype, index)
     y, ldy, y8, ld8, scale = _row_outputs(gate, rows, d, index, y, want_y, y8, scale, want_y8)
     st = L.esb_swiglu(gate.data_ptr(), ldg, up.data_ptr(), ldu, t, rows, d, _addr(y), ldy, _addr(y8),
-                      ld8, _addr(scale), _stream(stream))
+                      ld8, _addr(scale), _stream(None))
     if st:
         raise EsbError("esb_swiglu", st)
     return y, y8, scale
@@ -806,6 +820,9 @@ def esb_w4_quantize(w, group, factors=None, w4=None, stream=None):
     esb_w4_size(N, K, group) bytes.  factors: device fp32 candidates of the scale, as multiples
     of max|w| / 6 of the group (None: 1)."""
     L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_w4_quantize(w, group, factors, w4)
     N, K, ld = _matrix(w, "w")
     t = _type(w, "w", _FLOATS)
     if factors is not None:
@@ -813,7 +830,7 @@ def esb_w4_quantize(w, group, factors=None, w4=None, stream=None):
     w4 = _w4_buffer(w4, N, K, group, w)
     st = L.esb_w4_quantize(w.data_ptr(), ld, t, N, K, group, _addr(factors),
                            1 if factors is None else factors.numel(), w4.data_ptr(), w4.numel(),
-                           _stream(stream))
+                           _stream(None))
     if st:
         raise EsbError("esb_w4_quantize", st)
     return w4
@@ -822,6 +839,9 @@ def esb_w4_quantize(w, group, factors=None, w4=None, stream=None):
 def esb_w4_pack(codes, alpha, group, w4=None, stream=None):
     """The packed form of ESB(4,1) codes (N x K uint8) and bf16 scales (N x ceil(K / group))."""
     L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_w4_pack(codes, alpha, group, w4)
     N, K, ldc = _matrix(codes, "codes")
     if codes.dtype != _torch.uint8:
         raise TypeError("codes must be uint8")
@@ -829,7 +849,7 @@ def esb_w4_pack(codes, alpha, group, w4=None, stream=None):
                 codes.get_device())
     w4 = _w4_buffer(w4, N, K, group, codes)
     st = L.esb_w4_pack(codes.data_ptr(), ldc, alpha.data_ptr(), lda, N, K, group, w4.data_ptr(),
-                       w4.numel(), _stream(stream))
+                       w4.numel(), _stream(None))
     if st:
         raise EsbError("esb_w4_pack", st)
     return w4
@@ -839,6 +859,9 @@ def esb_w4_unpack(w4, N, K, group, values=None, alpha=None, stream=None):
     """(values, alpha): the unscaled values (N x K float8_e4m3fn, exact) and the group scales
     (N x ceil(K / group) bf16) of packed weights."""
     L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_w4_unpack(w4, N, K, group, values, alpha)
     index = w4.get_device()
     _w4_check(w4, index)
     _w4_holds(L, w4, N, K, group)
@@ -853,7 +876,7 @@ def esb_w4_unpack(w4, N, K, group, values=None, alpha=None, stream=None):
     else:
         lda = _like(alpha, "alpha", N, groups, _torch.bfloat16, index)
     st = L.esb_w4_unpack(w4.data_ptr(), N, K, group, values.data_ptr(), ldv, alpha.data_ptr(), lda,
-                         _stream(stream))
+                         _stream(None))
     if st:
         raise EsbError("esb_w4_unpack", st)
     return values, alpha
@@ -868,6 +891,9 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=N
     weights W (N x K); y in y_dtype (None: x's type; bf16 for float8).  workspace: at least
     esb_w4_gemm_workspace_size() bytes; without one the call allocates what it needs from torch."""
     L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_w4_gemm(x, w4, N, group, x_scale, y_dtype, y, workspace)
     M, K, ldx = _matrix(x, "x")
     tx = _type(x, "x", (ESB_F32, ESB_BF16, ESB_F16, ESB_E4M3))   # fp32: the library's refusal
     index = x.get_device()
@@ -890,7 +916,7 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=N
             workspace = x.new_empty(need, dtype=_torch.uint8)
     wp, wb = _ws(workspace)
     st = L.esb_w4_gemm(M, N, K, group, x.data_ptr(), ldx, tx, _addr(x_scale), w4.data_ptr(),
-                       y.data_ptr(), ldy, ty, wp, wb, _stream(stream))
+                       y.data_ptr(), ldy, ty, wp, wb, _stream(None))
     if st:
         raise EsbError("esb_w4_gemm", st)
     return y

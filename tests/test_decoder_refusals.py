@@ -57,6 +57,7 @@ def test_weights(L):
     assert size(0, 128, 128) == 0 and size(16, 0, 128) == 0
     assert size(-1, 128, 128) == 0 and size(16, -1, 128) == 0 and size(16, 128, 16) == 0
     assert size((1 << 31) - 1, 1, 128) == 0 and size(1 << 26, 1 << 20, 128) == 0
+    assert size(32, (1 << 30) + 1, 128) == 0 and size(32, 1 << 30, 128) > 1 << 34
     need = size(40, 200, 64)
     q = L.esb_w4_quantize
 

@@ -111,6 +111,42 @@ def test_every_row_alike(esb):
     assert bool(torch.isnan(y[7]).all()) and not bool(torch.isfinite(y[200]).any())
 
 
+@pytest.mark.parametrize("M", [3, 40, 300])
+def test_rows_without_a_scale(esb, M):
+    """8-bit rows of NaN under a NaN scale, as the row operators leave them, and a NaN byte alone."""
+    codes, alpha = weights(1, 200, 700, 64)
+    w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), 64)
+    xv, s = acts(2, M, 700, "e4m3")
+    xd, sd = xv.cuda(), s.cuda()
+    sd[0] = float("nan")
+    xd[0].view(torch.uint8).fill_(0x7F)
+    xd[2].view(torch.uint8)[699] = 0x7F
+    for y in (torch.bfloat16, torch.float32):
+        out = esb.esb_w4_gemm(xd, w4, 200, 64, x_scale=sd, y_dtype=y)
+        assert bool(torch.isnan(out[0]).all()) and bool(torch.isnan(out[2]).all())
+        keep = [i for i in range(M) if i not in (0, 2)]
+        check(out[keep], xv[keep], s[keep], codes, alpha, 64)
+
+
+def test_a_stream_of_its_own(esb):
+    """Calls on another stream than the current one: outputs and workspace belong to it."""
+    codes, alpha = weights(1, 512, 2048, 128)
+    w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), 128)
+    xv, _ = acts(3, 64, 2048, "bf16")
+    x = xv.cuda()
+    assert esb.esb_w4_gemm_workspace_size(64, 512, 2048, 128, 1, 1) > 0
+    want = esb.esb_w4_gemm(x, w4, 512, 128)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        for _ in range(20):
+            got = esb.esb_w4_gemm(x, w4, 512, 128, stream=stream)
+            junk = torch.full((1 << 20,), float("nan"), device="cuda")       # the current stream's memory
+        side.synchronize()
+        assert torch.equal(got, want)
+    del junk
+
+
 @pytest.mark.parametrize("M", [1, 20, 150, 600])
 @pytest.mark.parametrize("x", ["bf16", "e4m3"])
 def test_groups_without_a_scale_reach_their_outputs_only(esb, M, x):
