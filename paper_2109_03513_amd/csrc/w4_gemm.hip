@@ -537,7 +537,7 @@ constexpr int kShapes = 5;
 constexpr TileShape kShapes16[kShapes] = {{32, 256, 2, {0.36f, 0.58f}},
                                           {64, 256, 2, {0.615f, 1.025f}},
                                           {64, 256, 1, {0.54f}},
-                                          {128, 256, 1, {1.03f}},
+                                          {128, 256, 1, {1.00f}},
                                           {128, 256, 2, {1.10f, 1.96f}}};
 constexpr TileShape kShapes8[kShapes] = {{64, 128, 1, {0.35f}},
                                          {64, 128, 2, {0.44f, 0.66f}},
