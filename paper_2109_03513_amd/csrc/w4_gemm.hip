@@ -200,7 +200,8 @@ __device__ __forceinline__ int xcd_run(int id, int total) {
 // KW parts of WM x WN waves, each with a ring of its own, take every KW-th step of the tile, and the first
 // part adds their sums: a step's chain of barrier, LDS reads, decoding and dependent MFMAs is about
 // 1000 cycles that only other waves can fill (32 x 256, 64 steps, one workgroup per CU: 28 us with
-// one part, 21 with two, 17 with four).
+// one part, 21 with two, 17 with four; 64 bf16 rows of 9216 x 4096: 18.7 us in 32 x 256 tiles of two
+// parts, 16.8 in 32 x 128 of four; 128 of 4096 x 4096: 17.5 there, 13.2 in 32 x 64 of eight).
 //
 // F8: within one instruction, products below 2^-13 of its largest are dropped (measured with single
 // instructions).  Of 128 products of E4M3 rows that is at most 2^-6 and in practice some 10^-4 of
@@ -265,12 +266,12 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
     // Rows: DMA i of the wave serves rows 8 (wave + i NW) + lane / 8 and writes slot lane % 8 of each,
     // so it fetches piece (lane % 8) ^ (row / 2 % 8).  Through registers, the same rows and pieces.
     const X* xp[NX];
-    const int pc = (lane & 7) ^ (((8 * wave + (lane >> 3)) >> 1) & 7);      // 8 NW is a multiple of 16
-    static_assert(NW % 2 == 0, "the swizzle of a lane's rows is the same");
+    int pc[NX];
 #pragma unroll
     for (int i = 0; i < NX; i++) {
         const int64_t m = m0 + 8 * (wave + i * NW) + (lane >> 3);
-        xp[i] = (const X*)p.x + (m < p.M ? m : p.M - 1) * p.ldx + EP * pc;
+        pc[i] = (lane & 7) ^ (((8 * (wave + i * NW) + (lane >> 3)) >> 1) & 7);
+        xp[i] = (const X*)p.x + (m < p.M ? m : p.M - 1) * p.ldx + EP * pc[i];
     }
     // Weight tiles wave + i NW of the stage's [row tile][chunk]; rows of tiles past N read the last.
     const uint8_t* wp[NT];
@@ -287,10 +288,9 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
     // every stage issues the same number of DMAs, also past the last step
     auto fetch = [&](int s, uint8_t* slot) {
         if constexpr (DMA) {
-            const bool in = s * BK + EP * pc < K && s < end;
 #pragma unroll
             for (int i = 0; i < NX; i++)
-                dma16(in ? (const void*)(xp[i] + s * BK) : (const void*)kZero16, slot + 1024 * (wave + i * NW));
+                dma16(s * BK + EP * pc[i] < K && s < end ? (const void*)(xp[i] + s * BK) : (const void*)kZero16, slot + 1024 * (wave + i * NW));
         }
 #pragma unroll
         for (int i = 0; i < NT; i++) {
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
             for (int i = 0; i < NX; i++)
 #pragma unroll
                 for (int u = 0; u < (F8 ? 2 : 1); u++)
-                    st[i][u] = Act<X>::load(xp[i] + k + 8 * u, K - k - EP * pc - 8 * u);
+                    st[i][u] = Act<X>::load(xp[i] + k + 8 * u, K - k - EP * pc[i] - 8 * u);
         }
     };
     auto put = [&](uint8_t* slot) {
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
     const int swz = (r >> 1) & 7;
     constexpr int NF = F8 ? 2 : 4;      // MFMAs of a tile in a step
     // two behind where the registers allow, so that no sum is waited for
-    constexpr int U = TM * 2 * NG, LAG = TM == 4 && !(F8 && G == 128) ? 1 : 2;
+    constexpr int U = TM * 2 * NG, LAG = (TM == 4 && !(F8 && G == 128)) || (KW == 4 && !F8 && G == 32) ? 1 : 2;
     auto step = [&](const uint8_t* slot) {
         float a[2][NG];
         Frag wf[2][NF], x[NF];
@@ -524,30 +524,38 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4GemmParams p, int splits) {
     });
 }
 
-// The shapes of k_w4_tile and what a step of theirs costs, us on one CU holding 1 .. slots of its
-// workgroups (fitted to 24 shapes of 32 to 1024 rows, 4096 to 18432 outputs, K = 4096 and 9216, G = 128,
-// each with every shape and number of splits; the choice is within 5 % of the best in all but a few of
-// the 48, 13 % at worst).  Small tiles spread few rows over the chip, large ones read less per product;
-// the first and the third split a tile's steps over parts of a workgroup.
+// The shapes of k_w4_tile and what they cost, us: of a workgroup beyond a launch, of each further round of
+// workgroups, and of a step on one CU holding 1 .. slots of them (fitted to 24 shapes of 16 to 1024 rows,
+// 1024 to 18432 outputs, K = 4096 and 9216, G = 128, each with every shape and number of splits).  Small
+// tiles spread few rows over the chip, large ones read less per product; 32 x 64 and 32 x 128 tiles
+// split their steps over 8 and 4 parts of a workgroup.
 struct TileShape {
     int bm, bn, slots;
-    float step[3];
+    float fix, again, step[2];
 };
-constexpr int kShapes = 5;
-constexpr TileShape kShapes16[kShapes] = {{32, 256, 2, {0.36f, 0.58f}},
-                                          {64, 256, 2, {0.615f, 1.025f}},
-                                          {64, 256, 1, {0.54f}},
-                                          {128, 256, 1, {1.00f}},
-                                          {128, 256, 2, {1.10f, 1.96f}}};
-constexpr TileShape kShapes8[kShapes] = {{64, 128, 1, {0.35f}},
-                                         {64, 128, 2, {0.44f, 0.66f}},
-                                         {128, 128, 1, {0.56f}},
-                                         {128, 256, 1, {0.98f}},
-                                         {128, 256, 2, {1.09f, 1.72f}}};
+constexpr TileShape kShapes16[] = {{32, 64, 1, 0.5f, 4.0f, {0.105f}},
+                                   {64, 256, 2, 0.0f, 0.0f, {0.615f, 1.025f}},
+                                   {32, 128, 2, 0.0f, 1.0f, {0.185f, 0.285f}},
+                                   {64, 256, 1, 2.2f, 1.5f, {0.50f}},
+                                   {128, 256, 1, 0.0f, 0.0f, {1.00f}},
+                                   {128, 256, 2, 0.0f, 0.0f, {1.10f, 1.96f}}};
+constexpr TileShape kShapes8[] = {{32, 64, 1, 0.3f, 3.5f, {0.13f}},
+                                  {64, 128, 2, 0.0f, 0.0f, {0.44f, 0.66f}},
+                                  {32, 128, 1, 0.0f, 3.0f, {0.205f}},
+                                  {64, 128, 1, 1.7f, 5.0f, {0.26f}},
+                                  {128, 128, 1, 3.4f, 5.0f, {0.49f}},
+                                  {128, 256, 1, 0.0f, 0.0f, {0.98f}},
+                                  {128, 256, 2, 0.0f, 0.0f, {1.09f, 1.72f}}};
+// rows through registers: a step of small tiles costs more, 64 x 256 tiles lose to 32 x 256 at every size
+// (1024 rows of 4096 x 4096: 60.9 us against 50.0)
+constexpr TileShape kLoose16[] = {{32, 64, 1, 0.5f, 4.0f, {0.16f}}, {32, 256, 2, 0.0f, 0.0f, {0.53f, 0.66f}}};
+constexpr TileShape kLoose8[] = {{32, 64, 1, 0.3f, 3.5f, {0.25f}},
+                                 {64, 128, 1, 0.0f, 0.0f, {0.37f}},
+                                 {64, 128, 2, 0.0f, 0.0f, {0.44f, 0.66f}}};
 
 // The shape and the ranges of columns (splits) that should take the least time: rounds of full CUs,
 // then one of what is left; splits write and read fp32 sums at about 4 TB/s and launch one more kernel.
-// DMA == 0 has the first two.  room: bytes for the sums.
+// room: bytes for the sums.
 struct TilePlan {
     int shape, splits;
 };
@@ -559,17 +567,19 @@ TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, size_t room)
     const double cus = num_cus();
     TilePlan best = {0, 1};
     double least = 1e30;
-    // the last shape's registers do not hold two scales per step of its 128 x 64 waves
-    const int shapes = !dma ? 2 : L.group == 32 ? kShapes - 1 : kShapes;
+    const int shapes = dma ? (f8 ? 7 : 6) : f8 ? 3 : 2;
     for (int v = 0; v < shapes; v++) {
-        const TileShape& s = f8 ? kShapes8[v] : kShapes16[v];
+        // the last shape's registers do not hold the two scales that a step of groups of 32 has
+        if (L.group == 32 && v == 5) continue;
+        const TileShape& s = dma ? (f8 ? kShapes8[v] : kShapes16[v]) : f8 ? kLoose8[v] : kLoose16[v];
         const double tiles = (double)((M + s.bm - 1) / s.bm) * ((L.N + s.bn - 1) / s.bn);
         for (int z : {1, 2, 3, 4, 6, 8}) {
             if (steps < 4 * z && z > 1) break;
             if (sums_bytes(M, L, z) > room) break;
             const double held = ceil(tiles * z / cus), rounds = floor((held - 1) / s.slots);
             const int rest = (int)(held - rounds * s.slots);
-            double us = (rounds * s.step[s.slots - 1] + s.step[rest - 1]) * ceil((double)steps / z);
+            double us = s.fix + rounds * s.again +
+                        (rounds * s.step[s.slots - 1] + s.step[rest - 1]) * ceil((double)steps / z);
             if (z > 1) us += 4.5 + z * (double)M * L.tiles * 32 * 8 / 4e6;
             if (us < least) {
                 least = us;
@@ -638,39 +648,47 @@ hipError_t launch_shape(const W4GemmParams& p, int x_type, hipStream_t s) {
     const TilePlan t = tile_plan(p.M, p.L, F8, dma, p.ws_bytes);
     if constexpr (F8) {
         if (!dma) {
-            if (t.shape == 0) return launch_tile<X, 1, G, 1, 2, 2, 4, 2, 0>(p, t.splits, s);
+            if (t.shape == 0) return launch_tile<X, 1, G, 1, 1, 1, 8, 2, 0>(p, t.splits, s);
+            if (t.shape == 1) return launch_tile<X, 1, G, 1, 2, 2, 4, 2, 0>(p, t.splits, s);
             return launch_tile<X, 1, G, 1, 2, 2, 1, 4, 0>(p, t.splits, s);
         }
-        if (t.shape == 0) return launch_tile<X, 1, G, 1, 2, 2, 4, 2, 1>(p, t.splits, s);
+        if (t.shape == 0) return launch_tile<X, 1, G, 1, 1, 1, 8, 2, 1>(p, t.splits, s);
         if (t.shape == 1) return launch_tile<X, 1, G, 1, 2, 2, 1, 4, 1>(p, t.splits, s);
-        if (t.shape == 2) return launch_tile<X, 1, G, 2, 2, 2, 2, 2, 1>(p, t.splits, s);
-        if (t.shape == 3) return launch_tile<X, 1, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
+        if (t.shape == 2) return launch_tile<X, 1, G, 1, 1, 2, 4, 2, 1>(p, t.splits, s);
+        if (t.shape == 3) return launch_tile<X, 1, G, 1, 2, 2, 4, 2, 1>(p, t.splits, s);
+        if (t.shape == 4) return launch_tile<X, 1, G, 2, 2, 2, 2, 2, 1>(p, t.splits, s);
+        if (t.shape == 5) return launch_tile<X, 1, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
         return launch_tile<X, 1, G, 4, 1, 4, 1, 2, 1>(p, t.splits, s);
     } else {
         if constexpr (sizeof(X) == 2) {
             if (dma) {
-                if (t.shape == 0) return launch_tile<X, 0, G, 1, 1, 4, 2, 3, 1>(p, t.splits, s);
+                if (t.shape == 0) return launch_tile<X, 0, G, 1, 1, 1, 8, 2, 1>(p, t.splits, s);
                 if (t.shape == 1) return launch_tile<X, 0, G, 2, 1, 4, 1, 4, 1>(p, t.splits, s);
-                if (t.shape == 2) return launch_tile<X, 0, G, 2, 1, 4, 2, 4, 1>(p, t.splits, s);
-                if (t.shape == 3) return launch_tile<X, 0, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
+                if (t.shape == 2) return launch_tile<X, 0, G, 1, 1, 2, 4, 2, 1>(p, t.splits, s);
+                if (t.shape == 3) return launch_tile<X, 0, G, 2, 1, 4, 2, 4, 1>(p, t.splits, s);
+                if (t.shape == 4) return launch_tile<X, 0, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
                 if constexpr (G > 32) return launch_tile<X, 0, G, 4, 1, 4, 1, 3, 1>(p, t.splits, s);
             }
         }
-        if (t.shape == 0) return launch_tile<X, 0, G, 1, 1, 4, 2, 3, 0>(p, t.splits, s);
-        return launch_tile<X, 0, G, 2, 1, 4, 1, 4, 0>(p, t.splits, s);
+        if (t.shape == 0) return launch_tile<X, 0, G, 1, 1, 1, 8, 2, 0>(p, t.splits, s);
+        return launch_tile<X, 0, G, 1, 1, 4, 2, 3, 0>(p, t.splits, s);
     }
 }
 
-// A token's kernel reads the weights once, without LDS; it also reads every row in pieces, so that with
-// many weights and more than a few rows the tiles are faster (18432 x 4096: 8 rows 17.3 against 15.5 us,
-// 16 rows 23.5 against 16.2; 4096 x 9216, 16 rows: 12.8 against 16.4).
-bool takes_token(int64_t M, const W4Layout& L) {
-    return M <= 4 || (M <= 16 && (int64_t)L.N * L.K <= (int64_t)48 << 20);
+// A token's kernel reads the weights once, without LDS, but every row in pieces and the weights' decoding
+// once per wave: with more than a few rows it wins only while its workgroups come at about one per CU or
+// the weights are few.  us here against tiles, 16-bit / E4M3 rows: 16 rows of 4096 x 4096 7.2 : 11.1 / 7.3 :
+// 8.3, of 4096 x 9216 12.7 : 13.8 / 13.0 : 14.0, of 9216 x 1024 5.7 : 6.7 / 6.0 : 6.0, of 9216 x 4096
+// 15.5 : 12.1 / 15.8 : 9.8; 18432 x 4096 with 6 rows 15.3 : 15.9, 8 rows 17.3 : 15.7, E4M3 with 2 rows
+// 12.9 : 11.9 (9216 x 4096: 9.2 : 9.3).
+bool takes_token(int64_t M, const W4Layout& L, bool f8) {
+    const int64_t few = (2 * (int64_t)L.tiles <= num_cus() * 3 / 2 ? 40 : 12) << 20;
+    return M <= (f8 ? 2 : 6) || (M <= 16 && (int64_t)L.N * L.K <= few);
 }
 
 template <typename X, int G>
 hipError_t launch_g(const W4GemmParams& p, int x_type, hipStream_t s) {
-    if (takes_token(p.M, p.L)) {
+    if (takes_token(p.M, p.L, takes_f8(x_type, p.y_type, G))) {
         // 16 waves where the CUs get about one workgroup each, else 8 (one row, K = 9216, 4096 outputs:
         // 7.2 us against 9.0; K = 4096, 18432 outputs: 14.0 against 11.7)
         const unsigned grid = 2 * p.L.tiles;
@@ -695,8 +713,8 @@ hipError_t launch_x(const W4GemmParams& p, int x_type, hipStream_t s) {
 
 size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type) {
     M = M < kRowsOfALaunch ? M : kRowsOfALaunch;
-    if (L.K == 0 || takes_token(M, L)) return 0;
     const bool f8 = takes_f8(x_type, y_type, L.group);
+    if (L.K == 0 || takes_token(M, L, f8)) return 0;
     // rows of whole 16-byte pieces are expected to be aligned; others cannot be
     const int es = x_type == kE4M3 ? 1 : 2;
     const bool dma = (f8 || es == 2) && (int64_t)L.K * es % 16 == 0, copy = !dma && M >= kAlignRows;

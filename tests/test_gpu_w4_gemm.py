@@ -96,6 +96,21 @@ def test_larger_products(esb, M, N, K, x, group):
         check(esb.esb_w4_gemm(xv.cuda(), w4, N, group, x_scale=sd, y_dtype=y), xv, s, codes, alpha, group)
 
 
+@pytest.mark.parametrize("M,N,K", [(30, 2000, 9232), (64, 512, 9216), (500, 4090, 2064), (520, 4100, 528),
+                                   (1000, 4090, 4112), (2000, 4090, 1040), (2040, 4580, 528), (4090, 4090, 528)])
+@pytest.mark.parametrize("x", ["bf16", "e4m3"])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_tiles(esb, M, N, K, x, pad):
+    """Sizes that between them take every tile and number of column ranges, rows aligned and not."""
+    log("w4 gemm M=%d N=%d K=%d %s pad=%d" % (M, N, K, x, pad))
+    xv, s = acts(M + K, M, K, x)
+    xd = torch.empty(M, K + pad, dtype=XT[x], device="cuda")[:, :K]
+    xd.copy_(xv.cuda())
+    codes, alpha = weights(N, N, K, 128)
+    w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), 128)
+    check(esb.esb_w4_gemm(xd, w4, N, 128, x_scale=None if s is None else s.cuda()), xv, s, codes, alpha, 128)
+
+
 def test_every_row_alike(esb):
     """A row's output does not depend on the other rows of its call, beyond the order of sums."""
     codes, alpha = weights(1, 200, 700, 64)
@@ -128,13 +143,14 @@ def test_rows_without_a_scale(esb, M):
         check(out[keep], xv[keep], s[keep], codes, alpha, 64)
 
 
-def test_a_stream_of_its_own(esb):
+@pytest.mark.parametrize("K", [2048, 9216])
+def test_a_stream_of_its_own(esb, K):
     """Calls on another stream than the current one: outputs and workspace belong to it."""
-    codes, alpha = weights(1, 512, 2048, 128)
+    codes, alpha = weights(1, 512, K, 128)
     w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), 128)
-    xv, _ = acts(3, 64, 2048, "bf16")
+    xv, _ = acts(3, 64, K, "bf16")
     x = xv.cuda()
-    assert esb.esb_w4_gemm_workspace_size(64, 512, 2048, 128, 1, 1) > 0
+    assert K < 9216 or esb.esb_w4_gemm_workspace_size(64, 512, K, 128, 1, 1) > 0
     want = esb.esb_w4_gemm(x, w4, 512, 128)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
@@ -217,6 +233,7 @@ def test_weights_beyond_32_bits(esb):
 
 
 @pytest.mark.parametrize("M,N,K,x,group", [(20, 300, 520, "bf16", 64), (64, 512, 2048, "f16", 32),
+                                           (64, 512, 9216, "f16", 32), (30, 300, 9216, "e4m3", 128),
                                            (130, 257, 333, "bf16", 128), (150, 300, 777, "e4m3", 128),
                                            (140, 200, 640, "e4m3", 32)])
 def test_with_and_without_workspace(esb, M, N, K, x, group):
