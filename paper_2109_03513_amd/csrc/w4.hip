@@ -185,8 +185,12 @@ __device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
 // Codes: for 16-bit weights w / alpha is a tie or at least 2^-11 from one, so w (1/alpha) (1 + 2^-22)
 // rounds to the nearest value with ties up; 32-bit weights are compared with the exact bounds.
 //
-// Bound by the conversions to fp4 (a quarter of the fp32 rate, two values each): some 22 cycles of a
-// SIMD per 64 weights and candidate.
+// Bound by VALU issue (97 % of all cycles busy): for two weights and a candidate two products with 1/alpha,
+// a conversion to fp4 (a quarter of the fp32 rate), one back, two remainders and two squares, some 22
+// cycles of a SIMD per 64 weights.  4096 x 9216 bf16 weights, G = 128, 16 candidates: 101-110 us (the
+// bytes alone: 18); 1000 x 1999 fp16, G = 32, 8 candidates: 11 us.  Dot products of 16-bit pairs would
+// halve the sums but lose seven bits to cancellation, and fp4 from 16-bit products moves the cell
+// bounds: both would send groups by the percent, not by the ten-thousand, to the fp64 comparison.
 template <typename T, int G>
 __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __restrict__ w, int64_t ldw,
                                                      const float* __restrict__ factors, int nf,
@@ -303,7 +307,16 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
             uint4{packed[0], packed[2], packed[1], packed[3]};
 }
 
-// ESB(4,1) codes and row-major scales into the layout.
+// Four ESB(4,1) codes, one a byte, to E2M1 nibbles in the bytes 0 and 2: one more in the exponent field,
+// modulo 4, takes the all-ones (subnormal) binade to 0; zero has no sign.
+__device__ __forceinline__ uint32_t code_nibbles(uint32_t c) {
+    const uint32_t m = ((c & 0x07070707u) + 0x02020202u) & 0x07070707u;
+    const uint32_t n = m | (c & (m + 0x07070707u) & 0x08080808u);
+    return n | (n >> 4);
+}
+
+// ESB(4,1) codes and row-major scales into the layout: a byte in, half a byte out, bound by HBM (18432 x
+// 4096: 27 us, 4.3 TB/s; loading and packing byte by byte took 190).
 __global__ __launch_bounds__(256) void k_w4_pack(W4Layout L, const uint8_t* __restrict__ codes, int64_t ldc,
                                                  const __bf16* __restrict__ alpha, int64_t lda,
                                                  uint8_t* __restrict__ out) {
@@ -313,16 +326,18 @@ __global__ __launch_bounds__(256) void k_w4_pack(W4Layout L, const uint8_t* __re
 #pragma unroll
     for (int t = 0; t < 8; t++) {
         const int k = column(o, t);
-        uint32_t d = 0;
+        uint2 c = {0x06060606u, 0x06060606u};            // codes of zero
+        const uint8_t* src = codes + o.n * ldc + k;
+        if (o.n < L.N && k + 8 <= L.K) {
+            c = ((const Loose<uint2, uint8_t>*)src)->v;
+        } else if (o.n < L.N) {
+            uint32_t v[2] = {c.x, c.y};
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            if (o.n >= L.N || k + i >= L.K) continue;
-            const uint32_t c = codes[o.n * ldc + k + i];
-            // one more in the exponent field, modulo 4: the all-ones (subnormal) binade becomes 0
-            const uint32_t m = (c + 2) & 7;
-            d |= (m | (m ? c & 8 : 0)) << (4 * i);
+            for (int i = 0; i < 8; i++)
+                if (k + i < L.K) v[i >> 2] ^= (uint32_t)(src[i] ^ 6) << (8 * (i & 3));
+            c = uint2{v[0], v[1]};
         }
-        packed[t] = d;
+        packed[t] = __builtin_amdgcn_perm(code_nibbles(c.y), code_nibbles(c.x), 0x06040200u);
     }
     put_tiles(L, o, packed, out);
     __bf16* scales = (__bf16*)(out + L.scale_offset);
@@ -332,7 +347,7 @@ __global__ __launch_bounds__(256) void k_w4_pack(W4Layout L, const uint8_t* __re
         scales[scale_index(L, o, g)] = o.n < L.N && (int64_t)g * L.group < L.K ? alpha[o.n * lda + g] : (__bf16)0.0f;
 }
 
-// Unscaled values as E4M3 bytes, and row-major scales.
+// Unscaled values as E4M3 bytes, and row-major scales; bound by HBM (18432 x 4096: 22.6 us, 5.1 TB/s).
 __global__ __launch_bounds__(256) void k_w4_unpack(W4Layout L, const uint8_t* __restrict__ in,
                                                    uint8_t* __restrict__ values, int64_t ldv,
                                                    __bf16* __restrict__ alpha, int64_t lda) {
