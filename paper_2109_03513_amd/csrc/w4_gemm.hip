@@ -13,7 +13,7 @@
 //    E4M3 rows 7.1 us.
 //  * k_w4_tile: tiles of 32 to 128 rows, everything through a ring in LDS; with few tiles the
 //    reduction is split over workgroups and k_w4_sum adds the parts.  Few rows are bound by the chain of
-//    a step (64 fp16 rows of 9216 x 4096, G = 32: 18.5 us), many by power and by MFMA and VALU issue:
+//    a step (64 fp16 rows of 9216 x 4096, G = 32: 17.4 us), many by power and by MFMA and VALU issue:
 //    4096 E4M3 rows of 18432 x 4096, G = 128 272 us, 2.3 PFLOP/s, MFMA busy 53 % and VALU 51 % of cycles
 //    at 2.0 GHz; 1999 bf16 rows of 4096 x 9216, G = 64 146 us, 1.03 PFLOP/s, MFMA 42 %, VALU 46 %.
 //    With rows of zeros the same products take 20 to 25 % less; tiles of 128 x 512 and 256 x 256, which
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
     const int swz = (r >> 1) & 7;
     constexpr int NF = F8 ? 2 : 4;      // MFMAs of a tile in a step
     // two behind where the registers allow, so that no sum is waited for
-    constexpr int U = TM * 2 * NG, LAG = (TM == 4 && !(F8 && G == 128)) || (KW == 4 && !F8 && G == 32) ? 1 : 2;
+    constexpr int U = TM * 2 * NG, LAG = (TM == 4 && !(F8 && G == 128)) || (KW >= 4 && WN == 2 && !F8 && G == 32) ? 1 : 2;
     auto step = [&](const uint8_t* slot) {
         float a[2][NG];
         Frag wf[2][NF], x[NF];
@@ -535,8 +535,9 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4GemmParams p, int splits) {
 // The shapes of k_w4_tile and what they cost, us: of a workgroup beyond a launch, of each further round of
 // workgroups, and of a step on one CU holding 1 .. slots of them (fitted to 24 shapes of 16 to 1024 rows,
 // 1024 to 18432 outputs, K = 4096 and 9216, G = 128, each with every shape and number of splits).  Small
-// tiles spread few rows over the chip, large ones read less per product; 32 x 64 and 32 x 128 tiles
-// split their steps over 8 and 4 parts of a workgroup.
+// tiles spread few rows over the chip, large ones read less per product; 32 x 64 tiles split their steps
+// over 8 parts of a workgroup, 32 x 128 over 4, and over 8 where a CU gets only one (64 fp16 rows of
+// 9216 x 4096, G = 32: 18.9 us with 4, 17.4 with 8; 128 rows: 25.9 and 33.2).
 struct TileShape {
     int bm, bn, slots;
     float fix, again, step[2];
@@ -544,6 +545,7 @@ struct TileShape {
 constexpr TileShape kShapes16[] = {{32, 64, 1, 0.5f, 4.0f, {0.105f}},
                                    {64, 256, 2, 0.0f, 0.0f, {0.615f, 1.025f}},
                                    {32, 128, 2, 0.0f, 1.0f, {0.185f, 0.285f}},
+                                   {32, 128, 1, 1.3f, 4.0f, {0.16f}},
                                    {64, 256, 1, 2.2f, 1.5f, {0.50f}},
                                    {128, 256, 1, 0.0f, 0.0f, {1.00f}},
                                    {128, 256, 2, 0.0f, 0.0f, {1.10f, 1.96f}}};
@@ -575,10 +577,10 @@ TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, size_t room)
     const double cus = num_cus();
     TilePlan best = {0, 1};
     double least = 1e30;
-    const int shapes = dma ? (f8 ? 7 : 6) : f8 ? 3 : 2;
+    const int shapes = dma ? 7 : f8 ? 3 : 2;
     for (int v = 0; v < shapes; v++) {
         // the last shape's registers do not hold the two scales that a step of groups of 32 has
-        if (L.group == 32 && v == 5) continue;
+        if (L.group == 32 && v == 6) continue;
         const TileShape& s = dma ? (f8 ? kShapes8[v] : kShapes16[v]) : f8 ? kLoose8[v] : kLoose16[v];
         const double tiles = (double)((M + s.bm - 1) / s.bm) * ((L.N + s.bn - 1) / s.bn);
         for (int z : {1, 2, 3, 4, 6, 8}) {
@@ -673,8 +675,9 @@ hipError_t launch_shape(const W4GemmParams& p, int x_type, hipStream_t s) {
                 if (t.shape == 0) return launch_tile<X, 0, G, 1, 1, 1, 8, 2, 1>(p, t.splits, s);
                 if (t.shape == 1) return launch_tile<X, 0, G, 2, 1, 4, 1, 4, 1>(p, t.splits, s);
                 if (t.shape == 2) return launch_tile<X, 0, G, 1, 1, 2, 4, 2, 1>(p, t.splits, s);
-                if (t.shape == 3) return launch_tile<X, 0, G, 2, 1, 4, 2, 4, 1>(p, t.splits, s);
-                if (t.shape == 4) return launch_tile<X, 0, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
+                if (t.shape == 3) return launch_tile<X, 0, G, 1, 1, 2, 8, 2, 1>(p, t.splits, s);
+                if (t.shape == 4) return launch_tile<X, 0, G, 2, 1, 4, 2, 4, 1>(p, t.splits, s);
+                if (t.shape == 5) return launch_tile<X, 0, G, 2, 2, 4, 1, 4, 1>(p, t.splits, s);
                 if constexpr (G > 32) return launch_tile<X, 0, G, 4, 1, 4, 1, 3, 1>(p, t.splits, s);
             }
         }

@@ -96,19 +96,19 @@ def test_larger_products(esb, M, N, K, x, group):
         check(esb.esb_w4_gemm(xv.cuda(), w4, N, group, x_scale=sd, y_dtype=y), xv, s, codes, alpha, group)
 
 
-@pytest.mark.parametrize("M,N,K", [(30, 2000, 9232), (64, 512, 9216), (500, 4090, 2064), (520, 4100, 528),
+@pytest.mark.parametrize("M,N,K", [(30, 2000, 9232), (64, 512, 9216), (60, 9190, 4112), (500, 4090, 2064), (520, 4100, 528),
                                    (1000, 4090, 4112), (2000, 4090, 1040), (2040, 4580, 528), (4090, 4090, 528)])
 @pytest.mark.parametrize("x", ["bf16", "e4m3"])
-@pytest.mark.parametrize("pad", [0, 1])
-def test_tiles(esb, M, N, K, x, pad):
+@pytest.mark.parametrize("pad,group", [(0, 128), (0, 32), (1, 64)])
+def test_tiles(esb, M, N, K, x, pad, group):
     """Sizes that between them take every tile and number of column ranges, rows aligned and not."""
-    log("w4 gemm M=%d N=%d K=%d %s pad=%d" % (M, N, K, x, pad))
+    log("w4 gemm M=%d N=%d K=%d %s pad=%d group=%d" % (M, N, K, x, pad, group))
     xv, s = acts(M + K, M, K, x)
     xd = torch.empty(M, K + pad, dtype=XT[x], device="cuda")[:, :K]
     xd.copy_(xv.cuda())
-    codes, alpha = weights(N, N, K, 128)
-    w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), 128)
-    check(esb.esb_w4_gemm(xd, w4, N, 128, x_scale=None if s is None else s.cuda()), xv, s, codes, alpha, 128)
+    codes, alpha = weights(N, N, K, group)
+    w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), group)
+    check(esb.esb_w4_gemm(xd, w4, N, group, x_scale=None if s is None else s.cuda()), xv, s, codes, alpha, group)
 
 
 def test_every_row_alike(esb):
