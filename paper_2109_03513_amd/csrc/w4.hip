@@ -20,6 +20,8 @@
 //    operands of two 16x16x32 MFMAs over columns 0 .. 31 and 32 .. 63.
 // So every MFMA stays within one group of 32, 64 or 128.  The scales follow, [row tile][group][32
 // rows].  Rows and columns beyond N and K hold codes and scales of 0.
+#include <type_traits>
+
 #include "float_rows.h"
 
 namespace esb {
@@ -72,31 +74,42 @@ __device__ __forceinline__ int64_t scale_index(const W4Layout& L, const Owner& o
     return ((int64_t)o.nt * L.groups + g) * 32 + o.r;
 }
 
-// The quantizer's lanes hold four words (32 weights) each: of one tile for groups of 32 and 64, two
-// lanes to a row; of half a row tile and two tiles for groups of 128, four lanes to a row.
+// The quantizer's lanes hold one group's words of a row and half h: two for groups of 32 and four (32
+// weights) else; two lanes to a group, four for groups of 128.  For groups of 64 a wave takes a tile,
+// else half of the rows (blockIdx.y) of a tile's two groups or of two tiles.
 template <int G>
 struct Share {
-    int r, h, nt, kc;    // row and half in the tile, row tile, chunk of this lane
+    static constexpr int words = G == 32 ? 2 : 4;
+    int r, h, nt, kc, gi;    // row and half in the tile, row tile, chunk and group of this lane
     int64_t n;
+    static __host__ __device__ int across(const W4Layout& L) { return G == 128 ? (L.chunks + 1) / 2 : L.chunks; }
     __device__ __forceinline__ bool own(const W4Layout& L) {
         const int lane = threadIdx.x & 63;
         const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-        const int pairs = (L.chunks + 1) / 2;
-        if (wave >= (G == 128 ? (int64_t)L.tiles * 2 * pairs : (int64_t)L.tiles * L.chunks)) return false;
-        if (G == 128) {
-            r = 16 * (int)(wave / pairs & 1) + (lane & 15);
-            nt = (int)(wave / pairs / 2);
-            kc = 2 * (int)(wave % pairs) + (lane >> 4 & 1);
-        } else {
-            r = lane & 31;
-            nt = (int)(wave / L.chunks);
-            kc = (int)(wave % L.chunks);
-        }
+        const int per = across(L), e = lane >> 4 & 1;
+        if (wave >= (int64_t)L.tiles * per) return false;
+        const int q = (int)(wave % per);
+        nt = (int)(wave / per);
+        r = G == 64 ? lane & 31 : 16 * (int)blockIdx.y + (lane & 15);
+        kc = G == 128 ? 2 * q + e : q;
+        gi = G == 32 ? 2 * q + e : q;
         h = lane >> 5;
         n = 32 * (int64_t)nt + r;
         return true;
     }
-    __device__ __forceinline__ int column(int i) const { return 64 * kc + 8 * (2 * h + (i & 1) + 4 * (i >> 1)); }
+    __device__ __forceinline__ int column(int i) const {
+        return 64 * kc + 8 * (2 * h + (i & 1) + 4 * (G == 32 ? gi & 1 : i >> 1));
+    }
+    __device__ __forceinline__ void put(const W4Layout& L, const uint32_t (&w)[words], uint8_t* out) const {
+        if (kc >= L.chunks) return;
+        uint8_t* d = out + 1024 * ((int64_t)nt * L.chunks + kc) + 16 * (32 * h + r);
+        if constexpr (G == 32) {
+            *(uint32_t*)(d + 4 * (gi & 1)) = w[0];
+            *(uint32_t*)(d + 4 * (gi & 1) + 8) = w[1];
+        } else {
+            *(uint4*)d = uint4{w[0], w[2], w[1], w[3]};
+        }
+    }
 };
 // Over the lanes of a row.
 template <int G, typename F>
@@ -125,8 +138,8 @@ __device__ __forceinline__ double row_sum(double v) {
 
 // One group of a row's lanes, in any range of values: errors in fp64 from exact cell bounds.  Rare: it
 // reads the group's weights again rather than keep them.
-template <typename T, int G, int WG>
-__device__ __forceinline__ float search_exact(const Share<G>& o, const T* row, int K, int word, float top,
+template <typename T, int G>
+__device__ __forceinline__ float search_exact(const Share<G>& o, const T* row, int K, float top,
                                               const float* factors, int nf) {
     float alpha = __builtin_nanf("");
     double least = __builtin_inf();
@@ -136,7 +149,7 @@ __device__ __forceinline__ float search_exact(const Share<G>& o, const T* row, i
         if (!(f > 0.0f) || !(f < __builtin_inff())) continue;
         double err = 0.0;
 #pragma unroll 1
-        for (int t = word; t < word + WG; t++) {
+        for (int t = 0; t < o.words; t++) {
             const int k = o.column(t);
             const f32x8 x = __builtin_convertvector(load8(row + k, K - k), f32x8);
 #pragma unroll
@@ -188,7 +201,7 @@ __device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
 // Bound by VALU issue (97 % of all cycles busy): for two weights and a candidate two products with 1/alpha,
 // a conversion to fp4 (a quarter of the fp32 rate), one back, two remainders and two squares, some 22
 // cycles of a SIMD per 64 weights.  4096 x 9216 bf16 weights, G = 128, 16 candidates: 101-110 us (the
-// bytes alone: 18); 1000 x 1999 fp16, G = 32, 8 candidates: 11 us.  Dot products of 16-bit pairs would
+// bytes alone: 18); 1000 x 1999 fp16, G = 32, 8 candidates: 9 us (11 with both groups of a row in a lane).  Dot products of 16-bit pairs would
 // halve the sums but lose seven bits to cancellation, and fp4 from 16-bit products moves the cell
 // bounds: both would send groups by the percent, not by the ten-thousand, to the fp64 comparison.
 template <typename T, int G>
@@ -197,114 +210,106 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
                                                      uint8_t* __restrict__ out) {
     Share<G> o;
     if (!o.own(L)) return;
-    constexpr int WG = G == 32 ? 2 : 4;      // words of a lane in one group
+    constexpr int WG = Share<G>::words;
     const int lane = threadIdx.x & 63;
     const float fs = factors && lane < nf ? factors[lane] : 1.0f;
-    float v[32];
+    float n[8 * WG];
 #pragma unroll
-    for (int t = 0; t < 4; t++) {
+    for (int t = 0; t < WG; t++) {
         const int k = o.column(t);
         const f32x8 x = __builtin_convertvector(load8(w + o.n * ldw + k, o.n < L.N ? L.K - k : 0), f32x8);
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[8 * t + i] = x[i];
+        for (int i = 0; i < 8; i++) n[8 * t + i] = x[i];
     }
-    uint32_t packed[4];
-    __bf16* scales = (__bf16*)(out + L.scale_offset);
+    uint32_t packed[WG];
+    uint32_t m = 0;
 #pragma unroll
-    for (int g = 0; g < 4 / WG; g++) {
-        float* n = v + 8 * WG * g;
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8 * WG; i++) m = max(m, __float_as_uint(n[i]) & 0x7fffffffu);
-        m = over_row<G>(m, [](uint32_t a, uint32_t b) { return max(a, b); });
-        const float top = __uint_as_float(m);
-        const bool finite = m < 0x7f800000u;
+    for (int i = 0; i < 8 * WG; i++) m = max(m, __float_as_uint(n[i]) & 0x7fffffffu);
+    m = over_row<G>(m, [](uint32_t a, uint32_t b) { return max(a, b); });
+    const float top = __uint_as_float(m);
+    const bool finite = m < 0x7f800000u;
 
-        // 2^-shift brings the largest weight into [1, 2)
-        const int shift = finite && m ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
+    // 2^-shift brings the largest weight into [1, 2)
+    const int shift = finite && m ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;
 #pragma unroll
-        for (int i = 0; i < 8 * WG; i++) n[i] = finite ? __builtin_amdgcn_ldexpf(n[i], -shift) : 0.0f;
-        const float inf = __builtin_inff();
-        float alpha = __builtin_nanf(""), other = alpha, least = inf, second = inf, third = inf;
-        bool far = false, other_first = false;
-        for (int c = 0; c < nf; c++) {
-            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fs), c));
-            if (!(f > 0.0f) || !(f < __builtin_inff())) continue;
-            // x / 6 rounded correctly: the product with the reciprocal, corrected by its exact remainder
-            const float x6 = top * f, q6 = x6 * (1.0f / 6.0f), d6 = fmaf(fmaf(-6.0f, q6, x6), 1.0f / 6.0f, q6);
-            const float a = bf16_round(fmaxf(d6, kTiny));
-            const float as = m ? __builtin_amdgcn_ldexpf(a, -shift) : 1.0f;
-            const float inv = __builtin_amdgcn_rcpf(as);
-            far |= as < 0x1p-100f;
-            float sum[8] = {};
+    for (int i = 0; i < 8 * WG; i++) n[i] = finite ? __builtin_amdgcn_ldexpf(n[i], -shift) : 0.0f;
+    const float inf = __builtin_inff();
+    float alpha = __builtin_nanf(""), other = alpha, least = inf, second = inf, third = inf;
+    bool far = false, other_first = false;
+    for (int c = 0; c < nf; c++) {
+        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fs), c));
+        if (!(f > 0.0f) || !(f < __builtin_inff())) continue;
+        // x / 6 rounded correctly: the product with the reciprocal, corrected by its exact remainder
+        const float x6 = top * f, q6 = x6 * (1.0f / 6.0f), d6 = fmaf(fmaf(-6.0f, q6, x6), 1.0f / 6.0f, q6);
+        const float a = bf16_round(fmaxf(d6, kTiny));
+        const float as = m ? __builtin_amdgcn_ldexpf(a, -shift) : 1.0f;
+        const float inv = __builtin_amdgcn_rcpf(as);
+        far |= as < 0x1p-100f;
+        float sum[8] = {};
 #pragma unroll
-            for (int t = 0; t < WG; t++) {
-                const float* x = n + 8 * t;
-                const uint32_t q = to_e2m1(x, inv);
-                const auto d0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0);
-                const auto d1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1);
-                const auto d2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2);
-                const auto d3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3);
-                const float d[8] = {d0[0], d0[1], d1[0], d1[1], d2[0], d2[1], d3[0], d3[1]};
+        for (int t = 0; t < WG; t++) {
+            const float* x = n + 8 * t;
+            const uint32_t q = to_e2m1(x, inv);
+            const auto d0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0);
+            const auto d1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1);
+            const auto d2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2);
+            const auto d3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3);
+            const float d[8] = {d0[0], d0[1], d1[0], d1[1], d2[0], d2[1], d3[0], d3[1]};
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float e = fmaf(-as, d[i], x[i]);
-                    sum[i] = fmaf(e, e, sum[i]);
-                }
-            }
-            float err = row_sum<G>(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
-            // a candidate that overflows is passed over; one equal to a kept one adds nothing
-            err = x6 < inf && a != alpha && a != other ? err : inf;
-            const bool first = err < least, next = err < second;
-            other = first ? alpha : next ? a : other;
-            other_first = first || (other_first && !next);
-            alpha = first ? a : alpha;
-            third = fminf(third, fmaxf(second, err));
-            second = __builtin_amdgcn_fmed3f(least, second, err);
-            least = fminf(least, err);
-        }
-        const float near = least * (1.0f + 0x1p-19f);
-        if (__any(finite && m && (far || third <= near))) {
-            const float exact = search_exact<T, G, WG>(o, w + (o.n < L.N ? o.n : 0) * ldw, o.n < L.N ? L.K : 0, WG * g, top, factors, nf);
-            if (finite) alpha = exact;
-        } else if (__any(finite && m && second <= near)) {
-            const double e0 = row_sum<G>(exact_error<WG>(n, __builtin_amdgcn_ldexpf(alpha, -shift)));
-            const double e1 = row_sum<G>(exact_error<WG>(n, __builtin_amdgcn_ldexpf(other, -shift)));
-            if (second <= near && (other_first ? e1 <= e0 : e1 < e0)) alpha = other;
-        }
-        if (!finite) alpha = __builtin_nanf("");
-        const float as = __builtin_amdgcn_ldexpf(alpha, -shift);
-
-        // (1/as) of a scale far below the weights may be infinite
-        if (sizeof(T) == 2 && !__any(finite && m && as < 0x1p-100f)) {
-            const float inv = m && alpha == alpha ? 1.0f / as * (1.0f + 0x1p-22f) : 0.0f;
-#pragma unroll
-            for (int t = 0; t < WG; t++) {
-                const uint32_t q = to_e2m1(n + 8 * t, inv);
-                // zeros without a sign: bit 3 stays where a magnitude bit is set
-                packed[WG * g + t] = q & (0x77777777u | ((q & 0x77777777u) + 0x77777777u));
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < WG; t++) {
-                uint32_t d = 0;
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float x = __builtin_amdgcn_ldexpf(n[8 * t + i], shift);
-                    const uint32_t c = (uint32_t)magnitude_code(fabsf(x), alpha);
-                    d |= (c | (c && x < 0.0f ? 8u : 0u)) << (4 * i);
-                }
-                packed[WG * g + t] = d;
+            for (int i = 0; i < 8; i++) {
+                const float e = fmaf(-as, d[i], x[i]);
+                sum[i] = fmaf(e, e, sum[i]);
             }
         }
-        const int gi = G == 128 ? o.kc / 2 : 64 * o.kc / G + g;
-        if (o.h == 0 && (G < 128 || o.kc % 2 == 0))
-            scales[((int64_t)o.nt * L.groups + gi) * 32 + o.r] =
-                o.n < L.N && (int64_t)gi * G < L.K ? (__bf16)alpha : (__bf16)0.0f;
+        float err = row_sum<G>(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
+        // a candidate that overflows is passed over; one equal to a kept one adds nothing
+        err = x6 < inf && a != alpha && a != other ? err : inf;
+        const bool first = err < least, next = err < second;
+        other = first ? alpha : next ? a : other;
+        other_first = first || (other_first && !next);
+        alpha = first ? a : alpha;
+        third = fminf(third, fmaxf(second, err));
+        second = __builtin_amdgcn_fmed3f(least, second, err);
+        least = fminf(least, err);
     }
-    if (o.kc < L.chunks)
-        *(uint4*)(out + 1024 * ((int64_t)o.nt * L.chunks + o.kc) + 16 * (32 * o.h + o.r)) =
-            uint4{packed[0], packed[2], packed[1], packed[3]};
+    const float near = least * (1.0f + 0x1p-19f);
+    if (__any(finite && m && (far || third <= near))) {
+        const float exact = search_exact<T, G>(o, w + (o.n < L.N ? o.n : 0) * ldw, o.n < L.N ? L.K : 0, top, factors, nf);
+        if (finite) alpha = exact;
+    } else if (__any(finite && m && second <= near)) {
+        const double e0 = row_sum<G>(exact_error<WG>(n, __builtin_amdgcn_ldexpf(alpha, -shift)));
+        const double e1 = row_sum<G>(exact_error<WG>(n, __builtin_amdgcn_ldexpf(other, -shift)));
+        if (second <= near && (other_first ? e1 <= e0 : e1 < e0)) alpha = other;
+    }
+    if (!finite) alpha = __builtin_nanf("");
+    const float as = __builtin_amdgcn_ldexpf(alpha, -shift);
+
+    // (1/as) of a scale far below the weights may be infinite
+    if (sizeof(T) == 2 && !__any(finite && m && as < 0x1p-100f)) {
+        const float inv = m && alpha == alpha ? 1.0f / as * (1.0f + 0x1p-22f) : 0.0f;
+#pragma unroll
+        for (int t = 0; t < WG; t++) {
+            const uint32_t q = to_e2m1(n + 8 * t, inv);
+            // zeros without a sign: bit 3 stays where a magnitude bit is set
+            packed[t] = q & (0x77777777u | ((q & 0x77777777u) + 0x77777777u));
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < WG; t++) {
+            uint32_t d = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float x = __builtin_amdgcn_ldexpf(n[8 * t + i], shift);
+                const uint32_t c = (uint32_t)magnitude_code(fabsf(x), alpha);
+                d |= (c | (c && x < 0.0f ? 8u : 0u)) << (4 * i);
+            }
+            packed[t] = d;
+        }
+    }
+    if (o.h == 0 && (G < 128 || o.kc % 2 == 0))
+        ((__bf16*)(out + L.scale_offset))[((int64_t)o.nt * L.groups + o.gi) * 32 + o.r] =
+            o.n < L.N && (int64_t)o.gi * G < L.K ? (__bf16)alpha : (__bf16)0.0f;
+    o.put(L, packed, out);
 }
 
 // Four ESB(4,1) codes, one a byte, to E2M1 nibbles in the bytes 0 and 2: one more in the exponent field,
@@ -396,11 +401,14 @@ unsigned tile_blocks(const W4Layout& L) {   // a wave per two chunks
 template <typename T>
 hipError_t quantize_t(const W4Layout& L, const void* w, int64_t ldw, const float* f, int nf, void* out,
                       hipStream_t s) {
-    const int64_t waves = L.group == 128 ? (int64_t)L.tiles * 2 * ((L.chunks + 1) / 2) : (int64_t)L.tiles * L.chunks;
-    const unsigned b = (unsigned)((waves + 3) / 4);
-    if (L.group == 32) k_w4_quantize<T, 32><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
-    else if (L.group == 64) k_w4_quantize<T, 64><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
-    else k_w4_quantize<T, 128><<<b, 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
+    auto go = [&](auto group, auto kernel) {
+        constexpr int G = decltype(group)::value;
+        const int64_t waves = (int64_t)L.tiles * Share<G>::across(L);
+        kernel<<<dim3((unsigned)((waves + 3) / 4), G == 64 ? 1 : 2), 256, 0, s>>>(L, (const T*)w, ldw, f, nf, (uint8_t*)out);
+    };
+    if (L.group == 32) go(std::integral_constant<int, 32>(), k_w4_quantize<T, 32>);
+    else if (L.group == 64) go(std::integral_constant<int, 64>(), k_w4_quantize<T, 64>);
+    else go(std::integral_constant<int, 128>(), k_w4_quantize<T, 128>);
     return hipGetLastError();
 }
 
