@@ -201,9 +201,10 @@ __device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
 // Bound by VALU issue (97 % of all cycles busy): for two weights and a candidate two products with 1/alpha,
 // a conversion to fp4 (a quarter of the fp32 rate), one back, two remainders and two squares, some 22
 // cycles of a SIMD per 64 weights.  4096 x 9216 bf16 weights, G = 128, 16 candidates: 101-110 us (the
-// bytes alone: 18); 1000 x 1999 fp16, G = 32, 8 candidates: 9 us (11 with both groups of a row in a lane).  Dot products of 16-bit pairs would
-// halve the sums but lose seven bits to cancellation, and fp4 from 16-bit products moves the cell
-// bounds: both would send groups by the percent, not by the ten-thousand, to the fp64 comparison.
+// bytes alone: 18); 1000 x 1999 fp16, G = 32, 8 candidates: 9 us (11 with both groups in a lane).
+// Dot products of 16-bit pairs would halve the sums but lose seven bits to cancellation, and fp4 from
+// 16-bit products moves the cell bounds: both would send groups by the percent, not by the
+// ten-thousand, to the fp64 comparison.
 template <typename T, int G>
 __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __restrict__ w, int64_t ldw,
                                                      const float* __restrict__ factors, int nf,
