@@ -215,7 +215,7 @@ __device__ __forceinline__ int xcd_run(int id, int total) {
 // instructions).  Of 128 products of E4M3 rows that is at most 2^-6 and in practice some 10^-4 of
 // their root mean square: under the rounding of a 16-bit output (2^-9, 2^-12), so fp32 outputs
 // take the bf16 MFMAs, which keep every product.
-__device__ __align__(16) const uint8_t kZero16[16] = {0};
+__device__ __align__(16) const uint8_t kZeros[1024] = {0};
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
@@ -273,41 +273,50 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
 
     // Rows: DMA i of the wave serves rows 8 (wave + i NW) + lane / 8 and writes slot lane % 8 of each,
     // so it fetches piece (lane % 8) ^ (row / 2 % 8).  Through registers, the same rows and pieces.
-    const X* xp[NX];
+    const X* xb = (const X*)p.x + m0 * p.ldx;
+    int64_t xo[NX];
     int pc[NX];
 #pragma unroll
     for (int i = 0; i < NX; i++) {
         const int64_t m = m0 + 8 * (wave + i * NW) + (lane >> 3);
         pc[i] = (lane & 7) ^ (((8 * (wave + i * NW) + (lane >> 3)) >> 1) & 7);
-        xp[i] = (const X*)p.x + (m < p.M ? m : p.M - 1) * p.ldx + EP * pc[i];
+        xo[i] = ((m < p.M ? m : p.M - 1) - m0) * p.ldx + EP * pc[i];
     }
     // Weight tiles wave + i NW of the stage's [row tile][chunk]; rows of tiles past N read the last.
     const uint8_t* wp[NT];
 #pragma unroll
     for (int i = 0; i < NT; i++) {
         const int q = wave + i * NW;
-        wp[i] = p.w4 + ((int64_t)min(nt0 + q / NC, p.L.tiles - 1) * chunks + q % NC) * 1024 + 16 * lane;
+        wp[i] = p.w4 + ((int64_t)min(nt0 + q / NC, p.L.tiles - 1) * chunks + q % NC) * 1024;
     }
     // The wave's own scales, [row tile j][group g of the step][32 rows], 16 lanes each.
-    const int sj = (lane >> 4) / NG & 1, sg = (lane >> 4) % NG;
-    const uint8_t* sp = p.w4 + p.L.scale_offset +
-                        (int64_t)min(nt0 + 2 * wn + sj, p.L.tiles - 1) * p.L.groups * 64 + 4 * (lane & 15);
+    const int sj = (lane >> 4) / NG & 1, sg = (lane >> 4) % NG, snt = min(nt0 + 2 * wn, p.L.tiles - 1);
+    const uint8_t* sp = p.w4 + p.L.scale_offset + (int64_t)snt * p.L.groups * 64;
+    const uint32_t so = (uint32_t)(sj && snt + 1 < p.L.tiles ? p.L.groups * 64 : 0) + 4 * (lane & 15);
 
-    // every stage issues the same number of DMAs, also past the last step
+    // Every stage issues the same number of DMAs, also past the last step.  What differs between lanes fits
+    // 32 bits (rows closer than 2^24 elements), so a whole step's addresses are scalar but for one sum.
+    const int whole = p.ldx < 1 << 24 ? min(end, K / BK) : 0;
     auto fetch = [&](int s, uint8_t* slot) {
         if constexpr (DMA) {
+            if (s < whole) {
+                const char* base = (const char*)(xb + (int64_t)s * BK);
 #pragma unroll
-            for (int i = 0; i < NX; i++)
-                dma16(s * BK + EP * pc[i] < K && s < end ? (const void*)(xp[i] + s * BK) : (const void*)kZero16, slot + 1024 * (wave + i * NW));
+                for (int i = 0; i < NX; i++) dma16(base + (uint32_t)xo[i] * (uint32_t)sizeof(X), slot + 1024 * (wave + i * NW));
+            } else {
+#pragma unroll
+                for (int i = 0; i < NX; i++)
+                    dma16(s * BK + EP * pc[i] < K && s < end ? (const void*)(xb + xo[i] + s * BK) : (const void*)kZeros,
+                          slot + 1024 * (wave + i * NW));
+            }
         }
 #pragma unroll
         for (int i = 0; i < NT; i++) {
             const bool in = s * NC + (wave + i * NW) % NC < chunks;
-            dma16(in ? (const void*)(wp[i] + (int64_t)s * (NC * 1024)) : (const void*)kZero16,
-                    slot + XB + 1024 * (wave + i * NW));
+            dma16((in ? wp[i] + (int64_t)s * (NC * 1024) : kZeros) + (uint32_t)(16 * lane), slot + XB + 1024 * (wave + i * NW));
         }
         const int gi = min(F8 || G < 128 ? NG * s + sg : s >> 1, p.L.groups - 1);
-        dma4(sp + (int64_t)gi * 64, slot + XB + WB + 256 * wave);
+        dma4(sp + ((uint32_t)gi * 64 + so), slot + XB + WB + 256 * wave);
     };
     Raw st[DMA ? 1 : NX][F8 ? 2 : 1];
     auto load = [&](int s) {
@@ -316,13 +325,13 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
 #pragma unroll
             for (int i = 0; i < NX; i++)
 #pragma unroll
-                for (int u = 0; u < (F8 ? 2 : 1); u++) st[i][u] = Act<X>::load(xp[i] + k + 8 * u, 8);
+                for (int u = 0; u < (F8 ? 2 : 1); u++) st[i][u] = Act<X>::load(xb + xo[i] + k + 8 * u, 8);
         } else {
 #pragma unroll
             for (int i = 0; i < NX; i++)
 #pragma unroll
                 for (int u = 0; u < (F8 ? 2 : 1); u++)
-                    st[i][u] = Act<X>::load(xp[i] + k + 8 * u, K - k - EP * pc[i] - 8 * u);
+                    st[i][u] = Act<X>::load(xb + xo[i] + k + 8 * u, K - k - EP * pc[i] - 8 * u);
         }
     };
     auto put = [&](uint8_t* slot) {
