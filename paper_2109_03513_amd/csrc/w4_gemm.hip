@@ -13,9 +13,9 @@
 //    E4M3 rows 7.1 us.
 //  * k_w4_tile: tiles of 32 to 128 rows, everything through a ring in LDS; with few tiles the
 //    reduction is split over workgroups and k_w4_sum adds the parts.  Few rows are bound by the chain of
-//    a step (64 fp16 rows of 9216 x 4096, G = 32: 17.4 us), many by power and by MFMA and VALU issue:
-//    4096 E4M3 rows of 18432 x 4096, G = 128 272 us, 2.3 PFLOP/s, MFMA busy 53 % and VALU 51 % of cycles
-//    at 2.0 GHz; 1999 bf16 rows of 4096 x 9216, G = 64 146 us, 1.03 PFLOP/s, MFMA 42 %, VALU 46 %.
+//    a step (64 fp16 rows of 9216 x 4096, G = 32: 16.9 us), many by power and by MFMA and VALU issue:
+//    4096 E4M3 rows of 18432 x 4096, G = 128 276 us, 2.2 PFLOP/s, MFMA busy 55 % and VALU 48 % of cycles
+//    at 2.0 GHz; 1999 bf16 rows of 4096 x 9216, G = 64 146 us, 1.03 PFLOP/s, MFMA 46 %, VALU 46 %.
 //    With rows of zeros the same products take 20 to 25 % less; tiles of 128 x 512 and 256 x 256, which
 //    bring a quarter to a third fewer bytes per product into a CU, and an fma after every MFMA instead
 //    of in groups all came out within 4 % or slower.
