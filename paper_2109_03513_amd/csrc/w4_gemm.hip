@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
     // The wave's own scales, [row tile j][group g of the step][32 rows], 16 lanes each.
     const int sj = (lane >> 4) / NG & 1, sg = (lane >> 4) % NG, snt = min(nt0 + 2 * wn, p.L.tiles - 1);
     const uint8_t* sp = p.w4 + p.L.scale_offset + (int64_t)snt * p.L.groups * 64;
-    const uint32_t so = (uint32_t)(sj && snt + 1 < p.L.tiles ? p.L.groups * 64 : 0) + 4 * (lane & 15);
+    const uint32_t so = (sj && snt + 1 < p.L.tiles ? (uint32_t)p.L.groups * 64 : 0) + 4 * (lane & 15);
 
     // Every stage issues the same number of DMAs, also past the last step.  What differs between lanes fits
     // 32 bits (rows closer than 2^24 elements), so a whole step's addresses are scalar but for one sum.
