@@ -214,6 +214,24 @@ def test_offsets_beyond_32_bits(esb):
     check(yd, xv, s, codes, alpha, 32)
 
 
+@pytest.mark.parametrize("M", [1, 20, 150])
+@pytest.mark.parametrize("x", ["bf16", "e4m3"])
+@pytest.mark.parametrize("K,group", [((1 << 23) + 64, 64), ((1 << 24) + 96, 128)])
+def test_long_rows(esb, M, x, K, group):
+    """Rows of millions of columns, zeros but for the last ones: those meet their own weights."""
+    log("w4 gemm M=%d K=%d %s" % (M, K, x))
+    N, at = 40, K // group * group - 2 * group
+    g = torch.Generator(device="cuda").manual_seed(M)
+    codes = torch.randint(0, 16, (N, K), generator=g, dtype=torch.uint8, device="cuda")
+    alpha = (0.01 * (1 + torch.rand(N, -(-K // group), generator=g, device="cuda"))).to(torch.bfloat16)
+    w4 = esb.esb_w4_pack(codes, alpha, group)
+    xv, s = acts(M, M, K - at, x)
+    xd = torch.zeros(M, K, dtype=torch.uint8 if x == "e4m3" else XT[x], device="cuda").view(XT[x])
+    xd[:, at:] = xv.cuda()
+    y = esb.esb_w4_gemm(xd, w4, N, group, x_scale=None if s is None else s.cuda())
+    check(y, xv, s, codes[:, at:].cpu(), alpha[:, at // group:].cpu(), group)
+
+
 def test_weights_beyond_32_bits(esb):
     """Packed weights of more than 2^32 bytes: the last rows read their own tiles."""
     N, K, group = 270016, 32768, 128
