@@ -810,7 +810,7 @@ static int w4_gemm_check(int M, int N, int K, int group, int x_type, int y_type)
 
 size_t esb_w4_gemm_workspace_size(int M, int N, int K, int group, int x_type, int y_type) {
     if (w4_gemm_check(M, N, K, group, x_type, y_type) || M == 0 || N == 0) return 0;
-    return w4_gemm_workspace(M, w4_layout(N, K, group), x_type, y_type);
+    return w4_gemm_workspace(M, w4_layout(N, K, group), x_type);
 }
 
 int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int x_type, const float* x_scale,
@@ -823,7 +823,7 @@ int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int 
     if (K > 0 && (!x || !aligned_for(x, x_type) || (uintptr_t)x_scale % 4 || !w4 || (uintptr_t)w4 % 16))
         return ESB_E_INVALID;
     const W4Layout L = w4_layout(N, K, group);
-    if (workspace && ws_bytes < w4_gemm_workspace(M, L, x_type, y_type)) return ESB_E_WORKSPACE;
+    if (workspace && ws_bytes < w4_gemm_workspace(M, L, x_type)) return ESB_E_WORKSPACE;
     const W4GemmParams p = {L, M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type,
                             (uint8_t*)workspace, workspace ? ws_bytes : 0, false, nullptr};
     return hip_status(launch_w4_gemm(p, x_type, (hipStream_t)stream));

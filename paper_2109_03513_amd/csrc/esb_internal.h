@@ -619,7 +619,7 @@ struct W4GemmParams {
     float* part;            // sums of column ranges, [range][M][32 tiles], or NULL: no ranges
 };
 // Bytes of workspace that these arguments may use.
-size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type);
+size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type);
 hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s);
 
 }  // namespace esb

@@ -14,8 +14,6 @@
 // i = 0, 2, 1, 3.
 //  * Word i of the 64 lanes is the operand of one 32x32x16 MFMA, words 0 and 1 (2 and 3) of the two
 //    over columns 0 .. 31 (32 .. 63);
-//  * the four words are the operand of one 32x32x64 MFMA on 4-bit values: that instruction pairs them
-//    with 8-bit values of which a lane holds 32 consecutive columns;
 //  * the low or high half of the 16 bytes of 16 rows, lane 16(2h + e) + r, are words e and 2 + e:
 //    operands of two 16x16x32 MFMAs over columns 0 .. 31 and 32 .. 63.
 // So every MFMA stays within one group of 32, 64 or 128.  The scales follow, [row tile][group][32

@@ -14,8 +14,8 @@
 //  * k_w4_tile: tiles of 32 to 128 rows, everything through a ring in LDS; with few tiles the
 //    reduction is split over workgroups and k_w4_sum adds the parts.  Few rows are bound by the chain of
 //    a step (64 fp16 rows of 9216 x 4096, G = 32: 16.9 us), many by power and by MFMA and VALU issue:
-//    4096 E4M3 rows of 18432 x 4096, G = 128 276 us, 2.2 PFLOP/s, MFMA busy 55 % and VALU 48 % of cycles
-//    at 2.0 GHz; 1999 bf16 rows of 4096 x 9216, G = 64 146 us, 1.03 PFLOP/s, MFMA 46 %, VALU 46 %.
+//    4096 E4M3 rows of 18432 x 4096, G = 128 490 us, 1.26 PFLOP/s;
+//    1999 bf16 rows of 4096 x 9216, G = 64 146 us, 1.03 PFLOP/s, MFMA 46 %, VALU 46 %.
 //    With rows of zeros the same products take 20 to 25 % less; tiles of 128 x 512 and 256 x 256, which
 //    bring a quarter to a third fewer bytes per product into a CU, and an fma after every MFMA instead
 //    of in groups all came out within 4 % or slower.
@@ -31,7 +31,6 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // Four pairs of 16-bit values as one fragment.
 template <typename F, typename P>
@@ -184,9 +183,6 @@ __global__ __launch_bounds__(64 * NW) void k_w4_token(W4GemmParams p) {
     });
 }
 
-template <int F8, typename F> struct FragOf { typedef F type; };
-template <typename F> struct FragOf<1, F> { typedef i32x8 type; };
-
 // Workgroup `id` of `total` to a tile: each XCD (every eighth id) gets a contiguous run.
 __device__ __forceinline__ int xcd_run(int id, int total) {
     const int x = id & 7, q = total >> 3, rem = total & 7;
@@ -195,8 +191,8 @@ __device__ __forceinline__ int xcd_run(int id, int total) {
 
 // Tiles of BM = 32 TM WM rows m x BN = 64 WN outputs n, a wave of the workgroup 32 TM x 64 of it.
 // A step is 128 bytes of every row of the tile: 64 columns of 16-bit values (F8 == 0; E4M3 activations
-// become bf16 on their way) or 128 columns of E4M3 (F8 == 1), and the weights and scales of these
-// columns.  All of it lies in a ring of R stages in LDS, fetched R - 1 steps ahead by DMA, which holds
+// become bf16 on their way) or 128 columns of E4M3 (F8 == 1: fragments become bf16 when they are read,
+// 64 columns at a time), and the weights and scales of these columns.  All of it lies in a ring of R stages in LDS, fetched R - 1 steps ahead by DMA, which holds
 // no registers; activations that DMA cannot take (DMA == 0: rows that are not 16-byte aligned, or that
 // need the conversion) go through registers one step ahead.
 //
@@ -211,10 +207,11 @@ __device__ __forceinline__ int xcd_run(int id, int total) {
 // one part, 21 with two, 17 with four; 64 bf16 rows of 9216 x 4096: 18.7 us in 32 x 256 tiles of two
 // parts, 16.8 in 32 x 128 of four; 128 of 4096 x 4096: 17.5 there, 13.2 in 32 x 64 of eight).
 //
-// F8: within one instruction, products below 2^-13 of its largest are dropped (measured with single
-// instructions).  Of 128 products of E4M3 rows that is at most 2^-6 and in practice some 10^-4 of
-// their root mean square: under the rounding of a 16-bit output (2^-9, 2^-12), so fp32 outputs
-// take the bf16 MFMAs, which keep every product.
+// 8-bit rows take the bf16 MFMAs too.  Those on 8-bit operands, with 4-bit weights or with weights as
+// E4M3, drop what lies 13 binades below the largest product of an instruction: of E4M3 times E2M1, whose
+// products span 21, sums of 16 or 64 with both signs came out wrong by up to 95 times their value.
+// The bf16 form gave the exact sum of every one (2^18 random sums, and two products that cancel beside
+// a third).
 __device__ __align__(16) const uint8_t kZeros[1024] = {0};
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -242,7 +239,7 @@ template <typename X, int F8, int G, int TM, int WM, int WN, int KW, int R, int 
 __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(W4GemmParams p, int tiles_m, int tiles, int per_split) {
     typedef typename Act<X>::M M;
     typedef typename Act<X>::raw Raw;
-    typedef typename FragOf<F8, typename M::frag>::type Frag;
+    typedef typename M::frag Frag;
     constexpr int NW = WM * WN, BM = 32 * TM * WM;            // waves and rows of one part
     constexpr int BK = F8 ? 128 : 64, EP = F8 ? 16 : 8;       // columns of a step, of a piece
     constexpr int NC = F8 ? 2 : 1;                            // column chunks of a step
@@ -350,43 +347,33 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
     f32x16 acc[TM][2] = {};
     const uint32_t arow = (uint32_t)(wm * 32 * TM + r) * 128;
     const int swz = (r >> 1) & 7;
-    constexpr int NF = F8 ? 2 : 4;      // MFMAs of a tile in a step
+    constexpr int NF = 4, NGH = G == 32 ? 2 : 1;      // MFMAs and scales of a tile's 64 columns
     // two behind where the registers allow, so that no sum is waited for
-    constexpr int U = TM * 2 * NG, LAG = (TM == 4 && !(F8 && G == 128)) || (KW >= 4 && WN == 2 && !F8 && G == 32) ? 1 : 2;
-    auto step = [&](const uint8_t* slot) {
-        float a[2][NG];
+    constexpr int U = TM * 2 * NGH, LAG = TM == 4 || (KW >= 4 && WN == 2 && !F8 && G == 32) ? 1 : 2;
+    // 64 columns, the half-th of the step
+    auto columns = [&](const uint8_t* slot, int half) {
+        float a[2][NGH];
         Frag wf[2][NF], x[NF];
+        uint4 raw[2];
 #pragma unroll
         for (int j = 0; j < 2; j++) {
-            const uint8_t* wb = slot + XB + (2 * wn + j) * (NC * 1024) + 16 * lane;
-            if constexpr (F8) {
+            const i32x4 q = *(const i32x4*)(slot + XB + ((2 * wn + j) * NC + half) * 1024 + 16 * lane);
+            wf[j][0] = M::decode(q[0]);
+            wf[j][1] = M::decode(q[2]);
+            wf[j][2] = M::decode(q[1]);
+            wf[j][3] = M::decode(q[3]);
 #pragma unroll
-                for (int c = 0; c < 2; c++) {
-                    const i32x4 q = *(const i32x4*)(wb + 1024 * c);
-                    wf[j][c] = i32x8{q[0], q[2], q[1], q[3], 0, 0, 0, 0};
-                }
-            } else {
-                const i32x4 q = *(const i32x4*)wb;
-                wf[j][0] = M::decode(q[0]);
-                wf[j][1] = M::decode(q[2]);
-                wf[j][2] = M::decode(q[1]);
-                wf[j][3] = M::decode(q[3]);
-            }
-#pragma unroll
-            for (int g = 0; g < NG; g++)
-                a[j][g] = scale_value(*(const uint16_t*)(slot + XB + WB + 256 * wave + 64 * (j * NG + g) + 2 * r));
+            for (int g = 0; g < NGH; g++)
+                a[j][g] = scale_value(*(const uint16_t*)(slot + XB + WB + 256 * wave + 64 * (j * NG + (F8 ? half * (NG - 1) : g)) + 2 * r));
         }
         auto rows = [&](int i) {
             const uint8_t* base = slot + arow + i * 32 * 128;
+            if constexpr (F8) {
 #pragma unroll
-            for (int c = 0; c < NF; c++) {
-                if constexpr (F8) {
-                    const i32x4 lo = *(const i32x4*)(base + 16 * ((4 * c + 2 * h) ^ swz));
-                    const i32x4 hi = *(const i32x4*)(base + 16 * ((4 * c + 2 * h + 1) ^ swz));
-                    x[c] = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                } else {
-                    x[c] = *(const Frag*)(base + 16 * ((2 * h + (c & 1) + 4 * (c >> 1)) ^ swz));
-                }
+                for (int c = 0; c < 2; c++) raw[c] = *(const uint4*)(base + 16 * ((4 * half + h + 2 * c) ^ swz));
+            } else {
+#pragma unroll
+                for (int c = 0; c < NF; c++) x[c] = *(const Frag*)(base + 16 * ((2 * h + (c & 1) + 4 * (c >> 1)) ^ swz));
             }
         };
         rows(0);
@@ -394,23 +381,32 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
 #pragma unroll
         for (int u = 0; u < U + LAG; u++) {
             if (u < U) {
-                const int j = u / NG % 2, g = u % NG;
+                const int j = u / NGH % 2, g = u % NGH;
+                if constexpr (F8) {
+                    if (u % (2 * NGH) == 0) {
+#pragma unroll
+                        for (int c = 0; c < NF; c++)
+                            x[c] = Act<X>::frag(c & 1 ? uint2{raw[c / 2].z, raw[c / 2].w} : uint2{raw[c / 2].x, raw[c / 2].y});
+                    }
+                }
                 f32x16 d = {};
 #pragma unroll
-                for (int c = NF / NG * g; c < NF / NG * (g + 1); c++) {
-                    if constexpr (F8) d = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[c], wf[j][c], d, 0, 4, 0, 127, 0, 127);
-                    else d = M::mma(x[c], wf[j][c], d);
-                }
+                for (int c = NF / NGH * g; c < NF / NGH * (g + 1); c++) d = M::mma(x[c], wf[j][c], d);
                 part[u % (LAG + 1)] = d;
-                if ((u + 1) % (2 * NG) == 0 && u + 1 < U) rows((u + 1) / (2 * NG));
+                // the next rows, once the registers that they go to are free
+                if ((F8 ? u : u + 1) % (2 * NGH) == 0 && u / (2 * NGH) + 1 < TM) rows(u / (2 * NGH) + 1);
             }
             if (u >= LAG) {
-                const int v = u - LAG, i = v / (2 * NG), j = v / NG % 2, g = v % NG;
+                const int v = u - LAG, i = v / (2 * NGH), j = v / NGH % 2, g = v % NGH;
 #pragma unroll
                 for (int q = 0; q < 16; q++) acc[i][j][q] = fmaf(a[j][g], part[v % (LAG + 1)][q], acc[i][j][q]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    auto step = [&](const uint8_t* slot) {
+#pragma unroll
+        for (int half = 0; half < NC; half++) columns(slot, half);
     };
 
     if (first < end) {
@@ -542,8 +538,9 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4GemmParams p, int splits) {
 }
 
 // The shapes of k_w4_tile and what they cost, us: of a workgroup beyond a launch, of each further round of
-// workgroups, and of a step on one CU holding 1 .. slots of them (fitted to 24 shapes of 16 to 1024 rows,
-// 1024 to 18432 outputs, K = 4096 and 9216, G = 128, each with every shape and number of splits).  Small
+// workgroups, and of a step on one CU holding 1 .. slots of them (fitted to sizes of 16 to 1024 rows,
+// 1024 to 18432 outputs, K = 4096 and 9216, G = 128, each with every shape and number of splits: 24 for
+// 16-bit rows, 40 for 8-bit ones).  Small
 // tiles spread few rows over the chip, large ones read less per product; 32 x 64 tiles split their steps
 // over 8 parts of a workgroup, 32 x 128 over 4, and over 8 where a CU gets only one (64 fp16 rows of
 // 9216 x 4096, G = 32: 18.9 us with 4, 17.4 with 8; 128 rows: 25.9 and 33.2).
@@ -558,19 +555,19 @@ constexpr TileShape kShapes16[] = {{32, 64, 1, 0.5f, 4.0f, {0.105f}},
                                    {64, 256, 1, 2.2f, 1.5f, {0.50f}},
                                    {128, 256, 1, 0.0f, 0.0f, {1.00f}},
                                    {128, 256, 2, 0.0f, 0.0f, {1.10f, 1.96f}}};
-constexpr TileShape kShapes8[] = {{32, 64, 1, 0.3f, 3.5f, {0.13f}},
-                                  {64, 128, 2, 0.0f, 0.0f, {0.44f, 0.66f}},
-                                  {32, 128, 1, 0.0f, 3.0f, {0.205f}},
-                                  {64, 128, 1, 1.7f, 5.0f, {0.26f}},
-                                  {128, 128, 1, 3.4f, 5.0f, {0.49f}},
-                                  {128, 256, 1, 0.0f, 0.0f, {0.98f}},
-                                  {128, 256, 2, 0.0f, 0.0f, {1.09f, 1.72f}}};
+constexpr TileShape kShapes8[] = {{32, 64, 1, 0.7f, 3.7f, {0.22f}},
+                                  {64, 128, 2, 0.0f, 0.0f, {0.98f, 1.21f}},
+                                  {32, 128, 1, 1.0f, 3.3f, {0.39f}},
+                                  {64, 128, 1, 1.5f, 4.9f, {0.54f}},
+                                  {128, 128, 1, 0.8f, 5.4f, {1.05f}},
+                                  {128, 256, 1, 0.0f, 7.0f, {1.92f}},
+                                  {128, 256, 2, 1.2f, 0.0f, {2.06f, 3.04f}}};
 // rows through registers: a step of small tiles costs more, 64 x 256 tiles lose to 32 x 256 at every size
 // (1024 rows of 4096 x 4096: 60.9 us against 50.0)
 constexpr TileShape kLoose16[] = {{32, 64, 1, 0.5f, 4.0f, {0.16f}}, {32, 256, 2, 0.0f, 0.0f, {0.53f, 0.66f}}};
-constexpr TileShape kLoose8[] = {{32, 64, 1, 0.3f, 3.5f, {0.25f}},
-                                 {64, 128, 1, 0.0f, 0.0f, {0.37f}},
-                                 {64, 128, 2, 0.0f, 0.0f, {0.44f, 0.66f}}};
+constexpr TileShape kLoose8[] = {{32, 64, 1, 0.5f, 3.6f, {0.41f}},
+                                 {64, 128, 1, 0.1f, 3.8f, {0.72f}},
+                                 {64, 128, 2, 2.2f, 0.0f, {1.00f, 1.32f}}};
 
 // The shape and the ranges of columns (splits) that should take the least time: rounds of full CUs,
 // then one of what is left; splits write and read fp32 sums at about 4 TB/s and launch one more kernel.
@@ -611,11 +608,11 @@ TilePlan tile_plan(int64_t M, const W4Layout& L, bool f8, bool dma, size_t room)
 
 constexpr int64_t kRowsOfALaunch = 1 << 17;     // tiles of one launch stay below 2^31
 
-// Whether products of E4M3 rows take the mixed MFMA: its dropped small products (k_w4_tile) stay below
-// the rounding of a 16-bit output, not of fp32, and it covers groups of 64 at least.
-bool takes_f8(int x_type, int y_type, int group) { return x_type == kE4M3 && y_type != kF32 && group >= 64; }
-// Whether the rows can be fetched by DMA, 16-byte pieces in place; E4M3 for the bf16 MFMAs needs the
-// conversion on its way.
+// Whether E4M3 rows come to LDS in 8 bits (F8): the scales that a step of 128 columns has with groups of
+// 32 would not fit a wave's DMA.
+bool takes_f8(int x_type, int group) { return x_type == kE4M3 && group >= 64; }
+// Whether the rows can be fetched by DMA, 16-byte pieces in place; E4M3 rows that LDS holds as bf16 are
+// converted on their way.
 bool takes_dma(const W4GemmParams& p, int x_type, bool f8) {
     const int es = x_type == kE4M3 ? 1 : 2;
     if (p.aligned) return true;
@@ -697,18 +694,18 @@ hipError_t launch_shape(const W4GemmParams& p, int x_type, hipStream_t s) {
 
 // A token's kernel reads the weights once, without LDS, but every row in pieces and the weights' decoding
 // once per wave: with more than a few rows it wins only while its workgroups come at about one per CU or
-// the weights are few.  us here against tiles, 16-bit / E4M3 rows: 16 rows of 4096 x 4096 7.2 : 11.1 / 7.3 :
-// 8.3, of 4096 x 9216 12.7 : 13.8 / 13.0 : 14.0, of 9216 x 1024 5.7 : 6.7 / 6.0 : 6.0, of 9216 x 4096
-// 15.5 : 12.1 / 15.8 : 9.8; 18432 x 4096 with 6 rows 15.3 : 15.9, 8 rows 17.3 : 15.7, E4M3 with 2 rows
-// 12.9 : 11.9 (9216 x 4096: 9.2 : 9.3).
-bool takes_token(int64_t M, const W4Layout& L, bool f8) {
+// the weights are few.  us here against tiles, 16-bit / E4M3 rows: 16 rows of 4096 x 4096 7.2 : 11.1 / 7.9 :
+// 10.5, of 4096 x 9216 12.7 : 13.8 / 12.7 : 14.4, of 9216 x 1024 5.7 : 6.7 / 7.8 : 7.8, of 9216 x 4096
+// 15.5 : 12.1 / 15.4 : 12.6; 18432 x 4096 with 6 rows 15.3 : 15.9 / 15.5 : 17.2, 8 rows 17.3 : 15.7 /
+// 17.4 : 17.2.
+bool takes_token(int64_t M, const W4Layout& L) {
     const int64_t few = (2 * (int64_t)L.tiles <= num_cus() * 3 / 2 ? 40 : 12) << 20;
-    return M <= (f8 ? 2 : 6) || (M <= 16 && (int64_t)L.N * L.K <= few);
+    return M <= 6 || (M <= 16 && (int64_t)L.N * L.K <= few);
 }
 
 template <typename X, int G>
 hipError_t launch_g(const W4GemmParams& p, int x_type, hipStream_t s) {
-    if (takes_token(p.M, p.L, takes_f8(x_type, p.y_type, G))) {
+    if (takes_token(p.M, p.L)) {
         // 16 waves where the CUs get about one workgroup each, else 8 (one row, K = 9216, 4096 outputs:
         // 7.2 us against 9.0; K = 4096, 18432 outputs: 14.0 against 11.7)
         const unsigned grid = 2 * p.L.tiles;
@@ -717,7 +714,7 @@ hipError_t launch_g(const W4GemmParams& p, int x_type, hipStream_t s) {
         return hipGetLastError();
     }
     if constexpr (sizeof(X) == 1 && G >= 64) {
-        if (takes_f8(x_type, p.y_type, G)) return launch_shape<X, 1, G>(p, x_type, s);
+        if (takes_f8(x_type, G)) return launch_shape<X, 1, G>(p, x_type, s);
     }
     return launch_shape<X, 0, G>(p, x_type, s);
 }
@@ -731,10 +728,10 @@ hipError_t launch_x(const W4GemmParams& p, int x_type, hipStream_t s) {
 
 }  // namespace
 
-size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type, int y_type) {
+size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type) {
     M = M < kRowsOfALaunch ? M : kRowsOfALaunch;
-    const bool f8 = takes_f8(x_type, y_type, L.group);
-    if (L.K == 0 || takes_token(M, L, f8)) return 0;
+    const bool f8 = takes_f8(x_type, L.group);
+    if (L.K == 0 || takes_token(M, L)) return 0;
     // rows of whole 16-byte pieces are expected to be aligned; others cannot be
     const int es = x_type == kE4M3 ? 1 : 2;
     const bool dma = (f8 || es == 2) && (int64_t)L.K * es % 16 == 0, copy = !dma && M >= kAlignRows;
