@@ -409,34 +409,32 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
         for (int half = 0; half < NC; half++) columns(slot, half);
     };
 
-    if (first < end) {
-        // step first + i KW + part_k in slot i % R; a part's steps past the end add zeros
-        const int begin = first + part_k, turns = (end - first + KW - 1) / KW;
-        if constexpr (!DMA) {
-            load(begin);
-            put(ring);
-            load(begin + KW);
-        }
-#pragma unroll
-        for (int q = 0; q < R - 1; q++) fetch(begin + q * KW, ring + q * STAGE);
-        int cur = 0, last = R - 1;           // slots of this turn and of the one before it
-        for (int i = 0; i < turns; i++) {
-            const int s = begin + i * KW;
-            vm_wait<(R - 2) * PER>();        // this wave's part of step s has landed
-            lds_barrier();                   // all of it; every read of the last turn is done
-            __builtin_amdgcn_sched_barrier(0);
-            fetch(s + (R - 1) * KW, ring + last * STAGE);
-            if constexpr (!DMA) {
-                put(ring + (cur + 1 == R ? 0 : cur + 1) * STAGE);
-                load(s + 2 * KW);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            step(ring + cur * STAGE);
-            last = cur;
-            cur = cur + 1 == R ? 0 : cur + 1;
-        }
-        vm_wait<0>();                        // no DMA outlives its workgroup
+    // step first + i KW + part_k in slot i % R; a part's steps past the end add zeros
+    const int begin = first + part_k, turns = (end - first + KW - 1) / KW;
+    if constexpr (!DMA) {
+        load(begin);
+        put(ring);
+        load(begin + KW);
     }
+#pragma unroll
+    for (int q = 0; q < R - 1; q++) fetch(begin + q * KW, ring + q * STAGE);
+    int cur = 0, last = R - 1;           // slots of this turn and of the one before it
+    for (int i = 0; i < turns; i++) {
+        const int s = begin + i * KW;
+        vm_wait<(R - 2) * PER>();        // this wave's part of step s has landed
+        lds_barrier();                   // all of it; every read of the last turn is done
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(s + (R - 1) * KW, ring + last * STAGE);
+        if constexpr (!DMA) {
+            put(ring + (cur + 1 == R ? 0 : cur + 1) * STAGE);
+            load(s + 2 * KW);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        step(ring + cur * STAGE);
+        last = cur;
+        cur = cur + 1 == R ? 0 : cur + 1;
+    }
+    vm_wait<0>();                            // no DMA outlives its workgroup
     __syncthreads();
     if constexpr (KW > 1) {
         // the first part adds the sums of the others, in order
@@ -537,6 +535,18 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4GemmParams p, int splits) {
     });
 }
 
+// No columns: zeros, whatever x_scale holds.
+__global__ __launch_bounds__(256) void k_w4_zero(W4GemmParams p) {
+    const int64_t cols = (p.L.N + 7) / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.M * cols) return;
+    const int64_t m = i / cols;
+    const int n = 8 * (int)(i - m * cols);
+    with_y(p, [&](auto* y) {
+        typedef std::remove_reference_t<decltype(*y)> Y;
+        store8(y + m * p.ldy + n, typename Vec8<Y>::type{}, p.L.N - n);
+    });
+}
+
 // The shapes of k_w4_tile and what they cost, us: of a workgroup beyond a launch, of each further round of
 // workgroups, and of a step on one CU holding 1 .. slots of them (fitted to sizes of 16 to 1024 rows,
 // 1024 to 18432 outputs, K = 4096 and 9216, G = 128, each with every shape and number of splits: 24 for
@@ -622,8 +632,8 @@ bool takes_dma(const W4GemmParams& p, int x_type, bool f8) {
 template <typename X, int F8, int G, int TM, int WM, int WN, int KW, int R, int DMA>
 hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
     const int tm = (int)((p.M + 32 * TM * WM - 1) / (32 * TM * WM)), tn = (p.L.tiles + 2 * WN - 1) / (2 * WN);
-    const int steps = F8 ? (p.L.chunks + 1) / 2 : p.L.chunks, per = steps ? (steps + splits - 1) / splits : 0;
-    splits = steps ? (steps + per - 1) / per : 1;
+    const int steps = F8 ? (p.L.chunks + 1) / 2 : p.L.chunks, per = (steps + splits - 1) / splits;
+    splits = (steps + per - 1) / per;            // none without steps
     W4GemmParams q = p;
     q.part = splits > 1 ? (float*)p.ws : nullptr;
     k_w4_tile<X, F8, G, TM, WM, WN, KW, R, DMA><<<(unsigned)(tm * tn * splits), 64 * WM * WN * KW, 0, s>>>(q, tm, tm * tn, per);
@@ -726,6 +736,11 @@ hipError_t launch_x(const W4GemmParams& p, int x_type, hipStream_t s) {
     return launch_g<X, 128>(p, x_type, s);
 }
 
+hipError_t launch_zero(const W4GemmParams& p, hipStream_t s) {
+    k_w4_zero<<<(unsigned)((p.M * ((p.L.N + 7) / 8) + 255) / 256), 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t w4_gemm_workspace(int64_t M, const W4Layout& L, int x_type) {
@@ -746,9 +761,10 @@ hipError_t launch_w4_gemm(const W4GemmParams& p, int x_type, hipStream_t s) {
         q.x = (const char*)p.x + m * p.ldx * xs;
         if (p.x_scale) q.x_scale = p.x_scale + m;
         q.y = (char*)p.y + m * p.ldy * ys;
-        const hipError_t e = x_type == kBF16  ? launch_x<__bf16>(q, x_type, s)
-                             : x_type == kF16 ? launch_x<_Float16>(q, x_type, s)
-                                              : launch_x<uint8_t>(q, x_type, s);
+        const hipError_t e = p.L.K == 0        ? launch_zero(q, s)
+                             : x_type == kBF16 ? launch_x<__bf16>(q, x_type, s)
+                             : x_type == kF16  ? launch_x<_Float16>(q, x_type, s)
+                                               : launch_x<uint8_t>(q, x_type, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

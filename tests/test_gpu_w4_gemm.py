@@ -331,3 +331,19 @@ def test_refusals(esb):
         esb.esb_w4_gemm(x, w4, 20, 32, y=torch.zeros(2, 21, dtype=torch.bfloat16, device="cuda"))
     with pytest.raises(TypeError):
         esb.esb_w4_gemm(x, w4, 20, 32, y_dtype=torch.int32)
+
+
+@pytest.mark.parametrize("M", [1, 3, 17, 40, 128, 300])
+@pytest.mark.parametrize("x", ["bf16", "f16", "e4m3"])
+@pytest.mark.parametrize("y", ["bf16", "f16", "f32"])
+def test_no_columns(esb, M, x, y):
+    """K = 0 writes zeros, and them only, whatever the rows' scales hold."""
+    N = 77
+    none = torch.empty(1, dtype=torch.uint8, device="cuda")
+    xd = torch.empty(M, 0, dtype=XT[x], device="cuda")
+    s = torch.full((M,), float("nan"), device="cuda")
+    for group in (32, 64, 128):
+        for scale in (None, s):
+            out = torch.full((M, N + 5), 7.0, dtype=ref.TYPES[y], device="cuda")
+            esb.esb_w4_gemm(xd, none, N, group, x_scale=scale, y=out[:, :N])
+            assert not bool(out[:, :N].any()) and bool((out[:, N:] == 7).all())
