@@ -804,6 +804,8 @@ def _w4_buffer(w4, N, K, group, like):
 
 
 def _w4_check(w4, index):
+    if not isinstance(w4, _torch.Tensor) or not w4.is_cuda:
+        raise TypeError("w4 must be a CUDA (HIP) tensor")
     if w4.dtype != _torch.uint8 or w4.get_device() != index or not w4.is_contiguous():
         raise ValueError("w4 must be contiguous uint8 on cuda:%d" % index)
     return w4
@@ -862,7 +864,7 @@ def esb_w4_unpack(w4, N, K, group, values=None, alpha=None, stream=None):
     if stream is not None:
         with _on(stream):
             return esb_w4_unpack(w4, N, K, group, values, alpha)
-    index = w4.get_device()
+    index = w4.get_device() if isinstance(w4, _torch.Tensor) else -1
     _w4_check(w4, index)
     _w4_holds(L, w4, N, K, group)
     groups = -(-K // group) if group > 0 else 0

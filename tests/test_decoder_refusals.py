@@ -105,3 +105,14 @@ def test_products(L):
     assert size(1, 4096, 4096, 128, BF16, BF16) == 0 and size(4096, 18432, 4096, 128, E4M3, BF16) == 0
     assert size(2000, 4000, 4001, 64, BF16, BF16) >= 2000 * 4001 * 2       # rows to be aligned
     assert size(64, 4096, 4096, 100, BF16, BF16) == 0 and size(64, 4096, 4096, 128, F32, BF16) == 0
+
+
+def test_host_weights(L):
+    """Packed weights on the host are refused before anything is launched on their addresses."""
+    import torch
+    from paper_2109_03513_amd import esb
+    w4 = torch.zeros(L.esb_w4_size(32, 64, 32), dtype=torch.uint8)
+    with pytest.raises(TypeError):
+        esb.esb_w4_unpack(w4, 32, 64, 32)
+    with pytest.raises(TypeError):
+        esb.esb_w4_unpack(w4.numpy(), 32, 64, 32)
