@@ -916,6 +916,11 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=N
         need = L.esb_w4_gemm_workspace_size(M, N, K, group, tx, ty)
         if need:
             workspace = x.new_empty(need, dtype=_torch.uint8)
+    else:
+        if not isinstance(workspace, _torch.Tensor) or not workspace.is_cuda:
+            raise TypeError("workspace must be a CUDA (HIP) tensor")
+        if workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous on cuda:%d" % index)
     wp, wb = _ws(workspace)
     st = L.esb_w4_gemm(M, N, K, group, x.data_ptr(), ldx, tx, _addr(x_scale), w4.data_ptr(),
                        y.data_ptr(), ldy, ty, wp, wb, _stream(None))

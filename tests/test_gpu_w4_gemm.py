@@ -347,3 +347,22 @@ def test_no_columns(esb, M, x, y):
             out = torch.full((M, N + 5), 7.0, dtype=ref.TYPES[y], device="cuda")
             esb.esb_w4_gemm(xd, none, N, group, x_scale=scale, y=out[:, :N])
             assert not bool(out[:, :N].any()) and bool((out[:, N:] == 7).all())
+
+
+def test_workspaces_that_the_kernels_cannot_write(esb):
+    codes, alpha = weights(1, 512, 9216, 128)
+    w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), 128)
+    x = acts(2, 64, 9216, "bf16")[0].cuda()
+    need = esb.esb_w4_gemm_workspace_size(64, 512, 9216, 128, 1, 1)
+    with pytest.raises(TypeError):
+        esb.esb_w4_gemm(x, w4, 512, 128, workspace=torch.empty(need, dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        esb.esb_w4_gemm(x, w4, 512, 128, workspace=torch.empty(need, dtype=torch.uint8).numpy())
+    room = torch.zeros(2 * need, dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError):
+        esb.esb_w4_gemm(x, w4, 512, 128, workspace=room[::2])
+    with pytest.raises(esb.EsbError):
+        esb.esb_w4_gemm(x, w4, 512, 128, workspace=room[:need - 1])
+    assert not bool(room.any())
+    want = esb.esb_w4_gemm(x, w4, 512, 128)
+    assert torch.equal(esb.esb_w4_gemm(x, w4, 512, 128, workspace=room[:need]), want)
