@@ -23,14 +23,30 @@ namespace {
 constexpr float kE4M3Max = 448.0f;
 constexpr float kTiny = 0x1p-126f;
 
-// g / (1 + exp(-g)) within 9 roundings: exp by the hardware's exp2 of the rounded product -g log2(e),
-// corrected by what the product lost; the quotient by the hardware's reciprocal.
-__device__ __forceinline__ float silu(float g) {
-    const float c = __builtin_amdgcn_fmed3f(-g, -104.0f, 104.0f);     // exp is 0 or infinite beyond
+// exp(c) = 2^hi (1 + lo ln 2): hi the rounded product c log2(e), lo what the product lost.
+struct Exp2Parts {
+    float hi, lo;
+};
+__device__ __forceinline__ Exp2Parts exp2_parts(float c) {
     const float hi = c * 0x1.715476p+0f;
-    const float lo = fmaf(c, 0x1.4ae0cp-26f, fmaf(c, 0x1.715476p+0f, -hi));
-    const float e = __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0x1.62e43p-1f, 1.0f);
+    return {hi, fmaf(c, 0x1.4ae0cp-26f, fmaf(c, 0x1.715476p+0f, -hi))};
+}
+// g / (1 + exp(-g)) within 9 roundings for g >= kFar (and NaN): exp by the hardware's exp2, the quotient by
+// its reciprocal, whose results end at 2^-126, so at g = -87.
+constexpr float kFar = -64.0f;
+__device__ __forceinline__ float silu(float g) {
+    const Exp2Parts p = exp2_parts(__builtin_amdgcn_fmed3f(-g, -104.0f, 104.0f));   // exp is 0 beyond
+    const float e = __builtin_amdgcn_exp2f(p.hi) * fmaf(p.lo, 0x1.62e43p-1f, 1.0f);
     return g * __builtin_amdgcn_rcpf(1.0f + e);
+}
+// g / (1 + exp(-g)) * u for g < kFar, where it is g exp(g) u to fp32: the exponential's power of two is
+// applied last, so that only the result may leave the range of normal numbers (u 2^-16 does so only
+// under a result of 2^-190).  Below -256 it is 0 for every finite u; a gate of -infinity gives NaN.
+__device__ __forceinline__ float silu_far(float g, float u) {
+    const float c = fmaxf(g, -256.0f);
+    const Exp2Parts p = exp2_parts(c);
+    const float n = rintf(p.hi), m = __builtin_amdgcn_exp2f(p.hi - n) * fmaf(p.lo, 0x1.62e43p-1f, 1.0f);
+    return __builtin_amdgcn_ldexpf(c * m * (u * 0x1p-16f), (int)n + 16) + (g - c) * 0.0f;
 }
 
 // TPR threads to a row, NV vectors of eight elements to a thread (d <= 8 TPR NV).  With 64 threads a wave
@@ -78,8 +94,17 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows(RowsParams p) {
 #pragma unroll
                 for (int i = 0; i < 8; i++) ss = fma((double)x[i], (double)x[i], ss);
             } else {
+                const f32x8 g = x;
+                float least = g[0];
 #pragma unroll
-                for (int i = 0; i < 8; i++) x[i] = silu(x[i]) * y[i];
+                for (int i = 0; i < 8; i++) {
+                    x[i] = silu(g[i]) * y[i];
+                    least = fminf(least, g[i]);
+                }
+                if (least < kFar)
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        if (g[i] < kFar) x[i] = silu_far(g[i], y[i]);
             }
             v[u0 + u] = x;
         }

@@ -224,3 +224,26 @@ def test_refusals(esb):
         esb.esb_rmsnorm(x[:1].expand(4, 64), None, EPS)
     with pytest.raises(ValueError):
         esb.esb_swiglu(x, x[:3])
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_strongly_negative_gates(esb, t):
+    """Gates far below zero: small values, but whole ones, and a large `up` makes them large again.
+    The tolerance has no floor but half the output type's smallest step."""
+    dtype = ref.TYPES[t]
+    top = 6e4 if t == "f16" else 3e38
+    ups = [1.0, -1.0, 1e-4, 1e4, top] + ([2.0 ** 100, 1e-20, 1e-38] if t != "f16" else [])
+    g = torch.linspace(-260, -55, 821).to(dtype)
+    rows = [(g[i:i + 411], torch.full((411,), u).to(dtype)) for u in ups for i in (0, 410)]
+    g, u = [torch.stack(v) for v in zip(*rows)]
+    # one such gate among ordinary ones
+    g = torch.cat([g, torch.linspace(-4, 4, 411).to(dtype)[None]])
+    g[-1, 200] = -88.0
+    u = torch.cat([u, torch.full((1, 411), top / 8).to(dtype)])
+    y = ref.swiglu(g, u)
+    gy, g8, gs = esb.esb_swiglu(g.cuda(), u.cuda(), want_y=True)
+    ref.check_float(gy, y, GATE_REL)
+    assert float((gy[:, 0] != 0).sum()) >= 2 or t == "f16"
+    # bytes: where the row's largest value is a normal number
+    big = y.abs().amax(1) > 2.0 ** -110
+    ref.check_e4m3(g8[big.cuda()], gs[big.cuda()], y[big], GATE_REL, 2.0 ** -149)
