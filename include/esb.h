@@ -571,6 +571,8 @@ int esb_w4_unpack(const void* w4, int N, int K, int group, uint8_t* values, int6
  *   x_scale device, M fp32 (s_m), or NULL (ones);
  *   w4      device, the packed form of N x K weights with this group;
  *   y       device, M x N, y_type ESB_F32, ESB_BF16 or ESB_F16.
+ * Scales are finite or NaN: alpha NaN makes its outputs NaN, alpha infinite makes them infinite
+ * or, where parts of the group's sum are zero or differ in sign, NaN.
  * A group's products are exact and its sum is fp32, in an order fixed by the arguments, the
  * alignment of x and whether there is a workspace (the same call gives the same bits).
  *   workspace  device, 256-byte aligned, at least esb_w4_gemm_workspace_size() bytes (fp32 sums

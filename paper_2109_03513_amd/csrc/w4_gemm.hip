@@ -312,8 +312,10 @@ __global__ __launch_bounds__(64 * WM * WN * KW, KW == 4 ? 4 : 2) void k_w4_tile(
             const bool in = s * NC + (wave + i * NW) % NC < chunks;
             dma16((in ? wp[i] + (int64_t)s * (NC * 1024) : kZeros) + (uint32_t)(16 * lane), slot + XB + 1024 * (wave + i * NW));
         }
-        const int gi = min(F8 || G < 128 ? NG * s + sg : s >> 1, p.L.groups - 1);
-        dma4(sp + ((uint32_t)gi * 64 + so), slot + XB + WB + 256 * wave);
+        // steps past the end and groups past the last one get scales of 0: an infinite one of another
+        // step would make NaN of their sums of 0
+        const int gi = F8 || G < 128 ? NG * s + sg : s >> 1;
+        dma4(s < end && gi < p.L.groups ? sp + ((uint32_t)gi * 64 + so) : kZeros, slot + XB + WB + 256 * wave);
     };
     Raw st[DMA ? 1 : NX][F8 ? 2 : 1];
     auto load = [&](int s) {

@@ -366,3 +366,35 @@ def test_workspaces_that_the_kernels_cannot_write(esb):
     assert not bool(room.any())
     want = esb.esb_w4_gemm(x, w4, 512, 128)
     assert torch.equal(esb.esb_w4_gemm(x, w4, 512, 128, workspace=room[:need]), want)
+
+
+@pytest.mark.parametrize("M", [1, 7, 20, 64, 150, 600])
+@pytest.mark.parametrize("x,y", [("bf16", "bf16"), ("f16", "f32"), ("e4m3", "bf16"), ("e4m3", "f32")])
+@pytest.mark.parametrize("K", [300, 704, 9216, 9152])
+def test_infinite_scales(esb, M, x, y, K):
+    """An infinite scale reaches its outputs only; where it meets a whole group's sum (groups of 32 and
+    64), they are infinite with that sum's sign, whatever steps a tile or a range of columns adds."""
+    log("w4 gemm infinite scale M=%d K=%d %s" % (M, K, x))
+    N = 70
+    xv, s = acts(5, M, K, x)
+    for group in (32, 64, 128):
+        codes, alpha = weights(4, N, K, group)
+        groups = alpha.shape[1]
+        # the last group, and one within (a sum of +-8 steps at least: no cancellation to zero)
+        at = {5: groups - 1, 66: groups // 2, 40: 0}
+        for n, g in at.items():
+            alpha[n, g] = float("inf")
+        w4 = esb.esb_w4_pack(codes.cuda(), alpha.cuda(), group)
+        out = esb.esb_w4_gemm(xv.cuda(), w4, N, group, x_scale=None if s is None else s.cuda(),
+                              y_dtype=ref.TYPES[y]).cpu()
+        q = ref.CODE_VALUES[codes.long()]
+        for n, g in at.items():
+            c = slice(g * group, min((g + 1) * group, K))
+            part = xv[:, c].double() @ q[n, c]
+            sure = part.abs() > 1e-3 * (xv[:, c].double().abs() @ q[n, c].abs())
+            assert not bool(torch.isfinite(out[:, n]).any())
+            if group < 128:
+                want = torch.copysign(torch.full((M,), float("inf"), dtype=torch.float64), part)
+                assert torch.equal(out[:, n].double()[sure], want[sure]), (n, g)
+        keep = [n for n in range(N) if n not in at]
+        check(out[:, keep], xv, s, codes[keep], alpha[keep], group)
