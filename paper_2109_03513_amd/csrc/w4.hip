@@ -188,10 +188,16 @@ __device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
 
 // The search needs no exact codes: the error is continuous where a code changes, so a candidate's q is
 // the conversion to fp4 of w (1/alpha), and e = w - alpha q one fma.  The group is scaled by a power of
-// two that brings its largest weight into [1, 2), which keeps e^2 in range.  Sums of up to 128 squares
-// in 8 fp32 parts a lane are within 2^-20 of their value; where the second least is within 2^-19 of the
-// least (a few groups in ten thousand), the two are compared in fp64.  Three candidates so close, or
-// candidates far below the weights, are left to search_exact.
+// two that brings its largest weight into [1, 2), which keeps e^2 in range.  An error's sum is off by
+//  * 11 roundings of 2^-24: two in the square of a rounded e, nine sums on a square's way (four in its
+//    lane's part, three over the parts, two over the lanes of a row);
+//  * for 32-bit weights, q on the wrong side of a bound: 1/alpha is within 2^-23 and the product rounded,
+//    so |w| is then within 1.5 2^-23 of mid alpha (relative), and its square above the least one by up to
+//    28 times that (8 mid / gap, the most at 1.75 and 3.5), 2^-17.6.  16-bit weights are on a bound, where
+//    both squares are equal, or 2^-11 away.
+// So where the second least is within kNear of the least (a few groups in ten thousand, in a thousand for
+// 32-bit weights), the two are compared in fp64: kNear is above twice the first part plus the second.
+// Three candidates so close, or candidates far below the weights, are left to search_exact.
 //
 // Codes: for 16-bit weights w / alpha is a tie or at least 2^-11 from one, so w (1/alpha) (1 + 2^-22)
 // rounds to the nearest value with ties up; 32-bit weights are compared with the exact bounds.
@@ -199,10 +205,12 @@ __device__ __forceinline__ uint32_t to_e2m1(const float* x, float by) {
 // Bound by VALU issue (97 % of all cycles busy): for two weights and a candidate two products with 1/alpha,
 // a conversion to fp4 (a quarter of the fp32 rate), one back, two remainders and two squares, some 22
 // cycles of a SIMD per 64 weights.  4096 x 9216 bf16 weights, G = 128, 16 candidates: 101-110 us (the
-// bytes alone: 18); 1000 x 1999 fp16, G = 32, 8 candidates: 9 us (11 with both groups in a lane).
+// bytes alone: 18), fp32 weights 114 (bytes: 33); 1000 x 1999 fp16, G = 32, 8 candidates: 9 us (11 with both groups in a lane).
 // Dot products of 16-bit pairs would halve the sums but lose seven bits to cancellation, and fp4 from
 // 16-bit products moves the cell bounds: both would send groups by the percent, not by the
 // ten-thousand, to the fp64 comparison.
+template <typename T> constexpr float kNear = sizeof(T) == 4 ? 0x1p-17f : 0x1p-19f;
+
 template <typename T, int G>
 __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __restrict__ w, int64_t ldw,
                                                      const float* __restrict__ factors, int nf,
@@ -271,7 +279,7 @@ __global__ __launch_bounds__(256) void k_w4_quantize(W4Layout L, const T* __rest
         second = __builtin_amdgcn_fmed3f(least, second, err);
         least = fminf(least, err);
     }
-    const float near = least * (1.0f + 0x1p-19f);
+    const float near = least * (1.0f + kNear<T>);
     if (__any(finite && m && (far || third <= near))) {
         const float exact = search_exact<T, G>(o, w + (o.n < L.N ? o.n : 0) * ldw, o.n < L.N ? L.K : 0, top, factors, nf);
         if (finite) alpha = exact;

@@ -200,3 +200,58 @@ def test_refusals(esb):
     with pytest.raises(ValueError):
         esb.esb_w4_pack(torch.zeros(32, 64, dtype=torch.uint8, device="cuda"), w, 32)
     assert esb.esb_w4_quantize(torch.zeros(0, 64, device="cuda"), 32).numel() <= 1
+
+
+def near_groups(f1):
+    """Rows of 32 fp32 weights whose candidates 1 and f1 differ by a part in 10^6 or less, the first's error
+    the smaller one and nearly all of it one weight's next to a cell bound: (top, that weight, one more)."""
+    levels = ref.LEVELS.numpy()
+    mids = (levels[1:] + levels[:-1]) / 2
+
+    def squares(a, w):
+        return (w - a * levels[np.searchsorted(mids, w / a, side="right")]) ** 2
+
+    rows = []
+    for man in range(0, 128, 8):
+        a0 = 1 + man / 128
+        top = np.float32(6 * a0)
+        a1 = float(torch.tensor(float(np.float32(top * np.float32(f1)) / np.float32(6))).to(torch.bfloat16))
+        for mid in (5.0, 3.5, 2.5, 1.75):
+            for k in (-2, -1, 1, 2):
+                s = np.float32(mid * a0)
+                for _ in range(abs(k)):
+                    s = np.nextafter(s, np.float32(100 if k > 0 else 0))
+                two = np.array([top, s], dtype=np.float64)
+
+                def ratio(u):
+                    return ((squares(a1, two).sum() + squares(a1, u)) / (squares(a0, two).sum() + squares(a0, u))) - 1
+
+                u = np.linspace(0, 6 * a0, 1001)
+                f = ratio(u) - 4e-7
+                for i in np.nonzero(np.sign(f[1:]) != np.sign(f[:-1]))[0][:3]:
+                    lo, hi = u[i], u[i + 1]
+                    for _ in range(40):
+                        m = (lo + hi) / 2
+                        if np.sign(ratio(np.array([m]))[0] - 4e-7) == np.sign(f[i]):
+                            lo = m
+                        else:
+                            hi = m
+                    near = (np.float32(lo).view(np.uint32).astype(np.int64) + np.arange(-4, 5)).clip(0)
+                    near = near.astype(np.uint32).view(np.float32)
+                    off = ratio(near.astype(np.float64))
+                    rows += [(top, s, v) for v in near[(off > 1e-9) & (off < 1.5e-6)][:3]]
+    w = torch.zeros(len(rows), 32)
+    w[:, :3] = torch.tensor(rows)
+    return w
+
+
+@pytest.mark.parametrize("f1", [31 / 32, 0.9, 1.03])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_candidates_a_part_in_a_million_apart(esb, f1, group):
+    w = torch.nn.functional.pad(near_groups(f1), (0, group - 32))
+    assert w.shape[0] > 500
+    q, alpha = esb.esb_w4_unpack(esb.esb_w4_quantize(w.cuda(), group, torch.tensor([1.0, f1]).cuda()),
+                                 w.shape[0], group, group)
+    rq, ra = ref.quantize(w, group, [1.0, f1])
+    assert torch.equal(alpha.cpu().double(), ra)
+    assert torch.equal(q.cpu().double(), rq)
