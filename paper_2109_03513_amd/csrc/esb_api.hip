@@ -111,7 +111,7 @@ const char* esb_strerror(int status) {
         case ESB_OK: return "ok";
         case ESB_E_INVALID: return "invalid argument";
         case ESB_E_OVERFLOW: return "int32 accumulator bound exceeded";
-        case ESB_E_UNSUPPORTED: return "format, type or size outside what the kernels support";
+        case ESB_E_UNSUPPORTED: return "decoded integers exceed the split int8 range, or a format, type or size that is not supported";
         case ESB_E_HIP: return "HIP runtime error";
         case ESB_E_WORKSPACE: return "workspace missing or too small";
         case ESB_E_SCRATCH: return "input needs more scratch than the static device buffer holds";

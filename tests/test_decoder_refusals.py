@@ -116,3 +116,9 @@ def test_host_weights(L):
         esb.esb_w4_unpack(w4, 32, 64, 32)
     with pytest.raises(TypeError):
         esb.esb_w4_unpack(w4.numpy(), 32, 64, 32)
+
+
+def test_text_of_what_is_not_supported(L):
+    """One status for the products of codes and the decoder operators: its text names both reasons."""
+    text = L.esb_strerror(UNSUPPORTED)
+    assert b"decoded integers exceed the split int8 range" in text and b"type or size" in text
