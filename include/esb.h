@@ -573,14 +573,15 @@ int esb_w4_unpack(const void* w4, int N, int K, int group, uint8_t* values, int6
  *   y       device, M x N, y_type ESB_F32, ESB_BF16 or ESB_F16.
  * Scales are finite or NaN: alpha NaN makes its outputs NaN, alpha infinite makes them infinite
  * or, where parts of the group's sum are zero or differ in sign, NaN.
- * A group's products are exact and its sum is fp32, in an order fixed by the arguments, the
- * alignment of x and whether there is a workspace (the same call gives the same bits).
+ * Products are exact and sums fp32, a group of 128 in two parts, in an order fixed by the sizes,
+ * types and group, the alignment of x's rows and the size of the workspace (the same call gives the
+ * same bits).
  *   workspace  device, 256-byte aligned, at least esb_w4_gemm_workspace_size() bytes (fp32 sums
  *              of column ranges where few rows leave CUs idle; a copy of many rows whose
  *              lengths are not whole 16-byte pieces; 0 for most shapes), or NULL: neither.
  *              ESB_E_WORKSPACE if it is non-NULL and ws_bytes is too small.  It carries
  *              nothing between calls; concurrent calls need distinct ones.
- * K == 0 writes zeros; M == 0 or N == 0 enqueues nothing.
+ * K == 0 writes zeros, whatever x_scale holds; M == 0 or N == 0 enqueues nothing.
  */
 size_t esb_w4_gemm_workspace_size(int M, int N, int K, int group, int x_type, int y_type);
 int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int x_type,
