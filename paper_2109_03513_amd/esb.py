@@ -682,10 +682,10 @@ _FLOATS = (ESB_F32, ESB_BF16, ESB_F16)
 
 
 def _on(stream):
-    """Context in which `stream` (an object or a handle) is the current one: what a call allocates
-    then belongs to the stream that uses it."""
-    if isinstance(stream, int):
-        stream = _torch.cuda.ExternalStream(stream)
+    """Context in which `stream` (an object with .cuda_stream, or a handle) is the current one: what a
+    call allocates then belongs to the stream that uses it."""
+    if not isinstance(stream, _torch.cuda.Stream):
+        stream = _torch.cuda.ExternalStream(_stream(stream))
     return _torch.cuda.stream(stream)
 
 

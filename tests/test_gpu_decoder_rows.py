@@ -247,3 +247,29 @@ def test_strongly_negative_gates(esb, t):
     # bytes: where the row's largest value is a normal number
     big = y.abs().amax(1) > 2.0 ** -110
     ref.check_e4m3(g8[big.cuda()], gs[big.cuda()], y[big], GATE_REL, 2.0 ** -149)
+
+
+def test_stream_arguments(esb):
+    """What names a stream in this binding: a torch stream, its handle (0: the default stream) and any
+    object that holds one."""
+    x = make(8, 20, 384, torch.bfloat16).cuda()
+    want = esb.esb_rmsnorm(x, None, EPS)
+    w4 = esb.esb_w4_quantize(x, 32)
+    gate, (q, alpha) = esb.esb_swiglu(x, x), esb.esb_w4_unpack(w4, 20, 384, 32)
+    y = esb.esb_w4_gemm(x, w4, 20, 32)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    class Holder:
+        cuda_stream = side.cuda_stream
+
+    for stream in (side, side.cuda_stream, Holder(), 0, torch.cuda.default_stream()):
+        got = esb.esb_rmsnorm(x, None, EPS, stream=stream)
+        g = esb.esb_swiglu(x, x, stream=stream)
+        v4 = esb.esb_w4_quantize(x, 32, stream=stream)
+        v, a = esb.esb_w4_unpack(w4, 20, 384, 32, stream=stream)
+        p = esb.esb_w4_gemm(x, w4, 20, 32, stream=stream)
+        torch.cuda.synchronize()
+        for s, t in zip(want[2:] + gate[1:] + (w4, q, alpha, y), got[2:] + g[1:] + (v4, v, a, p)):
+            assert torch.equal(s.view(torch.uint8) if s.dtype.itemsize == 1 else s,
+                               t.view(torch.uint8) if t.dtype.itemsize == 1 else t)
