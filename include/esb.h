@@ -578,7 +578,8 @@ int esb_w4_unpack(const void* w4, int N, int K, int group, uint8_t* values, int6
  * same bits).
  *   workspace  device, 256-byte aligned, at least esb_w4_gemm_workspace_size() bytes (fp32 sums
  *              of column ranges where few rows leave CUs idle; a copy of many rows whose
- *              lengths are not whole 16-byte pieces; 0 for most shapes), or NULL: neither.
+ *              lengths are not whole 16-byte pieces or that are 8-bit under groups of 32; 0 for
+ *              most shapes), or NULL: neither.
  *              ESB_E_WORKSPACE if it is non-NULL and ws_bytes is too small.  It carries
  *              nothing between calls; concurrent calls need distinct ones.
  * K == 0 writes zeros, whatever x_scale holds; M == 0 or N == 0 enqueues nothing.

@@ -12,7 +12,7 @@
 // of 1000 6.7 us; one row of 4096 3.2 us, which is a launch and one round trip to memory.
 //
 // The sum of squares is held in fp64: squares of fp32 values up to the largest do not overflow,
-// and rstd is the correctly rounded fp32 value up to the last bit.  Everything else is fp32,
+// and rstd is the fp32 value next to the exact one (of rows above 2^126, a subnormal one of 22 bits).  Everything else is fp32,
 // rounded once to the output's type.
 #include "float_rows.h"
 

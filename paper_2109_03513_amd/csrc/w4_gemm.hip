@@ -14,9 +14,10 @@
 //  * k_w4_tile: tiles of 32 to 128 rows, everything through a ring in LDS; with few tiles the
 //    reduction is split over workgroups and k_w4_sum adds the parts.  Few rows are bound by the chain of
 //    a step (64 fp16 rows of 9216 x 4096, G = 32: 16.9 us), many by power and by MFMA and VALU issue:
-//    4096 E4M3 rows of 18432 x 4096, G = 128 490 us, 1.26 PFLOP/s;
-//    1999 bf16 rows of 4096 x 9216, G = 64 146 us, 1.03 PFLOP/s, MFMA 46 %, VALU 46 %.
-//    With rows of zeros the same products take 20 to 25 % less; tiles of 128 x 512 and 256 x 256, which
+//    4096 E4M3 rows of 18432 x 4096, G = 128 490 to 514 us by card, 1.20 to 1.26 PFLOP/s, MFMA busy
+//    56 % and VALU 61 % of cycles (bf16 rows 517 to 527); 1999 bf16 rows of 4096 x 9216, G = 64 146 us,
+//    1.03 PFLOP/s, MFMA 43 %, VALU 44 %.
+//    With bf16 rows of zeros the same products take 20 to 25 % less; tiles of 128 x 512 and 256 x 256, which
 //    bring a quarter to a third fewer bytes per product into a CU, and an fma after every MFMA instead
 //    of in groups all came out within 4 % or slower.
 #include <math.h>
@@ -648,8 +649,9 @@ hipError_t launch_tile(const W4GemmParams& p, int splits, hipStream_t s) {
 }
 
 // From so many rows on, rows that DMA cannot take are aligned first, where there is room for them (4000
-// outputs of K = 4001, us aligned first and not: bf16 64 rows 17.8 / 16.9, 512 rows 31.1 / 36.7, 4000 rows
-// 135 / 153; E4M3 64 rows 15.0 / 15.2, 128 rows 16.8 / 20.2, 4000 rows 74 / 123).
+// outputs of K = 4001, us aligned first and not: bf16 128 rows 15.8 / 16.8, 512 rows 29.9 / 35.8, 4000
+// rows 130 / 178; E4M3 128 rows 15.6 / 18.8, 512 rows 28.7 / 28.1, 4000 rows 124 / 181).  With fewer rows
+// it takes a workspace of the rows' size to save 1.5 to 4 us (64 rows: 15.1 / 16.6, E4M3 14.9 / 18.7).
 constexpr int64_t kAlignRows = 128;
 int64_t aligned_pitch(const W4Layout& L) { return 64 * (int64_t)L.chunks; }      // elements
 size_t aligned_bytes(int64_t M, const W4Layout& L, bool f8) { return (size_t)M * aligned_pitch(L) * (f8 ? 1 : 2); }
