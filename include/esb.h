@@ -589,6 +589,143 @@ int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int 
                 const float* x_scale, const void* w4, void* y, int64_t ldy, int y_type,
                 void* workspace, size_t ws_bytes, void* stream);
 
+/*
+ * A decoder's attention.  Heads are given with pitches, so that queries, keys and values may be the
+ * columns of one product's rows: element i of head h of token t is data[t * token_pitch +
+ * h * head_pitch + i], pitches in elements, at any element's alignment.  Pitches are not negative;
+ * outputs must not overlap themselves.  `type` is the type of every heads argument of a call.
+ * At most 4096 heads of a kind (more: ESB_E_UNSUPPORTED).
+ */
+typedef struct esb_heads {
+    void* data;          /* device */
+    int64_t token_pitch;
+    int64_t head_pitch;
+    int heads;
+} esb_heads;
+
+/*
+ * Rotation of the first `rot` elements of a head by the angles of its token's position (the rest
+ * stay): pairs (a, b) become (a c - b s, b c + a s), c = table[position][j], s = table[position]
+ * [rot / 2 + j]; pair j is elements (j, j + rot / 2), or (2 j, 2 j + 1) when `adjacent` is nonzero.
+ * A token whose position is not in 0 .. rows - 1 gets NaN in every element.
+ */
+typedef struct esb_rotation {
+    const float* table;       /* device, rows x rot fp32, contiguous: cosines, then sines */
+    int64_t rows;
+    int rot;                  /* even, 0 <= rot <= d */
+    int adjacent;
+    const int32_t* positions; /* device, one per token */
+} esb_rotation;
+
+/*
+ * esb_rope: the norm over a head and the rotation, of queries and / or keys in one pass:
+ *   y = rotate(x * rstd * w),   rstd = 1 / sqrt(mean(x^2) + eps)  (the sum of squares in fp64).
+ *   q, k      heads of d elements, either may be NULL (with its output and weights);
+ *   q_w, k_w  device, d fp32, or NULL (ones);
+ *   eps       positive and finite, or 0: no norm (then q_w and k_w are NULL);
+ *   rotation  NULL: none;
+ *   q_out, k_out  as many heads; may be the buffer of q or k (same pitches).
+ * type ESB_F32, ESB_BF16, ESB_F16; fp32 work, one rounding to `type`.  1 <= d <= 512 (more:
+ * ESB_E_UNSUPPORTED); tokens == 0 enqueues nothing.
+ */
+int esb_rope(const esb_heads* q, const esb_heads* k, int type, int64_t tokens, int d,
+             const float* q_w, const float* k_w, float eps, const esb_rotation* rotation,
+             const esb_heads* q_out, const esb_heads* k_out, void* stream);
+
+/*
+ * A paged cache of keys and values in ESB(4,1) codes (OCP E2M1) with a bf16 scale per 32 elements
+ * of a head: key[i] ~ alpha[i / 32] * q[i], values likewise; 9/16 byte an element.  A page holds
+ * `page` tokens of every head in esb_kv4_page_size bytes (0 for invalid arguments); slot n of the
+ * cache is token n % page of page n / page.  page: a power of two, 16 to 4096; d: a multiple of 32,
+ * at most 256 (else ESB_E_UNSUPPORTED).  With G = d / 32, a page is one block of 36 G page bytes
+ * per head, in it
+ *   keys    [token][4][G] 32-bit words, word (a, g) the E2M1 nibbles of elements
+ *           32 g + 8 a .. + 7, lowest first;
+ *   values  [token / 4][16][G][token % 4] bytes, byte (a, g) the nibbles of elements
+ *           32 g + 2 a (low) and + 1;
+ *   scales  of keys, then of values: bf16 [token / 4][G][token % 4].
+ * Calls write the slots that they are given and no others.
+ *
+ * esb_kv4_append: tokens into the cache, keys normed and rotated as by esb_rope (k_w, eps,
+ *   rotation), then y = fl32 of key or value (the norm and rotation in fp64) and per 32 elements
+ *     alpha = bf16(max(fl32(max|y| / 6), 2^-126)),  q = the value nearest to y / alpha
+ *   (ties to the larger magnitude, zero with sign 0); a NaN or an infinity among the 32 makes alpha
+ *   NaN and the codes 0.
+ *   q, q_w, q_out  queries of the same tokens, normed and rotated on the way; or NULL;
+ *   slots    device, one per token; tokens whose slot is not in the cache (such as -1) are not
+ *            stored.  A slot given twice holds parts of both tokens.
+ *   type ESB_F32, ESB_BF16, ESB_F16.  tokens == 0 enqueues nothing.
+ * esb_kv4_pack: given ESB(4,1) codes (one per byte, as esb_project writes them; device,
+ *   contiguous tokens x heads x d) and scales (bf16, tokens x heads x d / 32) into the cache.
+ * esb_kv4_unpack: the unscaled values as E4M3 bytes (exact; tokens x heads x d) and / or the
+ *   scales; any may be NULL, not all.  A slot that is not in the cache reads as zeros under NaN.
+ */
+typedef struct esb_kv4 {
+    void* data;        /* device, 16-byte aligned, pages * esb_kv4_page_size(page, heads, d) bytes */
+    int64_t pages;     /* less than 2^31 */
+    int page, heads, d;
+} esb_kv4;
+
+size_t esb_kv4_page_size(int page, int heads, int d);
+int esb_kv4_append(const esb_heads* q, const esb_heads* k, const esb_heads* v, int type,
+                   int64_t tokens, const float* q_w, const float* k_w, float eps,
+                   const esb_rotation* rotation, const int64_t* slots, const esb_kv4* cache,
+                   const esb_heads* q_out, void* stream);
+int esb_kv4_pack(const uint8_t* k, const void* k_alpha, const uint8_t* v, const void* v_alpha,
+                 int64_t tokens, const int64_t* slots, const esb_kv4* cache, void* stream);
+int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, uint8_t* k,
+                   void* k_alpha, uint8_t* v, void* v_alpha, void* stream);
+
+/*
+ * Attention over the cache, from one query per sequence (decoding) to many (drafts, parts of a
+ * prompt).  Sequence s has the n tokens starts[s] .. starts[s + 1] - 1 of q and lengths[s] keys in
+ * the cache, its own n among them; key j is token j % page of page pages[s][j / page], and query i
+ * (0 <= i < n) sees keys j <= lengths[s] - n + i:
+ *   o = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q . k_j - max_j).
+ *   q, out   tokens heads of d = cache->d; their number a multiple of cache->heads: query heads
+ *            h H / cache->heads .. share key head h.  ESB_BF16 or ESB_F16 (ESB_F32:
+ *            ESB_E_UNSUPPORTED).  out may not be the buffer of q;
+ *   starts   device, seqs + 1, ascending; or NULL: tokens == seqs, one token each.  Tokens past
+ *            the last sequence are left as they were;
+ *   lengths  device, one per sequence;
+ *   pages    device, seqs rows of `columns` page numbers, pitch page_pitch; entries behind a
+ *            sequence's last key are not read;
+ *   scale    positive and finite.
+ * A query that sees no key gets zeros.  What lies in the cache behind what a query sees does not
+ * reach it.  A length beyond columns * page makes the sequence's outputs NaN, a page number that is
+ * not the cache's those of the queries that see it.  Scores, statistics and sums are fp32; the
+ * products p_j alpha enter the matrix cores as bf16 (fp16 outputs: as two bf16, 16 bits).
+ *   workspace  device, 256-byte aligned, esb_kv4_attention_workspace_size() bytes (0 where keys
+ *              are not split over workgroups).  It carries nothing between calls; concurrent calls
+ *              need distinct ones.  Less or NULL: ESB_E_WORKSPACE.
+ * The order of sums is fixed by the sizes: the same call gives the same bits.
+ * ESB_E_UNSUPPORTED: 2^31 rows (tokens x heads), workgroups or columns * page or more.
+ * tokens == 0 or seqs == 0 enqueues nothing.
+ */
+size_t esb_kv4_attention_workspace_size(int64_t tokens, int q_heads, int d, int kv_heads, int seqs,
+                                        int has_starts, int64_t columns, int page);
+int esb_kv4_attention(const esb_heads* q, int type, int64_t tokens, const esb_kv4* cache, int seqs,
+                      const int32_t* starts, const int32_t* lengths, const int32_t* pages,
+                      int64_t page_pitch, int columns, float scale, const esb_heads* out,
+                      void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over whole prompts, packed one after the other: sequence s has the queries
+ * q_starts[s] .. q_starts[s + 1] - 1 and the keys k_starts[s] .. k_starts[s + 1] - 1.  With
+ * `causal` nonzero its last query sees every key, each one before it one key less (query i of n
+ * sees keys j <= m - n + i of m); else every query sees all.  The rest as esb_kv4_attention:
+ *   k, v     k_tokens heads of d, k->heads == v->heads dividing q->heads;
+ *   q_starts, k_starts  device, seqs + 1 each, ascending; k_starts NULL: q_starts (then k_tokens
+ *            == q_tokens).  Query rows past the last sequence are left as they were;
+ *   d        a multiple of 8, at most 256 (else ESB_E_UNSUPPORTED); ESB_BF16 or ESB_F16.
+ * A query that sees no key gets zeros; infinities and NaN in keys and values reach only the
+ * queries that see them.  Probabilities enter the matrix cores in `type`; the rest is fp32.
+ */
+int esb_attention(const esb_heads* q, const esb_heads* k, const esb_heads* v, int type,
+                  int64_t q_tokens, int64_t k_tokens, int d, int seqs, const int32_t* q_starts,
+                  const int32_t* k_starts, int causal, float scale, const esb_heads* out,
+                  void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,280 @@
+// Attention over packed prompts: o = softmax(scale q k^T) v, per sequence, causal or not, query heads in groups
+// that share a key head.
+//
+// A workgroup takes 128 rows (queries x heads of one group), 32 to a wave, and goes over the sequence's
+// keys in tiles that its waves share in LDS.  The scores are formed transposed, S^T = K Q^T, on 32x32x16 MFMAs:
+// a lane then holds, of one query, the keys that the second product O^T = V^T P^T wants of its operand, so
+// that the probabilities never leave their lane; V^T is read from the row-major tile by the
+// transposing LDS read.  One pass with a running maximum and sum; the maximum moves only when a score
+// passes it by 2^8, so most tiles scale nothing.  Probabilities are rounded to the type of v for the MFMA
+// (their sum is not): an error of the terms that is below the rounding of the output.
+#include <type_traits>
+
+#include "kv4.h"
+
+namespace esb {
+
+namespace {
+
+constexpr float kLazy = 8.0f;      // how far a score may pass the maximum (log2)
+constexpr float kNegInf = -__builtin_inff();
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+// Whether a maximum has to move from `top` for a score of `most`.
+__device__ __forceinline__ bool passes(float most, float top) {
+    return most > top + kLazy || (top == kNegInf && most > kNegInf);
+}
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// Tiles of KT keys x DP elements (the head's d, padded) in LDS, rows of DP / 8 16-byte pieces.  Piece c of a row is
+// at c ^ turn(row): keys so that 16 rows of one piece lie in distinct banks, values so that the 64 bytes
+// that a transposing read takes of eight rows do.
+template <int DP> struct TileOf {
+    static constexpr int kPieces = DP / 8;
+    static __device__ __forceinline__ int key_turn(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
+    static __device__ __forceinline__ int value_turn(int row) { return DP == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
+};
+
+template <typename V> __device__ __forceinline__ bool any_not_finite(V v) {
+    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+    const u16x8 b = __builtin_bit_cast(u16x8, v);
+    constexpr unsigned short e = std::is_same<V, bf16x8>::value ? 0x7f80 : 0x7c00;
+    bool r = false;
+#pragma unroll
+    for (int i = 0; i < 8; i++) r |= (b[i] & e) == e;
+    return r;
+}
+
+template <typename T, int DP, int KT>
+__global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
+    typedef typename Vec8<T>::type V;
+    typedef TileOf<DP> L;
+    constexpr int R = 128, P = L::kPieces, NP = KT * P / 256, DB = DP / 32, KB = KT / 32;
+    __shared__ V kt[KT * P];
+    __shared__ V vt[KT * P];
+    __shared__ int odd;       // a tile with masks holds values that are not finite
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int h = blockIdx.x % p.k.heads;
+    const int64_t slot = gridDim.x / p.k.heads - 1 - blockIdx.x / p.k.heads;      // the longest rows first
+    const Tile t = find_tile(p.q_starts, p.seqs, p.q_tokens, p.group, R, slot);
+    const int n = (int)(t.end - t.begin), rows = n * p.group;
+    if (t.index < 0 || (int64_t)t.index * R >= rows) return;
+    const int row0 = t.index * R;
+    const int64_t ka = min(max((int64_t)p.k_starts[t.seq], (int64_t)0), p.k_tokens);
+    const int nk = (int)(min(max((int64_t)p.k_starts[t.seq + 1], ka), p.k_tokens) - ka);
+    const int ahead = p.causal ? nk - n : nk;        // query i sees keys up to i + ahead
+    auto last_of = [&](int r) { return min(r / p.group + ahead, nk - 1); };
+    const int keys = last_of(min(row0 + R, rows) - 1) + 1;
+
+    const int row = row0 + 32 * wave + col;
+    const bool live = row < rows;
+    const int last = last_of(row);
+    const int wave_open = last_of(row0 + 32 * wave);                                    // all its rows see so far
+    const int wave_keys = row0 + 32 * wave < rows ? last_of(min(row0 + 32 * wave + 32, rows) - 1) + 1 : 0;
+
+    V qf[DP / 16];
+    {
+        const T* q = (const T*)p.q.p + (t.begin + row / p.group) * p.q.token + (h * p.group + row % p.group) * p.q.head;
+#pragma unroll
+        for (int s = 0; s < DP / 16; s++) {
+            const int e = 16 * s + 8 * half;
+            qf[s] = V{};
+            if (live && e < p.d) qf[s] = load8(q + e, 8);
+        }
+    }
+    const T* kp = (const T*)p.k.p + ka * p.k.token + h * p.k.head;
+    const T* vp = (const T*)p.v.p + ka * p.v.token + h * p.v.head;
+
+    V kr[NP], vr[NP];
+    auto fetch = [&](int j0) {
+#pragma unroll
+        for (int u = 0; u < NP; u++) {
+            const int id = tid + 256 * u, j = j0 + id / P, e = 8 * (id % P);
+            kr[u] = vr[u] = V{};
+            if (j < nk && e < p.d) {
+                kr[u] = load8(kp + (int64_t)j * p.k.token + e, 8);
+                vr[u] = load8(vp + (int64_t)j * p.v.token + e, 8);
+            }
+        }
+    };
+
+    f32x16 acc[DB] = {};
+    float top = kNegInf, sum = 0.0f;
+    f32x16 x[KB];
+
+    auto scores = [&](int j0, auto masks) {
+        constexpr bool MASK = decltype(masks)::value;
+#pragma unroll
+        for (int b = 0; b < KB; b++) {
+            x[b] = f32x16{};
+#pragma unroll
+            for (int s = 0; s < DP / 16; s++) {
+                const int r = 32 * b + col;
+                x[b] = mma(kt[r * P + ((2 * s + half) ^ L::key_turn(r))], qf[s], x[b]);
+            }
+        }
+        float most = kNegInf;
+#pragma unroll
+        for (int b = 0; b < KB; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                if (MASK && j0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3) > last) x[b][i] = kNegInf;
+                most = fmaxf(most, x[b][i]);
+            }
+        most *= p.scale;
+        if (__ballot(passes(most, top))) {
+            // row by row: what a row gives does not depend on its neighbours
+            const float all = fmaxf(most, other_half(most)), now = passes(all, top) ? all : top;
+            const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < DB; d++) acc[d] *= f;
+        }
+        const float m = top == kNegInf ? 0.0f : top;
+#pragma unroll
+        for (int b = 0; b < KB; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                x[b][i] = __builtin_amdgcn_exp2f(fmaf(x[b][i], p.scale, -m));
+                sum += x[b][i];
+            }
+    };
+    // Four keys from row r on of elements 32 d + lane % 32, by the 16 lanes that hold them row by row.
+    auto values4 = [&](int r, int d) {
+        const int row = r + ((lane & 15) >> 2), e = 32 * d + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
+        const int at = (row * P + ((e >> 3) ^ L::value_turn(row))) * 8 + (e & 7);
+        typedef __attribute__((address_space(3))) i16x4* lds;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)((T*)vt + at));
+    };
+    auto products = [&]() {
+#pragma unroll
+        for (int b = 0; b < KB; b++)
+#pragma unroll
+            for (int s = 0; s < 2; s++) {
+                f32x8 w;
+#pragma unroll
+                for (int i = 0; i < 8; i++) w[i] = x[b][8 * s + i];
+                const V pf = __builtin_convertvector(w, V);
+#pragma unroll
+                for (int d = 0; d < DB; d++) {
+                    const int r = 32 * b + 16 * s + 4 * half;
+                    const i16x4 lo = values4(r, d), hi = values4(r + 8, d);
+                    typedef short i16x8 __attribute__((ext_vector_type(8)));
+                    const i16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    acc[d] = mma(__builtin_bit_cast(V, v), pf, acc[d]);
+                }
+            }
+    };
+    // Values that are not finite, for the rows that see their keys only.
+    auto odd_values = [&](int j0) {
+#pragma unroll
+        for (int b = 0; b < KB; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float there = other_half(x[b][i]);
+#pragma unroll 1
+                for (int o = 0; o < 2; o++) {
+                    const int r = 32 * b + 8 * (i >> 2) + 4 * (half ^ o) + (i & 3);
+                    const float w = o ? there : x[b][i];
+                    if (j0 + r > last) continue;
+#pragma unroll
+                    for (int d = 0; d < DB; d++)
+#pragma unroll
+                        for (int k = 0; k < 16; k++) {
+                            const int e = 32 * d + 8 * (k >> 2) + 4 * half + (k & 3);
+                            const float v = (float)((const T*)vt)[(r * P + ((e >> 3) ^ L::value_turn(r))) * 8 + (e & 7)];
+                            if (!(fabsf(v) < __builtin_inff())) acc[d][k] = fmaf(w, v, acc[d][k]);
+                        }
+                }
+            }
+    };
+
+    if (keys > 0) fetch(0);
+    for (int j0 = 0; j0 < keys; j0 += KT) {
+        __syncthreads();
+        if (tid == 0) odd = 0;
+        const bool check = j0 + KT - 1 > last_of(row0);      // of the whole workgroup: some row has masks here
+        bool mine = false;
+#pragma unroll
+        for (int u = 0; u < NP; u++) {
+            const int id = tid + 256 * u, r = id / P, c = id % P;
+            kt[r * P + (c ^ L::key_turn(r))] = kr[u];
+            vt[r * P + (c ^ L::value_turn(r))] = vr[u];
+            if (check) mine |= any_not_finite(vr[u]);
+        }
+        __syncthreads();
+        if (check) {
+            if (mine) odd = 1;
+            __syncthreads();
+        }
+        const bool slow = check && odd;
+        if (j0 + KT < keys) fetch(j0 + KT);
+        if (j0 < wave_keys) {
+            if (j0 + KT - 1 > wave_open) scores(j0, std::true_type{});
+            else scores(j0, std::false_type{});
+        }
+        if (slow) {
+            if (j0 < wave_keys) odd_values(j0);
+            __syncthreads();
+#pragma unroll 1
+            for (int u = 0; u < NP; u++) {
+                V& v = vt[tid + 256 * u];
+                V w = v;
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (!(fabsf((float)w[i]) < __builtin_inff())) w[i] = (T)0.0f;
+                v = w;
+            }
+            __syncthreads();
+        }
+        if (j0 < wave_keys) products();
+    }
+
+    sum += other_half(sum);
+    if (!live) return;
+    const float f = last >= 0 ? 1.0f / sum : 0.0f;       // no key: zeros
+    T* o = (T*)p.o.p + (t.begin + row / p.group) * p.o.token + (h * p.group + row % p.group) * p.o.head;
+#pragma unroll
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int e = 32 * d + 8 * k + 4 * half;
+            if (e >= p.d) continue;
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            f32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = acc[d][4 * k + i] * f;
+            ((Loose<t4, T>*)(o + e))->v = __builtin_convertvector(w, t4);
+        }
+}
+
+template <typename T, int DP, int KT>
+hipError_t launch_d(const AttentionParams& p, hipStream_t s) {
+    const int64_t slots = p.q_tokens * p.group / 128 + p.seqs;
+    k_attention<T, DP, KT><<<(unsigned)(slots * p.k.heads), 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_t(const AttentionParams& p, hipStream_t s) {
+    if (p.d <= 64) return launch_d<T, 64, 64>(p, s);
+    if (p.d <= 128) return launch_d<T, 128, 64>(p, s);
+    return launch_d<T, 256, 32>(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_attention(int type, const AttentionParams& p, hipStream_t s) {
+    return type == kBF16 ? launch_t<__bf16>(p, s) : launch_t<_Float16>(p, s);
+}
+
+}  // namespace esb

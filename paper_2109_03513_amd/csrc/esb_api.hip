@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "esb_internal.h"
+#include "kv4.h"
 
 namespace esb {
 
@@ -827,6 +828,198 @@ int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int 
     const W4GemmParams p = {L, M, x, ldx, x_scale, (const uint8_t*)w4, y, ldy, y_type,
                             (uint8_t*)workspace, workspace ? ws_bytes : 0, false, nullptr};
     return hip_status(launch_w4_gemm(p, x_type, (hipStream_t)stream));
+}
+
+// ---------------------------------------------------------- a decoder's attention
+constexpr int kMostHeads = 4096;
+constexpr float kLog2E = 1.44269504088896340736f;
+
+static int heads_check(const esb_heads* v, int type, int64_t tokens, int d, bool out) {
+    if (!v || v->heads < 1 || v->token_pitch < 0 || v->head_pitch < 0) return ESB_E_INVALID;
+    if (v->heads > kMostHeads) return ESB_E_UNSUPPORTED;
+    if (tokens > 0 && (!v->data || !aligned_for(v->data, type))) return ESB_E_INVALID;
+    if (out && tokens > 0) {      // heads within tokens or tokens within heads, apart from each other
+        const int64_t t = tokens > 1 ? v->token_pitch : INT64_MAX, h = v->heads > 1 ? v->head_pitch : INT64_MAX;
+        if (t < d || h < d) return ESB_E_INVALID;
+        const bool in_tokens = tokens == 1 || v->heads == 1 || (t - d) / (v->heads - 1) >= h;
+        const bool in_heads = tokens == 1 || v->heads == 1 || (h - d) / (tokens - 1) >= t;
+        if (!in_tokens && !in_heads) return ESB_E_INVALID;
+    }
+    return ESB_OK;
+}
+
+static HeadsView view(const esb_heads* v) {
+    return v ? HeadsView{v->data, v->token_pitch, v->head_pitch, v->heads} : HeadsView{nullptr, 0, 0, 0};
+}
+
+// What esb_rope and esb_kv4_append share; fills the norm and the rotation.
+static int turn_check(HeadsParams* p, const float* q_w, const float* k_w, float eps, const esb_rotation* r) {
+    if (!(eps >= 0.0f) || eps == INFINITY || (eps == 0.0f && (q_w || k_w))) return ESB_E_INVALID;
+    if ((uintptr_t)q_w % 4 || (uintptr_t)k_w % 4) return ESB_E_INVALID;
+    p->qw = q_w, p->kw = k_w, p->eps = eps;
+    if (!r || r->rot == 0) return ESB_OK;
+    if (r->rot < 0 || r->rot > p->d || r->rot % 2 || r->rows < 0) return ESB_E_INVALID;
+    if (p->tokens > 0 && (!r->positions || (uintptr_t)r->positions % 4 || (r->rows > 0 && !r->table) ||
+                          (uintptr_t)r->table % 4))
+        return ESB_E_INVALID;
+    p->table = r->table, p->rows = r->rows, p->rot = r->rot, p->adjacent = r->adjacent, p->positions = r->positions;
+    return ESB_OK;
+}
+
+int esb_rope(const esb_heads* q, const esb_heads* k, int type, int64_t tokens, int d, const float* q_w,
+             const float* k_w, float eps, const esb_rotation* rotation, const esb_heads* q_out,
+             const esb_heads* k_out, void* stream) {
+    if (!float_type(type) || tokens < 0 || d < 1 || (!q && !k)) return ESB_E_INVALID;
+    if (d > 512) return ESB_E_UNSUPPORTED;
+    if ((!q && (q_w || q_out)) || (!k && (k_w || k_out))) return ESB_E_INVALID;
+    int st = ESB_OK;
+    if (q) {
+        if ((st = heads_check(q, type, tokens, d, false)) || (st = heads_check(q_out, type, tokens, d, true))) return st;
+        if (q->heads != q_out->heads) return ESB_E_INVALID;
+    }
+    if (k) {
+        if ((st = heads_check(k, type, tokens, d, false)) || (st = heads_check(k_out, type, tokens, d, true))) return st;
+        if (k->heads != k_out->heads) return ESB_E_INVALID;
+    }
+    HeadsParams p = {};
+    p.q = view(q), p.k = view(k), p.qo = view(q_out), p.ko = view(k_out);
+    p.tokens = tokens, p.d = d;
+    if ((st = turn_check(&p, q_w, k_w, eps, rotation)) || tokens == 0) return st;
+    return hip_status(launch_rope(type, p, (hipStream_t)stream));
+}
+
+static int kv4_shape(int page, int heads, int d) {
+    if (page < 1 || heads < 1 || d < 1) return ESB_E_INVALID;
+    if (page < 16 || page > 4096 || (page & (page - 1)) || d % 32 || d > 256 || heads > kMostHeads) return ESB_E_UNSUPPORTED;
+    return ESB_OK;
+}
+
+size_t esb_kv4_page_size(int page, int heads, int d) {
+    return kv4_shape(page, heads, d) ? 0 : (size_t)heads * page * 36 * (d / 32);
+}
+
+static int kv4_check(const esb_kv4* c, Kv4Layout* L) {
+    if (!c || c->pages < 0) return ESB_E_INVALID;
+    const int st = kv4_shape(c->page, c->heads, c->d);
+    if (st) return st;
+    if (c->pages > INT32_MAX) return ESB_E_UNSUPPORTED;
+    if ((c->pages > 0 && !c->data) || (uintptr_t)c->data % 16) return ESB_E_INVALID;
+    *L = {(uint8_t*)c->data, c->pages, c->page, __builtin_ctz((unsigned)c->page), c->heads, c->d / 32};
+    return ESB_OK;
+}
+
+int esb_kv4_append(const esb_heads* q, const esb_heads* k, const esb_heads* v, int type, int64_t tokens,
+                   const float* q_w, const float* k_w, float eps, const esb_rotation* rotation, const int64_t* slots,
+                   const esb_kv4* cache, const esb_heads* q_out, void* stream) {
+    HeadsParams p = {};
+    int st = kv4_check(cache, &p.cache);
+    if (st) return st;
+    const int d = cache->d;
+    if (!float_type(type) || tokens < 0 || (!q && (q_w || q_out))) return ESB_E_INVALID;
+    if ((st = heads_check(k, type, tokens, d, false)) || (st = heads_check(v, type, tokens, d, false))) return st;
+    if (k->heads != cache->heads || v->heads != cache->heads) return ESB_E_INVALID;
+    if (q) {
+        if ((st = heads_check(q, type, tokens, d, false)) || (st = heads_check(q_out, type, tokens, d, true))) return st;
+        if (q->heads != q_out->heads) return ESB_E_INVALID;
+    }
+    if (tokens > 0 && (!slots || (uintptr_t)slots % 8)) return ESB_E_INVALID;
+    p.q = view(q), p.k = view(k), p.v = view(v), p.qo = view(q_out);
+    p.tokens = tokens, p.d = d, p.slots = slots;
+    if ((st = turn_check(&p, q_w, k_w, eps, rotation)) || tokens == 0) return st;
+    return hip_status(launch_kv4_append(type, p, (hipStream_t)stream));
+}
+
+int esb_kv4_pack(const uint8_t* k, const void* k_alpha, const uint8_t* v, const void* v_alpha, int64_t tokens,
+                 const int64_t* slots, const esb_kv4* cache, void* stream) {
+    Kv4Layout L;
+    const int st = kv4_check(cache, &L);
+    if (st) return st;
+    if (tokens < 0) return ESB_E_INVALID;
+    if (tokens == 0) return ESB_OK;
+    if (!k || !k_alpha || !v || !v_alpha || !slots || (uintptr_t)k_alpha % 2 || (uintptr_t)v_alpha % 2 ||
+        (uintptr_t)slots % 8)
+        return ESB_E_INVALID;
+    return hip_status(launch_kv4_pack(L, tokens, slots, k, k_alpha, v, v_alpha, (hipStream_t)stream));
+}
+
+int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, uint8_t* k, void* k_alpha,
+                   uint8_t* v, void* v_alpha, void* stream) {
+    Kv4Layout L;
+    const int st = kv4_check(cache, &L);
+    if (st) return st;
+    if (tokens < 0) return ESB_E_INVALID;
+    if (tokens == 0) return ESB_OK;
+    if (!k && !k_alpha && !v && !v_alpha) return ESB_E_INVALID;
+    if (!slots || (uintptr_t)slots % 8 || (uintptr_t)k_alpha % 2 || (uintptr_t)v_alpha % 2) return ESB_E_INVALID;
+    return hip_status(launch_kv4_unpack(L, tokens, slots, k, k_alpha, v, v_alpha, (hipStream_t)stream));
+}
+
+// Sizes that the launches of both attentions count in 32 bits.
+static int attention_check(int type, int64_t tokens, int q_heads, int kv_heads, int seqs, float scale) {
+    if (type == ESB_F32) return ESB_E_UNSUPPORTED;
+    if ((type != ESB_BF16 && type != ESB_F16) || tokens < 0 || seqs < 0) return ESB_E_INVALID;
+    if (!(scale > 0.0f) || scale == INFINITY) return ESB_E_INVALID;
+    if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads) return ESB_E_INVALID;
+    if (tokens > INT32_MAX || tokens * q_heads > INT32_MAX || (tokens + seqs) * q_heads > INT32_MAX)
+        return ESB_E_UNSUPPORTED;
+    return ESB_OK;
+}
+
+size_t esb_kv4_attention_workspace_size(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, int has_starts,
+                                        int64_t columns, int page) {
+    if (kv4_shape(page, kv_heads, d) || q_heads > kMostHeads || columns < 0 || columns > INT32_MAX / page) return 0;
+    if (attention_check(ESB_BF16, tokens, q_heads, kv_heads, seqs, 1.0f) || tokens == 0 || seqs == 0) return 0;
+    return kv4_attention_workspace(tokens, q_heads, d, kv_heads, seqs, has_starts != 0, columns * page);
+}
+
+int esb_kv4_attention(const esb_heads* q, int type, int64_t tokens, const esb_kv4* cache, int seqs,
+                      const int32_t* starts, const int32_t* lengths, const int32_t* pages, int64_t page_pitch,
+                      int columns, float scale, const esb_heads* out, void* workspace, size_t ws_bytes, void* stream) {
+    Kv4AttentionParams p = {};
+    int st = kv4_check(cache, &p.cache);
+    if (st) return st;
+    if (!q || !out) return ESB_E_INVALID;
+    if ((st = attention_check(type, tokens, q->heads, cache->heads, seqs, scale))) return st;
+    const int d = cache->d;
+    if ((st = heads_check(q, type, tokens, d, false)) || (st = heads_check(out, type, tokens, d, true))) return st;
+    if (q->heads != out->heads || columns < 0 || page_pitch < columns) return ESB_E_INVALID;
+    if (columns > INT32_MAX / cache->page) return ESB_E_UNSUPPORTED;
+    if (!starts && tokens != seqs) return ESB_E_INVALID;
+    if (tokens == 0 || seqs == 0) return ESB_OK;
+    if (!lengths || (columns > 0 && (!pages || cache->pages == 0)) || (uintptr_t)starts % 4 || (uintptr_t)lengths % 4 ||
+        (uintptr_t)pages % 4 || (uintptr_t)workspace % 256 || q->data == out->data)
+        return ESB_E_INVALID;
+    const size_t need = esb_kv4_attention_workspace_size(tokens, q->heads, d, cache->heads, seqs, starts != nullptr,
+                                                         columns, cache->page);
+    if (need && (!workspace || ws_bytes < need)) return ESB_E_WORKSPACE;
+    p.q = view(q), p.o = view(out);
+    p.tokens = tokens, p.d = d, p.group = q->heads / cache->heads, p.seqs = seqs;
+    p.starts = starts, p.lengths = lengths, p.table = pages, p.table_pitch = page_pitch, p.columns = columns;
+    p.scale = scale * kLog2E, p.ws = (uint8_t*)workspace;
+    return hip_status(launch_kv4_attention(type, p, (hipStream_t)stream));
+}
+
+int esb_attention(const esb_heads* q, const esb_heads* k, const esb_heads* v, int type, int64_t q_tokens,
+                  int64_t k_tokens, int d, int seqs, const int32_t* q_starts, const int32_t* k_starts, int causal,
+                  float scale, const esb_heads* out, void* stream) {
+    if (!q || !k || !v || !out) return ESB_E_INVALID;
+    int st = attention_check(type, q_tokens, q->heads, k->heads, seqs, scale);
+    if (st) return st;
+    if (d < 1 || k_tokens < 0) return ESB_E_INVALID;
+    if (d % 8 || d > 256 || k_tokens > INT32_MAX) return ESB_E_UNSUPPORTED;
+    if ((st = heads_check(q, type, q_tokens, d, false)) || (st = heads_check(out, type, q_tokens, d, true)) ||
+        (st = heads_check(k, type, k_tokens, d, false)) || (st = heads_check(v, type, k_tokens, d, false)))
+        return st;
+    if (q->heads != out->heads || k->heads != v->heads) return ESB_E_INVALID;
+    if (!k_starts && k_tokens != q_tokens) return ESB_E_INVALID;
+    if (q_tokens == 0 || seqs == 0) return ESB_OK;
+    if (!q_starts || (uintptr_t)q_starts % 4 || (uintptr_t)k_starts % 4 || q->data == out->data) return ESB_E_INVALID;
+    AttentionParams p = {};
+    p.q = view(q), p.k = view(k), p.v = view(v), p.o = view(out);
+    p.q_tokens = q_tokens, p.k_tokens = k_tokens, p.d = d, p.group = q->heads / k->heads, p.seqs = seqs;
+    p.causal = causal != 0, p.q_starts = q_starts, p.k_starts = k_starts ? k_starts : q_starts;
+    p.scale = scale * kLog2E;
+    return hip_status(launch_attention(type, p, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,119 @@
+// Heads of a decoder's attention, and the 4-bit paged cache of its keys and values: what heads.hip,
+// kv4_attention.hip, attention.hip and the C ABI share.
+#pragma once
+
+#include "float_rows.h"
+
+namespace esb {
+
+// Element i of head h of token t at p[t * token + h * head + i].
+struct HeadsView {
+    void* p;
+    int64_t token, head;
+    int heads;
+};
+
+// A page holds `page` tokens (a power of two, at least 16) of every head, one block per head after
+// the other.  With G = d / 32 scale groups a block has 36 G bytes a token:
+//   keys    [token][4][G] words: the eight nibbles of elements 32 g + 8 a .. + 7 in word (a, g),
+//   values  [token / 4][16][G][token % 4] bytes: elements 32 g + 2 a, + 1 in byte (a, g),
+//   scales  of keys, then of values: [token / 4][G][token % 4] bf16.
+// So one 16-byte piece is what a lane of a 16x16x32 MFMA wants of a key (every G, its eight
+// elements of the contraction) and of four values (every G, its two rows of the output).
+struct Kv4Layout {
+    uint8_t* data;
+    int64_t pages;
+    int page, shift, heads, groups;
+    __host__ __device__ int64_t block_bytes() const { return (int64_t)36 * groups * page; }
+    __device__ __forceinline__ uint8_t* block(int64_t pg, int head) const {
+        return data + (pg * heads + head) * block_bytes();
+    }
+    __device__ __forceinline__ int values_at() const { return 16 * groups * page; }
+    __device__ __forceinline__ int key_scales_at() const { return 32 * groups * page; }
+    __device__ __forceinline__ int value_scales_at() const { return 34 * groups * page; }
+    // Scales start of the four-token run that holds token t of the block.
+    __device__ __forceinline__ int scale_run(int t) const { return (t >> 2) * 8 * groups; }
+};
+
+// Norm and rotation of heads, and their way into the cache (heads.hip).
+struct HeadsParams {
+    HeadsView q, k, v, qo, ko;      // v only with a cache; ko only without
+    int64_t tokens;
+    int d;
+    const float* qw;                // norm weights, or NULL (ones)
+    const float* kw;
+    float eps;                      // 0: no norm
+    const float* table;             // rows x rot: cosines, then sines
+    int64_t rows;
+    int rot, adjacent;              // rot 0: no rotation
+    const int32_t* positions;
+    const int64_t* slots;           // with a cache
+    Kv4Layout cache;
+};
+hipError_t launch_rope(int type, const HeadsParams& p, hipStream_t s);
+hipError_t launch_kv4_append(int type, const HeadsParams& p, hipStream_t s);
+// Codes (ESB(4,1), one a byte) and scales [tokens][heads][d], [tokens][heads][d / 32], contiguous, in and
+// out (values as E4M3 bytes); any of the four may be NULL on the way out.
+hipError_t launch_kv4_pack(const Kv4Layout& L, int64_t tokens, const int64_t* slots, const uint8_t* k,
+                           const void* ka, const uint8_t* v, const void* va, hipStream_t s);
+hipError_t launch_kv4_unpack(const Kv4Layout& L, int64_t tokens, const int64_t* slots, uint8_t* k, void* ka,
+                             uint8_t* v, void* va, hipStream_t s);
+
+// Attention over the cache (kv4_attention.hip).
+struct Kv4AttentionParams {
+    HeadsView q, o;
+    int64_t tokens;
+    Kv4Layout cache;
+    int d, group;                   // query heads per key head
+    int seqs;
+    const int32_t* starts;          // seqs + 1, or NULL: one token each
+    const int32_t* lengths;
+    const int32_t* table;           // pages of a sequence, pitch in elements
+    int64_t table_pitch;
+    int columns;
+    float scale;                    // of the products, times log2(e)
+    uint8_t* ws;
+};
+size_t kv4_attention_workspace(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts,
+                               int64_t longest);
+hipError_t launch_kv4_attention(int type, const Kv4AttentionParams& p, hipStream_t s);
+
+// Attention over packed prompts (attention.hip).
+struct AttentionParams {
+    HeadsView q, k, v, o;
+    int64_t q_tokens, k_tokens;
+    int d, group, seqs, causal;
+    const int32_t* q_starts;        // seqs + 1 each
+    const int32_t* k_starts;
+    float scale;                    // of the products, times log2(e)
+};
+hipError_t launch_attention(int type, const AttentionParams& p, hipStream_t s);
+
+// The sequence that tile `slot` belongs to, where the sequences' tiles of R rows are numbered from
+// first(s) = starts[s] * per / R + s (per rows a token): no sequence has more tiles than lie between
+// its own number and the next one's, so that tiles need no list.  Every lane of the wave gets the
+// answer; the starts may hold anything.
+struct Tile {
+    int seq, index;        // index: of the sequence's tiles
+    int64_t begin, end;    // its tokens
+};
+__device__ __forceinline__ Tile find_tile(const int32_t* starts, int seqs, int64_t tokens, int per, int R,
+                                          int64_t slot) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int s0 = 0; s0 < seqs; s0 += 64) {
+        const int s = s0 + lane;
+        bool before = false;
+        if (s < seqs) before = (int64_t)max(starts[s], 0) * per / R + s <= slot;
+        n += __builtin_popcountll(__ballot(before));
+    }
+    Tile t;
+    t.seq = __builtin_amdgcn_readfirstlane(max(n - 1, 0));
+    const int64_t a = min(max((int64_t)starts[t.seq], (int64_t)0), tokens);
+    const int64_t b = min(max((int64_t)starts[t.seq + 1], a), tokens);
+    t.begin = a, t.end = b;
+    t.index = (int)(slot - (a * per / R + t.seq));
+    return t;
+}
+
+}  // namespace esb

@@ -1,0 +1,494 @@
+// Attention over the 4-bit paged cache:
+//   o = softmax(scale q k^T) v over keys j <= length - n + i for the i-th of a sequence's n queries,
+//   k = alpha_k q_k, v = alpha_v q_v, alpha per 32 elements of a key's or value's head.
+//
+// The scores are formed transposed, S^T = K Q^T, on 16x16x32 MFMAs: E2M1 codes are exact in bf16 and fp16,
+// one MFMA covers one scale group, whose alpha multiplies its fp32 sum.  A lane then holds eight keys of one
+// query, which is what the second product O^T = V^T P^T wants of its operand: the probabilities never
+// leave the lane.  A value's alpha multiplies the probability (one operand per group), so its codes
+// go into the MFMA unscaled.  The product of probability and alpha is rounded to bf16 (for fp16 outputs to
+// the sum of two bf16, one more MFMA): 2^-9 of each of the terms that a softmax averages, which is
+// below the rounding of a bf16 output.
+//
+// A workgroup takes 16 NT rows (queries x heads that share a key head) and a run of keys; its four
+// waves take every fourth step of 32 keys, each with its own running maximum and sum, and join them in
+// LDS.  Few rows: the keys are split over workgroups too and k_join adds the parts.  The running
+// maximum moves only when a score passes it by 2^8, so most steps cross no lanes.
+#include <type_traits>
+
+#include "kv4.h"
+
+namespace esb {
+
+namespace {
+
+constexpr float kLazy = 8.0f;      // how far a score may pass the maximum (log2)
+constexpr float kNegInf = -__builtin_inff();
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int N> struct Words {
+    typedef uint32_t w __attribute__((ext_vector_type(N)));
+};
+
+template <typename F, typename P>
+__device__ __forceinline__ F join4(P a, P b, P c, P d) {
+    return __builtin_bit_cast(F, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                                       __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)});
+}
+// Eight nibbles, lowest first.
+__device__ __forceinline__ bf16x8 decode(uint32_t w, __bf16) {
+    return join4<bf16x8>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+}
+__device__ __forceinline__ f16x8 decode(uint32_t w, _Float16) {
+    return join4<f16x8>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3));
+}
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// Four bf16 scales as fp32.
+__device__ __forceinline__ f32x4 four(uint2 s) {
+    return f32x4{__uint_as_float(s.x << 16), __uint_as_float(s.x & 0xffff0000u), __uint_as_float(s.y << 16),
+                 __uint_as_float(s.y & 0xffff0000u)};
+}
+// Whether a maximum has to move from `top` for a score of `most`.
+__device__ __forceinline__ bool passes(float most, float top) {
+    return most > top + kLazy || (top == kNegInf && most > kNegInf);
+}
+// Over the four lanes that hold one column.
+__device__ __forceinline__ float column_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float column_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// What a wave brings of 32 keys, in two halves of 16.  Keys: the lane's words of key lane % 16; values: its
+// bytes of the run of four keys lane / 16; scales: of the same run.
+template <int CP> struct Step {
+    typename Words<CP>::w k[2], v[2];
+    uint2 ka[2][CP], va[2][CP];
+    int bad;             // halves whose page is none of the cache's
+};
+
+// A sequence as one workgroup sees it.
+struct Rows {
+    int seq, n, len;     // its queries, its cached keys
+    int64_t begin;       // its first query
+    int row0, rows;      // rows of the tile start here, of all
+    bool bad;            // its length passes its pages
+};
+
+__device__ __forceinline__ Rows find_rows(const Kv4AttentionParams& p, int64_t slot, int tiles, int R) {
+    Rows r;
+    int index;
+    if (p.starts) {
+        const Tile t = find_tile(p.starts, p.seqs, p.tokens, p.group, R, slot);
+        r.seq = t.seq, r.begin = t.begin, r.n = (int)(t.end - t.begin), index = t.index;
+    } else {
+        r.seq = (int)(slot / tiles), index = (int)(slot % tiles), r.begin = r.seq, r.n = 1;
+    }
+    r.rows = r.n * p.group;
+    r.row0 = index < 0 || (int64_t)index * R >= r.rows ? r.rows : index * R;
+    const int64_t len = p.lengths[r.seq];
+    r.bad = len > (int64_t)p.columns * p.cache.page;
+    r.len = r.bad || len < 0 ? 0 : (int)len;
+    return r;
+}
+
+template <typename T, int CP, int NT>
+__global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int chunks, int tiles, float* part,
+                                             float2* stats) {
+    typedef typename Vec8<T>::type V;
+    constexpr int R = 16 * NT;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int C = p.cache.groups;
+    int64_t id = blockIdx.x;
+    const int chunk = (int)(id % chunks);
+    id /= chunks;
+    const int h = (int)(id % p.cache.heads);
+    const Rows rw = find_rows(p, id / p.cache.heads, tiles, R);
+    if (rw.row0 >= rw.rows) return;
+    const int first = rw.len - rw.n;                    // the last key of query t is first + t
+    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
+    const int k0 = chunk * run, k1 = min(k0 + run, keys);
+    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
+    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
+
+    int last[NT];
+    V qf[NT][CP];
+#pragma unroll
+    for (int u = 0; u < NT; u++) {
+        const int r = rw.row0 + 16 * u + i, t = r / p.group;
+        last[u] = first + t;
+        const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
+#pragma unroll
+        for (int s = 0; s < CP; s++) {
+            qf[u][s] = V{};
+            if (r < rw.rows && s < C) qf[u][s] = load8(q + 32 * s + 8 * g, 8);
+        }
+    }
+
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    const int page = p.cache.page;
+    struct Ids {
+        int a, b;
+    };
+    auto ids = [&](int at) {      // pages of the halves of a step; halves past the last key take its page
+        const int a = __builtin_amdgcn_readfirstlane(min(at, keys - 1) >> p.cache.shift);
+        const int b = __builtin_amdgcn_readfirstlane(min(at + 16, keys - 1) >> p.cache.shift);
+        return Ids{table[a], table[b]};
+    };
+    auto load = [&](int at, Ids pg) {
+        Step<CP> st;
+        st.bad = 0;
+#pragma unroll
+        for (int hh = 0; hh < 2; hh++) {
+            int pid = __builtin_amdgcn_readfirstlane(hh ? pg.b : pg.a);
+            if (pid < 0 || pid >= p.cache.pages) pid = 0, st.bad |= 1 << hh;
+            const uint8_t* b = p.cache.block(pid, h);
+            const int t = (at + 16 * hh) & (page - 1);
+            // words past the head's groups are of what follows in the block, and nothing uses them
+            st.k[hh] = ((const Loose<typename Words<CP>::w, uint32_t>*)(b + (t + i) * 16 * C + g * 4 * C))->v;
+            st.v[hh] = ((const Loose<typename Words<CP>::w, uint32_t>*)(b + p.cache.values_at() + ((t >> 2) + g) * 64 * C +
+                                                            i * 4 * C))->v;
+            const uint8_t* ks = b + p.cache.key_scales_at() + ((t >> 2) + g) * 8 * C;
+            const uint8_t* vs = b + p.cache.value_scales_at() + ((t >> 2) + g) * 8 * C;
+#pragma unroll
+            for (int s = 0; s < CP; s++)
+                if (s < C) {
+                    st.ka[hh][s] = *(const uint2*)(ks + 8 * s);
+                    st.va[hh][s] = *(const uint2*)(vs + 8 * s);
+                }
+        }
+        return st;
+    };
+
+    f32x4 acc[NT][CP][2] = {};
+    float top[NT], sum[NT];      // the running maximum (times scale) and the lane's part of the sum
+#pragma unroll
+    for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
+
+    auto compute = [&](const Step<CP>& st, int at, auto masks) {
+        constexpr bool MASK = decltype(masks)::value;
+        f32x4 x[NT][2] = {};
+#pragma unroll
+        for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+            for (int s = 0; s < CP; s++)
+                if (s < C) {
+                    const V kf = decode(st.k[hh][s], T{});
+                    const f32x4 a = four(st.ka[hh][s]);
+#pragma unroll
+                    for (int u = 0; u < NT; u++) {
+                        const f32x4 z = mma(kf, qf[u][s], f32x4{0, 0, 0, 0});
+#pragma unroll
+                        for (int r = 0; r < 4; r++) x[u][hh][r] = fmaf(a[r], z[r], x[u][hh][r]);
+                    }
+                }
+        float most[NT];
+        bool moves = false;
+#pragma unroll
+        for (int u = 0; u < NT; u++) {
+            most[u] = kNegInf;
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    if (MASK) {
+                        if (st.bad >> hh & 1) x[u][hh][r] = __builtin_nanf("");
+                        if (at + 16 * hh + 4 * g + r > last[u]) x[u][hh][r] = kNegInf;
+                    }
+                    most[u] = fmaxf(most[u], x[u][hh][r]);
+                }
+            most[u] *= p.scale;
+            moves |= passes(most[u], top[u]);
+        }
+        if (__ballot(moves)) {
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                // row by row: what a row gives does not depend on its neighbours
+                const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
+                const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
+                top[u] = now;
+                sum[u] *= f;
+#pragma unroll
+                for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < NT; u++) {
+            const float m = top[u] == kNegInf ? 0.0f : top[u];
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    x[u][hh][r] = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
+                    sum[u] += x[u][hh][r];
+                }
+        }
+#pragma unroll
+        for (int c = 0; c < CP; c++)
+            if (c < C) {
+                // rows 32 c + 2 i and 32 c + 2 i + 1 of V^T: byte t of the group's word is key t of the run
+                uint32_t even[4], odd[4];
+#pragma unroll
+                for (int hh = 0; hh < 2; hh++) {
+                    const uint32_t w = st.v[hh][c];
+                    const uint32_t t0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
+                    const uint32_t t1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
+                    const uint32_t t2 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
+                    const uint32_t t3 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+                    even[2 * hh] = __builtin_amdgcn_perm(t1, t0, 0x05040100);
+                    even[2 * hh + 1] = __builtin_amdgcn_perm(t3, t2, 0x05040100);
+                    odd[2 * hh] = __builtin_amdgcn_perm(t1, t0, 0x07060302);
+                    odd[2 * hh + 1] = __builtin_amdgcn_perm(t3, t2, 0x07060302);
+                }
+                const bf16x8 v0 = join4<bf16x8>(even[0], even[1], even[2], even[3]);
+                const bf16x8 v1 = join4<bf16x8>(odd[0], odd[1], odd[2], odd[3]);
+                const f32x4 a0 = four(st.va[0][c]), a1 = four(st.va[1][c]);
+#pragma unroll
+                for (int u = 0; u < NT; u++) {
+                    f32x8 w;
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        w[r] = x[u][0][r] * a0[r];
+                        w[4 + r] = x[u][1][r] * a1[r];
+                        if (MASK) {      // scales behind the last key may be anything
+                            if (at + 4 * g + r > last[u]) w[r] = 0.0f;
+                            if (at + 16 + 4 * g + r > last[u]) w[4 + r] = 0.0f;
+                        }
+                    }
+                    const bf16x8 hi = __builtin_convertvector(w, bf16x8);
+                    acc[u][c][0] = mma(v0, hi, acc[u][c][0]);
+                    acc[u][c][1] = mma(v1, hi, acc[u][c][1]);
+                    if (std::is_same<T, _Float16>::value) {
+                        const bf16x8 lo = __builtin_convertvector(w - __builtin_convertvector(hi, f32x8), bf16x8);
+                        acc[u][c][0] = mma(v0, lo, acc[u][c][0]);
+                        acc[u][c][1] = mma(v1, lo, acc[u][c][1]);
+                    }
+                }
+            }
+    };
+
+    int at = k0 + 32 * wave;
+    if (at < k1) {
+        Step<CP> cur = load(at, ids(at));
+        Ids next = ids(at + 128);
+        for (; at < k1; at += 128) {
+            Step<CP> st = cur;
+            if (at + 128 < k1) cur = load(at + 128, next);
+            next = ids(at + 256);
+            if (at + 31 > open || st.bad) compute(st, at, std::true_type{});
+            else compute(st, at, std::false_type{});
+        }
+    }
+
+    // join the waves
+    __shared__ float2 waves[4][NT][16];
+    __shared__ float sums[4][16][132];
+    float factor[NT], total[NT];
+#pragma unroll
+    for (int u = 0; u < NT; u++) {
+        sum[u] = column_sum(sum[u]);
+        if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < NT; u++) {
+        float m = kNegInf;
+#pragma unroll
+        for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][i].x);
+        float l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+            const float2 o = waves[w][u][i];
+            l += o.x == kNegInf ? o.y : o.y * __builtin_amdgcn_exp2f(o.x - m);
+        }
+        factor[u] = top[u] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - m);
+        total[u] = l;
+        top[u] = m;
+    }
+    const int col = threadIdx.x >> 4, dd = 8 * (threadIdx.x & 15);
+#pragma unroll
+    for (int u = 0; u < NT; u++) {
+#pragma unroll
+        for (int c0 = 0; c0 < CP; c0 += 4) {
+            if (c0 >= C) continue;
+            __syncthreads();
+#pragma unroll
+            for (int c = c0; c < c0 + 4 && c < CP; c++)
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+#pragma unroll
+                    for (int e = 0; e < 2; e++)
+                        sums[wave][i][32 * (c - c0) + 8 * g + 2 * r + e] = acc[u][c][e][r] * factor[u];
+            __syncthreads();
+            const float m = __shfl(top[u], col), l = __shfl(total[u], col);
+            const int r = rw.row0 + 16 * u + col, e0 = 32 * c0 + dd;
+            if (r < rw.rows && e0 < 32 * C) {
+                f32x8 o = {};
+#pragma unroll
+                for (int w = 0; w < 4; w++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) o[e] += sums[w][col][dd + e];
+                const int t = r / p.group, head = h * p.group + r % p.group;
+                if (chunks > 1) {
+                    const int64_t at = ((rw.begin + t) * p.q.heads + head) * chunks + chunk;
+                    *(f32x8*)(part + at * 32 * C + e0) = o;
+                    if (e0 == 0) stats[at] = make_float2(m, l);
+                } else {
+                    if (rw.bad) o = f32x8{} + __builtin_nanf("");
+                    else if (first + t >= 0) o *= 1.0f / l;
+                    store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e0,
+                           __builtin_convertvector(o, V), 8);
+                }
+            }
+        }
+    }
+}
+
+// The parts of one row (query and head) joined: threads take four elements each, groups of threads the chunks
+// in turn.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join(Kv4AttentionParams p, int run, int chunks, const float* part,
+                                              const float2* stats) {
+    __shared__ float sums[256][4];
+    __shared__ float tops[256], totals[256];
+    const int64_t row = blockIdx.x, token = row / p.q.heads;
+    const int head = (int)(row % p.q.heads);
+    int seq = (int)token, n = 1, t = 0;
+    if (p.starts) {
+        int64_t before = 0;
+        const int lane = threadIdx.x & 63;
+        for (int s0 = 0; s0 < p.seqs; s0 += 64)
+            before += __builtin_popcountll(__ballot(s0 + lane < p.seqs && p.starts[s0 + lane] <= token));
+        seq = __builtin_amdgcn_readfirstlane((int)before - 1);
+        if (seq < 0) return;
+        const int64_t a = max(p.starts[seq], 0), b = min((int64_t)p.starts[seq + 1], p.tokens);
+        if (token >= b) return;
+        n = (int)(b - a), t = (int)(token - a);
+    }
+    const int64_t len = p.lengths[seq];
+    const bool bad = len > (int64_t)p.columns * p.cache.page;
+    const int keys = bad || len < 0 ? 0 : max((int)len - n + t + 1, 0);
+    const int used = (keys + run - 1) / run;
+    const int d = 32 * p.cache.groups, per = d / 4, groups = 256 / per;
+    const int e = 4 * (threadIdx.x % per), grp = threadIdx.x / per;
+    const float2* st = stats + row * chunks;
+    const float* pt = part + row * chunks * d + e;
+    float m = kNegInf, l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    if (grp < groups) {
+        for (int c = grp; c < used; c += groups) m = fmaxf(m, st[c].x);
+#pragma unroll 4
+        for (int c = grp; c < used; c += groups) {
+            const float2 s = st[c];
+            const float f = s.x == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(s.x - m);
+            l += f * s.y;
+            o += *(const f32x4*)(pt + (int64_t)c * d) * f;
+        }
+    }
+    tops[threadIdx.x] = m;
+    totals[threadIdx.x] = l;
+    *(f32x4*)sums[threadIdx.x] = o;
+    __syncthreads();
+    if (grp) return;
+    for (int w = 1; w < groups; w++) m = fmaxf(m, tops[threadIdx.x + w * per]);
+    l = 0.0f, o = f32x4{0, 0, 0, 0};
+    for (int w = 0; w < groups; w++) {
+        const int at = threadIdx.x + w * per;
+        const float f = tops[at] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(tops[at] - m);
+        l += f * totals[at];
+        o += *(const f32x4*)sums[at] * f;
+    }
+    if (bad) o = f32x4{0, 0, 0, 0} + __builtin_nanf("");
+    else if (keys) o *= 1.0f / l;
+    T* out = (T*)p.o.p + token * p.o.token + head * p.o.head + e;
+#pragma unroll
+    for (int k = 0; k < 4; k++) out[k] = (T)o[k];
+}
+
+// How a call is split, from what the host knows: rows of a tile, workgroups, and the runs of keys.
+struct Split {
+    int NT, tiles;       // tiles of a sequence of one query
+    int64_t slots;
+    int run, chunks;
+};
+
+Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts, int64_t longest) {
+    Split s;
+    const int group = q_heads / kv_heads;
+    const int64_t rows = starts ? (tokens + seqs - 1) / seqs * group : group;      // of a sequence, on average
+    s.NT = rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4;
+    const int R = 16 * s.NT;
+    s.tiles = (group + R - 1) / R;
+    s.slots = starts ? tokens * group / R + seqs : (int64_t)seqs * s.tiles;
+    const int64_t base = s.slots * kv_heads, want = (int64_t)6 * num_cus();
+    int64_t n = base < want ? (want + base - 1) / base : 1;
+    const int64_t most = (longest + 255) / 256;
+    if (n > most) n = most;
+    if (n < 1) n = 1;
+    int64_t run = ((longest + n - 1) / n + 127) / 128 * 128;
+    if (run < 128) run = 128;
+    s.run = (int)run;
+    s.chunks = (int)((longest + run - 1) / run);
+    if (s.chunks < 1) s.chunks = 1;
+    return s;
+}
+
+size_t stats_bytes(int64_t rows, int chunks) { return ((size_t)rows * chunks * sizeof(float2) + 255) & ~(size_t)255; }
+
+template <typename T, int CP, int NT>
+hipError_t launch_nt(const Kv4AttentionParams& p, const Split& sp, hipStream_t s) {
+    const int64_t grid = sp.slots * p.cache.heads * sp.chunks, rows = p.tokens * p.q.heads;
+    float2* stats = (float2*)p.ws;
+    float* part = (float*)(p.ws + stats_bytes(rows, sp.chunks));
+    k_kv4<T, CP, NT><<<(unsigned)grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || sp.chunks == 1) return e;
+    k_join<T><<<(unsigned)rows, 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
+    return hipGetLastError();
+}
+
+template <typename T, int CP>
+hipError_t launch_cp(const Kv4AttentionParams& p, const Split& sp, hipStream_t s) {
+    if (sp.NT == 1) return launch_nt<T, CP, 1>(p, sp, s);
+    if (sp.NT == 2 || CP == 8) return launch_nt<T, CP, 2>(p, sp, s);
+    return launch_nt<T, CP, CP == 8 ? 2 : 4>(p, sp, s);
+}
+
+template <typename T>
+hipError_t launch_t(const Kv4AttentionParams& p, hipStream_t s) {
+    const Split sp = split(p.tokens, p.q.heads, p.d, p.cache.heads, p.seqs, p.starts != nullptr,
+                           (int64_t)p.columns * p.cache.page);
+    if (p.d <= 64) return launch_cp<T, 2>(p, sp, s);
+    if (p.d <= 128) return launch_cp<T, 4>(p, sp, s);
+    return launch_cp<T, 8>(p, sp, s);
+}
+
+}  // namespace
+
+size_t kv4_attention_workspace(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts,
+                               int64_t longest) {
+    const Split s = split(tokens, q_heads, d, kv_heads, seqs, starts, longest);
+    if (s.chunks == 1) return 0;
+    const int64_t rows = tokens * q_heads;
+    return stats_bytes(rows, s.chunks) + (size_t)rows * s.chunks * d * sizeof(float);
+}
+
+hipError_t launch_kv4_attention(int type, const Kv4AttentionParams& p, hipStream_t s) {
+    return type == kBF16 ? launch_t<__bf16>(p, s) : launch_t<_Float16>(p, s);
+}
+
+}  // namespace esb

@@ -65,6 +65,21 @@ class PostDesc(ctypes.Structure):
                 ("k_sig", ctypes.c_int), ("codes", ctypes.c_void_p), ("absmax_out", ctypes.c_void_p)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_pitch", ctypes.c_int64),
+                ("head_pitch", ctypes.c_int64), ("heads", ctypes.c_int)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("rows", ctypes.c_int64), ("rot", ctypes.c_int),
+                ("adjacent", ctypes.c_int), ("positions", ctypes.c_void_p)]
+
+
+class Kv4(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page", ctypes.c_int),
+                ("heads", ctypes.c_int), ("d", ctypes.c_int)]
+
+
 def lib():
     """Load libesb.so (after torch, so that both share one HIP runtime)."""
     global _lib, _torch
@@ -133,6 +148,14 @@ def lib():
             "esb_w4_unpack": (i32, [P, i32, i32, i32, P, i64, P, i64, P]),
             "esb_w4_gemm_workspace_size": (sz, [i32, i32, i32, i32, i32, i32]),
             "esb_w4_gemm": (i32, [i32, i32, i32, i32, P, i64, i32, P, P, P, i64, i32, P, sz, P]),
+            "esb_rope": (i32, [P, P, i32, i64, i32, P, P, f32, P, P, P, P]),
+            "esb_kv4_page_size": (sz, [i32, i32, i32]),
+            "esb_kv4_append": (i32, [P, P, P, i32, i64, P, P, f32, P, P, P, P, P]),
+            "esb_kv4_pack": (i32, [P, P, P, P, i64, P, P, P]),
+            "esb_kv4_unpack": (i32, [P, i64, P, P, P, P, P, P]),
+            "esb_kv4_attention_workspace_size": (sz, [i64, i32, i32, i32, i32, i32, i64, i32]),
+            "esb_kv4_attention": (i32, [P, i32, i64, P, i32, P, P, P, i64, i32, f32, P, P, sz, P]),
+            "esb_attention": (i32, [P, P, P, i32, i64, i64, i32, i32, P, P, i32, f32, P, P]),
             "esb_gemm_packed": (i32, [i32, i32, i32, P, i64, i32, i32, P, P, i32, i32, P, P, P, i64,
                                       P, sz, P]),
         }
@@ -927,3 +950,284 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=N
     if st:
         raise EsbError("esb_w4_gemm", st)
     return y
+
+
+# ---- a decoder's attention ------------------------------------------------------------------
+
+
+def _same_device(index):
+    """Refuses tensors on another device than the current one, whose stream a call would use."""
+    if index != _torch.cuda.current_device():
+        raise ValueError("the tensors are on cuda:%d, which is not the current device" % index)
+
+
+def _heads(t, name, tokens=None, heads=None, d=None, like=None, out=False):
+    """Heads structure of a device tensor (tokens x heads x d, the elements of a head adjacent)."""
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError("%s must have three dimensions: tokens, heads, elements" % name)
+    n, h, e = shape
+    st, sh, se = t.stride()
+    if se != 1 and e > 1:
+        raise ValueError("%s must have adjacent elements of a head" % name)
+    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
+        raise ValueError("%s must be %s on cuda:%d" % (name, like.dtype, like.get_device()))
+    if (tokens is not None and n != tokens) or (heads is not None and h != heads) or (d is not None and e != d):
+        raise ValueError("%s must be %s x %s x %s" % (name, tokens, heads, d))
+    return Heads(t.data_ptr(), st, sh, h)
+
+
+def _indexes(t, name, n, dtype, index):
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    if t.dim() != 1:
+        raise ValueError("%s must have one dimension" % name)
+    _vector(t, name, n, dtype, index)
+
+
+def _weights(w, name, d, index):
+    if w is not None:
+        if not isinstance(w, _torch.Tensor) or not w.is_cuda:
+            raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+        _vector(w, name, d, _torch.float32, index)
+
+
+def _rotation(table, positions, adjacent, tokens, index):
+    """Rotation structure, or None without a table."""
+    if table is None:
+        if positions is not None:
+            raise ValueError("positions need a table")
+        return None
+    rows, rot, ld = _matrix(table, "table")
+    if table.dtype != _torch.float32:
+        raise TypeError("table must be fp32")
+    if table.get_device() != index or (ld != rot and rows > 1):
+        raise ValueError("table must be contiguous on cuda:%d" % index)
+    _indexes(positions, "positions", tokens, _torch.int32, index)
+    return Rotation(table.data_ptr(), rows, rot, 1 if adjacent else 0, positions.data_ptr())
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def esb_rope(q, k=None, table=None, positions=None, q_w=None, k_w=None, eps=0.0, adjacent=False,
+             q_out=None, k_out=None, stream=None):
+    """Heads normed (eps > 0; q_w, k_w: d fp32 or None) and rotated by their tokens' rows of `table`
+    (rows x rot fp32, cosines then sines; positions: tokens int32): q, k tokens x heads x d, fp32,
+    bf16 or fp16, either None; pairs (j, j + rot / 2), or `adjacent` ones.  Returns (q_out, k_out)."""
+    L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_rope(q, k, table, positions, q_w, k_w, eps, adjacent, q_out, k_out)
+    x = k if q is None else q
+    hx = _heads(x, "k" if q is None else "q")
+    t = _type(x, "q", _FLOATS)
+    tokens, _, d = x.shape
+    index = x.get_device()
+    _same_device(index)
+    sq = sk = so = sp = None
+    if q is not None:
+        sq = hx
+        if q_out is None:
+            q_out = q.new_empty(q.shape)
+        so = _heads(q_out, "q_out", tokens, q.shape[1], d, x)
+    if k is not None:
+        sk = hx if q is None else _heads(k, "k", tokens, None, d, x)
+        if k_out is None:
+            k_out = k.new_empty(k.shape)
+        sp = _heads(k_out, "k_out", tokens, k.shape[1], d, x)
+    _weights(q_w, "q_w", d, index)
+    _weights(k_w, "k_w", d, index)
+    r = _rotation(table, positions, adjacent, tokens, index)
+    st = L.esb_rope(_ref(sq), _ref(sk), t, tokens, d, _addr(q_w), _addr(k_w), eps, _ref(r), _ref(so),
+                    _ref(sp), _stream(None))
+    if st:
+        raise EsbError("esb_rope", st)
+    return q_out, k_out
+
+
+def esb_kv4_page_size(page, heads, d):
+    return int(lib().esb_kv4_page_size(page, heads, d))
+
+
+def _kv4(L, cache, page, heads, d, index=None):
+    """Kv4 structure of a cache tensor: pages x esb_kv4_page_size(page, heads, d) bytes."""
+    if not isinstance(cache, _torch.Tensor) or not cache.is_cuda:
+        raise TypeError("cache must be a CUDA (HIP) tensor")
+    size = L.esb_kv4_page_size(page, heads, d)
+    if size == 0:
+        raise EsbError("esb_kv4_page_size", ESB_E_UNSUPPORTED)
+    if cache.dtype != _torch.uint8 or not cache.is_contiguous() or cache.dim() != 2 or cache.shape[1] != size:
+        raise ValueError("cache must be contiguous uint8, pages x %d" % size)
+    if index is not None and cache.get_device() != index:
+        raise ValueError("cache must be on cuda:%d" % index)
+    return Kv4(cache.data_ptr(), cache.shape[0], page, heads, d)
+
+
+def esb_kv4_append(cache, page, k, v, slots, table=None, positions=None, k_w=None, eps=0.0, adjacent=False,
+                   q=None, q_w=None, q_out=None, stream=None):
+    """Keys (normed and rotated as by esb_rope) and values into the 4-bit cache (pages x
+    esb_kv4_page_size(page, heads, d) bytes): k, v tokens x heads x d, fp32, bf16 or fp16; slots:
+    tokens int64, slot n is token n % page of page n / page, those outside the cache are passed over.
+    q (tokens x any heads x d) is normed and rotated in the same launch; returns q_out, or None."""
+    L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_kv4_append(cache, page, k, v, slots, table, positions, k_w, eps, adjacent, q, q_w, q_out)
+    sk = _heads(k, "k")
+    t = _type(k, "k", _FLOATS)
+    tokens, heads, d = k.shape
+    index = k.get_device()
+    _same_device(index)
+    sv = _heads(v, "v", tokens, heads, d, k)
+    c = _kv4(L, cache, page, heads, d, index)
+    _indexes(slots, "slots", tokens, _torch.int64, index)
+    sq = so = None
+    if q is not None:
+        sq = _heads(q, "q", tokens, None, d, k)
+        if q_out is None:
+            q_out = q.new_empty(q.shape)
+        so = _heads(q_out, "q_out", tokens, q.shape[1], d, k)
+    _weights(q_w, "q_w", d, index)
+    _weights(k_w, "k_w", d, index)
+    r = _rotation(table, positions, adjacent, tokens, index)
+    st = L.esb_kv4_append(_ref(sq), ctypes.byref(sk), ctypes.byref(sv), t, tokens, _addr(q_w), _addr(k_w), eps,
+                          _ref(r), slots.data_ptr(), ctypes.byref(c), _ref(so), _stream(None))
+    if st:
+        raise EsbError("esb_kv4_append", st)
+    return q_out
+
+
+def esb_kv4_pack(cache, page, k, k_alpha, v, v_alpha, slots, stream=None):
+    """ESB(4,1) codes (uint8, tokens x heads x d) and bf16 scales (tokens x heads x d / 32) of keys and
+    values into the cache's slots."""
+    L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_kv4_pack(cache, page, k, k_alpha, v, v_alpha, slots)
+    _heads(k, "k")
+    tokens, heads, d = k.shape
+    index = k.get_device()
+    _same_device(index)
+    c = _kv4(L, cache, page, heads, d, index)
+    for x, name, e, dtype in ((k, "k", d, _torch.uint8), (v, "v", d, _torch.uint8),
+                              (k_alpha, "k_alpha", d // 32, _torch.bfloat16),
+                              (v_alpha, "v_alpha", d // 32, _torch.bfloat16)):
+        _heads(x, name, tokens, heads, e)
+        if x.dtype != dtype or x.get_device() != index or not x.is_contiguous():
+            raise ValueError("%s must be contiguous %s on cuda:%d" % (name, dtype, index))
+    _indexes(slots, "slots", tokens, _torch.int64, index)
+    st = L.esb_kv4_pack(k.data_ptr(), k_alpha.data_ptr(), v.data_ptr(), v_alpha.data_ptr(), tokens,
+                        slots.data_ptr(), ctypes.byref(c), _stream(None))
+    if st:
+        raise EsbError("esb_kv4_pack", st)
+    return cache
+
+
+def esb_kv4_unpack(cache, page, heads, d, slots, stream=None):
+    """(k, k_alpha, v, v_alpha) of the cache's slots: unscaled values (tokens x heads x d float8_e4m3fn,
+    exact) and scales (tokens x heads x d / 32 bf16)."""
+    L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_kv4_unpack(cache, page, heads, d, slots)
+    c = _kv4(L, cache, page, heads, d)
+    index = cache.get_device()
+    _same_device(index)
+    tokens = slots.numel() if isinstance(slots, _torch.Tensor) else 0
+    _indexes(slots, "slots", tokens, _torch.int64, index)
+    k, v = (cache.new_empty(tokens, heads, d, dtype=_torch.float8_e4m3fn) for _ in range(2))
+    ka, va = (cache.new_empty(tokens, heads, d // 32, dtype=_torch.bfloat16) for _ in range(2))
+    st = L.esb_kv4_unpack(ctypes.byref(c), tokens, slots.data_ptr(), k.data_ptr(), ka.data_ptr(), v.data_ptr(),
+                          va.data_ptr(), _stream(None))
+    if st:
+        raise EsbError("esb_kv4_unpack", st)
+    return k, ka, v, va
+
+
+def esb_kv4_attention_workspace_size(tokens, q_heads, d, kv_heads, seqs, has_starts, columns, page):
+    return int(lib().esb_kv4_attention_workspace_size(tokens, q_heads, d, kv_heads, seqs, 1 if has_starts else 0,
+                                                      columns, page))
+
+
+def esb_kv4_attention(q, cache, page, kv_heads, pages, lengths, starts=None, scale=None, out=None,
+                      workspace=None, stream=None):
+    """Attention of q (tokens x heads x d, bf16 or fp16) over the 4-bit cache.  pages: sequences x columns
+    int32 page numbers; lengths: sequences int32, the keys of each, its new tokens among them; starts:
+    sequences + 1 int32, first token of each in q, or None for one token each.  scale: None for
+    1 / sqrt(d).  Query i of n sees keys up to length - n + i.  Returns out (tokens x heads x d)."""
+    L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_kv4_attention(q, cache, page, kv_heads, pages, lengths, starts, scale, out, workspace)
+    sq = _heads(q, "q")
+    t = _type(q, "q", _FLOATS)      # fp32: the library's refusal
+    tokens, heads, d = q.shape
+    index = q.get_device()
+    _same_device(index)
+    c = _kv4(L, cache, page, kv_heads, d, index)
+    seqs, columns, pitch = _matrix(pages, "pages")
+    if pages.dtype != _torch.int32 or pages.get_device() != index:
+        raise ValueError("pages must be int32 on cuda:%d" % index)
+    _indexes(lengths, "lengths", seqs, _torch.int32, index)
+    if starts is not None:
+        _indexes(starts, "starts", seqs + 1, _torch.int32, index)
+    if out is None:
+        out = q.new_empty(q.shape)
+    so = _heads(out, "out", tokens, heads, d, q)
+    wp, wb = None, 0
+    if workspace is None:
+        wb = L.esb_kv4_attention_workspace_size(tokens, heads, d, kv_heads, seqs, 0 if starts is None else 1,
+                                                columns, page)
+        if wb:
+            workspace = q.new_empty(wb, dtype=_torch.uint8)
+            wp = workspace.data_ptr()
+    else:
+        if not isinstance(workspace, _torch.Tensor) or not workspace.is_cuda:
+            raise TypeError("workspace must be a CUDA (HIP) tensor")
+        if workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous on cuda:%d" % index)
+        wp, wb = _ws(workspace)
+    st = L.esb_kv4_attention(ctypes.byref(sq), t, tokens, ctypes.byref(c), seqs, _addr(starts), lengths.data_ptr(),
+                             pages.data_ptr(), pitch, columns, d ** -0.5 if scale is None else scale,
+                             ctypes.byref(so), wp, wb, _stream(None))
+    if st:
+        raise EsbError("esb_kv4_attention", st)
+    return out
+
+
+def esb_attention(q, k, v, q_starts, k_starts=None, causal=True, scale=None, out=None, stream=None):
+    """Attention over packed sequences: q (tokens x heads x d), k and v (tokens x kv heads x d), bf16 or
+    fp16; q_starts, k_starts: sequences + 1 int32, first token of each (k_starts None: q_starts).  causal:
+    query i of n sees keys up to m - n + i of m.  Returns out (q's shape)."""
+    L = _lib or lib()
+    if stream is not None:
+        with _on(stream):
+            return esb_attention(q, k, v, q_starts, k_starts, causal, scale, out)
+    sq = _heads(q, "q")
+    t = _type(q, "q", _FLOATS)      # fp32: the library's refusal
+    tokens, heads, d = q.shape
+    index = q.get_device()
+    _same_device(index)
+    sk = _heads(k, "k", None, None, d, q)
+    k_tokens = k.shape[0]
+    sv = _heads(v, "v", k_tokens, k.shape[1], d, q)
+    _indexes(q_starts, "q_starts", q_starts.numel() if isinstance(q_starts, _torch.Tensor) else 0, _torch.int32,
+             index)
+    seqs = q_starts.numel() - 1
+    if seqs < 0:
+        raise ValueError("q_starts must have a start and an end")
+    if k_starts is not None:
+        _indexes(k_starts, "k_starts", seqs + 1, _torch.int32, index)
+    if out is None:
+        out = q.new_empty(q.shape)
+    so = _heads(out, "out", tokens, heads, d, q)
+    st = L.esb_attention(ctypes.byref(sq), ctypes.byref(sk), ctypes.byref(sv), t, tokens, k_tokens, d, seqs,
+                         q_starts.data_ptr(), _addr(k_starts), 1 if causal else 0,
+                         d ** -0.5 if scale is None else scale, ctypes.byref(so), _stream(None))
+    if st:
+        raise EsbError("esb_attention", st)
+    return out
