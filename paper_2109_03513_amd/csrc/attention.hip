@@ -17,11 +17,19 @@ namespace esb {
 namespace {
 
 constexpr float kLazy = 8.0f;      // how far a score may pass the maximum (log2)
+constexpr float kLarge = 0x1p15f;    // in bf16 and fp16
 constexpr float kNegInf = -__builtin_inff();
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
+// 16 bytes a lane from g to the wave's place in LDS.
+__device__ __forceinline__ void dma16(const void* g, void* wave_base) {
+    __builtin_amdgcn_global_load_lds((global_void*)g, (lds_void*)wave_base, 16, 0, 0);
+}
 __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -43,25 +51,19 @@ template <int DP> struct TileOf {
     static __device__ __forceinline__ int value_turn(int row) { return DP == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
 };
 
-template <typename V> __device__ __forceinline__ bool any_not_finite(V v) {
-    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-    const u16x8 b = __builtin_bit_cast(u16x8, v);
-    constexpr unsigned short e = std::is_same<V, bf16x8>::value ? 0x7f80 : 0x7c00;
-    bool r = false;
-#pragma unroll
-    for (int i = 0; i < 8; i++) r |= (b[i] & e) == e;
-    return r;
+template <typename T> __device__ __forceinline__ bool finite(T v) {
+    constexpr uint16_t e = std::is_same<T, __bf16>::value ? 0x7f80 : 0x7c00;
+    return (__builtin_bit_cast(uint16_t, v) & e) != e;
 }
 
-template <typename T, int DP, int KT>
-__global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
+template <typename T, int DP, int KT, bool DMA>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionParams p) {
     typedef typename Vec8<T>::type V;
     typedef TileOf<DP> L;
     constexpr int R = 128, P = L::kPieces, NP = KT * P / 256, DB = DP / 32, KB = KT / 32;
-    __shared__ V kt[KT * P];
-    __shared__ V vt[KT * P];
-    __shared__ int odd;       // a tile with masks holds values that are not finite
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    __shared__ V tiles[2][2][KT * P];      // two stages of keys and values
+    __shared__ int odd;                    // some tile with masks holds values that are not finite
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
     const int h = blockIdx.x % p.k.heads;
     const int64_t slot = gridDim.x / p.k.heads - 1 - blockIdx.x / p.k.heads;      // the longest rows first
     const Tile t = find_tile(p.q_starts, p.seqs, p.q_tokens, p.group, R, slot);
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
     const int row = row0 + 32 * wave + col;
     const bool live = row < rows;
     const int last = last_of(row);
-    const int wave_open = last_of(row0 + 32 * wave);                                    // all its rows see so far
+    const int open = last_of(row0), wave_open = last_of(row0 + 32 * wave);      // every row sees keys up to here
     const int wave_keys = row0 + 32 * wave < rows ? last_of(min(row0 + 32 * wave + 32, rows) - 1) + 1 : 0;
 
     V qf[DP / 16];
@@ -93,15 +95,24 @@ __global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
     const T* kp = (const T*)p.k.p + ka * p.k.token + h * p.k.head;
     const T* vp = (const T*)p.v.p + ka * p.v.token + h * p.v.head;
 
-    V kr[NP], vr[NP];
-    auto fetch = [&](int j0) {
+    // A tile into LDS.  Rows past the last key and pieces past the head repeat the last one: the former are
+    // masked, the latter meet zeros of the query and outputs that are not stored.
+    const int most = p.d / 8 - 1;
+    auto fetch = [&](int j0, int stage) {
+        const T* kb = kp + (int64_t)j0 * p.k.token;
+        const T* vb = vp + (int64_t)j0 * p.v.token;
+        const int end = nk - 1 - j0;
 #pragma unroll
         for (int u = 0; u < NP; u++) {
-            const int id = tid + 256 * u, j = j0 + id / P, e = 8 * (id % P);
-            kr[u] = vr[u] = V{};
-            if (j < nk && e < p.d) {
-                kr[u] = load8(kp + (int64_t)j * p.k.token + e, 8);
-                vr[u] = load8(vp + (int64_t)j * p.v.token + e, 8);
+            const int id = tid + 256 * u, r = id / P, c = id % P, row = min(r, end);
+            const int ck = 8 * min(c ^ L::key_turn(r), most), cv = 8 * min(c ^ L::value_turn(r), most);
+            if (DMA) {      // rows' offsets fit 32 bits
+                const int at = __builtin_amdgcn_readfirstlane(id & ~63);
+                dma16(kb + (uint32_t)(row * (int)p.k.token + ck), &tiles[stage][0][at]);
+                dma16(vb + (uint32_t)(row * (int)p.v.token + cv), &tiles[stage][1][at]);
+            } else {
+                tiles[stage][0][id] = load8(kb + row * p.k.token + ck, 8);
+                tiles[stage][1][id] = load8(vb + row * p.v.token + cv, 8);
             }
         }
     };
@@ -110,8 +121,7 @@ __global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
     float top = kNegInf, sum = 0.0f;
     f32x16 x[KB];
 
-    auto scores = [&](int j0, auto masks) {
-        constexpr bool MASK = decltype(masks)::value;
+    auto scores = [&](int j0, const V* kt) {
 #pragma unroll
         for (int b = 0; b < KB; b++) {
             x[b] = f32x16{};
@@ -121,14 +131,19 @@ __global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
                 x[b] = mma(kt[r * P + ((2 * s + half) ^ L::key_turn(r))], qf[s], x[b]);
             }
         }
+        if (j0 + KT - 1 > wave_open) {
+            const int end = last - j0 - 4 * half;
+#pragma unroll
+            for (int b = 0; b < KB; b++)
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (32 * b + 8 * (i >> 2) + (i & 3) > end) x[b][i] = kNegInf;
+        }
         float most = kNegInf;
 #pragma unroll
         for (int b = 0; b < KB; b++)
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                if (MASK && j0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3) > last) x[b][i] = kNegInf;
-                most = fmaxf(most, x[b][i]);
-            }
+            for (int i = 0; i < 16; i++) most = fmaxf(most, x[b][i]);
         most *= p.scale;
         if (__ballot(passes(most, top))) {
             // row by row: what a row gives does not depend on its neighbours
@@ -148,14 +163,20 @@ __global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
                 sum += x[b][i];
             }
     };
-    // Four keys from row r on of elements 32 d + lane % 32, by the 16 lanes that hold them row by row.
-    auto values4 = [&](int r, int d) {
-        const int row = r + ((lane & 15) >> 2), e = 32 * d + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
-        const int at = (row * P + ((e >> 3) ^ L::value_turn(row))) * 8 + (e & 7);
+    // Keys r .. r + 3 and r + 8 .. r + 11 of element 32 d + lane % 32, by the 16 lanes that hold them row by row.
+    auto values = [&](const V* vt, int r, int d) {
+        typedef short i16x8 __attribute__((ext_vector_type(8)));
         typedef __attribute__((address_space(3))) i16x4* lds;
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)((T*)vt + at));
+        const int e = 32 * d + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
+        auto four = [&](int row) {
+            return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds)((T*)vt + (row * P + ((e >> 3) ^ L::value_turn(row))) * 8 + (e & 7)));
+        };
+        const i16x4 lo = four(r + ((lane & 15) >> 2)), hi = four(r + 8 + ((lane & 15) >> 2));
+        const i16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(V, v);
     };
-    auto products = [&]() {
+    auto products = [&](const V* vt) {
 #pragma unroll
         for (int b = 0; b < KB; b++)
 #pragma unroll
@@ -165,78 +186,66 @@ __global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
                 for (int i = 0; i < 8; i++) w[i] = x[b][8 * s + i];
                 const V pf = __builtin_convertvector(w, V);
 #pragma unroll
-                for (int d = 0; d < DB; d++) {
-                    const int r = 32 * b + 16 * s + 4 * half;
-                    const i16x4 lo = values4(r, d), hi = values4(r + 8, d);
-                    typedef short i16x8 __attribute__((ext_vector_type(8)));
-                    const i16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    acc[d] = mma(__builtin_bit_cast(V, v), pf, acc[d]);
-                }
-            }
-    };
-    // Values that are not finite, for the rows that see their keys only.
-    auto odd_values = [&](int j0) {
-#pragma unroll
-        for (int b = 0; b < KB; b++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const float there = other_half(x[b][i]);
-#pragma unroll 1
-                for (int o = 0; o < 2; o++) {
-                    const int r = 32 * b + 8 * (i >> 2) + 4 * (half ^ o) + (i & 3);
-                    const float w = o ? there : x[b][i];
-                    if (j0 + r > last) continue;
-#pragma unroll
-                    for (int d = 0; d < DB; d++)
-#pragma unroll
-                        for (int k = 0; k < 16; k++) {
-                            const int e = 32 * d + 8 * (k >> 2) + 4 * half + (k & 3);
-                            const float v = (float)((const T*)vt)[(r * P + ((e >> 3) ^ L::value_turn(r))) * 8 + (e & 7)];
-                            if (!(fabsf(v) < __builtin_inff())) acc[d][k] = fmaf(w, v, acc[d][k]);
-                        }
-                }
+                for (int d = 0; d < DB; d++) acc[d] = mma(values(vt, 32 * b + 16 * s + 4 * half, d), pf, acc[d]);
             }
     };
 
-    if (keys > 0) fetch(0);
-    for (int j0 = 0; j0 < keys; j0 += KT) {
-        __syncthreads();
-        if (tid == 0) odd = 0;
-        const bool check = j0 + KT - 1 > last_of(row0);      // of the whole workgroup: some row has masks here
-        bool mine = false;
+    if (tid == 0) odd = 0;
+    if (keys > 0) fetch(0, 0);
+    for (int j0 = 0, stage = 0; j0 < keys; j0 += KT, stage ^= 1) {
+        if (DMA) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wave's part of the tile
+        __syncthreads();                                  // everyone's; and no one reads the other stage any more
+        if (j0 + KT < keys) fetch(j0 + KT, stage ^ 1);
+        const V* kt = tiles[stage][0];
+        V* vt = tiles[stage][1];
+        if (j0 + KT - 1 > open) {
+            // values that are not finite would reach every row: zeros here, the rows that see them below
+            bool mine = false;
+#pragma unroll 1
+            for (int u = 0; u < NP; u++) {
+                V v = vt[tid + 256 * u];
+                bool any = false;
 #pragma unroll
-        for (int u = 0; u < NP; u++) {
-            const int id = tid + 256 * u, r = id / P, c = id % P;
-            kt[r * P + (c ^ L::key_turn(r))] = kr[u];
-            vt[r * P + (c ^ L::value_turn(r))] = vr[u];
-            if (check) mine |= any_not_finite(vr[u]);
-        }
-        __syncthreads();
-        if (check) {
+                for (int i = 0; i < 8; i++)
+                    if (!finite(v[i])) v[i] = (T)0.0f, any = true;
+                if (any) vt[tid + 256 * u] = v;
+                mine |= any;
+            }
             if (mine) odd = 1;
             __syncthreads();
         }
-        const bool slow = check && odd;
-        if (j0 + KT < keys) fetch(j0 + KT);
-        if (j0 < wave_keys) {
-            if (j0 + KT - 1 > wave_open) scores(j0, std::true_type{});
-            else scores(j0, std::false_type{});
-        }
-        if (slow) {
-            if (j0 < wave_keys) odd_values(j0);
-            __syncthreads();
-#pragma unroll 1
-            for (int u = 0; u < NP; u++) {
-                V& v = vt[tid + 256 * u];
-                V w = v;
+        if (j0 >= wave_keys) continue;
+        scores(j0, kt);
+        products(vt);
+    }
+    if (keys > 0) __syncthreads();
+    if (keys > 0 && odd) {
+        // a multiple of a number that overflows for every such value that a row sees, by products with ones
+        const int from = max(open + 1, 0) / KT * KT;
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if (!(fabsf((float)w[i]) < __builtin_inff())) w[i] = (T)0.0f;
-                v = w;
+        for (int d = 0; d < DB; d++) {
+            f32x16 up = {}, down = {};
+            const int e = 32 * d + col;
+#pragma unroll 1
+            for (int j0 = from; j0 < keys; j0 += 16) {
+                V plus, minus, sees;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int j = j0 + 8 * half + i;
+                    const T v = j < nk && e < p.d ? vp[(int64_t)j * p.v.token + e] : (T)0.0f;
+                    plus[i] = finite(v) || v < (T)0.0f ? (T)0.0f : (T)kLarge;
+                    minus[i] = finite(v) || v > (T)0.0f ? (T)0.0f : (T)-kLarge;
+                    sees[i] = j <= last ? (T)1.0f : (T)0.0f;
+                }
+                up = mma(plus, sees, up);
+                down = mma(minus, sees, down);
             }
-            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 16; i++) {      // the products overflow, and inf - inf is NaN
+                acc[d][i] += up[i] * 0x1p126f;
+                acc[d][i] += down[i] * 0x1p126f;
+            }
         }
-        if (j0 < wave_keys) products();
     }
 
     sum += other_half(sum);
@@ -257,10 +266,17 @@ __global__ __launch_bounds__(256) void k_attention(AttentionParams p) {
         }
 }
 
+// Whether DMA takes the rows: 16-byte pieces, and a tile's rows within 32-bit offsets.
+template <typename T> bool dma_takes(const HeadsView& v) {
+    return (uintptr_t)v.p % 16 == 0 && v.token % 8 == 0 && (v.heads == 1 || v.head % 8 == 0) && v.token < (1 << 24);
+}
+
 template <typename T, int DP, int KT>
 hipError_t launch_d(const AttentionParams& p, hipStream_t s) {
     const int64_t slots = p.q_tokens * p.group / 128 + p.seqs;
-    k_attention<T, DP, KT><<<(unsigned)(slots * p.k.heads), 256, 0, s>>>(p);
+    const unsigned grid = (unsigned)(slots * p.k.heads);
+    if (dma_takes<T>(p.k) && dma_takes<T>(p.v)) k_attention<T, DP, KT, true><<<grid, 256, 0, s>>>(p);
+    else k_attention<T, DP, KT, false><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 
