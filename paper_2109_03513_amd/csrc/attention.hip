@@ -23,12 +23,15 @@ constexpr float kNegInf = -__builtin_inff();
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_void;
+typedef __attribute__((address_space(3))) const void lds_void;
 
-// 16 bytes a lane from g to the wave's place in LDS.
-__device__ __forceinline__ void dma16(const void* g, void* wave_base) {
-    __builtin_amdgcn_global_load_lds((global_void*)g, (lds_void*)wave_base, 16, 0, 0);
+// 16 bytes a lane, from base + at of each, to LDS from the wave's place on.  Written out, so that reads of the other
+// stage do not wait for it: the compiler takes every LDS read behind a DMA for one of its data.  The
+// caller waits for vmcnt(0) before the barrier that hands the tile over.  (m0 is reserved: nothing else here uses it.)
+__device__ __forceinline__ void dma16(const void* base, uint32_t at, const void* wave_place) {
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)wave_place);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds), "v"(at), "s"(base) : "memory");
 }
 __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -97,22 +100,38 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
 
     // A tile into LDS.  Rows past the last key and pieces past the head repeat the last one: the former are
     // masked, the latter meet zeros of the query and outputs that are not stored.
-    const int most = p.d / 8 - 1;
+    const int most = p.d / 8 - 1, piece = tid % P, r0 = tid / P;
+    constexpr int RU = 256 / P;                 // rows that the workgroup brings at a time
+    // pieces by the row's turn, which repeats after two of them
+    const int ck[2] = {8 * min(piece ^ L::key_turn(r0), most), 8 * min(piece ^ L::key_turn(r0 + RU), most)};
+    const int cv[2] = {8 * min(piece ^ L::value_turn(r0), most), 8 * min(piece ^ L::value_turn(r0 + RU), most)};
+    const int k_pitch = (int)p.k.token, v_pitch = (int)p.v.token;      // DMA: tiles' offsets fit 32 bits
     auto fetch = [&](int j0, int stage) {
         const T* kb = kp + (int64_t)j0 * p.k.token;
         const T* vb = vp + (int64_t)j0 * p.v.token;
         const int end = nk - 1 - j0;
+        if (DMA) {
+            const int place = 64 * wave;
+            if (end >= KT - 1) {
 #pragma unroll
-        for (int u = 0; u < NP; u++) {
-            const int id = tid + 256 * u, r = id / P, c = id % P, row = min(r, end);
-            const int ck = 8 * min(c ^ L::key_turn(r), most), cv = 8 * min(c ^ L::value_turn(r), most);
-            if (DMA) {      // rows' offsets fit 32 bits
-                const int at = __builtin_amdgcn_readfirstlane(id & ~63);
-                dma16(kb + (uint32_t)(row * (int)p.k.token + ck), &tiles[stage][0][at]);
-                dma16(vb + (uint32_t)(row * (int)p.v.token + cv), &tiles[stage][1][at]);
+                for (int u = 0; u < NP; u++) {
+                    dma16(kb + (int64_t)(u * RU) * p.k.token, 2 * (uint32_t)(r0 * k_pitch + ck[u & 1]), &tiles[stage][0][place + 256 * u]);
+                    dma16(vb + (int64_t)(u * RU) * p.v.token, 2 * (uint32_t)(r0 * v_pitch + cv[u & 1]), &tiles[stage][1][place + 256 * u]);
+                }
             } else {
-                tiles[stage][0][id] = load8(kb + row * p.k.token + ck, 8);
-                tiles[stage][1][id] = load8(vb + row * p.v.token + cv, 8);
+#pragma unroll 1
+                for (int u = 0; u < NP; u++) {
+                    const int r = min(r0 + u * RU, end);
+                    dma16(kb, 2 * (uint32_t)(r * k_pitch + ck[u & 1]), &tiles[stage][0][place + 256 * u]);
+                    dma16(vb, 2 * (uint32_t)(r * v_pitch + cv[u & 1]), &tiles[stage][1][place + 256 * u]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < NP; u++) {
+                const int64_t r = min(r0 + u * RU, end);
+                tiles[stage][0][tid + 256 * u] = load8(kb + r * p.k.token + ck[u & 1], 8);
+                tiles[stage][1][tid + 256 * u] = load8(vb + r * p.v.token + cv[u & 1], 8);
             }
         }
     };
