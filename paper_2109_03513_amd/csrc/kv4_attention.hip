@@ -54,6 +54,24 @@ __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
+// Rows 32 c + 2 i and 32 c + 2 i + 1 of V^T, from the words of two runs: byte t of a word is key t of its run.
+__device__ __forceinline__ void value_pairs(uint32_t a, uint32_t b, bf16x8* even, bf16x8* odd) {
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int hh = 0; hh < 2; hh++) {
+        const uint32_t w = hh ? b : a;
+        const uint32_t t0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
+        const uint32_t t1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
+        const uint32_t t2 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
+        const uint32_t t3 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+        lo[2 * hh] = __builtin_amdgcn_perm(t1, t0, 0x05040100);
+        lo[2 * hh + 1] = __builtin_amdgcn_perm(t3, t2, 0x05040100);
+        hi[2 * hh] = __builtin_amdgcn_perm(t1, t0, 0x07060302);
+        hi[2 * hh + 1] = __builtin_amdgcn_perm(t3, t2, 0x07060302);
+    }
+    *even = join4<bf16x8>(lo[0], lo[1], lo[2], lo[3]);
+    *odd = join4<bf16x8>(hi[0], hi[1], hi[2], hi[3]);
+}
 // Four bf16 scales as fp32.
 __device__ __forceinline__ f32x4 four(uint2 s) {
     return f32x4{__uint_as_float(s.x << 16), __uint_as_float(s.x & 0xffff0000u), __uint_as_float(s.y << 16),
@@ -106,13 +124,15 @@ __device__ __forceinline__ Rows find_rows(const Kv4AttentionParams& p, int64_t s
     return r;
 }
 
-template <typename T, int CP, int NT>
+// CP: the head's groups, padded (FULL: exactly).  What is padded meets zeros of the query, or makes outputs that
+// are not stored; its scales repeat the last group's.
+template <typename T, int CP, int NT, bool FULL>
 __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int chunks, int tiles, float* part,
                                              float2* stats) {
     typedef typename Vec8<T>::type V;
     constexpr int R = 16 * NT;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int C = p.cache.groups;
+    const int C = FULL ? CP : p.cache.groups;
     int64_t id = blockIdx.x;
     const int chunk = (int)(id % chunks);
     id /= chunks;
@@ -165,11 +185,11 @@ __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int 
             const uint8_t* ks = b + p.cache.key_scales_at() + ((t >> 2) + g) * 8 * C;
             const uint8_t* vs = b + p.cache.value_scales_at() + ((t >> 2) + g) * 8 * C;
 #pragma unroll
-            for (int s = 0; s < CP; s++)
-                if (s < C) {
-                    st.ka[hh][s] = *(const uint2*)(ks + 8 * s);
-                    st.va[hh][s] = *(const uint2*)(vs + 8 * s);
-                }
+            for (int s = 0; s < CP; s++) {
+                const int g8 = FULL ? 8 * s : 8 * min(s, C - 1);
+                st.ka[hh][s] = *(const uint2*)(ks + g8);
+                st.va[hh][s] = *(const uint2*)(vs + g8);
+            }
         }
         return st;
     };
@@ -181,21 +201,20 @@ __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int 
 
     auto compute = [&](const Step<CP>& st, int at, auto masks) {
         constexpr bool MASK = decltype(masks)::value;
-        f32x4 x[NT][2] = {};
+        f32x4 x[NT][2];
 #pragma unroll
         for (int hh = 0; hh < 2; hh++)
 #pragma unroll
-            for (int s = 0; s < CP; s++)
-                if (s < C) {
-                    const V kf = decode(st.k[hh][s], T{});
-                    const f32x4 a = four(st.ka[hh][s]);
+            for (int s = 0; s < CP; s++) {
+                const V kf = decode(st.k[hh][s], T{});
+                const f32x4 a = four(st.ka[hh][s]);
 #pragma unroll
-                    for (int u = 0; u < NT; u++) {
-                        const f32x4 z = mma(kf, qf[u][s], f32x4{0, 0, 0, 0});
+                for (int u = 0; u < NT; u++) {
+                    const f32x4 z = mma(kf, qf[u][s], f32x4{0, 0, 0, 0});
 #pragma unroll
-                        for (int r = 0; r < 4; r++) x[u][hh][r] = fmaf(a[r], z[r], x[u][hh][r]);
-                    }
+                    for (int r = 0; r < 4; r++) x[u][hh][r] = s ? fmaf(a[r], z[r], x[u][hh][r]) : a[r] * z[r];
                 }
+            }
         float most[NT];
         bool moves = false;
 #pragma unroll
@@ -238,47 +257,32 @@ __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int 
                 }
         }
 #pragma unroll
-        for (int c = 0; c < CP; c++)
-            if (c < C) {
-                // rows 32 c + 2 i and 32 c + 2 i + 1 of V^T: byte t of the group's word is key t of the run
-                uint32_t even[4], odd[4];
+        for (int c = 0; c < CP; c++) {
+            bf16x8 v0, v1;
+            value_pairs(st.v[0][c], st.v[1][c], &v0, &v1);
+            const f32x4 a0 = four(st.va[0][c]), a1 = four(st.va[1][c]);
 #pragma unroll
-                for (int hh = 0; hh < 2; hh++) {
-                    const uint32_t w = st.v[hh][c];
-                    const uint32_t t0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
-                    const uint32_t t1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
-                    const uint32_t t2 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
-                    const uint32_t t3 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
-                    even[2 * hh] = __builtin_amdgcn_perm(t1, t0, 0x05040100);
-                    even[2 * hh + 1] = __builtin_amdgcn_perm(t3, t2, 0x05040100);
-                    odd[2 * hh] = __builtin_amdgcn_perm(t1, t0, 0x07060302);
-                    odd[2 * hh + 1] = __builtin_amdgcn_perm(t3, t2, 0x07060302);
+            for (int u = 0; u < NT; u++) {
+                f32x8 w;
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    w[r] = x[u][0][r] * a0[r];
+                    w[4 + r] = x[u][1][r] * a1[r];
+                    if (MASK) {      // scales behind the last key may be anything
+                        if (at + 4 * g + r > last[u]) w[r] = 0.0f;
+                        if (at + 16 + 4 * g + r > last[u]) w[4 + r] = 0.0f;
+                    }
                 }
-                const bf16x8 v0 = join4<bf16x8>(even[0], even[1], even[2], even[3]);
-                const bf16x8 v1 = join4<bf16x8>(odd[0], odd[1], odd[2], odd[3]);
-                const f32x4 a0 = four(st.va[0][c]), a1 = four(st.va[1][c]);
-#pragma unroll
-                for (int u = 0; u < NT; u++) {
-                    f32x8 w;
-#pragma unroll
-                    for (int r = 0; r < 4; r++) {
-                        w[r] = x[u][0][r] * a0[r];
-                        w[4 + r] = x[u][1][r] * a1[r];
-                        if (MASK) {      // scales behind the last key may be anything
-                            if (at + 4 * g + r > last[u]) w[r] = 0.0f;
-                            if (at + 16 + 4 * g + r > last[u]) w[4 + r] = 0.0f;
-                        }
-                    }
-                    const bf16x8 hi = __builtin_convertvector(w, bf16x8);
-                    acc[u][c][0] = mma(v0, hi, acc[u][c][0]);
-                    acc[u][c][1] = mma(v1, hi, acc[u][c][1]);
-                    if (std::is_same<T, _Float16>::value) {
-                        const bf16x8 lo = __builtin_convertvector(w - __builtin_convertvector(hi, f32x8), bf16x8);
-                        acc[u][c][0] = mma(v0, lo, acc[u][c][0]);
-                        acc[u][c][1] = mma(v1, lo, acc[u][c][1]);
-                    }
+                const bf16x8 hi = __builtin_convertvector(w, bf16x8);
+                acc[u][c][0] = mma(v0, hi, acc[u][c][0]);
+                acc[u][c][1] = mma(v1, hi, acc[u][c][1]);
+                if (std::is_same<T, _Float16>::value) {
+                    const bf16x8 lo = __builtin_convertvector(w - __builtin_convertvector(hi, f32x8), bf16x8);
+                    acc[u][c][0] = mma(v0, lo, acc[u][c][0]);
+                    acc[u][c][1] = mma(v1, lo, acc[u][c][1]);
                 }
             }
+        }
     };
 
     int at = k0 + 32 * wave;
@@ -358,6 +362,248 @@ __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int 
     }
 }
 
+// Few rows, one per (query, head): 16 / CP of them to a tile, whose columns are (row, scale group).  A column's query
+// has only its own group's elements, so that one MFMA after the other leaves each group's sum in a column
+// of its own, and a lane needs the scales of one group: four of a key's, four of a value's.  The sum over the
+// groups crosses CP neighbouring lanes; of O^T a column keeps the rows of its group.
+template <int CP> __device__ __forceinline__ float over_groups(float v) {
+    auto turned = [](float x, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v += turned(v, std::integral_constant<int, 0xb1>{});                  // lanes 1 0 3 2 of four
+    if (CP >= 4) v += turned(v, std::integral_constant<int, 0x4e>{});     // lanes 2 3 0 1
+    if (CP >= 8) v += turned(v, std::integral_constant<int, 0x141>{});    // eight lanes mirrored
+    return v;
+}
+
+template <typename T, int CP, int NT, bool FULL>
+__global__ __launch_bounds__(256) void k_kv4_few(Kv4AttentionParams p, int run, int chunks, int tiles, float* part,
+                                                 float2* stats) {
+    typedef typename Vec8<T>::type V;
+    typedef typename Words<CP>::w W;
+    constexpr int HR = 16 / CP, R = HR * NT;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = lane & 15, g = lane >> 4, own = i % CP;
+    const int C = FULL ? CP : p.cache.groups;
+    int64_t id = blockIdx.x;
+    const int chunk = (int)(id % chunks);
+    id /= chunks;
+    const int h = (int)(id % p.cache.heads);
+    const Rows rw = find_rows(p, id / p.cache.heads, tiles, R);
+    if (rw.row0 >= rw.rows) return;
+    const int first = rw.len - rw.n;                    // the last key of query t is first + t
+    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
+    const int k0 = chunk * run, k1 = min(k0 + run, keys);
+    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
+    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
+
+    int last[NT];
+    V qf[NT][CP];
+#pragma unroll
+    for (int u = 0; u < NT; u++) {
+        const int r = rw.row0 + HR * u + i / CP, t = r / p.group;
+        last[u] = first + t;
+        const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
+        V mine = {};
+        if (r < rw.rows && own < C) mine = load8(q + 32 * own + 8 * g, 8);
+#pragma unroll
+        for (int s = 0; s < CP; s++) qf[u][s] = s == own ? mine : V{};
+    }
+
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    const int page = p.cache.page;
+    struct Ids {
+        int a, b;
+    };
+    struct Piece {
+        W k[2], v[2];
+        uint2 ka[2], va[2];
+        int bad;
+    };
+    auto ids = [&](int at) {      // pages of the halves of a step; halves past the last key take its page
+        const int a = min(at, keys - 1) >> p.cache.shift, b = min(at + 16, keys - 1) >> p.cache.shift;
+        return Ids{table[a], table[b]};
+    };
+    // what a lane adds to a half's place in its block
+    const uint32_t k_at = i * 16 * C + g * 4 * C, v_at = g * 64 * C + i * 4 * C;
+    const uint32_t s_at = g * 8 * C + 8 * (FULL ? own : min(own, C - 1));
+    auto load = [&](int at, Ids pg) {
+        Piece st;
+        st.bad = 0;
+#pragma unroll
+        for (int hh = 0; hh < 2; hh++) {
+            int pid = __builtin_amdgcn_readfirstlane(hh ? pg.b : pg.a);
+            if (pid < 0 || pid >= p.cache.pages) pid = 0, st.bad |= 1 << hh;
+            const int t = (at + 16 * hh) & (page - 1);
+            // words past the head's groups are of what follows in the block, and nothing uses them
+            const uint8_t* b = p.cache.block(pid, h);
+            const uint8_t *kb = b + t * 16 * C, *vb = b + p.cache.values_at() + t * 16 * C;
+            const uint8_t *ks = b + p.cache.key_scales_at() + t * 2 * C, *vs = b + p.cache.value_scales_at() + t * 2 * C;
+            st.k[hh] = ((const Loose<W, uint32_t>*)(kb + k_at))->v;
+            st.v[hh] = ((const Loose<W, uint32_t>*)(vb + v_at))->v;
+            st.ka[hh] = *(const uint2*)(ks + s_at);
+            st.va[hh] = *(const uint2*)(vs + s_at);
+        }
+        return st;
+    };
+
+    f32x4 acc[NT][CP][2] = {};
+    float top[NT], sum[NT];
+#pragma unroll
+    for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
+
+    auto compute = [&](const Piece& st, int at) {
+        const bool masks = at + 31 > open || st.bad;
+        f32x4 x[NT][2];
+#pragma unroll
+        for (int hh = 0; hh < 2; hh++) {
+            f32x4 z[NT] = {};
+#pragma unroll
+            for (int s = 0; s < CP; s++) {
+                const V kf = decode(st.k[hh][s], T{});
+#pragma unroll
+                for (int u = 0; u < NT; u++) z[u] = mma(kf, qf[u][s], z[u]);
+            }
+            const f32x4 a = four(st.ka[hh]);
+#pragma unroll
+            for (int u = 0; u < NT; u++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) x[u][hh][r] = over_groups<CP>(a[r] * z[u][r]);
+        }
+        if (masks) {
+#pragma unroll
+            for (int u = 0; u < NT; u++)
+#pragma unroll
+                for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        if (st.bad >> hh & 1) x[u][hh][r] = __builtin_nanf("");
+                        if (at + 16 * hh + 4 * g + r > last[u]) x[u][hh][r] = kNegInf;
+                    }
+        }
+        float most[NT];
+        bool moves = false;
+#pragma unroll
+        for (int u = 0; u < NT; u++) {
+            most[u] = kNegInf;
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) most[u] = fmaxf(most[u], x[u][hh][r]);
+            most[u] *= p.scale;
+            moves |= passes(most[u], top[u]);
+        }
+        if (__ballot(moves)) {
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                // row by row: what a row gives does not depend on its neighbours
+                const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
+                const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
+                top[u] = now;
+                sum[u] *= f;
+#pragma unroll
+                for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
+            }
+        }
+        const f32x4 b[2] = {four(st.va[0]), four(st.va[1])};
+        bf16x8 hi[NT], lo[NT];
+#pragma unroll
+        for (int u = 0; u < NT; u++) {
+            const float m = top[u] == kNegInf ? 0.0f : top[u];
+            f32x8 w;
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
+                    sum[u] += e;
+                    w[4 * hh + r] = e * b[hh][r];
+                }
+            if (masks)      // scales behind the last key may be anything
+#pragma unroll
+                for (int r = 0; r < 8; r++)
+                    if (at + 4 * (r & 4) + 4 * g + (r & 3) > last[u]) w[r] = 0.0f;
+            hi[u] = __builtin_convertvector(w, bf16x8);
+            if (std::is_same<T, _Float16>::value)
+                lo[u] = __builtin_convertvector(w - __builtin_convertvector(hi[u], f32x8), bf16x8);
+        }
+#pragma unroll
+        for (int c = 0; c < CP; c++) {
+            bf16x8 v0, v1;
+            value_pairs(st.v[0][c], st.v[1][c], &v0, &v1);
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                acc[u][c][0] = mma(v0, hi[u], acc[u][c][0]);
+                acc[u][c][1] = mma(v1, hi[u], acc[u][c][1]);
+                if (std::is_same<T, _Float16>::value) {
+                    acc[u][c][0] = mma(v0, lo[u], acc[u][c][0]);
+                    acc[u][c][1] = mma(v1, lo[u], acc[u][c][1]);
+                }
+            }
+        }
+    };
+
+    int at = k0 + 32 * wave;
+    if (at < k1) {
+        Piece cur = load(at, ids(at));
+        Ids next = ids(at + 128);
+        for (; at < k1; at += 128) {
+            const Piece st = cur;
+            if (at + 128 < k1) cur = load(at + 128, next);
+            next = ids(at + 256);
+            compute(st, at);
+        }
+    }
+
+    // join the waves: each leaves its sums under the common maximum
+    __shared__ float2 waves[4][NT][16];
+    __shared__ __align__(16) float sums[4][R][32 * CP];
+#pragma unroll
+    for (int u = 0; u < NT; u++) {
+        sum[u] = column_sum(sum[u]);
+        if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < NT; u++) {
+        float m = kNegInf;
+#pragma unroll
+        for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][i].x);
+        const float f = top[u] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - m);
+        f32x8 o;
+#pragma unroll
+        for (int c = 0; c < CP; c++)
+            if (c == own)
+#pragma unroll
+                for (int r = 0; r < 8; r++) o[r] = acc[u][c][r & 1][r >> 1] * f;
+        *(f32x8*)&sums[wave][HR * u + i / CP][32 * own + 8 * g] = o;
+    }
+    __syncthreads();
+    const int row = threadIdx.x / (4 * CP), e = 8 * (threadIdx.x % (4 * CP)), r = rw.row0 + row;
+    if (row >= R || r >= rw.rows || e >= 32 * C) return;
+    float m = kNegInf, l = 0.0f;
+    const int u = row / HR, column = row % HR * CP;
+#pragma unroll
+    for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][column].x);
+    f32x8 o = {};
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        const float2 x = waves[w][u][column];
+        l += x.x == kNegInf ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - m);
+        o += *(const f32x8*)&sums[w][row][e];
+    }
+    const int t = r / p.group, head = h * p.group + r % p.group;
+    if (chunks > 1) {
+        const int64_t to = ((rw.begin + t) * p.q.heads + head) * chunks + chunk;
+        *(f32x8*)(part + to * 32 * C + e) = o;
+        if (e == 0) stats[to] = make_float2(m, l);
+    } else {
+        if (rw.bad) o = f32x8{} + __builtin_nanf("");
+        else if (first + t >= 0) o *= 1.0f / l;
+        store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e, __builtin_convertvector(o, V), 8);
+    }
+}
+
 // The parts of one row (query and head) joined: threads take four elements each, groups of threads the chunks
 // in turn.
 template <typename T>
@@ -421,6 +667,7 @@ __global__ __launch_bounds__(256) void k_join(Kv4AttentionParams p, int run, int
 
 // How a call is split, from what the host knows: rows of a tile, workgroups, and the runs of keys.
 struct Split {
+    bool few;            // columns are (row, group)
     int NT, tiles;       // tiles of a sequence of one query
     int64_t slots;
     int run, chunks;
@@ -430,8 +677,10 @@ Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool sta
     Split s;
     const int group = q_heads / kv_heads;
     const int64_t rows = starts ? (tokens + seqs - 1) / seqs * group : group;      // of a sequence, on average
-    s.NT = rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4;
-    const int R = 16 * s.NT;
+    const int narrow = d <= 64 ? 8 : d <= 128 ? 4 : 2;      // rows of a tile whose columns are (row, group)
+    s.few = rows <= 2 * narrow;
+    s.NT = s.few ? (rows <= narrow ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4;
+    const int R = (s.few ? narrow : 16) * s.NT;
     s.tiles = (group + R - 1) / R;
     s.slots = starts ? tokens * group / R + seqs : (int64_t)seqs * s.tiles;
     const int64_t base = s.slots * kv_heads, want = (int64_t)6 * num_cus();
@@ -449,32 +698,39 @@ Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool sta
 
 size_t stats_bytes(int64_t rows, int chunks) { return ((size_t)rows * chunks * sizeof(float2) + 255) & ~(size_t)255; }
 
-template <typename T, int CP, int NT>
+template <typename T, int CP, int NT, bool FULL>
 hipError_t launch_nt(const Kv4AttentionParams& p, const Split& sp, hipStream_t s) {
     const int64_t grid = sp.slots * p.cache.heads * sp.chunks, rows = p.tokens * p.q.heads;
     float2* stats = (float2*)p.ws;
     float* part = (float*)(p.ws + stats_bytes(rows, sp.chunks));
-    k_kv4<T, CP, NT><<<(unsigned)grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    if constexpr (NT <= 2) {
+        if (sp.few) k_kv4_few<T, CP, NT, FULL><<<(unsigned)grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    }
+    if (!sp.few) k_kv4<T, CP, NT, FULL><<<(unsigned)grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || sp.chunks == 1) return e;
     k_join<T><<<(unsigned)rows, 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
     return hipGetLastError();
 }
 
-template <typename T, int CP>
+template <typename T, int CP, bool FULL>
 hipError_t launch_cp(const Kv4AttentionParams& p, const Split& sp, hipStream_t s) {
-    if (sp.NT == 1) return launch_nt<T, CP, 1>(p, sp, s);
-    if (sp.NT == 2 || CP == 8) return launch_nt<T, CP, 2>(p, sp, s);
-    return launch_nt<T, CP, CP == 8 ? 2 : 4>(p, sp, s);
+    if (sp.NT == 1) return launch_nt<T, CP, 1, FULL>(p, sp, s);
+    if (sp.NT == 2) return launch_nt<T, CP, 2, FULL>(p, sp, s);
+    if constexpr (CP < 8) return launch_nt<T, CP, 4, FULL>(p, sp, s);
+    return hipErrorInvalidValue;      // not reached: split() gives long heads two tiles at most
 }
 
 template <typename T>
 hipError_t launch_t(const Kv4AttentionParams& p, hipStream_t s) {
     const Split sp = split(p.tokens, p.q.heads, p.d, p.cache.heads, p.seqs, p.starts != nullptr,
                            (int64_t)p.columns * p.cache.page);
-    if (p.d <= 64) return launch_cp<T, 2>(p, sp, s);
-    if (p.d <= 128) return launch_cp<T, 4>(p, sp, s);
-    return launch_cp<T, 8>(p, sp, s);
+    if (p.d == 64) return launch_cp<T, 2, true>(p, sp, s);
+    if (p.d == 128) return launch_cp<T, 4, true>(p, sp, s);
+    if (p.d == 256) return launch_cp<T, 8, true>(p, sp, s);
+    if (p.d < 64) return launch_cp<T, 2, false>(p, sp, s);
+    if (p.d < 128) return launch_cp<T, 4, false>(p, sp, s);
+    return launch_cp<T, 8, false>(p, sp, s);
 }
 
 }  // namespace
