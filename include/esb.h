@@ -694,7 +694,8 @@ int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, u
  * A query that sees no key gets zeros.  What lies in the cache behind what a query sees does not
  * reach it.  A length beyond columns * page makes the sequence's outputs NaN, a page number that is
  * not the cache's those of the queries that see it.  Scores, statistics and sums are fp32; the
- * products p_j alpha enter the matrix cores as bf16 (fp16 outputs: as two bf16, 16 bits).
+ * products p_j alpha enter the matrix cores as bf16 (fp16 outputs: as two bf16, 16 bits), or, with more
+ * than 64 rows a sequence on average (tokens x heads of a group), p_j as fp16.
  *   workspace  device, 256-byte aligned, esb_kv4_attention_workspace_size() bytes (0 where keys
  *              are not split over workgroups).  It carries nothing between calls; concurrent calls
  *              need distinct ones.  Less or NULL: ESB_E_WORKSPACE.

@@ -10,17 +10,14 @@
 // (their sum is not): an error of the terms that is below the rounding of the output.
 #include <type_traits>
 
-#include "kv4.h"
+#include "flash.h"
 
 namespace esb {
 
 namespace {
 
-constexpr float kLazy = 8.0f;      // how far a score may pass the maximum (log2)
 constexpr float kLarge = 0x1p15f;    // in bf16 and fp16
-constexpr float kNegInf = -__builtin_inff();
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 typedef __attribute__((address_space(3))) const void lds_void;
@@ -33,26 +30,9 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t at, const void*
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                  :: "s"(lds), "v"(at), "s"(base) : "memory");
 }
-__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-// Whether a maximum has to move from `top` for a score of `most`.
-__device__ __forceinline__ bool passes(float most, float top) {
-    return most > top + kLazy || (top == kNegInf && most > kNegInf);
-}
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
-
-// Tiles of KT keys x DP elements (the head's d, padded) in LDS, rows of DP / 8 16-byte pieces.  Piece c of a row is
-// at c ^ turn(row): keys so that 16 rows of one piece lie in distinct banks, values so that the 64 bytes
-// that a transposing read takes of eight rows do.
-template <int DP> struct TileOf {
-    static constexpr int kPieces = DP / 8;
-    static __device__ __forceinline__ int key_turn(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
-    static __device__ __forceinline__ int value_turn(int row) { return DP == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
-};
+// Values of a tile are rows of DP / 8 16-byte pieces too, piece c at c ^ value_turn(row), so that the 64 bytes that
+// a transposing read takes of eight rows lie in distinct banks.
+template <int DP> __device__ __forceinline__ int value_turn(int row) { return DP == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
 
 template <typename T> __device__ __forceinline__ bool finite(T v) {
     constexpr uint16_t e = std::is_same<T, __bf16>::value ? 0x7f80 : 0x7c00;
@@ -62,8 +42,7 @@ template <typename T> __device__ __forceinline__ bool finite(T v) {
 template <typename T, int DP, int KT, bool DMA>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionParams p) {
     typedef typename Vec8<T>::type V;
-    typedef TileOf<DP> L;
-    constexpr int R = 128, P = L::kPieces, NP = KT * P / 256, DB = DP / 32, KB = KT / 32;
+    constexpr int R = 128, P = DP / 8, NP = KT * P / 256, DB = DP / 32;
     __shared__ V tiles[2][2][KT * P];      // two stages of keys and values
     __shared__ int odd;                    // some tile with masks holds values that are not finite
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
@@ -85,14 +64,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
     const int open = last_of(row0), wave_open = last_of(row0 + 32 * wave);      // every row sees keys up to here
     const int wave_keys = row0 + 32 * wave < rows ? last_of(min(row0 + 32 * wave + 32, rows) - 1) + 1 : 0;
 
-    V qf[DP / 16];
+    Flash<T, DP, KT> fl;
+    fl.start();
     {
         const T* q = (const T*)p.q.p + (t.begin + row / p.group) * p.q.token + (h * p.group + row % p.group) * p.q.head;
 #pragma unroll
         for (int s = 0; s < DP / 16; s++) {
             const int e = 16 * s + 8 * half;
-            qf[s] = V{};
-            if (live && e < p.d) qf[s] = load8(q + e, 8);
+            fl.qf[s] = V{};
+            if (live && e < p.d) fl.qf[s] = load8(q + e, 8);
         }
     }
     const T* kp = (const T*)p.k.p + ka * p.k.token + h * p.k.head;
@@ -103,8 +83,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
     const int most = p.d / 8 - 1, piece = tid % P, r0 = tid / P;
     constexpr int RU = 256 / P;                 // rows that the workgroup brings at a time
     // pieces by the row's turn, which repeats after two of them
-    const int ck[2] = {8 * min(piece ^ L::key_turn(r0), most), 8 * min(piece ^ L::key_turn(r0 + RU), most)};
-    const int cv[2] = {8 * min(piece ^ L::value_turn(r0), most), 8 * min(piece ^ L::value_turn(r0 + RU), most)};
+    const int ck[2] = {8 * min(piece ^ key_turn<DP>(r0), most), 8 * min(piece ^ key_turn<DP>(r0 + RU), most)};
+    const int cv[2] = {8 * min(piece ^ value_turn<DP>(r0), most), 8 * min(piece ^ value_turn<DP>(r0 + RU), most)};
     const int k_pitch = (int)p.k.token, v_pitch = (int)p.v.token;      // DMA: tiles' offsets fit 32 bits
     auto fetch = [&](int j0, int stage) {
         const T* kb = kp + (int64_t)j0 * p.k.token;
@@ -136,52 +116,6 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
         }
     };
 
-    f32x16 acc[DB] = {};
-    float top = kNegInf, sum = 0.0f;
-    f32x16 x[KB];
-
-    auto scores = [&](int j0, const V* kt) {
-#pragma unroll
-        for (int b = 0; b < KB; b++) {
-            x[b] = f32x16{};
-#pragma unroll
-            for (int s = 0; s < DP / 16; s++) {
-                const int r = 32 * b + col;
-                x[b] = mma(kt[r * P + ((2 * s + half) ^ L::key_turn(r))], qf[s], x[b]);
-            }
-        }
-        if (j0 + KT - 1 > wave_open) {
-            const int end = last - j0 - 4 * half;
-#pragma unroll
-            for (int b = 0; b < KB; b++)
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (32 * b + 8 * (i >> 2) + (i & 3) > end) x[b][i] = kNegInf;
-        }
-        float most = kNegInf;
-#pragma unroll
-        for (int b = 0; b < KB; b++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) most = fmaxf(most, x[b][i]);
-        most *= p.scale;
-        if (__ballot(passes(most, top))) {
-            // row by row: what a row gives does not depend on its neighbours
-            const float all = fmaxf(most, other_half(most)), now = passes(all, top) ? all : top;
-            const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top - now);
-            top = now;
-            sum *= f;
-#pragma unroll
-            for (int d = 0; d < DB; d++) acc[d] *= f;
-        }
-        const float m = top == kNegInf ? 0.0f : top;
-#pragma unroll
-        for (int b = 0; b < KB; b++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-                x[b][i] = __builtin_amdgcn_exp2f(fmaf(x[b][i], p.scale, -m));
-                sum += x[b][i];
-            }
-    };
     // Keys r .. r + 3 and r + 8 .. r + 11 of element 32 d + lane % 32, by the 16 lanes that hold them row by row.
     auto values = [&](const V* vt, int r, int d) {
         typedef short i16x8 __attribute__((ext_vector_type(8)));
@@ -189,26 +123,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
         const int e = 32 * d + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
         auto four = [&](int row) {
             return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds)((T*)vt + (row * P + ((e >> 3) ^ L::value_turn(row))) * 8 + (e & 7)));
+                (lds)((T*)vt + (row * P + ((e >> 3) ^ value_turn<DP>(row))) * 8 + (e & 7)));
         };
         const i16x4 lo = four(r + ((lane & 15) >> 2)), hi = four(r + 8 + ((lane & 15) >> 2));
         const i16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(V, v);
     };
-    auto products = [&](const V* vt) {
-#pragma unroll
-        for (int b = 0; b < KB; b++)
-#pragma unroll
-            for (int s = 0; s < 2; s++) {
-                f32x8 w;
-#pragma unroll
-                for (int i = 0; i < 8; i++) w[i] = x[b][8 * s + i];
-                const V pf = __builtin_convertvector(w, V);
-#pragma unroll
-                for (int d = 0; d < DB; d++) acc[d] = mma(values(vt, 32 * b + 16 * s + 4 * half, d), pf, acc[d]);
-            }
-    };
-
     if (tid == 0) odd = 0;
     if (keys > 0) fetch(0, 0);
     for (int j0 = 0, stage = 0; j0 < keys; j0 += KT, stage ^= 1) {
@@ -234,8 +154,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
             __syncthreads();
         }
         if (j0 >= wave_keys) continue;
-        scores(j0, kt);
-        products(vt);
+        fl.scores(kt, p.scale, j0 + KT - 1 > wave_open, last - j0 - 4 * half);
+        fl.products([&](int r, int d) { return values(vt, r, d); });
     }
     if (keys > 0) __syncthreads();
     if (keys > 0 && odd) {
@@ -261,13 +181,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
             }
 #pragma unroll
             for (int i = 0; i < 16; i++) {      // the products overflow, and inf - inf is NaN
-                acc[d][i] += up[i] * 0x1p126f;
-                acc[d][i] += down[i] * 0x1p126f;
+                fl.acc[d][i] += up[i] * 0x1p126f;
+                fl.acc[d][i] += down[i] * 0x1p126f;
             }
         }
     }
 
-    sum += other_half(sum);
+    const float sum = fl.sum + other_half(fl.sum);
     if (!live) return;
     const float f = last >= 0 ? 1.0f / sum : 0.0f;       // no key: zeros
     T* o = (T*)p.o.p + (t.begin + row / p.group) * p.o.token + (h * p.group + row % p.group) * p.o.head;
@@ -280,7 +200,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
             typedef T t4 __attribute__((ext_vector_type(4)));
             f32x4 w;
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = acc[d][4 * k + i] * f;
+            for (int i = 0; i < 4; i++) w[i] = fl.acc[d][4 * k + i] * f;
             ((Loose<t4, T>*)(o + e))->v = __builtin_convertvector(w, t4);
         }
 }

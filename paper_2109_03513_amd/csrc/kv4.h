@@ -74,6 +74,17 @@ struct Kv4AttentionParams {
     float scale;                    // of the products, times log2(e)
     uint8_t* ws;
 };
+// How a call is split, from what the host knows (kv4_attention.hip).
+struct Kv4Split {
+    int kind;            // kKv4Few, kKv4Some, kKv4Many: which kernel
+    int NT, tiles;       // row tiles of a wave; tiles of a sequence of one query
+    int64_t slots;       // tiles of all sequences
+    int run, chunks;     // keys of a workgroup, and how many there are of such runs
+};
+constexpr int kKv4Few = 0, kKv4Some = 1, kKv4Many = 2;
+// The kernel of many rows (kv4_prompt.hip): 128 of them to a workgroup.
+hipError_t launch_kv4_many(int type, const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats,
+                           hipStream_t s);
 size_t kv4_attention_workspace(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts,
                                int64_t longest);
 hipError_t launch_kv4_attention(int type, const Kv4AttentionParams& p, hipStream_t s);
@@ -97,6 +108,20 @@ struct Tile {
     int seq, index;        // index: of the sequence's tiles
     int64_t begin, end;    // its tokens
 };
+// The sequence of a token: the last one that starts at it or before (seq < 0: none).
+__device__ __forceinline__ Tile find_sequence(const int32_t* starts, int seqs, int64_t tokens, int64_t token) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int s0 = 0; s0 < seqs; s0 += 64)
+        n += __builtin_popcountll(__ballot(s0 + lane < seqs && starts[min(s0 + lane, seqs - 1)] <= token));
+    Tile t;
+    t.seq = __builtin_amdgcn_readfirstlane(n - 1), t.index = 0;
+    t.begin = t.end = 0;
+    if (t.seq < 0) return t;
+    t.begin = min(max((int64_t)starts[t.seq], (int64_t)0), tokens);
+    t.end = min(max((int64_t)starts[t.seq + 1], t.begin), tokens);
+    return t;
+}
 __device__ __forceinline__ Tile find_tile(const int32_t* starts, int seqs, int64_t tokens, int per, int R,
                                           int64_t slot) {
     const int lane = threadIdx.x & 63;
@@ -114,6 +139,31 @@ __device__ __forceinline__ Tile find_tile(const int32_t* starts, int seqs, int64
     t.begin = a, t.end = b;
     t.index = (int)(slot - (a * per / R + t.seq));
     return t;
+}
+
+// A sequence as one workgroup sees it.
+struct Rows {
+    int seq, n, len;     // its queries, its cached keys
+    int64_t begin;       // its first query
+    int row0, rows;      // rows of the tile start here, of all
+    bool bad;            // its length passes its pages
+};
+
+__device__ __forceinline__ Rows find_rows(const Kv4AttentionParams& p, int64_t slot, int tiles, int R) {
+    Rows r;
+    int index;
+    if (p.starts) {
+        const Tile t = find_tile(p.starts, p.seqs, p.tokens, p.group, R, slot);
+        r.seq = t.seq, r.begin = t.begin, r.n = (int)(t.end - t.begin), index = t.index;
+    } else {
+        r.seq = (int)(slot / tiles), index = (int)(slot % tiles), r.begin = r.seq, r.n = 1;
+    }
+    r.rows = r.n * p.group;
+    r.row0 = index < 0 || (int64_t)index * R >= r.rows ? r.rows : index * R;
+    const int64_t len = p.lengths[r.seq];
+    r.bad = len > (int64_t)p.columns * p.cache.page;
+    r.len = r.bad || len < 0 ? 0 : (int)len;
+    return r;
 }
 
 }  // namespace esb

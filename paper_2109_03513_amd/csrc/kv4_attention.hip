@@ -16,14 +16,11 @@
 // maximum moves only when a score passes it by 2^8, so most steps cross no lanes.
 #include <type_traits>
 
-#include "kv4.h"
+#include "flash.h"
 
 namespace esb {
 
 namespace {
-
-constexpr float kLazy = 8.0f;      // how far a score may pass the maximum (log2)
-constexpr float kNegInf = -__builtin_inff();
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int N> struct Words {
@@ -77,10 +74,6 @@ __device__ __forceinline__ f32x4 four(uint2 s) {
     return f32x4{__uint_as_float(s.x << 16), __uint_as_float(s.x & 0xffff0000u), __uint_as_float(s.y << 16),
                  __uint_as_float(s.y & 0xffff0000u)};
 }
-// Whether a maximum has to move from `top` for a score of `most`.
-__device__ __forceinline__ bool passes(float most, float top) {
-    return most > top + kLazy || (top == kNegInf && most > kNegInf);
-}
 // Over the four lanes that hold one column.
 __device__ __forceinline__ float column_max(float v) {
     v = fmaxf(v, __shfl_xor(v, 16));
@@ -98,31 +91,6 @@ template <int CP> struct Step {
     uint2 ka[2][CP], va[2][CP];
     int bad;             // halves whose page is none of the cache's
 };
-
-// A sequence as one workgroup sees it.
-struct Rows {
-    int seq, n, len;     // its queries, its cached keys
-    int64_t begin;       // its first query
-    int row0, rows;      // rows of the tile start here, of all
-    bool bad;            // its length passes its pages
-};
-
-__device__ __forceinline__ Rows find_rows(const Kv4AttentionParams& p, int64_t slot, int tiles, int R) {
-    Rows r;
-    int index;
-    if (p.starts) {
-        const Tile t = find_tile(p.starts, p.seqs, p.tokens, p.group, R, slot);
-        r.seq = t.seq, r.begin = t.begin, r.n = (int)(t.end - t.begin), index = t.index;
-    } else {
-        r.seq = (int)(slot / tiles), index = (int)(slot % tiles), r.begin = r.seq, r.n = 1;
-    }
-    r.rows = r.n * p.group;
-    r.row0 = index < 0 || (int64_t)index * R >= r.rows ? r.rows : index * R;
-    const int64_t len = p.lengths[r.seq];
-    r.bad = len > (int64_t)p.columns * p.cache.page;
-    r.len = r.bad || len < 0 ? 0 : (int)len;
-    return r;
-}
 
 // CP: the head's groups, padded (FULL: exactly).  What is padded meets zeros of the query, or makes outputs that
 // are not stored; its scales repeat the last group's.
@@ -377,7 +345,7 @@ template <int CP> __device__ __forceinline__ float over_groups(float v) {
 }
 
 template <typename T, int CP, int NT, bool FULL>
-__global__ __launch_bounds__(256) void k_kv4_few(Kv4AttentionParams p, int run, int chunks, int tiles, float* part,
+__global__ __launch_bounds__(256, CP * NT <= 4 ? 3 : CP * NT <= 8 ? 2 : 1) void k_kv4_few(Kv4AttentionParams p, int run, int chunks, int tiles, float* part,
                                                  float2* stats) {
     typedef typename Vec8<T>::type V;
     typedef typename Words<CP>::w W;
@@ -604,8 +572,22 @@ __global__ __launch_bounds__(256) void k_kv4_few(Kv4AttentionParams p, int run, 
     }
 }
 
-// The parts of one row (query and head) joined: threads take four elements each, groups of threads the chunks
-// in turn.
+// What a join has to know of a row: the query's token and head, and its keys' runs.
+struct JoinRow {
+    bool live, bad;
+    int keys;
+};
+__device__ __forceinline__ JoinRow join_row(const Kv4AttentionParams& p, int seq, int64_t begin, int64_t end, int64_t token) {
+    const int64_t len = p.lengths[seq];
+    JoinRow r;
+    r.live = token >= begin && token < end;
+    r.bad = len > (int64_t)p.columns * p.cache.page;
+    r.keys = r.bad || len < 0 ? 0 : max((int)len - (int)(end - begin) + (int)(token - begin) + 1, 0);
+    return r;
+}
+
+// The parts of one row (query and head) joined, a workgroup to a row: threads take four elements each, groups of
+// threads the parts in turn, eight in flight.
 template <typename T>
 __global__ __launch_bounds__(256) void k_join(Kv4AttentionParams p, int run, int chunks, const float* part,
                                               const float2* stats) {
@@ -613,38 +595,44 @@ __global__ __launch_bounds__(256) void k_join(Kv4AttentionParams p, int run, int
     __shared__ float tops[256], totals[256];
     const int64_t row = blockIdx.x, token = row / p.q.heads;
     const int head = (int)(row % p.q.heads);
-    int seq = (int)token, n = 1, t = 0;
+    JoinRow jr;
     if (p.starts) {
-        int64_t before = 0;
-        const int lane = threadIdx.x & 63;
-        for (int s0 = 0; s0 < p.seqs; s0 += 64)
-            before += __builtin_popcountll(__ballot(s0 + lane < p.seqs && p.starts[s0 + lane] <= token));
-        seq = __builtin_amdgcn_readfirstlane((int)before - 1);
-        if (seq < 0) return;
-        const int64_t a = max(p.starts[seq], 0), b = min((int64_t)p.starts[seq + 1], p.tokens);
-        if (token >= b) return;
-        n = (int)(b - a), t = (int)(token - a);
+        const Tile t = find_sequence(p.starts, p.seqs, p.tokens, token);
+        if (t.seq < 0) return;
+        jr = join_row(p, t.seq, t.begin, t.end, token);
+    } else {
+        jr = join_row(p, (int)token, token, token + 1, token);
     }
-    const int64_t len = p.lengths[seq];
-    const bool bad = len > (int64_t)p.columns * p.cache.page;
-    const int keys = bad || len < 0 ? 0 : max((int)len - n + t + 1, 0);
-    const int used = (keys + run - 1) / run;
+    if (!jr.live) return;
+    const int used = (jr.keys + run - 1) / run;
     const int d = 32 * p.cache.groups, per = d / 4, groups = 256 / per;
     const int e = 4 * (threadIdx.x % per), grp = threadIdx.x / per;
     const float2* st = stats + row * chunks;
     const float* pt = part + row * chunks * d + e;
     float m = kNegInf, l = 0.0f;
     f32x4 o = {0, 0, 0, 0};
-    if (grp < groups) {
-        for (int c = grp; c < used; c += groups) m = fmaxf(m, st[c].x);
-#pragma unroll 4
-        for (int c = grp; c < used; c += groups) {
-            const float2 s = st[c];
-            const float f = s.x == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(s.x - m);
-            l += f * s.y;
-            o += *(const f32x4*)(pt + (int64_t)c * d) * f;
+    if (grp < groups)
+        for (int c0 = grp; c0 < used; c0 += 8 * groups) {
+            float2 s[8];
+            f32x4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const int c = c0 + k * groups;
+                s[k] = make_float2(kNegInf, 0.0f), v[k] = f32x4{0, 0, 0, 0};
+                if (c < used) s[k] = st[c], v[k] = *(const f32x4*)(pt + (int64_t)c * d);
+            }
+            float now = m;
+#pragma unroll
+            for (int k = 0; k < 8; k++) now = fmaxf(now, s[k].x);
+            const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+            l *= f, o *= f, m = now;
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const float g = s[k].x == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(s[k].x - m);
+                l = fmaf(g, s[k].y, l);
+                o += v[k] * g;
+            }
         }
-    }
     tops[threadIdx.x] = m;
     totals[threadIdx.x] = l;
     *(f32x4*)sums[threadIdx.x] = o;
@@ -658,34 +646,73 @@ __global__ __launch_bounds__(256) void k_join(Kv4AttentionParams p, int run, int
         l += f * totals[at];
         o += *(const f32x4*)sums[at] * f;
     }
-    if (bad) o = f32x4{0, 0, 0, 0} + __builtin_nanf("");
-    else if (keys) o *= 1.0f / l;
-    T* out = (T*)p.o.p + token * p.o.token + head * p.o.head + e;
-#pragma unroll
-    for (int k = 0; k < 4; k++) out[k] = (T)o[k];
+    if (jr.bad) o = f32x4{0, 0, 0, 0} + __builtin_nanf("");
+    else if (jr.keys) o *= 1.0f / l;
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    ((Loose<t4, T>*)((T*)p.o.p + token * p.o.token + head * p.o.head + e))->v = __builtin_convertvector(o, t4);
 }
 
-// How a call is split, from what the host knows: rows of a tile, workgroups, and the runs of keys.
-struct Split {
-    bool few;            // columns are (row, group)
-    int NT, tiles;       // tiles of a sequence of one query
-    int64_t slots;
-    int run, chunks;
-};
+// At most eight parts: a thread to four elements of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join_few(Kv4AttentionParams p, int run, int chunks, const float* part,
+                                                  const float2* stats) {
+    const int d = 32 * p.cache.groups, per = d / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / per, token = row / p.q.heads;
+    const int head = (int)(row % p.q.heads), e = 4 * (int)(id % per);
+    JoinRow jr;
+    jr.live = false;
+    if (p.starts) {
+        // the sequence of the workgroup's first token, then on from there
+        const Tile t = find_sequence(p.starts, p.seqs, p.tokens, (int64_t)blockIdx.x * 256 / per / p.q.heads);
+        int seq = t.seq;
+        while (seq + 1 < p.seqs && p.starts[seq + 1] <= token) seq++;
+        if (seq < 0) return;
+        const int64_t a = min(max((int64_t)p.starts[seq], (int64_t)0), p.tokens);
+        const int64_t b = min(max((int64_t)p.starts[seq + 1], a), p.tokens);
+        if (token < p.tokens) jr = join_row(p, seq, a, b, token);
+    } else if (token < p.tokens) {
+        jr = join_row(p, (int)token, token, token + 1, token);
+    }
+    if (!jr.live) return;
+    const int used = min((jr.keys + run - 1) / run, 8);
+    const float2* st = stats + row * chunks;
+    const float* pt = part + row * chunks * d + e;
+    float2 s[8];
+    f32x4 v[8];
+    float m = kNegInf, l = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; c++) {
+        s[c] = make_float2(kNegInf, 0.0f), v[c] = f32x4{0, 0, 0, 0};
+        if (c < used) s[c] = st[c], v[c] = *(const f32x4*)(pt + (int64_t)c * d);
+        m = fmaxf(m, s[c].x);
+    }
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < 8; c++) {
+        const float f = s[c].x == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(s[c].x - m);
+        l = fmaf(f, s[c].y, l);
+        o += v[c] * f;
+    }
+    if (jr.bad) o = f32x4{0, 0, 0, 0} + __builtin_nanf("");
+    else if (jr.keys) o *= 1.0f / l;
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    ((Loose<t4, T>*)((T*)p.o.p + token * p.o.token + head * p.o.head + e))->v = __builtin_convertvector(o, t4);
+}
 
-Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts, int64_t longest) {
-    Split s;
-    const int group = q_heads / kv_heads;
+Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts, int64_t longest) {
+    Kv4Split s;
+    const int group = q_heads / kv_heads, cus = num_cus();
     const int64_t rows = starts ? (tokens + seqs - 1) / seqs * group : group;      // of a sequence, on average
     const int narrow = d <= 64 ? 8 : d <= 128 ? 4 : 2;      // rows of a tile whose columns are (row, group)
-    s.few = rows <= 2 * narrow;
-    s.NT = s.few ? (rows <= narrow ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4;
-    const int R = (s.few ? narrow : 16) * s.NT;
+    s.kind = rows <= 2 * narrow ? kKv4Few : rows <= 64 ? kKv4Some : kKv4Many;
+    s.NT = rows <= (s.kind == kKv4Few ? narrow : 16) || (s.kind == kKv4Some && d > 128) ? 1 : 2;
+    const int R = s.kind == kKv4Many ? 128 : (s.kind == kKv4Few ? narrow : 16) * s.NT;
     s.tiles = (group + R - 1) / R;
     s.slots = starts ? tokens * group / R + seqs : (int64_t)seqs * s.tiles;
-    const int64_t base = s.slots * kv_heads, want = (int64_t)6 * num_cus();
-    int64_t n = base < want ? (want + base - 1) / base : 1;
-    const int64_t most = (longest + 255) / 256;
+    const int64_t base = s.slots * kv_heads;
+    // Few rows: parts of at least 384 keys, for twelve workgroups a CU.  Many: as many as run at once (two a CU).
+    int64_t n = s.kind == kKv4Many ? 2 * cus / base : (12 * cus + base - 1) / base;
+    const int64_t most = (longest + 383) / 384;
     if (n > most) n = most;
     if (n < 1) n = 1;
     int64_t run = ((longest + n - 1) / n + 127) / 128 * 128;
@@ -698,53 +725,57 @@ Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool sta
 
 size_t stats_bytes(int64_t rows, int chunks) { return ((size_t)rows * chunks * sizeof(float2) + 255) & ~(size_t)255; }
 
-template <typename T, int CP, int NT, bool FULL>
-hipError_t launch_nt(const Kv4AttentionParams& p, const Split& sp, hipStream_t s) {
-    const int64_t grid = sp.slots * p.cache.heads * sp.chunks, rows = p.tokens * p.q.heads;
-    float2* stats = (float2*)p.ws;
-    float* part = (float*)(p.ws + stats_bytes(rows, sp.chunks));
-    if constexpr (NT <= 2) {
-        if (sp.few) k_kv4_few<T, CP, NT, FULL><<<(unsigned)grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+template <typename T, int CP, bool FULL>
+hipError_t launch_cp(const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats, hipStream_t s) {
+    const unsigned grid = (unsigned)(sp.slots * p.cache.heads * sp.chunks);
+    if (sp.kind == kKv4Few) {
+        if (sp.NT == 1) k_kv4_few<T, CP, 1, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+        else k_kv4_few<T, CP, 2, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    } else {
+        // long heads: one tile, two would not fit the registers
+        if (sp.NT == 1) k_kv4<T, CP, 1, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+        else k_kv4<T, CP, CP == 8 ? 1 : 2, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
     }
-    if (!sp.few) k_kv4<T, CP, NT, FULL><<<(unsigned)grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || sp.chunks == 1) return e;
-    k_join<T><<<(unsigned)rows, 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
     return hipGetLastError();
 }
 
-template <typename T, int CP, bool FULL>
-hipError_t launch_cp(const Kv4AttentionParams& p, const Split& sp, hipStream_t s) {
-    if (sp.NT == 1) return launch_nt<T, CP, 1, FULL>(p, sp, s);
-    if (sp.NT == 2) return launch_nt<T, CP, 2, FULL>(p, sp, s);
-    if constexpr (CP < 8) return launch_nt<T, CP, 4, FULL>(p, sp, s);
-    return hipErrorInvalidValue;      // not reached: split() gives long heads two tiles at most
-}
-
 template <typename T>
-hipError_t launch_t(const Kv4AttentionParams& p, hipStream_t s) {
-    const Split sp = split(p.tokens, p.q.heads, p.d, p.cache.heads, p.seqs, p.starts != nullptr,
-                           (int64_t)p.columns * p.cache.page);
-    if (p.d == 64) return launch_cp<T, 2, true>(p, sp, s);
-    if (p.d == 128) return launch_cp<T, 4, true>(p, sp, s);
-    if (p.d == 256) return launch_cp<T, 8, true>(p, sp, s);
-    if (p.d < 64) return launch_cp<T, 2, false>(p, sp, s);
-    if (p.d < 128) return launch_cp<T, 4, false>(p, sp, s);
-    return launch_cp<T, 8, false>(p, sp, s);
+hipError_t launch_t(int type, const Kv4AttentionParams& p, hipStream_t s) {
+    const Kv4Split sp = split(p.tokens, p.q.heads, p.d, p.cache.heads, p.seqs, p.starts != nullptr,
+                              (int64_t)p.columns * p.cache.page);
+    const int64_t rows = p.tokens * p.q.heads;
+    float2* stats = (float2*)p.ws;
+    float* part = (float*)(p.ws + stats_bytes(rows, sp.chunks));
+    hipError_t e;
+    if (sp.kind == kKv4Many) e = launch_kv4_many(type, p, sp, part, stats, s);
+    else if (p.d == 64) e = launch_cp<T, 2, true>(p, sp, part, stats, s);
+    else if (p.d == 128) e = launch_cp<T, 4, true>(p, sp, part, stats, s);
+    else if (p.d == 256) e = launch_cp<T, 8, true>(p, sp, part, stats, s);
+    else if (p.d < 64) e = launch_cp<T, 2, false>(p, sp, part, stats, s);
+    else if (p.d < 128) e = launch_cp<T, 4, false>(p, sp, part, stats, s);
+    else e = launch_cp<T, 8, false>(p, sp, part, stats, s);
+    if (e != hipSuccess || sp.chunks == 1) return e;
+    if (sp.chunks <= 8) {
+        const int64_t threads = rows * (p.d / 4);
+        k_join_few<T><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
+    } else {
+        k_join<T><<<(unsigned)rows, 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
 size_t kv4_attention_workspace(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts,
                                int64_t longest) {
-    const Split s = split(tokens, q_heads, d, kv_heads, seqs, starts, longest);
+    const Kv4Split s = split(tokens, q_heads, d, kv_heads, seqs, starts, longest);
     if (s.chunks == 1) return 0;
     const int64_t rows = tokens * q_heads;
     return stats_bytes(rows, s.chunks) + (size_t)rows * s.chunks * d * sizeof(float);
 }
 
 hipError_t launch_kv4_attention(int type, const Kv4AttentionParams& p, hipStream_t s) {
-    return type == kBF16 ? launch_t<__bf16>(p, s) : launch_t<_Float16>(p, s);
+    return type == kBF16 ? launch_t<__bf16>(type, p, s) : launch_t<_Float16>(type, p, s);
 }
 
 }  // namespace esb

@@ -1,0 +1,283 @@
+// Attention over the 4-bit paged cache for many rows (a prompt or a part of one): kv4_attention.hip's definition, in
+// the form of attention.hip.  A workgroup of 128 rows decodes a tile of 64 keys and values once, with their
+// scales, into LDS as fp16, where its four waves read it.
+//
+// E2M1 times a bf16 scale has ten bits: exact in fp16, where its range allows.  So a tile's key scales are
+// brought below 2 by a power of two (the largest one's exponent, which the scores get back with the scale of the
+// softmax), the query's row likewise, and the value scales by the largest exponent met so far (when it grows, the
+// sums follow).  What then lies below fp16's normal numbers is off by 2^-25 of the largest of its tile.  The products
+// are fp16 MFMAs for both types of queries; probabilities are rounded to fp16.
+//
+// Values whose scale is not finite count as zero in the products, and their elements become NaN at the end for
+// the rows that see them.
+#include <type_traits>
+
+#include "flash.h"
+
+namespace esb {
+
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t bits(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ f16x2 halves(uint32_t v) { return __builtin_bit_cast(f16x2, v); }
+
+// The two nibbles of each byte of w, as fp16.
+__device__ __forceinline__ void pairs(uint32_t w, f16x2 (&o)[4]) {
+    o[0] = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0));
+    o[1] = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1));
+    o[2] = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2));
+    o[3] = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3));
+}
+__device__ __forceinline__ float bf16_value(uint32_t b) { return __uint_as_float(b << 16); }
+// Exponent field of a bf16 scale, 0 where it is not finite.
+__device__ __forceinline__ int exponent(uint32_t b) {
+    const int e = (b >> 7) & 0xff;
+    return e == 0xff ? 0 : e;
+}
+__device__ __forceinline__ int wave_max(int v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v = max(v, __shfl_xor(v, o));
+    return v;
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4AttentionParams p, int run, int chunks, int tiles,
+                                                                     float* part, float2* stats) {
+    typedef typename Vec8<T>::type V;
+    constexpr int KT = 64, R = 128, P = DP / 8, CP = DP / 32, DB = DP / 32;
+    typedef uint32_t W __attribute__((ext_vector_type(CP)));
+    __shared__ f16x8 kt[2][KT * P];              // rows of keys, pieces turned
+    __shared__ uint2 vt[2][KT / 4 * DP];         // runs of four keys, of every element
+    __shared__ int peaks[2][4][2];               // by wave: largest exponents of the key and the value scales
+    __shared__ int odd;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5, C = p.cache.groups;
+    int64_t id = blockIdx.x;
+    const int h = (int)(id % p.cache.heads);
+    id /= p.cache.heads;
+    const int chunk = (int)(id % chunks);
+    const Rows rw = find_rows(p, id / chunks, tiles, R);
+    if (rw.row0 >= rw.rows) return;
+    const int first = rw.len - rw.n;                    // the last key of query t is first + t
+    auto last_of = [&](int r) { return first + r / p.group; };
+    const int keys = max(last_of(min(rw.row0 + R, rw.rows) - 1) + 1, 0);
+    const int k0 = chunk * run, k1 = min(k0 + run, keys);
+    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
+
+    const int row = rw.row0 + 32 * wave + col;
+    const bool live = row < rw.rows;
+    const int last = last_of(row), wave_open = last_of(rw.row0 + 32 * wave);
+    const int wave_keys = rw.row0 + 32 * wave < rw.rows ? last_of(min(rw.row0 + 32 * wave + 32, rw.rows) - 1) + 1 : 0;
+    const int head = h * p.group + row % p.group;
+    const int64_t token = rw.begin + row / p.group;
+
+    Flash<_Float16, DP, KT> fl;
+    fl.start();
+    int q_exponent;
+    {
+        V raw[DP / 16];
+        uint32_t most = 0;
+        const T* q = (const T*)p.q.p + token * p.q.token + head * p.q.head;
+#pragma unroll
+        for (int s = 0; s < DP / 16; s++) {
+            const int e = 16 * s + 8 * half;
+            raw[s] = V{};
+            if (live && e < p.d) raw[s] = load8(q + e, 8);
+            const f32x8 v = __builtin_convertvector(raw[s], f32x8);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+                if (b <= 0x7f800000u) most = max(most, b);
+            }
+        }
+        most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+        q_exponent = (int)(most >> 23) - 127;
+#pragma unroll
+        for (int s = 0; s < DP / 16; s++) {
+            f32x8 v = __builtin_convertvector(raw[s], f32x8);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = __builtin_amdgcn_ldexpf(v[i], -q_exponent);
+            fl.qf[s] = __builtin_convertvector(v, f16x8);
+        }
+    }
+
+    // A thread's part of a tile: every group's word of key tid / 4, elements 8 (tid % 4) of a group on; and of the run of
+    // four values tid / 16 (of the same page), elements 2 (tid % 16) of a group on.
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    const int page = p.cache.page, key = tid >> 2, a4 = tid & 3, run4 = tid >> 4, a16 = tid & 15;
+    W kw, vw;
+    uint32_t ka[CP];
+    uint2 va[CP];
+    auto page_of = [&](int j0) { return table[min(j0 + key, keys - 1) >> p.cache.shift]; };
+    auto load = [&](int j0, int pid) {
+        const bool bad = pid < 0 || pid >= p.cache.pages;
+        const uint8_t* b = p.cache.block(bad ? 0 : pid, h);
+        const int t = (j0 + key) & (page - 1);
+        // words past the head's groups are of what follows in the block, and meet zeros of the query or make
+        // outputs that are not stored
+        kw = ((const Loose<W, uint32_t>*)(b + t * 16 * C + a4 * 4 * C))->v;
+        vw = ((const Loose<W, uint32_t>*)(b + p.cache.values_at() + (t >> 2) * 64 * C + a16 * 4 * C))->v;
+        const uint8_t* ks = b + p.cache.key_scales_at() + p.cache.scale_run(t) + (t & 3) * 2;
+        const uint8_t* vs = b + p.cache.value_scales_at() + p.cache.scale_run(t);
+#pragma unroll
+        for (int g = 0; g < CP; g++) {
+            const int at = 8 * min(g, C - 1);
+            ka[g] = *(const uint16_t*)(ks + at);
+            va[g] = *(const uint2*)(vs + at);
+        }
+        if (bad) {
+#pragma unroll
+            for (int g = 0; g < CP; g++) ka[g] = 0x7fc0;
+        }
+        if (j0 + KT > keys) {      // scales behind the last key may be anything
+            const int left = keys - j0 - 4 * run4;
+            const uint32_t x = left >= 2 ? ~0u : left == 1 ? 0xffffu : 0u, y = left >= 4 ? ~0u : left == 3 ? 0xffffu : 0u;
+#pragma unroll
+            for (int g = 0; g < CP; g++) {
+                if (j0 + key >= keys) ka[g] = 0;
+                va[g].x &= x, va[g].y &= y;
+            }
+        }
+    };
+    auto put_peaks = [&](int stage) {
+        int k = 0, v = 0;
+#pragma unroll
+        for (int g = 0; g < CP; g++) {
+            if (g % 4 == (CP >= 4 ? a4 : a4 % CP)) k = max(k, exponent(ka[g]));
+            if (g == a16 % CP)
+                v = max(max(exponent(va[g].x & 0xffff), exponent(va[g].x >> 16)), max(exponent(va[g].y & 0xffff), exponent(va[g].y >> 16)));
+        }
+        k = wave_max(k), v = wave_max(v);
+        if (lane == 0) peaks[stage][wave][0] = k, peaks[stage][wave][1] = v;
+    };
+    auto peak = [&](int stage, int what) {
+        return max(max(peaks[stage][0][what], peaks[stage][1][what]), max(peaks[stage][2][what], peaks[stage][3][what])) - 127;
+    };
+    auto decode = [&](int stage, int ke, int ve) {
+        bool mine = false;
+#pragma unroll
+        for (int g = 0; g < CP; g++) {
+            f16x2 o[4];
+            const _Float16 s = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(ka[g]), -ke);
+            pairs(kw[g], o);
+            const u32x4 k = {bits(o[0] * s), bits(o[1] * s), bits(o[2] * s), bits(o[3] * s)};
+            kt[stage][key * P + ((4 * g + a4) ^ key_turn<DP>(key))] = __builtin_bit_cast(f16x8, k);
+            float b[4] = {bf16_value(va[g].x), __uint_as_float(va[g].x & 0xffff0000u), bf16_value(va[g].y),
+                          __uint_as_float(va[g].y & 0xffff0000u)};
+            f16x2 s01, s23;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const bool fine = fabsf(b[i]) < __builtin_inff();
+                mine |= !fine;
+                const _Float16 v = fine ? (_Float16)__builtin_amdgcn_ldexpf(b[i], -ve) : (_Float16)0.0f;
+                if (i < 2) s01[i] = v;
+                else s23[i - 2] = v;
+            }
+            pairs(vw[g], o);      // o[t]: the two elements of key t
+            const uint32_t e01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x05040100);
+            const uint32_t e23 = __builtin_amdgcn_perm(bits(o[3]), bits(o[2]), 0x05040100);
+            const uint32_t o01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x07060302);
+            const uint32_t o23 = __builtin_amdgcn_perm(bits(o[3]), bits(o[2]), 0x07060302);
+            const u32x4 v = {bits(halves(e01) * s01), bits(halves(e23) * s23), bits(halves(o01) * s01), bits(halves(o23) * s23)};
+            *(u32x4*)&vt[stage][run4 * DP + 32 * g + 2 * a16] = v;
+        }
+        if (mine) odd = 1;
+    };
+
+    if (tid == 0) odd = 0;
+    int ke = 0, ve = -127;
+    if (k0 < k1) {
+        load(k0, page_of(k0));
+        int next = page_of(k0 + KT);
+        put_peaks(0);
+        __syncthreads();
+        ke = peak(0, 0), ve = peak(0, 1);
+        decode(0, ke, ve);
+        if (k0 + KT < k1) load(k0 + KT, next), next = page_of(k0 + 2 * KT);
+        for (int j0 = k0, stage = 0; j0 < k1; j0 += KT, stage ^= 1) {
+            const bool more = j0 + KT < k1;
+            int ke_next = ke, ve_next = ve;
+            if (more) put_peaks(stage ^ 1);
+            __syncthreads();      // this tile is there; the next one's peaks are; no one reads the other stage any more
+            if (more) {
+                ke_next = peak(stage ^ 1, 0), ve_next = max(ve, peak(stage ^ 1, 1));
+                decode(stage ^ 1, ke_next, ve_next);
+                if (j0 + 2 * KT < k1) load(j0 + 2 * KT, next), next = page_of(j0 + 3 * KT);
+            }
+            if (j0 < wave_keys) {
+                const uint2* vs = vt[stage];
+                fl.scores(kt[stage], __builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), j0 + KT - 1 > wave_open,
+                          last - j0 - 4 * half);
+                fl.products([&](int r, int d) {
+                    const uint2 lo = vs[(r >> 2) * DP + 32 * d + col], hi = vs[((r >> 2) + 2) * DP + 32 * d + col];
+                    return __builtin_bit_cast(f16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+                });
+                if (ve_next > ve) {
+                    const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
+#pragma unroll
+                    for (int d = 0; d < DB; d++) fl.acc[d] *= f;
+                }
+            }
+            ke = ke_next, ve = ve_next;
+        }
+        __syncthreads();
+        if (odd) {
+            for (int j = k0; j < k1; j++) {
+                const int pid = table[j >> p.cache.shift];
+                if (pid < 0 || pid >= p.cache.pages) continue;
+                const int t = j & (page - 1);
+                const uint8_t* vs = p.cache.block(pid, h) + p.cache.value_scales_at() + p.cache.scale_run(t) + (t & 3) * 2;
+#pragma unroll
+                for (int d = 0; d < DB; d++) {
+                    const uint32_t b = *(const uint16_t*)(vs + 8 * min(d, C - 1));
+                    if ((b & 0x7f80) == 0x7f80 && j <= last) fl.acc[d] = f32x16{} + __builtin_nanf("");
+                }
+            }
+        }
+    }
+
+    const float sum = fl.sum + other_half(fl.sum);
+    if (!live) return;
+    const int64_t to = (token * p.q.heads + head) * chunks + chunk;
+    const float f = chunks > 1 ? 1.0f : last >= 0 ? 1.0f / sum : 0.0f;       // no key: zeros
+    if (chunks > 1 && half == 0) stats[to] = make_float2(fl.top, sum);
+    T* o = (T*)p.o.p + token * p.o.token + head * p.o.head;
+#pragma unroll
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int e = 32 * d + 8 * k + 4 * half;
+            if (e >= p.d) continue;
+            f32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = __builtin_amdgcn_ldexpf(fl.acc[d][4 * k + i] * f, ve);
+            if (chunks > 1) {
+                *(f32x4*)(part + to * p.d + e) = w;
+            } else {
+                if (rw.bad) w = f32x4{0, 0, 0, 0} + __builtin_nanf("");
+                typedef T t4 __attribute__((ext_vector_type(4)));
+                ((Loose<t4, T>*)(o + e))->v = __builtin_convertvector(w, t4);
+            }
+        }
+}
+
+template <typename T>
+hipError_t launch_t(const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats, hipStream_t s) {
+    const unsigned grid = (unsigned)(sp.slots * p.cache.heads * sp.chunks);
+    if (p.d <= 64) k_kv4_many<T, 64><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    else if (p.d <= 128) k_kv4_many<T, 128><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    else k_kv4_many<T, 256><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_many(int type, const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats,
+                           hipStream_t s) {
+    return type == kBF16 ? launch_t<__bf16>(p, sp, part, stats, s) : launch_t<_Float16>(p, sp, part, stats, s);
+}
+
+}  // namespace esb

@@ -52,7 +52,8 @@ def codes(y):
 
 def attend(q, k, v, last, scale):
     """One sequence in 64 bits: q [n, heads, d], k, v [m, kv heads, d], row i sees keys up to last[i].
-    Returns (o, size, score): size = sum p |v| / sum p, score = the largest scale sum |q k| of a row."""
+    Returns (o, size, score, mass): size = sum p |v| / sum p, score = the largest scale sum |q k| of a row,
+    mass = sum |v| over the keys that a row sees."""
     n, heads, d = q.shape
     m, kv = k.shape[:2]
     q = q.double().reshape(n, kv, heads // kv, d).permute(1, 2, 0, 3).reshape(kv, -1, d)
@@ -71,15 +72,17 @@ def attend(q, k, v, last, scale):
 
     o = torch.where(none, 0.0, torch.matmul(p, v) / total)
     s = torch.where(none, 0.0, torch.matmul(p, v.abs()) / total)
-    return back(o), back(s), back(size[..., None])
+    return back(o), back(s), back(size[..., None]), back(torch.matmul(sees.double(), v.abs()))
 
 
-def check(got, o, size, score, keys, d, p_round):
+def check(got, o, size, score, mass, keys, d, p_round, p_step=0.0):
     """fp32 scores of d products (error at most (d + 4) u of their magnitudes' sum, and twice that of a
     term's weight, since the maximum moves too), sums of `keys` terms, one rounding of each weighted
-    probability to p_round, one of the output."""
+    probability to p_round, one of the output.  Probabilities whose type has a smallest step are off by half
+    of it too, p_step, where the largest is 1 or more (and so is their sum)."""
     rel = p_round + 2 * (d + 4) * U * score + (keys + 8) * U
     u, step = ROUND[got.dtype], STEP[got.dtype]
     off = (got.double() - o).abs()
-    allowed = rel * size + u * (o.abs() + rel * size) + step
+    work = rel * size + p_step * mass
+    allowed = work + u * (o.abs() + work) + step
     assert bool((off <= allowed).all()), float((off / allowed.clamp(min=1e-300)).nan_to_num(nan=1e30).max())

@@ -35,9 +35,8 @@ def verify(q, k, v, out, nq, nk, causal, scale=None):
         if n:
             last = torch.arange(n) + m - n if causal else torch.full((n,), m - 1)
             want = ref.attend(q[a:a + n], k[b:b + m], v[b:b + m], last, d ** -0.5 if scale is None else scale)
-            # fp16 probabilities below its normal numbers are off by 2^-25 of the largest
-            tiny = m * 2.0 ** -25 if q.dtype == torch.float16 else 0.0
-            ref.check(out[a:a + n], *want, keys=m, d=d, p_round=ref.ROUND[q.dtype] + tiny)
+            ref.check(out[a:a + n], *want, keys=m, d=d, p_round=ref.ROUND[q.dtype],
+                      p_step=2.0 ** -25 if q.dtype == torch.float16 else 0.0)
             if causal:
                 assert not bool(out[a:a + max(0, min(n, n - m))].any())
         a, b = a + n, b + m

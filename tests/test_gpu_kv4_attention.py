@@ -1,7 +1,9 @@
 """esb_kv4_attention against its definition in 64 bits on the cache's own values.
 
 Tolerances: attention_ref.check, from the roundings that the operator makes: fp32 scores and sums,
-p alpha in bf16 (2^-8) for bf16 outputs and in two bf16 (2^-17) for fp16, one rounding of the output."""
+p alpha in bf16 (2^-8) for bf16 outputs and in two bf16 (2^-17) for fp16, one rounding of the output.  With
+more than 64 rows a sequence on average (queries x heads of a group) the probabilities are rounded to fp16
+instead: 2^-11, and at least 2^-25."""
 import pytest
 import torch
 
@@ -60,13 +62,15 @@ def queries(seed, tokens, heads, d, dtype, size=0.6):
 
 def verify(c, q, out, counts, scale=None, skip=()):
     at = 0
+    many = -(-sum(counts) // len(counts)) * (q.shape[1] // c.heads) > 64
     for i, n in enumerate(counts):
         if i not in skip and n:
             k, v = c.read(i)
             m = k.shape[0]
             last = torch.arange(n) + m - n
             want = ref.attend(q[at:at + n], k, v, last, c.d ** -0.5 if scale is None else scale)
-            ref.check(out[at:at + n], *want, keys=m, d=c.d, p_round=P_ROUND[q.dtype])
+            p_round = 2.0 ** -11 if many else P_ROUND[q.dtype]
+            ref.check(out[at:at + n], *want, keys=m, d=c.d, p_round=p_round, p_step=2.0 ** -25 if many else 0.0)
             for t in range(min(n, max(0, n - m))):
                 assert not bool(out[at + t].any())
         at += n
@@ -108,7 +112,7 @@ def test_long_contexts(esb, t, kv, group, d, page, length):
 @pytest.mark.parametrize("t", ["bf16", "f16"])
 @pytest.mark.parametrize("kv,group,d,page", [(1, 1, 64, 16), (2, 7, 64, 16), (2, 4, 128, 64), (1, 5, 96, 32), (1, 3, 256, 16)])
 @pytest.mark.parametrize("counts,lengths", [([1, 5, 0, 3], [1, 5, 7, 700]), ([2, 64, 17], [40, 64, 1000]),
-                                            ([200, 1, 0, 0, 33], [200, 2000, 0, 5, 34]),
+                                            ([200, 1, 0, 0, 33], [200, 2000, 0, 5, 34]), ([300, 129], [4000, 6001]),
                                             ([5, 9, 4], [3, 0, 4])])       # fewer keys than queries
 def test_several_tokens(esb, t, kv, group, d, page, counts, lengths):
     log("kv4 tokens=%s lengths=%s kv=%d group=%d d=%d %s" % (counts, lengths, kv, group, d, t))
@@ -163,32 +167,57 @@ def test_large_scales_in_fp16(esb):
     q = (queries(14, 1, 2, 64, torch.float16) * 1e-5).to(torch.float16)
     out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths)
     verify(c, q, out, [1])
+    # as a prompt, both types, queries far below and above 1
+    for dtype, size in ((torch.float16, 1e-5), (torch.bfloat16, 1e-30), (torch.bfloat16, 1e5)):
+        a = torch.full((50, 1, 2), 1e6 if size < 1 else 1e-4, device="cuda").to(torch.bfloat16)
+        a[7] = a[7] * 64
+        esb.esb_kv4_pack(c.cache, 16, k, a * (1e25 if size < 1e-20 else 1), k, va, c.slots[0])
+        q = (queries(15, 50, 4, 64, torch.float32) * size).to(dtype)
+        out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=torch.tensor([0, 50], dtype=torch.int32, device="cuda"))
+        verify(c, q, out, [50])
 
 
-def test_not_finite(esb):
+def test_value_scales_that_grow(esb):
+    """Value scales over many powers of two along the keys, as the prompt form brings them to one."""
+    n = 500
+    c = Cache(esb, 33, [n], 1, 128, 16)
+    g = torch.Generator(device="cuda").manual_seed(34)
+    codes = torch.randint(0, 16, (n, 1, 128), generator=g, device="cuda", dtype=torch.uint8)
+    q = queries(35, n, 4, 128, torch.bfloat16)
+    starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    for shift in (torch.arange(n) // 20 - 12, 12 - torch.arange(n) // 20, torch.zeros(n)):
+        a = (0.4 * 2.0 ** shift.cuda().double())[:, None, None].expand(n, 1, 4).to(torch.bfloat16).contiguous()
+        esb.esb_kv4_pack(c.cache, 16, codes, torch.full_like(a, 0.3), codes, a, c.slots[0])
+        out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts)
+        verify(c, q, out, [n])
+
+
+@pytest.mark.parametrize("group", [1, 2, 16])      # by how many rows share keys: each kernel
+@pytest.mark.parametrize("d", [64, 96, 256])
+def test_not_finite(esb, group, d):
     """NaN scales reach the queries that see them, and no others; NaN queries themselves only."""
     counts, lengths = [40, 1], [60, 30]
-    c = Cache(esb, 15, lengths, 1, 64, 16)
-    q = queries(16, 41, 2, 64, torch.bfloat16)
+    c = Cache(esb, 15, lengths, 1, d, 16)
+    q = queries(16, 41, group, d, torch.bfloat16)
     starts = torch.tensor([0, 40, 41], dtype=torch.int32, device="cuda")
     clean = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts)
     for which in (0, 1):
-        codes = torch.zeros(1, 1, 64, dtype=torch.uint8, device="cuda")
-        nan = torch.full((1, 1, 2), float("nan"), dtype=torch.bfloat16, device="cuda")
+        codes = torch.zeros(1, 1, d, dtype=torch.uint8, device="cuda")
+        nan = torch.full((1, 1, d // 32), float("nan"), dtype=torch.bfloat16, device="cuda")
         one = torch.ones_like(nan)
-        c = Cache(esb, 15, lengths, 1, 64, 16)
+        c = Cache(esb, 15, lengths, 1, d, 16)
         # key 45 of sequence 0 is seen by its queries 25 ..
         esb.esb_kv4_pack(c.cache, 16, codes, nan if which == 0 else one, codes, nan if which else one, c.slots[0][45:46])
         out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts)
         assert torch.equal(out[:25], clean[:25]) and torch.equal(out[40:], clean[40:])
         assert bool(torch.isnan(out[25:40]).all())
-    q[3, 1, 5] = float("nan")
+    q[3, group - 1, 5] = float("nan")
     q[40, 0, 0] = float("inf")
-    c = Cache(esb, 15, lengths, 1, 64, 16)
+    c = Cache(esb, 15, lengths, 1, d, 16)
     out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts)
-    assert bool(torch.isnan(out[3, 1]).all()) and bool(torch.isnan(out[40, 0]).all())
-    keep = torch.ones(41, 2, dtype=torch.bool)
-    keep[3, 1] = keep[40, 0] = False
+    assert bool(torch.isnan(out[3, group - 1]).all()) and bool(torch.isnan(out[40, 0]).all())
+    keep = torch.ones(41, group, dtype=torch.bool)
+    keep[3, group - 1] = keep[40, 0] = False
     assert torch.equal(out[keep], clean[keep])
 
 
