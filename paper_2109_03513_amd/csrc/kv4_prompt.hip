@@ -37,10 +37,21 @@ __device__ __forceinline__ int exponent(uint32_t b) {
     const int e = (b >> 7) & 0xff;
     return e == 0xff ? 0 : e;
 }
+template <int CTRL> __device__ __forceinline__ int turned(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+}
+// The value of lane k of four.
+__device__ __forceinline__ uint32_t of_four(uint32_t v, int k) {
+    return (uint32_t)(k == 0 ? turned<0x00>((int)v) : k == 1 ? turned<0x55>((int)v) : k == 2 ? turned<0xaa>((int)v) : turned<0xff>((int)v));
+}
+// The largest of a wave's values, in every lane.
 __device__ __forceinline__ int wave_max(int v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = max(v, __shfl_xor(v, o));
-    return v;
+    v = max(v, turned<0xb1>(v));       // lanes 1 0 3 2 of four
+    v = max(v, turned<0x4e>(v));       // lanes 2 3 0 1
+    v = max(v, turned<0x141>(v));      // eight lanes mirrored
+    v = max(v, turned<0x140>(v));      // sixteen
+    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+               max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
 template <typename T, int DP>
@@ -50,7 +61,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4Attentio
     constexpr int KT = 64, R = 128, P = DP / 8, CP = DP / 32, DB = DP / 32;
     typedef uint32_t W __attribute__((ext_vector_type(CP)));
     __shared__ f16x8 kt[2][KT * P];              // rows of keys, pieces turned
-    __shared__ uint2 vt[2][KT / 4 * DP];         // runs of four keys, of every element
+    __shared__ f16x8 vt[2][KT / 8 * DP];         // [16 keys][half][element]: keys 4 half .. + 3 and 8 + 4 half .. + 3
+    __shared__ _Float16 vscales[4][4][4 * CP];   // a wave's: [run][group][key of the run]
     __shared__ int peaks[2][4][2];               // by wave: largest exponents of the key and the value scales
     __shared__ int odd;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -105,51 +117,37 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4Attentio
     }
 
     // A thread's part of a tile: every group's word of key tid / 4, elements 8 (tid % 4) of a group on; and of the run of
-    // four values tid / 16 (of the same page), elements 2 (tid % 16) of a group on.
+    // four values tid / 16 (of the same page), elements 2 (tid % 16) of a group on.  Of the scales of this key it
+    // brings those of groups tid % 4 (and four further), of the run's those that lie tid % 16 (and 16 further) on.
+    constexpr int NS = CP == 8 ? 2 : 1;
     const int32_t* table = p.table + rw.seq * p.table_pitch;
     const int page = p.cache.page, key = tid >> 2, a4 = tid & 3, run4 = tid >> 4, a16 = tid & 15;
     W kw, vw;
-    uint32_t ka[CP];
-    uint2 va[CP];
+    uint32_t ka[NS], va[NS];
     auto page_of = [&](int j0) { return table[min(j0 + key, keys - 1) >> p.cache.shift]; };
     auto load = [&](int j0, int pid) {
         const bool bad = pid < 0 || pid >= p.cache.pages;
         const uint8_t* b = p.cache.block(bad ? 0 : pid, h);
         const int t = (j0 + key) & (page - 1);
         // words past the head's groups are of what follows in the block, and meet zeros of the query or make
-        // outputs that are not stored
+        // outputs that are not stored; their scales repeat others
         kw = ((const Loose<W, uint32_t>*)(b + t * 16 * C + a4 * 4 * C))->v;
         vw = ((const Loose<W, uint32_t>*)(b + p.cache.values_at() + (t >> 2) * 64 * C + a16 * 4 * C))->v;
-        const uint8_t* ks = b + p.cache.key_scales_at() + p.cache.scale_run(t) + (t & 3) * 2;
-        const uint8_t* vs = b + p.cache.value_scales_at() + p.cache.scale_run(t);
+        const uint16_t* ks = (const uint16_t*)(b + p.cache.key_scales_at() + p.cache.scale_run(t)) + (t & 3);
+        const uint16_t* vs = (const uint16_t*)(b + p.cache.value_scales_at() + p.cache.scale_run(t));
 #pragma unroll
-        for (int g = 0; g < CP; g++) {
-            const int at = 8 * min(g, C - 1);
-            ka[g] = *(const uint16_t*)(ks + at);
-            va[g] = *(const uint2*)(vs + at);
-        }
-        if (bad) {
-#pragma unroll
-            for (int g = 0; g < CP; g++) ka[g] = 0x7fc0;
-        }
-        if (j0 + KT > keys) {      // scales behind the last key may be anything
-            const int left = keys - j0 - 4 * run4;
-            const uint32_t x = left >= 2 ? ~0u : left == 1 ? 0xffffu : 0u, y = left >= 4 ? ~0u : left == 3 ? 0xffffu : 0u;
-#pragma unroll
-            for (int g = 0; g < CP; g++) {
-                if (j0 + key >= keys) ka[g] = 0;
-                va[g].x &= x, va[g].y &= y;
+        for (int u = 0; u < NS; u++) {
+            ka[u] = bad ? 0x7fc0u : ks[4 * min(a4 + 4 * u, C - 1)];
+            va[u] = vs[min(a16 + 16 * u, 4 * C - 1)];
+            if (j0 + KT > keys) {      // scales behind the last key may be anything
+                if (j0 + key >= keys) ka[u] = 0;
+                if (j0 + 4 * run4 + (min(a16 + 16 * u, 4 * C - 1) & 3) >= keys) va[u] = 0;
             }
         }
     };
     auto put_peaks = [&](int stage) {
-        int k = 0, v = 0;
-#pragma unroll
-        for (int g = 0; g < CP; g++) {
-            if (g % 4 == (CP >= 4 ? a4 : a4 % CP)) k = max(k, exponent(ka[g]));
-            if (g == a16 % CP)
-                v = max(max(exponent(va[g].x & 0xffff), exponent(va[g].x >> 16)), max(exponent(va[g].y & 0xffff), exponent(va[g].y >> 16)));
-        }
+        int k = exponent(ka[0]), v = exponent(va[0]);
+        if (NS == 2) k = max(k, exponent(ka[NS - 1])), v = max(v, exponent(va[NS - 1]));
         k = wave_max(k), v = wave_max(v);
         if (lane == 0) peaks[stage][wave][0] = k, peaks[stage][wave][1] = v;
     };
@@ -157,34 +155,36 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4Attentio
         return max(max(peaks[stage][0][what], peaks[stage][1][what]), max(peaks[stage][2][what], peaks[stage][3][what])) - 127;
     };
     auto decode = [&](int stage, int ke, int ve) {
-        bool mine = false;
+        uint32_t ks[NS];      // twice in one word
+#pragma unroll
+        for (int u = 0; u < NS; u++) {
+            const _Float16 k = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(ka[u]), -ke);
+            ks[u] = bits(f16x2{k, k});
+            const float v = bf16_value(va[u]);
+            const bool fine = fabsf(v) < __builtin_inff();
+            if (!fine) odd = 1;
+            if (CP >= 4 || a16 < 8) vscales[wave][run4 & 3][a16 + 16 * u] = fine ? (_Float16)__builtin_amdgcn_ldexpf(v, -ve) : (_Float16)0.0f;
+        }
+        __builtin_amdgcn_wave_barrier();      // LDS serves a wave in order
+        const uint2* vs = (const uint2*)vscales[wave][run4 & 3];
+        f16x8* vo = &vt[stage][((run4 >> 2) * 2 + (run4 & 1)) * DP + 2 * a16];
 #pragma unroll
         for (int g = 0; g < CP; g++) {
             f16x2 o[4];
-            const _Float16 s = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(ka[g]), -ke);
             pairs(kw[g], o);
+            const f16x2 s = halves(of_four(ks[g / 4], g % 4));
             const u32x4 k = {bits(o[0] * s), bits(o[1] * s), bits(o[2] * s), bits(o[3] * s)};
             kt[stage][key * P + ((4 * g + a4) ^ key_turn<DP>(key))] = __builtin_bit_cast(f16x8, k);
-            float b[4] = {bf16_value(va[g].x), __uint_as_float(va[g].x & 0xffff0000u), bf16_value(va[g].y),
-                          __uint_as_float(va[g].y & 0xffff0000u)};
-            f16x2 s01, s23;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const bool fine = fabsf(b[i]) < __builtin_inff();
-                mine |= !fine;
-                const _Float16 v = fine ? (_Float16)__builtin_amdgcn_ldexpf(b[i], -ve) : (_Float16)0.0f;
-                if (i < 2) s01[i] = v;
-                else s23[i - 2] = v;
-            }
+            const f16x2 s01 = halves(vs[g].x), s23 = halves(vs[g].y);
             pairs(vw[g], o);      // o[t]: the two elements of key t
             const uint32_t e01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x05040100);
             const uint32_t e23 = __builtin_amdgcn_perm(bits(o[3]), bits(o[2]), 0x05040100);
             const uint32_t o01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x07060302);
             const uint32_t o23 = __builtin_amdgcn_perm(bits(o[3]), bits(o[2]), 0x07060302);
-            const u32x4 v = {bits(halves(e01) * s01), bits(halves(e23) * s23), bits(halves(o01) * s01), bits(halves(o23) * s23)};
-            *(u32x4*)&vt[stage][run4 * DP + 32 * g + 2 * a16] = v;
+            ((uint2*)(vo + 32 * g))[run4 >> 1 & 1] = uint2{bits(halves(e01) * s01), bits(halves(e23) * s23)};
+            ((uint2*)(vo + 32 * g + 1))[run4 >> 1 & 1] = uint2{bits(halves(o01) * s01), bits(halves(o23) * s23)};
         }
-        if (mine) odd = 1;
+        __builtin_amdgcn_wave_barrier();
     };
 
     if (tid == 0) odd = 0;
@@ -208,13 +208,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4Attentio
                 if (j0 + 2 * KT < k1) load(j0 + 2 * KT, next), next = page_of(j0 + 3 * KT);
             }
             if (j0 < wave_keys) {
-                const uint2* vs = vt[stage];
+                const f16x8* vs = vt[stage];
                 fl.scores(kt[stage], __builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), j0 + KT - 1 > wave_open,
                           last - j0 - 4 * half);
-                fl.products([&](int r, int d) {
-                    const uint2 lo = vs[(r >> 2) * DP + 32 * d + col], hi = vs[((r >> 2) + 2) * DP + 32 * d + col];
-                    return __builtin_bit_cast(f16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
-                });
+                fl.products([&](int r, int d) { return vs[((r >> 4) * 2 + half) * DP + 32 * d + col]; });
                 if (ve_next > ve) {
                     const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
 #pragma unroll
