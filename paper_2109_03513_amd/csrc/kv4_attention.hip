@@ -659,8 +659,16 @@ __global__ __launch_bounds__(256) void k_join_few(Kv4AttentionParams p, int run,
     const int d = 32 * p.cache.groups, per = d / 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / per, token = row / p.q.heads;
     const int head = (int)(row % p.q.heads), e = 4 * (int)(id % per);
+    if (token >= p.tokens) return;
+    // every part that there may be is on its way before the row's keys are known
+    const float2* st = stats + row * chunks;
+    const float* pt = part + row * chunks * d + e;
+    float2 s[8];
+    f32x4 v[8];
+#pragma unroll
+    for (int c = 0; c < 8; c++)
+        if (c < chunks) s[c] = st[c], v[c] = *(const f32x4*)(pt + (int64_t)c * d);
     JoinRow jr;
-    jr.live = false;
     if (p.starts) {
         // the sequence of the workgroup's first token, then on from there
         const Tile t = find_sequence(p.starts, p.seqs, p.tokens, (int64_t)blockIdx.x * 256 / per / p.q.heads);
@@ -669,21 +677,16 @@ __global__ __launch_bounds__(256) void k_join_few(Kv4AttentionParams p, int run,
         if (seq < 0) return;
         const int64_t a = min(max((int64_t)p.starts[seq], (int64_t)0), p.tokens);
         const int64_t b = min(max((int64_t)p.starts[seq + 1], a), p.tokens);
-        if (token < p.tokens) jr = join_row(p, seq, a, b, token);
-    } else if (token < p.tokens) {
+        jr = join_row(p, seq, a, b, token);
+    } else {
         jr = join_row(p, (int)token, token, token + 1, token);
     }
     if (!jr.live) return;
-    const int used = min((jr.keys + run - 1) / run, 8);
-    const float2* st = stats + row * chunks;
-    const float* pt = part + row * chunks * d + e;
-    float2 s[8];
-    f32x4 v[8];
+    const int used = min((jr.keys + run - 1) / run, chunks);
     float m = kNegInf, l = 0.0f;
 #pragma unroll
     for (int c = 0; c < 8; c++) {
-        s[c] = make_float2(kNegInf, 0.0f), v[c] = f32x4{0, 0, 0, 0};
-        if (c < used) s[c] = st[c], v[c] = *(const f32x4*)(pt + (int64_t)c * d);
+        if (c >= used) s[c] = make_float2(kNegInf, 0.0f), v[c] = f32x4{0, 0, 0, 0};
         m = fmaxf(m, s[c].x);
     }
     f32x4 o = {0, 0, 0, 0};
@@ -705,13 +708,13 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
     const int64_t rows = starts ? (tokens + seqs - 1) / seqs * group : group;      // of a sequence, on average
     const int narrow = d <= 64 ? 8 : d <= 128 ? 4 : 2;      // rows of a tile whose columns are (row, group)
     s.kind = rows <= 2 * narrow ? kKv4Few : rows <= 64 ? kKv4Some : kKv4Many;
-    s.NT = rows <= (s.kind == kKv4Few ? narrow : 16) || (s.kind == kKv4Some && d > 128) ? 1 : 2;
-    const int R = s.kind == kKv4Many ? 128 : (s.kind == kKv4Few ? narrow : 16) * s.NT;
+    s.NT = rows <= (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 192) || (s.kind == kKv4Some && d > 128) ? 1 : 2;
+    const int R = (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 128) * s.NT;
     s.tiles = (group + R - 1) / R;
     s.slots = starts ? tokens * group / R + seqs : (int64_t)seqs * s.tiles;
     const int64_t base = s.slots * kv_heads;
-    // Few rows: parts of at least 384 keys, for twelve workgroups a CU.  Many: as many as run at once (two a CU).
-    int64_t n = s.kind == kKv4Many ? 2 * cus / base : (12 * cus + base - 1) / base;
+    // Few rows: parts of at least 384 keys, for twelve workgroups a CU.  Many: as many as run at once (256 rows a CU).
+    int64_t n = s.kind == kKv4Many ? 2 / s.NT * cus / base : (12 * cus + base - 1) / base;
     const int64_t most = (longest + 383) / 384;
     if (n > most) n = most;
     if (n < 1) n = 1;

@@ -54,11 +54,11 @@ __device__ __forceinline__ int wave_max(int v) {
                max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4AttentionParams p, int run, int chunks, int tiles,
-                                                                     float* part, float2* stats) {
+template <typename T, int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4AttentionParams p, int run, int chunks, int tiles,
+                                                                        float* part, float2* stats) {
     typedef typename Vec8<T>::type V;
-    constexpr int KT = 64, R = 128, P = DP / 8, CP = DP / 32, DB = DP / 32;
+    constexpr int KT = 64, R = 32 * WAVES, P = DP / 8, CP = DP / 32, DB = DP / 32;
     typedef uint32_t W __attribute__((ext_vector_type(CP)));
     __shared__ f16x8 kt[2][KT * P];              // rows of keys, pieces turned
     __shared__ f16x8 vt[2][KT / 8 * DP];         // [16 keys][half][element]: keys 4 half .. + 3 and 8 + 4 half .. + 3
@@ -116,67 +116,88 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4Attentio
         }
     }
 
-    // A thread's part of a tile: every group's word of key tid / 4, elements 8 (tid % 4) of a group on; and of the run of
-    // four values tid / 16 (of the same page), elements 2 (tid % 16) of a group on.  Of the scales of this key it
-    // brings those of groups tid % 4 (and four further), of the run's those that lie tid % 16 (and 16 further) on.
-    constexpr int NS = CP == 8 ? 2 : 1;
+    // A thread's part of a tile's keys: every group's word of key at / 4, elements 8 (at % 4) of a group on, and of this
+    // key's scales those of groups at % 4 (and four further).  Of its values: every group's word of the run of four
+    // at / 16 (of the same page), elements 2 (at % 16) of a group on, and of this run's scales those that lie
+    // at % 16 (and 16 further) on.  With eight waves four bring the keys, four the values.
+    constexpr int NS = CP == 8 ? 2 : 1, at_mask = 255;
+    struct Item {
+        W w;
+        uint32_t s[NS];
+    };
+    Item items[WAVES == 8 ? 1 : 2];
+    const int at = tid & at_mask, mine = WAVES == 8 ? wave >> 2 : 0;      // 1: values
     const int32_t* table = p.table + rw.seq * p.table_pitch;
-    const int page = p.cache.page, key = tid >> 2, a4 = tid & 3, run4 = tid >> 4, a16 = tid & 15;
-    W kw, vw;
-    uint32_t ka[NS], va[NS];
+    const int page = p.cache.page, key = at >> 2, a4 = at & 3, run4 = at >> 4, a16 = at & 15;
     auto page_of = [&](int j0) { return table[min(j0 + key, keys - 1) >> p.cache.shift]; };
-    auto load = [&](int j0, int pid) {
+    auto load_keys = [&](Item& x, int j0, int pid) {
         const bool bad = pid < 0 || pid >= p.cache.pages;
         const uint8_t* b = p.cache.block(bad ? 0 : pid, h);
         const int t = (j0 + key) & (page - 1);
         // words past the head's groups are of what follows in the block, and meet zeros of the query or make
         // outputs that are not stored; their scales repeat others
-        kw = ((const Loose<W, uint32_t>*)(b + t * 16 * C + a4 * 4 * C))->v;
-        vw = ((const Loose<W, uint32_t>*)(b + p.cache.values_at() + (t >> 2) * 64 * C + a16 * 4 * C))->v;
+        x.w = ((const Loose<W, uint32_t>*)(b + t * 16 * C + a4 * 4 * C))->v;
         const uint16_t* ks = (const uint16_t*)(b + p.cache.key_scales_at() + p.cache.scale_run(t)) + (t & 3);
+#pragma unroll
+        for (int u = 0; u < NS; u++) {
+            x.s[u] = bad ? 0x7fc0u : ks[4 * min(a4 + 4 * u, C - 1)];
+            if (j0 + key >= keys) x.s[u] = 0;      // scales behind the last key may be anything
+        }
+    };
+    auto load_values = [&](Item& x, int j0, int pid) {
+        const uint8_t* b = p.cache.block(pid < 0 || pid >= p.cache.pages ? 0 : pid, h);
+        const int t = (j0 + key) & (page - 1);
+        x.w = ((const Loose<W, uint32_t>*)(b + p.cache.values_at() + (t >> 2) * 64 * C + a16 * 4 * C))->v;
         const uint16_t* vs = (const uint16_t*)(b + p.cache.value_scales_at() + p.cache.scale_run(t));
 #pragma unroll
         for (int u = 0; u < NS; u++) {
-            ka[u] = bad ? 0x7fc0u : ks[4 * min(a4 + 4 * u, C - 1)];
-            va[u] = vs[min(a16 + 16 * u, 4 * C - 1)];
-            if (j0 + KT > keys) {      // scales behind the last key may be anything
-                if (j0 + key >= keys) ka[u] = 0;
-                if (j0 + 4 * run4 + (min(a16 + 16 * u, 4 * C - 1) & 3) >= keys) va[u] = 0;
-            }
+            const int n = min(a16 + 16 * u, 4 * C - 1);
+            x.s[u] = vs[n];
+            if (j0 + 4 * run4 + (n & 3) >= keys) x.s[u] = 0;
         }
     };
-    auto put_peaks = [&](int stage) {
-        int k = exponent(ka[0]), v = exponent(va[0]);
-        if (NS == 2) k = max(k, exponent(ka[NS - 1])), v = max(v, exponent(va[NS - 1]));
-        k = wave_max(k), v = wave_max(v);
-        if (lane == 0) peaks[stage][wave][0] = k, peaks[stage][wave][1] = v;
+    auto put_peak = [&](const Item& x, int stage, int what) {
+        int e = exponent(x.s[0]);
+        if (NS == 2) e = max(e, exponent(x.s[NS - 1]));
+        e = wave_max(e);
+        if (lane == 0) peaks[stage][wave & 3][what] = e;
     };
     auto peak = [&](int stage, int what) {
         return max(max(peaks[stage][0][what], peaks[stage][1][what]), max(peaks[stage][2][what], peaks[stage][3][what])) - 127;
     };
-    auto decode = [&](int stage, int ke, int ve) {
+    auto decode_keys = [&](const Item& x, int stage, int ke) {
         uint32_t ks[NS];      // twice in one word
 #pragma unroll
         for (int u = 0; u < NS; u++) {
-            const _Float16 k = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(ka[u]), -ke);
+            const _Float16 k = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(x.s[u]), -ke);
             ks[u] = bits(f16x2{k, k});
-            const float v = bf16_value(va[u]);
+        }
+#pragma unroll
+        for (int g = 0; g < CP; g++) {
+            f16x2 o[4];
+            pairs(x.w[g], o);
+            const f16x2 s = halves(of_four(ks[g / 4], g % 4));
+            const u32x4 k = {bits(o[0] * s), bits(o[1] * s), bits(o[2] * s), bits(o[3] * s)};
+            kt[stage][key * P + ((4 * g + a4) ^ key_turn<DP>(key))] = __builtin_bit_cast(f16x8, k);
+        }
+    };
+    auto decode_values = [&](const Item& x, int stage, int ve) {
+        _Float16* own = vscales[wave & 3][run4 & 3];
+#pragma unroll
+        for (int u = 0; u < NS; u++) {
+            const float v = bf16_value(x.s[u]);
             const bool fine = fabsf(v) < __builtin_inff();
             if (!fine) odd = 1;
-            if (CP >= 4 || a16 < 8) vscales[wave][run4 & 3][a16 + 16 * u] = fine ? (_Float16)__builtin_amdgcn_ldexpf(v, -ve) : (_Float16)0.0f;
+            if (CP >= 4 || a16 < 8) own[a16 + 16 * u] = fine ? (_Float16)__builtin_amdgcn_ldexpf(v, -ve) : (_Float16)0.0f;
         }
         __builtin_amdgcn_wave_barrier();      // LDS serves a wave in order
-        const uint2* vs = (const uint2*)vscales[wave][run4 & 3];
+        const uint2* vs = (const uint2*)own;
         f16x8* vo = &vt[stage][((run4 >> 2) * 2 + (run4 & 1)) * DP + 2 * a16];
 #pragma unroll
         for (int g = 0; g < CP; g++) {
             f16x2 o[4];
-            pairs(kw[g], o);
-            const f16x2 s = halves(of_four(ks[g / 4], g % 4));
-            const u32x4 k = {bits(o[0] * s), bits(o[1] * s), bits(o[2] * s), bits(o[3] * s)};
-            kt[stage][key * P + ((4 * g + a4) ^ key_turn<DP>(key))] = __builtin_bit_cast(f16x8, k);
             const f16x2 s01 = halves(vs[g].x), s23 = halves(vs[g].y);
-            pairs(vw[g], o);      // o[t]: the two elements of key t
+            pairs(x.w[g], o);      // o[t]: the two elements of key t
             const uint32_t e01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x05040100);
             const uint32_t e23 = __builtin_amdgcn_perm(bits(o[3]), bits(o[2]), 0x05040100);
             const uint32_t o01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x07060302);
@@ -185,6 +206,18 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4Attentio
             ((uint2*)(vo + 32 * g + 1))[run4 >> 1 & 1] = uint2{bits(halves(o01) * s01), bits(halves(o23) * s23)};
         }
         __builtin_amdgcn_wave_barrier();
+    };
+    auto load = [&](int j0, int pid) {
+        if (WAVES == 4 || !mine) load_keys(items[0], j0, pid);
+        if (WAVES == 4 || mine) load_values(items[WAVES == 8 ? 0 : 1], j0, pid);
+    };
+    auto put_peaks = [&](int stage) {
+        if (WAVES == 4 || !mine) put_peak(items[0], stage, 0);
+        if (WAVES == 4 || mine) put_peak(items[WAVES == 8 ? 0 : 1], stage, 1);
+    };
+    auto decode = [&](int stage, int ke, int ve) {
+        if (WAVES == 4 || !mine) decode_keys(items[0], stage, ke);
+        if (WAVES == 4 || mine) decode_values(items[WAVES == 8 ? 0 : 1], stage, ve);
     };
 
     if (tid == 0) odd = 0;
@@ -261,13 +294,19 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv4_many(Kv4Attentio
         }
 }
 
+template <typename T, int DP>
+hipError_t launch_d(const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats, hipStream_t s) {
+    const unsigned grid = (unsigned)(sp.slots * p.cache.heads * sp.chunks);
+    if (sp.NT == 1) k_kv4_many<T, DP, 4><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    else k_kv4_many<T, DP, 8><<<grid, 512, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_t(const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats, hipStream_t s) {
-    const unsigned grid = (unsigned)(sp.slots * p.cache.heads * sp.chunks);
-    if (p.d <= 64) k_kv4_many<T, 64><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-    else if (p.d <= 128) k_kv4_many<T, 128><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-    else k_kv4_many<T, 256><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-    return hipGetLastError();
+    if (p.d <= 64) return launch_d<T, 64>(p, sp, part, stats, s);
+    if (p.d <= 128) return launch_d<T, 128>(p, sp, part, stats, s);
+    return launch_d<T, 256>(p, sp, part, stats, s);
 }
 
 }  // namespace
