@@ -154,7 +154,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
             __syncthreads();
         }
         if (j0 >= wave_keys) continue;
-        fl.scores(kt, p.scale, j0 + KT - 1 > wave_open, last - j0 - 4 * half);
+        fl.scores(kt);
+        fl.weights(p.scale, j0 + KT - 1 > wave_open, last - j0 - 4 * half);
         fl.products([&](int r, int d) { return values(vt, r, d); });
     }
     if (keys > 0) __syncthreads();

@@ -43,8 +43,8 @@ template <typename T, int DP, int KT> struct Flash {
         top = kNegInf, sum = 0.0f;
     }
 
-    // Scores of a tile and what exp makes of them.  masks: keys after `end`, counted from 4 (lane / 32), are not seen.
-    __device__ __forceinline__ void scores(const V* kt, float scale, bool masks, int end) {
+    // Scores of a tile.
+    __device__ __forceinline__ void scores(const V* kt) {
         const int col = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
 #pragma unroll
         for (int b = 0; b < KB; b++) {
@@ -55,6 +55,10 @@ template <typename T, int DP, int KT> struct Flash {
                 x[b] = mma(kt[r * P + ((2 * s + half) ^ key_turn<DP>(r))], qf[s], x[b]);
             }
         }
+    }
+
+    // What exp makes of them.  masks: keys after `end`, counted from 4 (lane / 32), are not seen.
+    __device__ __forceinline__ void weights(float scale, bool masks, int end) {
         if (masks) {
 #pragma unroll
             for (int b = 0; b < KB; b++)

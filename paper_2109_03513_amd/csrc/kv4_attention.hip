@@ -708,13 +708,13 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
     const int64_t rows = starts ? (tokens + seqs - 1) / seqs * group : group;      // of a sequence, on average
     const int narrow = d <= 64 ? 8 : d <= 128 ? 4 : 2;      // rows of a tile whose columns are (row, group)
     s.kind = rows <= 2 * narrow ? kKv4Few : rows <= 64 ? kKv4Some : kKv4Many;
-    s.NT = rows <= (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 192) || (s.kind == kKv4Some && d > 128) ? 1 : 2;
+    s.NT = rows <= (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 192) || (s.kind != kKv4Few && d > 128) ? 1 : 2;
     const int R = (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 128) * s.NT;
     s.tiles = (group + R - 1) / R;
     s.slots = starts ? tokens * group / R + seqs : (int64_t)seqs * s.tiles;
     const int64_t base = s.slots * kv_heads;
     // Few rows: parts of at least 384 keys, for twelve workgroups a CU.  Many: as many as run at once (256 rows a CU).
-    int64_t n = s.kind == kKv4Many ? 2 / s.NT * cus / base : (12 * cus + base - 1) / base;
+    int64_t n = s.kind == kKv4Many ? (d > 128 ? 1 : 2 / s.NT) * cus / base : (12 * cus + base - 1) / base;
     const int64_t most = (longest + 383) / 384;
     if (n > most) n = most;
     if (n < 1) n = 1;

@@ -59,11 +59,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
                                                                         float* part, float2* stats) {
     typedef typename Vec8<T>::type V;
     constexpr int KT = 64, R = 32 * WAVES, P = DP / 8, CP = DP / 32, DB = DP / 32;
-    typedef uint32_t W __attribute__((ext_vector_type(CP)));
     __shared__ f16x8 kt[2][KT * P];              // rows of keys, pieces turned
     __shared__ f16x8 vt[2][KT / 8 * DP];         // [16 keys][half][element]: keys 4 half .. + 3 and 8 + 4 half .. + 3
-    __shared__ _Float16 vscales[4][4][4 * CP];   // a wave's: [run][group][key of the run]
-    __shared__ int peaks[2][4][2];               // by wave: largest exponents of the key and the value scales
+    __shared__ _Float16 vscales[WAVES][16 / WAVES][4 * CP];      // a wave's: [run][group][key of the run]
+    __shared__ int2 peaks[2][WAVES];             // by wave: largest exponents of the key and the value scales
     __shared__ int odd;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5, C = p.cache.groups;
@@ -82,7 +81,6 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
     const int row = rw.row0 + 32 * wave + col;
     const bool live = row < rw.rows;
     const int last = last_of(row), wave_open = last_of(rw.row0 + 32 * wave);
-    const int wave_keys = rw.row0 + 32 * wave < rw.rows ? last_of(min(rw.row0 + 32 * wave + 32, rw.rows) - 1) + 1 : 0;
     const int head = h * p.group + row % p.group;
     const int64_t token = rw.begin + row / p.group;
 
@@ -116,108 +114,103 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
         }
     }
 
-    // A thread's part of a tile's keys: every group's word of key at / 4, elements 8 (at % 4) of a group on, and of this
-    // key's scales those of groups at % 4 (and four further).  Of its values: every group's word of the run of four
-    // at / 16 (of the same page), elements 2 (at % 16) of a group on, and of this run's scales those that lie
-    // at % 16 (and 16 further) on.  With eight waves four bring the keys, four the values.
-    constexpr int NS = CP == 8 ? 2 : 1, at_mask = 255;
-    struct Item {
-        W w;
-        uint32_t s[NS];
-    };
-    Item items[WAVES == 8 ? 1 : 2];
-    const int at = tid & at_mask, mine = WAVES == 8 ? wave >> 2 : 0;      // 1: values
+    // A thread's part of a tile: the words of CT groups (all, or with eight waves half of them) of one key, elements
+    // 8 a4 of a group on; and of a run of four values (of the same page), elements 2 a16 of a group on.  Of the scales it
+    // brings one of its key's (two for CT = 8), those of its groups by a4, and those of its run that lie a16 (and 16
+    // further) on; the others' come from its neighbours.
+    constexpr int H = WAVES / 4, CT = CP / H, NK = CT == 8 ? 2 : 1, NV = CP == 8 ? 2 : 1;
+    typedef uint32_t WT __attribute__((ext_vector_type(CT)));
+    const int key = tid / (4 * H), a4 = tid & 3, run4 = tid / (16 * H), a16 = tid & 15;
+    const int gk = H == 2 ? CT * (tid >> 2 & 1) : 0, gv = H == 2 ? CT * (tid >> 4 & 1) : 0;      // first groups
     const int32_t* table = p.table + rw.seq * p.table_pitch;
-    const int page = p.cache.page, key = at >> 2, a4 = at & 3, run4 = at >> 4, a16 = at & 15;
+    const int page = p.cache.page;
+    WT kw, vw;
+    uint32_t ka[NK], va[NV];
     auto page_of = [&](int j0) { return table[min(j0 + key, keys - 1) >> p.cache.shift]; };
-    auto load_keys = [&](Item& x, int j0, int pid) {
+    auto load = [&](int j0, int pid) {
         const bool bad = pid < 0 || pid >= p.cache.pages;
         const uint8_t* b = p.cache.block(bad ? 0 : pid, h);
         const int t = (j0 + key) & (page - 1);
         // words past the head's groups are of what follows in the block, and meet zeros of the query or make
         // outputs that are not stored; their scales repeat others
-        x.w = ((const Loose<W, uint32_t>*)(b + t * 16 * C + a4 * 4 * C))->v;
+        kw = ((const Loose<WT, uint32_t>*)(b + t * 16 * C + a4 * 4 * C + 4 * gk))->v;
+        vw = ((const Loose<WT, uint32_t>*)(b + p.cache.values_at() + (t >> 2) * 64 * C + a16 * 4 * C + 4 * gv))->v;
         const uint16_t* ks = (const uint16_t*)(b + p.cache.key_scales_at() + p.cache.scale_run(t)) + (t & 3);
-#pragma unroll
-        for (int u = 0; u < NS; u++) {
-            x.s[u] = bad ? 0x7fc0u : ks[4 * min(a4 + 4 * u, C - 1)];
-            if (j0 + key >= keys) x.s[u] = 0;      // scales behind the last key may be anything
-        }
-    };
-    auto load_values = [&](Item& x, int j0, int pid) {
-        const uint8_t* b = p.cache.block(pid < 0 || pid >= p.cache.pages ? 0 : pid, h);
-        const int t = (j0 + key) & (page - 1);
-        x.w = ((const Loose<W, uint32_t>*)(b + p.cache.values_at() + (t >> 2) * 64 * C + a16 * 4 * C))->v;
         const uint16_t* vs = (const uint16_t*)(b + p.cache.value_scales_at() + p.cache.scale_run(t));
 #pragma unroll
-        for (int u = 0; u < NS; u++) {
+        for (int u = 0; u < NK; u++) {
+            ka[u] = ks[4 * min(gk + a4 % CT + 4 * u, C - 1)];
+            if (bad) ka[u] = 0x7fc0u;
+            if (j0 + key >= keys) ka[u] = 0;      // scales behind the last key may be anything
+        }
+#pragma unroll
+        for (int u = 0; u < NV; u++) {
             const int n = min(a16 + 16 * u, 4 * C - 1);
-            x.s[u] = vs[n];
-            if (j0 + 4 * run4 + (n & 3) >= keys) x.s[u] = 0;
+            va[u] = vs[n];
+            if (j0 + 4 * run4 + (n & 3) >= keys) va[u] = 0;
         }
     };
-    auto put_peak = [&](const Item& x, int stage, int what) {
-        int e = exponent(x.s[0]);
-        if (NS == 2) e = max(e, exponent(x.s[NS - 1]));
-        e = wave_max(e);
-        if (lane == 0) peaks[stage][wave & 3][what] = e;
+    auto put_peaks = [&](int stage) {
+        int k = exponent(ka[0]), v = exponent(va[0]);
+        if (NK == 2) k = max(k, exponent(ka[NK - 1]));
+        if (NV == 2) v = max(v, exponent(va[NV - 1]));
+        k = wave_max(k), v = wave_max(v);
+        if (lane == 0) peaks[stage][wave] = make_int2(k, v);
     };
-    auto peak = [&](int stage, int what) {
-        return max(max(peaks[stage][0][what], peaks[stage][1][what]), max(peaks[stage][2][what], peaks[stage][3][what])) - 127;
+    auto peak = [&](int stage) {
+        int2 m = peaks[stage][0];
+#pragma unroll
+        for (int w = 1; w < WAVES; w++) m.x = max(m.x, peaks[stage][w].x), m.y = max(m.y, peaks[stage][w].y);
+        return make_int2(m.x - 127, m.y - 127);
     };
-    auto decode_keys = [&](const Item& x, int stage, int ke) {
-        uint32_t ks[NS];      // twice in one word
+    // The tile that was brought, as fp16 under the two exponents: share() first, then decoded() in registers, then put()
+    // into LDS, so that the arithmetic may run beside products of the other stage.
+    uint32_t ks[NK];      // key scales, twice in one word
+    uint2 vs4[CT];        // value scales of the run
+    u32x4 kd[CT], vd[CT];
+    auto share = [&](int ke, int ve) {
+        _Float16* own = vscales[wave][run4 & (4 / H - 1)];
 #pragma unroll
-        for (int u = 0; u < NS; u++) {
-            const _Float16 k = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(x.s[u]), -ke);
-            ks[u] = bits(f16x2{k, k});
-        }
-#pragma unroll
-        for (int g = 0; g < CP; g++) {
-            f16x2 o[4];
-            pairs(x.w[g], o);
-            const f16x2 s = halves(of_four(ks[g / 4], g % 4));
-            const u32x4 k = {bits(o[0] * s), bits(o[1] * s), bits(o[2] * s), bits(o[3] * s)};
-            kt[stage][key * P + ((4 * g + a4) ^ key_turn<DP>(key))] = __builtin_bit_cast(f16x8, k);
-        }
-    };
-    auto decode_values = [&](const Item& x, int stage, int ve) {
-        _Float16* own = vscales[wave & 3][run4 & 3];
-#pragma unroll
-        for (int u = 0; u < NS; u++) {
-            const float v = bf16_value(x.s[u]);
+        for (int u = 0; u < NV; u++) {
+            const float v = bf16_value(va[u]);
             const bool fine = fabsf(v) < __builtin_inff();
             if (!fine) odd = 1;
             if (CP >= 4 || a16 < 8) own[a16 + 16 * u] = fine ? (_Float16)__builtin_amdgcn_ldexpf(v, -ve) : (_Float16)0.0f;
         }
-        __builtin_amdgcn_wave_barrier();      // LDS serves a wave in order
-        const uint2* vs = (const uint2*)own;
-        f16x8* vo = &vt[stage][((run4 >> 2) * 2 + (run4 & 1)) * DP + 2 * a16];
 #pragma unroll
-        for (int g = 0; g < CP; g++) {
+        for (int u = 0; u < NK; u++) {
+            const _Float16 k = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(ka[u]), -ke);
+            ks[u] = bits(f16x2{k, k});
+        }
+        __builtin_amdgcn_wave_barrier();      // LDS serves a wave in order
+#pragma unroll
+        for (int g = 0; g < CT; g++) vs4[g] = ((const uint2*)own)[gv + g];
+        __builtin_amdgcn_wave_barrier();
+    };
+    auto decoded = [&]() {
+#pragma unroll
+        for (int g = 0; g < CT; g++) {
             f16x2 o[4];
-            const f16x2 s01 = halves(vs[g].x), s23 = halves(vs[g].y);
-            pairs(x.w[g], o);      // o[t]: the two elements of key t
+            pairs(kw[g], o);
+            const f16x2 s = halves(of_four(ks[g / 4], g % 4));
+            kd[g] = u32x4{bits(o[0] * s), bits(o[1] * s), bits(o[2] * s), bits(o[3] * s)};
+            const f16x2 s01 = halves(vs4[g].x), s23 = halves(vs4[g].y);
+            pairs(vw[g], o);      // o[t]: the two elements of key t
             const uint32_t e01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x05040100);
             const uint32_t e23 = __builtin_amdgcn_perm(bits(o[3]), bits(o[2]), 0x05040100);
             const uint32_t o01 = __builtin_amdgcn_perm(bits(o[1]), bits(o[0]), 0x07060302);
             const uint32_t o23 = __builtin_amdgcn_perm(bits(o[3]), bits(o[2]), 0x07060302);
-            ((uint2*)(vo + 32 * g))[run4 >> 1 & 1] = uint2{bits(halves(e01) * s01), bits(halves(e23) * s23)};
-            ((uint2*)(vo + 32 * g + 1))[run4 >> 1 & 1] = uint2{bits(halves(o01) * s01), bits(halves(o23) * s23)};
+            vd[g] = u32x4{bits(halves(e01) * s01), bits(halves(e23) * s23), bits(halves(o01) * s01), bits(halves(o23) * s23)};
         }
-        __builtin_amdgcn_wave_barrier();
     };
-    auto load = [&](int j0, int pid) {
-        if (WAVES == 4 || !mine) load_keys(items[0], j0, pid);
-        if (WAVES == 4 || mine) load_values(items[WAVES == 8 ? 0 : 1], j0, pid);
-    };
-    auto put_peaks = [&](int stage) {
-        if (WAVES == 4 || !mine) put_peak(items[0], stage, 0);
-        if (WAVES == 4 || mine) put_peak(items[WAVES == 8 ? 0 : 1], stage, 1);
-    };
-    auto decode = [&](int stage, int ke, int ve) {
-        if (WAVES == 4 || !mine) decode_keys(items[0], stage, ke);
-        if (WAVES == 4 || mine) decode_values(items[WAVES == 8 ? 0 : 1], stage, ve);
+    auto put = [&](int stage) {
+        uint2* vo = (uint2*)&vt[stage][((run4 >> 2) * 2 + (run4 & 1)) * DP + 32 * gv + 2 * a16] + (run4 >> 1 & 1);
+#pragma unroll
+        for (int g = 0; g < CT; g++) {
+            kt[stage][key * P + ((4 * (gk + g) + a4) ^ key_turn<DP>(key))] = __builtin_bit_cast(f16x8, kd[g]);
+            vo[64 * g] = uint2{vd[g][0], vd[g][1]};
+            vo[64 * g + 2] = uint2{vd[g][2], vd[g][3]};
+        }
     };
 
     if (tid == 0) odd = 0;
@@ -227,29 +220,34 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
         int next = page_of(k0 + KT);
         put_peaks(0);
         __syncthreads();
-        ke = peak(0, 0), ve = peak(0, 1);
-        decode(0, ke, ve);
-        if (k0 + KT < k1) load(k0 + KT, next), next = page_of(k0 + 2 * KT);
+        ke = peak(0).x, ve = peak(0).y;
+        share(ke, ve);
+        decoded();
+        put(0);
+        load(k0 + KT, next), next = page_of(k0 + 2 * KT);
+        // Past the last tile the same goes on with its last key's page, under scales of zero.
         for (int j0 = k0, stage = 0; j0 < k1; j0 += KT, stage ^= 1) {
-            const bool more = j0 + KT < k1;
-            int ke_next = ke, ve_next = ve;
-            if (more) put_peaks(stage ^ 1);
+            put_peaks(stage ^ 1);
             __syncthreads();      // this tile is there; the next one's peaks are; no one reads the other stage any more
-            if (more) {
-                ke_next = peak(stage ^ 1, 0), ve_next = max(ve, peak(stage ^ 1, 1));
-                decode(stage ^ 1, ke_next, ve_next);
-                if (j0 + 2 * KT < k1) load(j0 + 2 * KT, next), next = page_of(j0 + 3 * KT);
-            }
-            if (j0 < wave_keys) {
-                const f16x8* vs = vt[stage];
-                fl.scores(kt[stage], __builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), j0 + KT - 1 > wave_open,
-                          last - j0 - 4 * half);
-                fl.products([&](int r, int d) { return vs[((r >> 4) * 2 + half) * DP + 32 * d + col]; });
-                if (ve_next > ve) {
-                    const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
+            const int ke_next = peak(stage ^ 1).x, ve_next = max(ve, peak(stage ^ 1).y);
+            share(ke_next, ve_next);
+            fl.scores(kt[stage]);
+            decoded();
 #pragma unroll
-                    for (int d = 0; d < DB; d++) fl.acc[d] *= f;
-                }
+            for (int i = 0; i < DP / 8; i++) {      // between the MFMAs
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                     // LDS read
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                     // MFMA
+                __builtin_amdgcn_sched_group_barrier(0x002, H == 2 ? 4 : 7, 0);        // VALU
+            }
+            put(stage ^ 1);
+            load(j0 + 2 * KT, next), next = page_of(j0 + 3 * KT);
+            const f16x8* vs = vt[stage];
+            fl.weights(__builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), j0 + KT - 1 > wave_open, last - j0 - 4 * half);
+            fl.products([&](int r, int d) { return vs[((r >> 4) * 2 + half) * DP + 32 * d + col]; });
+            if (ve_next > ve) {
+                const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
+#pragma unroll
+                for (int d = 0; d < DB; d++) fl.acc[d] *= f;
             }
             ke = ke_next, ve = ve_next;
         }
@@ -297,8 +295,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
 template <typename T, int DP>
 hipError_t launch_d(const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats, hipStream_t s) {
     const unsigned grid = (unsigned)(sp.slots * p.cache.heads * sp.chunks);
+    // long heads: eight waves a CU would not fit the registers
+    constexpr int most = DP == 256 ? 4 : 8;
     if (sp.NT == 1) k_kv4_many<T, DP, 4><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-    else k_kv4_many<T, DP, 8><<<grid, 512, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+    else k_kv4_many<T, DP, most><<<grid, 64 * most, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
     return hipGetLastError();
 }
 
