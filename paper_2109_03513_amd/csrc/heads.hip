@@ -6,9 +6,10 @@
 //  * keys (normed and rotated so) and values into the 4-bit cache, with alpha = bf16(max|y| / 6) per
 //    32 elements and the nearest of the eight magnitudes to |y| / alpha, ties to the larger.
 //
-// A head has d / 8 lanes (8, 16, 32 or 64 by d), eight elements each; the partners of a rotation are
-// read from the head again, which its cache lines still hold, so nothing crosses lanes but
-// the sum of squares and the group's maximum.
+// A head has 4 to 64 lanes of a wave, each with sixteen elements: eight pairs of the rotation, or sixteen that stay.  So
+// no pair crosses lanes, and heads may be rotated in place; only the sum of squares does, and for
+// the cache a key's elements go through LDS once, into lanes of half a group.  A wave goes over heads of one
+// token, whose cosines and sines it keeps.
 //
 // Keys for the cache are computed in fp64 and rounded once to fp32 before they get their codes: the
 // same call gives the same codes wherever the borders lie.  esb_rope computes in fp32 around an fp64
@@ -23,9 +24,6 @@ constexpr float kTiny = 0x1p-126f;
 
 __device__ __forceinline__ float bf16_value(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
-__device__ __forceinline__ float root(float x) { return sqrtf(x); }
-__device__ __forceinline__ double root(double x) { return sqrt(x); }
-
 // Where elements e .. e + 7 of a token of a block are.
 __device__ __forceinline__ uint32_t* key_word(const Kv4Layout& L, uint8_t* b, int t, int e) {
     return (uint32_t*)(b + (int64_t)t * 16 * L.groups + ((e >> 3) & 3) * 4 * L.groups + (e >> 5) * 4);
@@ -39,9 +37,9 @@ __device__ __forceinline__ uint16_t* scale_at(const Kv4Layout& L, uint8_t* b, in
     return (uint16_t*)(b + region + L.scale_run(t) + g * 8 + (t & 3) * 2);
 }
 
-// Eight nibbles (and, by the first lane of four, the group's scale) of one token into its block.
+// Eight nibbles of one token into its block.
 template <bool KEY>
-__device__ __forceinline__ void store_codes(const Kv4Layout& L, uint8_t* b, int t, int e, uint32_t w, uint16_t alpha) {
+__device__ __forceinline__ void store_codes(const Kv4Layout& L, uint8_t* b, int t, int e, uint32_t w) {
     if (KEY) {
         *key_word(L, b, t, e) = w;
     } else {
@@ -49,23 +47,10 @@ __device__ __forceinline__ void store_codes(const Kv4Layout& L, uint8_t* b, int 
 #pragma unroll
         for (int i = 0; i < 4; i++) o[i * 4 * L.groups] = (uint8_t)(w >> (8 * i));
     }
-    if ((e & 31) == 0) *scale_at(L, b, KEY ? L.key_scales_at() : L.value_scales_at(), t, e >> 5) = alpha;
 }
 
-// Codes of eight elements of a group that four neighbouring lanes share.
-struct Codes {
-    uint32_t nibbles;
-    uint16_t alpha;
-};
-__device__ __forceinline__ Codes quantize(f32x8 y) {
-    uint32_t m = 0;      // max |y| on bit patterns: a NaN is above every number
-#pragma unroll
-    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(y[i]) & 0x7fffffffu);
-    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-    if (m >= 0x7f800000u) return {0, 0x7fc0};
-    const __bf16 a16 = (__bf16)fmaxf(__uint_as_float(m) / 6.0f, kTiny);
-    const float a = (float)a16;
+// Codes of eight elements y under the scale a.
+__device__ __forceinline__ uint32_t nibbles(f32x8 y, float a) {
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -75,7 +60,30 @@ __device__ __forceinline__ Codes quantize(f32x8 y) {
                            (v >= 2.5f * a) + (v >= 3.5f * a) + (v >= 5.0f * a);
         w |= (c | (y[i] < 0.0f && c ? 8u : 0u)) << (4 * i);
     }
-    return {w, __builtin_bit_cast(uint16_t, a16)};
+    return w;
+}
+// max |y| on bit patterns: a NaN is above every number.
+__device__ __forceinline__ uint32_t magnitude(f32x8 y) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(y[i]) & 0x7fffffffu);
+    return m;
+}
+// Codes and scale of sixteen elements from e on, half a group, whose other half a neighbouring lane has.
+template <bool KEY>
+__device__ __forceinline__ void store_half_group(const Kv4Layout& L, bool there, int64_t slot, int h, int e, f32x8 lo, f32x8 hi) {
+    uint32_t m = max(magnitude(lo), magnitude(hi));
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true));      // lanes 1 0 3 2 of four
+    const bool fine = m < 0x7f800000u;
+    const __bf16 a16 = (__bf16)fmaxf(__uint_as_float(m) / 6.0f, kTiny);
+    const float a = (float)a16;
+    if (!there) return;
+    uint8_t* b = L.block(slot >> L.shift, h);
+    const int t = (int)slot & (L.page - 1);
+    store_codes<KEY>(L, b, t, e, fine ? nibbles(lo, a) : 0u);
+    store_codes<KEY>(L, b, t, e + 8, fine ? nibbles(hi, a) : 0u);
+    if ((e & 31) == 0)
+        *scale_at(L, b, KEY ? L.key_scales_at() : L.value_scales_at(), t, e >> 5) = fine ? __builtin_bit_cast(uint16_t, a16) : (uint16_t)0x7fc0;
 }
 
 template <typename T>
@@ -83,88 +91,166 @@ __device__ __forceinline__ const T* head_at(const HeadsView& v, int64_t t, int h
     return (const T*)v.p + t * v.token + h * v.head;
 }
 
+template <int CTRL> __device__ __forceinline__ double turned(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// The sum over LPR neighbouring lanes, in each of them.
+template <int LPR> __device__ __forceinline__ double lanes_sum(double v) {
+    v += turned<0xb1>(v);                       // lanes 1 0 3 2 of four
+    v += turned<0x4e>(v);                       // lanes 2 3 0 1
+    if (LPR >= 8) v += turned<0x141>(v);        // eight lanes mirrored
+    if (LPR >= 16) v += turned<0x140>(v);       // sixteen
+    if (LPR >= 32) v += __shfl_xor(v, 16);
+    if (LPR >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// v in the precision of the work.  For fp64 anew wherever it is used: kept over a wave's steps, the wider copies
+// of weights and table would cost it half its registers.
+template <typename A> __device__ __forceinline__ A wide(float v) {
+    if (sizeof(A) == 8) asm volatile("" : "+v"(v));
+    return (A)v;
+}
+
+// Iterations of a wave: 64 / LPR heads of one kind (queries, keys, values) at a time, q_steps + k_steps + v_steps for a
+// token; a wave takes `per` of them in turn.
 template <typename T, typename A, int LPR, bool CACHE>
-__global__ __launch_bounds__(256) void k_heads(HeadsParams p, int64_t token0, uint32_t rows) {
-    typedef A a8 __attribute__((ext_vector_type(8)));
+__global__ __launch_bounds__(256) void k_heads(HeadsParams p, int64_t token0, uint32_t waves, int per) {
     typedef typename Vec8<T>::type V;
-    const uint32_t row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    if (row >= rows) return;
-    const uint32_t nq = p.q.heads, nk = p.k.heads, all = nq + nk + (CACHE ? p.v.heads : 0);
-    const int64_t t = token0 + row / all;
-    int h = row % all;
-    const int kind = h < (int)nq ? 0 : h < (int)(nq + nk) ? 1 : 2;
-    h -= kind == 0 ? 0 : kind == 1 ? nq : nq + nk;
-    const T* x = head_at<T>(kind == 0 ? p.q : kind == 1 ? p.k : p.v, t, h);
-    const int d = p.d, e = 8 * (threadIdx.x % LPR), n = d - e;
-    const bool in = n > 0;
-    a8 y = in ? __builtin_convertvector(load8(x + e, n), a8) : a8{};
-    if (kind < 2) {
-        const float* w = p.eps > 0.0f ? (kind == 0 ? p.qw : p.kw) : nullptr;
-        A rstd = 1;
-        if (p.eps > 0.0f) {
-            double ss = 0.0;
-#pragma unroll
-            for (int i = 0; i < 8; i++) ss = fma((double)y[i], (double)y[i], ss);
-#pragma unroll
-            for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor(ss, o);
-            rstd = (A)(1.0 / sqrt(ss / (double)d + (double)p.eps));
-            y *= rstd;
-            if (w && in) y *= __builtin_convertvector(load8(w + e, n), a8);
-        }
-        if (p.rot) {
-            const int64_t pos = p.positions[t];
-            const int rot = p.rot, half = rot >> 1;
-            if (pos < 0 || pos >= p.rows) {
-                y = a8{} + (A)__builtin_nan("");
-            } else if (in && e < rot) {
-                const float* c = p.table + pos * rot;
-                if (p.adjacent) {
-#pragma unroll
-                    for (int i = 0; i < 8; i += 2)
-                        if (e + i < rot) {
-                            const A co = c[(e + i) >> 1], si = c[half + ((e + i) >> 1)], a = y[i], b = y[i + 1];
-                            y[i] = fma(a, co, -(b * si));
-                            y[i + 1] = fma(b, co, a * si);
-                        }
-                } else if ((half & 7) == 0) {
-                    const bool low = e < half;
-                    const int at = low ? e : e - half, other = low ? e + half : at;
-                    a8 z = __builtin_convertvector(load8(x + other, 8), a8) * rstd;
-                    if (w) z *= __builtin_convertvector(load8(w + other, 8), a8);
-                    const f32x8 co = load8(c + at, 8), si = load8(c + half + at, 8);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const A s = low ? -(A)si[i] : (A)si[i];
-                        y[i] = fma(y[i], (A)co[i], z[i] * s);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; i++)
-                        if (e + i < rot) {
-                            const bool low = e + i < half;
-                            const int at = low ? e + i : e + i - half, other = low ? e + i + half : at;
-                            A z = (A)x[other] * rstd;
-                            if (w) z *= (A)w[other];
-                            const A s = low ? -(A)c[half + at] : (A)c[half + at];
-                            y[i] = fma(y[i], (A)c[at], z * s);
-                        }
-                }
+    constexpr int HW = 64 / LPR;
+    const int lane = threadIdx.x & 63, sub = lane / LPR, l = lane % LPR;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    __shared__ float rows[CACHE ? 4 : 1][CACHE ? HW * LPR * 16 : 1];
+    if (wave >= waves) return;
+    const int qs = (p.q.heads + HW - 1) / HW, ks = (p.k.heads + HW - 1) / HW, vs = CACHE ? (p.v.heads + HW - 1) / HW : 0;
+    const int all = qs + ks + vs;
+    const uint32_t parts = (all + per - 1) / per;
+    const int64_t t = token0 + wave / parts;
+    const int from = (int)(wave % parts) * per, to = min(from + per, all);
+
+    // The lane's two runs of eight elements, and how many of each there are: eight pairs (j, j + rot / 2) of the
+    // rotation, or of elements after it; adjacent pairs, and values: sixteen in a row.
+    const int d = p.d, rot = p.rot, half = rot >> 1, turning = (half + 7) >> 3;
+    int ea, eb, na, nb, pair = 8 * l;
+    if (p.adjacent || rot == 0) {
+        ea = 16 * l, eb = ea + 8, na = d - ea, nb = d - eb;
+    } else if (l < turning) {
+        ea = 8 * l, eb = half + ea, na = nb = half - ea;
+    } else {
+        ea = rot + 16 * (l - turning), eb = ea + 8, na = d - ea, nb = d - eb, pair = half;
+    }
+    const int64_t pos = rot && from < qs + ks ? p.positions[t] : 0;
+    const bool known = !rot || (pos >= 0 && pos < p.rows);
+    const int turns = half - pair;      // the lane's pairs that are rotated, from the first on
+    f32x8 c = {}, s = {};
+    if (known && turns > 0 && from < qs + ks) {
+        const float* row = p.table + pos * rot;
+        c = load8(row + pair, turns), s = load8(row + half + pair, turns);
+    }
+    int64_t slot = -1;
+    bool there = false;
+    if (CACHE) {
+        slot = p.slots[t];
+        there = slot >= 0 && (slot >> p.cache.shift) < p.cache.pages;
+    }
+
+    struct In {
+        V a, b;
+    };
+    auto step_of = [&](int i, int* kind) {      // the first head of the step's
+        *kind = i < qs ? 0 : i < qs + ks ? 1 : 2;
+        return HW * (i - (i < qs ? 0 : i < qs + ks ? qs : qs + ks)) + sub;
+    };
+    auto load = [&](int i) {
+        int kind;
+        const int h = step_of(i, &kind);
+        const HeadsView& v = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
+        In in = {V{}, V{}};
+        if (i < to && h < v.heads) {
+            const T* x = head_at<T>(v, t, h);
+            if (CACHE && kind == 2) {
+                if (16 * l < d) in.a = load8(x + 16 * l, 8), in.b = load8(x + 16 * l + 8, 8);
+            } else {
+                if (na > 0) in.a = load8(x + ea, na);
+                if (nb > 0) in.b = load8(x + eb, nb);
             }
         }
+        return in;
+    };
+    In next = load(from);
+    int weights_of = -1;
+    f32x8 wa, wb;
+    for (int i = from; i < to; i++) {
+        const In in = next;
+        next = load(i + 1);
+        int kind;
+        const int h = step_of(i, &kind);
+        if (CACHE && kind == 2) {
+            store_half_group<false>(p.cache, there && h < p.v.heads && 16 * l < d, slot, h, 16 * l, __builtin_convertvector(in.a, f32x8),
+                                    __builtin_convertvector(in.b, f32x8));
+            continue;
+        }
+        A rstd = 1;
+        if (p.eps > 0.0f) {
+            if (kind != weights_of) {
+                weights_of = kind;
+                wa = wb = f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+                const float* w = kind == 0 ? p.qw : p.kw;
+                if (w && na > 0) wa = load8(w + ea, na);
+                if (w && nb > 0) wb = load8(w + eb, nb);
+            }
+            double ss = 0.0;
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const double a = (double)(float)in.a[k], b = (double)(float)in.b[k];
+                ss = fma(a, a, fma(b, b, ss));
+            }
+            ss = lanes_sum<LPR>(ss);
+            rstd = (A)(1.0 / sqrt(ss / (double)d + (double)p.eps));
+        }
+        if (!known) rstd = (A)__builtin_nan("");
+        // element k of the lane's first run and of its second, normed
+        auto first = [&](int k) { return p.eps > 0.0f ? (A)(float)in.a[k] * rstd * wide<A>(wa[k]) : known ? (A)(float)in.a[k] : rstd; };
+        auto second = [&](int k) { return p.eps > 0.0f ? (A)(float)in.b[k] * rstd * wide<A>(wb[k]) : known ? (A)(float)in.b[k] : rstd; };
+        f32x8 lo, hi;
+        if (p.adjacent) {
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const A a = first(k), b = first(k + 1), c0 = wide<A>(c[k / 2]), s0 = wide<A>(s[k / 2]);
+                const bool t0 = k / 2 < turns, t1 = 4 + k / 2 < turns;
+                lo[k] = (float)(t0 ? fma(a, c0, -(b * s0)) : a), lo[k + 1] = (float)(t0 ? fma(b, c0, a * s0) : b);
+                const A u = second(k), v = second(k + 1), c1 = wide<A>(c[4 + k / 2]), s1 = wide<A>(s[4 + k / 2]);
+                hi[k] = (float)(t1 ? fma(u, c1, -(v * s1)) : u), hi[k + 1] = (float)(t1 ? fma(v, c1, u * s1) : v);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const A a = first(k), b = second(k), co = wide<A>(c[k]), si = wide<A>(s[k]);
+                lo[k] = (float)(k < turns ? fma(a, co, -(b * si)) : a), hi[k] = (float)(k < turns ? fma(b, co, a * si) : b);
+            }
+        }
+        if (!CACHE || kind == 0) {
+            const HeadsView& v = kind == 0 ? p.qo : p.ko;
+            if (h < v.heads) {
+                T* o = (T*)head_at<T>(v, t, h);
+                if (na > 0) store8(o + ea, __builtin_convertvector(lo, V), na);
+                if (nb > 0) store8(o + eb, __builtin_convertvector(hi, V), nb);
+            }
+            continue;
+        }
+        if (!p.adjacent && rot) {      // into sixteen elements in a row
+            float* row = rows[threadIdx.x >> 6] + sub * d;
+            if (na > 0) store8(row + ea, lo, na);
+            if (nb > 0) store8(row + eb, hi, nb);
+            __builtin_amdgcn_wave_barrier();      // LDS serves a wave in order
+            if (16 * l < d) lo = load8(row + 16 * l, 8), hi = load8(row + 16 * l + 8, 8);
+            __builtin_amdgcn_wave_barrier();
+        }
+        store_half_group<true>(p.cache, there && h < p.k.heads && 16 * l < d, slot, h, 16 * l, lo, hi);
     }
-    const f32x8 r = __builtin_convertvector(y, f32x8);
-    if (!CACHE || kind == 0) {
-        const HeadsView& o = kind == 0 ? p.qo : p.ko;
-        if (in) store8((T*)head_at<T>(o, t, h) + e, __builtin_convertvector(r, V), n);
-        return;
-    }
-    const Codes q = quantize(r);
-    const int64_t slot = p.slots[t];
-    if (!in || slot < 0 || (slot >> p.cache.shift) >= p.cache.pages) return;
-    uint8_t* b = p.cache.block(slot >> p.cache.shift, h);
-    const int at = (int)slot & (p.cache.page - 1);
-    if (kind == 1) store_codes<true>(p.cache, b, at, e, q.nibbles, q.alpha);
-    else store_codes<false>(p.cache, b, at, e, q.nibbles, q.alpha);
 }
 
 // ESB(4,1) codes 0 .. 7 are 1, 1.5, 2, 3, 4, 6, 0, 0.5: E2M1's order turned by two.
@@ -190,8 +276,11 @@ __global__ __launch_bounds__(256) void k_pack(Kv4Layout L, int64_t items, const 
         return w;
     };
     const int64_t s = row * L.groups + (e >> 5);
-    store_codes<true>(L, b, at, e, word(k), ka[s]);
-    store_codes<false>(L, b, at, e, word(v), va[s]);
+    store_codes<true>(L, b, at, e, word(k));
+    store_codes<false>(L, b, at, e, word(v));
+    if (e & 31) return;
+    *scale_at(L, b, L.key_scales_at(), at, e >> 5) = ka[s];
+    *scale_at(L, b, L.value_scales_at(), at, e >> 5) = va[s];
 }
 
 __global__ __launch_bounds__(256) void k_unpack(Kv4Layout L, int64_t items, const int64_t* slots, uint8_t* k,
@@ -230,12 +319,17 @@ __global__ __launch_bounds__(256) void k_unpack(Kv4Layout L, int64_t items, cons
 
 template <typename T, typename A, int LPR, bool CACHE>
 hipError_t launch_n(const HeadsParams& p, hipStream_t s) {
-    const int64_t all = (int64_t)p.q.heads + p.k.heads + (CACHE ? p.v.heads : 0);
-    const int64_t most = ((int64_t)1 << 28) / all;      // tokens of one launch
+    constexpr int HW = 64 / LPR;
+    auto steps = [](int heads) { return (heads + HW - 1) / HW; };
+    const int64_t all = (int64_t)steps(p.q.heads) + steps(p.k.heads) + (CACHE ? steps(p.v.heads) : 0);
+    // one step a wave while that makes up to eight waves a SIMD
+    const int64_t most_waves = 32 * num_cus();
+    int64_t per = (p.tokens * all + most_waves - 1) / most_waves;
+    if (per > all) per = all;
+    const int64_t parts = (all + per - 1) / per, most = ((int64_t)1 << 28) / parts;      // tokens of one launch
     for (int64_t t = 0; t < p.tokens; t += most) {
-        const uint32_t rows = (uint32_t)((p.tokens - t < most ? p.tokens - t : most) * all);
-        constexpr int per = 256 / LPR;
-        k_heads<T, A, LPR, CACHE><<<(rows + per - 1) / per, 256, 0, s>>>(p, t, rows);
+        const uint32_t waves = (uint32_t)((p.tokens - t < most ? p.tokens - t : most) * parts);
+        k_heads<T, A, LPR, CACHE><<<(waves + 3) / 4, 256, 0, s>>>(p, t, waves, (int)per);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -244,10 +338,17 @@ hipError_t launch_n(const HeadsParams& p, hipStream_t s) {
 
 template <typename T, typename A, bool CACHE>
 hipError_t launch_t(const HeadsParams& p, hipStream_t s) {
-    if (p.d <= 64) return launch_n<T, A, 8, CACHE>(p, s);
-    if (p.d <= 128) return launch_n<T, A, 16, CACHE>(p, s);
-    if (p.d <= 256) return launch_n<T, A, 32, CACHE>(p, s);
-    return launch_n<T, A, 64, false>(p, s);      // rope only: caches hold heads of at most 256
+    const int half = p.rot / 2;
+    int lanes = (p.d + 15) / 16;
+    if (!p.adjacent) {
+        const int n = (half + 7) / 8 + (p.d - p.rot + 15) / 16;
+        if (n > lanes) lanes = n;
+    }
+    if (lanes <= 4) return launch_n<T, A, 4, CACHE>(p, s);
+    if (lanes <= 8) return launch_n<T, A, 8, CACHE>(p, s);
+    if (lanes <= 16) return launch_n<T, A, 16, CACHE>(p, s);
+    if (lanes <= 32) return launch_n<T, A, 32, CACHE>(p, s);
+    return launch_n<T, A, 64, CACHE>(p, s);
 }
 
 // Launches of pieces of eight elements, in parts that a grid can hold.

@@ -128,6 +128,27 @@ def test_special_values(esb):
     assert bool(torch.isnan(got[3]).all()) and bool(torch.isnan(got[4, 0, 63]))
 
 
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("d,rot", [(64, 32), (80, 40), (128, 0), (100, 96)])
+def test_not_finite_stays_in_its_pair(esb, adjacent, d, rot):
+    """Without a norm what is not finite reaches its own pair, and where nothing rotates itself only."""
+    x = make(9, 3, 2, d, dtype=torch.bfloat16)
+    tab, pos = ref.table(9, rot), torch.tensor([0, 5, 8], dtype=torch.int32)
+    how = dict(table=tab.cuda(), positions=pos.cuda()) if rot else {}
+    clean, _ = esb.esb_rope(x.cuda(), None, adjacent=adjacent, **how)
+    for at in {0, rot // 2, max(rot - 1, 0), rot, d - 1} - {d}:
+        y = x.clone()
+        y[1, 1, at] = float("inf")
+        got, _ = esb.esb_rope(y.cuda(), None, adjacent=adjacent, **how)
+        pair = {at}
+        if at < rot:
+            pair = {at, at ^ 1} if adjacent else {at, (at + rot // 2) % rot}
+        keep = torch.ones_like(got, dtype=torch.bool)
+        keep[1, 1, list(pair)] = False
+        assert torch.equal(got[keep], clean[keep])
+        assert not bool(torch.isfinite(got[1, 1, list(pair)]).any())
+
+
 def test_positions_outside_the_table(esb):
     x = make(5, 5, 3, 96, dtype=torch.bfloat16)
     tab = ref.table(20, 64)
