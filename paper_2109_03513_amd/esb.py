@@ -6,6 +6,7 @@ missing the import of any entry point raises; there is no fallback.
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -955,14 +956,35 @@ def esb_w4_gemm(x, w4, N, group, x_scale=None, y_dtype=None, y=None, workspace=N
 # ---- a decoder's attention ------------------------------------------------------------------
 
 
-def _same_device(index):
-    """Refuses tensors on another device than the current one, whose stream a call would use."""
-    if index != _torch.cuda.current_device():
-        raise ValueError("the tensors are on cuda:%d, which is not the current device" % index)
+# esb_heads, esb_rotation and esb_kv4 as bytes (the fields of Heads, Rotation and Kv4), which cost a call less
+# than structures.
+_HEADS = struct.Struct("@Pqqi4x").pack
+_ROTATION = struct.Struct("@PqiiP").pack
+_KV4 = struct.Struct("@Pqiii4x").pack
 
 
-def _heads(t, name, tokens=None, heads=None, d=None, like=None, out=False):
-    """Heads structure of a device tensor (tokens x heads x d, the elements of a head adjacent)."""
+def _here(index):
+    """Handle of the current stream of device `index`, which has to be the current device."""
+    torch = _torch
+    c = torch._C
+    try:
+        current = c._cuda_getDevice()
+        if current == index:
+            return c._cuda_getCurrentRawStream(index)
+    except AttributeError:
+        current = torch.cuda.current_device()
+        if current == index:
+            return torch.cuda.current_stream().cuda_stream
+    raise ValueError("the tensors are on cuda:%d, which is not the current device" % index)
+
+
+def _cuda_tensor(t, name):
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+
+
+def _heads(t, name):
+    """(tokens, heads, elements, device, esb_heads) of a device tensor, the elements of a head adjacent."""
     if not isinstance(t, _torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA (HIP) tensor" % name)
     shape = t.shape
@@ -972,45 +994,47 @@ def _heads(t, name, tokens=None, heads=None, d=None, like=None, out=False):
     st, sh, se = t.stride()
     if se != 1 and e > 1:
         raise ValueError("%s must have adjacent elements of a head" % name)
-    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
-        raise ValueError("%s must be %s on cuda:%d" % (name, like.dtype, like.get_device()))
-    if (tokens is not None and n != tokens) or (heads is not None and h != heads) or (d is not None and e != d):
-        raise ValueError("%s must be %s x %s x %s" % (name, tokens, heads, d))
-    return Heads(t.data_ptr(), st, sh, h)
+    return n, h, e, t.get_device(), _HEADS(t.data_ptr(), st, sh, h)
 
 
-def _indexes(t, name, n, dtype, index):
-    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
-    if t.dim() != 1:
-        raise ValueError("%s must have one dimension" % name)
-    _vector(t, name, n, dtype, index)
+def _heads_like(t, name, tokens, heads, d, dtype, index):
+    """esb_heads of a tensor that has to have this shape (heads None: any number) and type, on this device."""
+    n, h, e, i, packed = _heads(t, name)
+    if t.dtype != dtype or i != index:
+        raise ValueError("%s must be %s on cuda:%d" % (name, dtype, index))
+    if n != tokens or e != d or (heads is not None and h != heads):
+        raise ValueError("%s must be %d x %s x %d" % (name, tokens, heads or "heads", d))
+    return packed
+
+
+def _numbers(t, name, n, dtype, index):
+    """Address of n contiguous elements in one dimension."""
+    _cuda_tensor(t, name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.shape != (n,) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous elements on cuda:%d" % (name, n, index))
+    return t.data_ptr()
 
 
 def _weights(w, name, d, index):
-    if w is not None:
-        if not isinstance(w, _torch.Tensor) or not w.is_cuda:
-            raise TypeError("%s must be a CUDA (HIP) tensor" % name)
-        _vector(w, name, d, _torch.float32, index)
+    return None if w is None else _numbers(w, name, d, _torch.float32, index)
 
 
 def _rotation(table, positions, adjacent, tokens, index):
-    """Rotation structure, or None without a table."""
+    """esb_rotation, or None without a table."""
     if table is None:
         if positions is not None:
             raise ValueError("positions need a table")
         return None
-    rows, rot, ld = _matrix(table, "table")
+    _cuda_tensor(table, "table")
     if table.dtype != _torch.float32:
         raise TypeError("table must be fp32")
-    if table.get_device() != index or (ld != rot and rows > 1):
-        raise ValueError("table must be contiguous on cuda:%d" % index)
-    _indexes(positions, "positions", tokens, _torch.int32, index)
-    return Rotation(table.data_ptr(), rows, rot, 1 if adjacent else 0, positions.data_ptr())
-
-
-def _ref(s):
-    return None if s is None else ctypes.byref(s)
+    if table.dim() != 2 or table.get_device() != index or not table.is_contiguous():
+        raise ValueError("table must be contiguous rows on cuda:%d" % index)
+    rows, rot = table.shape
+    at = _numbers(positions, "positions", tokens, _torch.int32, index)
+    return _ROTATION(table.data_ptr(), rows, rot, 1 if adjacent else 0, at)
 
 
 def esb_rope(q, k=None, table=None, positions=None, q_w=None, k_w=None, eps=0.0, adjacent=False,
@@ -1022,28 +1046,26 @@ def esb_rope(q, k=None, table=None, positions=None, q_w=None, k_w=None, eps=0.0,
     if stream is not None:
         with _on(stream):
             return esb_rope(q, k, table, positions, q_w, k_w, eps, adjacent, q_out, k_out)
-    x = k if q is None else q
-    hx = _heads(x, "k" if q is None else "q")
-    t = _type(x, "q", _FLOATS)
-    tokens, _, d = x.shape
-    index = x.get_device()
-    _same_device(index)
+    x, name = (k, "k") if q is None else (q, "q")
+    tokens, heads, d, index, hx = _heads(x, name)
+    t, dtype = _type(x, name, _FLOATS), x.dtype
+    stream = _here(index)
     sq = sk = so = sp = None
     if q is not None:
         sq = hx
         if q_out is None:
-            q_out = q.new_empty(q.shape)
-        so = _heads(q_out, "q_out", tokens, q.shape[1], d, x)
+            q_out = q.new_empty((tokens, heads, d))
+        so = _heads_like(q_out, "q_out", tokens, heads, d, dtype, index)
     if k is not None:
-        sk = hx if q is None else _heads(k, "k", tokens, None, d, x)
+        if q is None:
+            sk = hx
+        else:
+            sk, heads = _heads_like(k, "k", tokens, None, d, dtype, index), k.shape[1]
         if k_out is None:
-            k_out = k.new_empty(k.shape)
-        sp = _heads(k_out, "k_out", tokens, k.shape[1], d, x)
-    _weights(q_w, "q_w", d, index)
-    _weights(k_w, "k_w", d, index)
-    r = _rotation(table, positions, adjacent, tokens, index)
-    st = L.esb_rope(_ref(sq), _ref(sk), t, tokens, d, _addr(q_w), _addr(k_w), eps, _ref(r), _ref(so),
-                    _ref(sp), _stream(None))
+            k_out = k.new_empty((tokens, heads, d))
+        sp = _heads_like(k_out, "k_out", tokens, heads, d, dtype, index)
+    st = L.esb_rope(sq, sk, t, tokens, d, _weights(q_w, "q_w", d, index), _weights(k_w, "k_w", d, index), eps,
+                    _rotation(table, positions, adjacent, tokens, index), so, sp, stream)
     if st:
         raise EsbError("esb_rope", st)
     return q_out, k_out
@@ -1053,18 +1075,17 @@ def esb_kv4_page_size(page, heads, d):
     return int(lib().esb_kv4_page_size(page, heads, d))
 
 
-def _kv4(L, cache, page, heads, d, index=None):
-    """Kv4 structure of a cache tensor: pages x esb_kv4_page_size(page, heads, d) bytes."""
-    if not isinstance(cache, _torch.Tensor) or not cache.is_cuda:
-        raise TypeError("cache must be a CUDA (HIP) tensor")
+def _kv4(L, cache, page, heads, d, index):
+    """esb_kv4 of a cache tensor: pages x esb_kv4_page_size(page, heads, d) bytes."""
+    _cuda_tensor(cache, "cache")
     size = L.esb_kv4_page_size(page, heads, d)
     if size == 0:
         raise EsbError("esb_kv4_page_size", ESB_E_UNSUPPORTED)
     if cache.dtype != _torch.uint8 or not cache.is_contiguous() or cache.dim() != 2 or cache.shape[1] != size:
         raise ValueError("cache must be contiguous uint8, pages x %d" % size)
-    if index is not None and cache.get_device() != index:
+    if cache.get_device() != index:
         raise ValueError("cache must be on cuda:%d" % index)
-    return Kv4(cache.data_ptr(), cache.shape[0], page, heads, d)
+    return _KV4(cache.data_ptr(), cache.shape[0], page, heads, d)
 
 
 def esb_kv4_append(cache, page, k, v, slots, table=None, positions=None, k_w=None, eps=0.0, adjacent=False,
@@ -1077,25 +1098,20 @@ def esb_kv4_append(cache, page, k, v, slots, table=None, positions=None, k_w=Non
     if stream is not None:
         with _on(stream):
             return esb_kv4_append(cache, page, k, v, slots, table, positions, k_w, eps, adjacent, q, q_w, q_out)
-    sk = _heads(k, "k")
-    t = _type(k, "k", _FLOATS)
-    tokens, heads, d = k.shape
-    index = k.get_device()
-    _same_device(index)
-    sv = _heads(v, "v", tokens, heads, d, k)
+    tokens, heads, d, index, sk = _heads(k, "k")
+    t, dtype = _type(k, "k", _FLOATS), k.dtype
+    stream = _here(index)
+    sv = _heads_like(v, "v", tokens, heads, d, dtype, index)
     c = _kv4(L, cache, page, heads, d, index)
-    _indexes(slots, "slots", tokens, _torch.int64, index)
+    at = _numbers(slots, "slots", tokens, _torch.int64, index)
     sq = so = None
     if q is not None:
-        sq = _heads(q, "q", tokens, None, d, k)
+        sq, heads = _heads_like(q, "q", tokens, None, d, dtype, index), q.shape[1]
         if q_out is None:
-            q_out = q.new_empty(q.shape)
-        so = _heads(q_out, "q_out", tokens, q.shape[1], d, k)
-    _weights(q_w, "q_w", d, index)
-    _weights(k_w, "k_w", d, index)
-    r = _rotation(table, positions, adjacent, tokens, index)
-    st = L.esb_kv4_append(_ref(sq), ctypes.byref(sk), ctypes.byref(sv), t, tokens, _addr(q_w), _addr(k_w), eps,
-                          _ref(r), slots.data_ptr(), ctypes.byref(c), _ref(so), _stream(None))
+            q_out = q.new_empty((tokens, heads, d))
+        so = _heads_like(q_out, "q_out", tokens, heads, d, dtype, index)
+    st = L.esb_kv4_append(sq, sk, sv, t, tokens, _weights(q_w, "q_w", d, index), _weights(k_w, "k_w", d, index), eps,
+                          _rotation(table, positions, adjacent, tokens, index), at, c, so, stream)
     if st:
         raise EsbError("esb_kv4_append", st)
     return q_out
@@ -1108,20 +1124,17 @@ def esb_kv4_pack(cache, page, k, k_alpha, v, v_alpha, slots, stream=None):
     if stream is not None:
         with _on(stream):
             return esb_kv4_pack(cache, page, k, k_alpha, v, v_alpha, slots)
-    _heads(k, "k")
-    tokens, heads, d = k.shape
-    index = k.get_device()
-    _same_device(index)
+    tokens, heads, d, index, _ = _heads(k, "k")
+    stream = _here(index)
     c = _kv4(L, cache, page, heads, d, index)
     for x, name, e, dtype in ((k, "k", d, _torch.uint8), (v, "v", d, _torch.uint8),
                               (k_alpha, "k_alpha", d // 32, _torch.bfloat16),
                               (v_alpha, "v_alpha", d // 32, _torch.bfloat16)):
-        _heads(x, name, tokens, heads, e)
-        if x.dtype != dtype or x.get_device() != index or not x.is_contiguous():
-            raise ValueError("%s must be contiguous %s on cuda:%d" % (name, dtype, index))
-    _indexes(slots, "slots", tokens, _torch.int64, index)
+        _heads_like(x, name, tokens, heads, e, dtype, index)
+        if not x.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
     st = L.esb_kv4_pack(k.data_ptr(), k_alpha.data_ptr(), v.data_ptr(), v_alpha.data_ptr(), tokens,
-                        slots.data_ptr(), ctypes.byref(c), _stream(None))
+                        _numbers(slots, "slots", tokens, _torch.int64, index), c, stream)
     if st:
         raise EsbError("esb_kv4_pack", st)
     return cache
@@ -1134,15 +1147,16 @@ def esb_kv4_unpack(cache, page, heads, d, slots, stream=None):
     if stream is not None:
         with _on(stream):
             return esb_kv4_unpack(cache, page, heads, d, slots)
-    c = _kv4(L, cache, page, heads, d)
-    index = cache.get_device()
-    _same_device(index)
-    tokens = slots.numel() if isinstance(slots, _torch.Tensor) else 0
-    _indexes(slots, "slots", tokens, _torch.int64, index)
-    k, v = (cache.new_empty(tokens, heads, d, dtype=_torch.float8_e4m3fn) for _ in range(2))
-    ka, va = (cache.new_empty(tokens, heads, d // 32, dtype=_torch.bfloat16) for _ in range(2))
-    st = L.esb_kv4_unpack(ctypes.byref(c), tokens, slots.data_ptr(), k.data_ptr(), ka.data_ptr(), v.data_ptr(),
-                          va.data_ptr(), _stream(None))
+    _cuda_tensor(slots, "slots")
+    index, tokens = slots.get_device(), slots.numel()
+    stream = _here(index)
+    c = _kv4(L, cache, page, heads, d, index)
+    at = _numbers(slots, "slots", tokens, _torch.int64, index)
+    k = cache.new_empty((tokens, heads, d), dtype=_torch.float8_e4m3fn)
+    v = cache.new_empty((tokens, heads, d), dtype=_torch.float8_e4m3fn)
+    ka = cache.new_empty((tokens, heads, d // 32), dtype=_torch.bfloat16)
+    va = cache.new_empty((tokens, heads, d // 32), dtype=_torch.bfloat16)
+    st = L.esb_kv4_unpack(c, tokens, at, k.data_ptr(), ka.data_ptr(), v.data_ptr(), va.data_ptr(), stream)
     if st:
         raise EsbError("esb_kv4_unpack", st)
     return k, ka, v, va
@@ -1163,21 +1177,18 @@ def esb_kv4_attention(q, cache, page, kv_heads, pages, lengths, starts=None, sca
     if stream is not None:
         with _on(stream):
             return esb_kv4_attention(q, cache, page, kv_heads, pages, lengths, starts, scale, out, workspace)
-    sq = _heads(q, "q")
-    t = _type(q, "q", _FLOATS)      # fp32: the library's refusal
-    tokens, heads, d = q.shape
-    index = q.get_device()
-    _same_device(index)
+    tokens, heads, d, index, sq = _heads(q, "q")
+    t, dtype = _type(q, "q", _FLOATS), q.dtype      # fp32: the library's refusal
+    stream = _here(index)
     c = _kv4(L, cache, page, kv_heads, d, index)
     seqs, columns, pitch = _matrix(pages, "pages")
     if pages.dtype != _torch.int32 or pages.get_device() != index:
         raise ValueError("pages must be int32 on cuda:%d" % index)
-    _indexes(lengths, "lengths", seqs, _torch.int32, index)
-    if starts is not None:
-        _indexes(starts, "starts", seqs + 1, _torch.int32, index)
+    kept = _numbers(lengths, "lengths", seqs, _torch.int32, index)
+    first = None if starts is None else _numbers(starts, "starts", seqs + 1, _torch.int32, index)
     if out is None:
-        out = q.new_empty(q.shape)
-    so = _heads(out, "out", tokens, heads, d, q)
+        out = q.new_empty((tokens, heads, d))
+    so = _heads_like(out, "out", tokens, heads, d, dtype, index)
     wp, wb = None, 0
     if workspace is None:
         wb = L.esb_kv4_attention_workspace_size(tokens, heads, d, kv_heads, seqs, 0 if starts is None else 1,
@@ -1186,14 +1197,12 @@ def esb_kv4_attention(q, cache, page, kv_heads, pages, lengths, starts=None, sca
             workspace = q.new_empty(wb, dtype=_torch.uint8)
             wp = workspace.data_ptr()
     else:
-        if not isinstance(workspace, _torch.Tensor) or not workspace.is_cuda:
-            raise TypeError("workspace must be a CUDA (HIP) tensor")
+        _cuda_tensor(workspace, "workspace")
         if workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous on cuda:%d" % index)
         wp, wb = _ws(workspace)
-    st = L.esb_kv4_attention(ctypes.byref(sq), t, tokens, ctypes.byref(c), seqs, _addr(starts), lengths.data_ptr(),
-                             pages.data_ptr(), pitch, columns, d ** -0.5 if scale is None else scale,
-                             ctypes.byref(so), wp, wb, _stream(None))
+    st = L.esb_kv4_attention(sq, t, tokens, c, seqs, first, kept, pages.data_ptr(), pitch, columns,
+                             d ** -0.5 if scale is None else scale, so, wp, wb, stream)
     if st:
         raise EsbError("esb_kv4_attention", st)
     return out
@@ -1207,27 +1216,24 @@ def esb_attention(q, k, v, q_starts, k_starts=None, causal=True, scale=None, out
     if stream is not None:
         with _on(stream):
             return esb_attention(q, k, v, q_starts, k_starts, causal, scale, out)
-    sq = _heads(q, "q")
-    t = _type(q, "q", _FLOATS)      # fp32: the library's refusal
-    tokens, heads, d = q.shape
-    index = q.get_device()
-    _same_device(index)
-    sk = _heads(k, "k", None, None, d, q)
-    k_tokens = k.shape[0]
-    sv = _heads(v, "v", k_tokens, k.shape[1], d, q)
-    _indexes(q_starts, "q_starts", q_starts.numel() if isinstance(q_starts, _torch.Tensor) else 0, _torch.int32,
-             index)
+    tokens, heads, d, index, sq = _heads(q, "q")
+    t, dtype = _type(q, "q", _FLOATS), q.dtype      # fp32: the library's refusal
+    stream = _here(index)
+    _cuda_tensor(k, "k")
+    k_tokens, kv_heads = k.shape[0], k.shape[1] if k.dim() > 1 else 0
+    sk = _heads_like(k, "k", k_tokens, kv_heads, d, dtype, index)
+    sv = _heads_like(v, "v", k_tokens, kv_heads, d, dtype, index)
+    _cuda_tensor(q_starts, "q_starts")
     seqs = q_starts.numel() - 1
     if seqs < 0:
         raise ValueError("q_starts must have a start and an end")
-    if k_starts is not None:
-        _indexes(k_starts, "k_starts", seqs + 1, _torch.int32, index)
+    first = _numbers(q_starts, "q_starts", seqs + 1, _torch.int32, index)
+    k_first = None if k_starts is None else _numbers(k_starts, "k_starts", seqs + 1, _torch.int32, index)
     if out is None:
-        out = q.new_empty(q.shape)
-    so = _heads(out, "out", tokens, heads, d, q)
-    st = L.esb_attention(ctypes.byref(sq), ctypes.byref(sk), ctypes.byref(sv), t, tokens, k_tokens, d, seqs,
-                         q_starts.data_ptr(), _addr(k_starts), 1 if causal else 0,
-                         d ** -0.5 if scale is None else scale, ctypes.byref(so), _stream(None))
+        out = q.new_empty((tokens, heads, d))
+    so = _heads_like(out, "out", tokens, heads, d, dtype, index)
+    st = L.esb_attention(sq, sk, sv, t, tokens, k_tokens, d, seqs, first, k_first, 1 if causal else 0,
+                         d ** -0.5 if scale is None else scale, so, stream)
     if st:
         raise EsbError("esb_attention", st)
     return out
