@@ -689,7 +689,7 @@ int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, u
  *            the last sequence are left as they were;
  *   lengths  device, one per sequence;
  *   pages    device, seqs rows of `columns` page numbers, pitch page_pitch; entries behind a
- *            sequence's last key are not read;
+ *            sequence's last key may hold anything;
  *   scale    positive and finite.
  * A query that sees no key gets zeros.  What lies in the cache behind what a query sees does not
  * reach it.  A length beyond columns * page makes the sequence's outputs NaN, a page number that is
@@ -700,7 +700,8 @@ int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, u
  *              are not split over workgroups).  It carries nothing between calls; concurrent calls
  *              need distinct ones.  Less or NULL: ESB_E_WORKSPACE.
  * The order of sums is fixed by the sizes: the same call gives the same bits.
- * ESB_E_UNSUPPORTED: 2^31 rows (tokens x heads), workgroups or columns * page or more.
+ * ESB_E_UNSUPPORTED: 2^31 or more rows (tokens x heads) or workgroups, columns * page above
+ * 2^31 - 8193.
  * tokens == 0 or seqs == 0 enqueues nothing.
  */
 size_t esb_kv4_attention_workspace_size(int64_t tokens, int q_heads, int d, int kv_heads, int seqs,

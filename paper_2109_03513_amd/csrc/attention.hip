@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
     const int h = blockIdx.x % p.k.heads;
     const int64_t slot = gridDim.x / p.k.heads - 1 - blockIdx.x / p.k.heads;      // the longest rows first
-    const Tile t = find_tile(p.q_starts, p.seqs, p.q_tokens, p.group, R, slot);
+    const Tile t = find_tile(p.q_starts, p.seqs, p.q_tokens, p.group, R, slot, nullptr, nullptr);
     const int n = (int)(t.end - t.begin), rows = n * p.group;
     if (t.index < 0 || (int64_t)t.index * R >= rows) return;
     const int row0 = t.index * R;

@@ -832,6 +832,7 @@ int esb_w4_gemm(int M, int N, int K, int group, const void* x, int64_t ldx, int 
 
 // ---------------------------------------------------------- a decoder's attention
 constexpr int kMostHeads = 4096;
+constexpr int kMostKeys = INT32_MAX - 8192;      // of a sequence: steps past the last key stay within 32 bits
 constexpr float kLog2E = 1.44269504088896340736f;
 
 static int heads_check(const esb_heads* v, int type, int64_t tokens, int d, bool out) {
@@ -967,7 +968,7 @@ static int attention_check(int type, int64_t tokens, int q_heads, int kv_heads, 
 
 size_t esb_kv4_attention_workspace_size(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, int has_starts,
                                         int64_t columns, int page) {
-    if (kv4_shape(page, kv_heads, d) || q_heads > kMostHeads || columns < 0 || columns > INT32_MAX / page) return 0;
+    if (kv4_shape(page, kv_heads, d) || q_heads > kMostHeads || columns < 0 || columns > kMostKeys / page) return 0;
     if (attention_check(ESB_BF16, tokens, q_heads, kv_heads, seqs, 1.0f) || tokens == 0 || seqs == 0) return 0;
     return kv4_attention_workspace(tokens, q_heads, d, kv_heads, seqs, has_starts != 0, columns * page);
 }
@@ -983,7 +984,7 @@ int esb_kv4_attention(const esb_heads* q, int type, int64_t tokens, const esb_kv
     const int d = cache->d;
     if ((st = heads_check(q, type, tokens, d, false)) || (st = heads_check(out, type, tokens, d, true))) return st;
     if (q->heads != out->heads || columns < 0 || page_pitch < columns) return ESB_E_INVALID;
-    if (columns > INT32_MAX / cache->page) return ESB_E_UNSUPPORTED;
+    if (columns > kMostKeys / cache->page) return ESB_E_UNSUPPORTED;
     if (!starts && tokens != seqs) return ESB_E_INVALID;
     if (tokens == 0 || seqs == 0) return ESB_OK;
     if (!lengths || (columns > 0 && (!pages || cache->pages == 0)) || (uintptr_t)starts % 4 || (uintptr_t)lengths % 4 ||

@@ -122,22 +122,30 @@ __device__ __forceinline__ Tile find_sequence(const int32_t* starts, int seqs, i
     t.end = min(max((int64_t)starts[t.seq + 1], t.begin), tokens);
     return t;
 }
-__device__ __forceinline__ Tile find_tile(const int32_t* starts, int seqs, int64_t tokens, int per, int R,
-                                          int64_t slot) {
+__device__ __forceinline__ Tile find_tile(const int32_t* starts, int seqs, int64_t tokens, int per, int R, int64_t slot,
+                                          const int32_t* lengths, int* length) {
     const int lane = threadIdx.x & 63;
-    int n = 0;
-    for (int s0 = 0; s0 < seqs; s0 += 64) {
-        const int s = s0 + lane;
-        bool before = false;
-        if (s < seqs) before = (int64_t)max(starts[s], 0) * per / R + s <= slot;
-        n += __builtin_popcountll(__ballot(before));
-    }
     Tile t;
-    t.seq = __builtin_amdgcn_readfirstlane(max(n - 1, 0));
-    const int64_t a = min(max((int64_t)starts[t.seq], (int64_t)0), tokens);
-    const int64_t b = min(max((int64_t)starts[t.seq + 1], a), tokens);
-    t.begin = a, t.end = b;
-    t.index = (int)(slot - (a * per / R + t.seq));
+    int64_t a, b;
+    if (seqs < 64) {      // starts and lengths in one trip to memory
+        const int start = starts[min(lane, seqs)], kept = lengths ? lengths[min(lane, seqs - 1)] : 0;
+        const bool before = lane < seqs && (int64_t)max(start, 0) * per / R + lane <= slot;
+        t.seq = max(__builtin_popcountll(__ballot(before)) - 1, 0);
+        a = __builtin_amdgcn_readlane(start, t.seq), b = __builtin_amdgcn_readlane(start, t.seq + 1);
+        if (lengths) *length = __builtin_amdgcn_readlane(kept, t.seq);
+    } else {
+        int n = 0;
+        for (int s0 = 0; s0 < seqs; s0 += 64) {
+            const int s = min(s0 + lane, seqs - 1);
+            n += __builtin_popcountll(__ballot(s0 + lane < seqs && (int64_t)max(starts[s], 0) * per / R + s <= slot));
+        }
+        t.seq = __builtin_amdgcn_readfirstlane(max(n - 1, 0));
+        a = starts[t.seq], b = starts[t.seq + 1];
+        if (lengths) *length = lengths[t.seq];
+    }
+    t.begin = min(max(a, (int64_t)0), tokens);
+    t.end = min(max(b, t.begin), tokens);
+    t.index = (int)(slot - (t.begin * per / R + t.seq));
     return t;
 }
 
@@ -151,16 +159,17 @@ struct Rows {
 
 __device__ __forceinline__ Rows find_rows(const Kv4AttentionParams& p, int64_t slot, int tiles, int R) {
     Rows r;
-    int index;
+    int index, kept;
     if (p.starts) {
-        const Tile t = find_tile(p.starts, p.seqs, p.tokens, p.group, R, slot);
+        const Tile t = find_tile(p.starts, p.seqs, p.tokens, p.group, R, slot, p.lengths, &kept);
         r.seq = t.seq, r.begin = t.begin, r.n = (int)(t.end - t.begin), index = t.index;
     } else {
         r.seq = (int)(slot / tiles), index = (int)(slot % tiles), r.begin = r.seq, r.n = 1;
+        kept = p.lengths[r.seq];
     }
     r.rows = r.n * p.group;
     r.row0 = index < 0 || (int64_t)index * R >= r.rows ? r.rows : index * R;
-    const int64_t len = p.lengths[r.seq];
+    const int64_t len = kept;
     r.bad = len > (int64_t)p.columns * p.cache.page;
     r.len = r.bad || len < 0 ? 0 : (int)len;
     return r;

@@ -107,18 +107,22 @@ __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int 
     const int h = (int)(id % p.cache.heads);
     const Rows rw = find_rows(p, id / p.cache.heads, tiles, R);
     if (rw.row0 >= rw.rows) return;
-    const int first = rw.len - rw.n;                    // the last key of query t is first + t
-    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
-    const int k0 = chunk * run, k1 = min(k0 + run, keys);
-    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
-    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
 
-    int last[NT];
+    // the first pages and the queries are asked for before the sequence's length is there
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    const int page = p.cache.page;
+    struct Ids {
+        int a, b;
+    };
+    auto ids = [&](int at) {      // pages of the halves of a step; behind the last key whatever the table holds
+        return Ids{table[min(at >> p.cache.shift, p.columns - 1)], table[min((at + 16) >> p.cache.shift, p.columns - 1)]};
+    };
+    const int at0 = chunk * run + 32 * wave;
+    Ids next = p.columns > 0 ? ids(at0) : Ids{0, 0};
     V qf[NT][CP];
 #pragma unroll
     for (int u = 0; u < NT; u++) {
         const int r = rw.row0 + 16 * u + i, t = r / p.group;
-        last[u] = first + t;
         const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
 #pragma unroll
         for (int s = 0; s < CP; s++) {
@@ -127,16 +131,16 @@ __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int 
         }
     }
 
-    const int32_t* table = p.table + rw.seq * p.table_pitch;
-    const int page = p.cache.page;
-    struct Ids {
-        int a, b;
-    };
-    auto ids = [&](int at) {      // pages of the halves of a step; halves past the last key take its page
-        const int a = __builtin_amdgcn_readfirstlane(min(at, keys - 1) >> p.cache.shift);
-        const int b = __builtin_amdgcn_readfirstlane(min(at + 16, keys - 1) >> p.cache.shift);
-        return Ids{table[a], table[b]};
-    };
+    const int first = rw.len - rw.n;                    // the last key of query t is first + t
+    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
+    const int k0 = chunk * run, k1 = min(k0 + run, keys);
+    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
+    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
+
+    int last[NT];
+#pragma unroll
+    for (int u = 0; u < NT; u++) last[u] = first + (rw.row0 + 16 * u + i) / p.group;
+
     auto load = [&](int at, Ids pg) {
         Step<CP> st;
         st.bad = 0;
@@ -253,10 +257,10 @@ __global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int 
         }
     };
 
-    int at = k0 + 32 * wave;
+    int at = at0;
     if (at < k1) {
-        Step<CP> cur = load(at, ids(at));
-        Ids next = ids(at + 128);
+        Step<CP> cur = load(at, next);
+        next = ids(at + 128);
         for (; at < k1; at += 128) {
             Step<CP> st = cur;
             if (at + 128 < k1) cur = load(at + 128, next);
@@ -359,18 +363,22 @@ __global__ __launch_bounds__(256, CP * NT <= 4 ? 3 : CP * NT <= 8 ? 2 : 1) void 
     const int h = (int)(id % p.cache.heads);
     const Rows rw = find_rows(p, id / p.cache.heads, tiles, R);
     if (rw.row0 >= rw.rows) return;
-    const int first = rw.len - rw.n;                    // the last key of query t is first + t
-    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
-    const int k0 = chunk * run, k1 = min(k0 + run, keys);
-    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
-    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
 
-    int last[NT];
+    // the first pages and the queries are asked for before the sequence's length is there
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    const int page = p.cache.page;
+    struct Ids {
+        int a, b;
+    };
+    auto ids = [&](int at) {      // pages of the halves of a step; behind the last key whatever the table holds
+        return Ids{table[min(at >> p.cache.shift, p.columns - 1)], table[min((at + 16) >> p.cache.shift, p.columns - 1)]};
+    };
+    const int at0 = chunk * run + 32 * wave;
+    Ids next = p.columns > 0 ? ids(at0) : Ids{0, 0};
     V qf[NT][CP];
 #pragma unroll
     for (int u = 0; u < NT; u++) {
         const int r = rw.row0 + HR * u + i / CP, t = r / p.group;
-        last[u] = first + t;
         const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
         V mine = {};
         if (r < rw.rows && own < C) mine = load8(q + 32 * own + 8 * g, 8);
@@ -378,19 +386,20 @@ __global__ __launch_bounds__(256, CP * NT <= 4 ? 3 : CP * NT <= 8 ? 2 : 1) void 
         for (int s = 0; s < CP; s++) qf[u][s] = s == own ? mine : V{};
     }
 
-    const int32_t* table = p.table + rw.seq * p.table_pitch;
-    const int page = p.cache.page;
-    struct Ids {
-        int a, b;
-    };
+    const int first = rw.len - rw.n;                    // the last key of query t is first + t
+    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
+    const int k0 = chunk * run, k1 = min(k0 + run, keys);
+    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
+    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
+
+    int last[NT];
+#pragma unroll
+    for (int u = 0; u < NT; u++) last[u] = first + (rw.row0 + HR * u + i / CP) / p.group;
+
     struct Piece {
         W k[2], v[2];
         uint2 ka[2], va[2];
         int bad;
-    };
-    auto ids = [&](int at) {      // pages of the halves of a step; halves past the last key take its page
-        const int a = min(at, keys - 1) >> p.cache.shift, b = min(at + 16, keys - 1) >> p.cache.shift;
-        return Ids{table[a], table[b]};
     };
     // what a lane adds to a half's place in its block
     const uint32_t k_at = i * 16 * C + g * 4 * C, v_at = g * 64 * C + i * 4 * C;
@@ -511,10 +520,10 @@ __global__ __launch_bounds__(256, CP * NT <= 4 ? 3 : CP * NT <= 8 ? 2 : 1) void 
         }
     };
 
-    int at = k0 + 32 * wave;
+    int at = at0;
     if (at < k1) {
-        Piece cur = load(at, ids(at));
-        Ids next = ids(at + 128);
+        Piece cur = load(at, next);
+        next = ids(at + 128);
         for (; at < k1; at += 128) {
             const Piece st = cur;
             if (at + 128 < k1) cur = load(at + 128, next);
@@ -713,9 +722,9 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
     s.tiles = (group + R - 1) / R;
     s.slots = starts ? tokens * group / R + seqs : (int64_t)seqs * s.tiles;
     const int64_t base = s.slots * kv_heads;
-    // Few rows: parts of at least 384 keys, for twelve workgroups a CU.  Many: as many as run at once (256 rows a CU).
+    // Few rows: parts of about 576 keys (five steps a wave), for twelve workgroups a CU.  Many: as many as run at once (256 rows a CU).
     int64_t n = s.kind == kKv4Many ? (d > 128 ? 1 : 2 / s.NT) * cus / base : (12 * cus + base - 1) / base;
-    const int64_t most = (longest + 383) / 384;
+    const int64_t most = (longest + 575) / 576;
     if (n > most) n = most;
     if (n < 1) n = 1;
     int64_t run = ((longest + n - 1) / n + 127) / 128 * 128;

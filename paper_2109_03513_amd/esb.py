@@ -1007,6 +1007,14 @@ def _heads_like(t, name, tokens, heads, d, dtype, index):
     return packed
 
 
+def _heads_out(out, name, x, tokens, heads, d, dtype, index):
+    """An output as given or new beside x, and its esb_heads."""
+    if out is None:
+        out = x.new_empty((tokens, heads, d))
+        return out, _HEADS(out.data_ptr(), heads * d, d, heads)
+    return out, _heads_like(out, name, tokens, heads, d, dtype, index)
+
+
 def _numbers(t, name, n, dtype, index):
     """Address of n contiguous elements in one dimension."""
     _cuda_tensor(t, name)
@@ -1053,17 +1061,13 @@ def esb_rope(q, k=None, table=None, positions=None, q_w=None, k_w=None, eps=0.0,
     sq = sk = so = sp = None
     if q is not None:
         sq = hx
-        if q_out is None:
-            q_out = q.new_empty((tokens, heads, d))
-        so = _heads_like(q_out, "q_out", tokens, heads, d, dtype, index)
+        q_out, so = _heads_out(q_out, "q_out", q, tokens, heads, d, dtype, index)
     if k is not None:
         if q is None:
             sk = hx
         else:
             sk, heads = _heads_like(k, "k", tokens, None, d, dtype, index), k.shape[1]
-        if k_out is None:
-            k_out = k.new_empty((tokens, heads, d))
-        sp = _heads_like(k_out, "k_out", tokens, heads, d, dtype, index)
+        k_out, sp = _heads_out(k_out, "k_out", k, tokens, heads, d, dtype, index)
     st = L.esb_rope(sq, sk, t, tokens, d, _weights(q_w, "q_w", d, index), _weights(k_w, "k_w", d, index), eps,
                     _rotation(table, positions, adjacent, tokens, index), so, sp, stream)
     if st:
@@ -1075,12 +1079,10 @@ def esb_kv4_page_size(page, heads, d):
     return int(lib().esb_kv4_page_size(page, heads, d))
 
 
-def _kv4(L, cache, page, heads, d, index):
+def _kv4(cache, page, heads, d, index):
     """esb_kv4 of a cache tensor: pages x esb_kv4_page_size(page, heads, d) bytes."""
     _cuda_tensor(cache, "cache")
-    size = L.esb_kv4_page_size(page, heads, d)
-    if size == 0:
-        raise EsbError("esb_kv4_page_size", ESB_E_UNSUPPORTED)
+    size = heads * page * 36 * (d // 32)      # of shapes that the library takes; it refuses the others
     if cache.dtype != _torch.uint8 or not cache.is_contiguous() or cache.dim() != 2 or cache.shape[1] != size:
         raise ValueError("cache must be contiguous uint8, pages x %d" % size)
     if cache.get_device() != index:
@@ -1102,14 +1104,12 @@ def esb_kv4_append(cache, page, k, v, slots, table=None, positions=None, k_w=Non
     t, dtype = _type(k, "k", _FLOATS), k.dtype
     stream = _here(index)
     sv = _heads_like(v, "v", tokens, heads, d, dtype, index)
-    c = _kv4(L, cache, page, heads, d, index)
+    c = _kv4(cache, page, heads, d, index)
     at = _numbers(slots, "slots", tokens, _torch.int64, index)
     sq = so = None
     if q is not None:
         sq, heads = _heads_like(q, "q", tokens, None, d, dtype, index), q.shape[1]
-        if q_out is None:
-            q_out = q.new_empty((tokens, heads, d))
-        so = _heads_like(q_out, "q_out", tokens, heads, d, dtype, index)
+        q_out, so = _heads_out(q_out, "q_out", q, tokens, heads, d, dtype, index)
     st = L.esb_kv4_append(sq, sk, sv, t, tokens, _weights(q_w, "q_w", d, index), _weights(k_w, "k_w", d, index), eps,
                           _rotation(table, positions, adjacent, tokens, index), at, c, so, stream)
     if st:
@@ -1126,7 +1126,7 @@ def esb_kv4_pack(cache, page, k, k_alpha, v, v_alpha, slots, stream=None):
             return esb_kv4_pack(cache, page, k, k_alpha, v, v_alpha, slots)
     tokens, heads, d, index, _ = _heads(k, "k")
     stream = _here(index)
-    c = _kv4(L, cache, page, heads, d, index)
+    c = _kv4(cache, page, heads, d, index)
     for x, name, e, dtype in ((k, "k", d, _torch.uint8), (v, "v", d, _torch.uint8),
                               (k_alpha, "k_alpha", d // 32, _torch.bfloat16),
                               (v_alpha, "v_alpha", d // 32, _torch.bfloat16)):
@@ -1150,7 +1150,7 @@ def esb_kv4_unpack(cache, page, heads, d, slots, stream=None):
     _cuda_tensor(slots, "slots")
     index, tokens = slots.get_device(), slots.numel()
     stream = _here(index)
-    c = _kv4(L, cache, page, heads, d, index)
+    c = _kv4(cache, page, heads, d, index)
     at = _numbers(slots, "slots", tokens, _torch.int64, index)
     k = cache.new_empty((tokens, heads, d), dtype=_torch.float8_e4m3fn)
     v = cache.new_empty((tokens, heads, d), dtype=_torch.float8_e4m3fn)
@@ -1180,15 +1180,13 @@ def esb_kv4_attention(q, cache, page, kv_heads, pages, lengths, starts=None, sca
     tokens, heads, d, index, sq = _heads(q, "q")
     t, dtype = _type(q, "q", _FLOATS), q.dtype      # fp32: the library's refusal
     stream = _here(index)
-    c = _kv4(L, cache, page, kv_heads, d, index)
+    c = _kv4(cache, page, kv_heads, d, index)
     seqs, columns, pitch = _matrix(pages, "pages")
     if pages.dtype != _torch.int32 or pages.get_device() != index:
         raise ValueError("pages must be int32 on cuda:%d" % index)
     kept = _numbers(lengths, "lengths", seqs, _torch.int32, index)
     first = None if starts is None else _numbers(starts, "starts", seqs + 1, _torch.int32, index)
-    if out is None:
-        out = q.new_empty((tokens, heads, d))
-    so = _heads_like(out, "out", tokens, heads, d, dtype, index)
+    out, so = _heads_out(out, "out", q, tokens, heads, d, dtype, index)
     wp, wb = None, 0
     if workspace is None:
         wb = L.esb_kv4_attention_workspace_size(tokens, heads, d, kv_heads, seqs, 0 if starts is None else 1,
@@ -1229,9 +1227,7 @@ def esb_attention(q, k, v, q_starts, k_starts=None, causal=True, scale=None, out
         raise ValueError("q_starts must have a start and an end")
     first = _numbers(q_starts, "q_starts", seqs + 1, _torch.int32, index)
     k_first = None if k_starts is None else _numbers(k_starts, "k_starts", seqs + 1, _torch.int32, index)
-    if out is None:
-        out = q.new_empty((tokens, heads, d))
-    so = _heads_like(out, "out", tokens, heads, d, dtype, index)
+    out, so = _heads_out(out, "out", q, tokens, heads, d, dtype, index)
     st = L.esb_attention(sq, sk, sv, t, tokens, k_tokens, d, seqs, first, k_first, 1 if causal else 0,
                          d ** -0.5 if scale is None else scale, so, stream)
     if st:

@@ -200,8 +200,10 @@ def test_binding_refusals(esb):
                 dict(v=x.half()), dict(slots=slots[:3]), dict(k=x[0]), dict(q=x[:2])):
         with pytest.raises(ValueError):
             esb.esb_kv4_append(**{**dict(cache=cache, page=16, k=x, v=x, slots=slots), **bad})
-    with pytest.raises(esb.EsbError):
-        esb.esb_kv4_append(cache, 24, x, x, slots)
+    for page, d in ((24, 64), (8, 64), (16, 48)):      # shapes that the library does not take
+        y = x[..., :d]
+        with pytest.raises(esb.EsbError):
+            esb.esb_kv4_append(cache.new_zeros(2, 2 * page * 36 * (d // 32)), page, y, y, slots)
     with pytest.raises(TypeError):
         esb.esb_kv4_append(cache, 16, x, x, slots.int())
     with pytest.raises(TypeError):
