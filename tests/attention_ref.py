@@ -68,7 +68,7 @@ def attend(q, k, v, last, scale):
     none = ~sees.any(1)[None, :, None]
 
     def back(t):
-        return t.reshape(kv, heads // kv, n, -1).permute(2, 0, 1, 3).reshape(n, heads, -1)
+        return t.reshape(kv, heads // kv, n, t.shape[2]).permute(2, 0, 1, 3).reshape(n, heads, t.shape[2])
 
     o = torch.where(none, 0.0, torch.matmul(p, v) / total)
     s = torch.where(none, 0.0, torch.matmul(p, v.abs()) / total)
