@@ -126,27 +126,31 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
     const int page = p.cache.page;
     WT kw, vw;
     uint32_t ka[NK], va[NV];
-    auto page_of = [&](int j0) { return table[min(j0 + key, keys - 1) >> p.cache.shift]; };
+    // a wave's keys lie in sixteen in a row, so in one page
+    const int wave_key = __builtin_amdgcn_readfirstlane(key & ~15), in16 = key & 15;
+    const uint32_t k_at = in16 * 16 * C + a4 * 4 * C + 4 * gk, v_at = (in16 >> 2) * 64 * C + a16 * 4 * C + 4 * gv;
+    auto page_of = [&](int j0) { return table[min(j0 + wave_key, keys - 1) >> p.cache.shift]; };
     auto load = [&](int j0, int pid) {
+        pid = __builtin_amdgcn_readfirstlane(pid);
         const bool bad = pid < 0 || pid >= p.cache.pages;
-        const uint8_t* b = p.cache.block(bad ? 0 : pid, h);
-        const int t = (j0 + key) & (page - 1);
+        const int t = (j0 + wave_key) & (page - 1);
         // words past the head's groups are of what follows in the block, and meet zeros of the query or make
         // outputs that are not stored; their scales repeat others
-        kw = ((const Loose<WT, uint32_t>*)(b + t * 16 * C + a4 * 4 * C + 4 * gk))->v;
-        vw = ((const Loose<WT, uint32_t>*)(b + p.cache.values_at() + (t >> 2) * 64 * C + a16 * 4 * C + 4 * gv))->v;
-        const uint16_t* ks = (const uint16_t*)(b + p.cache.key_scales_at() + p.cache.scale_run(t)) + (t & 3);
-        const uint16_t* vs = (const uint16_t*)(b + p.cache.value_scales_at() + p.cache.scale_run(t));
+        const uint8_t* b = p.cache.block(bad ? 0 : pid, h);
+        kw = ((const Loose<WT, uint32_t>*)(b + t * 16 * C + k_at))->v;
+        vw = ((const Loose<WT, uint32_t>*)(b + p.cache.values_at() + t * 16 * C + v_at))->v;
+        const uint8_t *ks = b + p.cache.key_scales_at() + p.cache.scale_run(t), *vs = b + p.cache.value_scales_at() + p.cache.scale_run(t);
+        const uint32_t run = (in16 >> 2) * 8 * C;
 #pragma unroll
         for (int u = 0; u < NK; u++) {
-            ka[u] = ks[4 * min(gk + a4 % CT + 4 * u, C - 1)];
+            ka[u] = *(const uint16_t*)(ks + (run + 8 * min(gk + a4 % CT + 4 * u, C - 1) + 2 * (in16 & 3)));
             if (bad) ka[u] = 0x7fc0u;
             if (j0 + key >= keys) ka[u] = 0;      // scales behind the last key may be anything
         }
 #pragma unroll
         for (int u = 0; u < NV; u++) {
             const int n = min(a16 + 16 * u, 4 * C - 1);
-            va[u] = vs[n];
+            va[u] = *(const uint16_t*)(vs + (run + 2 * n));
             if (j0 + 4 * run4 + (n & 3) >= keys) va[u] = 0;
         }
     };
