@@ -39,21 +39,28 @@ template <typename T> __device__ __forceinline__ bool finite(T v) {
     return (__builtin_bit_cast(uint16_t, v) & e) != e;
 }
 
-template <typename T, int DP, int KT, bool DMA>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionParams p) {
+// KS: sets of four waves that take every KS-th tile, each in stages of its own, and join their sums at the end.
+template <typename T, int DP, int KT, int KS, bool DMA>
+__global__ __launch_bounds__(256 * KS, DP == 256 ? 1 : 2) void k_attention(AttentionParams p) {
     typedef typename Vec8<T>::type V;
     constexpr int R = 128, P = DP / 8, NP = KT * P / 256, DB = DP / 32;
-    __shared__ V tiles[2][2][KT * P];      // two stages of keys and values
+    __shared__ V all_tiles[KS][2][2][KT * P];      // two stages of keys and values
+    __shared__ float2 other_stats[KS == 2 ? 256 : 1];
     __shared__ int odd;                    // some tile with masks holds values that are not finite
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    const int set = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    V (&tiles)[2][2][KT * P] = all_tiles[set];
     const int h = blockIdx.x % p.k.heads;
     const int64_t slot = gridDim.x / p.k.heads - 1 - blockIdx.x / p.k.heads;      // the longest rows first
+    const int k_start = p.seqs < 64 ? p.k_starts[min(lane, p.seqs)] : 0;
     const Tile t = find_tile(p.q_starts, p.seqs, p.q_tokens, p.group, R, slot, nullptr, nullptr);
     const int n = (int)(t.end - t.begin), rows = n * p.group;
     if (t.index < 0 || (int64_t)t.index * R >= rows) return;
     const int row0 = t.index * R;
-    const int64_t ka = min(max((int64_t)p.k_starts[t.seq], (int64_t)0), p.k_tokens);
-    const int nk = (int)(min(max((int64_t)p.k_starts[t.seq + 1], ka), p.k_tokens) - ka);
+    const int k_from = p.seqs < 64 ? __builtin_amdgcn_readlane(k_start, t.seq) : p.k_starts[t.seq];
+    const int k_to = p.seqs < 64 ? __builtin_amdgcn_readlane(k_start, t.seq + 1) : p.k_starts[t.seq + 1];
+    const int64_t ka = min(max((int64_t)k_from, (int64_t)0), p.k_tokens);
+    const int nk = (int)(min(max((int64_t)k_to, ka), p.k_tokens) - ka);
     const int ahead = p.causal ? nk - n : nk;        // query i sees keys up to i + ahead
     auto last_of = [&](int r) { return min(r / p.group + ahead, nk - 1); };
     const int keys = last_of(min(row0 + R, rows) - 1) + 1;
@@ -130,26 +137,28 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
         return __builtin_bit_cast(V, v);
     };
     if (tid == 0) odd = 0;
-    if (keys > 0) fetch(0, 0);
-    for (int j0 = 0, stage = 0; j0 < keys; j0 += KT, stage ^= 1) {
+    if (KT * set < keys) fetch(KT * set, 0);
+    for (int first = 0, stage = 0; first < keys; first += KT * KS, stage ^= 1) {
+        const int j0 = first + KT * set;
         if (DMA) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wave's part of the tile
         __syncthreads();                                  // everyone's; and no one reads the other stage any more
-        if (j0 + KT < keys) fetch(j0 + KT, stage ^ 1);
+        if (j0 + KT * KS < keys) fetch(j0 + KT * KS, stage ^ 1);
         const V* kt = tiles[stage][0];
         V* vt = tiles[stage][1];
-        if (j0 + KT - 1 > open) {
+        if (first + KT * KS - 1 > open) {
             // values that are not finite would reach every row: zeros here, the rows that see them below
             bool mine = false;
+            if (j0 < keys)
 #pragma unroll 1
-            for (int u = 0; u < NP; u++) {
-                V v = vt[tid + 256 * u];
-                bool any = false;
+                for (int u = 0; u < NP; u++) {
+                    V v = vt[tid + 256 * u];
+                    bool any = false;
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if (!finite(v[i])) v[i] = (T)0.0f, any = true;
-                if (any) vt[tid + 256 * u] = v;
-                mine |= any;
-            }
+                    for (int i = 0; i < 8; i++)
+                        if (!finite(v[i])) v[i] = (T)0.0f, any = true;
+                    if (any) vt[tid + 256 * u] = v;
+                    mine |= any;
+                }
             if (mine) odd = 1;
             __syncthreads();
         }
@@ -158,10 +167,33 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attention(AttentionP
         fl.weights(p.scale, j0 + KT - 1 > wave_open, last - j0 - 4 * half);
         fl.products([&](int r, int d) { return values(vt, r, d); });
     }
-    if (keys > 0) __syncthreads();
+    if constexpr (KS == 2) {
+        __syncthreads();
+        float* other = (float*)all_tiles + tid;
+        if (set == 1) {
+            other_stats[tid] = make_float2(fl.top, fl.sum);
+#pragma unroll
+            for (int d = 0; d < DB; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) other[256 * (16 * d + i)] = fl.acc[d][i];
+        }
+        __syncthreads();
+        if (set == 1) return;
+        const float2 o = other_stats[tid];
+        const float now = fmaxf(fl.top, o.x);
+        const float f = fl.top == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(fl.top - now);
+        const float g = o.x == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(o.x - now);
+        fl.sum = fl.sum * f + o.y * g;
+#pragma unroll
+        for (int d = 0; d < DB; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) fl.acc[d][i] = fl.acc[d][i] * f + other[256 * (16 * d + i)] * g;
+    } else if (keys > 0) {
+        __syncthreads();
+    }
     if (keys > 0 && odd) {
         // a multiple of a number that overflows for every such value that a row sees, by products with ones
-        const int from = max(open + 1, 0) / KT * KT;
+        const int from = max(open + 1, 0) / (KT * KS) * (KT * KS);
 #pragma unroll
         for (int d = 0; d < DB; d++) {
             f32x16 up = {}, down = {};
@@ -215,8 +247,16 @@ template <typename T, int DP, int KT>
 hipError_t launch_d(const AttentionParams& p, hipStream_t s) {
     const int64_t slots = p.q_tokens * p.group / 128 + p.seqs;
     const unsigned grid = (unsigned)(slots * p.k.heads);
-    if (dma_takes<T>(p.k) && dma_takes<T>(p.v)) k_attention<T, DP, KT, true><<<grid, 256, 0, s>>>(p);
-    else k_attention<T, DP, KT, false><<<grid, 256, 0, s>>>(p);
+    const bool dma = dma_takes<T>(p.k) && dma_takes<T>(p.v);
+    // Few workgroups: their keys in two sets of waves.  Long heads have no registers for a second set.
+    if constexpr (DP < 256)
+        if (grid <= 2u * num_cus() && p.k_tokens >= (int64_t)256 * p.seqs) {
+            if (dma) k_attention<T, DP, KT, 2, true><<<grid, 512, 0, s>>>(p);
+            else k_attention<T, DP, KT, 2, false><<<grid, 512, 0, s>>>(p);
+            return hipGetLastError();
+        }
+    if (dma) k_attention<T, DP, KT, 1, true><<<grid, 256, 0, s>>>(p);
+    else k_attention<T, DP, KT, 1, false><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 

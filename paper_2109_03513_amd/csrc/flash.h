@@ -47,14 +47,14 @@ template <typename T, int DP, int KT> struct Flash {
     __device__ __forceinline__ void scores(const V* kt) {
         const int col = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-        for (int b = 0; b < KB; b++) {
-            x[b] = f32x16{};
+        for (int b = 0; b < KB; b++) x[b] = f32x16{};
 #pragma unroll
-            for (int s = 0; s < DP / 16; s++) {
+        for (int s = 0; s < DP / 16; s++)
+#pragma unroll
+            for (int b = 0; b < KB; b++) {
                 const int r = 32 * b + col;
                 x[b] = mma(kt[r * P + ((2 * s + half) ^ key_turn<DP>(r))], qf[s], x[b]);
             }
-        }
     }
 
     // What exp makes of them.  masks: keys after `end`, counted from 4 (lane / 32), are not seen.
