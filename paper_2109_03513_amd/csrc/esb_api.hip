@@ -857,7 +857,7 @@ static HeadsView view(const esb_heads* v) {
 static int turn_check(HeadsParams* p, const float* q_w, const float* k_w, float eps, const esb_rotation* r) {
     if (!(eps >= 0.0f) || eps == INFINITY || (eps == 0.0f && (q_w || k_w))) return ESB_E_INVALID;
     if ((uintptr_t)q_w % 4 || (uintptr_t)k_w % 4) return ESB_E_INVALID;
-    p->qw = q_w, p->kw = k_w, p->eps = eps;
+    p->qw = q_w, p->kw = k_w, p->eps = eps, p->inv_d = 1.0 / p->d;
     if (!r || r->rot == 0) return ESB_OK;
     if (r->rot < 0 || r->rot > p->d || r->rot % 2 || r->rows < 0) return ESB_E_INVALID;
     if (p->tokens > 0 && (!r->positions || (uintptr_t)r->positions % 4 || (r->rows > 0 && !r->table) ||

@@ -49,16 +49,17 @@ __device__ __forceinline__ void store_codes(const Kv4Layout& L, uint8_t* b, int 
     }
 }
 
-// Codes of eight elements y under the scale a.
+// Codes of eight elements y under the scale a.  The borders are exact in fp32: three bits times eight.
 __device__ __forceinline__ uint32_t nibbles(f32x8 y, float a) {
+    const float b1 = 0.25f * a, b2 = 0.75f * a, b3 = 1.25f * a, b4 = 1.75f * a, b5 = 2.5f * a, b6 = 3.5f * a, b7 = 5.0f * a;
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const float v = fabsf(y[i]);
-        // the borders are exact in fp32: three bits times eight
-        const uint32_t c = (v >= 0.25f * a) + (v >= 0.75f * a) + (v >= 1.25f * a) + (v >= 1.75f * a) +
-                           (v >= 2.5f * a) + (v >= 3.5f * a) + (v >= 5.0f * a);
-        w |= (c | (y[i] < 0.0f && c ? 8u : 0u)) << (4 * i);
+        const bool c4 = v >= b4, c2 = v >= (c4 ? b6 : b2);
+        const bool c1 = v >= (c4 ? (c2 ? b7 : b5) : (c2 ? b3 : b1));
+        const uint32_t c = (c4 ? 4u : 0u) + (c2 ? 2u : 0u) + (c1 ? 1u : 0u);
+        w |= (c ? c | (__float_as_uint(y[i]) >> 28 & 8u) : 0u) << (4 * i);
     }
     return w;
 }
@@ -108,6 +109,14 @@ template <int LPR> __device__ __forceinline__ double lanes_sum(double v) {
     return v;
 }
 
+// 1 / sqrt(x) for positive x, by the hardware's approximation and two Newton steps: within a few 2^-53.
+__device__ __forceinline__ double reciprocal_root(double x) {
+    const double y0 = __builtin_amdgcn_rsq(x);
+    const double y1 = fma(0.5 * y0, fma(-x * y0, y0, 1.0), y0);
+    const double y2 = fma(0.5 * y1, fma(-x * y1, y1, 1.0), y1);
+    return x < __builtin_inf() ? y2 : y0;      // 0 for infinity
+}
+
 // v in the precision of the work.  For fp64 anew wherever it is used: kept over a wave's steps, the wider copies
 // of weights and table would cost it half its registers.
 template <typename A> __device__ __forceinline__ A wide(float v) {
@@ -142,21 +151,10 @@ __global__ __launch_bounds__(256) void k_heads(HeadsParams p, int64_t token0, ui
     } else {
         ea = rot + 16 * (l - turning), eb = ea + 8, na = d - ea, nb = d - eb, pair = half;
     }
-    const int64_t pos = rot && from < qs + ks ? p.positions[t] : 0;
-    const bool known = !rot || (pos >= 0 && pos < p.rows);
-    const int turns = half - pair;      // the lane's pairs that are rotated, from the first on
-    f32x8 c = {}, s = {};
-    if (known && turns > 0 && from < qs + ks) {
-        const float* row = p.table + pos * rot;
-        c = load8(row + pair, turns), s = load8(row + half + pair, turns);
-    }
-    int64_t slot = -1;
-    bool there = false;
-    if (CACHE) {
-        slot = p.slots[t];
-        there = slot >= 0 && (slot >> p.cache.shift) < p.cache.pages;
-    }
-
+    // the position, the slot and the first heads are asked for at once, then the table's row
+    const bool turned_step = from < qs + ks;
+    const int64_t pos = rot && turned_step ? p.positions[t] : 0;
+    const int64_t slot = CACHE ? p.slots[t] : -1;
     struct In {
         V a, b;
     };
@@ -181,6 +179,14 @@ __global__ __launch_bounds__(256) void k_heads(HeadsParams p, int64_t token0, ui
         return in;
     };
     In next = load(from);
+    const bool known = !rot || (pos >= 0 && pos < p.rows);
+    const bool there = CACHE && slot >= 0 && (slot >> p.cache.shift) < p.cache.pages;
+    const int turns = half - pair;      // the lane's pairs that are rotated, from the first on
+    f32x8 c = {}, s = {};
+    if (known && turns > 0 && turned_step) {
+        const float* row = p.table + pos * rot;
+        c = load8(row + pair, turns), s = load8(row + half + pair, turns);
+    }
     int weights_of = -1;
     f32x8 wa, wb;
     for (int i = from; i < to; i++) {
@@ -209,7 +215,7 @@ __global__ __launch_bounds__(256) void k_heads(HeadsParams p, int64_t token0, ui
                 ss = fma(a, a, fma(b, b, ss));
             }
             ss = lanes_sum<LPR>(ss);
-            rstd = (A)(1.0 / sqrt(ss / (double)d + (double)p.eps));
+            rstd = (A)reciprocal_root(fma(ss, p.inv_d, (double)p.eps));
         }
         if (!known) rstd = (A)__builtin_nan("");
         // element k of the lane's first run and of its second, normed
@@ -322,8 +328,8 @@ hipError_t launch_n(const HeadsParams& p, hipStream_t s) {
     constexpr int HW = 64 / LPR;
     auto steps = [](int heads) { return (heads + HW - 1) / HW; };
     const int64_t all = (int64_t)steps(p.q.heads) + steps(p.k.heads) + (CACHE ? steps(p.v.heads) : 0);
-    // one step a wave while that makes up to eight waves a SIMD
-    const int64_t most_waves = 32 * num_cus();
+    // one step a wave while that makes up to four waves a SIMD, about what the registers allow
+    const int64_t most_waves = 16 * num_cus();
     int64_t per = (p.tokens * all + most_waves - 1) / most_waves;
     if (per > all) per = all;
     const int64_t parts = (all + per - 1) / per, most = ((int64_t)1 << 28) / parts;      // tokens of one launch

@@ -43,6 +43,7 @@ struct HeadsParams {
     const float* qw;                // norm weights, or NULL (ones)
     const float* kw;
     float eps;                      // 0: no norm
+    double inv_d;                   // 1 / d
     const float* table;             // rows x rot: cosines, then sines
     int64_t rows;
     int rot, adjacent;              // rot 0: no rotation
