@@ -690,7 +690,7 @@ int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, u
  *   lengths  device, one per sequence;
  *   pages    device, seqs rows of `columns` page numbers, pitch page_pitch; entries behind a
  *            sequence's last key may hold anything;
- *   scale    positive and finite.
+ *   scale    positive, and finite times log2(e).
  * A query that sees no key gets zeros.  What lies in the cache behind what a query sees does not
  * reach it.  A length beyond columns * page makes the sequence's outputs NaN, a page number that is
  * not the cache's those of the queries that see it.  Scores, statistics and sums are fp32; the
@@ -720,7 +720,7 @@ int esb_kv4_attention(const esb_heads* q, int type, int64_t tokens, const esb_kv
  *   q_starts, k_starts  device, seqs + 1 each, ascending; k_starts NULL: q_starts (then k_tokens
  *            == q_tokens).  Query rows past the last sequence are left as they were;
  *   d        a multiple of 8, at most 256 (else ESB_E_UNSUPPORTED); ESB_BF16 or ESB_F16.
- * A query that sees no key gets zeros; infinities and NaN in keys and values reach only the
+ * out may not be the buffer of q, k or v.  A query that sees no key gets zeros; infinities and NaN in keys and values reach only the
  * queries that see them.  Probabilities enter the matrix cores in `type`; the rest is fp32.
  */
 int esb_attention(const esb_heads* q, const esb_heads* k, const esb_heads* v, int type,

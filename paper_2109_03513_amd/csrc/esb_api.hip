@@ -959,7 +959,7 @@ int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, u
 static int attention_check(int type, int64_t tokens, int q_heads, int kv_heads, int seqs, float scale) {
     if (type == ESB_F32) return ESB_E_UNSUPPORTED;
     if ((type != ESB_BF16 && type != ESB_F16) || tokens < 0 || seqs < 0) return ESB_E_INVALID;
-    if (!(scale > 0.0f) || scale == INFINITY) return ESB_E_INVALID;
+    if (!(scale > 0.0f) || scale * kLog2E == INFINITY) return ESB_E_INVALID;
     if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads) return ESB_E_INVALID;
     if (tokens > INT32_MAX || tokens * q_heads > INT32_MAX || (tokens + seqs) * q_heads > INT32_MAX)
         return ESB_E_UNSUPPORTED;
@@ -1014,7 +1014,8 @@ int esb_attention(const esb_heads* q, const esb_heads* k, const esb_heads* v, in
     if (q->heads != out->heads || k->heads != v->heads) return ESB_E_INVALID;
     if (!k_starts && k_tokens != q_tokens) return ESB_E_INVALID;
     if (q_tokens == 0 || seqs == 0) return ESB_OK;
-    if (!q_starts || (uintptr_t)q_starts % 4 || (uintptr_t)k_starts % 4 || q->data == out->data) return ESB_E_INVALID;
+    if (!q_starts || (uintptr_t)q_starts % 4 || (uintptr_t)k_starts % 4) return ESB_E_INVALID;
+    if (out->data == q->data || out->data == k->data || out->data == v->data) return ESB_E_INVALID;
     AttentionParams p = {};
     p.q = view(q), p.k = view(k), p.v = view(v), p.o = view(out);
     p.q_tokens = q_tokens, p.k_tokens = k_tokens, p.d = d, p.group = q->heads / k->heads, p.seqs = seqs;

@@ -155,7 +155,8 @@ def test_attention(esb):
     for bad in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(t=E4M3), dict(nq=-1), dict(nk=-1), dict(d=0),
                 dict(seqs=-1), dict(qs=None), dict(qs=ODD), dict(ks=ODD), dict(nk=4), dict(scale=0.0),
                 dict(scale=float("nan")), dict(k=H(n=3), v=H(n=3)), dict(v=H(n=2)), dict(o=H(n=4, data=OTHER)),
-                dict(o=H(n=8)), dict(k=H(data=None)), dict(q=H(n=8, data=ODD)), dict(o=H(n=8, data=OTHER, head=0))):
+                dict(o=H(n=8)), dict(k=H(data=None)), dict(q=H(n=8, data=ODD)), dict(o=H(n=8, data=OTHER, head=0)), dict(scale=3e38),
+                dict(k=H(data=OTHER)), dict(v=H(data=OTHER))):
         assert attend(**bad) == INVALID, bad
     assert attend(t=F32) == UNSUPPORTED
     assert attend(d=60) == UNSUPPORTED and attend(d=264) == UNSUPPORTED
