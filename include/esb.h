@@ -699,9 +699,10 @@ int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, u
  *   workspace  device, 256-byte aligned, esb_kv4_attention_workspace_size() bytes (0 where keys
  *              are not split over workgroups).  It carries nothing between calls; concurrent calls
  *              need distinct ones.  Less or NULL: ESB_E_WORKSPACE.
- * The order of sums is fixed by the sizes: the same call gives the same bits.
+ * The order of sums is fixed by the sizes, the starts and the lengths: the same call gives the
+ * same bits, and the last bits of a sequence's outputs may be others beside other sequences.
  * ESB_E_UNSUPPORTED: 2^31 or more rows (tokens x heads) or workgroups, columns * page above
- * 2^31 - 8193.
+ * 2^31 - 8193, or more work than 2^30 steps (of 128 keys of a tile of rows).
  * tokens == 0 or seqs == 0 enqueues nothing.
  */
 size_t esb_kv4_attention_workspace_size(int64_t tokens, int q_heads, int d, int kv_heads, int seqs,
@@ -720,8 +721,9 @@ int esb_kv4_attention(const esb_heads* q, int type, int64_t tokens, const esb_kv
  *   q_starts, k_starts  device, seqs + 1 each, ascending; k_starts NULL: q_starts (then k_tokens
  *            == q_tokens).  Query rows past the last sequence are left as they were;
  *   d        a multiple of 8, at most 256 (else ESB_E_UNSUPPORTED); ESB_BF16 or ESB_F16.
- * out may not be the buffer of q, k or v.  A query that sees no key gets zeros; infinities and NaN in keys and values reach only the
- * queries that see them.  Probabilities enter the matrix cores in `type`; the rest is fp32.
+ * out may not be the buffer of q, k or v.  A query that sees no key gets zeros; infinities and NaN
+ * in keys and values reach only the queries that see them.  Probabilities enter the matrix cores in
+ * `type`; the rest is fp32.
  */
 int esb_attention(const esb_heads* q, const esb_heads* k, const esb_heads* v, int type,
                   int64_t q_tokens, int64_t k_tokens, int d, int seqs, const int32_t* q_starts,

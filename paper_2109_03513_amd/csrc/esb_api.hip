@@ -990,6 +990,8 @@ int esb_kv4_attention(const esb_heads* q, int type, int64_t tokens, const esb_kv
     if (!lengths || (columns > 0 && (!pages || cache->pages == 0)) || (uintptr_t)starts % 4 || (uintptr_t)lengths % 4 ||
         (uintptr_t)pages % 4 || (uintptr_t)workspace % 256 || q->data == out->data)
         return ESB_E_INVALID;
+    if (!kv4_attention_counts(tokens, q->heads, d, cache->heads, seqs, starts != nullptr, (int64_t)columns * cache->page))
+        return ESB_E_UNSUPPORTED;
     const size_t need = esb_kv4_attention_workspace_size(tokens, q->heads, d, cache->heads, seqs, starts != nullptr,
                                                          columns, cache->page);
     if (need && (!workspace || ws_bytes < need)) return ESB_E_WORKSPACE;

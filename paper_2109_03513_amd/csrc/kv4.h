@@ -78,7 +78,9 @@ struct Kv4AttentionParams {
 // How a call is split, from what the host knows (kv4_attention.hip).
 struct Kv4Split {
     int kind;            // kKv4Few, kKv4Some, kKv4Many: which kernel
-    int NT, tiles;       // row tiles of a wave; tiles of a sequence of one query
+    int NT, R;           // row tiles of a wave; rows of a workgroup
+    int count;           // workgroups that share the work evenly; 0: each has a run of a tile's keys
+    int tiles;           // tiles of a sequence of one query
     int64_t slots;       // tiles of all sequences
     int run, chunks;     // keys of a workgroup, and how many there are of such runs
 };
@@ -88,6 +90,8 @@ hipError_t launch_kv4_many(int type, const Kv4AttentionParams& p, const Kv4Split
                            hipStream_t s);
 size_t kv4_attention_workspace(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts,
                                int64_t longest);
+// Whether the call's workgroups and units of work are within 32 bits.
+bool kv4_attention_counts(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts, int64_t longest);
 hipError_t launch_kv4_attention(int type, const Kv4AttentionParams& p, hipStream_t s);
 
 // Attention over packed prompts (attention.hip).
@@ -175,5 +179,108 @@ __device__ __forceinline__ Rows find_rows(const Kv4AttentionParams& p, int64_t s
     r.len = r.bad || len < 0 ? 0 : (int)len;
     return r;
 }
+
+// Work shared evenly: a unit is 128 keys of one item (tile of R rows, key head, sequence), units are numbered through
+// the items, sequences first, then heads, then tiles, and workgroup w of `count` has the units from w * per on,
+// whatever items they belong to.  Every wave works this out by itself from the starts and lengths, a sequence to a
+// lane, and keeps it in LDS, as registers are short in the loops between.
+struct Kv4Item {
+    Rows rw;
+    int h, begin, end;     // the key head; the item's units
+    int from, to;          // its units that were asked for
+};
+// The sum of v over the lanes up to each: within rows of sixteen, then from row to row.
+__device__ __forceinline__ int scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // from the lane 1, 2, 4, 8 below
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // rows 1 and 3: the last of the row before
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // rows 2 and 3: lane 31
+}
+
+struct Kv4Walk {
+    const Kv4AttentionParams& p;
+    int (*const kept)[64];            // the wave's, of 64 sequences: units to its end, tiles, steps, queries, keys, begin
+    const int R;
+    int total, per;                   // units, and of a workgroup
+    int s0, before, units;            // the first of those sequences, units before it and of the 64
+
+    __device__ __forceinline__ Kv4Walk(const Kv4AttentionParams& q, int (*lds)[6][64], int rows_of_tile, int count)
+        : p(q), kept(lds[threadIdx.x >> 6]), R(rows_of_tile) {
+        asm volatile("" ::"s"(count));      // asked for with the first arguments, not when it is used
+        total = 0;
+        bool falls = false;
+        for (int s = 0; s < p.seqs; s += 64) {
+            falls |= look(s);
+            total += units;
+        }
+        if (falls) total = 0;      // starts that do not ascend: nothing, as their sum may pass the tokens
+        per = (unsigned)(total + count - 1) / (unsigned)count;
+        before = 0;
+        if (p.seqs > 64) s0 = -64, units = 0;
+    }
+    __device__ __forceinline__ bool look(int first) {
+        const int lane = threadIdx.x & 63, s = first + lane, at = min(s, p.seqs - 1);
+        int64_t a = at, b = at + 1;
+        bool falls = false;
+        if (p.starts) {
+            a = p.starts[at], b = p.starts[at + 1], falls = __any(b < a);
+            a = min(max(a, (int64_t)0), p.tokens), b = min(max(b, a), p.tokens);
+        }
+        const int64_t keys = p.lengths[at];
+        const bool fits = keys <= (int64_t)p.columns * p.cache.page;
+        const int len = fits ? (int)max(keys, (int64_t)0) : -1;      // -1: passes its pages
+        const int n = (int)(b - a), tiles = s < p.seqs ? (int)((unsigned)(n * p.group + R - 1) / (unsigned)R) : 0;
+        const int steps = max((len + 127) >> 7, 1);
+        const int u = scan(tiles * p.cache.heads * steps);
+        kept[0][lane] = u, kept[1][lane] = tiles, kept[2][lane] = steps;
+        kept[3][lane] = n, kept[4][lane] = len, kept[5][lane] = (int)a;
+        __builtin_amdgcn_wave_barrier();
+        s0 = first, units = __builtin_amdgcn_readlane(u, 63);
+        return falls;
+    }
+    // The item of unit u, not below those asked for before; of its units those up to `end`.
+    __device__ __forceinline__ Kv4Item item(int u, int end) {
+        while (u >= before + units) {
+            before += units;
+            look(s0 + 64);
+        }
+        const int l = __builtin_ctzll(__ballot(u < before + kept[0][threadIdx.x & 63]));
+        const int t = of(1, l), k = of(2, l);
+        Kv4Item it = numbered(l, (unsigned)(u - before - of(0, l) + t * p.cache.heads * k) / (unsigned)k);
+        it.from = u, it.to = min(it.end, end);
+        return it;
+    }
+    // Item `number` of all, or one of no units.
+    __device__ __forceinline__ Kv4Item item(int number) {
+        if (s0 < 0) look(0);
+        for (;;) {
+            const int items = scan(kept[1][threadIdx.x & 63] * p.cache.heads);
+            const uint64_t has = __ballot(number < items);
+            if (has) {
+                const int l = __builtin_ctzll(has);
+                return numbered(l, number - __builtin_amdgcn_readlane(items, l) + of(1, l) * p.cache.heads);
+            }
+            if (s0 + 64 >= p.seqs) return Kv4Item{};
+            number -= __builtin_amdgcn_readlane(items, 63), before += units;
+            look(s0 + 64);
+        }
+    }
+
+  private:
+    __device__ __forceinline__ int of(int what, int l) { return __builtin_amdgcn_readfirstlane(kept[what][l]); }
+    // Item `number` of lane l's sequence.
+    __device__ __forceinline__ Kv4Item numbered(int l, int number) {
+        Kv4Item it;
+        const int t = of(1, l), k = of(2, l), len = of(4, l);
+        it.h = (unsigned)number / (unsigned)t;
+        it.begin = it.from = before + of(0, l) - (t * p.cache.heads - number) * k, it.end = it.to = it.begin + k;
+        it.rw.seq = s0 + l, it.rw.n = of(3, l), it.rw.begin = of(5, l);
+        it.rw.bad = len < 0, it.rw.len = max(len, 0);
+        it.rw.rows = it.rw.n * p.group, it.rw.row0 = (number - it.h * t) * R;
+        return it;
+    }
+};
 
 }  // namespace esb

@@ -10,10 +10,12 @@
 // the sum of two bf16, one more MFMA): 2^-9 of each of the terms that a softmax averages, which is
 // below the rounding of a bf16 output.
 //
-// A workgroup takes 16 NT rows (queries x heads that share a key head) and a run of keys; its four
+// A workgroup takes 16 NT rows (queries x heads that share a key head) and some of their keys; its four
 // waves take every fourth step of 32 keys, each with its own running maximum and sum, and join them in
-// LDS.  Few rows: the keys are split over workgroups too and k_join adds the parts.  The running
-// maximum moves only when a score passes it by 2^8, so most steps cross no lanes.
+// LDS.  The keys are split over workgroups too, in runs or in even shares of all work (split() below),
+// and a k_join_... adds the parts.  The running maximum moves only when a score passes it by 2^8, so
+// most steps cross no lanes.
+#include <algorithm>
 #include <type_traits>
 
 #include "flash.h"
@@ -21,6 +23,8 @@
 namespace esb {
 
 namespace {
+
+constexpr int kRuns = 16;      // parts of a row that one thread joins, at most
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int N> struct Words {
@@ -92,245 +96,288 @@ template <int CP> struct Step {
     int bad;             // halves whose page is none of the cache's
 };
 
+// What a workgroup has: keys from .. to - 1 of a tile of rows and a head, item by item.  EVEN: its share of all
+// units; else one run of keys, chosen by the host.
+template <bool EVEN> struct Work {
+    Kv4Walk walk;
+    int unit, first, last;
+    Rows rw;
+    int h, from, to, place;
+    bool whole;                       // no other workgroup has keys of it
+    __device__ __forceinline__ Work(const Kv4AttentionParams& p, const Kv4Split& sp, int R, int (*kept)[6][64])
+        : walk(p, kept, R, sp.count) {
+        first = unit = (int)blockIdx.x * walk.per, last = min(unit + walk.per, walk.total);
+    }
+    __device__ __forceinline__ bool next() {
+        if (unit >= last) return false;
+        const Kv4Item it = walk.item(unit, last);
+        unit = it.to;
+        rw = it.rw, h = it.h, from = 128 * (it.from - it.begin), to = 128 * (it.to - it.begin);
+        whole = it.from == it.begin && it.to == it.end;
+        place = 2 * blockIdx.x + (it.begin > first ? 1 : 0);      // what began before or with its units: 0
+        return true;
+    }
+};
+template <> struct Work<false> {
+    Rows rw;
+    int h, from, to, place;
+    bool whole, more;
+    __device__ __forceinline__ Work(const Kv4AttentionParams& p, const Kv4Split& sp, int R, int (*)[6][64]) {
+        int64_t id = blockIdx.x;
+        place = (int)(id % sp.chunks);
+        id /= sp.chunks;
+        h = (int)(id % p.cache.heads);
+        rw = find_rows(p, id / p.cache.heads, sp.tiles, R);
+        from = place * sp.run, to = from + sp.run, whole = sp.chunks == 1, more = rw.row0 < rw.rows;
+    }
+    __device__ __forceinline__ bool next() {
+        const bool had = more;
+        more = false;
+        return had;
+    }
+};
+
 // CP: the head's groups, padded (FULL: exactly).  What is padded meets zeros of the query, or makes outputs that
 // are not stored; its scales repeat the last group's.
-template <typename T, int CP, int NT, bool FULL>
-__global__ __launch_bounds__(256) void k_kv4(Kv4AttentionParams p, int run, int chunks, int tiles, float* part,
-                                             float2* stats) {
+template <typename T, int CP, int NT, bool FULL, bool EVEN>
+__global__ __launch_bounds__(256, CP * NT <= 2 ? 3 : CP * NT <= 4 ? 2 : 1)
+void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
     typedef typename Vec8<T>::type V;
     constexpr int R = 16 * NT;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
     const int C = FULL ? CP : p.cache.groups;
-    int64_t id = blockIdx.x;
-    const int chunk = (int)(id % chunks);
-    id /= chunks;
-    const int h = (int)(id % p.cache.heads);
-    const Rows rw = find_rows(p, id / p.cache.heads, tiles, R);
-    if (rw.row0 >= rw.rows) return;
-
-    // the first pages and the queries are asked for before the sequence's length is there
-    const int32_t* table = p.table + rw.seq * p.table_pitch;
-    const int page = p.cache.page;
-    struct Ids {
-        int a, b;
-    };
-    auto ids = [&](int at) {      // pages of the halves of a step; behind the last key whatever the table holds
-        return Ids{table[min(at >> p.cache.shift, p.columns - 1)], table[min((at + 16) >> p.cache.shift, p.columns - 1)]};
-    };
-    const int at0 = chunk * run + 32 * wave;
-    Ids next = p.columns > 0 ? ids(at0) : Ids{0, 0};
-    V qf[NT][CP];
+    __shared__ int kept[EVEN ? 4 : 1][6][64];
+    asm volatile("" ::"s"(part), "s"(stats));      // asked for with the first arguments, not when they are used
+    Work<EVEN> work(p, sp, R, kept);
+    while (work.next()) {
+        const Rows& rw = work.rw;
+        const int h = work.h;
+        const int32_t* table = p.table + rw.seq * p.table_pitch;
+        const int page = p.cache.page;
+        struct Ids {
+            int a, b;
+        };
+        auto ids = [&](int at) {      // pages of the halves of a step; behind the last key whatever the table holds
+            return Ids{table[min(at >> p.cache.shift, p.columns - 1)],
+                       table[min((at + 16) >> p.cache.shift, p.columns - 1)]};
+        };
+        const int at0 = work.from + 32 * wave;
+        Ids next = p.columns > 0 ? ids(at0) : Ids{0, 0};
+        V qf[NT][CP];
 #pragma unroll
-    for (int u = 0; u < NT; u++) {
-        const int r = rw.row0 + 16 * u + i, t = r / p.group;
-        const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
-#pragma unroll
-        for (int s = 0; s < CP; s++) {
-            qf[u][s] = V{};
-            if (r < rw.rows && s < C) qf[u][s] = load8(q + 32 * s + 8 * g, 8);
-        }
-    }
-
-    const int first = rw.len - rw.n;                    // the last key of query t is first + t
-    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
-    const int k0 = chunk * run, k1 = min(k0 + run, keys);
-    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
-    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
-
-    int last[NT];
-#pragma unroll
-    for (int u = 0; u < NT; u++) last[u] = first + (rw.row0 + 16 * u + i) / p.group;
-
-    auto load = [&](int at, Ids pg) {
-        Step<CP> st;
-        st.bad = 0;
-#pragma unroll
-        for (int hh = 0; hh < 2; hh++) {
-            int pid = __builtin_amdgcn_readfirstlane(hh ? pg.b : pg.a);
-            if (pid < 0 || pid >= p.cache.pages) pid = 0, st.bad |= 1 << hh;
-            const uint8_t* b = p.cache.block(pid, h);
-            const int t = (at + 16 * hh) & (page - 1);
-            // words past the head's groups are of what follows in the block, and nothing uses them
-            st.k[hh] = ((const Loose<typename Words<CP>::w, uint32_t>*)(b + (t + i) * 16 * C + g * 4 * C))->v;
-            st.v[hh] = ((const Loose<typename Words<CP>::w, uint32_t>*)(b + p.cache.values_at() + ((t >> 2) + g) * 64 * C +
-                                                            i * 4 * C))->v;
-            const uint8_t* ks = b + p.cache.key_scales_at() + ((t >> 2) + g) * 8 * C;
-            const uint8_t* vs = b + p.cache.value_scales_at() + ((t >> 2) + g) * 8 * C;
+        for (int u = 0; u < NT; u++) {
+            const int r = rw.row0 + 16 * u + i, t = r / p.group;
+            const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
 #pragma unroll
             for (int s = 0; s < CP; s++) {
-                const int g8 = FULL ? 8 * s : 8 * min(s, C - 1);
-                st.ka[hh][s] = *(const uint2*)(ks + g8);
-                st.va[hh][s] = *(const uint2*)(vs + g8);
+                qf[u][s] = V{};
+                if (r < rw.rows && s < C) qf[u][s] = load8(q + 32 * s + 8 * g, 8);
             }
         }
-        return st;
-    };
 
-    f32x4 acc[NT][CP][2] = {};
-    float top[NT], sum[NT];      // the running maximum (times scale) and the lane's part of the sum
-#pragma unroll
-    for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
+        const int first = rw.len - rw.n;                    // the last key of query t is first + t
+        const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
+        const int k1 = min(work.to, keys);
+        const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
 
-    auto compute = [&](const Step<CP>& st, int at, auto masks) {
-        constexpr bool MASK = decltype(masks)::value;
-        f32x4 x[NT][2];
+        int last[NT];
 #pragma unroll
-        for (int hh = 0; hh < 2; hh++)
+        for (int u = 0; u < NT; u++) last[u] = first + (rw.row0 + 16 * u + i) / p.group;
+
+        auto load = [&](int at, Ids pg) {
+            Step<CP> st;
+            st.bad = 0;
 #pragma unroll
-            for (int s = 0; s < CP; s++) {
-                const V kf = decode(st.k[hh][s], T{});
-                const f32x4 a = four(st.ka[hh][s]);
+            for (int hh = 0; hh < 2; hh++) {
+                int pid = __builtin_amdgcn_readfirstlane(hh ? pg.b : pg.a);
+                if (pid < 0 || pid >= p.cache.pages) pid = 0, st.bad |= 1 << hh;
+                const uint8_t* b = p.cache.block(pid, h);
+                const int t = (at + 16 * hh) & (page - 1);
+                // words past the head's groups are of what follows in the block, and nothing uses them
+                st.k[hh] = ((const Loose<typename Words<CP>::w, uint32_t>*)(b + (t + i) * 16 * C + g * 4 * C))->v;
+                st.v[hh] = ((const Loose<typename Words<CP>::w, uint32_t>*)(b + p.cache.values_at() + ((t >> 2) + g) * 64 * C +
+                                                                i * 4 * C))->v;
+                const uint8_t* ks = b + p.cache.key_scales_at() + ((t >> 2) + g) * 8 * C;
+                const uint8_t* vs = b + p.cache.value_scales_at() + ((t >> 2) + g) * 8 * C;
+#pragma unroll
+                for (int s = 0; s < CP; s++) {
+                    const int g8 = FULL ? 8 * s : 8 * min(s, C - 1);
+                    st.ka[hh][s] = *(const uint2*)(ks + g8);
+                    st.va[hh][s] = *(const uint2*)(vs + g8);
+                }
+            }
+            return st;
+        };
+
+        f32x4 acc[NT][CP][2] = {};
+        float top[NT], sum[NT];      // the running maximum (times scale) and the lane's part of the sum
+#pragma unroll
+        for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
+
+        auto compute = [&](const Step<CP>& st, int at, auto masks) {
+            constexpr bool MASK = decltype(masks)::value;
+            f32x4 x[NT][2];
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                for (int s = 0; s < CP; s++) {
+                    const V kf = decode(st.k[hh][s], T{});
+                    const f32x4 a = four(st.ka[hh][s]);
+#pragma unroll
+                    for (int u = 0; u < NT; u++) {
+                        const f32x4 z = mma(kf, qf[u][s], f32x4{0, 0, 0, 0});
+#pragma unroll
+                        for (int r = 0; r < 4; r++) x[u][hh][r] = s ? fmaf(a[r], z[r], x[u][hh][r]) : a[r] * z[r];
+                    }
+                }
+            float most[NT];
+            bool moves = false;
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                most[u] = kNegInf;
+#pragma unroll
+                for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        if (MASK) {
+                            if (st.bad >> hh & 1) x[u][hh][r] = __builtin_nanf("");
+                            if (at + 16 * hh + 4 * g + r > last[u]) x[u][hh][r] = kNegInf;
+                        }
+                        most[u] = fmaxf(most[u], x[u][hh][r]);
+                    }
+                most[u] *= p.scale;
+                moves |= passes(most[u], top[u]);
+            }
+            if (__ballot(moves)) {
 #pragma unroll
                 for (int u = 0; u < NT; u++) {
-                    const f32x4 z = mma(kf, qf[u][s], f32x4{0, 0, 0, 0});
+                    // row by row: what a row gives does not depend on its neighbours
+                    const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
+                    const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
+                    top[u] = now;
+                    sum[u] *= f;
 #pragma unroll
-                    for (int r = 0; r < 4; r++) x[u][hh][r] = s ? fmaf(a[r], z[r], x[u][hh][r]) : a[r] * z[r];
+                    for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
                 }
             }
-        float most[NT];
-        bool moves = false;
-#pragma unroll
-        for (int u = 0; u < NT; u++) {
-            most[u] = kNegInf;
-#pragma unroll
-            for (int hh = 0; hh < 2; hh++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    if (MASK) {
-                        if (st.bad >> hh & 1) x[u][hh][r] = __builtin_nanf("");
-                        if (at + 16 * hh + 4 * g + r > last[u]) x[u][hh][r] = kNegInf;
-                    }
-                    most[u] = fmaxf(most[u], x[u][hh][r]);
-                }
-            most[u] *= p.scale;
-            moves |= passes(most[u], top[u]);
-        }
-        if (__ballot(moves)) {
 #pragma unroll
             for (int u = 0; u < NT; u++) {
-                // row by row: what a row gives does not depend on its neighbours
-                const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
-                const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
-                top[u] = now;
-                sum[u] *= f;
+                const float m = top[u] == kNegInf ? 0.0f : top[u];
 #pragma unroll
-                for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
+                for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        x[u][hh][r] = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
+                        sum[u] += x[u][hh][r];
+                    }
             }
-        }
 #pragma unroll
-        for (int u = 0; u < NT; u++) {
-            const float m = top[u] == kNegInf ? 0.0f : top[u];
+            for (int c = 0; c < CP; c++) {
+                bf16x8 v0, v1;
+                value_pairs(st.v[0][c], st.v[1][c], &v0, &v1);
+                const f32x4 a0 = four(st.va[0][c]), a1 = four(st.va[1][c]);
 #pragma unroll
-            for (int hh = 0; hh < 2; hh++)
+                for (int u = 0; u < NT; u++) {
+                    f32x8 w;
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    x[u][hh][r] = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
-                    sum[u] += x[u][hh][r];
-                }
-        }
-#pragma unroll
-        for (int c = 0; c < CP; c++) {
-            bf16x8 v0, v1;
-            value_pairs(st.v[0][c], st.v[1][c], &v0, &v1);
-            const f32x4 a0 = four(st.va[0][c]), a1 = four(st.va[1][c]);
-#pragma unroll
-            for (int u = 0; u < NT; u++) {
-                f32x8 w;
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    w[r] = x[u][0][r] * a0[r];
-                    w[4 + r] = x[u][1][r] * a1[r];
-                    if (MASK) {      // scales behind the last key may be anything
-                        if (at + 4 * g + r > last[u]) w[r] = 0.0f;
-                        if (at + 16 + 4 * g + r > last[u]) w[4 + r] = 0.0f;
+                    for (int r = 0; r < 4; r++) {
+                        w[r] = x[u][0][r] * a0[r];
+                        w[4 + r] = x[u][1][r] * a1[r];
+                        if (MASK) {      // scales behind the last key may be anything
+                            if (at + 4 * g + r > last[u]) w[r] = 0.0f;
+                            if (at + 16 + 4 * g + r > last[u]) w[4 + r] = 0.0f;
+                        }
+                    }
+                    const bf16x8 hi = __builtin_convertvector(w, bf16x8);
+                    acc[u][c][0] = mma(v0, hi, acc[u][c][0]);
+                    acc[u][c][1] = mma(v1, hi, acc[u][c][1]);
+                    if (std::is_same<T, _Float16>::value) {
+                        const bf16x8 lo = __builtin_convertvector(w - __builtin_convertvector(hi, f32x8), bf16x8);
+                        acc[u][c][0] = mma(v0, lo, acc[u][c][0]);
+                        acc[u][c][1] = mma(v1, lo, acc[u][c][1]);
                     }
                 }
-                const bf16x8 hi = __builtin_convertvector(w, bf16x8);
-                acc[u][c][0] = mma(v0, hi, acc[u][c][0]);
-                acc[u][c][1] = mma(v1, hi, acc[u][c][1]);
-                if (std::is_same<T, _Float16>::value) {
-                    const bf16x8 lo = __builtin_convertvector(w - __builtin_convertvector(hi, f32x8), bf16x8);
-                    acc[u][c][0] = mma(v0, lo, acc[u][c][0]);
-                    acc[u][c][1] = mma(v1, lo, acc[u][c][1]);
+            }
+        };
+
+        int at = at0;
+        if (at < k1) {
+            Step<CP> cur = load(at, next);
+            next = ids(at + 128);
+            for (; at < k1; at += 128) {
+                Step<CP> st = cur;
+                if (at + 128 < k1) cur = load(at + 128, next);
+                next = ids(at + 256);
+                if (at + 31 > open || st.bad) compute(st, at, std::true_type{});
+                else compute(st, at, std::false_type{});
+            }
+        }
+
+        const bool whole = work.whole;
+        // join the waves
+        __shared__ float2 waves[4][NT][16];
+        __shared__ float sums[4][16][132];
+        float factor[NT], total[NT];
+#pragma unroll
+        for (int u = 0; u < NT; u++) {
+            sum[u] = column_sum(sum[u]);
+            if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < NT; u++) {
+            float m = kNegInf;
+#pragma unroll
+            for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][i].x);
+            float l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                const float2 o = waves[w][u][i];
+                l += o.x == kNegInf ? o.y : o.y * __builtin_amdgcn_exp2f(o.x - m);
+            }
+            factor[u] = top[u] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - m);
+            total[u] = l;
+            top[u] = m;
+        }
+        const int col = threadIdx.x >> 4, dd = 8 * (threadIdx.x & 15);
+#pragma unroll
+        for (int u = 0; u < NT; u++) {
+#pragma unroll
+            for (int c0 = 0; c0 < CP; c0 += 4) {
+                if (c0 >= C) continue;
+                __syncthreads();
+#pragma unroll
+                for (int c = c0; c < c0 + 4 && c < CP; c++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++)
+#pragma unroll
+                        for (int e = 0; e < 2; e++)
+                            sums[wave][i][32 * (c - c0) + 8 * g + 2 * r + e] = acc[u][c][e][r] * factor[u];
+                __syncthreads();
+                const float m = __shfl(top[u], col), l = __shfl(total[u], col);
+                const int r = rw.row0 + 16 * u + col, e0 = 32 * c0 + dd;
+                if (r < rw.rows && e0 < 32 * C) {
+                    f32x8 o = {};
+#pragma unroll
+                    for (int w = 0; w < 4; w++)
+#pragma unroll
+                        for (int e = 0; e < 8; e++) o[e] += sums[w][col][dd + e];
+                    const int t = r / p.group, head = h * p.group + r % p.group;
+                    if (!whole) {
+                        const int64_t at = EVEN ? (int64_t)work.place * R + 16 * u + col
+                                                : ((rw.begin + t) * p.q.heads + head) * sp.chunks + work.place;
+                        *(f32x8*)(part + at * 32 * C + e0) = o;
+                        if (e0 == 0) stats[at] = make_float2(m, l);
+                    } else {
+                        if (rw.bad) o = f32x8{} + __builtin_nanf("");
+                        else if (first + t >= 0) o *= 1.0f / l;
+                        store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e0,
+                               __builtin_convertvector(o, V), 8);
+                    }
                 }
             }
         }
-    };
-
-    int at = at0;
-    if (at < k1) {
-        Step<CP> cur = load(at, next);
-        next = ids(at + 128);
-        for (; at < k1; at += 128) {
-            Step<CP> st = cur;
-            if (at + 128 < k1) cur = load(at + 128, next);
-            next = ids(at + 256);
-            if (at + 31 > open || st.bad) compute(st, at, std::true_type{});
-            else compute(st, at, std::false_type{});
-        }
-    }
-
-    // join the waves
-    __shared__ float2 waves[4][NT][16];
-    __shared__ float sums[4][16][132];
-    float factor[NT], total[NT];
-#pragma unroll
-    for (int u = 0; u < NT; u++) {
-        sum[u] = column_sum(sum[u]);
-        if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < NT; u++) {
-        float m = kNegInf;
-#pragma unroll
-        for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][i].x);
-        float l = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; w++) {
-            const float2 o = waves[w][u][i];
-            l += o.x == kNegInf ? o.y : o.y * __builtin_amdgcn_exp2f(o.x - m);
-        }
-        factor[u] = top[u] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - m);
-        total[u] = l;
-        top[u] = m;
-    }
-    const int col = threadIdx.x >> 4, dd = 8 * (threadIdx.x & 15);
-#pragma unroll
-    for (int u = 0; u < NT; u++) {
-#pragma unroll
-        for (int c0 = 0; c0 < CP; c0 += 4) {
-            if (c0 >= C) continue;
-            __syncthreads();
-#pragma unroll
-            for (int c = c0; c < c0 + 4 && c < CP; c++)
-#pragma unroll
-                for (int r = 0; r < 4; r++)
-#pragma unroll
-                    for (int e = 0; e < 2; e++)
-                        sums[wave][i][32 * (c - c0) + 8 * g + 2 * r + e] = acc[u][c][e][r] * factor[u];
-            __syncthreads();
-            const float m = __shfl(top[u], col), l = __shfl(total[u], col);
-            const int r = rw.row0 + 16 * u + col, e0 = 32 * c0 + dd;
-            if (r < rw.rows && e0 < 32 * C) {
-                f32x8 o = {};
-#pragma unroll
-                for (int w = 0; w < 4; w++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) o[e] += sums[w][col][dd + e];
-                const int t = r / p.group, head = h * p.group + r % p.group;
-                if (chunks > 1) {
-                    const int64_t at = ((rw.begin + t) * p.q.heads + head) * chunks + chunk;
-                    *(f32x8*)(part + at * 32 * C + e0) = o;
-                    if (e0 == 0) stats[at] = make_float2(m, l);
-                } else {
-                    if (rw.bad) o = f32x8{} + __builtin_nanf("");
-                    else if (first + t >= 0) o *= 1.0f / l;
-                    store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e0,
-                           __builtin_convertvector(o, V), 8);
-                }
-            }
-        }
+        if (EVEN) __syncthreads();      // the next item uses the same LDS
     }
 }
 
@@ -348,236 +395,243 @@ template <int CP> __device__ __forceinline__ float over_groups(float v) {
     return v;
 }
 
-template <typename T, int CP, int NT, bool FULL>
-__global__ __launch_bounds__(256, CP * NT <= 4 ? 3 : CP * NT <= 8 ? 2 : 1) void k_kv4_few(Kv4AttentionParams p, int run, int chunks, int tiles, float* part,
-                                                 float2* stats) {
+template <typename T, int CP, int NT, bool FULL, bool EVEN>
+__global__ __launch_bounds__(256, CP * NT <= 2 ? 4 : CP * NT <= 4 ? 3 : CP * NT <= 8 ? 2 : 1)
+void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
     typedef typename Vec8<T>::type V;
     typedef typename Words<CP>::w W;
     constexpr int HR = 16 / CP, R = HR * NT;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i = lane & 15, g = lane >> 4, own = i % CP;
     const int C = FULL ? CP : p.cache.groups;
-    int64_t id = blockIdx.x;
-    const int chunk = (int)(id % chunks);
-    id /= chunks;
-    const int h = (int)(id % p.cache.heads);
-    const Rows rw = find_rows(p, id / p.cache.heads, tiles, R);
-    if (rw.row0 >= rw.rows) return;
+    __shared__ int kept[EVEN ? 4 : 1][6][64];
+    asm volatile("" ::"s"(part), "s"(stats));      // asked for with the first arguments, not when they are used
+    Work<EVEN> work(p, sp, R, kept);
+    while (work.next()) {
+        const Rows& rw = work.rw;
+        const int h = work.h;
+        int thread = threadIdx.x;
+        if (EVEN) asm volatile("" : "+v"(thread));      // nothing of the lane is kept from item to item: registers are short
+        const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+        const int i = lane & 15, g = lane >> 4, own = i % CP;
 
-    // the first pages and the queries are asked for before the sequence's length is there
-    const int32_t* table = p.table + rw.seq * p.table_pitch;
-    const int page = p.cache.page;
-    struct Ids {
-        int a, b;
-    };
-    auto ids = [&](int at) {      // pages of the halves of a step; behind the last key whatever the table holds
-        return Ids{table[min(at >> p.cache.shift, p.columns - 1)], table[min((at + 16) >> p.cache.shift, p.columns - 1)]};
-    };
-    const int at0 = chunk * run + 32 * wave;
-    Ids next = p.columns > 0 ? ids(at0) : Ids{0, 0};
-    V qf[NT][CP];
+        const int32_t* table = p.table + rw.seq * p.table_pitch;
+        const int page = p.cache.page;
+        struct Ids {
+            int a, b;
+        };
+        auto ids = [&](int at) {      // pages of the halves of a step; behind the last key whatever the table holds
+            return Ids{table[min(at >> p.cache.shift, p.columns - 1)],
+                       table[min((at + 16) >> p.cache.shift, p.columns - 1)]};
+        };
+        const int at0 = work.from + 32 * wave;
+        Ids next = p.columns > 0 ? ids(at0) : Ids{0, 0};
+        V qf[NT][CP];
 #pragma unroll
-    for (int u = 0; u < NT; u++) {
-        const int r = rw.row0 + HR * u + i / CP, t = r / p.group;
-        const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
-        V mine = {};
-        if (r < rw.rows && own < C) mine = load8(q + 32 * own + 8 * g, 8);
+        for (int u = 0; u < NT; u++) {
+            const int r = rw.row0 + HR * u + i / CP, t = r / p.group;
+            const T* q = (const T*)p.q.p + (rw.begin + t) * p.q.token + (h * p.group + r % p.group) * p.q.head;
+            V mine = {};
+            if (r < rw.rows && own < C) mine = load8(q + 32 * own + 8 * g, 8);
 #pragma unroll
-        for (int s = 0; s < CP; s++) qf[u][s] = s == own ? mine : V{};
-    }
-
-    const int first = rw.len - rw.n;                    // the last key of query t is first + t
-    const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
-    const int k0 = chunk * run, k1 = min(k0 + run, keys);
-    if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
-    const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
-
-    int last[NT];
-#pragma unroll
-    for (int u = 0; u < NT; u++) last[u] = first + (rw.row0 + HR * u + i / CP) / p.group;
-
-    struct Piece {
-        W k[2], v[2];
-        uint2 ka[2], va[2];
-        int bad;
-    };
-    // what a lane adds to a half's place in its block
-    const uint32_t k_at = i * 16 * C + g * 4 * C, v_at = g * 64 * C + i * 4 * C;
-    const uint32_t s_at = g * 8 * C + 8 * (FULL ? own : min(own, C - 1));
-    auto load = [&](int at, Ids pg) {
-        Piece st;
-        st.bad = 0;
-#pragma unroll
-        for (int hh = 0; hh < 2; hh++) {
-            int pid = __builtin_amdgcn_readfirstlane(hh ? pg.b : pg.a);
-            if (pid < 0 || pid >= p.cache.pages) pid = 0, st.bad |= 1 << hh;
-            const int t = (at + 16 * hh) & (page - 1);
-            // words past the head's groups are of what follows in the block, and nothing uses them
-            const uint8_t* b = p.cache.block(pid, h);
-            const uint8_t *kb = b + t * 16 * C, *vb = b + p.cache.values_at() + t * 16 * C;
-            const uint8_t *ks = b + p.cache.key_scales_at() + t * 2 * C, *vs = b + p.cache.value_scales_at() + t * 2 * C;
-            st.k[hh] = ((const Loose<W, uint32_t>*)(kb + k_at))->v;
-            st.v[hh] = ((const Loose<W, uint32_t>*)(vb + v_at))->v;
-            st.ka[hh] = *(const uint2*)(ks + s_at);
-            st.va[hh] = *(const uint2*)(vs + s_at);
+            for (int s = 0; s < CP; s++) qf[u][s] = s == own ? mine : V{};
         }
-        return st;
-    };
 
-    f32x4 acc[NT][CP][2] = {};
-    float top[NT], sum[NT];
-#pragma unroll
-    for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
+        const int first = rw.len - rw.n;                    // the last key of query t is first + t
+        const int keys = max(first + (min(rw.row0 + R, rw.rows) - 1) / p.group + 1, 0);
+        const int k1 = min(work.to, keys);
+        const int open = first + rw.row0 / p.group;         // keys up to here are seen by every row
 
-    auto compute = [&](const Piece& st, int at) {
-        const bool masks = at + 31 > open || st.bad;
-        f32x4 x[NT][2];
+        int last[NT];
 #pragma unroll
-        for (int hh = 0; hh < 2; hh++) {
-            f32x4 z[NT] = {};
+        for (int u = 0; u < NT; u++) last[u] = first + (rw.row0 + HR * u + i / CP) / p.group;
+
+        struct Piece {
+            W k[2], v[2];
+            uint2 ka[2], va[2];
+            int bad;
+        };
+        // what a lane adds to a half's place in its block
+        const uint32_t k_at = i * 16 * C + g * 4 * C, v_at = g * 64 * C + i * 4 * C;
+        const uint32_t s_at = g * 8 * C + 8 * (FULL ? own : min(own, C - 1));
+        auto load = [&](int at, Ids pg) {
+            Piece st;
+            st.bad = 0;
 #pragma unroll
-            for (int s = 0; s < CP; s++) {
-                const V kf = decode(st.k[hh][s], T{});
-#pragma unroll
-                for (int u = 0; u < NT; u++) z[u] = mma(kf, qf[u][s], z[u]);
+            for (int hh = 0; hh < 2; hh++) {
+                int pid = __builtin_amdgcn_readfirstlane(hh ? pg.b : pg.a);
+                if (pid < 0 || pid >= p.cache.pages) pid = 0, st.bad |= 1 << hh;
+                const int t = (at + 16 * hh) & (page - 1);
+                // words past the head's groups are of what follows in the block, and nothing uses them
+                const uint8_t* b = p.cache.block(pid, h);
+                const uint8_t *kb = b + t * 16 * C, *vb = b + p.cache.values_at() + t * 16 * C;
+                const uint8_t* ks = b + p.cache.key_scales_at() + t * 2 * C;
+                const uint8_t* vs = b + p.cache.value_scales_at() + t * 2 * C;
+                st.k[hh] = ((const Loose<W, uint32_t>*)(kb + k_at))->v;
+                st.v[hh] = ((const Loose<W, uint32_t>*)(vb + v_at))->v;
+                st.ka[hh] = *(const uint2*)(ks + s_at);
+                st.va[hh] = *(const uint2*)(vs + s_at);
             }
-            const f32x4 a = four(st.ka[hh]);
+            return st;
+        };
+
+        f32x4 acc[NT][CP][2] = {};
+        float top[NT], sum[NT];
 #pragma unroll
-            for (int u = 0; u < NT; u++)
+        for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
+
+        auto compute = [&](const Piece& st, int at) {
+            const bool masks = at + 31 > open || st.bad;
+            f32x4 x[NT][2];
 #pragma unroll
-                for (int r = 0; r < 4; r++) x[u][hh][r] = over_groups<CP>(a[r] * z[u][r]);
-        }
-        if (masks) {
+            for (int hh = 0; hh < 2; hh++) {
+                f32x4 z[NT] = {};
 #pragma unroll
-            for (int u = 0; u < NT; u++)
+                for (int s = 0; s < CP; s++) {
+                    const V kf = decode(st.k[hh][s], T{});
+#pragma unroll
+                    for (int u = 0; u < NT; u++) z[u] = mma(kf, qf[u][s], z[u]);
+                }
+                const f32x4 a = four(st.ka[hh]);
+#pragma unroll
+                for (int u = 0; u < NT; u++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) x[u][hh][r] = over_groups<CP>(a[r] * z[u][r]);
+            }
+            if (masks) {
+#pragma unroll
+                for (int u = 0; u < NT; u++)
+#pragma unroll
+                    for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            if (st.bad >> hh & 1) x[u][hh][r] = __builtin_nanf("");
+                            if (at + 16 * hh + 4 * g + r > last[u]) x[u][hh][r] = kNegInf;
+                        }
+            }
+            float most[NT];
+            bool moves = false;
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                most[u] = kNegInf;
+#pragma unroll
+                for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) most[u] = fmaxf(most[u], x[u][hh][r]);
+                most[u] *= p.scale;
+                moves |= passes(most[u], top[u]);
+            }
+            if (__ballot(moves)) {
+#pragma unroll
+                for (int u = 0; u < NT; u++) {
+                    // row by row: what a row gives does not depend on its neighbours
+                    const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
+                    const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
+                    top[u] = now;
+                    sum[u] *= f;
+#pragma unroll
+                    for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
+                }
+            }
+            const f32x4 b[2] = {four(st.va[0]), four(st.va[1])};
+            bf16x8 hi[NT], lo[NT];
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                const float m = top[u] == kNegInf ? 0.0f : top[u];
+                f32x8 w;
 #pragma unroll
                 for (int hh = 0; hh < 2; hh++)
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        if (st.bad >> hh & 1) x[u][hh][r] = __builtin_nanf("");
-                        if (at + 16 * hh + 4 * g + r > last[u]) x[u][hh][r] = kNegInf;
+                        const float e = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
+                        sum[u] += e;
+                        w[4 * hh + r] = e * b[hh][r];
                     }
-        }
-        float most[NT];
-        bool moves = false;
+                if (masks)      // scales behind the last key may be anything
 #pragma unroll
-        for (int u = 0; u < NT; u++) {
-            most[u] = kNegInf;
-#pragma unroll
-            for (int hh = 0; hh < 2; hh++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) most[u] = fmaxf(most[u], x[u][hh][r]);
-            most[u] *= p.scale;
-            moves |= passes(most[u], top[u]);
-        }
-        if (__ballot(moves)) {
-#pragma unroll
-            for (int u = 0; u < NT; u++) {
-                // row by row: what a row gives does not depend on its neighbours
-                const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
-                const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
-                top[u] = now;
-                sum[u] *= f;
-#pragma unroll
-                for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
+                    for (int r = 0; r < 8; r++)
+                        if (at + 4 * (r & 4) + 4 * g + (r & 3) > last[u]) w[r] = 0.0f;
+                hi[u] = __builtin_convertvector(w, bf16x8);
+                if (std::is_same<T, _Float16>::value)
+                    lo[u] = __builtin_convertvector(w - __builtin_convertvector(hi[u], f32x8), bf16x8);
             }
-        }
-        const f32x4 b[2] = {four(st.va[0]), four(st.va[1])};
-        bf16x8 hi[NT], lo[NT];
 #pragma unroll
-        for (int u = 0; u < NT; u++) {
-            const float m = top[u] == kNegInf ? 0.0f : top[u];
-            f32x8 w;
+            for (int c = 0; c < CP; c++) {
+                bf16x8 v0, v1;
+                value_pairs(st.v[0][c], st.v[1][c], &v0, &v1);
 #pragma unroll
-            for (int hh = 0; hh < 2; hh++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
-                    sum[u] += e;
-                    w[4 * hh + r] = e * b[hh][r];
-                }
-            if (masks)      // scales behind the last key may be anything
-#pragma unroll
-                for (int r = 0; r < 8; r++)
-                    if (at + 4 * (r & 4) + 4 * g + (r & 3) > last[u]) w[r] = 0.0f;
-            hi[u] = __builtin_convertvector(w, bf16x8);
-            if (std::is_same<T, _Float16>::value)
-                lo[u] = __builtin_convertvector(w - __builtin_convertvector(hi[u], f32x8), bf16x8);
-        }
-#pragma unroll
-        for (int c = 0; c < CP; c++) {
-            bf16x8 v0, v1;
-            value_pairs(st.v[0][c], st.v[1][c], &v0, &v1);
-#pragma unroll
-            for (int u = 0; u < NT; u++) {
-                acc[u][c][0] = mma(v0, hi[u], acc[u][c][0]);
-                acc[u][c][1] = mma(v1, hi[u], acc[u][c][1]);
-                if (std::is_same<T, _Float16>::value) {
-                    acc[u][c][0] = mma(v0, lo[u], acc[u][c][0]);
-                    acc[u][c][1] = mma(v1, lo[u], acc[u][c][1]);
+                for (int u = 0; u < NT; u++) {
+                    acc[u][c][0] = mma(v0, hi[u], acc[u][c][0]);
+                    acc[u][c][1] = mma(v1, hi[u], acc[u][c][1]);
+                    if (std::is_same<T, _Float16>::value) {
+                        acc[u][c][0] = mma(v0, lo[u], acc[u][c][0]);
+                        acc[u][c][1] = mma(v1, lo[u], acc[u][c][1]);
+                    }
                 }
             }
-        }
-    };
+        };
 
-    int at = at0;
-    if (at < k1) {
-        Piece cur = load(at, next);
-        next = ids(at + 128);
-        for (; at < k1; at += 128) {
-            const Piece st = cur;
-            if (at + 128 < k1) cur = load(at + 128, next);
-            next = ids(at + 256);
-            compute(st, at);
+        int at = at0;
+        if (at < k1) {
+            Piece cur = load(at, next);
+            next = ids(at + 128);
+            for (; at < k1; at += 128) {
+                const Piece st = cur;
+                if (at + 128 < k1) cur = load(at + 128, next);
+                next = ids(at + 256);
+                compute(st, at);
+            }
         }
-    }
 
-    // join the waves: each leaves its sums under the common maximum
-    __shared__ float2 waves[4][NT][16];
-    __shared__ __align__(16) float sums[4][R][32 * CP];
+        const bool whole = work.whole;
+        // join the waves: each leaves its sums under the common maximum
+        __shared__ float2 waves[4][NT][16];
+        __shared__ __align__(16) float sums[4][R][32 * CP];
 #pragma unroll
-    for (int u = 0; u < NT; u++) {
-        sum[u] = column_sum(sum[u]);
-        if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
-    }
-    __syncthreads();
+        for (int u = 0; u < NT; u++) {
+            sum[u] = column_sum(sum[u]);
+            if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
+        }
+        __syncthreads();
 #pragma unroll
-    for (int u = 0; u < NT; u++) {
-        float m = kNegInf;
+        for (int u = 0; u < NT; u++) {
+            float m = kNegInf;
 #pragma unroll
-        for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][i].x);
-        const float f = top[u] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - m);
-        f32x8 o;
+            for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][i].x);
+            const float f = top[u] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - m);
+            f32x8 o;
 #pragma unroll
-        for (int c = 0; c < CP; c++)
-            if (c == own)
+            for (int c = 0; c < CP; c++)
+                if (c == own)
 #pragma unroll
-                for (int r = 0; r < 8; r++) o[r] = acc[u][c][r & 1][r >> 1] * f;
-        *(f32x8*)&sums[wave][HR * u + i / CP][32 * own + 8 * g] = o;
-    }
-    __syncthreads();
-    const int row = threadIdx.x / (4 * CP), e = 8 * (threadIdx.x % (4 * CP)), r = rw.row0 + row;
-    if (row >= R || r >= rw.rows || e >= 32 * C) return;
-    float m = kNegInf, l = 0.0f;
-    const int u = row / HR, column = row % HR * CP;
+                    for (int r = 0; r < 8; r++) o[r] = acc[u][c][r & 1][r >> 1] * f;
+            *(f32x8*)&sums[wave][HR * u + i / CP][32 * own + 8 * g] = o;
+        }
+        __syncthreads();
+        const int row = thread / (4 * CP), e = 8 * (thread % (4 * CP)), r = rw.row0 + row;
+        if (row < R && r < rw.rows && e < 32 * C) {
+            float m = kNegInf, l = 0.0f;
+            const int u = row / HR, column = row % HR * CP;
 #pragma unroll
-    for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][column].x);
-    f32x8 o = {};
+            for (int w = 0; w < 4; w++) m = fmaxf(m, waves[w][u][column].x);
+            f32x8 o = {};
 #pragma unroll
-    for (int w = 0; w < 4; w++) {
-        const float2 x = waves[w][u][column];
-        l += x.x == kNegInf ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - m);
-        o += *(const f32x8*)&sums[w][row][e];
-    }
-    const int t = r / p.group, head = h * p.group + r % p.group;
-    if (chunks > 1) {
-        const int64_t to = ((rw.begin + t) * p.q.heads + head) * chunks + chunk;
-        *(f32x8*)(part + to * 32 * C + e) = o;
-        if (e == 0) stats[to] = make_float2(m, l);
-    } else {
-        if (rw.bad) o = f32x8{} + __builtin_nanf("");
-        else if (first + t >= 0) o *= 1.0f / l;
-        store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e, __builtin_convertvector(o, V), 8);
+            for (int w = 0; w < 4; w++) {
+                const float2 x = waves[w][u][column];
+                l += x.x == kNegInf ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - m);
+                o += *(const f32x8*)&sums[w][row][e];
+            }
+            const int t = r / p.group, head = h * p.group + r % p.group;
+            if (!whole) {
+                const int64_t to = EVEN ? (int64_t)work.place * R + row
+                                        : ((rw.begin + t) * p.q.heads + head) * sp.chunks + work.place;
+                *(f32x8*)(part + to * 32 * C + e) = o;
+                if (e == 0) stats[to] = make_float2(m, l);
+            } else {
+                if (rw.bad) o = f32x8{} + __builtin_nanf("");
+                else if (first + t >= 0) o *= 1.0f / l;
+                store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e, __builtin_convertvector(o, V), 8);
+            }
+        }
+        if (EVEN) __syncthreads();      // the next item uses the same LDS
     }
 }
 
@@ -598,7 +652,7 @@ __device__ __forceinline__ JoinRow join_row(const Kv4AttentionParams& p, int seq
 // The parts of one row (query and head) joined, a workgroup to a row: threads take four elements each, groups of
 // threads the parts in turn, eight in flight.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join(Kv4AttentionParams p, int run, int chunks, const float* part,
+__global__ __launch_bounds__(256) void k_join_row(Kv4AttentionParams p, int run, int chunks, const float* part,
                                               const float2* stats) {
     __shared__ float sums[256][4];
     __shared__ float tops[256], totals[256];
@@ -661,9 +715,82 @@ __global__ __launch_bounds__(256) void k_join(Kv4AttentionParams p, int run, int
     ((Loose<t4, T>*)((T*)p.o.p + token * p.o.token + head * p.o.head + e))->v = __builtin_convertvector(o, t4);
 }
 
-// At most eight parts: a thread to four elements of a row.
+// The parts of an item joined, `rows` of its R rows: threads to four elements each, sets of threads the parts in turn,
+// eight in flight.  ITEMS: a workgroup has the item of its number, else the last one that workgroup blockIdx.x began.
+template <typename T, bool ITEMS>
+__global__ __launch_bounds__(256) void k_join_items(Kv4AttentionParams p, int R, int rows, int count, const float* part,
+                                              const float2* stats) {
+    __shared__ float sums[256][4];
+    __shared__ float tops[256], totals[256];
+    __shared__ int kept[4][6][64];
+    Kv4Walk walk(p, kept, R, count);
+    if (walk.total == 0) return;
+    Kv4Item it;
+    int w = blockIdx.x;
+    if (ITEMS) {
+        it = walk.item(w);
+        w = it.begin / walk.per;
+    } else {
+        const int u1 = min((w + 1) * walk.per, walk.total);
+        if (w * walk.per >= u1) return;
+        it = walk.item(u1 - 1, u1);
+        if (it.begin < w * walk.per) return;
+    }
+    const int u0 = w * walk.per, parts = (it.end - 1) / walk.per - w + 1;
+    if (it.end <= it.begin || parts == 1) return;
+    const int d = 32 * p.cache.groups, per = d / 4, sets = 256 / per / rows;
+    const int e = 4 * (threadIdx.x % per), set = threadIdx.x / per / rows;
+    const int row = blockIdx.y * rows + threadIdx.x / per % rows;
+    const int r = it.rw.row0 + row, t = r / p.group, head = it.h * p.group + r % p.group;
+    const bool live = set < sets && r < it.rw.rows;
+    auto place = [&](int k) { return (int64_t)(2 * (w + k) + (k == 0 && it.begin > u0 ? 1 : 0)) * R + row; };
+    float m = kNegInf, l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    if (live)
+        for (int k0 = set; k0 < parts; k0 += 8 * sets) {
+            float2 s[8];
+            f32x4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int k = k0 + i * sets;
+                s[i] = make_float2(kNegInf, 0.0f), v[i] = f32x4{0, 0, 0, 0};
+                if (k < parts) s[i] = stats[place(k)], v[i] = *(const f32x4*)(part + place(k) * d + e);
+            }
+            float now = m;
+#pragma unroll
+            for (int i = 0; i < 8; i++) now = fmaxf(now, s[i].x);
+            const float f = m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+            l *= f, o *= f, m = now;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float g = s[i].x == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(s[i].x - m);
+                l = fmaf(g, s[i].y, l);
+                o += v[i] * g;
+            }
+        }
+    tops[threadIdx.x] = m;
+    totals[threadIdx.x] = l;
+    *(f32x4*)sums[threadIdx.x] = o;
+    __syncthreads();
+    if (set || !live) return;
+    const int step = per * rows;
+    for (int k = 1; k < sets; k++) m = fmaxf(m, tops[threadIdx.x + k * step]);
+    l = 0.0f, o = f32x4{0, 0, 0, 0};
+    for (int k = 0; k < sets; k++) {
+        const int at = threadIdx.x + k * step;
+        const float f = tops[at] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(tops[at] - m);
+        l += f * totals[at];
+        o += *(const f32x4*)sums[at] * f;
+    }
+    if (it.rw.bad) o = f32x4{} + __builtin_nanf("");
+    else if (it.rw.len - it.rw.n + t >= 0) o *= 1.0f / l;      // no key: zeros
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    ((Loose<t4, T>*)((T*)p.o.p + (it.rw.begin + t) * p.o.token + head * p.o.head + e))->v = __builtin_convertvector(o, t4);
+}
+
+// At most kRuns parts: a thread to four elements of a row.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_few(Kv4AttentionParams p, int run, int chunks, const float* part,
+__global__ __launch_bounds__(256) void k_join_runs(Kv4AttentionParams p, int run, int chunks, const float* part,
                                                   const float2* stats) {
     const int d = 32 * p.cache.groups, per = d / 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / per, token = row / p.q.heads;
@@ -672,10 +799,10 @@ __global__ __launch_bounds__(256) void k_join_few(Kv4AttentionParams p, int run,
     // every part that there may be is on its way before the row's keys are known
     const float2* st = stats + row * chunks;
     const float* pt = part + row * chunks * d + e;
-    float2 s[8];
-    f32x4 v[8];
+    float2 s[kRuns];
+    f32x4 v[kRuns];
 #pragma unroll
-    for (int c = 0; c < 8; c++)
+    for (int c = 0; c < kRuns; c++)
         if (c < chunks) s[c] = st[c], v[c] = *(const f32x4*)(pt + (int64_t)c * d);
     JoinRow jr;
     if (p.starts) {
@@ -694,13 +821,13 @@ __global__ __launch_bounds__(256) void k_join_few(Kv4AttentionParams p, int run,
     const int used = min((jr.keys + run - 1) / run, chunks);
     float m = kNegInf, l = 0.0f;
 #pragma unroll
-    for (int c = 0; c < 8; c++) {
+    for (int c = 0; c < kRuns; c++) {
         if (c >= used) s[c] = make_float2(kNegInf, 0.0f), v[c] = f32x4{0, 0, 0, 0};
         m = fmaxf(m, s[c].x);
     }
     f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-    for (int c = 0; c < 8; c++) {
+    for (int c = 0; c < kRuns; c++) {
         const float f = s[c].x == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(s[c].x - m);
         l = fmaf(f, s[c].y, l);
         o += v[c] * f;
@@ -712,43 +839,87 @@ __global__ __launch_bounds__(256) void k_join_few(Kv4AttentionParams p, int run,
 }
 
 Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts, int64_t longest) {
-    Kv4Split s;
+    Kv4Split s = {};
     const int group = q_heads / kv_heads, cus = num_cus();
     const int64_t rows = starts ? (tokens + seqs - 1) / seqs * group : group;      // of a sequence, on average
-    const int narrow = d <= 64 ? 8 : d <= 128 ? 4 : 2;      // rows of a tile whose columns are (row, group)
+    const int cp = d <= 64 ? 2 : d <= 128 ? 4 : 8, narrow = 16 / cp;      // rows of a tile whose columns are (row, group)
     s.kind = rows <= 2 * narrow ? kKv4Few : rows <= 64 ? kKv4Some : kKv4Many;
     s.NT = rows <= (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 192) || (s.kind != kKv4Few && d > 128) ? 1 : 2;
-    const int R = (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 128) * s.NT;
-    s.tiles = (group + R - 1) / R;
-    s.slots = starts ? tokens * group / R + seqs : (int64_t)seqs * s.tiles;
-    const int64_t base = s.slots * kv_heads;
-    // Few rows: parts of about 576 keys (five steps a wave), for twelve workgroups a CU.  Many: as many as run at once (256 rows a CU).
-    int64_t n = s.kind == kKv4Many ? (d > 128 ? 1 : 2 / s.NT) * cus / base : (12 * cus + base - 1) / base;
-    const int64_t most = (longest + 575) / 576;
-    if (n > most) n = most;
-    if (n < 1) n = 1;
-    int64_t run = ((longest + n - 1) / n + 127) / 128 * 128;
-    if (run < 128) run = 128;
+    s.R = (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 128) * s.NT;
+    s.chunks = 1;
+    s.tiles = (group + s.R - 1) / s.R;
+    s.slots = starts ? tokens * group / s.R + seqs : (int64_t)seqs * s.tiles;
+    if (s.kind != kKv4Many) {
+        // workgroups that run at once, by the registers that their kernels take
+        const int few = cp * s.NT == 2 ? 4 : cp * s.NT == 4 ? 3 : cp * s.NT == 8 ? 2 : 1;
+        const int some = cp * s.NT == 2 ? 3 : cp * s.NT == 4 ? 2 : 1;
+        const int64_t at_once = cus * (s.kind == kKv4Few ? few : some), base = s.slots * kv_heads;
+        // Even shares of the work, where there is much: heavy workgroups from four units each on (64 sequences of 2048
+        // keys, heads of 128: 8 queries of 4 heads 71 us, 134 in runs; 2 queries 41 and 63; 16 sequences of 1024, 8
+        // queries 21 and 30).  They cost two to seven us more where there is little (one sequence of 32768, one query
+        // of 4 heads 18 and 15 in runs; 64 of 512, 24 and 12), and a workgroup of one tile is light enough that runs of
+        // the shorter contexts fill the card (256 of 1024: 83 and 68; of up to 8192 as they come, 64: 85 and 90).
+        // Tiles of long heads have no registers for it (256: 8 queries 277, 240 in runs).
+        const bool light = s.kind == kKv4Few && s.NT == 1;
+        if (base * ((longest + 127) / 128) >= (light ? 16 : 4) * at_once && longest >= (light ? 4096 : 256) &&
+            (s.kind == kKv4Few || d <= 128)) {
+            s.count = (int)at_once;
+            return s;
+        }
+        // parts of about 576 keys (five steps a wave), for twelve workgroups a CU
+        const int64_t n = std::max(std::min((12 * cus + base - 1) / base, (longest + 575) / 576), (int64_t)1);
+        const int64_t run = std::max(((longest + n - 1) / n + 127) / 128 * 128, (int64_t)128);
+        s.run = (int)run;
+        s.chunks = std::max((int)((longest + run - 1) / run), 1);
+        return s;
+    }
+    // What takes the least time: rounds of as many workgroups as run at once (256 rows a CU, 128 of long heads), each
+    // as long as its part of the keys; and the join, which moves a part's sums in about the time of 1700 keys (two
+    // sequences of 8192 keys, 512 queries of 32 heads of 128: 290 us whole, 192 in two parts; 16 of 2048, 64 queries: 87
+    // and 122).
+    const int64_t tiles = starts ? std::max(tokens * group / s.R, std::min((int64_t)seqs, tokens)) : s.slots;
+    const int64_t base = tiles * kv_heads, at_once = (d > 128 ? 1 : 2 / s.NT) * cus;
+    int64_t n = 1;
+    double least = 0.0;
+    for (int64_t m = 1; m <= kRuns && 576 * (m - 1) < longest; m++) {
+        const double rounds = (double)((base * m + at_once - 1) / at_once) / m;
+        const double time = rounds + (m > 1 ? 1700.0 * m / longest * base / at_once : 0.0);
+        if (m == 1 || time < least) least = time, n = m;
+    }
+    const int64_t run = std::max(((longest + n - 1) / n + 127) / 128 * 128, (int64_t)128);
     s.run = (int)run;
-    s.chunks = (int)((longest + run - 1) / run);
-    if (s.chunks < 1) s.chunks = 1;
+    s.chunks = std::max((int)((longest + run - 1) / run), 1);
     return s;
 }
 
-size_t stats_bytes(int64_t rows, int chunks) { return ((size_t)rows * chunks * sizeof(float2) + 255) & ~(size_t)255; }
+// Rows of partial sums that a call keeps.
+int64_t places(const Kv4Split& s, int64_t rows) {
+    return s.count ? (int64_t)2 * s.count * s.R : s.chunks > 1 ? rows * s.chunks : 0;
+}
+size_t stats_bytes(int64_t places) { return ((size_t)places * sizeof(float2) + 255) & ~(size_t)255; }
 
-template <typename T, int CP, bool FULL>
+template <typename T, int CP, bool FULL, bool EVEN>
 hipError_t launch_cp(const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats, hipStream_t s) {
-    const unsigned grid = (unsigned)(sp.slots * p.cache.heads * sp.chunks);
+    const unsigned grid = (unsigned)(EVEN ? sp.count : sp.slots * p.cache.heads * sp.chunks);
     if (sp.kind == kKv4Few) {
-        if (sp.NT == 1) k_kv4_few<T, CP, 1, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-        else k_kv4_few<T, CP, 2, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-    } else {
-        // long heads: one tile, two would not fit the registers
-        if (sp.NT == 1) k_kv4<T, CP, 1, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
-        else k_kv4<T, CP, CP == 8 ? 1 : 2, FULL><<<grid, 256, 0, s>>>(p, sp.run, sp.chunks, sp.tiles, part, stats);
+        if (sp.NT == 1) k_kv4_few<T, CP, 1, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
+        else k_kv4_few<T, CP, 2, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
+    } else if constexpr (!EVEN || CP < 8) {
+        // long heads: one tile, two would not fit the registers, nor one with what an even share takes
+        if (sp.NT == 1) k_kv4<T, CP, 1, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
+        else k_kv4<T, CP, CP == 8 ? 1 : 2, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
     }
     return hipGetLastError();
+}
+
+template <typename T, bool EVEN>
+hipError_t launch_d(const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats, hipStream_t s) {
+    if (p.d == 64) return launch_cp<T, 2, true, EVEN>(p, sp, part, stats, s);
+    if (p.d == 128) return launch_cp<T, 4, true, EVEN>(p, sp, part, stats, s);
+    if (p.d == 256) return launch_cp<T, 8, true, EVEN>(p, sp, part, stats, s);
+    if (p.d < 64) return launch_cp<T, 2, false, EVEN>(p, sp, part, stats, s);
+    if (p.d < 128) return launch_cp<T, 4, false, EVEN>(p, sp, part, stats, s);
+    return launch_cp<T, 8, false, EVEN>(p, sp, part, stats, s);
 }
 
 template <typename T>
@@ -757,22 +928,23 @@ hipError_t launch_t(int type, const Kv4AttentionParams& p, hipStream_t s) {
                               (int64_t)p.columns * p.cache.page);
     const int64_t rows = p.tokens * p.q.heads;
     float2* stats = (float2*)p.ws;
-    float* part = (float*)(p.ws + stats_bytes(rows, sp.chunks));
-    hipError_t e;
-    if (sp.kind == kKv4Many) e = launch_kv4_many(type, p, sp, part, stats, s);
-    else if (p.d == 64) e = launch_cp<T, 2, true>(p, sp, part, stats, s);
-    else if (p.d == 128) e = launch_cp<T, 4, true>(p, sp, part, stats, s);
-    else if (p.d == 256) e = launch_cp<T, 8, true>(p, sp, part, stats, s);
-    else if (p.d < 64) e = launch_cp<T, 2, false>(p, sp, part, stats, s);
-    else if (p.d < 128) e = launch_cp<T, 4, false>(p, sp, part, stats, s);
-    else e = launch_cp<T, 8, false>(p, sp, part, stats, s);
-    if (e != hipSuccess || sp.chunks == 1) return e;
-    if (sp.chunks <= 8) {
-        const int64_t threads = rows * (p.d / 4);
-        k_join_few<T><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
-    } else {
-        k_join<T><<<(unsigned)rows, 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
+    float* part = (float*)(p.ws + stats_bytes(places(sp, rows)));
+    if (sp.count) {
+        const hipError_t e = launch_d<T, true>(p, sp, part, stats, s);
+        if (e != hipSuccess) return e;
+        const int at_a_time = std::max(sp.R / 4, 1);
+        const dim3 grid((unsigned)std::min(sp.slots * p.cache.heads, (int64_t)sp.count), sp.R / at_a_time);
+        auto join = grid.x < (unsigned)sp.count ? k_join_items<T, true> : k_join_items<T, false>;
+        join<<<grid, 256, 0, s>>>(p, sp.R, at_a_time, sp.count, part, stats);
+        return hipGetLastError();
     }
+    const hipError_t e = sp.kind == kKv4Many ? launch_kv4_many(type, p, sp, part, stats, s)
+                                             : launch_d<T, false>(p, sp, part, stats, s);
+    if (e != hipSuccess || sp.chunks == 1) return e;
+    const int64_t threads = rows * (p.d / 4);
+    const unsigned blocks = (unsigned)((threads + 255) / 256);
+    if (sp.chunks <= kRuns) k_join_runs<T><<<blocks, 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
+    else k_join_row<T><<<(unsigned)rows, 256, 0, s>>>(p, sp.run, sp.chunks, part, stats);
     return hipGetLastError();
 }
 
@@ -781,9 +953,16 @@ hipError_t launch_t(int type, const Kv4AttentionParams& p, hipStream_t s) {
 size_t kv4_attention_workspace(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts,
                                int64_t longest) {
     const Kv4Split s = split(tokens, q_heads, d, kv_heads, seqs, starts, longest);
-    if (s.chunks == 1) return 0;
-    const int64_t rows = tokens * q_heads;
-    return stats_bytes(rows, s.chunks) + (size_t)rows * s.chunks * d * sizeof(float);
+    const int64_t n = places(s, tokens * q_heads);
+    return n ? stats_bytes(n) + (size_t)n * d * sizeof(float) : 0;
+}
+
+bool kv4_attention_counts(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts, int64_t longest) {
+    const Kv4Split s = split(tokens, q_heads, d, kv_heads, seqs, starts, longest);
+    const int64_t group = q_heads / kv_heads;
+    if (tokens * group > INT32_MAX - 256) return false;
+    if (!s.count) return s.slots * kv_heads <= INT32_MAX / s.chunks;
+    return s.slots * kv_heads <= (1 << 30) / ((longest + 127) / 128 + 1);
 }
 
 hipError_t launch_kv4_attention(int type, const Kv4AttentionParams& p, hipStream_t s) {

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
     if (chunks > 1 && k0 >= k1) return;                 // the join does not look at it
 
     const int row = rw.row0 + 32 * wave + col;
-    const bool live = row < rw.rows;
+    const bool live = row < rw.rows, alive = rw.row0 + 32 * wave < rw.rows;      // the lane's row, any of the wave's
     const int last = last_of(row), wave_open = last_of(rw.row0 + 32 * wave);
     const int head = h * p.group + row % p.group;
     const int64_t token = rw.begin + row / p.group;
@@ -235,23 +235,29 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv4_many(Kv4A
             __syncthreads();      // this tile is there; the next one's peaks are; no one reads the other stage any more
             const int ke_next = peak(stage ^ 1).x, ve_next = max(ve, peak(stage ^ 1).y);
             share(ke_next, ve_next);
-            fl.scores(kt[stage]);
-            decoded();
+            if (alive) {
+                fl.scores(kt[stage]);
+                decoded();
 #pragma unroll
-            for (int i = 0; i < DP / 8; i++) {      // between the MFMAs
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                     // LDS read
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                     // MFMA
-                __builtin_amdgcn_sched_group_barrier(0x002, H == 2 ? 4 : 7, 0);        // VALU
+                for (int i = 0; i < DP / 8; i++) {      // between the MFMAs
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                     // LDS read
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                     // MFMA
+                    __builtin_amdgcn_sched_group_barrier(0x002, H == 2 ? 4 : 7, 0);        // VALU
+                }
+            } else {
+                decoded();
             }
             put(stage ^ 1);
             load(j0 + 2 * KT, next), next = page_of(j0 + 3 * KT);
-            const f16x8* vs = vt[stage];
-            fl.weights(__builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), j0 + KT - 1 > wave_open, last - j0 - 4 * half);
-            fl.products([&](int r, int d) { return vs[((r >> 4) * 2 + half) * DP + 32 * d + col]; });
-            if (ve_next > ve) {
-                const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
+            if (alive) {
+                const f16x8* vs = vt[stage];
+                fl.weights(__builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), j0 + KT - 1 > wave_open, last - j0 - 4 * half);
+                fl.products([&](int r, int d) { return vs[((r >> 4) * 2 + half) * DP + 32 * d + col]; });
+                if (ve_next > ve) {
+                    const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
 #pragma unroll
-                for (int d = 0; d < DB; d++) fl.acc[d] *= f;
+                    for (int d = 0; d < DB; d++) fl.acc[d] *= f;
+                }
             }
             ke = ke_next, ve = ve_next;
         }

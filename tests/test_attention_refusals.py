@@ -137,6 +137,7 @@ def test_cache_attention(esb):
         assert attend(**bad) == INVALID, bad
     assert attend(t=F32) == UNSUPPORTED
     assert attend(columns=1 << 28, pitch=1 << 28) == UNSUPPORTED
+    assert attend(columns=1 << 24, pitch=1 << 24, tokens=1 << 18, seqs=1 << 18) == UNSUPPORTED
     assert attend(tokens=1 << 28, seqs=1 << 28) == UNSUPPORTED
     assert attend(ws=None) == WORKSPACE and attend(wb=need - 1) == WORKSPACE
     none = H(n=8, data=None)

@@ -336,3 +336,83 @@ def test_streams(esb):
         out = esb.esb_kv4_attention(y, c.cache, 64, 2, c.pages, c.lengths, stream=given)
         s.synchronize()
         assert torch.equal(out, want)
+
+
+def wide(seqs, heads, counts, group, d, page):
+    """Columns of a page table over which a call's work is shared evenly, whatever tile it takes: at least 20480
+    steps of 128 keys where each sequence has one tile of rows."""
+    return 128 // page * (-(-20480 // (seqs * heads)) + 32) if page <= 128 else 20480 // (seqs * heads) + 32
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("kv,group,d,page", [(1, 1, 32, 16), (2, 4, 128, 64), (1, 7, 64, 16), (3, 12, 64, 32),
+                                             (1, 40, 128, 64), (2, 3, 96, 128), (1, 20, 96, 16), (2, 2, 256, 16),
+                                             (1, 4, 160, 64), (1, 30, 64, 64)])
+@pytest.mark.parametrize("many", [False, True])
+def test_even_shares(esb, t, kv, group, d, page, many):
+    """Work that workgroups share evenly: sequences that end inside a share, take several, have no token or no key;
+    fewer and more sequences than a wave has lanes, one of them longer than all others."""
+    seqs = 150 if many else 13
+    lengths = [(53 * i) % 400 if i % 5 else (i // 5) % 3 for i in range(seqs)]
+    lengths[seqs // 2], lengths[-1] = 2600, 129
+    c = Cache(esb, 70, lengths, kv, d, page, columns=wide(seqs, kv, 1, group, d, page))
+    q = queries(71, seqs, kv * group, d, ref.TYPES[t])
+    verify(c, q, esb.esb_kv4_attention(q, c.cache, page, kv, c.pages, c.lengths), [1] * seqs)
+    counts = [(7 * i) % 4 for i in range(seqs)]
+    q = queries(72, sum(counts) + 3, kv * group, d, ref.TYPES[t])
+    starts = torch.tensor([sum(counts[:i]) for i in range(seqs + 1)], dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 3.0)
+    esb.esb_kv4_attention(q, c.cache, page, kv, c.pages, c.lengths, starts=starts, out=out)
+    verify(c, q, out, counts)
+    assert bool((out[sum(counts):] == 3.0).all())
+
+
+def test_even_shares_of_anything(esb):
+    """The same over bad lengths and pages, and starts that do not ascend or leave the tokens."""
+    lengths = [100, 90, 700, 70]
+    c = Cache(esb, 73, lengths, 2, 128, 16, columns=wide(4, 2, 1, 8, 128, 16))
+    q = queries(74, 4, 16, 128, torch.bfloat16)
+    clean = esb.esb_kv4_attention(q, c.cache, 16, 2, c.pages, c.lengths)
+    c.lengths[0] = c.columns * 16 + 1
+    c.lengths[3] = -5
+    for page in (-1, c.cache.shape[0], 2 ** 31 - 1):
+        c.pages[2, 30] = page
+        out = esb.esb_kv4_attention(q, c.cache, 16, 2, c.pages, c.lengths)
+        assert bool(torch.isnan(out[0]).all()) and bool(torch.isnan(out[2]).all())
+        assert not bool(out[3].any())
+        # cut elsewhere: probabilities rounded under another maximum (twice 2^-9 of a mean of |v|, which is below
+        # 2: codes of 1.9 on average, scales about 0.4), and a bf16 step of the output
+        torch.testing.assert_close(out[1], clean[1], rtol=2.0 ** -7, atol=2.0 ** -7)
+    q = queries(75, 30, 16, 128, torch.bfloat16)
+    buf = torch.full((50, 16, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    for s in ([0, -5, 40, 7, 30], [10, 5, 2, 0, 0], [2 ** 31 - 1, 0, 9, 2 ** 31 - 1, 5], [-2 ** 31, 20, 10, 30, 30],
+              [0, 30, 0, 30, 0], [-9, -7, -2, 5, 2 ** 31 - 1]):
+        starts = torch.tensor(s, dtype=torch.int32, device="cuda")
+        esb.esb_kv4_attention(q, c.cache, 16, 2, c.pages, c.lengths, starts=starts, out=buf[10:40])
+        assert bool((buf[:10] == 3.0).all()) and bool((buf[40:] == 3.0).all())
+
+
+def test_even_shares_in_graphs(esb):
+    """Two captured calls that share work evenly over one workspace; the lengths change between replays."""
+    seqs = 9
+    lengths = [300 * i + 40 for i in range(seqs)]
+    c = Cache(esb, 76, lengths, 2, 128, 64, columns=wide(seqs, 2, 1, 8, 128, 64))
+    qs = [queries(s, seqs, 16, 128, torch.bfloat16) for s in (77, 78)]
+    need = esb.esb_kv4_attention_workspace_size(seqs, 16, 128, 2, seqs, False, c.columns, 64)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    now = c.lengths.clone()
+    graphs, outs = [], []
+    esb.esb_kv4_attention(qs[0], c.cache, 64, 2, c.pages, now, workspace=ws)
+    torch.cuda.synchronize()
+    for x in qs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(esb.esb_kv4_attention(x, c.cache, 64, 2, c.pages, now, workspace=ws))
+        graphs.append(g)
+    for turn in range(4):
+        now.copy_((c.lengths - 13 * turn * torch.arange(seqs, device="cuda")).int())
+        graphs[0].replay()
+        graphs[1].replay()
+        for x, out in zip(qs, outs):
+            assert torch.equal(out, esb.esb_kv4_attention(x, c.cache, 64, 2, c.pages, now))
+        torch.cuda.synchronize()
