@@ -932,9 +932,12 @@ hipError_t launch_t(int type, const Kv4AttentionParams& p, hipStream_t s) {
     if (sp.count) {
         const hipError_t e = launch_d<T, true>(p, sp, part, stats, s);
         if (e != hipSuccess) return e;
-        const int at_a_time = std::max(sp.R / 4, 1);
-        const dim3 grid((unsigned)std::min(sp.slots * p.cache.heads, (int64_t)sp.count), sp.R / at_a_time);
-        auto join = grid.x < (unsigned)sp.count ? k_join_items<T, true> : k_join_items<T, false>;
+        // As many rows as fit, or four workgroups to an item of many parts.
+        const bool items = sp.slots * p.cache.heads < sp.count;
+        int at_a_time = 8 * sp.slots * p.cache.heads < sp.count ? std::max(sp.R / 4, 1) : sp.R;
+        while (at_a_time * (p.d / 4) > 256) at_a_time /= 2;
+        const dim3 grid((unsigned)(items ? sp.slots * p.cache.heads : sp.count), sp.R / at_a_time);
+        auto join = items ? k_join_items<T, true> : k_join_items<T, false>;
         join<<<grid, 256, 0, s>>>(p, sp.R, at_a_time, sp.count, part, stats);
         return hipGetLastError();
     }
