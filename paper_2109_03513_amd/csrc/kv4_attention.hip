@@ -843,7 +843,11 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
     const int group = q_heads / kv_heads, cus = num_cus();
     const int64_t rows = starts ? (tokens + seqs - 1) / seqs * group : group;      // of a sequence, on average
     const int cp = d <= 64 ? 2 : d <= 128 ? 4 : 8, narrow = 16 / cp;      // rows of a tile whose columns are (row, group)
-    s.kind = rows <= 2 * narrow ? kKv4Few : rows <= 64 ? kKv4Some : kKv4Many;
+    // Few rows: to one tile of short heads, to two of others.  64 sequences, us in tiles of (row, group) and in tiles of 16
+    // rows: heads of 64, 16 rows of 8192 keys 101 and 87; of 128, 8 rows of 4096 70 and 70; of 256, 4 rows of 4096 152 and
+    // 249.  Many: past 64 rows.  64 sequences of 2048 keys in tiles of 16 and of 128 rows: 64 rows 138 and 145, 96 rows 196
+    // and 150 (eight sequences: 28 and 39, 41 and 50).
+    s.kind = rows <= (cp == 2 ? 1 : 2) * narrow ? kKv4Few : rows <= 64 ? kKv4Some : kKv4Many;
     s.NT = rows <= (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 192) || (s.kind != kKv4Few && d > 128) ? 1 : 2;
     s.R = (s.kind == kKv4Few ? narrow : s.kind == kKv4Some ? 16 : 128) * s.NT;
     s.chunks = 1;
@@ -858,7 +862,7 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
         // keys, heads of 128: 8 queries of 4 heads 71 us, 134 in runs; 2 queries 41 and 63; 16 sequences of 1024, 8
         // queries 21 and 30).  They cost two to seven us more where there is little (one sequence of 32768, one query
         // of 4 heads 18 and 15 in runs; 64 of 512, 24 and 12), and a workgroup of one tile is light enough that runs of
-        // the shorter contexts fill the card (256 of 1024: 83 and 68; of up to 8192 as they come, 64: 85 and 90).
+        // the shorter contexts fill the card (256 of 1024: 83 and 68; 64 ragged ones up to 8192: 82 and 90).
         // Tiles of long heads have no registers for it (256: 8 queries 277, 240 in runs).
         const bool light = s.kind == kKv4Few && s.NT == 1;
         if (base * ((longest + 127) / 128) >= (light ? 16 : 4) * at_once && longest >= (light ? 4096 : 256) &&
@@ -903,7 +907,7 @@ hipError_t launch_cp(const Kv4AttentionParams& p, const Kv4Split& sp, float* par
     const unsigned grid = (unsigned)(EVEN ? sp.count : sp.slots * p.cache.heads * sp.chunks);
     if (sp.kind == kKv4Few) {
         if (sp.NT == 1) k_kv4_few<T, CP, 1, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
-        else k_kv4_few<T, CP, 2, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
+        else if constexpr (CP > 2) k_kv4_few<T, CP, 2, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
     } else if constexpr (!EVEN || CP < 8) {
         // long heads: one tile, two would not fit the registers, nor one with what an even share takes
         if (sp.NT == 1) k_kv4<T, CP, 1, FULL, EVEN><<<grid, 256, 0, s>>>(p, sp, part, stats);
