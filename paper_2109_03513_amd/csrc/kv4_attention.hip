@@ -137,6 +137,10 @@ template <> struct Work<false> {
     }
 };
 
+// Rows of heads in tiles of sixteen, one scale group to an MFMA.  Bound by VALU issue (decoding a group's codes, its
+// scales and exp2, once for 16 NT rows): 64 sequences of 2048 keys, 8 queries of 4 heads of 128 to a key head, 71 us,
+// 240 TFLOP/s; drafts of five tokens, fp16 heads of 64, 15.2 us and 4 of joins, latency.  Waves without LDS in the loop:
+// each loads its own keys, two steps in flight.
 // CP: the head's groups, padded (FULL: exactly).  What is padded meets zeros of the query, or makes outputs that
 // are not stored; its scales repeat the last group's.
 template <typename T, int CP, int NT, bool FULL, bool EVEN>
@@ -384,7 +388,10 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 // Few rows, one per (query, head): 16 / CP of them to a tile, whose columns are (row, scale group).  A column's query
 // has only its own group's elements, so that one MFMA after the other leaves each group's sum in a column
 // of its own, and a lane needs the scales of one group: four of a key's, four of a value's.  The sum over the
-// groups crosses CP neighbouring lanes; of O^T a column keeps the rows of its group.
+// groups crosses CP neighbouring lanes; of O^T a column keeps the rows of its group.  Against a tile of 16 rows, most of
+// them empty: fewer scales, and registers for three workgroups a CU instead of two (64 ragged sequences up to 8192 keys,
+// 4 heads of 128 to a key head: 127 -> 91 us).  Bound by HBM: those 386 MB in 77 us, 5.0 TB/s (a copy moves 5.2); one
+// sequence of 32768 keys 12.7 us, 3.0 TB/s, launch and ramp.
 template <int CP> __device__ __forceinline__ float over_groups(float v) {
     auto turned = [](float x, auto ctrl) {
         return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
