@@ -283,4 +283,45 @@ struct Kv4Walk {
     }
 };
 
+// What a workgroup has: keys from .. to - 1 of a tile of rows and a head, item by item.  EVEN: its share of all
+// units; else one run of keys, chosen by the host.
+template <bool EVEN> struct Work {
+    Kv4Walk walk;
+    int unit, first, last;
+    Rows rw;
+    int h, from, to, place;
+    bool whole;                       // no other workgroup has keys of it
+    __device__ __forceinline__ Work(const Kv4AttentionParams& p, const Kv4Split& sp, int R, int (*kept)[6][64])
+        : walk(p, kept, R, sp.count) {
+        first = unit = (int)blockIdx.x * walk.per, last = min(unit + walk.per, walk.total);
+    }
+    __device__ __forceinline__ bool next() {
+        if (unit >= last) return false;
+        const Kv4Item it = walk.item(unit, last);
+        unit = it.to;
+        rw = it.rw, h = it.h, from = 128 * (it.from - it.begin), to = 128 * (it.to - it.begin);
+        whole = it.from == it.begin && it.to == it.end;
+        place = 2 * blockIdx.x + (it.begin > first ? 1 : 0);      // what began before or with its units: 0
+        return true;
+    }
+};
+template <> struct Work<false> {
+    Rows rw;
+    int h, from, to, place;
+    bool whole, more;
+    __device__ __forceinline__ Work(const Kv4AttentionParams& p, const Kv4Split& sp, int R, int (*)[6][64]) {
+        int64_t id = blockIdx.x;
+        place = (int)(id % sp.chunks);
+        id /= sp.chunks;
+        h = (int)(id % p.cache.heads);
+        rw = find_rows(p, id / p.cache.heads, sp.tiles, R);
+        from = place * sp.run, to = from + sp.run, whole = sp.chunks == 1, more = rw.row0 < rw.rows;
+    }
+    __device__ __forceinline__ bool next() {
+        const bool had = more;
+        more = false;
+        return had;
+    }
+};
+
 }  // namespace esb

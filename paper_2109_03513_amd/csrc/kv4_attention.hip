@@ -96,47 +96,6 @@ template <int CP> struct Step {
     int bad;             // halves whose page is none of the cache's
 };
 
-// What a workgroup has: keys from .. to - 1 of a tile of rows and a head, item by item.  EVEN: its share of all
-// units; else one run of keys, chosen by the host.
-template <bool EVEN> struct Work {
-    Kv4Walk walk;
-    int unit, first, last;
-    Rows rw;
-    int h, from, to, place;
-    bool whole;                       // no other workgroup has keys of it
-    __device__ __forceinline__ Work(const Kv4AttentionParams& p, const Kv4Split& sp, int R, int (*kept)[6][64])
-        : walk(p, kept, R, sp.count) {
-        first = unit = (int)blockIdx.x * walk.per, last = min(unit + walk.per, walk.total);
-    }
-    __device__ __forceinline__ bool next() {
-        if (unit >= last) return false;
-        const Kv4Item it = walk.item(unit, last);
-        unit = it.to;
-        rw = it.rw, h = it.h, from = 128 * (it.from - it.begin), to = 128 * (it.to - it.begin);
-        whole = it.from == it.begin && it.to == it.end;
-        place = 2 * blockIdx.x + (it.begin > first ? 1 : 0);      // what began before or with its units: 0
-        return true;
-    }
-};
-template <> struct Work<false> {
-    Rows rw;
-    int h, from, to, place;
-    bool whole, more;
-    __device__ __forceinline__ Work(const Kv4AttentionParams& p, const Kv4Split& sp, int R, int (*)[6][64]) {
-        int64_t id = blockIdx.x;
-        place = (int)(id % sp.chunks);
-        id /= sp.chunks;
-        h = (int)(id % p.cache.heads);
-        rw = find_rows(p, id / p.cache.heads, sp.tiles, R);
-        from = place * sp.run, to = from + sp.run, whole = sp.chunks == 1, more = rw.row0 < rw.rows;
-    }
-    __device__ __forceinline__ bool next() {
-        const bool had = more;
-        more = false;
-        return had;
-    }
-};
-
 // Rows of heads in tiles of sixteen, one scale group to an MFMA.  Bound by VALU issue (decoding a group's codes, its
 // scales and exp2, once for 16 NT rows): 64 sequences of 2048 keys, 8 queries of 4 heads of 128 to a key head, 71 us,
 // 240 TFLOP/s; drafts of five tokens, fp16 heads of 64, 15.2 us and 4 of joins, latency.  Waves without LDS in the loop:
@@ -885,9 +844,12 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
         return s;
     }
     // What takes the least time: rounds of as many workgroups as run at once (256 rows a CU, 128 of long heads), each
-    // as long as its part of the keys; and the join, which moves a part's sums in about the time of 1700 keys (two
-    // sequences of 8192 keys, 512 queries of 32 heads of 128: 290 us whole, 192 in two parts; 16 of 2048, 64 queries: 87
-    // and 122).
+    // as long as its part of the keys; and the join, which moves a part's sums in about the time of 1700 keys.  Heads of
+    // 128, 32 over 8, us: two sequences of 8192 keys and 512 queries 290 whole, 192 in two parts; 16 of 2048 and 64 queries
+    // 87 and 122.  Or even shares, of which each workgroup and each tile leaves a part: for sequences of different
+    // lengths, which runs of one length do not fit, where they are not a fifth behind (two ragged ones of up to 512 over
+    // 8192 172 -> 146, two equal ones 217 and 222, one of 16384 179 and 191); where the first queries of a tile see few
+    // of its keys the shares would not be even.
     const int64_t tiles = starts ? std::max(tokens * group / s.R, std::min((int64_t)seqs, tokens)) : s.slots;
     const int64_t base = tiles * kv_heads, at_once = (d > 128 ? 1 : 2 / s.NT) * cus;
     int64_t n = 1;
@@ -896,6 +858,11 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
         const double rounds = (double)((base * m + at_once - 1) / at_once) / m;
         const double time = rounds + (m > 1 ? 1700.0 * m / longest * base / at_once : 0.0);
         if (m == 1 || time < least) least = time, n = m;
+    }
+    const double even = (double)base / at_once + 1700.0 / longest * (base + at_once) / at_once;
+    if (even < (seqs > 1 ? 1.2 : 1.0) * least && d <= 128 && 4 * (rows / group) <= longest) {
+        s.count = (int)at_once;
+        return s;
     }
     const int64_t run = std::max(((longest + n - 1) / n + 127) / 128 * 128, (int64_t)128);
     s.run = (int)run;
@@ -941,7 +908,8 @@ hipError_t launch_t(int type, const Kv4AttentionParams& p, hipStream_t s) {
     float2* stats = (float2*)p.ws;
     float* part = (float*)(p.ws + stats_bytes(places(sp, rows)));
     if (sp.count) {
-        const hipError_t e = launch_d<T, true>(p, sp, part, stats, s);
+        const hipError_t e = sp.kind == kKv4Many ? launch_kv4_many(type, p, sp, part, stats, s)
+                                                 : launch_d<T, true>(p, sp, part, stats, s);
         if (e != hipSuccess) return e;
         // As many rows as fit, or four workgroups to an item of many parts.
         const bool items = sp.slots * p.cache.heads < sp.count;

@@ -367,6 +367,24 @@ def test_even_shares(esb, t, kv, group, d, page, many):
     assert bool((out[sum(counts):] == 3.0).all())
 
 
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("kv,group,d,page", [(2, 4, 128, 64), (1, 7, 64, 16), (1, 1, 32, 16), (2, 3, 96, 32)])
+@pytest.mark.parametrize("size", [40, 130])
+def test_even_shares_of_many_rows(esb, t, kv, group, d, page, size):
+    """Parts of prompts, some empty, some without keys before them, over a table of many columns."""
+    counts = [size, 0, 3 * size, 1, 2 * size + 7, size // 2]
+    counts = [n * 4 // group if n > 1 else n for n in counts]
+    lengths = [n + k for n, k in zip(counts, [700, 5, 0, 300, 1100, 64])]
+    lengths[5] = max(counts[5] - 9, 0)      # the first tokens see nothing
+    c = Cache(esb, 79, lengths, kv, d, page, columns=400000 // page)
+    q = queries(80, sum(counts) + 3, kv * group, d, ref.TYPES[t])
+    starts = torch.tensor([sum(counts[:i]) for i in range(7)], dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 3.0)
+    esb.esb_kv4_attention(q, c.cache, page, kv, c.pages, c.lengths, starts=starts, out=out)
+    verify(c, q, out, counts)
+    assert bool((out[sum(counts):] == 3.0).all())
+
+
 def test_even_shares_of_anything(esb):
     """The same over bad lengths and pages, and starts that do not ascend or leave the tokens."""
     lengths = [100, 90, 700, 70]
