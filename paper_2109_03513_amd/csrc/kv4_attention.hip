@@ -24,6 +24,7 @@ namespace esb {
 
 namespace {
 
+constexpr int kMostEven = 1024;      // sequences among which work is shared evenly, at most
 constexpr int kRuns = 16;      // parts of a row that one thread joins, at most
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -829,10 +830,11 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
         // queries 21 and 30).  They cost two to seven us more where there is little (one sequence of 32768, one query
         // of 4 heads 18 and 15 in runs; 64 of 512, 24 and 12), and a workgroup of one tile is light enough that runs of
         // the shorter contexts fill the card (256 of 1024: 83 and 68; 64 ragged ones up to 8192: 82 and 90).
-        // Tiles of long heads have no registers for it (256: 8 queries 277, 240 in runs).
+        // Tiles of long heads have no registers for it (256: 8 queries 277, 240 in runs).  Of thousands of sequences there
+        // are enough workgroups without, and each would go over all their lengths.
         const bool light = s.kind == kKv4Few && s.NT == 1;
         if (base * ((longest + 127) / 128) >= (light ? 16 : 4) * at_once && longest >= (light ? 4096 : 256) &&
-            (s.kind == kKv4Few || d <= 128)) {
+            (s.kind == kKv4Few || d <= 128) && seqs <= kMostEven) {
             s.count = (int)at_once;
             return s;
         }
@@ -860,7 +862,8 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
         if (m == 1 || time < least) least = time, n = m;
     }
     const double even = (double)base / at_once + 1700.0 / longest * (base + at_once) / at_once;
-    if (even < (seqs > 1 ? 1.2 : 1.0) * least && d <= 128 && 4 * (rows / group) <= longest) {
+    if (even < (seqs > 1 ? 1.2 : 1.0) * least && d <= 128 && 4 * (rows / group) <= longest &&
+        seqs <= kMostEven) {
         s.count = (int)at_once;
         return s;
     }
