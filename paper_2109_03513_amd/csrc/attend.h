@@ -30,7 +30,7 @@ template <int DP> __device__ __forceinline__ int key_turn(int row) { return DP =
 // A lane holds one row (lane % 32): of the scores S^T = K Q^T of a 32-key block keys 8 (i / 4) + 4 (lane / 32) + i % 4,
 // which are those that the second product O^T = V^T P^T wants of its operand, eight at a time; of O^T the
 // elements 32 d + 8 (i / 4) + 4 (lane / 32) + i % 4.
-template <typename T, int DP, int KT> struct Flash {
+template <typename T, int DP, int KT> struct Attend {
     typedef typename Vec8<T>::type V;
     static constexpr int P = DP / 8, DB = DP / 32, KB = KT / 32;
     V qf[DP / 16];       // elements 16 s + 8 (lane / 32) .. + 7 of the row

@@ -10,7 +10,7 @@
 // (their sum is not): an error of the terms that is below the rounding of the output.
 #include <type_traits>
 
-#include "flash.h"
+#include "attend.h"
 
 namespace esb {
 
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256 * KS, DP == 256 ? 1 : 2) void k_attention(Atten
     const int open = last_of(row0), wave_open = last_of(row0 + 32 * wave);      // every row sees keys up to here
     const int wave_keys = row0 + 32 * wave < rows ? last_of(min(row0 + 32 * wave + 32, rows) - 1) + 1 : 0;
 
-    Flash<T, DP, KT> fl;
+    Attend<T, DP, KT> fl;
     fl.start();
     {
         const T* q = (const T*)p.q.p + (t.begin + row / p.group) * p.q.token + (h * p.group + row % p.group) * p.q.head;

@@ -18,7 +18,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "flash.h"
+#include "attend.h"
 
 namespace esb {
 

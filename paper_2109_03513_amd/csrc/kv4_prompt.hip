@@ -12,7 +12,7 @@
 // the rows that see them.
 #include <type_traits>
 
-#include "flash.h"
+#include "attend.h"
 
 namespace esb {
 
@@ -89,7 +89,7 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
         const int head = h * p.group + row % p.group;
         const int64_t token = rw.begin + row / p.group;
 
-        Flash<_Float16, DP, KT> fl;
+        Attend<_Float16, DP, KT> fl;
         fl.start();
         int q_exponent;
         {
