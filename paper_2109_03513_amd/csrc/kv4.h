@@ -85,7 +85,7 @@ struct Kv4Split {
     int run, chunks;     // keys of a workgroup, and how many there are of such runs
 };
 constexpr int kKv4Few = 0, kKv4Some = 1, kKv4Many = 2;
-// The kernel of many rows (kv4_prompt.hip): 128 of them to a workgroup.
+// The kernel of many rows (kv4_prompt.hip): R of them to a workgroup.
 hipError_t launch_kv4_many(int type, const Kv4AttentionParams& p, const Kv4Split& sp, float* part, float2* stats,
                            hipStream_t s);
 size_t kv4_attention_workspace(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool starts,
