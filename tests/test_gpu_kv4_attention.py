@@ -385,6 +385,17 @@ def test_even_shares_of_many_rows(esb, t, kv, group, d, page, size):
     assert bool((out[sum(counts):] == 3.0).all())
 
 
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("kv,group,d,page", [(1, 96, 64, 16), (2, 65, 128, 64), (1, 200, 96, 32), (1, 300, 256, 64)])
+@pytest.mark.parametrize("columns", [None, 4096])
+def test_large_groups(esb, t, kv, group, d, page, columns):
+    """One query a sequence, whose heads alone are many rows."""
+    lengths = [1, 0, 65, 700, 64, 2000, 129]
+    c = Cache(esb, 81, lengths, kv, d, page, columns=columns)
+    q = queries(82, len(lengths), kv * group, d, ref.TYPES[t])
+    verify(c, q, esb.esb_kv4_attention(q, c.cache, page, kv, c.pages, c.lengths), [1] * len(lengths))
+
+
 def test_even_shares_of_anything(esb):
     """The same over bad lengths and pages, and starts that do not ascend or leave the tokens."""
     lengths = [100, 90, 700, 70]
