@@ -351,7 +351,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 // groups crosses CP neighbouring lanes; of O^T a column keeps the rows of its group.  Against a tile of 16 rows, most of
 // them empty: fewer scales, and registers for three workgroups a CU instead of two (64 ragged sequences up to 8192 keys,
 // 4 heads of 128 to a key head: 127 -> 91 us).  Bound by HBM: those 386 MB in 77 us, 5.0 TB/s (a copy moves 5.2); one
-// sequence of 32768 keys 12.7 us, 3.0 TB/s, launch and ramp.
+// sequence of 32768 keys 12.1 us, 3.1 TB/s, launch and ramp.
 template <int CP> __device__ __forceinline__ float over_groups(float v) {
     auto turned = [](float x, auto ctrl) {
         return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
@@ -820,6 +820,7 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
     s.chunks = 1;
     s.tiles = (group + s.R - 1) / s.R;
     s.slots = starts ? tokens * group / s.R + seqs : (int64_t)seqs * s.tiles;
+    const int64_t tiles = starts ? std::max(tokens * group / s.R, std::min((int64_t)seqs, tokens)) : s.slots;      // about
     if (s.kind != kKv4Many) {
         // workgroups that run at once, by the registers that their kernels take
         const int few = cp * s.NT == 2 ? 4 : cp * s.NT == 4 ? 3 : cp * s.NT == 8 ? 2 : 1;
@@ -828,8 +829,8 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
         // Even shares of the work, where there is much: heavy workgroups from four units each on (64 sequences of 2048
         // keys, heads of 128: 8 queries of 4 heads 71 us, 134 in runs; 2 queries 41 and 63; 16 sequences of 1024, 8
         // queries 21 and 30).  They cost two to seven us more where there is little (one sequence of 32768, one query
-        // of 4 heads 18 and 15 in runs; 64 of 512, 24 and 12), and a workgroup of one tile is light enough that runs of
-        // the shorter contexts fill the card (256 of 1024: 83 and 68; 64 ragged ones up to 8192: 82 and 90).
+        // of 4 heads 18 and 15 in runs; 64 of 512, 24 and 12), and workgroups of one tile are light enough that runs of
+        // the shorter contexts fill the card (256 of 1024: 83 and 54; 64 ragged ones up to 8192: 82 and 90).
         // Tiles of long heads have no registers for it (256: 8 queries 277, 240 in runs).  Of thousands of sequences there
         // are enough workgroups without, and each would go over all their lengths.
         const bool light = s.kind == kKv4Few && s.NT == 1;
@@ -838,11 +839,29 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
             s.count = (int)at_once;
             return s;
         }
-        // parts of about 576 keys (five steps a wave), for twelve workgroups a CU
-        const int64_t n = std::max(std::min((12 * cus + base - 1) / base, (longest + 575) / 576), (int64_t)1);
-        const int64_t run = std::max(((longest + n - 1) / n + 127) / 128 * 128, (int64_t)128);
-        s.run = (int)run;
-        s.chunks = std::max((int)((longest + run - 1) / run), 1);
+        // Whole, or runs of a power of two of keys (runs of 3, 5 or 6 times 128 measured up to a fifth slower than those of
+        // 4 and 8), whichever takes the least time, counted in about 2.1 ns: a key of a head of 128 takes three alone on a
+        // CU, five beside another workgroup, eight beside two; a workgroup 1430 before and after its keys, the join 1900
+        // and ten a part.  One query of 4 heads, us in runs of 512, 1024, 2048: a sequence of 32768 keys 16.4, 16.8, 23.2;
+        // of 131072 39, 35, 31; 64 of 2048 35, 35 and 27, then whole; 256 of 1024 68 and, whole, 54.
+        const double key = cp / 4.0 * s.NT * (s.kind == kKv4Few ? 1 : 2);
+        auto time = [&](int64_t run, int64_t parts) {
+            const int64_t workgroups = tiles * kv_heads * parts;
+            auto round = [&](int64_t some) {      // of so many workgroups at once
+                const int64_t beside = (some + cus - 1) / cus;
+                return some ? run * key * (beside == 1 ? 3 : beside == 2 ? 5 : 3 * beside - 1) + 1430.0 : 0.0;
+            };
+            return workgroups / at_once * round(at_once) + round(workgroups % at_once) +
+                   (parts > 1 ? 1900.0 + 10.0 * parts : 0.0);
+        };
+        int64_t best = std::max((longest + 127) / 128 * 128, (int64_t)128);
+        double least = time(best, 1);
+        for (int64_t run = 128; run < longest; run *= 2) {
+            const double t = time(run, (longest + run - 1) / run);
+            if (t < least) least = t, best = run;
+        }
+        s.run = (int)best;
+        s.chunks = std::max((int)((longest + best - 1) / best), 1);
         return s;
     }
     // What takes the least time: rounds of as many workgroups as run at once (256 rows a CU, 128 of long heads), each
@@ -852,7 +871,6 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
     // lengths, which runs of one length do not fit, where they are not a fifth behind (two ragged ones of up to 512 over
     // 8192 172 -> 146, two equal ones 217 and 222, one of 16384 179 and 191); where the first queries of a tile see few
     // of its keys the shares would not be even.
-    const int64_t tiles = starts ? std::max(tokens * group / s.R, std::min((int64_t)seqs, tokens)) : s.slots;
     const int64_t base = tiles * kv_heads, at_once = (d > 128 ? 1 : 2 / s.NT) * cus;
     int64_t n = 1;
     double least = 0.0;
