@@ -829,21 +829,23 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
         // Even shares of the work, where there is much: heavy workgroups from four units each on (64 sequences of 2048
         // keys, heads of 128: 8 queries of 4 heads 71 us, 134 in runs; 2 queries 41 and 63; 16 sequences of 1024, 8
         // queries 21 and 30).  They cost two to seven us more where there is little (one sequence of 32768, one query
-        // of 4 heads 18 and 15 in runs; 64 of 512, 24 and 12), and workgroups of one tile are light enough that runs of
-        // the shorter contexts fill the card (256 of 1024: 83 and 54; 64 ragged ones up to 8192: 82 and 90).
-        // Tiles of long heads have no registers for it (256: 8 queries 277, 240 in runs).  Of thousands of sequences there
-        // are enough workgroups without, and each would go over all their lengths.
+        // of 4 heads 18 and 15 in runs; 64 of 512, 24 and 12).  Workgroups of one tile are light enough that whole
+        // contexts fill the card (64 of 8192 keys: 121 and 108; as many ragged ones 82 and 81), but a sequence of 32768
+        // by itself takes 207 whole: shares for contexts from 4096 on, which may be as different as that.  Tiles of long
+        // heads have no registers for it (256: 8 queries 277, 240 in runs).  Of thousands of sequences there are enough
+        // workgroups without, and each would go over all their lengths.
         const bool light = s.kind == kKv4Few && s.NT == 1;
         if (base * ((longest + 127) / 128) >= (light ? 16 : 4) * at_once && longest >= (light ? 4096 : 256) &&
             (s.kind == kKv4Few || d <= 128) && seqs <= kMostEven) {
             s.count = (int)at_once;
             return s;
         }
-        // Whole, or runs of a power of two of keys (runs of 3, 5 or 6 times 128 measured up to a fifth slower than those of
-        // 4 and 8), whichever takes the least time, counted in about 2.1 ns: a key of a head of 128 takes three alone on a
-        // CU, five beside another workgroup, eight beside two; a workgroup 1430 before and after its keys, the join 1900
-        // and ten a part.  One query of 4 heads, us in runs of 512, 1024, 2048: a sequence of 32768 keys 16.4, 16.8, 23.2;
-        // of 131072 39, 35, 31; 64 of 2048 35, 35 and 27, then whole; 256 of 1024 68 and, whole, 54.
+        // Whole to 4096 keys, or runs of a power of two up to 2048, so that one long sequence is not left alone (runs of 3,
+        // 5 or 6 times 128 measured up to a fifth slower than those of 4 and 8), whichever takes the least time, counted in
+        // about 2.1 ns: a key of a head of 128 takes three alone on a CU, five beside another workgroup, eight beside two;
+        // a workgroup 1430 before and after its keys, the join 1900 and ten a part.  One query of 4 heads, us in runs of
+        // 512, 1024, 2048: a sequence of 32768 keys 16.4, 16.8, 23.2; of 131072 39, 35, 31; 64 of 2048 35, 35 and, whole,
+        // 27; 256 of 1024 68 and, whole, 54.
         const double key = cp / 4.0 * s.NT * (s.kind == kKv4Few ? 1 : 2);
         auto time = [&](int64_t run, int64_t parts) {
             const int64_t workgroups = tiles * kv_heads * parts;
@@ -854,9 +856,9 @@ Kv4Split split(int64_t tokens, int q_heads, int d, int kv_heads, int seqs, bool 
             return workgroups / at_once * round(at_once) + round(workgroups % at_once) +
                    (parts > 1 ? 1900.0 + 10.0 * parts : 0.0);
         };
-        int64_t best = std::max((longest + 127) / 128 * 128, (int64_t)128);
-        double least = time(best, 1);
-        for (int64_t run = 128; run < longest; run *= 2) {
+        int64_t best = longest <= 4096 ? std::max((longest + 127) / 128 * 128, (int64_t)128) : 2048;
+        double least = time(best, (longest + best - 1) / best);
+        for (int64_t run = 128; run < longest && run <= 2048; run *= 2) {
             const double t = time(run, (longest + run - 1) / run);
             if (t < least) least = t, best = run;
         }
