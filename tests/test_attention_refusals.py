@@ -112,14 +112,14 @@ def test_cache(esb):
 def test_cache_attention(esb):
     L = esb.lib()
     size = L.esb_kv4_attention_workspace_size
-    need = size(3, 8, 64, 4, 3, 0, 64, 16)
+    need = size(3, 8, 64, 4, 3, 0, 640, 16)
     assert need > 0 and size(3, 8, 64, 4, 3, 0, 0, 16) == 0
     for bad in ((-1, 8, 64, 4, 3, 0, 64, 16), (3, 7, 64, 4, 3, 0, 64, 16), (3, 8, 48, 4, 3, 0, 64, 16),
                 (3, 8, 64, 4, -3, 0, 64, 16), (3, 8, 64, 4, 3, 0, -1, 16), (3, 8, 64, 4, 3, 0, 1 << 40, 16),
                 (3, 8, 64, 4, 3, 0, 64, 20)):
         assert size(*bad) == 0, bad
 
-    def attend(q=0, t=BF16, tokens=3, c=0, seqs=3, starts=None, lengths=FAKE, pages=FAKE, pitch=64, columns=64,
+    def attend(q=0, t=BF16, tokens=3, c=0, seqs=3, starts=None, lengths=FAKE, pages=FAKE, pitch=640, columns=640,
                scale=0.1, o=0, ws=FAKE, wb=need):
         q = heads(esb, n=8) if q == 0 else q
         o = heads(esb, n=8, data=OTHER) if o == 0 else o
@@ -129,7 +129,7 @@ def test_cache_attention(esb):
 
     H = lambda **kw: heads(esb, **kw)  # noqa: E731
     for bad in (dict(q=None), dict(o=None), dict(c=None), dict(t=E4M3), dict(tokens=-1), dict(tokens=2), dict(seqs=-1),
-                dict(lengths=None), dict(pages=None), dict(pitch=63), dict(columns=-1), dict(scale=0.0),
+                dict(lengths=None), dict(pages=None), dict(pitch=639), dict(columns=-1), dict(scale=0.0),
                 dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(o=H(n=8)),
                 dict(q=H(n=6), o=H(n=6, data=OTHER)), dict(o=H(n=4, data=OTHER)), dict(starts=ODD), dict(lengths=ODD),
                 dict(pages=ODD), dict(ws=FAKE + 16), dict(q=H(n=8, data=ODD)), dict(o=H(n=8, data=OTHER, token=0)),
