@@ -109,7 +109,7 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 }
             }
             most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-            q_exponent = (int)(most >> 23) - 127;
+            q_exponent = most ? (int)(most >> 23) - 127 : 0;
 #pragma unroll
             for (int s = 0; s < DP / 16; s++) {
                 f32x8 v = __builtin_convertvector(raw[s], f32x8);
@@ -257,7 +257,10 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 load(j0 + 2 * KT, next), next = page_of(j0 + 3 * KT);
                 if (alive) {
                     const f16x8* vs = vt[stage];
-                    fl.weights(__builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), j0 + KT - 1 > wave_open, last - j0 - 4 * half);
+                    // at least the smallest normal number, under which all scores are as good as zero: a zero would make
+                    // masked ones, -infinity, NaN
+                    const float scale = fmaxf(__builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), 0x1p-126f);
+                    fl.weights(scale, j0 + KT - 1 > wave_open, last - j0 - 4 * half);
                     fl.products([&](int r, int d) { return vs[((r >> 4) * 2 + half) * DP + 32 * d + col]; });
                     if (ve_next > ve) {
                         const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
