@@ -7,6 +7,9 @@
 namespace esb {
 
 constexpr float kLazy = 8.0f;      // how far a score may pass the maximum (log2)
+// A maximum m from which on scores are rounded before it is taken from them: x scale - m in one rounding is off by the
+// rounding of m itself, 2^-24 of it, which soon is more than exp2 may be given.
+constexpr float kFar = 0x1p20f;
 constexpr float kNegInf = -__builtin_inff();
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -82,6 +85,12 @@ template <typename T, int DP, int KT> struct Attend {
             for (int d = 0; d < DB; d++) acc[d] *= f;
         }
         const float m = top == kNegInf ? 0.0f : top;
+        if (__builtin_expect(__ballot(fabsf(m) > kFar) != 0, 0)) {      // those rows only
+            const float by = fabsf(m) > kFar ? scale : 1.0f;
+#pragma unroll
+            for (int b = 0; b < KB; b++) x[b] *= by;
+            scale = fabsf(m) > kFar ? 1.0f : scale;
+        }
 #pragma unroll
         for (int b = 0; b < KB; b++)
 #pragma unroll

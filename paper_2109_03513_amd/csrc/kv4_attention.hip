@@ -224,6 +224,14 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                     for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
                 }
             }
+            float scale[NT];
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                scale[u] = p.scale;
+                const bool far = fabsf(top[u]) > kFar && top[u] > kNegInf;
+                if (__builtin_expect(__ballot(far) != 0, 0) && far)
+                    x[u][0] *= p.scale, x[u][1] *= p.scale, scale[u] = 1.0f;
+            }
 #pragma unroll
             for (int u = 0; u < NT; u++) {
                 const float m = top[u] == kNegInf ? 0.0f : top[u];
@@ -231,7 +239,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 for (int hh = 0; hh < 2; hh++)
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        x[u][hh][r] = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
+                        x[u][hh][r] = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], scale[u], -m));
                         sum[u] += x[u][hh][r];
                     }
             }
@@ -498,6 +506,14 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                     for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
                 }
             }
+            float scale[NT];
+#pragma unroll
+            for (int u = 0; u < NT; u++) {
+                scale[u] = p.scale;
+                const bool far = fabsf(top[u]) > kFar && top[u] > kNegInf;
+                if (__builtin_expect(__ballot(far) != 0, 0) && far)
+                    x[u][0] *= p.scale, x[u][1] *= p.scale, scale[u] = 1.0f;
+            }
             const f32x4 b[2] = {four(st.va[0]), four(st.va[1])};
             bf16x8 hi[NT], lo[NT];
 #pragma unroll
@@ -508,7 +524,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 for (int hh = 0; hh < 2; hh++)
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
+                        const float e = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], scale[u], -m));
                         sum[u] += e;
                         w[4 * hh + r] = e * b[hh][r];
                     }

@@ -1,0 +1,38 @@
+"""esb_attention at the ends of its types.  Tolerances as in test_gpu_attention."""
+import pytest
+import torch
+
+import attention_ref as ref
+from test_gpu_attention import esb, make, starts  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def verify(q, k, v, out, causal=True, scale=None):
+    """One sequence.  A weight below fp32's smallest normal number, beside a largest one of at least 1, may count
+    as zero: that is 2^-126 of the sum of |v|."""
+    n, m, d = q.shape[0], k.shape[0], q.shape[2]
+    last = torch.arange(n) + m - n if causal else torch.full((n,), m - 1)
+    want = ref.attend(q, k, v, last, d ** -0.5 if scale is None else scale)
+    ref.check(out, *want, keys=m, d=d, p_round=ref.ROUND[q.dtype],
+              p_step=2.0 ** -25 if q.dtype == torch.float16 else 2.0 ** -126)
+
+
+@pytest.mark.parametrize("power", [10, 18, 24, 32, 60])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("n", [150, 1200])
+def test_large_scores(esb, power, d, n):  # noqa: F811
+    """Scores of about 2^power, finite: the largest takes all, and nothing is NaN."""
+    q, k, v = (make(s, n, h, d, dtype=BF16) for s, h in ((46, 2), (47, 1), (48, 1)))
+    k = (k.double() * 2.0 ** power).to(BF16)
+    verify(q, k, v, esb.esb_attention(q, k, v, starts([n])))
+    verify(q, k, v, esb.esb_attention(q, k, v, starts([n]), causal=False), causal=False)
+
+
+@pytest.mark.parametrize("power", [18, 30])
+def test_large_scores_f16(esb, power):  # noqa: F811
+    n = 300
+    q, k, v = (make(s, n, h, 64, dtype=torch.float16) for s, h in ((46, 2), (47, 1), (48, 1)))
+    q, k = ((x.double() * 2.0 ** (power // 2 - 3)).to(torch.float16) for x in (q, k))
+    verify(q, k, v, esb.esb_attention(q, k, v, starts([n])))

@@ -56,3 +56,45 @@ def test_tiny_products(esb):  # noqa: F811
         q = queries(7, 40, 4, 128, BF16, size=size)
         out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([40]), scale=scale)
         verify(c, q, out, [40], scale=scale)
+
+
+LEAST = 2.0 ** -126
+
+
+def verify_rows(c, q, out, rows, scale=None, at=0):
+    """Those rows of sequence `at`, whose queries q are, by what they see.  A weight below fp32's smallest normal
+    number, beside a largest one of at least 1, may count as zero: that is LEAST of the sum of |v|."""
+    k, v = c.read(at)
+    n = q.shape[0]
+    last = torch.arange(n) + k.shape[0] - n
+    rows = torch.as_tensor(rows)
+    m = int(last[rows].max()) + 1
+    many = n * (q.shape[1] // c.heads) > 64
+    want = ref.attend(q[rows], k[:m], v[:m], last[rows], c.d ** -0.5 if scale is None else scale)
+    p_round = 2.0 ** -11 if many else 2.0 ** -8 if q.dtype == BF16 else 2.0 ** -16
+    ref.check(out[rows], *want, keys=m, d=c.d, p_round=p_round, p_step=2.0 ** -25 if many else LEAST)
+
+
+@pytest.mark.parametrize("power", [10, 18, 24, 32, 60])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (256, 16)])
+@pytest.mark.parametrize("group,n", [FEW, SOME, MANY, (16, None)])
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("columns", [None, 8192])
+def test_large_scores(esb, power, d, page, group, n, t, columns):  # noqa: F811
+    """Scores of about 2^power, finite: the largest takes all, and nothing is NaN.  The queries before a row of such
+    scores, and heads beside it, are as they were."""
+    c = Cache(esb, 80, [300], 1, d, page, columns=columns)
+    g = torch.Generator(device="cuda").manual_seed(81)
+    codes = [torch.randint(0, 16, (300, 1, d), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    a = (0.4 * torch.exp(0.3 * torch.randn(300, 1, d // 32, generator=g, device="cuda"))).to(BF16)
+    esb.esb_kv4_pack(c.cache, page, codes[0], (a.double() * 2.0 ** power).to(BF16), codes[1], a, c.slots[0])
+    q = queries(82, n or 1, group, d, ref.TYPES[t])
+    call = lambda q: esb.esb_kv4_attention(q, c.cache, page, 1, c.pages, c.lengths, starts=starts([n or 1]))  # noqa: E731
+    verify_rows(c, q, call(q), range(n or 1))
+    q[:, :, :] = (q.double() * 2.0 ** -min(power, 12)).to(q.dtype)
+    want = call(q)
+    far = q.clone()
+    far[-1, -1] = 30000.0
+    out = call(far)
+    assert bool(torch.isfinite(out).all())
+    assert torch.equal(out.flatten(0, 1)[:-1], want.flatten(0, 1)[:-1])
