@@ -692,10 +692,13 @@ int esb_kv4_unpack(const esb_kv4* cache, int64_t tokens, const int64_t* slots, u
  *            sequence's last key may hold anything;
  *   scale    positive, and finite times log2(e).
  * A query that sees no key gets zeros.  What lies in the cache behind what a query sees does not
- * reach it.  A length beyond columns * page makes the sequence's outputs NaN, a page number that is
- * not the cache's those of the queries that see it.  Scores, statistics and sums are fp32; the
- * products p_j alpha enter the matrix cores as bf16 (fp16 outputs: as two bf16, 16 bits), or, with more
- * than 64 rows a sequence on average (tokens x heads of a group), p_j as fp16.
+ * reach it, but that p_j may be rounded otherwise (below).  A length beyond columns * page makes the
+ * sequence's outputs NaN, a page number that is not the cache's those of the queries that see it.
+ * Scores, statistics and sums are fp32, of 32 elements first of q and the codes (|q| < 2^120); the
+ * products p_j alpha enter the matrix cores as bf16 (fp16 outputs: as two bf16, 16 bits).  With more
+ * than 64 rows a sequence on average (tokens x heads of a group) p_j enters as fp16, with q, k and v
+ * as fp16 too, brought there by powers of two where that costs them no bit; where it would, p_j alpha
+ * enters as two bf16 and the rest as above, but scales below 2^-125 count as zero beside ones from 2^-97 on.
  *   workspace  device, 256-byte aligned, esb_kv4_attention_workspace_size() bytes (0 where keys
  *              are not split over workgroups).  It carries nothing between calls; concurrent calls
  *              need distinct ones.  Less or NULL: ESB_E_WORKSPACE.

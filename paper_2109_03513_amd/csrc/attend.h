@@ -13,6 +13,31 @@ constexpr float kFar = 0x1p20f;
 constexpr float kNegInf = -__builtin_inff();
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename F, typename P>
+__device__ __forceinline__ F join4(P a, P b, P c, P d) {
+    return __builtin_bit_cast(F, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                                       __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)});
+}
+// Eight nibbles, lowest first.
+__device__ __forceinline__ bf16x8 decode(uint32_t w, __bf16) {
+    return join4<bf16x8>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+}
+__device__ __forceinline__ f16x8 decode(uint32_t w, _Float16) {
+    return join4<f16x8>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3));
+}
+// Four bf16 scales as fp32.
+__device__ __forceinline__ f32x4 four(uint2 s) {
+    return f32x4{__uint_as_float(s.x << 16), __uint_as_float(s.x & 0xffff0000u), __uint_as_float(s.y << 16),
+                 __uint_as_float(s.y & 0xffff0000u)};
+}
 
 __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -21,8 +46,8 @@ __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 // Whether a maximum has to move from `top` for a score of `most`.
-__device__ __forceinline__ bool passes(float most, float top) {
-    return most > top + kLazy || (top == kNegInf && most > kNegInf);
+__device__ __forceinline__ bool passes(float most, float top, float lazy = kLazy) {
+    return most > top + lazy || (top == kNegInf && most > kNegInf);
 }
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
@@ -61,7 +86,7 @@ template <typename T, int DP, int KT> struct Attend {
     }
 
     // What exp makes of them.  masks: keys after `end`, counted from 4 (lane / 32), are not seen.
-    __device__ __forceinline__ void weights(float scale, bool masks, int end) {
+    __device__ __forceinline__ void weights(float scale, bool masks, int end, float lazy = kLazy) {
         if (masks) {
 #pragma unroll
             for (int b = 0; b < KB; b++)
@@ -75,9 +100,9 @@ template <typename T, int DP, int KT> struct Attend {
 #pragma unroll
             for (int i = 0; i < 16; i++) most = fmaxf(most, x[b][i]);
         most *= scale;
-        if (__ballot(passes(most, top))) {
+        if (__ballot(passes(most, top, lazy))) {
             // row by row: what a row gives does not depend on its neighbours
-            const float all = fmaxf(most, other_half(most)), now = passes(all, top) ? all : top;
+            const float all = fmaxf(most, other_half(most)), now = passes(all, top, lazy) ? all : top;
             const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= f;

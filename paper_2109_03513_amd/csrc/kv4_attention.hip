@@ -27,29 +27,10 @@ namespace {
 constexpr int kMostEven = 1024;      // sequences among which work is shared evenly, at most
 constexpr int kRuns = 16;      // parts of a row that one thread joins, at most
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int N> struct Words {
     typedef uint32_t w __attribute__((ext_vector_type(N)));
 };
 
-template <typename F, typename P>
-__device__ __forceinline__ F join4(P a, P b, P c, P d) {
-    return __builtin_bit_cast(F, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
-                                       __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)});
-}
-// Eight nibbles, lowest first.
-__device__ __forceinline__ bf16x8 decode(uint32_t w, __bf16) {
-    return join4<bf16x8>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
-}
-__device__ __forceinline__ f16x8 decode(uint32_t w, _Float16) {
-    return join4<f16x8>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0),
-                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1),
-                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2),
-                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3));
-}
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -73,11 +54,6 @@ __device__ __forceinline__ void value_pairs(uint32_t a, uint32_t b, bf16x8* even
     }
     *even = join4<bf16x8>(lo[0], lo[1], lo[2], lo[3]);
     *odd = join4<bf16x8>(hi[0], hi[1], hi[2], hi[3]);
-}
-// Four bf16 scales as fp32.
-__device__ __forceinline__ f32x4 four(uint2 s) {
-    return f32x4{__uint_as_float(s.x << 16), __uint_as_float(s.x & 0xffff0000u), __uint_as_float(s.y << 16),
-                 __uint_as_float(s.y & 0xffff0000u)};
 }
 // Over the four lanes that hold one column.
 __device__ __forceinline__ float column_max(float v) {

@@ -3,10 +3,18 @@
 // with their scales, into LDS as fp16, where its waves read it.
 //
 // E2M1 times a bf16 scale has ten bits: exact in fp16, where its range allows.  So a tile's key scales are
-// brought below 2 by a power of two (the largest one's exponent, which the scores get back with the scale of the
-// softmax), the query's row likewise, and the value scales by the largest exponent met so far (when it grows, the
-// sums follow).  What then lies below fp16's normal numbers is off by 2^-25 of the largest of its tile.  The products
-// are fp16 MFMAs for both types of queries; probabilities are rounded to fp16.
+// brought below 2^(kUp + 1) by a power of two (which the scores get back with the scale of the softmax), a row of bf16
+// queries to the end of fp16 likewise, and the value scales by the largest exponent met so far (when it grows, the
+// sums follow).  Then scales down to 2^-kSpread of the largest keep all their bits, elements of a query down to 2^-32.  The
+// products are fp16 MFMAs for both types of queries; probabilities are rounded to fp16.
+//
+// Larger keys and values that a row does not see, or gives no weight, must not cost it the bits of those that it
+// sees.  So where scales or a query's elements lie further apart, the item is gone over once more in the form of
+// kv4_attention.hip (wide_pass), whose scales stay fp32: codes and queries as they are into the MFMAs, a key's scale on
+// the sum of its group, a value's on the probability, which enters as two bf16.  Looking for that costs -3 to 3 % (heads of
+// 64 to 128, us, without and with: the two ragged sequences below 141 and 141, 2048 queries over 8192 keys 300 and 305, 64
+// over 2048 33.9 and 34.8), 4 % for heads of 256 (269 and 279).  Scales below 2^-125 are those of zeros: they are not
+// looked for, so that zeros among other tokens stay as fast.
 //
 // Values whose scale is not finite count as zero in the products, and their elements become NaN at the end for
 // the rows that see them.
@@ -19,7 +27,6 @@ namespace esb {
 namespace {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t bits(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
 __device__ __forceinline__ f16x2 halves(uint32_t v) { return __builtin_bit_cast(f16x2, v); }
@@ -37,6 +44,12 @@ __device__ __forceinline__ int exponent(uint32_t b) {
     const int e = (b >> 7) & 0xff;
     return e == 0xff ? 0 : e;
 }
+constexpr int kUp = 12;          // a tile's largest scale is brought to this exponent: times 6 it is within fp16
+constexpr int kSpread = 28;      // 2^(kUp - kSpread) in eight bits times 0.5 is a multiple of 2^-24, fp16's smallest step
+constexpr int kBias = 127 + kUp;
+// Whether a scale of at least 2^-125 lies too far below 2^(e + kUp): is_below(scale, limit(e)).
+__device__ __forceinline__ uint32_t limit(int e) { return (uint32_t)max(e + kBias - kSpread - 2, 0); }
+__device__ __forceinline__ bool is_below(uint32_t b, uint32_t limit) { return (b >> 7 & 0xff) - 2u < limit; }
 template <int CTRL> __device__ __forceinline__ int turned(int v) {
     return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
 }
@@ -54,6 +67,105 @@ __device__ __forceinline__ int wave_max(int v) {
                max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
+// The fallback for an item, which usual data never takes: its keys k0 .. k1 - 1 for the 32 rows of a wave from `row0` on,
+// in fp32 but for codes and queries, and its outputs (to < 0) or its part: the first row's place among the parts (EVEN),
+// or the part's number.  Maxima move at once, so that no weight is above 1.  Operands come straight from the
+// cache, and the scores are formed again for every 32 elements of the output, so that the kernel's registers
+// are those of the usual pass (with all accumulators at once they spilled, for 8 % of the usual pass's time).
+template <typename T, bool EVEN>
+__device__ __forceinline__ void wide_pass(const Kv4AttentionParams& p, const Rows& rw, int h, int k0, int k1, int row0, int64_t to,
+                                          int chunks, float* part, float2* stats) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));      // nothing is kept from before the usual pass
+    const int col = lane & 31, half = lane >> 5, C = p.cache.groups, page = p.cache.page;
+    const int row = row0 + col, last = rw.len - rw.n + row / p.group, head = h * p.group + row % p.group;
+    const int64_t token = rw.begin + row / p.group;
+    const bool live = row < rw.rows, whole = to < 0;
+    k1 = min(k1, rw.len - rw.n + (min(row0 + 32, rw.rows) - 1) / p.group + 1);
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    const T* q = (const T*)p.q.p + token * p.q.token + head * p.q.head + 8 * half;
+    // key j's place in its page, from the last key on that key's; a token's run of four shares it
+    struct Place {
+        const uint8_t* block;
+        int t;
+        bool bad;
+    };
+    auto place = [&](int j) {
+        j = min(j, k1 - 1);
+        const int pid = table[j >> p.cache.shift];
+        const bool bad = pid < 0 || pid >= p.cache.pages;
+        return Place{p.cache.block(bad ? 0 : pid, h), j & (page - 1), bad};
+    };
+#pragma unroll 1
+    for (int d = 0; d < C; d++) {
+        Attend<_Float16, 32, 32> fl;
+        fl.start();
+#pragma unroll 1
+        for (int j0 = k0; j0 < k1; j0 += 32) {
+            fl.x[0] = f32x16{};
+#pragma unroll 1
+            for (int g = 0; g < C; g++) {
+                const Place mine = place(j0 + col);
+                const uint8_t* words = mine.block + mine.t * 16 * C + half * 4 * C + 4 * g;
+                typename Vec8<T>::type q0 = {}, q1 = {};
+                if (live) q0 = load8(q + 32 * g, 8), q1 = load8(q + 32 * g + 16, 8);
+                f32x16 z = mma(decode(*(const uint32_t*)words, T{}), q0, f32x16{});
+                z = mma(decode(*(const uint32_t*)(words + 8 * C), T{}), q1, z);
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const Place run = place(j0 + 8 * r + 4 * half);
+                    f32x4 a = four(*(const uint2*)(run.block + p.cache.key_scales_at() + p.cache.scale_run(run.t) + 8 * g));
+                    if (run.bad) a = f32x4{} + __builtin_nanf("");
+#pragma unroll
+                    for (int i = 0; i < 4; i++) fl.x[0][4 * r + i] = fmaf(a[i], z[4 * r + i], fl.x[0][4 * r + i]);
+                }
+            }
+            fl.weights(p.scale, true, last - j0 - 4 * half, 0.0f);
+#pragma unroll
+            for (int s = 0; s < 2; s++) {
+                // keys `at` .. + 3 and `at` + 8 .. + 11 in turn; a byte has elements 2 a and 2 a + 1 of a key
+                const int at = j0 + 16 * s + 4 * half;
+                uint32_t w[2];
+                f32x8 pa;
+#pragma unroll
+                for (int r = 0; r < 2; r++) {
+                    const Place run = place(at + 8 * r);
+                    const uint8_t* v = run.block + p.cache.values_at() + ((run.t >> 2) * 16 + (col >> 1)) * 4 * C;
+                    w[r] = *(const uint32_t*)(v + 4 * d) >> 4 * (col & 1) & 0x0f0f0f0fu;
+                    const f32x4 a = four(*(const uint2*)(run.block + p.cache.value_scales_at() + p.cache.scale_run(run.t) + 8 * d));
+#pragma unroll
+                    for (int i = 0; i < 4; i++)      // scales behind the last key may be anything
+                        pa[2 * i + r] = at + 8 * r + i > last ? 0.0f : fl.x[0][8 * s + 4 * r + i] * a[i];
+                }
+                const bf16x8 v = decode(w[0] | w[1] << 4, __bf16{});
+                const bf16x8 hi = __builtin_convertvector(pa, bf16x8);
+                const bf16x8 lo = __builtin_convertvector(pa - __builtin_convertvector(hi, f32x8), bf16x8);
+                fl.acc[0] = mma(v, hi, fl.acc[0]);
+                fl.acc[0] = mma(v, lo, fl.acc[0]);
+            }
+        }
+        const float sum = fl.sum + other_half(fl.sum);
+        if (!live) continue;
+        const int64_t at = EVEN ? to + col : (token * p.q.heads + head) * chunks + to;
+        const float f = !whole ? 1.0f : last >= 0 ? 1.0f / sum : 0.0f;
+        if (!whole && half == 0 && d == 0) stats[at] = make_float2(fl.top, sum);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int e = 32 * d + 8 * k + 4 * half;
+            f32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = fl.acc[0][4 * k + i] * f;
+            if (!whole) {
+                *(f32x4*)(part + at * p.d + e) = w;
+            } else {
+                if (rw.bad) w = f32x4{} + __builtin_nanf("");
+                typedef T t4 __attribute__((ext_vector_type(4)));
+                ((Loose<t4, T>*)((T*)p.o.p + token * p.o.token + head * p.o.head + e))->v = __builtin_convertvector(w, t4);
+            }
+        }
+    }
+}
+
 // Bound by the matrix cores and VALU in turn, and by what the fewest tiles leave idle: 2048 queries of 32 heads of 128
 // over 16384 keys 583 to 635 us by card, 870 to 940 TFLOP/s; two ragged sequences of up to 512 over 8192 keys 146, 575.
 // Decoded in registers by each wave it was 378, into LDS by four waves 236, scales shared by the
@@ -67,7 +179,8 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
     __shared__ f16x8 vt[2][KT / 8 * DP];         // [16 keys][half][element]: keys 4 half .. + 3 and 8 + 4 half .. + 3
     __shared__ _Float16 vscales[WAVES][16 / WAVES][4 * CP];      // a wave's: [run][group][key of the run]
     __shared__ int2 peaks[2][WAVES];             // by wave: largest exponents of the key and the value scales
-    __shared__ int odd;
+    __shared__ int odd;                          // some value's scale is not finite
+    __shared__ int wide;                         // scales, or a query's elements, lie too far apart
     __shared__ int kept[EVEN ? WAVES : 1][6][64];
     Work<EVEN> work(p, sp, R, kept);
     while (work.next()) {
@@ -91,10 +204,11 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 
         Attend<_Float16, DP, KT> fl;
         fl.start();
-        int q_exponent;
+        int q_exponent = 0;
+        bool q_wide = false;
         {
             V raw[DP / 16];
-            uint32_t most = 0;
+            uint32_t most = 0, least = ~0u;
             const T* q = (const T*)p.q.p + token * p.q.token + head * p.q.head;
 #pragma unroll
             for (int s = 0; s < DP / 16; s++) {
@@ -106,10 +220,14 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 for (int i = 0; i < 8; i++) {
                     const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
                     if (b <= 0x7f800000u) most = max(most, b);
+                    least = min(least, b - 1);      // but for zero
                 }
             }
             most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-            q_exponent = most ? (int)(most >> 23) - 127 : 0;
+            if (std::is_same<T, __bf16>::value && most && most < 0x7f800000u) {
+                q_exponent = (int)(most >> 23) - 127 - 15;
+                q_wide = (least >> 23) + 32 < (most >> 23);
+            }
 #pragma unroll
             for (int s = 0; s < DP / 16; s++) {
                 f32x8 v = __builtin_convertvector(raw[s], f32x8);
@@ -171,7 +289,7 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
             int2 m = peaks[stage][0];
 #pragma unroll
             for (int w = 1; w < WAVES; w++) m.x = max(m.x, peaks[stage][w].x), m.y = max(m.y, peaks[stage][w].y);
-            return make_int2(m.x - 127, m.y - 127);
+            return make_int2(m.x - kBias, m.y - kBias);
         };
         // The tile that was brought, as fp16 under the two exponents: share() first, then decoded() in registers, then
         // put() into LDS, so that the arithmetic may run beside products of the other stage.
@@ -180,18 +298,23 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
         u32x4 kd[CT], vd[CT];
         auto share = [&](int ke, int ve) {
             _Float16* own = vscales[wave][run4 & (4 / H - 1)];
+            const uint32_t lk = limit(ke), lv = limit(ve);
+            bool below = false;
 #pragma unroll
             for (int u = 0; u < NV; u++) {
                 const float v = bf16_value(va[u]);
                 const bool fine = fabsf(v) < __builtin_inff();
                 if (!fine) odd = 1;
+                below |= is_below(va[u], lv);
                 if (CP >= 4 || a16 < 8) own[a16 + 16 * u] = fine ? (_Float16)__builtin_amdgcn_ldexpf(v, -ve) : (_Float16)0.0f;
             }
 #pragma unroll
             for (int u = 0; u < NK; u++) {
+                below |= is_below(ka[u], lk);
                 const _Float16 k = (_Float16)__builtin_amdgcn_ldexpf(bf16_value(ka[u]), -ke);
                 ks[u] = bits(f16x2{k, k});
             }
+            if (__builtin_expect(__ballot(below) != 0, 0)) wide = 1;
             __builtin_amdgcn_wave_barrier();      // LDS serves a wave in order
 #pragma unroll
             for (int g = 0; g < CT; g++) vs4[g] = ((const uint2*)own)[gv + g];
@@ -223,14 +346,15 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
             }
         };
 
-        if (tid == 0) odd = 0;
-        int ke = 0, ve = -127;
+        if (tid == 0) odd = wide = 0;
+        int ke = 0, ve = -kBias, ve_first = -kBias;
         if (k0 < k1) {
             load(k0, page_of(k0));
             int next = page_of(k0 + KT);
             put_peaks(0);
             __syncthreads();
-            ke = peak(0).x, ve = peak(0).y;
+            if (q_wide) wide = 1;
+            ke = peak(0).x, ve = ve_first = peak(0).y;
             share(ke, ve);
             decoded();
             put(0);
@@ -258,20 +382,32 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 if (alive) {
                     const f16x8* vs = vt[stage];
                     // at least the smallest normal number, under which all scores are as good as zero: a zero would make
-                    // masked ones, -infinity, NaN
-                    const float scale = fmaxf(__builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), 0x1p-126f);
+                    // masked ones, -infinity, NaN; and no infinity, which would make NaN of scores of zero
+                    const float scale = __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(p.scale, q_exponent + ke), 0x1p-126f,
+                                                                0x1.fffffep127f);
                     fl.weights(scale, j0 + KT - 1 > wave_open, last - j0 - 4 * half);
                     fl.products([&](int r, int d) { return vs[((r >> 4) * 2 + half) * DP + 32 * d + col]; });
                     if (ve_next > ve) {
                         const float f = __builtin_amdgcn_ldexpf(1.0f, max(ve - ve_next, -126));
 #pragma unroll
                         for (int d = 0; d < DB; d++) fl.acc[d] *= f;
+                        // sums keep their bits while they come down by less than 2^60; before ve_first there were zeros
+                        if (ve < 2 - kBias) ve_first = ve_next;
+                        if (ve_next - ve_first > 60) wide = 1;
                     }
                 }
                 ke = ke_next, ve = ve_next;
             }
             __syncthreads();
-            if (odd) {
+            if (__builtin_expect(wide, 0)) {
+                if (alive)
+                    wide_pass<T, EVEN>(p, rw, h, k0, k1, rw.row0 + 32 * wave,
+                                       work.whole ? -1 : EVEN ? (int64_t)work.place * R + 32 * wave : work.place, sp.chunks, part, stats);
+                if (!EVEN) return;
+                __syncthreads();
+                continue;
+            }
+            if (__builtin_expect(odd, 0)) {
                 for (int j = k0; j < k1; j++) {
                     const int pid = table[j >> p.cache.shift];
                     if (pid < 0 || pid >= p.cache.pages) continue;

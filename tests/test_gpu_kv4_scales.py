@@ -98,3 +98,108 @@ def test_large_scores(esb, power, d, page, group, n, t, columns):  # noqa: F811
     out = call(far)
     assert bool(torch.isfinite(out).all())
     assert torch.equal(out.flatten(0, 1)[:-1], want.flatten(0, 1)[:-1])
+
+
+def spread(esb, c, seed, alpha_k, alpha_v):  # noqa: F811
+    """Keys and values of sequence 0 with the given scales (tokens x heads x groups)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = c.slots[0].numel()
+    k, v = (torch.randint(0, 16, (n, c.heads, c.d), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2))
+    esb.esb_kv4_pack(c.cache, c.page, k, alpha_k.to(BF16), v, alpha_v.to(BF16), c.slots[0])
+
+
+@pytest.mark.parametrize("power", [13, 20, 24, 30, 40, 100])
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 16), (128, 64), (256, 32)])
+@pytest.mark.parametrize("group,n", [SOME, MANY])
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("columns", [None, 8192])
+def test_large_scales_out_of_sight(esb, power, what, d, page, group, n, t, columns):  # noqa: F811
+    """A later key or value that is 2^power times the others does not reach the queries before it."""
+    log("kv4 out of sight 2^%d %s d=%d group=%d %s columns=%s" % (power, what, d, group, t, columns))
+    for before in (30, 333):                # a first tile of keys, and after several
+        c = Cache(esb, 40, [before + n], 1, d, page, columns=columns)
+        g = torch.Generator(device="cuda").manual_seed(41)
+        a = [0.4 * torch.exp(0.3 * torch.randn(before + n, 1, d // 32, generator=g, device="cuda")) for _ in range(2)]
+        at = before + n - 9                 # the last nine queries see it
+        a[what == "v"][at] *= 2.0 ** power
+        spread(esb, c, 42, *a)
+        q = queries(43, n, group, d, ref.TYPES[t])
+        out = esb.esb_kv4_attention(q, c.cache, page, 1, c.pages, c.lengths, starts=starts([n]))
+        verify_rows(c, q, out, range(n - 9))
+        if t == "bf16":
+            verify_rows(c, q, out, range(n))
+
+
+@pytest.mark.parametrize("power", [16, 24, 40, 100, -24, -60])
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (224, 16)])
+@pytest.mark.parametrize("group,n", [FEW, SOME, MANY])
+def test_groups_far_apart(esb, power, what, d, page, group, n):  # noqa: F811
+    """One scale group of a head 2^power times the others: each keeps its bits."""
+    log("kv4 groups 2^%d %s d=%d group=%d n=%s" % (power, what, d, group, n))
+    c = Cache(esb, 50, [200], 1, d, page)
+    g = torch.Generator(device="cuda").manual_seed(51)
+    a = [0.4 * torch.exp(0.3 * torch.randn(200, 1, d // 32, generator=g, device="cuda")) for _ in range(2)]
+    a[what == "v"][:, :, 1] *= 2.0 ** power
+    spread(esb, c, 52, *a)
+    q = queries(53, n or 1, group, d, BF16)
+    if what == "k":
+        q[:, :, 32:64] *= 2.0 ** -min(abs(power), 60) if power > 0 else 1      # scores that the other groups decide
+    out = esb.esb_kv4_attention(q, c.cache, page, 1, c.pages, c.lengths, starts=starts([n or 1]))
+    verify_rows(c, q, out, range(n or 1))
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (256, 16)])
+@pytest.mark.parametrize("columns", [None, 8192])
+def test_keys_far_apart(esb, d, page, columns):  # noqa: F811
+    """Scales of keys and values anywhere over 2^80, seen by all; queries whose elements are as far apart."""
+    c = Cache(esb, 60, [300], 1, d, page, columns=columns)
+    g = torch.Generator(device="cuda").manual_seed(61)
+    for wide_q in (False, True):
+        a = [2.0 ** torch.randint(-60, 20, (300, 1, d // 32), generator=g, device="cuda").double() for _ in range(2)]
+        spread(esb, c, 62, *a)
+        q = queries(63, 40, 8, d, torch.float32)
+        if wide_q:
+            q = q * 2.0 ** torch.randint(-60, 1, q.shape, generator=g, device="cuda").float()
+        out = esb.esb_kv4_attention(q.to(BF16), c.cache, page, 1, c.pages, c.lengths, starts=starts([40]))
+        verify_rows(c, q.to(BF16), out, range(40))
+
+
+def test_zero_tokens_among_others(esb):  # noqa: F811
+    """Appended zeros have the least scale of all, beside ordinary keys and values."""
+    n, d = 200, 128
+    c = Cache(esb, 64, [n], 1, d, 16)
+    k, v = queries(65, n, 1, d, BF16), queries(66, n, 1, d, BF16)
+    k[50:90], v[70:120] = 0, 0
+    k[130, :, 32:64], v[131, :, 64:] = 0, 0
+    esb.esb_kv4_append(c.cache, 16, k, v, c.slots[0])
+    q = queries(67, 60, 4, d, BF16)
+    out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([60]))
+    verify(c, q, out, [60])
+
+
+def test_far_apart_in_graphs(esb):  # noqa: F811
+    """A captured call whose cache takes the usual way in one replay and the other in the next."""
+    c = Cache(esb, 90, [400], 1, 128, 16, columns=8192)
+    g = torch.Generator(device="cuda").manual_seed(91)
+    a = 0.4 * torch.exp(0.3 * torch.randn(400, 1, 4, generator=g, device="cuda"))
+    spread(esb, c, 92, a, a)
+    near = c.cache.clone()
+    a[380, 0, 2] *= 2.0 ** 40
+    a[3, 0, 1] *= 2.0 ** -50
+    spread(esb, c, 92, a, a)
+    caches = [near, c.cache.clone()]
+    q = queries(93, 40, 8, 128, BF16)
+    st = starts([40])
+    want = [esb.esb_kv4_attention(q, x, 16, 1, c.pages, c.lengths, starts=st) for x in caches]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=st)
+    for turn in range(5):
+        c.cache.copy_(caches[turn % 2])
+        graph.replay()
+        assert torch.equal(out, want[turn % 2])
+        torch.cuda.synchronize()
+        verify_rows(c, q, out, range(40))
