@@ -1,5 +1,6 @@
-// One pass of softmax attention over tiles of keys in LDS, as attention.hip and kv4_prompt.hip share it: 32 rows
-// (queries x heads) to a wave, on 32x32x16 MFMAs, with a running maximum and sum.
+// What the attention kernels share: one pass of softmax attention over tiles of keys in LDS (attention.hip, kv4_prompt.hip),
+// 32 rows (queries x heads) to a wave, on 32x32x16 MFMAs, with a running maximum and sum; the decoding of the 4-bit
+// cache, and the fallback over it for numbers that lie too far apart for the usual passes.
 #pragma once
 
 #include "kv4.h"
@@ -141,5 +142,105 @@ template <typename T, int DP, int KT> struct Attend {
             }
     }
 };
+
+// The fallback for an item over the 4-bit cache, which usual data never takes: keys k0 .. k1 - 1 for the rows from `row0` on
+// that `mask` has, by one wave, in fp32 but for codes and queries: a key's scale is on the sum of its group, a value's on the
+// probability, which enters as two bf16.  Maxima move at once, so that no weight is above 1.  It leaves the outputs
+// (to < 0) or the item's part: the first row's place among the parts (EVEN), or the part's number.  Operands come straight
+// from the cache, and the scores are formed again for every 32 elements of the output, so that a kernel's registers are
+// those of its usual pass (with all accumulators at once that of kv4_prompt.hip spilled, for 8 % of its time).
+template <typename T, bool EVEN>
+__device__ __forceinline__ void wide_pass(const Kv4AttentionParams& p, const Rows& rw, int h, int k0, int k1, int row0, uint32_t mask, int64_t to,
+                                          int chunks, float* part, float2* stats) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));      // nothing is kept from before the usual pass
+    const int col = lane & 31, half = lane >> 5, C = p.cache.groups, page = p.cache.page;
+    const int row = row0 + col, last = rw.len - rw.n + row / p.group, head = h * p.group + row % p.group;
+    const int64_t token = rw.begin + row / p.group;
+    const bool live = row < rw.rows && mask >> col & 1, whole = to < 0;
+    k1 = min(k1, rw.len - rw.n + (min(row0 + 32, rw.rows) - 1) / p.group + 1);
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    const T* q = (const T*)p.q.p + token * p.q.token + head * p.q.head + 8 * half;
+    // key j's place in its page, from the last key on that key's; a token's run of four shares it
+    struct Place {
+        const uint8_t* block;
+        int t;
+        bool bad;
+    };
+    auto place = [&](int j) {
+        j = min(j, k1 - 1);
+        const int pid = table[j >> p.cache.shift];
+        const bool bad = pid < 0 || pid >= p.cache.pages;
+        return Place{p.cache.block(bad ? 0 : pid, h), j & (page - 1), bad};
+    };
+#pragma unroll 1
+    for (int d = 0; d < C; d++) {
+        Attend<_Float16, 32, 32> fl;
+        fl.start();
+#pragma unroll 1
+        for (int j0 = k0; j0 < k1; j0 += 32) {
+            fl.x[0] = f32x16{};
+#pragma unroll 1
+            for (int g = 0; g < C; g++) {
+                const Place mine = place(j0 + col);
+                const uint8_t* words = mine.block + mine.t * 16 * C + half * 4 * C + 4 * g;
+                typename Vec8<T>::type q0 = {}, q1 = {};
+                if (live) q0 = load8(q + 32 * g, 8), q1 = load8(q + 32 * g + 16, 8);
+                f32x16 z = mma(decode(*(const uint32_t*)words, T{}), q0, f32x16{});
+                z = mma(decode(*(const uint32_t*)(words + 8 * C), T{}), q1, z);
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const Place run = place(j0 + 8 * r + 4 * half);
+                    f32x4 a = four(*(const uint2*)(run.block + p.cache.key_scales_at() + p.cache.scale_run(run.t) + 8 * g));
+                    if (run.bad) a = f32x4{} + __builtin_nanf("");
+#pragma unroll
+                    for (int i = 0; i < 4; i++) fl.x[0][4 * r + i] = fmaf(a[i], z[4 * r + i], fl.x[0][4 * r + i]);
+                }
+            }
+            fl.weights(p.scale, true, last - j0 - 4 * half, 0.0f);
+#pragma unroll
+            for (int s = 0; s < 2; s++) {
+                // keys `at` .. + 3 and `at` + 8 .. + 11 in turn; a byte has elements 2 a and 2 a + 1 of a key
+                const int at = j0 + 16 * s + 4 * half;
+                uint32_t w[2];
+                f32x8 pa;
+#pragma unroll
+                for (int r = 0; r < 2; r++) {
+                    const Place run = place(at + 8 * r);
+                    const uint8_t* v = run.block + p.cache.values_at() + ((run.t >> 2) * 16 + (col >> 1)) * 4 * C;
+                    w[r] = *(const uint32_t*)(v + 4 * d) >> 4 * (col & 1) & 0x0f0f0f0fu;
+                    const f32x4 a = four(*(const uint2*)(run.block + p.cache.value_scales_at() + p.cache.scale_run(run.t) + 8 * d));
+#pragma unroll
+                    for (int i = 0; i < 4; i++)      // scales behind the last key may be anything
+                        pa[2 * i + r] = at + 8 * r + i > last ? 0.0f : fl.x[0][8 * s + 4 * r + i] * a[i];
+                }
+                const bf16x8 v = decode(w[0] | w[1] << 4, __bf16{});
+                const bf16x8 hi = __builtin_convertvector(pa, bf16x8);
+                const bf16x8 lo = __builtin_convertvector(pa - __builtin_convertvector(hi, f32x8), bf16x8);
+                fl.acc[0] = mma(v, hi, fl.acc[0]);
+                fl.acc[0] = mma(v, lo, fl.acc[0]);
+            }
+        }
+        const float sum = fl.sum + other_half(fl.sum);
+        if (!live) continue;
+        const int64_t at = EVEN ? to + col : (token * p.q.heads + head) * chunks + to;
+        const float f = !whole ? 1.0f : last >= 0 ? 1.0f / sum : 0.0f;
+        if (!whole && half == 0 && d == 0) stats[at] = make_float2(fl.top, sum);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int e = 32 * d + 8 * k + 4 * half;
+            f32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = fl.acc[0][4 * k + i] * f;
+            if (!whole) {
+                *(f32x4*)(part + at * p.d + e) = w;
+            } else {
+                if (rw.bad) w = f32x4{} + __builtin_nanf("");
+                typedef T t4 __attribute__((ext_vector_type(4)));
+                ((Loose<t4, T>*)((T*)p.o.p + token * p.o.token + head * p.o.head + e))->v = __builtin_convertvector(w, t4);
+            }
+        }
+    }
+}
 
 }  // namespace esb

@@ -14,7 +14,8 @@
 // waves take every fourth step of 32 keys, each with its own running maximum and sum, and join them in
 // LDS.  The keys are split over workgroups too, in runs or in even shares of all work (split() below),
 // and a k_join_... adds the parts.  The running maximum moves only when a score passes it by 2^8, so
-// most steps cross no lanes.
+// most steps cross no lanes; where sums of values near the end of fp32 leave it for that, their rows are gone over once
+// more (wide_pass).
 #include <algorithm>
 #include <type_traits>
 
@@ -25,6 +26,7 @@ namespace esb {
 namespace {
 
 constexpr int kMostEven = 1024;      // sequences among which work is shared evenly, at most
+constexpr uint32_t kLarge = 0x71800000;      // 2^100: as many parts of it as there may be are within fp32
 constexpr int kRuns = 16;      // parts of a row that one thread joins, at most
 
 template <int N> struct Words {
@@ -63,6 +65,24 @@ __device__ __forceinline__ float column_max(float v) {
 __device__ __forceinline__ float column_sum(float v) {
     v += __shfl_xor(v, 16);
     return v + __shfl_xor(v, 32);
+}
+
+// Whether sums of weights of up to 2^kLazy times values are not finite, or so large that those of further parts might leave
+// fp32.  Such rows take wide_pass.
+__device__ __forceinline__ bool is_large(f32x8 o) {
+    int above = 0;
+    uint32_t below = 0;      // by sign
+#pragma unroll
+    for (int e = 0; e < 8; e++) above = max(above, __float_as_int(o[e])), below = max(below, __float_as_uint(o[e]));
+    return above >= (int)kLarge || below >= (kLarge | 0x80000000u);
+}
+// The rows of which some of a wave's lanes, N to a row, say so.
+template <int N> __device__ __forceinline__ uint32_t rows_of(uint64_t lanes) {
+    uint32_t rows = 0;
+#pragma unroll
+    for (int j = 0; j < 64 / N; j++)
+        if (lanes >> N * j & ((1ull << N) - 1)) rows |= 1u << j;
+    return rows;
 }
 
 // What a wave brings of 32 keys, in two halves of 16.  Keys: the lane's words of key lane % 16; values: its
@@ -288,6 +308,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
             top[u] = m;
         }
         const int col = threadIdx.x >> 4, dd = 8 * (threadIdx.x & 15);
+        uint32_t large = 0;      // rows of this wave's
 #pragma unroll
         for (int u = 0; u < NT; u++) {
 #pragma unroll
@@ -304,12 +325,13 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 __syncthreads();
                 const float m = __shfl(top[u], col), l = __shfl(total[u], col);
                 const int r = rw.row0 + 16 * u + col, e0 = 32 * c0 + dd;
+                f32x8 o = {};
                 if (r < rw.rows && e0 < 32 * C) {
-                    f32x8 o = {};
 #pragma unroll
                     for (int w = 0; w < 4; w++)
 #pragma unroll
                         for (int e = 0; e < 8; e++) o[e] += sums[w][col][dd + e];
+                    large |= is_large(o) ? 1u << (16 * u) : 0;
                     const int t = r / p.group, head = h * p.group + r % p.group;
                     if (!whole) {
                         const int64_t at = EVEN ? (int64_t)work.place * R + 16 * u + col
@@ -324,6 +346,14 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                     }
                 }
             }
+        }
+        if (__builtin_expect(__any(large), 0)) {
+            __threadfence();      // its stores come after those above
+            uint32_t mask = 0;
+#pragma unroll
+            for (int u = 0; u < NT; u++) mask |= rows_of<16>(__ballot(large >> (16 * u) & 1)) << (16 * u + 4 * wave);
+            wide_pass<T, EVEN>(p, rw, h, work.from, work.to, rw.row0, mask, whole ? -1 : EVEN ? (int64_t)work.place * R : work.place,
+                               sp.chunks, part, stats);
         }
         if (EVEN) __syncthreads();      // the next item uses the same LDS
     }
@@ -566,6 +596,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
         }
         __syncthreads();
         const int row = thread / (4 * CP), e = 8 * (thread % (4 * CP)), r = rw.row0 + row;
+        bool large = false;
         if (row < R && r < rw.rows && e < 32 * C) {
             float m = kNegInf, l = 0.0f;
             const int u = row / HR, column = row % HR * CP;
@@ -578,6 +609,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 l += x.x == kNegInf ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - m);
                 o += *(const f32x8*)&sums[w][row][e];
             }
+            large = is_large(o);
             const int t = r / p.group, head = h * p.group + r % p.group;
             if (!whole) {
                 const int64_t to = EVEN ? (int64_t)work.place * R + row
@@ -589,6 +621,11 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 else if (first + t >= 0) o *= 1.0f / l;
                 store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e, __builtin_convertvector(o, V), 8);
             }
+        }
+        if (__builtin_expect(__any(large), 0)) {
+            __threadfence();      // its stores come after those above
+            wide_pass<T, EVEN>(p, rw, h, work.from, work.to, rw.row0, rows_of<4 * CP>(__ballot(large)) << (16 / CP * wave),
+                               whole ? -1 : EVEN ? (int64_t)work.place * R : work.place, sp.chunks, part, stats);
         }
         if (EVEN) __syncthreads();      // the next item uses the same LDS
     }

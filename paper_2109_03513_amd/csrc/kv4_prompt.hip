@@ -47,6 +47,7 @@ __device__ __forceinline__ int exponent(uint32_t b) {
 constexpr int kUp = 12;          // a tile's largest scale is brought to this exponent: times 6 it is within fp16
 constexpr int kSpread = 28;      // 2^(kUp - kSpread) in eight bits times 0.5 is a multiple of 2^-24, fp16's smallest step
 constexpr int kBias = 127 + kUp;
+constexpr int kMost = 80 - kUp;      // values below 2^84 under weights of up to 2^8 have sums within fp32
 // Whether a scale of at least 2^-125 lies too far below 2^(e + kUp): is_below(scale, limit(e)).
 __device__ __forceinline__ uint32_t limit(int e) { return (uint32_t)max(e + kBias - kSpread - 2, 0); }
 __device__ __forceinline__ bool is_below(uint32_t b, uint32_t limit) { return (b >> 7 & 0xff) - 2u < limit; }
@@ -65,105 +66,6 @@ __device__ __forceinline__ int wave_max(int v) {
     v = max(v, turned<0x140>(v));      // sixteen
     return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
                max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
-}
-
-// The fallback for an item, which usual data never takes: its keys k0 .. k1 - 1 for the 32 rows of a wave from `row0` on,
-// in fp32 but for codes and queries, and its outputs (to < 0) or its part: the first row's place among the parts (EVEN),
-// or the part's number.  Maxima move at once, so that no weight is above 1.  Operands come straight from the
-// cache, and the scores are formed again for every 32 elements of the output, so that the kernel's registers
-// are those of the usual pass (with all accumulators at once they spilled, for 8 % of the usual pass's time).
-template <typename T, bool EVEN>
-__device__ __forceinline__ void wide_pass(const Kv4AttentionParams& p, const Rows& rw, int h, int k0, int k1, int row0, int64_t to,
-                                          int chunks, float* part, float2* stats) {
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));      // nothing is kept from before the usual pass
-    const int col = lane & 31, half = lane >> 5, C = p.cache.groups, page = p.cache.page;
-    const int row = row0 + col, last = rw.len - rw.n + row / p.group, head = h * p.group + row % p.group;
-    const int64_t token = rw.begin + row / p.group;
-    const bool live = row < rw.rows, whole = to < 0;
-    k1 = min(k1, rw.len - rw.n + (min(row0 + 32, rw.rows) - 1) / p.group + 1);
-    const int32_t* table = p.table + rw.seq * p.table_pitch;
-    const T* q = (const T*)p.q.p + token * p.q.token + head * p.q.head + 8 * half;
-    // key j's place in its page, from the last key on that key's; a token's run of four shares it
-    struct Place {
-        const uint8_t* block;
-        int t;
-        bool bad;
-    };
-    auto place = [&](int j) {
-        j = min(j, k1 - 1);
-        const int pid = table[j >> p.cache.shift];
-        const bool bad = pid < 0 || pid >= p.cache.pages;
-        return Place{p.cache.block(bad ? 0 : pid, h), j & (page - 1), bad};
-    };
-#pragma unroll 1
-    for (int d = 0; d < C; d++) {
-        Attend<_Float16, 32, 32> fl;
-        fl.start();
-#pragma unroll 1
-        for (int j0 = k0; j0 < k1; j0 += 32) {
-            fl.x[0] = f32x16{};
-#pragma unroll 1
-            for (int g = 0; g < C; g++) {
-                const Place mine = place(j0 + col);
-                const uint8_t* words = mine.block + mine.t * 16 * C + half * 4 * C + 4 * g;
-                typename Vec8<T>::type q0 = {}, q1 = {};
-                if (live) q0 = load8(q + 32 * g, 8), q1 = load8(q + 32 * g + 16, 8);
-                f32x16 z = mma(decode(*(const uint32_t*)words, T{}), q0, f32x16{});
-                z = mma(decode(*(const uint32_t*)(words + 8 * C), T{}), q1, z);
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const Place run = place(j0 + 8 * r + 4 * half);
-                    f32x4 a = four(*(const uint2*)(run.block + p.cache.key_scales_at() + p.cache.scale_run(run.t) + 8 * g));
-                    if (run.bad) a = f32x4{} + __builtin_nanf("");
-#pragma unroll
-                    for (int i = 0; i < 4; i++) fl.x[0][4 * r + i] = fmaf(a[i], z[4 * r + i], fl.x[0][4 * r + i]);
-                }
-            }
-            fl.weights(p.scale, true, last - j0 - 4 * half, 0.0f);
-#pragma unroll
-            for (int s = 0; s < 2; s++) {
-                // keys `at` .. + 3 and `at` + 8 .. + 11 in turn; a byte has elements 2 a and 2 a + 1 of a key
-                const int at = j0 + 16 * s + 4 * half;
-                uint32_t w[2];
-                f32x8 pa;
-#pragma unroll
-                for (int r = 0; r < 2; r++) {
-                    const Place run = place(at + 8 * r);
-                    const uint8_t* v = run.block + p.cache.values_at() + ((run.t >> 2) * 16 + (col >> 1)) * 4 * C;
-                    w[r] = *(const uint32_t*)(v + 4 * d) >> 4 * (col & 1) & 0x0f0f0f0fu;
-                    const f32x4 a = four(*(const uint2*)(run.block + p.cache.value_scales_at() + p.cache.scale_run(run.t) + 8 * d));
-#pragma unroll
-                    for (int i = 0; i < 4; i++)      // scales behind the last key may be anything
-                        pa[2 * i + r] = at + 8 * r + i > last ? 0.0f : fl.x[0][8 * s + 4 * r + i] * a[i];
-                }
-                const bf16x8 v = decode(w[0] | w[1] << 4, __bf16{});
-                const bf16x8 hi = __builtin_convertvector(pa, bf16x8);
-                const bf16x8 lo = __builtin_convertvector(pa - __builtin_convertvector(hi, f32x8), bf16x8);
-                fl.acc[0] = mma(v, hi, fl.acc[0]);
-                fl.acc[0] = mma(v, lo, fl.acc[0]);
-            }
-        }
-        const float sum = fl.sum + other_half(fl.sum);
-        if (!live) continue;
-        const int64_t at = EVEN ? to + col : (token * p.q.heads + head) * chunks + to;
-        const float f = !whole ? 1.0f : last >= 0 ? 1.0f / sum : 0.0f;
-        if (!whole && half == 0 && d == 0) stats[at] = make_float2(fl.top, sum);
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const int e = 32 * d + 8 * k + 4 * half;
-            f32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = fl.acc[0][4 * k + i] * f;
-            if (!whole) {
-                *(f32x4*)(part + at * p.d + e) = w;
-            } else {
-                if (rw.bad) w = f32x4{} + __builtin_nanf("");
-                typedef T t4 __attribute__((ext_vector_type(4)));
-                ((Loose<t4, T>*)((T*)p.o.p + token * p.o.token + head * p.o.head + e))->v = __builtin_convertvector(w, t4);
-            }
-        }
-    }
 }
 
 // Bound by the matrix cores and VALU in turn, and by what the fewest tiles leave idle: 2048 queries of 32 heads of 128
@@ -353,8 +255,8 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
             int next = page_of(k0 + KT);
             put_peaks(0);
             __syncthreads();
-            if (q_wide) wide = 1;
             ke = peak(0).x, ve = ve_first = peak(0).y;
+            if (q_wide || ve > kMost) wide = 1;
             share(ke, ve);
             decoded();
             put(0);
@@ -393,7 +295,7 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                         for (int d = 0; d < DB; d++) fl.acc[d] *= f;
                         // sums keep their bits while they come down by less than 2^60; before ve_first there were zeros
                         if (ve < 2 - kBias) ve_first = ve_next;
-                        if (ve_next - ve_first > 60) wide = 1;
+                        if (ve_next - ve_first > 60 || ve_next > kMost) wide = 1;
                     }
                 }
                 ke = ke_next, ve = ve_next;
@@ -401,7 +303,7 @@ void k_kv4_many(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
             __syncthreads();
             if (__builtin_expect(wide, 0)) {
                 if (alive)
-                    wide_pass<T, EVEN>(p, rw, h, k0, k1, rw.row0 + 32 * wave,
+                    wide_pass<T, EVEN>(p, rw, h, k0, k1, rw.row0 + 32 * wave, ~0u,
                                        work.whole ? -1 : EVEN ? (int64_t)work.place * R + 32 * wave : work.place, sp.chunks, part, stats);
                 if (!EVEN) return;
                 __syncthreads();

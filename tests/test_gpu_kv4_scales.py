@@ -203,3 +203,25 @@ def test_far_apart_in_graphs(esb):  # noqa: F811
         assert torch.equal(out, want[turn % 2])
         torch.cuda.synchronize()
         verify_rows(c, q, out, range(40))
+
+
+@pytest.mark.parametrize("power", [100, 118, 121, 124])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (256, 16)])
+@pytest.mark.parametrize("group,n", [FEW, SOME, MANY, (16, None), (32, None)])
+@pytest.mark.parametrize("columns", [None, 8192])
+def test_largest_values(esb, power, d, page, group, n, columns):  # noqa: F811
+    """Values near the end of bf16 under weights that grow by less than 2^8: outputs are finite, and so are the sums."""
+    log("kv4 largest values 2^%d d=%d group=%d n=%s columns=%s" % (power, d, group, n, columns))
+    m = 700 if columns else 150
+    c = Cache(esb, 70, [m], 1, d, page, columns=columns)
+    codes = torch.full((m, 1, d), 0, dtype=torch.uint8, device="cuda")      # ones
+    up = torch.arange(m, device="cuda").float() / m
+    a = up[:, None, None].expand(m, 1, d // 32).to(BF16).contiguous()
+    # one value in 60 is large, or sums of 700 would leave fp32 themselves
+    va = torch.where(torch.arange(m, device="cuda") % 60 == 7, 2.0 ** power, 2.0 ** (power - 9))
+    va = va[:, None, None].expand(m, 1, d // 32).to(BF16).contiguous()
+    esb.esb_kv4_pack(c.cache, page, codes, a, codes, va, c.slots[0])
+    # scores from 0 to 5.4 (log2: 7.8)
+    q = torch.full((n or 1, group, d), 5.4 / d, dtype=BF16, device="cuda")
+    out = esb.esb_kv4_attention(q, c.cache, page, 1, c.pages, c.lengths, starts=starts([n or 1]), scale=1.0)
+    verify_rows(c, q, out, range(n or 1), scale=1.0)
