@@ -3,6 +3,8 @@
 // cache, and the fallback over it for numbers that lie too far apart for the usual passes.
 #pragma once
 
+#include <type_traits>
+
 #include "kv4.h"
 
 namespace esb {
@@ -62,9 +64,12 @@ template <int DP> __device__ __forceinline__ int key_turn(int row) { return DP =
 template <typename T, int DP, int KT> struct Attend {
     typedef typename Vec8<T>::type V;
     static constexpr int P = DP / 8, DB = DP / 32, KB = KT / 32;
+    // How far `top` is set above the maximum: weights of bf16 values are then at most 1, as their sums might leave fp32; fp16
+    // needs its whole range for the weights, and its values have none to speak of.
+    static constexpr float kLift = std::is_same<T, __bf16>::value ? kLazy : 0.0f;
     V qf[DP / 16];       // elements 16 s + 8 (lane / 32) .. + 7 of the row
     f32x16 acc[DB], x[KB];
-    float top, sum;      // the running maximum (times scale), and the lane's part of the sum
+    float top, sum;      // the running maximum (times scale, and lifted), and the lane's part of the sum
 
     __device__ __forceinline__ void start() {
 #pragma unroll
@@ -101,9 +106,9 @@ template <typename T, int DP, int KT> struct Attend {
 #pragma unroll
             for (int i = 0; i < 16; i++) most = fmaxf(most, x[b][i]);
         most *= scale;
-        if (__ballot(passes(most, top, lazy))) {
+        if (__ballot(passes(most, top, lazy - kLift))) {
             // row by row: what a row gives does not depend on its neighbours
-            const float all = fmaxf(most, other_half(most)), now = passes(all, top, lazy) ? all : top;
+            const float all = fmaxf(most, other_half(most)), now = passes(all, top, lazy - kLift) ? all + kLift : top;
             const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= f;

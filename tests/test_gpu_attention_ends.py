@@ -36,3 +36,24 @@ def test_large_scores_f16(esb, power):  # noqa: F811
     q, k, v = (make(s, n, h, 64, dtype=torch.float16) for s, h in ((46, 2), (47, 1), (48, 1)))
     q, k = ((x.double() * 2.0 ** (power // 2 - 3)).to(torch.float16) for x in (q, k))
     verify(q, k, v, esb.esb_attention(q, k, v, starts([n])))
+
+
+@pytest.mark.parametrize("power", [100, 118, 122, 126])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("n", [150, 1200])
+def test_largest_values(esb, power, d, n):  # noqa: F811
+    """Values near the end of bf16 under weights that grow by less than 2^8: outputs are finite."""
+    up = torch.arange(n, device="cuda").float() / n
+    k = up[:, None, None].expand(n, 1, d).to(BF16).contiguous()
+    v = torch.where(torch.arange(n, device="cuda") % 200 == 110, 2.0 ** power, 2.0 ** (power - 11))
+    v = v[:, None, None].expand(n, 1, d).to(BF16).contiguous()
+    q = torch.full((n, 2, d), 5.4 / d, dtype=BF16, device="cuda")
+    verify(q, k, v, esb.esb_attention(q, k, v, starts([n]), scale=1.0), scale=1.0)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_smallest_values(esb, d):  # noqa: F811
+    n = 300
+    q, k, v = (make(s, n, h, d, dtype=BF16) for s, h in ((43, 2), (44, 1), (45, 1)))
+    v = (v.double() * 2.0 ** -120).to(BF16)
+    verify(q, k, v, esb.esb_attention(q, k, v, starts([n])))
