@@ -108,7 +108,7 @@ template <typename T, int DP, int KT> struct Attend {
         most *= scale;
         if (__ballot(passes(most, top, lazy - kLift))) {
             // row by row: what a row gives does not depend on its neighbours
-            const float all = fmaxf(most, other_half(most)), now = passes(all, top, lazy - kLift) ? all + kLift : top;
+            const float all = fmaxf(most, other_half(most)), now = !passes(all, top, lazy - kLift) ? top : kLift > 0.0f ? all + kLift : all;
             const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= f;

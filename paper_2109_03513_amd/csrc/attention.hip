@@ -43,8 +43,9 @@ template <typename T> __device__ __forceinline__ bool finite(T v) {
 // heads of 128, 527 to 559 us by card for 550 GFLOP, 1.0 PFLOP/s, where a library product reaches 1.22.  Tiles by loads to
 // registers 1110 us, by DMA in two stages 582, that written out 529.  32 rows to a wave and 64 keys to a tile: what
 // the registers of two workgroups a CU hold.
-// KS: sets of four waves that take every KS-th tile, each in stages of its own, and join their sums at the end.
-template <typename T, int DP, int KT, int KS, bool DMA>
+// KS: sets of four waves that take every KS-th tile, each in stages of its own, and join their sums at the end.  FULL: heads
+// of DP elements; else their rows end before the tiles'.
+template <typename T, int DP, int KT, int KS, bool DMA, bool FULL>
 __global__ __launch_bounds__(256 * KS, DP == 256 ? 1 : 2) void k_attention(AttentionParams p) {
     typedef typename Vec8<T>::type V;
     constexpr int R = 128, P = DP / 8, NP = KT * P / 256, DB = DP / 32;
@@ -89,13 +90,19 @@ __global__ __launch_bounds__(256 * KS, DP == 256 ? 1 : 2) void k_attention(Atten
     const T* kp = (const T*)p.k.p + ka * p.k.token + h * p.k.head;
     const T* vp = (const T*)p.v.p + ka * p.v.token + h * p.v.head;
 
-    // A tile into LDS.  Rows past the last key and pieces past the head repeat the last one: the former are
-    // masked, the latter meet zeros of the query and outputs that are not stored.
+    // A tile into LDS.  Rows past the last key repeat the last one, and are masked.  Pieces past the head are zeros from the
+    // start on for keys, as an infinity would make NaN of the query's zeros, and repeat the last one for values, whose outputs
+    // there are not stored.
     const int most = p.d / 8 - 1, piece = tid % P, r0 = tid / P;
     constexpr int RU = 256 / P;                 // rows that the workgroup brings at a time
     // pieces by the row's turn, which repeats after two of them
     const int ck[2] = {8 * min(piece ^ key_turn<DP>(r0), most), 8 * min(piece ^ key_turn<DP>(r0 + RU), most)};
     const int cv[2] = {8 * min(piece ^ value_turn<DP>(r0), most), 8 * min(piece ^ value_turn<DP>(r0 + RU), most)};
+    auto held = [&](int u) { return FULL || (piece ^ key_turn<DP>(r0 + (u & 1) * RU)) <= most; };
+    if (!FULL)
+#pragma unroll
+        for (int u = 0; u < NP; u++)
+            if (!held(u)) tiles[0][0][tid + 256 * u] = tiles[1][0][tid + 256 * u] = V{};
     const int k_pitch = (int)p.k.token, v_pitch = (int)p.v.token;      // DMA: tiles' offsets fit 32 bits
     auto fetch = [&](int j0, int stage) {
         const T* kb = kp + (int64_t)j0 * p.k.token;
@@ -103,25 +110,45 @@ __global__ __launch_bounds__(256 * KS, DP == 256 ? 1 : 2) void k_attention(Atten
         const int end = nk - 1 - j0;
         if (DMA) {
             const int place = 64 * wave;
-            if (end >= KT - 1) {
+            const bool all = end >= KT - 1;
+            auto key = [&](int u) {
+                const int r = all ? r0 : min(r0 + u * RU, end);
+                dma16(all ? kb + (int64_t)(u * RU) * p.k.token : kb, 2 * (uint32_t)(r * k_pitch + ck[u & 1]), &tiles[stage][0][place + 256 * u]);
+            };
+            auto value = [&](int u) {
+                const int r = all ? r0 : min(r0 + u * RU, end);
+                dma16(all ? vb + (int64_t)(u * RU) * p.v.token : vb, 2 * (uint32_t)(r * v_pitch + cv[u & 1]), &tiles[stage][1][place + 256 * u]);
+            };
+            if (!FULL)      // lanes apart, whose pieces are the same ones in every row, or every other one
+#pragma unroll
+                for (int turn = 0; turn < (DP == 256 ? 2 : 1); turn++)
+                    if (held(turn)) {
+                        if (all) {
+#pragma unroll
+                            for (int u = turn; u < NP; u += DP == 256 ? 2 : 1) key(u);
+                        } else {
+#pragma unroll 1
+                            for (int u = turn; u < NP; u += DP == 256 ? 2 : 1) key(u);
+                        }
+                    }
+            if (all) {
 #pragma unroll
                 for (int u = 0; u < NP; u++) {
-                    dma16(kb + (int64_t)(u * RU) * p.k.token, 2 * (uint32_t)(r0 * k_pitch + ck[u & 1]), &tiles[stage][0][place + 256 * u]);
-                    dma16(vb + (int64_t)(u * RU) * p.v.token, 2 * (uint32_t)(r0 * v_pitch + cv[u & 1]), &tiles[stage][1][place + 256 * u]);
+                    if (FULL) key(u);
+                    value(u);
                 }
             } else {
 #pragma unroll 1
                 for (int u = 0; u < NP; u++) {
-                    const int r = min(r0 + u * RU, end);
-                    dma16(kb, 2 * (uint32_t)(r * k_pitch + ck[u & 1]), &tiles[stage][0][place + 256 * u]);
-                    dma16(vb, 2 * (uint32_t)(r * v_pitch + cv[u & 1]), &tiles[stage][1][place + 256 * u]);
+                    if (FULL) key(u);
+                    value(u);
                 }
             }
         } else {
 #pragma unroll
             for (int u = 0; u < NP; u++) {
                 const int64_t r = min(r0 + u * RU, end);
-                tiles[stage][0][tid + 256 * u] = load8(kb + r * p.k.token + ck[u & 1], 8);
+                if (held(u)) tiles[stage][0][tid + 256 * u] = load8(kb + r * p.k.token + ck[u & 1], 8);
                 tiles[stage][1][tid + 256 * u] = load8(vb + r * p.v.token + cv[u & 1], 8);
             }
         }
@@ -247,7 +274,7 @@ template <typename T> bool dma_takes(const HeadsView& v) {
     return (uintptr_t)v.p % 16 == 0 && v.token % 8 == 0 && (v.heads == 1 || v.head % 8 == 0) && v.token < (1 << 24);
 }
 
-template <typename T, int DP, int KT>
+template <typename T, int DP, int KT, bool FULL>
 hipError_t launch_d(const AttentionParams& p, hipStream_t s) {
     const int64_t slots = p.q_tokens * p.group / 128 + p.seqs;
     const unsigned grid = (unsigned)(slots * p.k.heads);
@@ -257,20 +284,23 @@ hipError_t launch_d(const AttentionParams& p, hipStream_t s) {
     // and 174, eight sequences of 512 43 and 56).  Long heads have no registers for a second set.
     if constexpr (DP < 256)
         if (grid <= 2u * num_cus() && p.k_tokens >= (int64_t)256 * p.seqs) {
-            if (dma) k_attention<T, DP, KT, 2, true><<<grid, 512, 0, s>>>(p);
-            else k_attention<T, DP, KT, 2, false><<<grid, 512, 0, s>>>(p);
+            if (dma) k_attention<T, DP, KT, 2, true, FULL><<<grid, 512, 0, s>>>(p);
+            else k_attention<T, DP, KT, 2, false, FULL><<<grid, 512, 0, s>>>(p);
             return hipGetLastError();
         }
-    if (dma) k_attention<T, DP, KT, 1, true><<<grid, 256, 0, s>>>(p);
-    else k_attention<T, DP, KT, 1, false><<<grid, 256, 0, s>>>(p);
+    if (dma) k_attention<T, DP, KT, 1, true, FULL><<<grid, 256, 0, s>>>(p);
+    else k_attention<T, DP, KT, 1, false, FULL><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_t(const AttentionParams& p, hipStream_t s) {
-    if (p.d <= 64) return launch_d<T, 64, 64>(p, s);
-    if (p.d <= 128) return launch_d<T, 128, 64>(p, s);
-    return launch_d<T, 256, 32>(p, s);
+    if (p.d == 64) return launch_d<T, 64, 64, true>(p, s);
+    if (p.d == 128) return launch_d<T, 128, 64, true>(p, s);
+    if (p.d == 256) return launch_d<T, 256, 32, true>(p, s);
+    if (p.d < 64) return launch_d<T, 64, 64, false>(p, s);
+    if (p.d < 128) return launch_d<T, 128, 64, false>(p, s);
+    return launch_d<T, 256, 32, false>(p, s);
 }
 
 }  // namespace

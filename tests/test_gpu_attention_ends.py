@@ -57,3 +57,30 @@ def test_smallest_values(esb, d):  # noqa: F811
     q, k, v = (make(s, n, h, d, dtype=BF16) for s, h in ((43, 2), (44, 1), (45, 1)))
     v = (v.double() * 2.0 ** -120).to(BF16)
     verify(q, k, v, esb.esb_attention(q, k, v, starts([n])))
+
+
+@pytest.mark.parametrize("d", [8, 40, 64, 80, 96, 120, 128, 136, 192, 248, 256])
+@pytest.mark.parametrize("pitched", [False, True])
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+def test_keys_of_minus_infinity(esb, d, pitched, t):  # noqa: F811
+    """A key whose score is -infinity drops out wherever in the head its infinity lies; +infinity is NaN."""
+    n, dtype = 150, ref.TYPES[t]
+    q, k, v = (make(s, n, h, d, dtype=dtype) for s, h in ((40, 2), (41, 1), (42, 1)))
+    q = q.abs() + 0.5
+    for at, where, value in ((0, d - 1, -1), (70, d - 8, -1), (100, d - 3, -1), (101, 0, -1), (147, d - 1, 1)):
+        k[at, 0, where] = value * float("inf")
+    if pitched:      # rows that are not aligned
+        wide = torch.zeros(n, d + 1, dtype=dtype, device="cuda")
+        wide[:, 1:] = k[:, 0]
+        k = wide[:, None, 1:]
+    out = esb.esb_attention(q, k, v, starts([n])).cpu()
+    want = ref.attend(q.cpu(), k.cpu(), v.cpu(), torch.arange(n), d ** -0.5)[0]
+    assert torch.equal(torch.isnan(out), torch.isnan(want))
+    assert bool(torch.isnan(out[0]).all()) and not bool(torch.isnan(out[1:147]).any()) and bool(torch.isnan(out[147:]).all())
+    # without those keys the others' weights are the same
+    keep = [i for i in range(147) if i not in (0, 70, 100, 101)]
+    for i in (120, 146):
+        seen = [j for j in keep if j <= i]
+        o = ref.attend(q[i:i + 1], k[seen], v[seen], torch.tensor([len(seen) - 1]), d ** -0.5)
+        ref.check(out[i:i + 1].cuda(), *o, keys=len(seen), d=d, p_round=ref.ROUND[dtype],
+                  p_step=2.0 ** -25 if t == "f16" else 0.0)
