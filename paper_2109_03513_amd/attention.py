@@ -6,8 +6,8 @@
     q, k normed and rotated, k and v kept         esb_kv4_append
     o = softmax(q k^T / sqrt(d)) v                esb_kv4_attention, from the cache
   whole prompts (prompt):
-    q, k normed and rotated                       esb_rope
-    k and v kept                                  esb_kv4_append
+    q, k normed and rotated, k and v kept         esb_kv4_append
+    k normed and rotated                          esb_rope
     o from k and v themselves                     esb_attention
     y = o W_out^T                                 esb_w4_gemm
 
@@ -77,8 +77,9 @@ class CachedAttention:
     def prompt(self, x, residual, slots, positions, starts):
         """Whole prompts, packed; starts: sequences + 1 int32.  Returns (y, z)."""
         z, q, k, v = self._heads(x, residual)
-        q, k = esb.esb_rope(q, k, self.table, positions, **self.norms)
-        esb.esb_kv4_append(self.cache, self.page, k, v, slots)
+        # the cache takes k as it is, as in a step: rounded heads would get other codes
+        q = esb.esb_kv4_append(self.cache, self.page, k, v, slots, self.table, positions, q=q, **self.norms)
+        k = esb.esb_rope(None, k, self.table, positions, k_w=self.norms["k_w"], eps=self.norms["eps"])[1]
         o = esb.esb_attention(q, k, v, starts)
         return self._product(o), z
 

@@ -133,3 +133,13 @@ def test_refusals(at):
     for bad in (dict(w_qkv=w[0][:-1]), dict(w_out=w[1][:, 1:]), dict(q_norm=table[0]), dict(page=24)):
         with pytest.raises(ValueError):
             at.CachedAttention(**{**dict(w_qkv=w[0], w_out=w[1], heads=2, kv_heads=1, table=table, pages=2, page=16), **bad})
+
+
+@pytest.mark.parametrize("heads,kv,d,dtype,norms", [(4, 2, 64, torch.bfloat16, True), (6, 1, 32, torch.float16, False)])
+def test_prompts_and_steps_keep_the_same(at, heads, kv, d, dtype, norms):
+    """The same tokens leave the same codes in the cache, as a prompt or as steps of many tokens."""
+    a, b = (Model(at, heads, kv, d, dtype, norms) for _ in range(2))
+    x, r, slots, pos, starts, lengths = a.batch([40, 9, 25], 1)
+    a.b.prompt(x.cuda(), r.cuda(), slots, pos, starts)
+    b.b.step(x.cuda(), r.cuda(), slots, pos, b.pages, lengths, starts)
+    assert torch.equal(a.b.cache, b.b.cache)
