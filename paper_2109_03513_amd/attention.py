@@ -64,7 +64,7 @@ class CachedAttention:
         return z, y[:, :self.heads], y[:, self.heads:-self.kv_heads], y[:, -self.kv_heads:]
 
     def _product(self, o):
-        return esb.esb_w4_gemm(o.view(o.shape[0], -1), self.out, self.hidden, self.group)
+        return esb.esb_w4_gemm(o.flatten(1), self.out, self.hidden, self.group)
 
     def step(self, x, residual, slots, positions, pages, lengths, starts=None):
         """x, residual: tokens x hidden (bf16 or fp16); starts: sequences + 1 int32, or None for one token

@@ -143,3 +143,11 @@ def test_prompts_and_steps_keep_the_same(at, heads, kv, d, dtype, norms):
     a.b.prompt(x.cuda(), r.cuda(), slots, pos, starts)
     b.b.step(x.cuda(), r.cuda(), slots, pos, b.pages, lengths, starts)
     assert torch.equal(a.b.cache, b.b.cache)
+
+
+def test_no_tokens(at):
+    """A batch without tokens gives as many."""
+    m = Model(at, 4, 2, 64, torch.bfloat16, True)
+    x, r, slots, pos, starts, lengths = m.batch([0, 0, 0], 1)
+    for out in (m.b.prompt(x.cuda(), r.cuda(), slots, pos, starts), m.b.step(x.cuda(), r.cuda(), slots, pos, m.pages, lengths, starts)):
+        assert [tuple(t.shape) for t in out] == [tuple(x.shape)] * 2
