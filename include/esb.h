@@ -656,7 +656,8 @@ int esb_rope(const esb_heads* q, const esb_heads* k, int type, int64_t tokens, i
  *            stored.  A slot given twice holds parts of both tokens.
  *   type ESB_F32, ESB_BF16, ESB_F16.  tokens == 0 enqueues nothing.
  * esb_kv4_pack: given ESB(4,1) codes (one per byte, as esb_project writes them; device,
- *   contiguous tokens x heads x d) and scales (bf16, tokens x heads x d / 32) into the cache.
+ *   contiguous tokens x heads x d) and scales (bf16, tokens x heads x d / 32; infinities are kept
+ *   as NaN) into the cache.
  * esb_kv4_unpack: the unscaled values as E4M3 bytes (exact; tokens x heads x d) and / or the
  *   scales; any may be NULL, not all.  A slot that is not in the cache reads as zeros under NaN.
  */

@@ -290,8 +290,9 @@ __global__ __launch_bounds__(256) void k_pack(Kv4Layout L, int64_t items, const 
     store_codes<true>(L, b, at, e, word(k));
     store_codes<false>(L, b, at, e, word(v));
     if (e & 31) return;
-    *scale_at(L, b, L.key_scales_at(), at, e >> 5) = ka[s];
-    *scale_at(L, b, L.value_scales_at(), at, e >> 5) = va[s];
+    auto kept = [](uint16_t a) { return (a & 0x7f80) == 0x7f80 ? (uint16_t)0x7fc0 : a; };      // infinities as NaN
+    *scale_at(L, b, L.key_scales_at(), at, e >> 5) = kept(ka[s]);
+    *scale_at(L, b, L.value_scales_at(), at, e >> 5) = kept(va[s]);
 }
 
 __global__ __launch_bounds__(256) void k_unpack(Kv4Layout L, int64_t items, const int64_t* slots, uint8_t* k,

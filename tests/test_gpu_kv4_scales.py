@@ -225,3 +225,24 @@ def test_largest_values(esb, power, d, page, group, n, columns):  # noqa: F811
     q = torch.full((n or 1, group, d), 5.4 / d, dtype=BF16, device="cuda")
     out = esb.esb_kv4_attention(q, c.cache, page, 1, c.pages, c.lengths, starts=starts([n or 1]), scale=1.0)
     verify_rows(c, q, out, range(n or 1), scale=1.0)
+
+
+@pytest.mark.parametrize("group,n", [FEW, SOME, MANY])
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("d", [64, 96])
+def test_infinite_scales(esb, group, n, what, value, d):  # noqa: F811
+    """Packed infinities are kept as NaN: whoever sees one gets NaN, from every kernel alike."""
+    c = Cache(esb, 94, [100], 1, d, 16)
+    q = queries(95, n or 1, group, d, BF16)
+    clean = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([n or 1]))
+    codes = torch.randint(0, 16, (1, 1, d), device="cuda", dtype=torch.uint8)
+    a = torch.full((1, 1, d // 32), value, dtype=BF16, device="cuda")
+    at = 99 if n is None else 80            # seen by the only query, or by those from 20 on
+    esb.esb_kv4_pack(c.cache, 16, codes, a if what == "k" else torch.ones_like(a), codes, a if what == "v" else torch.ones_like(a),
+                     c.slots[0][at:at + 1])
+    _, ka, _, va = esb.esb_kv4_unpack(c.cache, 16, 1, d, c.slots[0][at:at + 1])
+    assert bool(torch.isnan(ka if what == "k" else va).all())
+    out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([n or 1]))
+    first = 0 if n is None else 20
+    assert torch.equal(out[:first], clean[:first]) and bool(torch.isnan(out[first:]).all())
