@@ -725,6 +725,8 @@ int esb_kv4_attention(const esb_heads* q, int type, int64_t tokens, const esb_kv
  *   q_starts, k_starts  device, seqs + 1 each, ascending; k_starts NULL: q_starts (then k_tokens
  *            == q_tokens).  Query rows past the last sequence are left as they were;
  *   d        a multiple of 8, at most 256 (else ESB_E_UNSUPPORTED); ESB_BF16 or ESB_F16.
+ * ESB_E_UNSUPPORTED: (q_tokens + seqs) * q->heads of 2^31 or more, more than 2^31 - 8193 keys or
+ * rows (q_tokens times the heads of a group).
  * out may not be the buffer of q, k or v.  A query that sees no key gets zeros; infinities and NaN
  * in keys and values reach only the queries that see them.  Probabilities enter the matrix cores in
  * `type`; the rest is fp32.

@@ -1009,7 +1009,8 @@ int esb_attention(const esb_heads* q, const esb_heads* k, const esb_heads* v, in
     int st = attention_check(type, q_tokens, q->heads, k->heads, seqs, scale);
     if (st) return st;
     if (d < 1 || k_tokens < 0) return ESB_E_INVALID;
-    if (d % 8 || d > 256 || k_tokens > INT32_MAX) return ESB_E_UNSUPPORTED;
+    if (d % 8 || d > 256 || k_tokens > kMostKeys) return ESB_E_UNSUPPORTED;
+    if (q_tokens * (q->heads / k->heads) > INT32_MAX - 8192) return ESB_E_UNSUPPORTED;      // rows: so do the tiles' last
     if ((st = heads_check(q, type, q_tokens, d, false)) || (st = heads_check(out, type, q_tokens, d, true)) ||
         (st = heads_check(k, type, k_tokens, d, false)) || (st = heads_check(v, type, k_tokens, d, false)))
         return st;

@@ -180,3 +180,22 @@ def test_host_tensors(esb):
         esb.esb_kv4_attention(x, torch.zeros(2, 4608, dtype=torch.uint8), 16, 4, n[:, None], n)
     with pytest.raises(TypeError):
         esb.esb_attention(x, x, x, n)
+
+
+def test_attention_of_most_rows_and_keys(esb):
+    """Rows and keys whose tiles would end past 32 bits: their indexes, and the loop over the keys, would wrap."""
+    L = esb.lib()
+    one = heads(esb, n=1, d=8)
+    out = heads(esb, n=1, d=8, data=OTHER)
+    most = (1 << 31) - 1
+
+    def attend(nq, nk, seqs=1):
+        return L.esb_attention(ref(one), ref(one), ref(one), BF16, nq, nk, 8, seqs, FAKE, FAKE, 1, 0.1, ref(out), None)
+
+    for nk in (most, most - 64, most - 8191):
+        assert attend(3, nk) == UNSUPPORTED, nk
+    for nq in (most - 1, most - 100, most - 8191):
+        assert attend(nq, 3) == UNSUPPORTED, nq
+    # a group of heads counts each of them
+    q, o = (heads(esb, n=64, d=8, data=x) for x in (FAKE, OTHER))
+    assert L.esb_attention(ref(q), ref(one), ref(one), BF16, (1 << 25) - 2, 3, 8, 1, FAKE, FAKE, 1, 0.1, ref(o), None) == UNSUPPORTED
