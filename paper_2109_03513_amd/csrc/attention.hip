@@ -39,7 +39,7 @@ template <typename T> __device__ __forceinline__ bool finite(T v) {
     return (__builtin_bit_cast(uint16_t, v) & e) != e;
 }
 
-// Bound by MFMA and VALU issue (49 and 46 % of all SIMD cycles; they add up) at a power-limited clock: causal prompts,
+// Bound by MFMA and VALU issue (50 and 47 % of all SIMD cycles; they add up) at a power-limited clock: causal prompts,
 // heads of 128, 527 to 559 us by card for 550 GFLOP, 1.0 PFLOP/s, where a library product reaches 1.22.  Tiles by loads to
 // registers 1110 us, by DMA in two stages 582, that written out 529.  32 rows to a wave and 64 keys to a tile: what
 // the registers of two workgroups a CU hold.

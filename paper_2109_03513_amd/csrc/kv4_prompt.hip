@@ -13,7 +13,7 @@
 // kv4_attention.hip (wide_pass), whose scales stay fp32: codes and queries as they are into the MFMAs, a key's scale on
 // the sum of its group, a value's on the probability, which enters as two bf16.  Looking for that costs -3 to 3 % (heads of
 // 64 to 128, us, without and with: the two ragged sequences below 141 and 141, 2048 queries over 8192 keys 300 and 305, 64
-// over 2048 33.9 and 34.8), 4 % for heads of 256 (269 and 279).  Scales below 2^-125 are those of zeros: they are not
+// over 2048 33.9 and 34.6), and heads of 256 nothing (268).  Scales below 2^-125 are those of zeros: they are not
 // looked for, so that zeros among other tokens stay as fast.
 //
 // Values whose scale is not finite count as zero in the products, and their elements become NaN at the end for
@@ -69,7 +69,7 @@ __device__ __forceinline__ int wave_max(int v) {
 }
 
 // Bound by the matrix cores and VALU in turn, and by what the fewest tiles leave idle: 2048 queries of 32 heads of 128
-// over 16384 keys 583 to 635 us by card, 870 to 940 TFLOP/s; two ragged sequences of up to 512 over 8192 keys 146, 575.
+// over 16384 keys 583 to 635 us by card, 870 to 940 TFLOP/s; two ragged sequences of up to 512 over 8192 keys 141, 596.
 // Decoded in registers by each wave it was 378, into LDS by four waves 236, scales shared by the
 // lanes of a group 191, by eight waves for twice the rows 172, in even shares 146, each with the join.
 template <typename T, int DP, int WAVES, bool EVEN>

@@ -8,7 +8,7 @@ import torch
 
 import attention_ref as ref
 from gpuutil import log
-from test_gpu_kv4_attention import Cache, esb, queries, verify  # noqa: F401
+from test_gpu_kv4_attention import Cache, esb, queries, verify, wide  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 BF16, F16 = torch.bfloat16, torch.float16
@@ -61,7 +61,7 @@ def test_tiny_products(esb):  # noqa: F811
 LEAST = 2.0 ** -126
 
 
-def verify_rows(c, q, out, rows, scale=None, at=0):
+def verify_rows(c, q, out, rows, scale=None, at=0, many=None):
     """Those rows of sequence `at`, whose queries q are, by what they see.  A weight below fp32's smallest normal
     number, beside a largest one of at least 1, may count as zero: that is LEAST of the sum of |v|."""
     k, v = c.read(at)
@@ -69,7 +69,7 @@ def verify_rows(c, q, out, rows, scale=None, at=0):
     last = torch.arange(n) + k.shape[0] - n
     rows = torch.as_tensor(rows)
     m = int(last[rows].max()) + 1
-    many = n * (q.shape[1] // c.heads) > 64
+    many = n * (q.shape[1] // c.heads) > 64 if many is None else many
     want = ref.attend(q[rows], k[:m], v[:m], last[rows], c.d ** -0.5 if scale is None else scale)
     p_round = 2.0 ** -11 if many else 2.0 ** -8 if q.dtype == BF16 else 2.0 ** -16
     ref.check(out[rows], *want, keys=m, d=c.d, p_round=p_round, p_step=2.0 ** -25 if many else LEAST)
@@ -246,3 +246,54 @@ def test_infinite_scales(esb, group, n, what, value, d):  # noqa: F811
     out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([n or 1]))
     first = 0 if n is None else 20
     assert torch.equal(out[:first], clean[:first]) and bool(torch.isnan(out[first:]).all())
+
+
+@pytest.mark.parametrize("kv,group,d,page", [(1, 1, 32, 16), (2, 4, 128, 64), (1, 7, 64, 16), (3, 12, 64, 32), (1, 40, 128, 64),
+                                             (2, 2, 256, 16), (1, 30, 96, 64), (1, 90, 128, 64), (1, 70, 64, 16)])
+@pytest.mark.parametrize("several", [False, True])
+def test_far_apart_in_even_shares(esb, kv, group, d, page, several):  # noqa: F811
+    """The same in work that workgroups share evenly: beside ordinary sequences some whose values are near the end
+    of bf16, some whose scales are far apart, some of zeros; items that begin and end in any share."""
+    seqs = 13
+    lengths = [(53 * i) % 400 + 5 for i in range(seqs)]
+    lengths[6] = 2600
+    counts = [1 + (7 * i) % 4 if several else 1 for i in range(seqs)]
+    c = Cache(esb, 96, lengths, kv, d, page, columns=wide(seqs, kv, 1, group, d, page))
+    g = torch.Generator(device="cuda").manual_seed(97)
+    for i in range(seqs):
+        if i % 4 == 3:
+            continue
+        n, ones = lengths[i], torch.ones(lengths[i], kv, d // 32, device="cuda")
+        codes = [torch.randint(0, 16, (n, kv, d), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+        a, va = 0.3 * ones, 0.4 * ones
+        if i % 4 == 0:          # weights that grow by less than 2^8
+            codes = [torch.zeros_like(x) for x in codes]
+            a = ones * (torch.arange(n, device="cuda") / n)[:, None, None]
+            va = ones * torch.where(torch.arange(n, device="cuda") % 90 == 7, 2.0 ** 122, 2.0 ** 110)[:, None, None]
+        elif i % 4 == 1:
+            a, va = (x * 2.0 ** torch.randint(-40, 1, x.shape, generator=g, device="cuda") for x in (a, va))
+        else:
+            codes, a, va = [torch.full_like(x, 6) for x in codes], 2.0 ** -126 * ones, 2.0 ** -126 * ones
+        esb.esb_kv4_pack(c.cache, page, codes[0], a.to(BF16), codes[1], va.to(BF16), c.slots[i])
+    q = queries(98, sum(counts), kv * group, d, BF16)
+    at = [sum(counts[:i]) for i in range(seqs)]
+    for i in range(0, seqs, 4):
+        q[at[i]:at[i] + counts[i]] = 5.4 / d
+    st = starts(counts) if several else None
+    out = esb.esb_kv4_attention(q, c.cache, page, kv, c.pages, c.lengths, starts=st, scale=1.0)
+    many = -(-sum(counts) // seqs) * group > 64
+    for i in range(seqs):
+        verify_rows(c, q[at[i]:at[i] + counts[i]], out[at[i]:at[i] + counts[i]], range(counts[i]), scale=1.0, at=i, many=many)
+    assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("group,n", [FEW, SOME, MANY])
+@pytest.mark.parametrize("power", [10, 40])
+def test_large_negative_scores(esb, group, n, power):  # noqa: F811
+    c = Cache(esb, 99, [200], 1, 64, 16)
+    codes = torch.randint(0, 6, (200, 1, 64), device="cuda", dtype=torch.uint8, generator=torch.Generator(device="cuda").manual_seed(1))
+    a = torch.full((200, 1, 2), 2.0 ** power, device="cuda").to(BF16)
+    esb.esb_kv4_pack(c.cache, 16, codes, a, codes, torch.ones_like(a), c.slots[0])
+    q = -queries(100, n or 1, group, 64, BF16).abs()
+    out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([n or 1]))
+    verify_rows(c, q, out, range(n or 1))
