@@ -148,6 +148,26 @@ template <typename T, int DP, int KT> struct Attend {
     }
 };
 
+// Whether some value's scale among keys k0 .. k1 - 1 is finite and so large (from 2^56 on) that sums of values under weights
+// of up to 2^kLazy can near the end of fp32: what is not finite for another reason stays so.
+__device__ __forceinline__ bool large_values(const Kv4AttentionParams& p, const Rows& rw, int h, int k0, int k1) {
+    const int32_t* table = p.table + rw.seq * p.table_pitch;
+    bool found = false;
+    k1 = min(k1, rw.len);
+#pragma unroll 1
+    for (int j = k0 + 4 * (threadIdx.x & 63); j < k1; j += 256) {
+        const int pid = table[j >> p.cache.shift], t = j & (p.cache.page - 1);
+        if (pid < 0 || pid >= p.cache.pages) continue;
+        const uint8_t* run = p.cache.block(pid, h) + p.cache.value_scales_at() + p.cache.scale_run(t);
+#pragma unroll 1
+        for (int k = 0; k < 4 * p.cache.groups; k++) {
+            const uint32_t e = ((const uint16_t*)run)[k] >> 7 & 0xff;
+            found |= e >= 127 + 56 && e < 255;
+        }
+    }
+    return __any(found);
+}
+
 // The fallback for an item over the 4-bit cache, which usual data never takes: keys k0 .. k1 - 1 for the rows from `row0` on
 // that `mask` has, by one wave, in fp32 but for codes and queries: a key's scale is on the sum of its group, a value's on the
 // probability, which enters as two bf16.  Maxima move at once, so that no weight is above 1.  It leaves the outputs

@@ -68,7 +68,7 @@ __device__ __forceinline__ float column_sum(float v) {
 }
 
 // Whether sums of weights of up to 2^kLazy times values are not finite, or so large that those of further parts might leave
-// fp32.  Such rows take wide_pass.
+// fp32.  Such rows take wide_pass, if it is for their values.
 __device__ __forceinline__ bool is_large(f32x8 o) {
     int above = 0;
     uint32_t below = 0;      // by sign
@@ -347,7 +347,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 }
             }
         }
-        if (__builtin_expect(__any(large), 0)) {
+        if (__builtin_expect(__any(large), 0) && large_values(p, rw, h, work.from, work.to)) {
             __threadfence();      // its stores come after those above
             uint32_t mask = 0;
 #pragma unroll
@@ -622,7 +622,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e, __builtin_convertvector(o, V), 8);
             }
         }
-        if (__builtin_expect(__any(large), 0)) {
+        if (__builtin_expect(__any(large), 0) && large_values(p, rw, h, work.from, work.to)) {
             __threadfence();      // its stores come after those above
             wide_pass<T, EVEN>(p, rw, h, work.from, work.to, rw.row0, rows_of<4 * CP>(__ballot(large)) << (16 / CP * wave),
                                whole ? -1 : EVEN ? (int64_t)work.place * R : work.place, sp.chunks, part, stats);
