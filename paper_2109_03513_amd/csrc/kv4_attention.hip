@@ -14,8 +14,9 @@
 // waves take every fourth step of 32 keys, each with its own running maximum and sum, and join them in
 // LDS.  The keys are split over workgroups too, in runs or in even shares of all work (split() below),
 // and a k_join_... adds the parts.  The running maximum moves only when a score passes it by 2^8, so
-// most steps cross no lanes; where sums of values near the end of fp32 leave it for that, their rows are gone over once
-// more (wide_pass).
+// most steps cross no lanes.  Rows whose sums near the end of fp32 for that, or whose maximum is beyond 2^20, so that x
+// scale - m in one rounding is off by too much, are gone over once more (wide_pass): looking for them costs 1 %, checks
+// within the loop cost up to 5.
 #include <algorithm>
 #include <type_traits>
 
@@ -76,6 +77,11 @@ __device__ __forceinline__ bool is_large(f32x8 o) {
     for (int e = 0; e < 8; e++) above = max(above, __float_as_int(o[e])), below = max(below, __float_as_uint(o[e]));
     return above >= (int)kLarge || below >= (kLarge | 0x80000000u);
 }
+// Whether weights under this maximum may be off by more than exp2 may be given (kFar), even infinite: rows whose maximum was
+// far in some wave, at some time, take it too.  A wave tells by the sign of its sum.
+__device__ __forceinline__ bool is_far(float m) { return fabsf(m) > kFar && fabsf(m) < __builtin_inff(); }
+__device__ __forceinline__ float marked(float sum, int mark) { return __builtin_copysignf(sum, mark ? -1.0f : 1.0f); }
+__device__ __forceinline__ bool is_marked(float sum) { return __float_as_int(sum) < 0; }
 // The rows of which some of a wave's lanes, N to a row, say so.
 template <int N> __device__ __forceinline__ uint32_t rows_of(uint64_t lanes) {
     uint32_t rows = 0;
@@ -171,6 +177,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 
         f32x4 acc[NT][CP][2] = {};
         float top[NT], sum[NT];      // the running maximum (times scale) and the lane's part of the sum
+        int distant = 0;             // bit u: the maximum was far (is_far) at some time
 #pragma unroll
         for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
 
@@ -215,18 +222,11 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                     const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
                     const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
                     top[u] = now;
+                    if (is_far(now)) distant |= 1 << u;
                     sum[u] *= f;
 #pragma unroll
                     for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
                 }
-            }
-            float scale[NT];
-#pragma unroll
-            for (int u = 0; u < NT; u++) {
-                scale[u] = p.scale;
-                const bool far = fabsf(top[u]) > kFar && top[u] > kNegInf;
-                if (__builtin_expect(__ballot(far) != 0, 0) && far)
-                    x[u][0] *= p.scale, x[u][1] *= p.scale, scale[u] = 1.0f;
             }
 #pragma unroll
             for (int u = 0; u < NT; u++) {
@@ -235,7 +235,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 for (int hh = 0; hh < 2; hh++)
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        x[u][hh][r] = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], scale[u], -m));
+                        x[u][hh][r] = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
                         sum[u] += x[u][hh][r];
                     }
             }
@@ -286,10 +286,11 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
         __shared__ float2 waves[4][NT][16];
         __shared__ float sums[4][16][132];
         float factor[NT], total[NT];
+        int apart = 0;      // bit u: the column's row of tile u had a far maximum
 #pragma unroll
         for (int u = 0; u < NT; u++) {
             sum[u] = column_sum(sum[u]);
-            if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
+            if (g == 0) waves[wave][u][i] = make_float2(top[u], marked(sum[u], distant >> u & 1));
         }
         __syncthreads();
 #pragma unroll
@@ -301,14 +302,15 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 #pragma unroll
             for (int w = 0; w < 4; w++) {
                 const float2 o = waves[w][u][i];
-                l += o.x == kNegInf ? o.y : o.y * __builtin_amdgcn_exp2f(o.x - m);
+                if (is_marked(o.y)) apart |= 1 << u;
+                l += o.x == kNegInf ? fabsf(o.y) : fabsf(o.y) * __builtin_amdgcn_exp2f(o.x - m);
             }
             factor[u] = top[u] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - m);
             total[u] = l;
             top[u] = m;
         }
         const int col = threadIdx.x >> 4, dd = 8 * (threadIdx.x & 15);
-        uint32_t large = 0;      // rows of this wave's
+        uint32_t large = 0, far = 0;      // bit 16 u: of tile u
 #pragma unroll
         for (int u = 0; u < NT; u++) {
 #pragma unroll
@@ -324,6 +326,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                             sums[wave][i][32 * (c - c0) + 8 * g + 2 * r + e] = acc[u][c][e][r] * factor[u];
                 __syncthreads();
                 const float m = __shfl(top[u], col), l = __shfl(total[u], col);
+                const bool distant = __shfl(apart, col) >> u & 1;
                 const int r = rw.row0 + 16 * u + col, e0 = 32 * c0 + dd;
                 f32x8 o = {};
                 if (r < rw.rows && e0 < 32 * C) {
@@ -332,6 +335,7 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 #pragma unroll
                         for (int e = 0; e < 8; e++) o[e] += sums[w][col][dd + e];
                     large |= is_large(o) ? 1u << (16 * u) : 0;
+                    far |= distant ? 1u << (16 * u) : 0;
                     const int t = r / p.group, head = h * p.group + r % p.group;
                     if (!whole) {
                         const int64_t at = EVEN ? (int64_t)work.place * R + 16 * u + col
@@ -347,13 +351,15 @@ void k_kv4(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 }
             }
         }
-        if (__builtin_expect(__any(large), 0) && large_values(p, rw, h, work.from, work.to)) {
-            __threadfence();      // its stores come after those above
+        if (__builtin_expect(__any(large | far), 0)) {
+            if (!large_values(p, rw, h, work.from, work.to)) large = 0;
+            __threadfence();      // what follows comes after the stores above
             uint32_t mask = 0;
 #pragma unroll
-            for (int u = 0; u < NT; u++) mask |= rows_of<16>(__ballot(large >> (16 * u) & 1)) << (16 * u + 4 * wave);
-            wide_pass<T, EVEN>(p, rw, h, work.from, work.to, rw.row0, mask, whole ? -1 : EVEN ? (int64_t)work.place * R : work.place,
-                               sp.chunks, part, stats);
+            for (int u = 0; u < NT; u++) mask |= rows_of<16>(__ballot((large | far) >> (16 * u) & 1)) << (16 * u + 4 * wave);
+            if (mask)
+                wide_pass<T, EVEN>(p, rw, h, work.from, work.to, rw.row0, mask, whole ? -1 : EVEN ? (int64_t)work.place * R : work.place,
+                                   sp.chunks, part, stats);
         }
         if (EVEN) __syncthreads();      // the next item uses the same LDS
     }
@@ -456,6 +462,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 
         f32x4 acc[NT][CP][2] = {};
         float top[NT], sum[NT];
+        int distant = 0;
 #pragma unroll
         for (int u = 0; u < NT; u++) top[u] = kNegInf, sum[u] = 0.0f;
 
@@ -507,18 +514,11 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                     const float all = column_max(most[u]), now = passes(all, top[u]) ? all : top[u];
                     const float f = now == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top[u] - now);
                     top[u] = now;
+                    if (is_far(now)) distant |= 1 << u;
                     sum[u] *= f;
 #pragma unroll
                     for (int c = 0; c < CP; c++) acc[u][c][0] *= f, acc[u][c][1] *= f;
                 }
-            }
-            float scale[NT];
-#pragma unroll
-            for (int u = 0; u < NT; u++) {
-                scale[u] = p.scale;
-                const bool far = fabsf(top[u]) > kFar && top[u] > kNegInf;
-                if (__builtin_expect(__ballot(far) != 0, 0) && far)
-                    x[u][0] *= p.scale, x[u][1] *= p.scale, scale[u] = 1.0f;
             }
             const f32x4 b[2] = {four(st.va[0]), four(st.va[1])};
             bf16x8 hi[NT], lo[NT];
@@ -530,7 +530,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 for (int hh = 0; hh < 2; hh++)
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], scale[u], -m));
+                        const float e = __builtin_amdgcn_exp2f(fmaf(x[u][hh][r], p.scale, -m));
                         sum[u] += e;
                         w[4 * hh + r] = e * b[hh][r];
                     }
@@ -577,7 +577,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 #pragma unroll
         for (int u = 0; u < NT; u++) {
             sum[u] = column_sum(sum[u]);
-            if (g == 0) waves[wave][u][i] = make_float2(top[u], sum[u]);
+            if (g == 0) waves[wave][u][i] = make_float2(top[u], marked(sum[u], distant >> u & 1));
         }
         __syncthreads();
 #pragma unroll
@@ -596,7 +596,7 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
         }
         __syncthreads();
         const int row = thread / (4 * CP), e = 8 * (thread % (4 * CP)), r = rw.row0 + row;
-        bool large = false;
+        bool large = false, far = false;
         if (row < R && r < rw.rows && e < 32 * C) {
             float m = kNegInf, l = 0.0f;
             const int u = row / HR, column = row % HR * CP;
@@ -606,7 +606,8 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
 #pragma unroll
             for (int w = 0; w < 4; w++) {
                 const float2 x = waves[w][u][column];
-                l += x.x == kNegInf ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - m);
+                far |= is_marked(x.y);
+                l += x.x == kNegInf ? fabsf(x.y) : fabsf(x.y) * __builtin_amdgcn_exp2f(x.x - m);
                 o += *(const f32x8*)&sums[w][row][e];
             }
             large = is_large(o);
@@ -622,10 +623,13 @@ void k_kv4_few(Kv4AttentionParams p, Kv4Split sp, float* part, float2* stats) {
                 store8((T*)p.o.p + (rw.begin + t) * p.o.token + head * p.o.head + e, __builtin_convertvector(o, V), 8);
             }
         }
-        if (__builtin_expect(__any(large), 0) && large_values(p, rw, h, work.from, work.to)) {
-            __threadfence();      // its stores come after those above
-            wide_pass<T, EVEN>(p, rw, h, work.from, work.to, rw.row0, rows_of<4 * CP>(__ballot(large)) << (16 / CP * wave),
-                               whole ? -1 : EVEN ? (int64_t)work.place * R : work.place, sp.chunks, part, stats);
+        if (__builtin_expect(__any(large || far), 0)) {
+            if (!large_values(p, rw, h, work.from, work.to)) large = false;
+            __threadfence();      // what follows comes after the stores above
+            const uint32_t mask = rows_of<4 * CP>(__ballot(large || far)) << (16 / CP * wave);
+            if (mask)
+                wide_pass<T, EVEN>(p, rw, h, work.from, work.to, rw.row0, mask, whole ? -1 : EVEN ? (int64_t)work.place * R : work.place,
+                                   sp.chunks, part, stats);
         }
         if (EVEN) __syncthreads();      // the next item uses the same LDS
     }

@@ -297,3 +297,21 @@ def test_large_negative_scores(esb, group, n, power):  # noqa: F811
     q = -queries(100, n or 1, group, 64, BF16).abs()
     out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([n or 1]))
     verify_rows(c, q, out, range(n or 1))
+
+
+@pytest.mark.parametrize("group,n", [FEW, SOME, MANY, (16, None)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("columns", [None, 8192])
+@pytest.mark.parametrize("at", [0, 96, 200, 640])
+def test_large_negative_scores_beside_others(esb, group, n, d, columns, at):  # noqa: F811
+    """Runs of keys whose scores are about -2^40 have no weight beside ordinary ones."""
+    c = Cache(esb, 101, [700], 1, d, 16, columns=columns)
+    g = torch.Generator(device="cuda").manual_seed(102)
+    codes = torch.randint(0, 6, (700, 1, d), device="cuda", dtype=torch.uint8, generator=g)
+    v = torch.randint(0, 16, (700, 1, d), device="cuda", dtype=torch.uint8, generator=g)
+    a = 0.1 * torch.exp(0.3 * torch.randn(700, 1, d // 32, device="cuda", generator=g))
+    a[at:at + 150] *= 2.0 ** 40
+    esb.esb_kv4_pack(c.cache, 16, codes, a.to(BF16), v, torch.ones_like(a).to(BF16), c.slots[0])
+    q = -queries(103, n or 1, group, d, BF16).abs()
+    out = esb.esb_kv4_attention(q, c.cache, 16, 1, c.pages, c.lengths, starts=starts([n or 1]))
+    verify_rows(c, q, out, range(n or 1))
